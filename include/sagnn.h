@@ -60,6 +60,10 @@ enum {
 
 #define SAGNN_ACT_IDENTITY 0
 #define SAGNN_ACT_RELU 1
+#define SAGNN_ACT_SILU 2 /* z / (1 + exp(-z)); group_norm_act_fwd / _bwd only */
+
+#define SAGNN_F32 0  /* storage types of the calls that take one */
+#define SAGNN_BF16 1
 
 #define SAGNN_GEMM_FP32 0 /* fp32 operands, fp32 MFMA                          */
 #define SAGNN_GEMM_BF16 1 /* operands rounded to bfloat16 (RNE), fp32 accumulate */
@@ -147,7 +151,8 @@ int spmm_plan_needed_rows_noalloc(const int32_t* d_rowptr, const int32_t* d_coli
  * set-up calls (spmm_plan_needed_rows, spmm_csr_prepare, spmm_csr_prepare_tuned, spmm_split_colblocks,
  * spmm_csr_transpose) copy small results back and synchronise that stream, so they cannot be
  * recorded into a graph.  The per-step calls (spmm_pack_rows, spmm_csr_tallskinny,
- * dense_gemm_act, gcn_layer_fwd, gcn_layer_bwd, spmm_stage_loop) only launch kernels and, in the
+ * dense_gemm_act, gcn_layer_fwd, gcn_layer_bwd, spmm_stage_loop, grouped_gemm_act, grouped_gemm_bwd,
+ * group_norm_act_fwd, group_norm_act_bwd, grad_global_norm, grad_clip_norm, grad_scale_to_norm) only launch kernels and, in the
  * stage loop, record and wait for events between its two streams (forked from and joined back
  * into the product stream): no host synchronisation, no memset, no allocation.  They may be
  * captured into a HIP graph and replayed; a replay gives the same bits as the eager calls.
@@ -579,6 +584,103 @@ int spmm_stage_loop(const sagnn_stage* h_stages, int32_t n_stages, int64_t m, co
  */
 int spmm_volume_stats(const int64_t* h_counts, int32_t P, int32_t f, int32_t elem_bytes,
                       double* h_out);
+
+/* ---------------------------------------------------------------------------------------
+ * Rows ordered by type, a weight matrix for each type (vertices of several types, edges of several relations).
+ *
+ * d_off (device, n_groups+1 int32, ascending, d_off[0] = 0, d_off[n_groups] <= m): row r belongs to group g where
+ * d_off[g] <= r < d_off[g+1].  Groups may be empty.  spmm_perm_from_labels gives such an order and its offsets.
+ * The calls read d_off on the device and wait for nothing.
+ *
+ *   grouped_gemm_act:  Y[r, :] = act(X[r, :] op(W[g])) .* [mask[r, :] > 0]
+ *       transW = 0: W[g] is kdim x nout (ldw) at d_W + g * stride_w;  transW = 1: nout x kdim, used as W[g]^T
+ *       act: SAGNN_ACT_IDENTITY or SAGNN_ACT_RELU (a NaN stays one);  d_mask (m x nout, ldmask) may be NULL
+ *   grouped_gemm_bwd, G = dLoss/d(X W) (m x nout, ldg), W[g] kdim x nout:
+ *       dX[r, :] = (G[r, :] W[g]^T) .* [mask[r, :] > 0]     skipped if d_dX == NULL; d_mask (m x kdim) may be NULL
+ *       dW[g]    = sum over the rows of g of X[r, :]^T G[r, :]   fp32, n_groups x kdim x nout, dense; zeros for an
+ *                                                           empty group; skipped if d_dW == NULL
+ *   Rows behind d_off[n_groups]: zeros in Y and dX, not part of dW (their X and G are not used).
+ *
+ * dtype: SAGNN_F32 or SAGNN_BF16, the type of X, W, G, mask, Y and dX; dW is fp32.  prec: as in dense_gemm_act for
+ * fp32 tensors, SAGNN_GEMM_FP32 for bfloat16 ones (whose products are exact).  All sums are fp32, their order is a
+ * fixed function of the arguments and d_off: the same bits every time.  Results are rounded once.
+ * Any widths up to SAGNN_GROUPED_MAX_WIDTH, any leading dimensions not below the width, pointers aligned to their
+ * element; tensors with 16-byte aligned rows are read faster.  n_groups <= SAGNN_GROUPED_MAX.  Outputs must not overlap
+ * inputs.  d_ws of grouped_gemm_bwd: grouped_gemm_bwd_workspace_bytes() bytes, 4-byte aligned, needed for dW only.
+ * Offsets that do not ascend give unspecified results (nothing is read or written outside the tensors).
+ */
+#define SAGNN_GROUPED_MAX 65536
+#define SAGNN_GROUPED_MAX_WIDTH 65536
+int grouped_gemm_act(int32_t dtype, const void* d_X, int64_t ldx, const void* d_W, int64_t ldw, int64_t stride_w,
+                     int32_t transW, const int32_t* d_off, int32_t n_groups, int64_t m, int32_t kdim, int32_t nout,
+                     int32_t prec, int32_t act, const void* d_mask, int64_t ldmask, void* d_Y, int64_t ldy,
+                     void* stream);
+int grouped_gemm_bwd_workspace_bytes(int64_t m, int32_t n_groups, int32_t kdim, int32_t nout, size_t* bytes);
+int grouped_gemm_bwd(int32_t dtype, const void* d_X, int64_t ldx, const void* d_W, int64_t ldw, int64_t stride_w,
+                     const int32_t* d_off, int32_t n_groups, int64_t m, int32_t kdim, int32_t nout, int32_t prec,
+                     const void* d_G, int64_t ldg, const void* d_mask, int64_t ldmask, void* d_dX, int64_t lddx,
+                     float* d_dW, void* d_ws, size_t ws_bytes, void* stream);
+
+/* ---------------------------------------------------------------------------------------
+ * Group norm with an activation, channels last: X is m x C, its rows lie in n_seg segments (the graphs of a batch), its
+ * C channels in n_groups groups of D = C / n_groups.  Over the rows of segment b and the channels of group q
+ * (n = rows * D values):
+ *
+ *   mean = sum x / n,  var = sum (x - mean)^2 / n,  rstd = 1 / sqrt(var + eps)
+ *   z = (x - mean) rstd gamma[c] + beta[c],  Y = act(z)      act: SAGNN_ACT_IDENTITY, _RELU or _SILU
+ *
+ * and backward, with G = dLoss/dY, xh = (x - mean) rstd, h = G act'(z):
+ *   dgamma[c] = sum over all rows of h xh,  dbeta[c] = sum of h
+ *   dX = rstd (h gamma[c] - sum(h gamma) / n - xh sum(h gamma xh) / n)     sums over segment and group
+ *
+ * d_seg (device, n_seg+1 int32, ascending, d_seg[0] = 0, d_seg[n_seg] <= m) or NULL for n_seg segments of m / n_seg rows
+ * each.  Segments may be empty (mean 0, rstd 1 / sqrt(eps)).  Rows behind the last segment: zeros in Y and dX, no part
+ * of any sum.  max_rows: rows of the longest segment if the caller knows it, 0 if not; it only chooses between forms.
+ * dtype: type of X, Y, G, dX; gamma, beta (each may be NULL: 1, 0), mean, rstd (n_seg x n_groups), dgamma, dbeta (each
+ * may be NULL) are fp32.  mean and rstd are outputs forward and inputs backward.  Mean and variance are summed in 64 bits.
+ * Orders of sums are fixed: the same bits every time.  Any C up to SAGNN_NORM_MAX_WIDTH, n_groups <= SAGNN_NORM_MAX_GROUPS,
+ * any leading dimensions not below C, tensors aligned to their element.  Y may be X, dX may be G or X.
+ * d_ws: group_norm_workspace_bytes() bytes (serves both directions), 16-byte aligned.
+ */
+#define SAGNN_NORM_MAX_WIDTH 16384
+#define SAGNN_NORM_MAX_GROUPS 1024
+int group_norm_workspace_bytes(int64_t m, int32_t n_seg, int32_t C, int32_t n_groups, size_t* bytes);
+int group_norm_act_fwd(int32_t dtype, const void* d_X, int64_t ldx, const int32_t* d_seg, int32_t n_seg,
+                       int64_t max_rows, int64_t m, int32_t C, int32_t n_groups, const float* d_gamma,
+                       const float* d_beta, double eps, int32_t act, void* d_Y, int64_t ldy, float* d_mean,
+                       float* d_rstd, void* d_ws, size_t ws_bytes, void* stream);
+int group_norm_act_bwd(int32_t dtype, const void* d_X, int64_t ldx, const void* d_G, int64_t ldg,
+                       const int32_t* d_seg, int32_t n_seg, int64_t max_rows, int64_t m, int32_t C, int32_t n_groups,
+                       const float* d_gamma, const float* d_beta, int32_t act, const float* d_mean,
+                       const float* d_rstd, void* d_dX, int64_t lddx, float* d_dgamma, float* d_dbeta, void* d_ws,
+                       size_t ws_bytes, void* stream);
+
+/* ---------------------------------------------------------------------------------------
+ * Global 2-norm of a model's gradients, and clipping.
+ *
+ *   norm = sqrt(sum over all tensors and values of g^2)          (squares and sums in 64 bits, d_norm in fp32)
+ *   d_out = d_in * min(1, max_norm / norm)                       (the factor in fp32, one rounding to the type)
+ *
+ * grad_global_norm writes the norm, grad_clip_norm the norm and the scaled tensors, grad_scale_to_norm scales by a norm that is
+ * already there (joined across processes, say).  A norm of 0 scales by 1.  An infinite norm scales by 0 and a NaN makes
+ * every value NaN, as the formula has it; d_norm tells.  max_norm: positive, finite.
+ * h_grads: n tensors of contiguous values, of either type, any size (0 too), aligned to their element.  d_out may be d_in;
+ * apart from that nothing that is written may overlap another tensor of the list (SAGNN_EINVAL; grad_global_norm ignores
+ * d_out).  n <= SAGNN_GRAD_MAX.  The list is read before the call returns.  Orders of sums are fixed.
+ * d_ws: grad_norm_workspace_bytes() bytes, 8-byte aligned.
+ */
+#define SAGNN_GRAD_MAX 65536
+typedef struct sagnn_grad {
+  const void* d_in;
+  void* d_out;
+  int64_t n;
+  int64_t dtype; /* SAGNN_F32 or SAGNN_BF16 */
+} sagnn_grad;
+int grad_norm_workspace_bytes(int32_t n, size_t* bytes);
+int grad_global_norm(const sagnn_grad* h_grads, int32_t n, float* d_norm, void* d_ws, size_t ws_bytes, void* stream);
+int grad_clip_norm(const sagnn_grad* h_grads, int32_t n, double max_norm, float* d_norm, void* d_ws, size_t ws_bytes,
+                   void* stream);
+int grad_scale_to_norm(const sagnn_grad* h_grads, int32_t n, double max_norm, const float* d_norm, void* stream);
 
 #ifdef __cplusplus
 }

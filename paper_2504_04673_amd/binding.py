@@ -12,7 +12,8 @@ import torch
 
 from . import build as _build
 
-ACT_IDENTITY, ACT_RELU = 0, 1
+ACT_IDENTITY, ACT_RELU, ACT_SILU = 0, 1, 2
+F32, BF16 = 0, 1
 GEMM_FP32, GEMM_BF16, GEMM_FP32_BF16X3 = 0, 1, 2
 PLAN_VALIDATE, PLAN_OBLIVIOUS, PLAN_MULTIPASS = 1, 2, 4
 
@@ -25,6 +26,9 @@ EXPORTS = [
     "spmm_split_workspace_bytes", "spmm_split_colblocks", "spmm_stage_loop", "spmm_volume_stats",
     "spmm_transpose_workspace_bytes", "spmm_csr_transpose",
     "spmm_permute_workspace_bytes", "spmm_perm_from_labels", "spmm_csr_permute_symmetric",
+    "grouped_gemm_act", "grouped_gemm_bwd_workspace_bytes", "grouped_gemm_bwd",
+    "group_norm_workspace_bytes", "group_norm_act_fwd", "group_norm_act_bwd",
+    "grad_norm_workspace_bytes", "grad_global_norm", "grad_clip_norm", "grad_scale_to_norm",
 ]
 
 
@@ -154,6 +158,18 @@ def lib():
         L.spmm_permute_workspace_bytes.argtypes = [i64, i64, psz]
         L.spmm_perm_from_labels.argtypes = [vp, i64, i32, vp, vp, vp, vp, sz, vp]
         L.spmm_csr_permute_symmetric.argtypes = [vp, vp, vp, i64, i64, vp, vp, vp, vp, vp, sz, vp]
+        f64 = ctypes.c_double
+        L.grouped_gemm_act.argtypes = [i32, vp, i64, vp, i64, i64, i32, vp, i32, i64, i32, i32, i32, i32, vp, i64, vp, i64, vp]
+        L.grouped_gemm_bwd_workspace_bytes.argtypes = [i64, i32, i32, i32, psz]
+        L.grouped_gemm_bwd.argtypes = [i32, vp, i64, vp, i64, i64, vp, i32, i64, i32, i32, i32, vp, i64, vp, i64, vp, i64, vp, vp, sz, vp]
+        L.group_norm_workspace_bytes.argtypes = [i64, i32, i32, i32, psz]
+        L.group_norm_act_fwd.argtypes = [i32, vp, i64, vp, i32, i64, i64, i32, i32, vp, vp, f64, i32, vp, i64, vp, vp, vp, sz, vp]
+        L.group_norm_act_bwd.argtypes = [i32, vp, i64, vp, i64, vp, i32, i64, i64, i32, i32, vp, vp, i32, vp, vp, vp, i64, vp, vp, vp,
+                                         sz, vp]
+        L.grad_norm_workspace_bytes.argtypes = [i32, psz]
+        L.grad_global_norm.argtypes = [vp, i32, vp, vp, sz, vp]
+        L.grad_clip_norm.argtypes = [vp, i32, f64, vp, vp, sz, vp]
+        L.grad_scale_to_norm.argtypes = [vp, i32, f64, vp, vp]
         for name in EXPORTS[3:]:
             getattr(L, name).restype = ctypes.c_int
         _lib = L
@@ -165,8 +181,11 @@ class ArgumentError(ctypes.ArgumentError, TypeError):
 
 
 _bound = None
-# the calls of a step: integers and pointers only
-STEP_CALLS = ("spmm_plan_needed_rows", "spmm_pack_rows", "spmm_csr_tallskinny", "dense_gemm_act", "gcn_layer_fwd", "gcn_layer_bwd")
+# the calls of a step: integers and pointers, and one double at most
+STEP_CALLS = ("spmm_plan_needed_rows", "spmm_pack_rows", "spmm_csr_tallskinny", "dense_gemm_act", "gcn_layer_fwd", "gcn_layer_bwd",
+              "grouped_gemm_act", "grouped_gemm_bwd", "group_norm_act_fwd", "group_norm_act_bwd", "grad_global_norm", "grad_clip_norm",
+              "grad_scale_to_norm")
+_KIND = {ctypes.c_void_p: "p", ctypes.c_double: "d"}
 
 
 def _extension():
@@ -189,7 +208,7 @@ def _calls():
         L, ext = lib(), _extension()
         _bound = types.SimpleNamespace(**{
             name: ext.bind(ctypes.cast(getattr(L, name), ctypes.c_void_p).value,
-                           "".join("p" if t is ctypes.c_void_p else "i" for t in getattr(L, name).argtypes), ArgumentError)
+                           "".join(_KIND.get(t, "i") for t in getattr(L, name).argtypes), ArgumentError)
             if ext else _by_ctypes(getattr(L, name)) for name in STEP_CALLS})
     return _bound
 
@@ -683,3 +702,187 @@ def spmm_csr_permute_symmetric(rowptr, colidx, val, inv):
                                             _ptr(cip), _ptr(vap), _ptr(ws), ws.numel(), _stream()),
            "spmm_csr_permute_symmetric")
     return rpp, cip[:nnz], vap[:nnz]
+
+
+_DTYPE = {torch.float32: F32, torch.bfloat16: BF16}
+
+
+def _typed(t: torch.Tensor, name: str, dtype=None):
+    """A row-major matrix of fp32 or bfloat16 (of `dtype` where that is given), possibly a column slice of a wider one."""
+    if not t.is_cuda:
+        raise ValueError(f"{name} must be a CUDA/HIP tensor (there is no CPU path)")
+    if t.dim() != 2 or t.dtype not in _DTYPE or (dtype is not None and t.dtype is not dtype):
+        raise ValueError(f"{name}: expected a 2-D tensor of " + (str(dtype) if dtype is not None else "float32 or bfloat16"))
+    if not t.is_contiguous() and t.shape[0] > 1 and t.shape[1] > 0 and ((t.shape[1] > 1 and t.stride(1) != 1) or t.stride(0) < t.shape[1]):
+        raise ValueError(f"{name}: rows must be contiguous (unit stride inside a row) and must not overlap")
+    return t
+
+
+def _shape(t: torch.Tensor, shape, name: str):
+    if tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name}: expected {tuple(shape)}, got {tuple(t.shape)}")
+    return t
+
+
+def _weights(W: torch.Tensor, dtype):
+    """Weight matrices one behind the other, each row-major: leading dimension and distance of two."""
+    if not W.is_cuda:
+        raise ValueError("W must be a CUDA/HIP tensor (there is no CPU path)")
+    if W.dim() != 3 or W.dtype is not dtype:
+        raise ValueError(f"W: expected a 3-D tensor of {dtype}")
+    g, a, b = W.shape
+    if W.is_contiguous():
+        return b, a * b
+    ld, stride = W.stride(1) if a > 1 else max(b, 1), W.stride(0) if g > 1 else 0
+    if (b > 1 and W.stride(2) != 1) or ld < b or stride < 0:
+        raise ValueError("W: rows must be contiguous (unit stride inside a row) and must not overlap")
+    return ld, stride
+
+
+def _offsets(off: torch.Tensor, name: str):
+    off = _dev(off, torch.int32, name)
+    if off.dim() != 1 or off.numel() < 2:
+        raise ValueError(f"{name}: expected one offset more than there are parts")
+    return off
+
+
+def grouped_gemm_act(X, W, off, transW=False, prec=GEMM_FP32, act=ACT_IDENTITY, mask=None, out=None):
+    """Y[r, :] = act(X[r, :] op(W[g])) .* [mask[r, :] > 0] for the rows off[g] <= r < off[g+1] of each type g; rows behind the
+    last type are zeros.  X: m x kdim, W: types x kdim x nout (types x nout x kdim with transW), float32 or bfloat16;
+    off: int32 on the device, one more than there are types."""
+    X = _typed(X, "X")
+    ldw, stride_w = _weights(W, X.dtype)
+    off = _offsets(off, "off")
+    m, kdim = X.shape
+    types, nout = off.numel() - 1, W.shape[1 if transW else 2]
+    _shape(W, (types, nout, kdim) if transW else (types, kdim, nout), "W")
+    if mask is not None:
+        _shape(_typed(mask, "mask", X.dtype), (m, nout), "mask")
+    if out is None:
+        out = torch.empty((m, nout), dtype=X.dtype, device=X.device)
+    _shape(_typed(out, "out", X.dtype), (m, nout), "out")
+    _check(_calls().grouped_gemm_act(_DTYPE[X.dtype], _ptr(X), _ld(X), _ptr(W), ldw, stride_w, int(transW), _ptr(off), types, m, kdim,
+                                     nout, prec, act, _ptr(mask), _ld(mask) if mask is not None else 0, _ptr(out), _ld(out), _stream()),
+           "grouped_gemm_act")
+    return out
+
+
+def grouped_gemm_bwd(X, W, off, G, mask=None, prec=GEMM_FP32, want_dx=True, want_dw=True):
+    """Gradients of grouped_gemm_act (transW = False, identity): dX[r, :] = (G[r, :] W[g]^T) .* [mask[r, :] > 0] in X's type and
+    dW[g] = X_g^T G_g in float32.  Returns (dX, dW), None for what is not wanted (X or W may be None then: X only where
+    want_dw is False, W never, its shape is needed)."""
+    G = _typed(G, "G")
+    ldw, stride_w = _weights(W, G.dtype)
+    off = _offsets(off, "off")
+    m, nout = G.shape
+    types, kdim = off.numel() - 1, W.shape[1]
+    _shape(W, (types, kdim, nout), "W")
+    if X is not None:
+        _shape(_typed(X, "X", G.dtype), (m, kdim), "X")
+    elif want_dw:
+        raise ValueError("the gradient of W needs X")
+    if mask is not None:
+        _shape(_typed(mask, "mask", G.dtype), (m, kdim), "mask")
+    dX = torch.empty((m, kdim), dtype=G.dtype, device=G.device) if want_dx else None
+    dW = ws = None
+    if want_dw:
+        dW = torch.empty((types, kdim, nout), dtype=torch.float32, device=G.device)
+        b = ctypes.c_size_t(0)
+        _check(lib().grouped_gemm_bwd_workspace_bytes(m, types, kdim, nout, ctypes.byref(b)), "grouped_gemm_bwd_workspace_bytes")
+        ws = _ws(b.value, G.device)
+    _check(_calls().grouped_gemm_bwd(_DTYPE[G.dtype], _ptr(X), _ld(X) if X is not None else kdim, _ptr(W), ldw, stride_w, _ptr(off), types,
+                                     m, kdim, nout, prec, _ptr(G), _ld(G), _ptr(mask), _ld(mask) if mask is not None else 0, _ptr(dX), kdim,
+                                     _ptr(dW), _ptr(ws), ws.numel() if ws is not None else 0, _stream()), "grouped_gemm_bwd")
+    return dX, dW
+
+
+def _norm_args(X, groups, gamma, beta, seg, n_seg):
+    X = _typed(X, "X")
+    m, c = X.shape
+    if seg is not None:
+        seg = _offsets(seg, "seg")
+        n_seg = seg.numel() - 1
+    for name, t in (("gamma", gamma), ("beta", beta)):
+        if t is not None:
+            _shape(_dev(t, torch.float32, name), (c,), name)
+    b = ctypes.c_size_t(0)
+    _check(lib().group_norm_workspace_bytes(m, n_seg, c, groups, ctypes.byref(b)), "group_norm_workspace_bytes")
+    return X, m, c, seg, n_seg, _ws(b.value, X.device)
+
+
+def group_norm_act(X, groups, gamma=None, beta=None, seg=None, n_seg=1, max_rows=0, eps=1e-5, act=ACT_IDENTITY, out=None):
+    """Group norm with an activation, channels last: Y = act((X - mean) rstd gamma + beta), mean and variance over the rows of a
+    segment and each of `groups` groups of channels.  seg: int32 on the device, one more than there are segments (rows behind
+    the last are zeros in Y), or None for n_seg segments of equal length; max_rows: rows of the longest one where it is known.
+    Returns (Y, mean, rstd), the last two float32, segments x groups."""
+    X, m, c, seg, n_seg, ws = _norm_args(X, groups, gamma, beta, seg, n_seg)
+    if out is None:
+        out = torch.empty((m, c), dtype=X.dtype, device=X.device)
+    _shape(_typed(out, "out", X.dtype), (m, c), "out")
+    mean = torch.empty((n_seg, groups), dtype=torch.float32, device=X.device)
+    rstd = torch.empty((n_seg, groups), dtype=torch.float32, device=X.device)
+    _check(_calls().group_norm_act_fwd(_DTYPE[X.dtype], _ptr(X), _ld(X), _ptr(seg), n_seg, max_rows, m, c, groups, _ptr(gamma), _ptr(beta),
+                                       eps, act, _ptr(out), _ld(out), _ptr(mean), _ptr(rstd), _ptr(ws), ws.numel(), _stream()),
+           "group_norm_act_fwd")
+    return out, mean, rstd
+
+
+def group_norm_act_bwd(X, G, mean, rstd, groups, gamma=None, beta=None, seg=None, n_seg=1, max_rows=0, act=ACT_IDENTITY, out=None):
+    """Gradients of group_norm_act for G = dLoss/dY, with the mean and rstd that it returned.  Returns (dX, dgamma, dbeta)."""
+    X, m, c, seg, n_seg, ws = _norm_args(X, groups, gamma, beta, seg, n_seg)
+    _shape(_typed(G, "G", X.dtype), (m, c), "G")
+    for name, t in (("mean", mean), ("rstd", rstd)):
+        _shape(_dev(t, torch.float32, name), (n_seg, groups), name)
+    if out is None:
+        out = torch.empty((m, c), dtype=X.dtype, device=X.device)
+    _shape(_typed(out, "out", X.dtype), (m, c), "out")
+    dgamma = torch.empty(c, dtype=torch.float32, device=X.device)
+    dbeta = torch.empty(c, dtype=torch.float32, device=X.device)
+    _check(_calls().group_norm_act_bwd(_DTYPE[X.dtype], _ptr(X), _ld(X), _ptr(G), _ld(G), _ptr(seg), n_seg, max_rows, m, c, groups,
+                                       _ptr(gamma), _ptr(beta), act, _ptr(mean), _ptr(rstd), _ptr(out), _ld(out), _ptr(dgamma), _ptr(dbeta),
+                                       _ptr(ws), ws.numel(), _stream()), "group_norm_act_bwd")
+    return out, dgamma, dbeta
+
+
+def _grad_list(grads, out=None):
+    """struct sagnn_grad of the C header for each tensor, as rows of 64-bit integers."""
+    if out is None:
+        out = grads
+    elif len(out) != len(grads):
+        raise ValueError("out: expected as many tensors as there are gradients")
+    rows = []
+    for g, o in zip(grads, out):
+        kind = _DTYPE.get(g.dtype)
+        if kind is None or not g.is_cuda or not g.is_contiguous():
+            raise ValueError("gradients: expected contiguous float32 or bfloat16 CUDA/HIP tensors (there is no CPU path)")
+        if o is not g and (o.dtype is not g.dtype or not o.is_cuda or not o.is_contiguous() or o.shape != g.shape):
+            raise ValueError("out: expected contiguous tensors like the gradients")
+        rows.append((g.data_ptr(), o.data_ptr(), g.numel(), kind))
+    return np.array(rows, dtype=np.int64) if rows else None, len(rows)
+
+
+def _grad_ws(n, device):
+    b = ctypes.c_size_t(0)
+    _check(lib().grad_norm_workspace_bytes(n, ctypes.byref(b)), "grad_norm_workspace_bytes")
+    return _ws(b.value, device), torch.empty(1, dtype=torch.float32, device=device)
+
+
+def grad_global_norm(grads):
+    """The 2-norm over all tensors of the list, a float32 tensor of one element on the device."""
+    rows, n = _grad_list(grads)
+    ws, norm = _grad_ws(n, grads[0].device if n else "cuda")
+    _check(_calls().grad_global_norm(rows, n, _ptr(norm), _ptr(ws), ws.numel(), _stream()), "grad_global_norm")
+    return norm
+
+
+def grad_clip_norm(grads, max_norm: float, norm=None, out=None):
+    """Scales the tensors of the list by min(1, max_norm / norm), in place or into `out` (tensors like them).  norm: what
+    grad_global_norm returned, perhaps joined across processes; None computes it.  Returns the norm (on the device)."""
+    rows, n = _grad_list(grads, out)
+    if norm is not None:
+        _shape(_dev(norm, torch.float32, "norm"), (1,), "norm")
+        _check(_calls().grad_scale_to_norm(rows, n, max_norm, _ptr(norm), _stream()), "grad_scale_to_norm")
+        return norm
+    ws, norm = _grad_ws(n, grads[0].device if n else "cuda")
+    _check(_calls().grad_clip_norm(rows, n, max_norm, _ptr(norm), _ptr(ws), ws.numel(), _stream()), "grad_clip_norm")
+    return norm

@@ -1,0 +1,390 @@
+// Products of rows ordered by type with a weight matrix for each type: arguments, the search for a tile's group,
+// staging of operands, and the kernels that stage through registers.  One source file per operand mode instantiates them.
+#pragma once
+#include <initializer_list>
+
+#include "common.h"
+#include "gemm.h"
+
+namespace sagnn {
+
+struct GroupedArgs {
+  const void* X; int64_t ldx;                    // m x kdim
+  const void* W; int64_t ldw; int64_t stride_w;  // groups of kdim x nout, or nout x kdim
+  const void* G; int64_t ldg;                    // weight gradient: m x nout
+  const int32_t* off; int32_t groups;
+  int64_t m; int32_t kdim, nout;
+  int32_t act;
+  const void* mask; int64_t ldmask;
+  void* Y; int64_t ldy;                          // m x nout
+  float* dW; float* partial;                     // weight gradient: groups x kdim x nout, sums of cut groups
+  int64_t chunk;                                 // weight gradient: rows that one workgroup sums at most
+  int32_t row_tiles, col_tiles;                  // of the launch
+};
+
+// Rows of group g as the kernels see them: whatever d_off holds, they lie inside [0, m).
+__device__ __forceinline__ int64_t grouped_row(const int32_t* __restrict__ off, int32_t g, int64_t m) {
+  const int64_t r = off[g];
+  return r < 0 ? 0 : (r > m ? m : r);
+}
+
+struct GroupTile {
+  int32_t g;              // == groups: the rows behind the last group
+  int64_t r0, end;        // first row of the tile, end of the group
+};
+
+// Tile t of the groups' rows cut into tiles of BM, groups ascending, the rows behind the last group as one group
+// more.  Every wavefront looks for itself: 64 groups a round, a scan over the lanes.  False: no such tile.
+template <int BM>
+__device__ __forceinline__ bool grouped_find(const GroupedArgs& a, int32_t t, GroupTile& found) {
+  const int lane = threadIdx.x & 63;
+  int32_t before = 0;
+  for (int32_t g0 = 0; g0 <= a.groups; g0 += 64) {
+    const int32_t g = g0 + lane;
+    const int64_t lo = g <= a.groups ? grouped_row(a.off, g, a.m) : 0;
+    const int64_t hi = g < a.groups ? grouped_row(a.off, g + 1, a.m) : (g == a.groups ? a.m : 0);
+    const int32_t tiles = hi > lo ? (int32_t)((hi - lo + BM - 1) / BM) : 0;
+    int32_t upto = tiles;
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) {
+      const int32_t x = __shfl_up(upto, d);
+      if (lane >= d) upto += x;
+    }
+    const uint64_t past = __ballot(before + upto > t);
+    if (past) {
+      const int f = __builtin_ctzll(past);
+      const int32_t first = before + __builtin_amdgcn_readlane(upto, f) - __builtin_amdgcn_readlane(tiles, f);
+      const int64_t l = __builtin_amdgcn_readlane((int32_t)lo, f), h = __builtin_amdgcn_readlane((int32_t)hi, f);
+      found.g = g0 + f;
+      found.r0 = l + (int64_t)(t - first) * BM;
+      found.end = h;
+      return true;
+    }
+    before += __builtin_amdgcn_readlane(upto, 63);
+  }
+  return false;
+}
+
+// The weight gradient cuts the rows into chunks whatever the groups are; a workgroup sums one group's rows of one
+// chunk.  Walking along the rows, each such pair (chunk c, group g) is met at its own c + g, so that this number
+// names it; not every number does.  Rows [r0, r1) of the pair that p names; cut: the group has rows in other chunks.
+struct GroupPart { int32_t g; int64_t r0, r1; int32_t c; bool cut, first; };
+__device__ __forceinline__ bool grouped_part(const GroupedArgs& a, int32_t p, GroupPart& part) {
+  const int lane = threadIdx.x & 63;
+  int32_t count = 0;                              // groups that begin at numbers up to p
+  for (int32_t g0 = 0; g0 < a.groups; g0 += 64) {
+    const int32_t g = g0 + lane;
+    const int32_t begin = g < a.groups ? (int32_t)(grouped_row(a.off, g, a.m) / a.chunk) + g : INT32_MAX;
+    const uint64_t upto = __ballot(begin <= p);
+    count += __popcll(upto);
+    if (upto != ~0ull) break;
+  }
+  if (count == 0) return false;
+  part.g = __builtin_amdgcn_readfirstlane(count - 1);
+  const int64_t lo = grouped_row(a.off, part.g, a.m), hi = grouped_row(a.off, part.g + 1, a.m);
+  part.c = p - part.g;
+  const int64_t c0 = lo / a.chunk, c1 = hi > lo ? (hi - 1) / a.chunk : c0;
+  if (part.c < c0 || part.c > c1) return false;
+  part.first = part.c == c0;
+  part.cut = c1 > c0;
+  part.r0 = part.first ? lo : part.c * a.chunk;
+  part.r1 = hi < (part.c + 1) * a.chunk ? hi : (part.c + 1) * a.chunk;
+  return true;
+}
+
+// At most one cut group runs into a chunk and one out of it, so the sum of a cut group's part has a place of its own.
+__device__ __forceinline__ int64_t grouped_partial_slot(const GroupPart& p) { return 2 * (int64_t)p.c + (p.first ? 1 : 0); }
+
+// ------------------------------------------------------------------------------------------
+// Operand tiles of ROWS rows (or columns of the right operand) by BK of the summed index.  TR: the summed index is the
+// outer one in memory, so a tile lies as [BK][ROWS], otherwise as [ROWS][BK]; LDS keeps the order of memory, and the
+// transposition happens on the way into the matrix cores.
+// A row of LDS is longer than its tile so that the reads of a wavefront spread over the banks.
+template <int PREC, bool TR, int ROWS, int BK>
+struct TileShape {
+  static constexpr bool F32 = PREC == SAGNN_GEMM_FP32;
+  static constexpr int kPlanes = PREC == SAGNN_GEMM_FP32_BF16X3 ? 3 : 1;
+  static constexpr int kOuter = TR ? BK : ROWS, kInner = TR ? ROWS : BK;
+  static constexpr int kPitch = F32 ? (TR ? ROWS + 8 : BK + 4) : (TR ? ROWS + 32 : BK + 8);
+  static constexpr int kPlane = kOuter * kPitch;                       // elements
+  static constexpr int kBytes = kPlane * kPlanes * (F32 ? 4 : 2);
+};
+
+template <typename T>
+struct __attribute__((packed)) Unaligned { T v; };
+
+template <typename S, int PREC, bool TR, int ROWS, int BK, int THREADS>
+struct TileLoad {
+  using Shape = TileShape<PREC, TR, ROWS, BK>;
+  static constexpr int V = 16 / sizeof(S);
+  static constexpr int kPerRow = Shape::kInner / V;
+  static constexpr int N = Shape::kOuter * kPerRow / THREADS;
+  static_assert(N * THREADS == Shape::kOuter * kPerRow, "tile and workgroup must match");
+  struct __attribute__((aligned(16))) Vec { S x[V]; };
+  Vec v[N];
+
+  // the tile at `base` (leading dimension ld), of which `rows` rows and `sum` of the summed index are there (both
+  // may exceed the tile; at least one of each).  Zeros beyond `sum`; rows beyond `rows` are zeros or any row's.
+  __device__ __forceinline__ void load(const S* __restrict__ base, int64_t ld, int rows, int sum) {
+    const int outer_end = TR ? sum : rows, inner_end = TR ? rows : sum;
+    if (inner_end >= Shape::kInner && (!TR || sum >= BK)) {
+#pragma unroll
+      for (int u = 0; u < N; ++u) {
+        const int w = threadIdx.x + u * THREADS;
+        int o = w / kPerRow;
+        if (!TR) o = o < outer_end ? o : outer_end - 1;
+        const S* p = base + (int64_t)o * ld + (w % kPerRow) * V;
+        // (any element's alignment: the memory instructions take it)
+        v[u] = *reinterpret_cast<const Vec*>(&reinterpret_cast<const Unaligned<Vec>*>(p)->v);
+      }
+      return;
+    }
+#pragma unroll
+    for (int u = 0; u < N; ++u) {
+      const int w = threadIdx.x + u * THREADS, o = w / kPerRow, i = (w % kPerRow) * V;
+      const int there = o < outer_end ? inner_end - i : 0;
+      const S* p = base + (int64_t)o * ld + i;
+      if (there >= V) {
+        v[u] = *reinterpret_cast<const Vec*>(&reinterpret_cast<const Unaligned<Vec>*>(p)->v);
+      } else {
+#pragma unroll
+        for (int e = 0; e < V; ++e) v[u].x[e] = e < there ? p[e] : (S)0.f;
+      }
+    }
+  }
+
+  __device__ __forceinline__ void store(char* smem) const {
+#pragma unroll
+    for (int u = 0; u < N; ++u) {
+      const int w = threadIdx.x + u * THREADS, at = (w / kPerRow) * Shape::kPitch + (w % kPerRow) * V;
+      if constexpr (PREC == SAGNN_GEMM_FP32) {
+        *reinterpret_cast<Vec*>(reinterpret_cast<float*>(smem) + at) = v[u];
+      } else if constexpr (sizeof(S) == 2) {
+        *reinterpret_cast<Vec*>(reinterpret_cast<__bf16*>(smem) + at) = v[u];
+      } else {
+        bf16x4 t[3];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          __bf16 t1 = (__bf16)v[u].x[e], t2 = t1, t3 = t1;
+          if constexpr (PREC == SAGNN_GEMM_FP32_BF16X3) split3(v[u].x[e], t1, t2, t3);
+          t[0][e] = t1; t[1][e] = t2; t[2][e] = t3;
+        }
+#pragma unroll
+        for (int q = 0; q < Shape::kPlanes; ++q)
+          *reinterpret_cast<bf16x4*>(reinterpret_cast<__bf16*>(smem) + q * Shape::kPlane + at) = t[q];
+      }
+    }
+  }
+};
+
+typedef short short4v __attribute__((ext_vector_type(4)));
+
+// 32 rows (or columns) from `row0` on, 16 of the summed index from `k0` on: the operand of one 32x32x16 instruction.
+// A lane has row lane % 32 and the eight sums of its half.  TR: two transposing reads; sixteen lanes read four rows of
+// 32 bytes, and each gets a column of four.
+template <typename Shape, bool TR>
+__device__ __forceinline__ bf16x8 tile_operand(const __bf16* tile, int row0, int k0) {
+  const int lane = threadIdx.x & 63;
+  if constexpr (!TR) {
+    return *reinterpret_cast<const bf16x8*>(tile + (row0 + (lane & 31)) * Shape::kPitch + k0 + (lane >> 5) * 8);
+  } else {
+    const __bf16* p = tile + (k0 + (lane >> 5) * 8 + ((lane & 15) >> 2)) * Shape::kPitch + row0 + (lane & 16) + (lane & 3) * 4;
+    using L = __attribute__((address_space(3))) short4v;
+    union { short4v h[2]; bf16x8 x; } r;
+    r.h[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((L*)p);
+    r.h[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((L*)(p + 4 * Shape::kPitch));
+    return r.x;
+  }
+}
+
+// acc += A B over one staged step.  The workgroup's WM x WN wavefronts own TM x TN tiles of 32 x 32 each.
+template <int PREC, bool TRA, bool TRB, int WM, int WN, int TM, int TN, int BK>
+__device__ __forceinline__ void tile_multiply(const char* sa, const char* sb, floatx16 (&acc)[TM][TN]) {
+  using SA = TileShape<PREC, TRA, WM * TM * 32, BK>;
+  using SB = TileShape<PREC, TRB, WN * TN * 32, BK>;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int ra = (wave / WN) * TM * 32, rb = (wave % WN) * TN * 32;
+  if constexpr (PREC == SAGNN_GEMM_FP32) {
+    const float* A = reinterpret_cast<const float*>(sa);
+    const float* B = reinterpret_cast<const float*>(sb);
+    const int r = lane & 31, h = lane >> 5;
+    // eight sums a turn: the lower half of the wavefront takes the first four, the upper one the others
+#pragma unroll
+    for (int k = 0; k < BK; k += 8) {
+      float x[TM][4], y[TN][4];
+#pragma unroll
+      for (int t = 0; t < TM; ++t) {
+        if constexpr (!TRA) *reinterpret_cast<float4*>(x[t]) = *reinterpret_cast<const float4*>(A + (ra + t * 32 + r) * SA::kPitch + k + 4 * h);
+        else
+#pragma unroll
+          for (int i = 0; i < 4; ++i) x[t][i] = A[(k + 4 * h + i) * SA::kPitch + ra + t * 32 + r];
+      }
+#pragma unroll
+      for (int t = 0; t < TN; ++t) {
+        if constexpr (!TRB) *reinterpret_cast<float4*>(y[t]) = *reinterpret_cast<const float4*>(B + (rb + t * 32 + r) * SB::kPitch + k + 4 * h);
+        else
+#pragma unroll
+          for (int i = 0; i < 4; ++i) y[t][i] = B[(k + 4 * h + i) * SB::kPitch + rb + t * 32 + r];
+      }
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int tm = 0; tm < TM; ++tm)
+#pragma unroll
+          for (int tn = 0; tn < TN; ++tn)
+            acc[tm][tn] = __builtin_amdgcn_mfma_f32_32x32x2f32(x[tm][i], y[tn][i], acc[tm][tn], 0, 0, 0);
+    }
+  } else {
+    const __bf16* A = reinterpret_cast<const __bf16*>(sa);
+    const __bf16* B = reinterpret_cast<const __bf16*>(sb);
+    constexpr int P = SA::kPlanes;
+#pragma unroll
+    for (int k = 0; k < BK; k += 16) {
+      bf16x8 x[P][TM], y[P][TN];
+#pragma unroll
+      for (int q = 0; q < P; ++q) {
+#pragma unroll
+        for (int t = 0; t < TM; ++t) x[q][t] = tile_operand<SA, TRA>(A + q * SA::kPlane, ra + t * 32, k);
+#pragma unroll
+        for (int t = 0; t < TN; ++t) y[q][t] = tile_operand<SB, TRB>(B + q * SB::kPlane, rb + t * 32, k);
+      }
+      // split mode: the six products down to 2^-16 of the leading one, smallest first
+      constexpr int pair[6][2] = {{2, 0}, {0, 2}, {1, 1}, {1, 0}, {0, 1}, {0, 0}};
+#pragma unroll
+      for (int s = P == 3 ? 0 : 5; s < 6; ++s)
+#pragma unroll
+        for (int tm = 0; tm < TM; ++tm)
+#pragma unroll
+          for (int tn = 0; tn < TN; ++tn)
+            acc[tm][tn] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x[pair[s][0]][tm], y[pair[s][1]][tn], acc[tm][tn], 0, 0, 0);
+    }
+  }
+}
+
+// acc = A B over `sum` of the summed index: a step of both operands is loaded into registers while the one before it
+// is multiplied out of LDS.
+template <typename S, int PREC, bool TRA, bool TRB, int WM, int WN, int TM, int TN, int BK>
+__device__ __forceinline__ void tile_product(const S* A, int64_t lda, int rows, const S* B, int64_t ldb, int cols, int64_t sum,
+                                             char* smem, floatx16 (&acc)[TM][TN]) {
+  constexpr int THREADS = WM * WN * 64;
+  using SA = TileShape<PREC, TRA, WM * TM * 32, BK>;
+  TileLoad<S, PREC, TRA, WM * TM * 32, BK, THREADS> la;
+  TileLoad<S, PREC, TRB, WN * TN * 32, BK, THREADS> lb;
+#pragma unroll
+  for (int tm = 0; tm < TM; ++tm)
+#pragma unroll
+    for (int tn = 0; tn < TN; ++tn)
+#pragma unroll
+      for (int v = 0; v < 16; ++v) acc[tm][tn][v] = 0.f;
+  if (sum <= 0) return;
+  auto left = [&](int64_t k) { return (int)(sum - k < BK ? sum - k : BK); };
+  la.load(A, lda, rows, left(0));
+  lb.load(B, ldb, cols, left(0));
+  for (int64_t k = 0; k < sum; k += BK) {
+    la.store(smem);
+    lb.store(smem + SA::kBytes);
+    __syncthreads();
+    if (k + BK < sum) {
+      la.load(A + (k + BK) * (TRA ? lda : 1), lda, rows, left(k + BK));
+      lb.load(B + (k + BK) * (TRB ? ldb : 1), ldb, cols, left(k + BK));
+    }
+    tile_multiply<PREC, TRA, TRB, WM, WN, TM, TN, BK>(smem, smem + SA::kBytes, acc);
+    __syncthreads();
+  }
+}
+
+// f(row, column, sum) of the values that a lane holds, rows and columns relative to the workgroup's tile
+template <int WM, int WN, int TM, int TN, typename F>
+__device__ __forceinline__ void tile_each(const floatx16 (&acc)[TM][TN], F f) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+#pragma unroll
+  for (int tm = 0; tm < TM; ++tm)
+#pragma unroll
+    for (int v = 0; v < 16; ++v)
+#pragma unroll
+      for (int tn = 0; tn < TN; ++tn)
+        f(((wave / WN) * TM + tm) * 32 + 8 * (v / 4) + 4 * (lane >> 5) + v % 4, ((wave % WN) * TN + tn) * 32 + (lane & 31), acc[tm][tn][v]);
+}
+
+// Workgroups of one launch are dealt to the XCDs in turn: neighbouring tiles go to the same one.
+__device__ __forceinline__ int32_t xcd_run(int32_t id, int32_t n) {
+  const int32_t each = n / 8, more = n % 8, x = id % 8;
+  return x * each + (x < more ? x : more) + id / 8;
+}
+
+template <typename S, int PREC, bool WT, int WM, int WN, int TM, int TN, int BK>
+__global__ __launch_bounds__(WM * WN * 64) void grouped_kernel(const GroupedArgs a) {
+  constexpr int BM = WM * TM * 32, BN = WN * TN * 32;
+  __shared__ __attribute__((aligned(16))) char smem[TileShape<PREC, false, BM, BK>::kBytes + TileShape<PREC, !WT, BN, BK>::kBytes];
+  const int32_t id = xcd_run(blockIdx.x, gridDim.x);
+  GroupTile t;
+  if (!grouped_find<BM>(a, id / a.col_tiles, t)) return;
+  const int64_t c0 = (int64_t)(id % a.col_tiles) * BN;
+  const int rows = (int)(t.end - t.r0 < BM ? t.end - t.r0 : BM), cols = (int)(a.nout - c0 < BN ? a.nout - c0 : BN);
+  floatx16 acc[TM][TN];
+  const S* W = reinterpret_cast<const S*>(a.W) + (t.g < a.groups ? t.g * a.stride_w : 0) + c0 * (WT ? a.ldw : 1);
+  tile_product<S, PREC, false, !WT, WM, WN, TM, TN, BK>(reinterpret_cast<const S*>(a.X) + t.r0 * a.ldx, a.ldx, rows, W, a.ldw, cols,
+                                                        t.g < a.groups ? a.kdim : 0, smem, acc);
+  S* Y = reinterpret_cast<S*>(a.Y) + t.r0 * a.ldy + c0;
+  const S* mask = a.mask ? reinterpret_cast<const S*>(a.mask) + t.r0 * a.ldmask + c0 : nullptr;
+  const bool relu = a.act == SAGNN_ACT_RELU;
+  tile_each<WM, WN, TM, TN>(acc, [&](int r, int c, float y) {
+    if (r >= rows || c >= cols) return;
+    if (relu && y < 0.f) y = 0.f;
+    if (mask && !((float)mask[(int64_t)r * a.ldmask + c] > 0.f)) y = 0.f;
+    Y[(int64_t)r * a.ldy + c] = (S)y;
+  });
+}
+
+template <typename S, int PREC, int WM, int WN, int TM, int TN, int BK>
+__global__ __launch_bounds__(WM * WN * 64) void grouped_tn_kernel(const GroupedArgs a) {
+  constexpr int BM = WM * TM * 32, BN = WN * TN * 32;
+  __shared__ __attribute__((aligned(16))) char smem[TileShape<PREC, true, BM, BK>::kBytes + TileShape<PREC, true, BN, BK>::kBytes];
+  const int32_t id = xcd_run(blockIdx.x, gridDim.x), tiles = a.row_tiles * a.col_tiles;
+  GroupPart p;
+  if (!grouped_part(a, id / tiles, p)) return;
+  const int64_t k0 = (int64_t)(id % tiles / a.col_tiles) * BM, c0 = (int64_t)(id % tiles % a.col_tiles) * BN;
+  const int rows = (int)(a.kdim - k0 < BM ? a.kdim - k0 : BM), cols = (int)(a.nout - c0 < BN ? a.nout - c0 : BN);
+  floatx16 acc[TM][TN];
+  tile_product<S, PREC, true, true, WM, WN, TM, TN, BK>(reinterpret_cast<const S*>(a.X) + p.r0 * a.ldx + k0, a.ldx, rows,
+                                                        reinterpret_cast<const S*>(a.G) + p.r0 * a.ldg + c0, a.ldg, cols, p.r1 - p.r0, smem, acc);
+  float* out = (p.cut ? a.partial + grouped_partial_slot(p) * a.kdim * a.nout : a.dW + (int64_t)p.g * a.kdim * a.nout) + k0 * a.nout + c0;
+  tile_each<WM, WN, TM, TN>(acc, [&](int r, int c, float y) {
+    if (r < rows && c < cols) out[(int64_t)r * a.nout + c] = y;
+  });
+}
+
+// Tiles that a launch can take: rows of X (of W for the weight gradient) by columns
+enum { kTile128 = 0, kTile64 = 1, kTile32x128 = 2 };
+inline int grouped_tile_rows(int tile) { return tile == kTile128 ? 128 : (tile == kTile64 ? 64 : 32); }
+inline int grouped_tile_cols(int tile) { return tile == kTile64 ? 64 : 128; }
+
+// one launch of `blocks` workgroups; per operand mode (and storage type)
+#define SAGNN_GROUPED_MODE(name)                                                                                       \
+  int grouped_##name(const GroupedArgs& a, int tile, bool trans_w, int64_t blocks, hipStream_t s);                      \
+  int grouped_tn_##name(const GroupedArgs& a, int tile, int64_t blocks, hipStream_t s);
+SAGNN_GROUPED_MODE(fp32)
+SAGNN_GROUPED_MODE(fp32_bf16)
+SAGNN_GROUPED_MODE(fp32_bf16x3)
+SAGNN_GROUPED_MODE(bf16)
+#undef SAGNN_GROUPED_MODE
+
+template <typename S, int PREC, int BK, bool WT>
+int grouped_launch(const GroupedArgs& a, int tile, int64_t blocks, hipStream_t s) {
+  const dim3 grid((uint32_t)blocks), block(256);
+  if (tile == kTile128) grouped_kernel<S, PREC, WT, 2, 2, 2, 2, BK><<<grid, block, 0, s>>>(a);
+  else if (tile == kTile64) grouped_kernel<S, PREC, WT, 2, 2, 1, 1, BK><<<grid, block, 0, s>>>(a);
+  else grouped_kernel<S, PREC, WT, 1, 4, 1, 1, BK><<<grid, block, 0, s>>>(a);
+  SAGNN_LAUNCH_CHECK();
+  return SAGNN_OK;
+}
+template <typename S, int PREC, int BK>
+int grouped_tn_launch(const GroupedArgs& a, int tile, int64_t blocks, hipStream_t s) {
+  const dim3 grid((uint32_t)blocks), block(256);
+  if (tile == kTile128) grouped_tn_kernel<S, PREC, 2, 2, 2, 2, BK><<<grid, block, 0, s>>>(a);
+  else grouped_tn_kernel<S, PREC, 2, 2, 1, 1, BK><<<grid, block, 0, s>>>(a);
+  SAGNN_LAUNCH_CHECK();
+  return SAGNN_OK;
+}
+
+}  // namespace sagnn

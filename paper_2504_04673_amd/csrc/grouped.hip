@@ -1,0 +1,138 @@
+// Products of rows ordered by type (see grouped.h): entry points, the choice of tiles, and the sum of the parts of a
+// group whose rows were cut.
+#include "grouped.h"
+
+namespace sagnn {
+namespace {
+
+// dW[g] = the sum of its parts, chunks ascending; a group of one part was written by the product itself.
+__global__ __launch_bounds__(256) void grouped_join_kernel(const GroupedArgs a) {
+  const int32_t g = blockIdx.y;
+  const int64_t lo = grouped_row(a.off, g, a.m), hi = grouped_row(a.off, g + 1, a.m), size = (int64_t)a.kdim * a.nout;
+  if (hi <= lo) return;
+  const int64_t c0 = lo / a.chunk, c1 = (hi - 1) / a.chunk;
+  if (c0 == c1) return;
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < size; i += (int64_t)gridDim.x * 256) {
+    float sum = a.partial[(2 * c0 + 1) * size + i];
+#pragma unroll 8
+    for (int64_t c = c0 + 1; c <= c1; ++c) sum += a.partial[2 * c * size + i];
+    a.dW[g * size + i] = sum;
+  }
+}
+
+bool valid(int32_t dtype, int32_t prec, int64_t m, int32_t groups, int32_t kdim, int32_t nout) {
+  return (dtype == SAGNN_F32 || (dtype == SAGNN_BF16 && prec == SAGNN_GEMM_FP32)) && prec >= SAGNN_GEMM_FP32 && prec <= SAGNN_GEMM_FP32_BF16X3 &&
+         m >= 0 && m <= INT32_MAX && groups >= 1 && groups <= SAGNN_GROUPED_MAX && kdim >= 1 && kdim <= SAGNN_GROUPED_MAX_WIDTH &&
+         nout >= 1 && nout <= SAGNN_GROUPED_MAX_WIDTH;
+}
+bool element_aligned(const void* p, int32_t dtype) { return (reinterpret_cast<uintptr_t>(p) & (dtype == SAGNN_BF16 ? 1u : 3u)) == 0; }
+
+int launch_rows(const GroupedArgs& g, int32_t dtype, int32_t prec, bool trans_w, hipStream_t s) {
+  GroupedArgs a = g;
+  const int64_t mean = a.m / a.groups;
+  auto count = [&](int tile) {
+    return (a.m / grouped_tile_rows(tile) + a.groups + 1) * ceil_div(a.nout, grouped_tile_cols(tile));
+  };
+  const int tile = mean <= 32 ? kTile32x128 : (count(kTile128) < 256 ? kTile64 : kTile128);
+  a.row_tiles = (int32_t)(a.m / grouped_tile_rows(tile) + a.groups + 1);
+  a.col_tiles = (int32_t)ceil_div(a.nout, grouped_tile_cols(tile));
+  const int64_t blocks = (int64_t)a.row_tiles * a.col_tiles;
+  if (blocks > INT32_MAX) return SAGNN_EINVAL;
+  if (dtype == SAGNN_BF16) return grouped_bf16(a, tile, trans_w, blocks, s);
+  return prec == SAGNN_GEMM_FP32 ? grouped_fp32(a, tile, trans_w, blocks, s)
+         : prec == SAGNN_GEMM_BF16 ? grouped_fp32_bf16(a, tile, trans_w, blocks, s) : grouped_fp32_bf16x3(a, tile, trans_w, blocks, s);
+}
+
+struct TnPlan { int tile; int64_t row_tiles, col_tiles, chunk, chunks; };
+TnPlan tn_plan(int64_t m, int32_t kdim, int32_t nout) {
+  TnPlan p{};
+  p.tile = kdim <= 64 || nout <= 64 ? kTile64 : kTile128;
+  p.row_tiles = ceil_div(kdim, grouped_tile_rows(p.tile));
+  p.col_tiles = ceil_div(nout, grouped_tile_cols(p.tile));
+  int64_t chunks = 512 / (p.row_tiles * p.col_tiles);
+  chunks = chunks < ceil_div(m, 256) ? chunks : ceil_div(m, 256);
+  if (chunks < 1) chunks = 1;
+  p.chunk = round_up((size_t)ceil_div(m > 0 ? m : 1, chunks), 64);
+  p.chunks = ceil_div(m > 0 ? m : 1, p.chunk);
+  return p;
+}
+size_t tn_ws_bytes(int64_t m, int32_t kdim, int32_t nout) {
+  const TnPlan p = tn_plan(m, kdim, nout);
+  return p.chunks > 1 ? (size_t)(2 * p.chunks) * kdim * nout * 4 : 0;
+}
+
+int launch_tn(const GroupedArgs& g, int32_t dtype, int32_t prec, hipStream_t s) {
+  GroupedArgs a = g;
+  const TnPlan p = tn_plan(a.m, a.kdim, a.nout);
+  a.chunk = p.chunk;
+  a.row_tiles = (int32_t)p.row_tiles;
+  a.col_tiles = (int32_t)p.col_tiles;
+  const int64_t blocks = (p.chunks + a.groups) * p.row_tiles * p.col_tiles;
+  if (blocks > INT32_MAX) return SAGNN_EINVAL;
+  const int rc = dtype == SAGNN_BF16 ? grouped_tn_bf16(a, p.tile, blocks, s)
+                 : prec == SAGNN_GEMM_FP32 ? grouped_tn_fp32(a, p.tile, blocks, s)
+                 : prec == SAGNN_GEMM_BF16 ? grouped_tn_fp32_bf16(a, p.tile, blocks, s) : grouped_tn_fp32_bf16x3(a, p.tile, blocks, s);
+  if (rc != SAGNN_OK || p.chunks == 1) return rc;
+  int64_t wide = ceil_div((int64_t)a.kdim * a.nout, 256);
+  if (wide > 1024) wide = 1024;
+  grouped_join_kernel<<<dim3((uint32_t)wide, (uint32_t)a.groups), 256, 0, s>>>(a);
+  SAGNN_LAUNCH_CHECK();
+  return SAGNN_OK;
+}
+
+}  // namespace
+}  // namespace sagnn
+
+SAGNN_EXPORT int grouped_gemm_act(int32_t dtype, const void* d_X, int64_t ldx, const void* d_W, int64_t ldw, int64_t stride_w,
+                                  int32_t transW, const int32_t* d_off, int32_t n_groups, int64_t m, int32_t kdim, int32_t nout,
+                                  int32_t prec, int32_t act, const void* d_mask, int64_t ldmask, void* d_Y, int64_t ldy, void* stream) {
+  using namespace sagnn;
+  if (!valid(dtype, prec, m, n_groups, kdim, nout) || (transW & ~1) || (act != SAGNN_ACT_IDENTITY && act != SAGNN_ACT_RELU)) return SAGNN_EINVAL;
+  if (ldx < kdim || ldy < nout || ldw < (transW ? kdim : nout) || stride_w < 0 || (d_mask && ldmask < nout)) return SAGNN_EINVAL;
+  if (m == 0) return SAGNN_OK;
+  if (!d_X || !d_W || !d_off || !d_Y) return SAGNN_EINVAL;
+  for (const void* p : {d_X, d_W, d_mask, (const void*)d_Y})
+    if (!element_aligned(p, dtype)) return SAGNN_EINVAL;
+  if (!element_aligned(d_off, SAGNN_F32)) return SAGNN_EINVAL;
+  GroupedArgs a{};
+  a.X = d_X; a.ldx = ldx; a.W = d_W; a.ldw = ldw; a.stride_w = stride_w; a.off = d_off; a.groups = n_groups;
+  a.m = m; a.kdim = kdim; a.nout = nout; a.act = act; a.mask = d_mask; a.ldmask = ldmask; a.Y = d_Y; a.ldy = ldy;
+  return launch_rows(a, dtype, prec, transW != 0, (hipStream_t)stream);
+}
+
+SAGNN_EXPORT int grouped_gemm_bwd_workspace_bytes(int64_t m, int32_t n_groups, int32_t kdim, int32_t nout, size_t* bytes) {
+  using namespace sagnn;
+  if (!bytes || !valid(SAGNN_F32, SAGNN_GEMM_FP32, m, n_groups, kdim, nout)) return SAGNN_EINVAL;
+  *bytes = tn_ws_bytes(m, kdim, nout);
+  return SAGNN_OK;
+}
+
+SAGNN_EXPORT int grouped_gemm_bwd(int32_t dtype, const void* d_X, int64_t ldx, const void* d_W, int64_t ldw, int64_t stride_w,
+                                  const int32_t* d_off, int32_t n_groups, int64_t m, int32_t kdim, int32_t nout, int32_t prec,
+                                  const void* d_G, int64_t ldg, const void* d_mask, int64_t ldmask, void* d_dX, int64_t lddx,
+                                  float* d_dW, void* d_ws, size_t ws_bytes, void* stream) {
+  using namespace sagnn;
+  if (!valid(dtype, prec, m, n_groups, kdim, nout) || ldg < nout) return SAGNN_EINVAL;
+  if (d_dX && (ldw < nout || stride_w < 0 || lddx < kdim || (d_mask && ldmask < kdim))) return SAGNN_EINVAL;
+  if (d_dW && ldx < kdim) return SAGNN_EINVAL;
+  if ((m > 0 && (!d_G || (d_dX && !d_W) || (d_dW && !d_X))) || ((m > 0 || d_dW) && !d_off)) return SAGNN_EINVAL;
+  for (const void* p : {d_X, d_W, d_G, d_mask, (const void*)d_dX})
+    if (!element_aligned(p, dtype)) return SAGNN_EINVAL;
+  if (!element_aligned(d_off, SAGNN_F32) || !element_aligned(d_dW, SAGNN_F32) || !element_aligned(d_ws, SAGNN_F32)) return SAGNN_EINVAL;
+  if (d_dW && ws_bytes < tn_ws_bytes(m, kdim, nout)) return SAGNN_ECAPACITY;
+  if (d_dW && !d_ws && tn_ws_bytes(m, kdim, nout) > 0) return SAGNN_EINVAL;
+  hipStream_t s = (hipStream_t)stream;
+  GroupedArgs a{};
+  a.off = d_off; a.groups = n_groups; a.m = m;
+  if (d_dX && m > 0) {       // (G W^T: the stored W read as the transposed one of a product with kdim and nout exchanged)
+    a.X = d_G; a.ldx = ldg; a.W = d_W; a.ldw = ldw; a.stride_w = stride_w; a.kdim = nout; a.nout = kdim;
+    a.mask = d_mask; a.ldmask = ldmask; a.Y = d_dX; a.ldy = lddx;
+    const int rc = launch_rows(a, dtype, prec, true, s);
+    if (rc != SAGNN_OK) return rc;
+  }
+  if (d_dW) {
+    a.X = d_X; a.ldx = ldx; a.G = d_G; a.ldg = ldg; a.kdim = kdim; a.nout = nout; a.dW = d_dW; a.partial = (float*)d_ws;
+    return launch_tn(a, dtype, prec, s);
+  }
+  return SAGNN_OK;
+}

@@ -1,0 +1,11 @@
+// The grouped products of grouped.h: bfloat16 tensors.
+#include "grouped.h"
+
+namespace sagnn {
+int grouped_bf16(const GroupedArgs& a, int tile, bool trans_w, int64_t blocks, hipStream_t s) {
+  return trans_w ? grouped_launch<__bf16, SAGNN_GEMM_BF16, 64, true>(a, tile, blocks, s) : grouped_launch<__bf16, SAGNN_GEMM_BF16, 64, false>(a, tile, blocks, s);
+}
+int grouped_tn_bf16(const GroupedArgs& a, int tile, int64_t blocks, hipStream_t s) {
+  return grouped_tn_launch<__bf16, SAGNN_GEMM_BF16, 64>(a, tile, blocks, s);
+}
+}  // namespace sagnn
