@@ -33,31 +33,59 @@ struct GroupTile {
   int64_t r0, end;        // first row of the tile, end of the group
 };
 
-// Tile t of the groups' rows cut into tiles of BM, groups ascending, the rows behind the last group as one group
-// more.  Every wavefront looks for itself: 64 groups a round, a scan over the lanes.  False: no such tile.
+// Workgroups of one launch are dealt to the XCDs in turn: neighbours among n tiles go to the same one.
+__device__ __forceinline__ int32_t xcd_run(int32_t id, int32_t n) {
+  const int32_t each = n / 8, more = n % 8, x = id % 8;
+  return x * each + (x < more ? x : more) + id / 8;
+}
+
+// Tiles of BM rows of group g, and the group's rows (g == groups: the rows behind the last group; beyond: none)
 template <int BM>
-__device__ __forceinline__ bool grouped_find(const GroupedArgs& a, int32_t t, GroupTile& found) {
+__device__ __forceinline__ int32_t grouped_tiles(const GroupedArgs& a, int32_t g, int64_t& lo, int64_t& hi) {
+  lo = g <= a.groups ? grouped_row(a.off, g, a.m) : 0;
+  hi = g < a.groups ? grouped_row(a.off, g + 1, a.m) : (g == a.groups ? a.m : 0);
+  return hi > lo ? (int32_t)((hi - lo + BM - 1) / BM) : 0;
+}
+__device__ __forceinline__ int32_t wave_sums(int32_t x) {     // of the lanes up to each
   const int lane = threadIdx.x & 63;
+#pragma unroll
+  for (int d = 1; d < 64; d *= 2) {
+    const int32_t y = __shfl_up(x, d);
+    if (lane >= d) x += y;
+  }
+  return x;
+}
+
+// The tile of this workgroup: the groups' rows cut into tiles of BM, groups ascending, columns fastest.  How many there are only
+// d_off tells, and the launch has workgroups for the most there can be; the XCDs share those that there are (dealt by
+// the launch's size, the last XCDs got the missing ones: 8192^3 in five rounds instead of four).  Every wavefront looks
+// for itself: 64 groups a round, a scan over the lanes.  False: no tile.
+template <int BM>
+__device__ __forceinline__ bool grouped_find(const GroupedArgs& a, GroupTile& found, int32_t& col) {
+  const int lane = threadIdx.x & 63;
+  int64_t lo, hi;
+  int32_t tiles = grouped_tiles<BM>(a, lane, lo, hi), upto = wave_sums(tiles);
+  int32_t total = __builtin_amdgcn_readlane(upto, 63);
+  for (int32_t g0 = 64; g0 <= a.groups; g0 += 64) {
+    int64_t l, h;
+    total += __builtin_amdgcn_readlane(wave_sums(grouped_tiles<BM>(a, g0 + lane, l, h)), 63);
+  }
+  if ((int64_t)blockIdx.x >= (int64_t)total * a.col_tiles) return false;
+  const int32_t id = xcd_run(blockIdx.x, total * a.col_tiles), t = id / a.col_tiles;
+  col = id % a.col_tiles;
   int32_t before = 0;
   for (int32_t g0 = 0; g0 <= a.groups; g0 += 64) {
-    const int32_t g = g0 + lane;
-    const int64_t lo = g <= a.groups ? grouped_row(a.off, g, a.m) : 0;
-    const int64_t hi = g < a.groups ? grouped_row(a.off, g + 1, a.m) : (g == a.groups ? a.m : 0);
-    const int32_t tiles = hi > lo ? (int32_t)((hi - lo + BM - 1) / BM) : 0;
-    int32_t upto = tiles;
-#pragma unroll
-    for (int d = 1; d < 64; d *= 2) {
-      const int32_t x = __shfl_up(upto, d);
-      if (lane >= d) upto += x;
+    if (g0) {
+      tiles = grouped_tiles<BM>(a, g0 + lane, lo, hi);
+      upto = wave_sums(tiles);
     }
     const uint64_t past = __ballot(before + upto > t);
     if (past) {
       const int f = __builtin_ctzll(past);
       const int32_t first = before + __builtin_amdgcn_readlane(upto, f) - __builtin_amdgcn_readlane(tiles, f);
-      const int64_t l = __builtin_amdgcn_readlane((int32_t)lo, f), h = __builtin_amdgcn_readlane((int32_t)hi, f);
       found.g = g0 + f;
-      found.r0 = l + (int64_t)(t - first) * BM;
-      found.end = h;
+      found.r0 = __builtin_amdgcn_readlane((int32_t)lo, f) + (int64_t)(t - first) * BM;
+      found.end = __builtin_amdgcn_readlane((int32_t)hi, f);
       return true;
     }
     before += __builtin_amdgcn_readlane(upto, 63);
@@ -69,8 +97,13 @@ __device__ __forceinline__ bool grouped_find(const GroupedArgs& a, int32_t t, Gr
 // chunk.  Walking along the rows, each such pair (chunk c, group g) is met at its own c + g, so that this number
 // names it; not every number does.  Rows [r0, r1) of the pair that p names; cut: the group has rows in other chunks.
 struct GroupPart { int32_t g; int64_t r0, r1; int32_t c; bool cut, first; };
-__device__ __forceinline__ bool grouped_part(const GroupedArgs& a, int32_t p, GroupPart& part) {
+__device__ __forceinline__ bool grouped_part(const GroupedArgs& a, GroupPart& part, int32_t& tile) {
   const int lane = threadIdx.x & 63;
+  // Eight tiles or more: each XCD has a run of them, for every pair (the last pairs may not be there).
+  const int32_t tiles = a.row_tiles * a.col_tiles, id = (int32_t)blockIdx.x;
+  int32_t p = id / tiles;
+  tile = id % tiles;
+  if (tiles % 8 == 0) tile = xcd_run(tile, tiles);
   int32_t count = 0;                              // groups that begin at numbers up to p
   for (int32_t g0 = 0; g0 < a.groups; g0 += 64) {
     const int32_t g = g0 + lane;
@@ -306,20 +339,14 @@ __device__ __forceinline__ void tile_each(const floatx16 (&acc)[TM][TN], F f) {
         f(((wave / WN) * TM + tm) * 32 + 8 * (v / 4) + 4 * (lane >> 5) + v % 4, ((wave % WN) * TN + tn) * 32 + (lane & 31), acc[tm][tn][v]);
 }
 
-// Workgroups of one launch are dealt to the XCDs in turn: neighbouring tiles go to the same one.
-__device__ __forceinline__ int32_t xcd_run(int32_t id, int32_t n) {
-  const int32_t each = n / 8, more = n % 8, x = id % 8;
-  return x * each + (x < more ? x : more) + id / 8;
-}
-
 template <typename S, int PREC, bool WT, int WM, int WN, int TM, int TN, int BK>
 __global__ __launch_bounds__(WM * WN * 64) void grouped_kernel(const GroupedArgs a) {
   constexpr int BM = WM * TM * 32, BN = WN * TN * 32;
   __shared__ __attribute__((aligned(16))) char smem[TileShape<PREC, false, BM, BK>::kBytes + TileShape<PREC, !WT, BN, BK>::kBytes];
-  const int32_t id = xcd_run(blockIdx.x, gridDim.x);
   GroupTile t;
-  if (!grouped_find<BM>(a, id / a.col_tiles, t)) return;
-  const int64_t c0 = (int64_t)(id % a.col_tiles) * BN;
+  int32_t col;
+  if (!grouped_find<BM>(a, t, col)) return;
+  const int64_t c0 = (int64_t)col * BN;
   const int rows = (int)(t.end - t.r0 < BM ? t.end - t.r0 : BM), cols = (int)(a.nout - c0 < BN ? a.nout - c0 : BN);
   floatx16 acc[TM][TN];
   const S* W = reinterpret_cast<const S*>(a.W) + (t.g < a.groups ? t.g * a.stride_w : 0) + c0 * (WT ? a.ldw : 1);
@@ -340,10 +367,10 @@ template <typename S, int PREC, int WM, int WN, int TM, int TN, int BK>
 __global__ __launch_bounds__(WM * WN * 64) void grouped_tn_kernel(const GroupedArgs a) {
   constexpr int BM = WM * TM * 32, BN = WN * TN * 32;
   __shared__ __attribute__((aligned(16))) char smem[TileShape<PREC, true, BM, BK>::kBytes + TileShape<PREC, true, BN, BK>::kBytes];
-  const int32_t id = xcd_run(blockIdx.x, gridDim.x), tiles = a.row_tiles * a.col_tiles;
   GroupPart p;
-  if (!grouped_part(a, id / tiles, p)) return;
-  const int64_t k0 = (int64_t)(id % tiles / a.col_tiles) * BM, c0 = (int64_t)(id % tiles % a.col_tiles) * BN;
+  int32_t tile;
+  if (!grouped_part(a, p, tile)) return;
+  const int64_t k0 = (int64_t)(tile / a.col_tiles) * BM, c0 = (int64_t)(tile % a.col_tiles) * BN;
   const int rows = (int)(a.kdim - k0 < BM ? a.kdim - k0 : BM), cols = (int)(a.nout - c0 < BN ? a.nout - c0 : BN);
   floatx16 acc[TM][TN];
   tile_product<S, PREC, true, true, WM, WN, TM, TN, BK>(reinterpret_cast<const S*>(a.X) + p.r0 * a.ldx + k0, a.ldx, rows,
@@ -355,9 +382,9 @@ __global__ __launch_bounds__(WM * WN * 64) void grouped_tn_kernel(const GroupedA
 }
 
 // Tiles that a launch can take: rows of X (of W for the weight gradient) by columns
-enum { kTile128 = 0, kTile64 = 1, kTile32x128 = 2 };
-inline int grouped_tile_rows(int tile) { return tile == kTile128 ? 128 : (tile == kTile64 ? 64 : 32); }
-inline int grouped_tile_cols(int tile) { return tile == kTile64 ? 64 : 128; }
+enum { kTile128 = 0, kTile64 = 1, kTile32x128 = 2, kDirect256 = 3 };
+inline int grouped_tile_rows(int tile) { return tile == kDirect256 ? 256 : tile == kTile128 ? 128 : (tile == kTile64 ? 64 : 32); }
+inline int grouped_tile_cols(int tile) { return tile == kDirect256 ? 256 : tile == kTile64 ? 64 : 128; }
 
 // one launch of `blocks` workgroups; per operand mode (and storage type)
 #define SAGNN_GROUPED_MODE(name)                                                                                       \

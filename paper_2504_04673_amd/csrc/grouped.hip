@@ -27,13 +27,21 @@ bool valid(int32_t dtype, int32_t prec, int64_t m, int32_t groups, int32_t kdim,
 }
 bool element_aligned(const void* p, int32_t dtype) { return (reinterpret_cast<uintptr_t>(p) & (dtype == SAGNN_BF16 ? 1u : 3u)) == 0; }
 
+// Whether the kernels that load into LDS directly take an operand: rows of whole granules, offsets inside a tile below 2^31
+bool direct_rows(const void* p, int64_t ld, int64_t width) {
+  return (reinterpret_cast<uintptr_t>(p) & 15) == 0 && ld % 8 == 0 && width % 8 == 0 && ld <= (1 << 20);
+}
+
 int launch_rows(const GroupedArgs& g, int32_t dtype, int32_t prec, bool trans_w, hipStream_t s) {
   GroupedArgs a = g;
   const int64_t mean = a.m / a.groups;
   auto count = [&](int tile) {
     return (a.m / grouped_tile_rows(tile) + a.groups + 1) * ceil_div(a.nout, grouped_tile_cols(tile));
   };
-  const int tile = mean <= 32 ? kTile32x128 : (count(kTile128) < 256 ? kTile64 : kTile128);
+  int tile = mean <= 32 ? kTile32x128 : (count(kTile128) < 256 ? kTile64 : kTile128);
+  if (dtype == SAGNN_BF16 && tile == kTile128 && count(kDirect256) >= 128 && direct_rows(a.X, a.ldx, a.kdim) && direct_rows(a.W, a.ldw, a.nout) &&
+      a.stride_w % 8 == 0 && direct_rows(a.Y, a.ldy, 0) && (!a.mask || direct_rows(a.mask, a.ldmask, 0)))
+    tile = kDirect256;
   a.row_tiles = (int32_t)(a.m / grouped_tile_rows(tile) + a.groups + 1);
   a.col_tiles = (int32_t)ceil_div(a.nout, grouped_tile_cols(tile));
   const int64_t blocks = (int64_t)a.row_tiles * a.col_tiles;
@@ -44,26 +52,33 @@ int launch_rows(const GroupedArgs& g, int32_t dtype, int32_t prec, bool trans_w,
 }
 
 struct TnPlan { int tile; int64_t row_tiles, col_tiles, chunk, chunks; };
-TnPlan tn_plan(int64_t m, int32_t kdim, int32_t nout) {
+// Chunks of rows.  More of them fill the chip where the matrices are small or one group has most rows; but a group that a chunk's end cuts
+// costs its matrix written twice, read twice and written once more, against 2 rows of arithmetic each for the chunk: not above
+// an eighth of that time where there are as many workgroups as half the CUs anyway (16 groups of 16384 x 2048 x 1024: 16 chunks
+// 202 us, 4 chunks 139).
+TnPlan tn_plan(int64_t m, int32_t kdim, int32_t nout, bool direct) {
   TnPlan p{};
-  p.tile = kdim <= 64 || nout <= 64 ? kTile64 : kTile128;
+  p.tile = kdim <= 64 || nout <= 64 ? kTile64 : direct && kdim >= 256 && nout >= 256 ? kDirect256 : kTile128;
   p.row_tiles = ceil_div(kdim, grouped_tile_rows(p.tile));
   p.col_tiles = ceil_div(nout, grouped_tile_cols(p.tile));
-  int64_t chunks = 512 / (p.row_tiles * p.col_tiles);
-  chunks = chunks < ceil_div(m, 256) ? chunks : ceil_div(m, 256);
+  const int64_t tiles = p.row_tiles * p.col_tiles, rare = m / (direct ? 8192 : 2048);
+  int64_t chunks = 512 / tiles < rare ? 512 / tiles : rare;
+  if (chunks < 128 / tiles) chunks = 128 / tiles;
+  if (chunks > ceil_div(m, 256)) chunks = ceil_div(m, 256);
   if (chunks < 1) chunks = 1;
   p.chunk = round_up((size_t)ceil_div(m > 0 ? m : 1, chunks), 64);
   p.chunks = ceil_div(m > 0 ? m : 1, p.chunk);
   return p;
 }
 size_t tn_ws_bytes(int64_t m, int32_t kdim, int32_t nout) {
-  const TnPlan p = tn_plan(m, kdim, nout);
-  return p.chunks > 1 ? (size_t)(2 * p.chunks) * kdim * nout * 4 : 0;
+  const int64_t a = tn_plan(m, kdim, nout, false).chunks, b = tn_plan(m, kdim, nout, true).chunks, chunks = a > b ? a : b;
+  return chunks > 1 ? (size_t)(2 * chunks) * kdim * nout * 4 : 0;
 }
 
 int launch_tn(const GroupedArgs& g, int32_t dtype, int32_t prec, hipStream_t s) {
   GroupedArgs a = g;
-  const TnPlan p = tn_plan(a.m, a.kdim, a.nout);
+  const TnPlan p = tn_plan(a.m, a.kdim, a.nout, dtype == SAGNN_BF16 && direct_rows(a.X, a.ldx, a.kdim) && direct_rows(a.G, a.ldg, a.nout) &&
+                                                    aligned16(a.dW) && aligned16(a.partial));
   a.chunk = p.chunk;
   a.row_tiles = (int32_t)p.row_tiles;
   a.col_tiles = (int32_t)p.col_tiles;
