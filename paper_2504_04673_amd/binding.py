@@ -2,6 +2,7 @@
 from __future__ import annotations
 
 import ctypes
+import functools
 import importlib
 import os
 import types
@@ -188,10 +189,10 @@ STEP_CALLS = ("spmm_plan_needed_rows", "spmm_pack_rows", "spmm_csr_tallskinny", 
 _KIND = {ctypes.c_void_p: "p", ctypes.c_double: "d"}
 
 
-def _extension():
-    """csrc/marshal.c as built for this interpreter; None where it is not."""
+def _extension(name="_marshal", path=None):
+    """csrc/marshal.c (or another) as built for this interpreter; None where it is not."""
     try:
-        return importlib.import_module(f"{__package__}._marshal") if os.path.exists(_build.MARSHAL) else None
+        return importlib.import_module(f"{__package__}.{name}") if os.path.exists(path or _build.MARSHAL) else None
     except ImportError:
         return None
 
@@ -787,9 +788,7 @@ def grouped_gemm_bwd(X, W, off, G, mask=None, prec=GEMM_FP32, want_dx=True, want
     dW = ws = None
     if want_dw:
         dW = torch.empty((types, kdim, nout), dtype=torch.float32, device=G.device)
-        b = ctypes.c_size_t(0)
-        _check(lib().grouped_gemm_bwd_workspace_bytes(m, types, kdim, nout, ctypes.byref(b)), "grouped_gemm_bwd_workspace_bytes")
-        ws = _ws(b.value, G.device)
+        ws = _ws(_bytes_of("grouped_gemm_bwd_workspace_bytes", m, types, kdim, nout), G.device)
     _check(_calls().grouped_gemm_bwd(_DTYPE[G.dtype], _ptr(X), _ld(X) if X is not None else kdim, _ptr(W), ldw, stride_w, _ptr(off), types,
                                      m, kdim, nout, prec, _ptr(G), _ld(G), _ptr(mask), _ld(mask) if mask is not None else 0, _ptr(dX), kdim,
                                      _ptr(dW), _ptr(ws), ws.numel() if ws is not None else 0, _stream()), "grouped_gemm_bwd")
@@ -805,9 +804,7 @@ def _norm_args(X, groups, gamma, beta, seg, n_seg):
     for name, t in (("gamma", gamma), ("beta", beta)):
         if t is not None:
             _shape(_dev(t, torch.float32, name), (c,), name)
-    b = ctypes.c_size_t(0)
-    _check(lib().group_norm_workspace_bytes(m, n_seg, c, groups, ctypes.byref(b)), "group_norm_workspace_bytes")
-    return X, m, c, seg, n_seg, _ws(b.value, X.device)
+    return X, m, c, seg, n_seg, _ws(_bytes_of("group_norm_workspace_bytes", m, n_seg, c, groups), X.device)
 
 
 def group_norm_act(X, groups, gamma=None, beta=None, seg=None, n_seg=1, max_rows=0, eps=1e-5, act=ACT_IDENTITY, out=None):
@@ -819,8 +816,7 @@ def group_norm_act(X, groups, gamma=None, beta=None, seg=None, n_seg=1, max_rows
     if out is None:
         out = torch.empty((m, c), dtype=X.dtype, device=X.device)
     _shape(_typed(out, "out", X.dtype), (m, c), "out")
-    mean = torch.empty((n_seg, groups), dtype=torch.float32, device=X.device)
-    rstd = torch.empty((n_seg, groups), dtype=torch.float32, device=X.device)
+    mean, rstd = torch.empty((2, n_seg, groups), dtype=torch.float32, device=X.device).unbind()
     _check(_calls().group_norm_act_fwd(_DTYPE[X.dtype], _ptr(X), _ld(X), _ptr(seg), n_seg, max_rows, m, c, groups, _ptr(gamma), _ptr(beta),
                                        eps, act, _ptr(out), _ld(out), _ptr(mean), _ptr(rstd), _ptr(ws), ws.numel(), _stream()),
            "group_norm_act_fwd")
@@ -836,35 +832,48 @@ def group_norm_act_bwd(X, G, mean, rstd, groups, gamma=None, beta=None, seg=None
     if out is None:
         out = torch.empty((m, c), dtype=X.dtype, device=X.device)
     _shape(_typed(out, "out", X.dtype), (m, c), "out")
-    dgamma = torch.empty(c, dtype=torch.float32, device=X.device)
-    dbeta = torch.empty(c, dtype=torch.float32, device=X.device)
+    dgamma, dbeta = torch.empty((2, c), dtype=torch.float32, device=X.device).unbind()
     _check(_calls().group_norm_act_bwd(_DTYPE[X.dtype], _ptr(X), _ld(X), _ptr(G), _ld(G), _ptr(seg), n_seg, max_rows, m, c, groups,
                                        _ptr(gamma), _ptr(beta), act, _ptr(mean), _ptr(rstd), _ptr(out), _ld(out), _ptr(dgamma), _ptr(dbeta),
                                        _ptr(ws), ws.numel(), _stream()), "group_norm_act_bwd")
     return out, dgamma, dbeta
 
 
-def _grad_list(grads, out=None):
-    """struct sagnn_grad of the C header for each tensor, as rows of 64-bit integers."""
-    if out is None:
-        out = grads
-    elif len(out) != len(grads):
-        raise ValueError("out: expected as many tensors as there are gradients")
+def _rows_in_python(grads, out):
     rows = []
-    for g, o in zip(grads, out):
+    for g, o in zip(grads, grads if out is None else out, strict=True):
         kind = _DTYPE.get(g.dtype)
         if kind is None or not g.is_cuda or not g.is_contiguous():
             raise ValueError("gradients: expected contiguous float32 or bfloat16 CUDA/HIP tensors (there is no CPU path)")
         if o is not g and (o.dtype is not g.dtype or not o.is_cuda or not o.is_contiguous() or o.shape != g.shape):
             raise ValueError("out: expected contiguous tensors like the gradients")
         rows.append((g.data_ptr(), o.data_ptr(), g.numel(), kind))
-    return np.array(rows, dtype=np.int64) if rows else None, len(rows)
+    return np.array(rows, dtype=np.int64).tobytes()
+
+
+_rows = None
+
+
+def _grad_list(grads, out=None):
+    """struct sagnn_grad of the C header for each tensor, one behind the other."""
+    global _rows
+    if _rows is None:                      # csrc/gradlist.cpp, or the same in Python where it is not built
+        ext = _extension("_gradlist", _build.GRADLIST)
+        _rows = ext.rows if ext else _rows_in_python
+    rows = _rows(grads, out)
+    return rows, len(rows) // 32
+
+
+@functools.lru_cache(maxsize=256)
+def _bytes_of(query: str, *sizes) -> int:
+    """What a workspace query of the library says, a function of the sizes alone."""
+    b = ctypes.c_size_t(0)
+    _check(getattr(lib(), query)(*sizes, ctypes.byref(b)), query)
+    return b.value
 
 
 def _grad_ws(n, device):
-    b = ctypes.c_size_t(0)
-    _check(lib().grad_norm_workspace_bytes(n, ctypes.byref(b)), "grad_norm_workspace_bytes")
-    return _ws(b.value, device), torch.empty(1, dtype=torch.float32, device=device)
+    return _ws(_bytes_of("grad_norm_workspace_bytes", n), device), torch.empty(1, dtype=torch.float32, device=device)
 
 
 def grad_global_norm(grads):

@@ -14,6 +14,9 @@ LIB = os.path.join(_HERE, "libsagnn.so")
 # csrc/marshal.c, the calls of binding.py: for one interpreter's headers, which its name carries
 MARSHAL_SOURCE = os.path.join(CSRC, "marshal.c")
 MARSHAL = os.path.join(_HERE, "_marshal" + sysconfig.get_config_var("EXT_SUFFIX"))
+# csrc/gradlist.cpp, lists of tensors for the gradient calls: against torch's headers
+GRADLIST_SOURCE = os.path.join(CSRC, "gradlist.cpp")
+GRADLIST = os.path.join(_HERE, "_gradlist" + sysconfig.get_config_var("EXT_SUFFIX"))
 OBJDIR = os.path.join(_HERE, "_build")
 SOURCES = ["api.hip", "pack.hip", "plan.hip", "spmm.hip", "spmm_flat.hip", "spmm_sweep.hip", "gemm_nn_bf16.hip", "gemm_nn_fp32.hip", "gemm_nn_bf16x3.hip", "gemm.hip", "stages.hip", "radix.hip",
            "fused.hip", "permute.hip", "sweep_plan.hip", "tiles.hip", "grouped.hip", "grouped_fp32.hip", "grouped_fp32_bf16.hip",
@@ -37,11 +40,15 @@ def stale() -> bool:
     if not os.path.exists(LIB):
         return True
     t = os.path.getmtime(LIB)
-    return any(os.path.getmtime(d) > t for d in sources() + HEADERS) or marshal_stale()
+    return any(os.path.getmtime(d) > t for d in sources() + HEADERS) or marshal_stale() or gradlist_stale()
 
 
 def marshal_stale() -> bool:
     return not os.path.exists(MARSHAL) or os.path.getmtime(MARSHAL_SOURCE) > os.path.getmtime(MARSHAL)
+
+
+def gradlist_stale() -> bool:
+    return not os.path.exists(GRADLIST) or os.path.getmtime(GRADLIST_SOURCE) > os.path.getmtime(GRADLIST)
 
 
 def _run(cmd, verbose):
@@ -76,17 +83,34 @@ def build_hip(verbose: bool = False, incremental: bool = False, jobs: int = 8) -
         if os.path.exists(MARSHAL):
             os.remove(MARSHAL)                # (of another source)
         warnings.warn(f"calls go through ctypes: {e}")
+    try:
+        build_gradlist(verbose)
+    except (OSError, RuntimeError) as e:      # no C++ compiler: binding.py asks the tensors one by one
+        if os.path.exists(GRADLIST):
+            os.remove(GRADLIST)
+        warnings.warn(f"lists of tensors are read in Python: {e}")
     return LIB
 
 
-def build_marshal(verbose: bool = False) -> str:
+def _build_extension(cmd, target, verbose) -> str:
     """Compiled beside its place and moved there whole: another process may be loading it."""
-    part = f"{MARSHAL}.{os.getpid()}"
+    part = f"{target}.{os.getpid()}"
     try:
-        _run([os.environ.get("CC", "gcc"), "-O2", "-Wall", "-shared", "-fPIC", "-I" + sysconfig.get_paths()["include"], "-o", part,
-              MARSHAL_SOURCE], verbose)
-        os.replace(part, MARSHAL)
+        _run([*cmd, "-shared", "-fPIC", "-I" + sysconfig.get_paths()["include"], "-o", part], verbose)
+        os.replace(part, target)
     finally:
         if os.path.exists(part):
             os.remove(part)
-    return MARSHAL
+    return target
+
+
+def build_marshal(verbose: bool = False) -> str:
+    return _build_extension([os.environ.get("CC", "gcc"), "-O2", "-Wall", MARSHAL_SOURCE], MARSHAL, verbose)
+
+
+def build_gradlist(verbose: bool = False) -> str:
+    import torch
+    from torch.utils.cpp_extension import include_paths
+    libs = os.path.join(os.path.dirname(torch.__file__), "lib")
+    return _build_extension([os.environ.get("CXX", "g++"), "-O2", "-std=c++17", GRADLIST_SOURCE, *["-I" + i for i in include_paths()],
+                             "-L" + libs, "-lc10", "-ltorch_cpu", "-ltorch_python"], GRADLIST, verbose)

@@ -11,7 +11,9 @@ namespace {
 constexpr int kThreads = 256;
 constexpr int kMaxBlocks = 2048;     // workgroups of a launch that sums, and the sums that it leaves
 constexpr int kListed = 120;         // tensors that one launch takes: they travel as its arguments (4 KB at most)
-constexpr int kPiece = 16384;        // values that a workgroup takes at a time
+// Values that a workgroup takes at a time: so many that kMaxBlocks workgroups have one each, within these bounds (120
+// tensors, 10 M values: 16384 each 10 us to sum and 14 to scale, 4096 to 6144 ... see list_of)
+constexpr int kLeastPiece = 2048, kMostPiece = 16384;
 
 struct List {
   const void* in[kListed];
@@ -19,7 +21,7 @@ struct List {
   int32_t first[kListed + 1];        // pieces before the tensor
   uint32_t last[kListed];            // values of its last piece
   uint8_t bf16[kListed];
-  int32_t count;
+  int32_t count, piece;              // tensors, values of a piece
 };
 static_assert(sizeof(List) <= 3800, "arguments of a launch");
 
@@ -47,6 +49,16 @@ __device__ __forceinline__ double sum_piece(const S* __restrict__ p, int n) {
   constexpr int V = 16 / sizeof(S);
   double s = 0.;
   int i = threadIdx.x * V;
+  for (; i + 3 * kThreads * V + V <= n; i += 4 * kThreads * V) {        // (four loads in flight)
+    Whole<S, V> w[4];
+#pragma unroll
+    for (int u = 0; u < 4; ++u) __builtin_memcpy(&w[u], reinterpret_cast<const Packed<S, V>*>(p + i + u * kThreads * V), 16);
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int u = 0; u < 4; ++u)
+#pragma unroll
+      for (int e = 0; e < V; ++e) s = fma((double)(float)w[u].x[e], (double)(float)w[u].x[e], s);
+  }
   for (; i + V <= n; i += kThreads * V) {
     Whole<S, V> w;
     __builtin_memcpy(&w, reinterpret_cast<const Packed<S, V>*>(p + i), 16);
@@ -61,6 +73,18 @@ template <typename S>
 __device__ __forceinline__ void scale_piece(const S* p, S* q, int n, float c) {
   constexpr int V = 16 / sizeof(S);
   int i = threadIdx.x * V;
+  for (; i + 3 * kThreads * V + V <= n; i += 4 * kThreads * V) {
+    Whole<S, V> w[4];
+#pragma unroll
+    for (int u = 0; u < 4; ++u) __builtin_memcpy(&w[u], reinterpret_cast<const Packed<S, V>*>(p + i + u * kThreads * V), 16);
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+#pragma unroll
+      for (int e = 0; e < V; ++e) w[u].x[e] = (S)((float)w[u].x[e] * c);
+      __builtin_memcpy(reinterpret_cast<Packed<S, V>*>(q + i + u * kThreads * V), &w[u], 16);
+    }
+  }
   for (; i + V <= n; i += kThreads * V) {
     Whole<S, V> w;
     __builtin_memcpy(&w, reinterpret_cast<const Packed<S, V>*>(p + i), 16);
@@ -86,9 +110,9 @@ __global__ __launch_bounds__(kThreads) void grad_sum_kernel(const List l, double
   for (int32_t piece = blockIdx.x; piece < l.first[l.count]; piece += gridDim.x) {
     const int t = find_tensor(l, piece);
     const int32_t at = piece - l.first[t];
-    const int n = piece + 1 == l.first[t + 1] ? (int)l.last[t] : kPiece;
-    s += l.bf16[t] ? sum_piece(reinterpret_cast<const __bf16*>(l.in[t]) + (int64_t)at * kPiece, n)
-                   : sum_piece(reinterpret_cast<const float*>(l.in[t]) + (int64_t)at * kPiece, n);
+    const int n = piece + 1 == l.first[t + 1] ? (int)l.last[t] : l.piece;
+    s += l.bf16[t] ? sum_piece(reinterpret_cast<const __bf16*>(l.in[t]) + (int64_t)at * l.piece, n)
+                   : sum_piece(reinterpret_cast<const float*>(l.in[t]) + (int64_t)at * l.piece, n);
   }
   s = block_sum(s);
   if (threadIdx.x == 0) sums[blockIdx.x] = s;
@@ -115,38 +139,47 @@ __global__ __launch_bounds__(kThreads) void grad_scale_kernel(const List l, cons
   for (int32_t piece = l.first[l.count] - 1 - (int32_t)blockIdx.x; piece >= 0; piece -= gridDim.x) {
     const int t = find_tensor(l, piece);
     if (c == 1.f && l.in[t] == l.out[t]) continue;   // (nothing changes)
-    const int64_t at = (int64_t)(piece - l.first[t]) * kPiece;
-    const int k = piece + 1 == l.first[t + 1] ? (int)l.last[t] : kPiece;
+    const int64_t at = (int64_t)(piece - l.first[t]) * l.piece;
+    const int k = piece + 1 == l.first[t + 1] ? (int)l.last[t] : l.piece;
     if (l.bf16[t]) scale_piece(reinterpret_cast<const __bf16*>(l.in[t]) + at, reinterpret_cast<__bf16*>(l.out[t]) + at, k, c);
     else scale_piece(reinterpret_cast<const float*>(l.in[t]) + at, reinterpret_cast<float*>(l.out[t]) + at, k, c);
   }
 }
 
-int64_t pieces_of(const sagnn_grad& g) { return ceil_div(g.n, kPiece); }
 int grid_of(int64_t pieces) { return (int)(pieces < kMaxBlocks ? pieces : kMaxBlocks); }
 
 // The tensors in lists of one launch each: f(list, pieces)
 template <typename F>
 int each_list(const sagnn_grad* h, int32_t n, F f) {
-  List l;
-  l.count = 0;
-  l.first[0] = 0;
-  for (int32_t i = 0; i < n; ++i) {
-    if (h[i].n == 0) continue;
-    const int64_t pieces = pieces_of(h[i]);
-    if (l.count == kListed || l.first[l.count] + pieces > INT32_MAX) {
-      const int rc = f(l, l.first[l.count]);
-      if (rc != SAGNN_OK) return rc;
-      l.count = 0;
+  for (int32_t i = 0; i < n;) {
+    List l;
+    l.count = 0;
+    l.first[0] = 0;
+    int64_t values = 0;
+    int32_t end = i;
+    for (int32_t c = 0; end < n && c < kListed; ++end) {
+      if (h[end].n == 0) continue;
+      if (c > 0 && values + h[end].n > (int64_t)kLeastPiece * (1 << 30)) break;
+      values += h[end].n;
+      ++c;
     }
-    l.in[l.count] = h[i].d_in;
-    l.out[l.count] = h[i].d_out;
-    l.last[l.count] = (uint32_t)(h[i].n - (pieces - 1) * kPiece);
-    l.bf16[l.count] = h[i].dtype == SAGNN_BF16;
-    l.first[l.count + 1] = l.first[l.count] + (int32_t)pieces;
-    ++l.count;
+    const int64_t each = (int64_t)round_up((size_t)ceil_div(values > 0 ? values : 1, kMaxBlocks), kLeastPiece);
+    l.piece = (int32_t)(each < kMostPiece ? each : kMostPiece);
+    for (; i < end; ++i) {
+      if (h[i].n == 0) continue;
+      const int64_t pieces = ceil_div(h[i].n, l.piece);
+      l.in[l.count] = h[i].d_in;
+      l.out[l.count] = h[i].d_out;
+      l.last[l.count] = (uint32_t)(h[i].n - (pieces - 1) * l.piece);
+      l.bf16[l.count] = h[i].dtype == SAGNN_BF16;
+      l.first[l.count + 1] = l.first[l.count] + (int32_t)pieces;
+      ++l.count;
+    }
+    if (!l.count) continue;
+    const int rc = f(l, (int64_t)l.first[l.count]);
+    if (rc != SAGNN_OK) return rc;
   }
-  return l.count ? f(l, l.first[l.count]) : SAGNN_OK;
+  return SAGNN_OK;
 }
 
 struct Span { uintptr_t begin, end; bool written; };
@@ -156,7 +189,7 @@ int check(const sagnn_grad* h, int32_t n, bool written) {
   if (n < 0 || n > SAGNN_GRAD_MAX || (n > 0 && !h)) return SAGNN_EINVAL;
   for (int32_t i = 0; i < n; ++i) {
     const uintptr_t size = h[i].dtype == SAGNN_BF16 ? 2 : 4;
-    if ((h[i].dtype != SAGNN_F32 && h[i].dtype != SAGNN_BF16) || h[i].n < 0 || h[i].n > ((int64_t)1 << 44)) return SAGNN_EINVAL;
+    if ((h[i].dtype != SAGNN_F32 && h[i].dtype != SAGNN_BF16) || h[i].n < 0 || h[i].n > ((int64_t)1 << 40)) return SAGNN_EINVAL;
     if (h[i].n == 0) continue;
     if (!h[i].d_in || ((uintptr_t)h[i].d_in & (size - 1))) return SAGNN_EINVAL;
     if (written && (!h[i].d_out || ((uintptr_t)h[i].d_out & (size - 1)))) return SAGNN_EINVAL;

@@ -1,10 +1,11 @@
 // Group norm with an activation over the rows of a segment, channels last: y = act((x - mean) rstd gamma + beta), mean
 // and variance over a segment's rows and a group's channels; forward and backward.
 //
-// The rows are cut into chunks whatever the segments are, one workgroup each.  Walking along the rows, the pair (chunk
-// c, segment b) is met at its own c + b, so that the sums of a segment's parts lie behind one another in a table with
-// room for chunks + segments of them.  A launch sums the parts, one joins them, one writes the rows: x is read twice
-// (dy too), the price of the dependence.
+// Two forms.  Where the longest segment (the caller says how long) and some groups of channels fit a workgroup's registers, one
+// workgroup reads them once, reduces, and writes: the bytes bound it.  Otherwise the rows are cut into chunks whatever the
+// segments are, one workgroup each.  Walking along the rows, the pair (chunk c, segment b) is met at its own c + b, so that the
+// sums of a segment's parts lie behind one another in a table with room for chunks + segments of them.  A launch sums
+// the parts, one joins them, one writes the rows: x is read twice (dy too), the price of the dependence.
 #include <type_traits>
 
 #include "common.h"
@@ -25,30 +26,75 @@ struct NormArgs {
   double eps; int32_t act;
   float* dgamma; float* dbeta;
   int64_t chunk, chunks;             // rows of a chunk, chunks
+  int64_t table;                     // rows of `rows`
+  int32_t slab;                      // channels of a workgroup, where it takes whole segments
   double2* parts;                    // (chunks + segments) x groups
   float2* sums;                      // backward, segments x groups: the two sums over a group, divided by its size
-  float2* rows;                      // backward, chunks x C: sums of h xh and h over the rows of a chunk
+  float2* rows;                      // backward, table x C: sums of h xh and h over the rows of a chunk (of some segments)
 };
 
 template <typename S, int V>
 struct __attribute__((packed)) Packed { S x[V]; };
 
+template <typename S, int V>
+struct __attribute__((aligned(sizeof(S) * V))) Whole { S x[V]; };
+template <typename S, int V>
+struct Two { Whole<S, V> a, b; };
+
 // V neighbouring values at any element's alignment
 template <typename S, int V>
-__device__ __forceinline__ void load(const S* p, float (&v)[V]) {
-  struct __attribute__((aligned(sizeof(S) * V))) Whole { S x[V]; };
-  Whole w;
+__device__ __forceinline__ Whole<S, V> fetch(const S* p) {
+  Whole<S, V> w;
   __builtin_memcpy(&w, reinterpret_cast<const Packed<S, V>*>(p), sizeof(w));
-#pragma unroll
-  for (int i = 0; i < V; ++i) v[i] = (float)w.x[i];
+  return w;
 }
 template <typename S, int V>
 __device__ __forceinline__ void store(S* p, const float (&v)[V]) {
-  struct __attribute__((aligned(sizeof(S) * V))) Whole { S x[V]; };
-  Whole w;
+  Whole<S, V> w;
 #pragma unroll
   for (int i = 0; i < V; ++i) w.x[i] = (S)v[i];
   __builtin_memcpy(reinterpret_cast<Packed<S, V>*>(p), &w, sizeof(w));
+}
+// (what is kept stays as it was loaded: worked out once for both uses, it took four registers a 16-byte vector more)
+template <typename S, int V>
+__device__ __forceinline__ void keep(Whole<S, V>& w) {
+  constexpr int kBytes = sizeof(S) * V;
+  if constexpr (kBytes == 4) {
+    uint32_t r = __builtin_bit_cast(uint32_t, w);
+    asm volatile("" : "+v"(r));
+    w = __builtin_bit_cast(Whole<S, V>, r);
+  } else if constexpr (kBytes > 4) {
+    typedef uint32_t Raw __attribute__((ext_vector_type(kBytes / 4)));
+    Raw r = __builtin_bit_cast(Raw, w);
+    asm volatile("" : "+v"(r));
+    w = __builtin_bit_cast(Whole<S, V>, r);
+  } else {
+    uint16_t r = __builtin_bit_cast(uint16_t, w);
+    asm volatile("" : "+v"(r));
+    w = __builtin_bit_cast(Whole<S, V>, r);
+  }
+}
+template <typename S, int V>
+__device__ __forceinline__ void store_zeros(S* p) {
+  float z[V];
+#pragma unroll
+  for (int i = 0; i < V; ++i) z[i] = 0.f;
+  store<S, V>(p, z);
+}
+
+// Rows r, r + step, ... below end: N of them are fetched before the first is used.
+template <int N, typename F, typename U>
+__device__ __forceinline__ void each_row(int64_t r, int64_t end, int step, F get, U use) {
+  using W = decltype(get(r));
+  for (; r + (N - 1) * step < end; r += N * step) {
+    W w[N];
+#pragma unroll
+    for (int n = 0; n < N; ++n) w[n] = get(r + n * step);
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int n = 0; n < N; ++n) use(r + n * step, w[n]);
+  }
+  for (; r < end; r += step) use(r, get(r));
 }
 
 __device__ __forceinline__ int64_t seg_row(const NormArgs& a, int64_t b) {
@@ -151,18 +197,25 @@ __device__ __forceinline__ void to_groups(const NormArgs& a, const Lay& l, int c
   }
 }
 
-__device__ __forceinline__ float act_value(float z, int act) {
-  if (act == SAGNN_ACT_RELU) return z < 0.f ? 0.f : z;
-  if (act == SAGNN_ACT_SILU) return z / (1.f + __expf(-z));
+// 1 / (1 + exp(-z)) by the machine's exponential and reciprocal (an ulp each); a division in its place is ten instructions.
+__device__ __forceinline__ float sigmoid(float z) {
+  return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(z * -1.44269504f));
+}
+template <int ACT>
+__device__ __forceinline__ float act_value(float z) {
+  if (ACT == SAGNN_ACT_RELU) return z < 0.f ? 0.f : z;
+  if (ACT == SAGNN_ACT_SILU) return z * sigmoid(z);
   return z;
 }
-__device__ __forceinline__ float act_slope(float z, int act) {
-  if (act == SAGNN_ACT_RELU) return z > 0.f ? 1.f : 0.f;
-  if (act == SAGNN_ACT_SILU) {
-    const float t = 1.f / (1.f + __expf(-z));
-    return t * (1.f + z * (1.f - t));
+// g act'(z)
+template <int ACT>
+__device__ __forceinline__ float act_gradient(float g, float z) {
+  if (ACT == SAGNN_ACT_RELU) return z > 0.f ? g : g == g ? 0.f : g;      // (0 times a NaN)
+  if (ACT == SAGNN_ACT_SILU) {
+    const float t = sigmoid(z);
+    return g * fmaf(z * t, 1.f - t, t);
   }
-  return 1.f;
+  return g;
 }
 
 // Sum and sum of squares of a part, in 64 bits: whatever the mean is against the deviation, their difference holds.
@@ -183,16 +236,14 @@ __global__ __launch_bounds__(kThreads) void norm_sum_kernel(const NormArgs a) {
 #pragma unroll
       for (int i = 0; i < V; ++i) p[i] = q[i] = 0.;
       if (l.ty < l.rows)
-        for (int64_t r = r0 + l.ty; r < r1; r += l.rows) {
-          float x[V];
-          load<S, V>(X + r * a.ldx + ch, x);
+        each_row<4>(r0 + l.ty, r1, l.rows, [&](int64_t r) { return fetch<S, V>(X + r * a.ldx + ch); }, [&](int64_t, const Whole<S, V>& w) {
 #pragma unroll
           for (int i = 0; i < V; ++i) {
-            const double d = x[i];
+            const double d = (float)w.x[i];
             p[i] += d;
-            q[i] += d * d;
+            q[i] = fma(d, d, q[i]);
           }
-        }
+        });
       to_groups<V>(a, l, vec0 * V, p, q, sm, acc);
     }
     __syncthreads();
@@ -231,52 +282,60 @@ __global__ __launch_bounds__(kThreads) void norm_join_kernel(const NormArgs a) {
   }
 }
 
-template <typename S, int V>
+// What a vector's channels make of its values: z = scale x + shift, (x - mean) rstd = rstd x + base.  (A mean far from zero costs
+// the digits that its own rounding costs.)  N: groups that a vector can have, 1 where a group is whole vectors, else V.
+template <int V, int N>
+struct Channel {
+  float scale[V], shift[V], rstd[N], base[N];
+  __device__ __forceinline__ void read(const NormArgs& a, int32_t b, int ch) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const int64_t g = (int64_t)b * a.groups + (ch + i) / a.D;
+      rstd[i] = a.rstd[g];
+      base[i] = a.mean[g];
+    }
+    affine(a, ch);
+  }
+  // `base` holds the mean
+  __device__ __forceinline__ void affine(const NormArgs& a, int ch) {
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+      scale[i] = (a.gamma ? a.gamma[ch + i] : 1.f) * rstd[i % N];
+      shift[i] = fmaf(-base[i % N], scale[i], a.beta ? a.beta[ch + i] : 0.f);
+    }
+#pragma unroll
+    for (int i = 0; i < N; ++i) base[i] = -base[i] * rstd[i];
+  }
+};
+
+template <typename S, int V, int ACT>
 __global__ __launch_bounds__(kThreads) void norm_write_kernel(const NormArgs a) {
   const S* X = reinterpret_cast<const S*>(a.X);
   S* Y = reinterpret_cast<S*>(a.Y);
-  each_part(a, blockIdx.x, [&](int32_t b, int64_t r0, int64_t r1) {
+  // (last chunk first: what was read last is still in the caches)
+  each_part(a, a.chunks - 1 - blockIdx.x, [&](int32_t b, int64_t r0, int64_t r1) {
     const bool none = b < 0 || b >= a.segments;
     for (int vec0 = 0; vec0 * V < a.C; vec0 += kThreads) {
       const Lay l = lay<V>(a, vec0);
       if (l.ty >= l.rows) continue;
       const int ch = (vec0 + l.tx) * V;
-      float mean[V], scale[V], beta[V];
-#pragma unroll
-      for (int i = 0; i < V; ++i) {
-        const int64_t g = none ? 0 : (int64_t)b * a.groups + (ch + i) / a.D;
-        mean[i] = none ? 0.f : a.mean[g];
-        scale[i] = (none ? 0.f : a.rstd[g]) * (a.gamma ? a.gamma[ch + i] : 1.f);
-        beta[i] = a.beta ? a.beta[ch + i] : 0.f;
+      if (none) {
+        for (int64_t r = r0 + l.ty; r < r1; r += l.rows) store_zeros<S, V>(Y + r * a.ldy + ch);
+        continue;
       }
-      for (int64_t r = r0 + l.ty; r < r1; r += l.rows) {
-        float x[V];
-        load<S, V>(X + r * a.ldx + ch, x);
+      Channel<V, V> k;
+      k.read(a, b, ch);
+      each_row<4>(r0 + l.ty, r1, l.rows, [&](int64_t r) { return fetch<S, V>(X + r * a.ldx + ch); }, [&](int64_t r, const Whole<S, V>& w) {
+        float y[V];
 #pragma unroll
-        for (int i = 0; i < V; ++i) x[i] = none ? 0.f : act_value((x[i] - mean[i]) * scale[i] + beta[i], a.act);
-        store<S, V>(Y + r * a.ldy + ch, x);
-      }
+        for (int i = 0; i < V; ++i) y[i] = act_value<ACT>(fmaf((float)w.x[i], k.scale[i], k.shift[i]));
+        store<S, V>(Y + r * a.ldy + ch, y);
+      });
     }
   });
 }
 
-// What a channel's values need backward
-template <int V>
-struct Channel {
-  float mean[V], rstd[V], gamma[V], beta[V];
-  __device__ __forceinline__ void read(const NormArgs& a, int32_t b, int ch) {
-#pragma unroll
-    for (int i = 0; i < V; ++i) {
-      const int64_t g = (int64_t)b * a.groups + (ch + i) / a.D;
-      mean[i] = a.mean[g];
-      rstd[i] = a.rstd[g];
-      gamma[i] = a.gamma ? a.gamma[ch + i] : 1.f;
-      beta[i] = a.beta ? a.beta[ch + i] : 0.f;
-    }
-  }
-};
-
-template <typename S, int V>
+template <typename S, int V, int ACT>
 __global__ __launch_bounds__(kThreads) void norm_bwd_sum_kernel(const NormArgs a) {
   extern __shared__ __attribute__((aligned(16))) char smem[];
   double2* acc = reinterpret_cast<double2*>(smem);
@@ -296,24 +355,22 @@ __global__ __launch_bounds__(kThreads) void norm_bwd_sum_kernel(const NormArgs a
 #pragma unroll
       for (int i = 0; i < V; ++i) p[i] = q[i] = 0.f;
       if (l.ty < l.rows) {
-        Channel<V> k;
+        Channel<V, V> k;
         k.read(a, b, ch);
-        for (int64_t r = r0 + l.ty; r < r1; r += l.rows) {
-          float x[V], h[V];
-          load<S, V>(X + r * a.ldx + ch, x);
-          load<S, V>(G + r * a.ldg + ch, h);
+        each_row<2>(r0 + l.ty, r1, l.rows, [&](int64_t r) { return Two<S, V>{fetch<S, V>(X + r * a.ldx + ch), fetch<S, V>(G + r * a.ldg + ch)}; },
+                    [&](int64_t, const Two<S, V>& w) {
 #pragma unroll
           for (int i = 0; i < V; ++i) {
-            const float xh = (x[i] - k.mean[i]) * k.rstd[i];
-            h[i] *= act_slope(xh * k.gamma[i] + k.beta[i], a.act);
-            p[i] += h[i];
-            q[i] += h[i] * xh;
+            const float x = (float)w.a.x[i], h = act_gradient<ACT>((float)w.b.x[i], fmaf(x, k.scale[i], k.shift[i]));
+            p[i] += h;
+            q[i] = fmaf(h, fmaf(x, k.rstd[i], k.base[i]), q[i]);
           }
-        }
+        });
 #pragma unroll
         for (int i = 0; i < V; ++i) {
-          dp[i] = (double)p[i] * k.gamma[i];
-          dq[i] = (double)q[i] * k.gamma[i];
+          const float gamma = a.gamma ? a.gamma[ch + i] : 1.f;
+          dp[i] = (double)p[i] * gamma;
+          dq[i] = (double)q[i] * gamma;
         }
       }
       to_groups<V>(a, l, vec0 * V, dp, dq, sm, acc);
@@ -348,33 +405,41 @@ __global__ __launch_bounds__(kThreads) void norm_bwd_sum_kernel(const NormArgs a
     for (int x = threadIdx.x; x < a.C; x += kThreads) a.rows[c * a.C + x] = make_float2(0.f, 0.f);
 }
 
-// Workgroups below `wide`: 64 channels of gamma and beta each, a row of the table for each wavefront in turn; the others:
-// a segment and group for each wavefront.
-__global__ __launch_bounds__(kThreads) void norm_bwd_join_kernel(const NormArgs a, int32_t wide) {
+// Workgroups below `wide`: sixteen channels of gamma and beta each, 64 rows of the table at a time; the others: a segment and group
+// for each wavefront.  (With a row of 64 channels for each of four wavefronts 1037 rows took 67 us.)
+constexpr int kJoinThreads = 1024;
+__global__ __launch_bounds__(kJoinThreads) void norm_bwd_join_kernel(const NormArgs a, int32_t wide) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   if ((int)blockIdx.x < wide) {
-    __shared__ double2 sm[kThreads];
-    const int ch = (int)blockIdx.x * 64 + lane;
+    __shared__ double2 sm[kJoinThreads / 64][16];
+    const int ch = (int)blockIdx.x * 16 + (threadIdx.x & 15);
     double2 s = make_double2(0., 0.);
-    if (ch < a.C)
-      for (int64_t c = wave; c < a.chunks; c += kThreads / 64) {
-        const float2 p = a.rows[c * a.C + ch];
-        s.x += p.x;
-        s.y += p.y;
+    if (ch < a.C) {
+      const float2* p = a.rows + ch;
+#pragma unroll 8
+      for (int64_t c = threadIdx.x >> 4; c < a.table; c += kJoinThreads / 16) {
+        const float2 v = p[c * a.C];
+        s.x += v.x;
+        s.y += v.y;
       }
-    sm[threadIdx.x] = s;
+    }
+    for (int d = 16; d < 64; d *= 2) {
+      s.x += __shfl_xor(s.x, d);
+      s.y += __shfl_xor(s.y, d);
+    }
+    if (lane < 16) sm[wave][lane] = s;
     __syncthreads();
-    if (wave == 0 && ch < a.C) {
-      for (int w = 1; w < kThreads / 64; ++w) {
-        s.x += sm[w * 64 + lane].x;
-        s.y += sm[w * 64 + lane].y;
+    if (threadIdx.x < 16 && ch < a.C) {
+      for (int w = 1; w < kJoinThreads / 64; ++w) {
+        s.x += sm[w][lane].x;
+        s.y += sm[w][lane].y;
       }
       if (a.dgamma) a.dgamma[ch] = (float)s.x;
       if (a.dbeta) a.dbeta[ch] = (float)s.y;
     }
     return;
   }
-  const int64_t at = (int64_t)(blockIdx.x - wide) * (kThreads / 64) + wave;
+  const int64_t at = (int64_t)(blockIdx.x - wide) * (kJoinThreads / 64) + wave;
   if (at >= (int64_t)a.segments * a.groups) return;
   const int32_t b = (int32_t)(at / a.groups), g = (int32_t)(at % a.groups);
   const int64_t lo = seg_row(a, b), hi = seg_row(a, b + 1);
@@ -383,43 +448,325 @@ __global__ __launch_bounds__(kThreads) void norm_bwd_join_kernel(const NormArgs 
   if (lane == 0) a.sums[at] = make_float2((float)(s.x / n), (float)(s.y / n));
 }
 
-template <typename S, int V>
+// dx = h gamma rstd - rstd s1 - rstd s2 (rstd x + base) = h scale + tilt x + level, s1 and s2 the means of the group's sums
+__device__ __forceinline__ void input_line(float rstd, float base, float2 s, float& tilt, float& level) {
+  tilt = -rstd * s.y * rstd;
+  level = -rstd * fmaf(s.y, base, s.x);
+}
+
+template <typename S, int V, int ACT>
 __global__ __launch_bounds__(kThreads) void norm_bwd_write_kernel(const NormArgs a) {
   const S* X = reinterpret_cast<const S*>(a.X);
   const S* G = reinterpret_cast<const S*>(a.G);
   S* Y = reinterpret_cast<S*>(a.Y);
-  each_part(a, blockIdx.x, [&](int32_t b, int64_t r0, int64_t r1) {
+  // (last chunk first: what was read last is still in the caches)
+  each_part(a, a.chunks - 1 - blockIdx.x, [&](int32_t b, int64_t r0, int64_t r1) {
     const bool none = b < 0 || b >= a.segments;
     for (int vec0 = 0; vec0 * V < a.C; vec0 += kThreads) {
       const Lay l = lay<V>(a, vec0);
       if (l.ty >= l.rows) continue;
       const int ch = (vec0 + l.tx) * V;
-      Channel<V> k;
-      float2 s[V];
-      if (!none) {
-        k.read(a, b, ch);
-#pragma unroll
-        for (int i = 0; i < V; ++i) s[i] = a.sums[(int64_t)b * a.groups + (ch + i) / a.D];
+      if (none) {
+        for (int64_t r = r0 + l.ty; r < r1; r += l.rows) store_zeros<S, V>(Y + r * a.ldy + ch);
+        continue;
       }
-      for (int64_t r = r0 + l.ty; r < r1; r += l.rows) {
-        float x[V], h[V];
-        if (none) {
+      Channel<V, V> k;
+      k.read(a, b, ch);
+      float tilt[V], level[V];
 #pragma unroll
-          for (int i = 0; i < V; ++i) x[i] = 0.f;
-        } else {
-          load<S, V>(X + r * a.ldx + ch, x);
-          load<S, V>(G + r * a.ldg + ch, h);
+      for (int i = 0; i < V; ++i) input_line(k.rstd[i], k.base[i], a.sums[(int64_t)b * a.groups + (ch + i) / a.D], tilt[i], level[i]);
+      each_row<2>(r0 + l.ty, r1, l.rows, [&](int64_t r) { return Two<S, V>{fetch<S, V>(X + r * a.ldx + ch), fetch<S, V>(G + r * a.ldg + ch)}; },
+                  [&](int64_t r, const Two<S, V>& w) {
+        float y[V];
 #pragma unroll
-          for (int i = 0; i < V; ++i) {
-            const float xh = (x[i] - k.mean[i]) * k.rstd[i];
-            h[i] *= act_slope(xh * k.gamma[i] + k.beta[i], a.act);
-            x[i] = (h[i] * k.gamma[i] - s[i].x - xh * s[i].y) * k.rstd[i];
-          }
+        for (int i = 0; i < V; ++i) {
+          const float x = (float)w.a.x[i], h = act_gradient<ACT>((float)w.b.x[i], fmaf(x, k.scale[i], k.shift[i]));
+          y[i] = fmaf(h, k.scale[i], fmaf(x, tilt[i], level[i]));
         }
-        store<S, V>(Y + r * a.ldy + ch, x);
-      }
+        store<S, V>(Y + r * a.ldy + ch, y);
+      });
     }
   });
+}
+
+// ------------------------------------------------------------------------------------------
+// Whole segments: a workgroup (of 64, 256 or 512 threads) has a slab of channels, whole groups and whole vectors, of one
+// segment after the other.  A thread keeps up to kKept vectors in registers between the sum and the write; what a
+// segment has beyond that (it is longer than the caller said) is read again.
+constexpr int kMostTeam = 512, kKept = 8;
+// Backward two operands are kept, as vectors of 8 bytes: half the registers for what goes with a channel.  128 registers are
+// sixteen wavefronts on a CU (as vectors of 16 bytes with twice the registers, eight wavefronts: subgraphs of 250 x 256 710 us).
+constexpr int kKeptBackward = 13;
+constexpr int64_t kWholeLd = 1 << 16;      // (what a workgroup keeps lies within 2^31 bytes)
+
+struct Team { int tx, ty, per_row, rows, c0, width, vec; };
+template <int V>
+__device__ __forceinline__ Team team(const NormArgs& a, int slab) {
+  Team t;
+  t.c0 = slab * a.slab;
+  t.width = a.C - t.c0 < a.slab ? a.C - t.c0 : a.slab;
+  t.per_row = t.width / V;
+  t.rows = (int)blockDim.x / t.per_row;
+  t.ty = (int)threadIdx.x / t.per_row;
+  t.tx = (int)threadIdx.x % t.per_row;
+  return t;
+}
+
+// Sums p[], q[] per thread and channel (N = 1: and vector) -> out[group of the slab], for all threads to read.
+template <int V, int N>
+__device__ __forceinline__ void team_groups(const NormArgs& a, const Team& t, const double (&p)[N], const double (&q)[N], double2* sm, double2* out) {
+  const int lane = threadIdx.x & 63, waves = blockDim.x >> 6, groups = t.width / a.D;
+  __syncthreads();                                          // (the last segment's sums have been read)
+  if constexpr (N == 1) {                                   // a vector lies in one group
+    if (t.ty < t.rows) sm[t.tx * t.rows + t.ty] = make_double2(p[0], q[0]);
+    __syncthreads();
+    const int each = t.rows * (a.D / V);                    // (a group's sums lie one behind the other)
+    // as many lanes to a group as there are; a power of two, so that they join by shuffles
+    int lanes = 64;
+    while (lanes > 1 && (int)blockDim.x / lanes < groups) lanes /= 2;
+    for (int g0 = 0; g0 < groups; g0 += (int)blockDim.x / lanes) {
+      const int g = g0 + (int)threadIdx.x / lanes;
+      double2 v = make_double2(0., 0.);
+      if (g < groups)
+        for (int i = (int)threadIdx.x % lanes; i < each; i += lanes) {
+          v.x += sm[g * each + i].x;
+          v.y += sm[g * each + i].y;
+        }
+      for (int d = lanes / 2; d; d /= 2) {
+        v.x += __shfl_xor(v.x, d);
+        v.y += __shfl_xor(v.y, d);
+      }
+      if (g < groups && threadIdx.x % lanes == 0) out[g] = v;
+    }
+  } else {
+    if (t.ty < t.rows)
+#pragma unroll
+      for (int i = 0; i < V; ++i) sm[t.ty * t.width + t.tx * V + i] = make_double2(p[i], q[i]);
+    __syncthreads();
+    for (int g = threadIdx.x >> 6; g < groups; g += waves) {
+      double2 v = make_double2(0., 0.);
+      for (int i = lane; i < t.rows * a.D; i += 64) {
+        const double2 x = sm[i / a.D * t.width + g * a.D + i % a.D];
+        v.x += x.x;
+        v.y += x.y;
+      }
+      for (int d = 32; d; d /= 2) {
+        v.x += __shfl_xor(v.x, d);
+        v.y += __shfl_xor(v.y, d);
+      }
+      if (lane == 0) out[g] = v;
+    }
+  }
+  __syncthreads();
+}
+
+// Rows behind the last segment: zeros, by the workgroups beyond the segments'
+template <typename S, int V>
+__device__ __forceinline__ void team_zeros(const NormArgs& a, const Team& t, int64_t at, int64_t of) {
+  const int64_t rest = seg_row(a, a.segments);
+  S* Y = reinterpret_cast<S*>(a.Y) + t.c0 + t.tx * V;
+  if (t.ty < t.rows)
+    for (int64_t r = rest + at * t.rows + t.ty; r < a.m; r += of * t.rows) store_zeros<S, V>(Y + r * a.ldy);
+}
+
+// V values at a uniform row's address and a lane's bytes from it
+template <typename S, int V>
+__device__ __forceinline__ Whole<S, V> fetch_at(const void* row, uint32_t lane) {
+  return fetch<S, V>(reinterpret_cast<const S*>(reinterpret_cast<const char*>(row) + lane));
+}
+
+template <typename S, int V, int N, int ACT>
+__global__ __launch_bounds__(kMostTeam) void norm_whole_kernel(const NormArgs a, int32_t slabs) {
+  extern __shared__ __attribute__((aligned(16))) char smem[];
+  const Team t = team<V>(a, (int)(blockIdx.x % slabs));
+  const int64_t b = blockIdx.x / slabs, blocks = gridDim.x / slabs;
+  if (b >= a.segments) {
+    team_zeros<S, V>(a, t, b - a.segments, blocks - a.segments);
+    return;
+  }
+  double2* sums = reinterpret_cast<double2*>(smem);
+  double2* sm = sums + a.slab / a.D;
+  const int64_t lo = seg_row(a, b), hi = seg_row(a, b + 1);
+  const int ch = t.c0 + t.tx * V;
+  // rows lo + ty + n * t.rows: a lane's part of the address does not change
+  const uint32_t vx = (uint32_t)((t.ty * a.ldx + ch) * sizeof(S)), vy = (uint32_t)((t.ty * a.ldy + ch) * sizeof(S));
+  auto x_row = [&](int64_t n) { return reinterpret_cast<const S*>(a.X) + (lo + n * t.rows) * a.ldx; };
+  auto y_row = [&](int64_t n) { return reinterpret_cast<char*>(reinterpret_cast<S*>(a.Y) + (lo + n * t.rows) * a.ldy); };
+  const int64_t mine = t.ty < t.rows && hi - lo > t.ty ? (hi - lo - t.ty + t.rows - 1) / t.rows : 0;
+  const int there = mine < kKept ? (int)mine : kKept;
+  Whole<S, V> kept[kKept];
+  if (hi > lo) {                                            // (what is not there is a row that is: no branches)
+    const uint32_t step = (uint32_t)(t.rows * a.ldx * sizeof(S)), at = mine ? vx : (uint32_t)(ch * sizeof(S));
+#pragma unroll
+    for (int n = 0; n < kKept; ++n) kept[n] = fetch_at<S, V>(x_row(0), at + (n < there ? n * step : 0));
+  }
+  double p[N], q[N];
+#pragma unroll
+  for (int i = 0; i < N; ++i) p[i] = q[i] = 0.;
+  auto add = [&](const Whole<S, V>& w) {
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+      const double d = (float)w.x[i];
+      p[i % N] += d;
+      q[i % N] = fma(d, d, q[i % N]);
+    }
+  };
+#pragma unroll
+  for (int n = 0; n < kKept; ++n) {
+    keep(kept[n]);
+    if (n < there) add(kept[n]);
+  }
+  for (int64_t n = kKept; n < mine; ++n) add(fetch_at<S, V>(x_row(n), vx));
+  team_groups<V, N>(a, t, p, q, sm, sums);
+  const double n_values = hi > lo ? (double)(hi - lo) * a.D : 1.;
+  for (int g = threadIdx.x; g < t.width / a.D; g += blockDim.x) {
+    const double mean = sums[g].x / n_values, var = sums[g].y / n_values - mean * mean;
+    const float m = (float)mean, r = (float)(1. / sqrt((var < 0. ? 0. : var) + a.eps));
+    const int64_t at = b * a.groups + t.c0 / a.D + g;
+    a.mean[at] = m;
+    a.rstd[at] = r;
+    sums[g] = make_double2(m, r);
+  }
+  __syncthreads();
+  if (mine == 0) return;
+  Channel<V, N> k;
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    const double2 s = sums[(t.tx * V + i) / a.D];
+    k.base[i] = (float)s.x;
+    k.rstd[i] = (float)s.y;
+  }
+  k.affine(a, ch);
+  auto put = [&](int64_t n, const Whole<S, V>& w) {
+    float y[V];
+#pragma unroll
+    for (int i = 0; i < V; ++i) y[i] = act_value<ACT>(fmaf((float)w.x[i], k.scale[i], k.shift[i]));
+    store<S, V>(reinterpret_cast<S*>(y_row(n) + vy), y);
+  };
+#pragma unroll
+  for (int n = 0; n < kKept; ++n) {
+    keep(kept[n]);
+    if (n < there) put(n, kept[n]);
+  }
+  for (int64_t n = kKept; n < mine; ++n) put(n, fetch_at<S, V>(x_row(n), vx));
+}
+
+// Backward: workgroups take segments in turn and keep gamma's and beta's sums until their last one.
+template <typename S, int V, int N, int ACT>
+__global__ __launch_bounds__(kMostTeam, 4) void norm_bwd_whole_kernel(const NormArgs a, int32_t slabs) {
+  extern __shared__ __attribute__((aligned(16))) char smem[];
+  // (a vector of several groups has their means and sums beside it)
+  // g act'(z) takes g's place where that loses nothing: in fp32, and where it is g or 0
+  constexpr bool kExact = sizeof(S) == 4 || ACT != SAGNN_ACT_SILU;
+  constexpr int K = N == 1 ? kKeptBackward : kKeptBackward / 2;
+  const Team t = team<V>(a, (int)(blockIdx.x % slabs));
+  const int64_t stripe = blockIdx.x / slabs, stripes = gridDim.x / slabs;
+  double2* sums = reinterpret_cast<double2*>(smem);
+  double2* sm = sums + a.slab / a.D;
+  float2* all = reinterpret_cast<float2*>(sm + blockDim.x * N) + threadIdx.x;     // this thread's, V of them
+#pragma unroll
+  for (int i = 0; i < V; ++i) all[i * blockDim.x] = make_float2(0.f, 0.f);
+  const int ch = t.c0 + t.tx * V;
+  const uint32_t vx = (uint32_t)((t.ty * a.ldx + ch) * sizeof(S)), vg = (uint32_t)((t.ty * a.ldg + ch) * sizeof(S)),
+                 vy = (uint32_t)((t.ty * a.ldy + ch) * sizeof(S));
+  for (int64_t b = stripe; b < a.segments; b += stripes) {
+    const int64_t lo = seg_row(a, b), hi = seg_row(a, b + 1);
+    auto x_row = [&](int64_t n) { return reinterpret_cast<const S*>(a.X) + (lo + n * t.rows) * a.ldx; };
+    auto g_row = [&](int64_t n) { return reinterpret_cast<const S*>(a.G) + (lo + n * t.rows) * a.ldg; };
+    auto y_row = [&](int64_t n) { return reinterpret_cast<char*>(reinterpret_cast<S*>(a.Y) + (lo + n * t.rows) * a.ldy); };
+    const int64_t mine = t.ty < t.rows && hi - lo > t.ty ? (hi - lo - t.ty + t.rows - 1) / t.rows : 0;
+    const int there = mine < K ? (int)mine : K;
+    Whole<S, V> x[K], h[K];
+    if (hi > lo) {
+      const uint32_t step_x = (uint32_t)(t.rows * a.ldx * sizeof(S)), step_g = (uint32_t)(t.rows * a.ldg * sizeof(S)),
+                     at_x = mine ? vx : (uint32_t)(ch * sizeof(S)), at_g = mine ? vg : (uint32_t)(ch * sizeof(S));
+#pragma unroll
+      for (int n = 0; n < K; ++n) {
+        x[n] = fetch_at<S, V>(x_row(0), at_x + (n < there ? n * step_x : 0));
+        h[n] = fetch_at<S, V>(g_row(0), at_g + (n < there ? n * step_g : 0));
+        __builtin_amdgcn_sched_barrier(0);                  // (addresses one after the other)
+      }
+    }
+    Channel<V, N> k;
+    k.read(a, (int32_t)b, ch);
+    double dp[N], dq[N];
+#pragma unroll
+    for (int i = 0; i < N; ++i) dp[i] = dq[i] = 0.;
+    {
+      float p[V], q[V];
+#pragma unroll
+      for (int i = 0; i < V; ++i) p[i] = q[i] = 0.f;
+      auto add = [&](const Whole<S, V>& w, Whole<S, V>& g) {
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+          const float v = (float)w.x[i], y = act_gradient<ACT>((float)g.x[i], fmaf(v, k.scale[i], k.shift[i]));
+          p[i] += y;
+          q[i] = fmaf(y, fmaf(v, k.rstd[i % N], k.base[i % N]), q[i]);
+          if (kExact) g.x[i] = (S)y;
+        }
+      };
+#pragma unroll
+      for (int n = 0; n < K; ++n) {
+        keep(x[n]);
+        keep(h[n]);
+        if (n < there) add(x[n], h[n]);
+        __builtin_amdgcn_sched_barrier(0);                 // (one vector's temporaries at a time)
+      }
+      for (int64_t n = K; n < mine; ++n) {
+        Whole<S, V> g = fetch_at<S, V>(g_row(n), vg);
+        add(fetch_at<S, V>(x_row(n), vx), g);
+      }
+#pragma unroll
+      for (int i = 0; i < V; ++i) {
+        float2 s = all[i * blockDim.x];
+        s.x += q[i];
+        s.y += p[i];
+        all[i * blockDim.x] = s;
+        const float gamma = a.gamma ? a.gamma[ch + i] : 1.f;
+        dp[i % N] += (double)p[i] * gamma;
+        dq[i % N] += (double)q[i] * gamma;
+      }
+    }
+    team_groups<V, N>(a, t, dp, dq, sm, sums);
+    const double n_values = hi > lo ? 1. / ((double)(hi - lo) * a.D) : 1.;
+    if (mine == 0) continue;
+    float tilt[N], level[N];
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const double2 v = sums[(t.tx * V + i) / a.D];
+      input_line(k.rstd[i], k.base[i], make_float2((float)(v.x * n_values), (float)(v.y * n_values)), tilt[i], level[i]);
+    }
+    auto put = [&](int64_t n, const Whole<S, V>& w, const Whole<S, V>& g, bool done) {
+      float y[V];
+#pragma unroll
+      for (int i = 0; i < V; ++i) {
+        const float v = (float)w.x[i], d = done ? (float)g.x[i] : act_gradient<ACT>((float)g.x[i], fmaf(v, k.scale[i], k.shift[i]));
+        y[i] = fmaf(d, k.scale[i], fmaf(v, tilt[i % N], level[i % N]));
+      }
+      store<S, V>(reinterpret_cast<S*>(y_row(n) + vy), y);
+    };
+#pragma unroll
+    for (int n = 0; n < K; ++n) {
+      keep(x[n]);
+      keep(h[n]);
+      if (n < there) put(n, x[n], h[n], kExact);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    for (int64_t n = K; n < mine; ++n) put(n, fetch_at<S, V>(x_row(n), vx), fetch_at<S, V>(g_row(n), vg), false);
+  }
+  team_zeros<S, V>(a, t, stripe, stripes);
+  // this workgroup's row of the table of gamma's and beta's sums
+  __syncthreads();
+  const float2* of = reinterpret_cast<const float2*>(sm + blockDim.x * N);
+  for (int c = threadIdx.x; c < t.width; c += blockDim.x) {
+    float2 s = make_float2(0.f, 0.f);
+    for (int y = 0; y < t.rows; ++y) {
+      const float2 v = of[(c % V) * blockDim.x + y * t.per_row + c / V];
+      s.x += v.x;
+      s.y += v.y;
+    }
+    a.rows[stripe * a.C + t.c0 + c] = s;
+  }
 }
 
 // Values that a thread takes at a time: what 16 bytes hold, and a divisor of the width
@@ -430,6 +777,7 @@ int vector_of(int32_t dtype, int32_t C) {
 }
 
 struct NormPlan { int64_t chunk, chunks; size_t parts, sums, rows, total; };
+constexpr int kMostStripes = 2048;
 NormPlan norm_plan(int64_t m, int32_t segments, int32_t C, int32_t groups) {
   NormPlan p{};
   // 2048 workgroups fill the chip; a chunk has eight rows of 256 threads or more
@@ -442,11 +790,45 @@ NormPlan norm_plan(int64_t m, int32_t segments, int32_t C, int32_t groups) {
   auto take = [&](size_t bytes) { const size_t o = off; off += round_up(bytes, 256); return o; };
   p.parts = take((size_t)(p.chunks + segments) * groups * sizeof(double2));
   p.sums = take((size_t)segments * groups * sizeof(float2));
-  p.rows = take((size_t)p.chunks * C * sizeof(float2));
+  p.rows = take((size_t)(segments < kMostStripes && segments > p.chunks ? segments : p.chunks > kMostStripes || segments < kMostStripes ? p.chunks : kMostStripes) *
+                C * sizeof(float2));
   p.total = off;
   return p;
 }
 
+// Whole segments: channels of a workgroup (0: not that way), workgroups beside one another, threads
+struct WholePlan { int32_t slab, slabs, threads; };
+WholePlan whole_plan(int64_t m, int64_t max_rows, int32_t C, int32_t D, int v, int size, int kept) {
+  WholePlan w{};
+  int64_t rows = max_rows > 0 && max_rows < m ? max_rows : m;
+  if (rows < 1) rows = 1;
+  int32_t unit = D;                                         // whole groups and whole vectors
+  while (unit % v) unit += D;
+  const int64_t most = (int64_t)kMostTeam * kept;          // vectors that a workgroup keeps
+  int64_t units = most / (rows * (unit / v));
+  if (unit / v > kMostTeam || units < 1) return w;
+  if (units > kMostTeam / (unit / v)) units = kMostTeam / (unit / v);
+  const int64_t all = ceil_div(C, unit);
+  if (units > all) units = all;
+  units = ceil_div(all, ceil_div(all, units));              // slabs of like width
+  // less than a cache line of a row for each workgroup reads lines twice
+  if (units < all && units * unit * size < 128) return w;
+  w.slab = (int32_t)(units * unit);
+  w.slabs = (int32_t)ceil_div(C, w.slab);
+  const int64_t vectors = rows * (w.slab / v);
+  w.threads = vectors <= 64 * 4 && w.slab / v <= 64 ? 64 : vectors <= 256 * 4 && w.slab / v <= 256 ? 256 : kMostTeam;
+  return w;
+}
+size_t whole_lds(const WholePlan& w, int32_t D, int v, bool backward) {
+  return ((size_t)(w.slab / D) + (size_t)w.threads * (D % v == 0 ? 1 : v)) * sizeof(double2) + (backward ? (size_t)w.threads * v * sizeof(float2) : 0);
+}
+
+template <typename F>
+int by_act(int32_t act, F f) {
+  if (act == SAGNN_ACT_RELU) return f(std::integral_constant<int, SAGNN_ACT_RELU>{});
+  if (act == SAGNN_ACT_SILU) return f(std::integral_constant<int, SAGNN_ACT_SILU>{});
+  return f(std::integral_constant<int, SAGNN_ACT_IDENTITY>{});
+}
 template <typename F>
 int by_vector(int32_t dtype, int v, F f) {
   if (dtype == SAGNN_BF16) {
@@ -496,9 +878,20 @@ SAGNN_EXPORT int group_norm_act_fwd(int32_t dtype, const void* d_X, int64_t ldx,
   a.D = C / n_groups; a.gamma = d_gamma; a.beta = d_beta; a.mean = d_mean; a.rstd = d_rstd; a.eps = eps; a.act = act;
   a.chunk = p.chunk; a.chunks = p.chunks; a.parts = (double2*)((char*)d_ws + p.parts);
   hipStream_t s = (hipStream_t)stream;
-  return by_vector(dtype, vector_of(dtype, C), [&](auto V, auto zero) {
-    constexpr int v = decltype(V)::value;
+  return by_act(act, [&](auto A) { return by_vector(dtype, vector_of(dtype, C), [&](auto V, auto zero) {
+    constexpr int v = decltype(V)::value, ACT = decltype(A)::value;
     using S = decltype(zero);
+    const WholePlan w = whole_plan(m, max_rows, C, a.D, v, sizeof(S), kKept);
+    if (w.slab && m > 0 && ldx <= kWholeLd && ldy <= kWholeLd) {
+      a.slab = w.slab;
+      const int64_t blocks = ((int64_t)n_seg + (d_seg ? 16 : 0)) * w.slabs;       // (rows behind the last segment)
+      if (blocks <= INT32_MAX) {
+        if (a.D % v == 0) norm_whole_kernel<S, v, 1, ACT><<<dim3((uint32_t)blocks), (uint32_t)w.threads, whole_lds(w, a.D, v, false), s>>>(a, w.slabs);
+        else norm_whole_kernel<S, v, v, ACT><<<dim3((uint32_t)blocks), (uint32_t)w.threads, whole_lds(w, a.D, v, false), s>>>(a, w.slabs);
+        SAGNN_LAUNCH_CHECK();
+        return (int)SAGNN_OK;
+      }
+    }
     if (m > 0) {
       norm_sum_kernel<S, v><<<dim3((uint32_t)p.chunks), kThreads, (size_t)n_groups * 16 + kThreads * v * 16, s>>>(a);
       SAGNN_LAUNCH_CHECK();
@@ -506,11 +899,11 @@ SAGNN_EXPORT int group_norm_act_fwd(int32_t dtype, const void* d_X, int64_t ldx,
     norm_join_kernel<<<dim3((uint32_t)ceil_div((int64_t)n_seg * n_groups, kThreads / 64)), kThreads, 0, s>>>(a);
     SAGNN_LAUNCH_CHECK();
     if (m > 0) {
-      norm_write_kernel<S, v><<<dim3((uint32_t)p.chunks), kThreads, 0, s>>>(a);
+      norm_write_kernel<S, v, ACT><<<dim3((uint32_t)p.chunks), kThreads, 0, s>>>(a);
       SAGNN_LAUNCH_CHECK();
     }
     return (int)SAGNN_OK;
-  });
+  }); });
 }
 
 SAGNN_EXPORT int group_norm_act_bwd(int32_t dtype, const void* d_X, int64_t ldx, const void* d_G, int64_t ldg, const int32_t* d_seg,
@@ -532,22 +925,36 @@ SAGNN_EXPORT int group_norm_act_bwd(int32_t dtype, const void* d_X, int64_t ldx,
   a.C = C; a.groups = n_groups; a.D = C / n_groups; a.gamma = d_gamma; a.beta = d_beta; a.mean = const_cast<float*>(d_mean);
   a.rstd = const_cast<float*>(d_rstd); a.act = act; a.dgamma = d_dgamma; a.dbeta = d_dbeta; a.chunk = p.chunk; a.chunks = p.chunks;
   a.parts = (double2*)((char*)d_ws + p.parts); a.sums = (float2*)((char*)d_ws + p.sums); a.rows = (float2*)((char*)d_ws + p.rows);
-  if (m == 0) a.chunks = 0;
+  a.table = m > 0 ? p.chunks : 0;
   hipStream_t s = (hipStream_t)stream;
-  return by_vector(dtype, vector_of(dtype, C), [&](auto V, auto zero) {
-    constexpr int v = decltype(V)::value;
+  return by_act(act, [&](auto A) { return by_vector(dtype, vector_of(dtype, C), [&](auto V, auto zero) {
+    constexpr int v = decltype(V)::value, ACT = decltype(A)::value;
     using S = decltype(zero);
+    const int32_t wide = (int32_t)ceil_div(C, 16);
+    constexpr int u = v * sizeof(S) > 8 ? v / 2 : v;
+    const WholePlan w = whole_plan(m, max_rows, C, a.D, u, sizeof(S), a.D % u == 0 ? kKeptBackward : kKeptBackward / 2);
+    if (w.slab && m > 0 && ldx <= kWholeLd && ldg <= kWholeLd && lddx <= kWholeLd) {
+      a.slab = w.slab;
+      a.table = n_seg < kMostStripes ? n_seg : kMostStripes;
+      const size_t lds = whole_lds(w, a.D, u, true);
+      const dim3 grid((uint32_t)(a.table * w.slabs));
+      if (a.D % u == 0) norm_bwd_whole_kernel<S, u, 1, ACT><<<grid, (uint32_t)w.threads, lds, s>>>(a, w.slabs);
+      else norm_bwd_whole_kernel<S, u, u, ACT><<<grid, (uint32_t)w.threads, lds, s>>>(a, w.slabs);
+      SAGNN_LAUNCH_CHECK();
+      norm_bwd_join_kernel<<<dim3((uint32_t)wide), kJoinThreads, 0, s>>>(a, wide);
+      SAGNN_LAUNCH_CHECK();
+      return (int)SAGNN_OK;
+    }
     if (m > 0) {
-      norm_bwd_sum_kernel<S, v><<<dim3((uint32_t)p.chunks), kThreads, (size_t)n_groups * 16 + kThreads * v * 16, s>>>(a);
+      norm_bwd_sum_kernel<S, v, ACT><<<dim3((uint32_t)p.chunks), kThreads, (size_t)n_groups * 16 + kThreads * v * 16, s>>>(a);
       SAGNN_LAUNCH_CHECK();
     }
-    const int32_t wide = (int32_t)ceil_div(C, 64);
-    norm_bwd_join_kernel<<<dim3((uint32_t)(wide + ceil_div((int64_t)n_seg * n_groups, kThreads / 64))), kThreads, 0, s>>>(a, wide);
+    norm_bwd_join_kernel<<<dim3((uint32_t)(wide + ceil_div((int64_t)n_seg * n_groups, kJoinThreads / 64))), kJoinThreads, 0, s>>>(a, wide);
     SAGNN_LAUNCH_CHECK();
     if (m > 0) {
-      norm_bwd_write_kernel<S, v><<<dim3((uint32_t)p.chunks), kThreads, 0, s>>>(a);
+      norm_bwd_write_kernel<S, v, ACT><<<dim3((uint32_t)p.chunks), kThreads, 0, s>>>(a);
       SAGNN_LAUNCH_CHECK();
     }
     return (int)SAGNN_OK;
-  });
+  }); });
 }
