@@ -22,7 +22,7 @@ SOURCES = ["api.hip", "pack.hip", "plan.hip", "spmm.hip", "spmm_flat.hip", "spmm
            "fused.hip", "permute.hip", "sweep_plan.hip", "tiles.hip", "grouped.hip", "grouped_fp32.hip", "grouped_fp32_bf16.hip",
            "grouped_fp32_bf16x3.hip", "grouped_bf16.hip", "group_norm.hip", "grad_norm.hip"]
 HEADERS = [os.path.join(CSRC, "common.h"), os.path.join(CSRC, "rowload.h"), os.path.join(CSRC, "gemm.h"),
-           os.path.join(CSRC, "gemm_nn.h"), os.path.join(CSRC, "grouped.h"), os.path.join(CSRC, "grouped_direct.h"), os.path.join(INCLUDE, "sagnn.h")]
+           os.path.join(CSRC, "gemm_nn.h"), os.path.join(CSRC, "grouped.h"), os.path.join(CSRC, "grouped_direct.h"), os.path.join(CSRC, "grouped_staged.h"), os.path.join(INCLUDE, "sagnn.h")]
 
 HIPCC_FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-fvisibility=hidden",

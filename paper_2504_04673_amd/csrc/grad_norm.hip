@@ -9,10 +9,11 @@ namespace sagnn {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kMaxBlocks = 2048;     // workgroups of a launch that sums, and the sums that it leaves
+constexpr int kMaxBlocks = 1024;     // workgroups of a launch that sums, and the sums that it leaves
 constexpr int kListed = 120;         // tensors that one launch takes: they travel as its arguments (4 KB at most)
-// Values that a workgroup takes at a time: so many that kMaxBlocks workgroups have one each, within these bounds (120
-// tensors, 10 M values: 16384 each 10 us to sum and 14 to scale, 4096 to 6144 ... see list_of)
+// Values that a workgroup takes at a time: so many that kMaxBlocks workgroups have one each, within these bounds.  (More
+// workgroups are more sums for each of them to join: 2 x 10 M values, 2048 workgroups 8.5 us to sum and 16.7 to scale, 1024 8.9 and
+// 14.7, 512 10.1 and 14.1; half a billion 188 and 361, 186 and 358, 212 and 352.)
 constexpr int kLeastPiece = 2048, kMostPiece = 16384;
 
 struct List {

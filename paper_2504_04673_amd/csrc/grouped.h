@@ -20,6 +20,7 @@ struct GroupedArgs {
   float* dW; float* partial;                     // weight gradient: groups x kdim x nout, sums of cut groups
   int64_t chunk;                                 // weight gradient: rows that one workgroup sums at most
   int32_t row_tiles, col_tiles;                  // of the launch
+  int32_t pairs;                                 // weight gradient: numbers of pairs of a chunk and a group
 };
 
 // Rows of group g as the kernels see them: whatever d_off holds, they lie inside [0, m).
@@ -96,14 +97,22 @@ __device__ __forceinline__ bool grouped_find(const GroupedArgs& a, GroupTile& fo
 // The weight gradient cuts the rows into chunks whatever the groups are; a workgroup sums one group's rows of one
 // chunk.  Walking along the rows, each such pair (chunk c, group g) is met at its own c + g, so that this number
 // names it; not every number does.  Rows [r0, r1) of the pair that p names; cut: the group has rows in other chunks.
+constexpr int32_t kManyPairs = 32;
 struct GroupPart { int32_t g; int64_t r0, r1; int32_t c; bool cut, first; };
 __device__ __forceinline__ bool grouped_part(const GroupedArgs& a, GroupPart& part, int32_t& tile) {
   const int lane = threadIdx.x & 63;
-  // Eight tiles or more: each XCD has a run of them, for every pair (the last pairs may not be there).
+  // Tiles of a pair read the same rows.  Many pairs: an XCD has all tiles of every eighth; few: a run of the tiles of each.
+  // (The last pairs may not be there, so that the XCDs share them in any case.)
   const int32_t tiles = a.row_tiles * a.col_tiles, id = (int32_t)blockIdx.x;
   int32_t p = id / tiles;
   tile = id % tiles;
-  if (tiles % 8 == 0) tile = xcd_run(tile, tiles);
+  if (a.pairs >= kManyPairs) {
+    p = id / 8 / tiles * 8 + id % 8;
+    tile = id / 8 % tiles;
+    if (p >= a.pairs) return false;
+  } else if (tiles % 8 == 0) {
+    tile = xcd_run(tile, tiles);
+  }
   int32_t count = 0;                              // groups that begin at numbers up to p
   for (int32_t g0 = 0; g0 < a.groups; g0 += 64) {
     const int32_t g = g0 + lane;
@@ -328,15 +337,35 @@ __device__ __forceinline__ void tile_product(const S* A, int64_t lda, int rows, 
 
 // f(row, column, sum) of the values that a lane holds, rows and columns relative to the workgroup's tile
 template <int WM, int WN, int TM, int TN, typename F>
-__device__ __forceinline__ void tile_each(const floatx16 (&acc)[TM][TN], F f) {
+__device__ __forceinline__ void tile_each(floatx16 (&acc)[TM][TN], F f) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
 #pragma unroll
   for (int tm = 0; tm < TM; ++tm)
 #pragma unroll
     for (int v = 0; v < 16; ++v)
 #pragma unroll
-      for (int tn = 0; tn < TN; ++tn)
-        f(((wave / WN) * TM + tm) * 32 + 8 * (v / 4) + 4 * (lane >> 5) + v % 4, ((wave % WN) * TN + tn) * 32 + (lane & 31), acc[tm][tn][v]);
+      for (int tn = 0; tn < TN; ++tn) {
+        float y = acc[tm][tn][v];
+        f(((wave / WN) * TM + tm) * 32 + 8 * (v / 4) + 4 * (lane >> 5) + v % 4, ((wave % WN) * TN + tn) * 32 + (lane & 31), y);
+        acc[tm][tn][v] = y;
+      }
+}
+
+// Results of a tile at row r0, column c0 -> Y, through activation and mask
+template <typename S, int WM, int WN, int TM, int TN>
+__device__ __forceinline__ void tile_store(const GroupedArgs& a, int64_t r0, int64_t c0, int rows, int cols, floatx16 (&acc)[TM][TN]) {
+  S* Y = reinterpret_cast<S*>(a.Y) + r0 * a.ldy + c0;
+  const bool relu = a.act == SAGNN_ACT_RELU;
+  if (a.mask) {                                 // (all loads ahead of the stores, which the compiler could not pass)
+    const S* mask = reinterpret_cast<const S*>(a.mask) + r0 * a.ldmask + c0;
+    tile_each<WM, WN, TM, TN>(acc, [&](int r, int c, float& y) {
+      const S z = mask[(int64_t)(r < rows ? r : rows - 1) * a.ldmask + (c < cols ? c : cols - 1)];
+      y = (float)z > 0.f ? y : 0.f;
+    });
+  }
+  tile_each<WM, WN, TM, TN>(acc, [&](int r, int c, float& y) {
+    if (r < rows && c < cols) Y[(int64_t)r * a.ldy + c] = (S)(relu && y < 0.f ? 0.f : y);
+  });
 }
 
 template <typename S, int PREC, bool WT, int WM, int WN, int TM, int TN, int BK>
@@ -352,15 +381,7 @@ __global__ __launch_bounds__(WM * WN * 64) void grouped_kernel(const GroupedArgs
   const S* W = reinterpret_cast<const S*>(a.W) + (t.g < a.groups ? t.g * a.stride_w : 0) + c0 * (WT ? a.ldw : 1);
   tile_product<S, PREC, false, !WT, WM, WN, TM, TN, BK>(reinterpret_cast<const S*>(a.X) + t.r0 * a.ldx, a.ldx, rows, W, a.ldw, cols,
                                                         t.g < a.groups ? a.kdim : 0, smem, acc);
-  S* Y = reinterpret_cast<S*>(a.Y) + t.r0 * a.ldy + c0;
-  const S* mask = a.mask ? reinterpret_cast<const S*>(a.mask) + t.r0 * a.ldmask + c0 : nullptr;
-  const bool relu = a.act == SAGNN_ACT_RELU;
-  tile_each<WM, WN, TM, TN>(acc, [&](int r, int c, float y) {
-    if (r >= rows || c >= cols) return;
-    if (relu && y < 0.f) y = 0.f;
-    if (mask && !((float)mask[(int64_t)r * a.ldmask + c] > 0.f)) y = 0.f;
-    Y[(int64_t)r * a.ldy + c] = (S)y;
-  });
+  tile_store<S, WM, WN, TM, TN>(a, t.r0, c0, rows, cols, acc);
 }
 
 template <typename S, int PREC, int WM, int WN, int TM, int TN, int BK>
@@ -376,15 +397,21 @@ __global__ __launch_bounds__(WM * WN * 64) void grouped_tn_kernel(const GroupedA
   tile_product<S, PREC, true, true, WM, WN, TM, TN, BK>(reinterpret_cast<const S*>(a.X) + p.r0 * a.ldx + k0, a.ldx, rows,
                                                         reinterpret_cast<const S*>(a.G) + p.r0 * a.ldg + c0, a.ldg, cols, p.r1 - p.r0, smem, acc);
   float* out = (p.cut ? a.partial + grouped_partial_slot(p) * a.kdim * a.nout : a.dW + (int64_t)p.g * a.kdim * a.nout) + k0 * a.nout + c0;
-  tile_each<WM, WN, TM, TN>(acc, [&](int r, int c, float y) {
+  tile_each<WM, WN, TM, TN>(acc, [&](int r, int c, float& y) {
     if (r < rows && c < cols) out[(int64_t)r * a.nout + c] = y;
   });
 }
 
-// Tiles that a launch can take: rows of X (of W for the weight gradient) by columns
-enum { kTile128 = 0, kTile64 = 1, kTile32x128 = 2, kDirect256 = 3 };
-inline int grouped_tile_rows(int tile) { return tile == kDirect256 ? 256 : tile == kTile128 ? 128 : (tile == kTile64 ? 64 : 32); }
-inline int grouped_tile_cols(int tile) { return tile == kDirect256 ? 256 : tile == kTile64 ? 64 : 128; }
+// Tiles that a launch can take, rows of X (of W for the weight gradient) by columns
+enum GroupedTile { kTile128, kTile128x64, kTile128x32, kTile64, kTile32x128, kDirect256, kStaged256x128, kStaged128x256, kGroupedTiles };
+inline int grouped_tile_rows(int tile) {
+  constexpr int rows[kGroupedTiles] = {128, 128, 128, 64, 32, 256, 256, 128};
+  return rows[tile];
+}
+inline int grouped_tile_cols(int tile) {
+  constexpr int cols[kGroupedTiles] = {128, 64, 32, 64, 128, 256, 128, 256};
+  return cols[tile];
+}
 
 // one launch of `blocks` workgroups; per operand mode (and storage type)
 #define SAGNN_GROUPED_MODE(name)                                                                                       \
@@ -400,6 +427,8 @@ template <typename S, int PREC, int BK, bool WT>
 int grouped_launch(const GroupedArgs& a, int tile, int64_t blocks, hipStream_t s) {
   const dim3 grid((uint32_t)blocks), block(256);
   if (tile == kTile128) grouped_kernel<S, PREC, WT, 2, 2, 2, 2, BK><<<grid, block, 0, s>>>(a);
+  else if (tile == kTile128x64) grouped_kernel<S, PREC, WT, 2, 2, 2, 1, BK><<<grid, block, 0, s>>>(a);
+  else if (tile == kTile128x32) grouped_kernel<S, PREC, WT, 4, 1, 1, 1, BK><<<grid, block, 0, s>>>(a);
   else if (tile == kTile64) grouped_kernel<S, PREC, WT, 2, 2, 1, 1, BK><<<grid, block, 0, s>>>(a);
   else grouped_kernel<S, PREC, WT, 1, 4, 1, 1, BK><<<grid, block, 0, s>>>(a);
   SAGNN_LAUNCH_CHECK();
@@ -409,7 +438,10 @@ template <typename S, int PREC, int BK>
 int grouped_tn_launch(const GroupedArgs& a, int tile, int64_t blocks, hipStream_t s) {
   const dim3 grid((uint32_t)blocks), block(256);
   if (tile == kTile128) grouped_tn_kernel<S, PREC, 2, 2, 2, 2, BK><<<grid, block, 0, s>>>(a);
-  else grouped_tn_kernel<S, PREC, 2, 2, 1, 1, BK><<<grid, block, 0, s>>>(a);
+  else if (tile == kTile128x64) grouped_tn_kernel<S, PREC, 2, 2, 2, 1, BK><<<grid, block, 0, s>>>(a);
+  else if (tile == kTile128x32) grouped_tn_kernel<S, PREC, 4, 1, 1, 1, BK><<<grid, block, 0, s>>>(a);
+  else if (tile == kTile64) grouped_tn_kernel<S, PREC, 2, 2, 1, 1, BK><<<grid, block, 0, s>>>(a);
+  else grouped_tn_kernel<S, PREC, 1, 4, 1, 1, BK><<<grid, block, 0, s>>>(a);
   SAGNN_LAUNCH_CHECK();
   return SAGNN_OK;
 }

@@ -6,12 +6,24 @@ namespace sagnn {
 namespace {
 
 // dW[g] = the sum of its parts, chunks ascending; a group of one part was written by the product itself.
-__global__ __launch_bounds__(256) void grouped_join_kernel(const GroupedArgs a) {
+__global__ __launch_bounds__(256) void grouped_join_kernel(const GroupedArgs a, bool four) {
   const int32_t g = blockIdx.y;
   const int64_t lo = grouped_row(a.off, g, a.m), hi = grouped_row(a.off, g + 1, a.m), size = (int64_t)a.kdim * a.nout;
   if (hi <= lo) return;
   const int64_t c0 = lo / a.chunk, c1 = (hi - 1) / a.chunk;
   if (c0 == c1) return;
+  if (four) {                                 // (a multiple of four, and aligned so)
+    for (int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4; i < size; i += (int64_t)gridDim.x * 1024) {
+      float4 sum = *reinterpret_cast<const float4*>(a.partial + (2 * c0 + 1) * size + i);
+#pragma unroll 4
+      for (int64_t c = c0 + 1; c <= c1; ++c) {
+        const float4 x = *reinterpret_cast<const float4*>(a.partial + 2 * c * size + i);
+        sum.x += x.x; sum.y += x.y; sum.z += x.z; sum.w += x.w;
+      }
+      *reinterpret_cast<float4*>(a.dW + g * size + i) = sum;
+    }
+    return;
+  }
   for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < size; i += (int64_t)gridDim.x * 256) {
     float sum = a.partial[(2 * c0 + 1) * size + i];
 #pragma unroll 8
@@ -32,16 +44,54 @@ bool direct_rows(const void* p, int64_t ld, int64_t width) {
   return (reinterpret_cast<uintptr_t>(p) & 15) == 0 && ld % 8 == 0 && width % 8 == 0 && ld <= (1 << 20);
 }
 
+constexpr int64_t kStagedLd = 1 << 20;     // (offsets inside a tile of 256 rows below 2^31)
+
+// Which tiles an operation can have: through registers any (staged: fp32 tensors), straight into LDS bfloat16 ones
+enum { kAny = 0, kDirect = 1, kStaged = 2 };
+
+// What a tile costs: how well it feeds the matrix cores (rates of 8192 x 4096 x 4096, 128 x 128 = 1), and how much of the summed index its
+// beginning and end are worth.  Small tiles are several to a CU, which hides both; the large ones are alone there.
+struct TileCost { double rate, ends; };
+TileCost tile_cost(int32_t dtype, int32_t prec, int tile) {
+  static constexpr TileCost fp32[kGroupedTiles] = {{1., 48}, {.98, 24}, {.91, 12}, {.95, 8}, {.85, 16}, {0, 0}, {0, 0}, {0, 0}};
+  static constexpr TileCost rounded[kGroupedTiles] = {{1., 128}, {.76, 128}, {.62, 32}, {.49, 8}, {.25, 16}, {0, 0}, {1.08, 160}, {1.08, 160}};
+  static constexpr TileCost split[kGroupedTiles] = {{1., 33}, {.87, 24}, {.67, 8}, {.76, 8}, {.65, 8}, {0, 0}, {1.18, 54}, {1.18, 54}};
+  static constexpr TileCost bf16[kGroupedTiles] = {{1., 128}, {.81, 128}, {.66, 32}, {.66, 32}, {.39, 32}, {1.69, 350}, {0, 0}, {0, 0}};
+  return dtype == SAGNN_BF16 ? bf16[tile] : prec == SAGNN_GEMM_FP32 ? fp32[tile] : prec == SAGNN_GEMM_BF16 ? rounded[tile] : split[tile];
+}
+
+// The tile with the least cost: `rows` rows in `parts` ragged parts by `cols` columns, `times` over, `sum` of the summed index.  Tiles are
+// whole, so each part leaves half a tile empty; a launch lasts as long as its fullest CU; and a tile alone on a CU waits for its
+// loads.
+int choose_tile(int32_t dtype, int32_t prec, int ways, int64_t rows, int64_t parts, int64_t cols, int64_t times, int64_t sum, bool whole) {
+  int best = kTile128;
+  double least = 1e300;
+  for (int tile = 0; tile < kGroupedTiles; ++tile) {
+    const TileCost c = tile_cost(dtype, prec, tile);
+    if (c.rate == 0 || (tile == kDirect256 && !(ways & kDirect)) || ((tile == kStaged256x128 || tile == kStaged128x256) && !(ways & kStaged))) continue;
+    const int64_t h = grouped_tile_rows(tile), w = grouped_tile_cols(tile);
+    const int64_t tiles = (ceil_div(rows, h) + (parts < rows ? parts : rows) / 2) * ceil_div(cols, w) * times;
+    const double turns = tiles <= 256 ? 1.25 : whole && tiles < 4 * 256 ? (double)ceil_div(tiles, 256) : tiles / 256.;
+    const double cost = turns * h * w * (sum + c.ends) / c.rate;
+    if (cost < least) {
+      least = cost;
+      best = tile;
+    }
+  }
+  return best;
+}
+
 int launch_rows(const GroupedArgs& g, int32_t dtype, int32_t prec, bool trans_w, hipStream_t s) {
   GroupedArgs a = g;
-  const int64_t mean = a.m / a.groups;
-  auto count = [&](int tile) {
-    return (a.m / grouped_tile_rows(tile) + a.groups + 1) * ceil_div(a.nout, grouped_tile_cols(tile));
-  };
-  int tile = mean <= 32 ? kTile32x128 : (count(kTile128) < 256 ? kTile64 : kTile128);
-  if (dtype == SAGNN_BF16 && tile == kTile128 && count(kDirect256) >= 128 && direct_rows(a.X, a.ldx, a.kdim) && direct_rows(a.W, a.ldw, a.nout) &&
-      a.stride_w % 8 == 0 && direct_rows(a.Y, a.ldy, 0) && (!a.mask || direct_rows(a.mask, a.ldmask, 0)))
-    tile = kDirect256;
+  int ways = kAny;
+  if (dtype == SAGNN_BF16) {
+    if (direct_rows(a.X, a.ldx, a.kdim) && direct_rows(a.W, a.ldw, a.nout) && a.stride_w % 8 == 0 && direct_rows(a.Y, a.ldy, 0) &&
+        (!a.mask || direct_rows(a.mask, a.ldmask, 0)))
+      ways = kDirect;
+  } else if (a.ldx <= kStagedLd && a.ldw <= kStagedLd) {
+    ways = kStaged;
+  }
+  const int tile = choose_tile(dtype, prec, ways, a.m, a.groups, a.nout, 1, a.kdim, true);
   a.row_tiles = (int32_t)(a.m / grouped_tile_rows(tile) + a.groups + 1);
   a.col_tiles = (int32_t)ceil_div(a.nout, grouped_tile_cols(tile));
   const int64_t blocks = (int64_t)a.row_tiles * a.col_tiles;
@@ -51,17 +101,19 @@ int launch_rows(const GroupedArgs& g, int32_t dtype, int32_t prec, bool trans_w,
          : prec == SAGNN_GEMM_BF16 ? grouped_fp32_bf16(a, tile, trans_w, blocks, s) : grouped_fp32_bf16x3(a, tile, trans_w, blocks, s);
 }
 
+// The weight gradient's tiles and chunks of rows.  Chunks fill the chip where the matrices are small or one group has most rows (170003 x 128 x 128
+// in 4 groups, three terms: 83 chunks 95 us, 256 chunks 62); but a group that a chunk's end cuts costs its matrix written twice, read
+// twice and written once more, so a chunk has 640 rows or more, and 8192 where the arithmetic is fastest (16 groups of 16384 x
+// 2048 x 1024, bfloat16: 16 chunks 191 us, 4 chunks 106), but never fewer than as many as give half the CUs work.
 struct TnPlan { int tile; int64_t row_tiles, col_tiles, chunk, chunks; };
-// Chunks of rows.  More of them fill the chip where the matrices are small or one group has most rows; but a group that a chunk's end cuts
-// costs its matrix written twice, read twice and written once more, against 2 rows of arithmetic each for the chunk: not above
-// an eighth of that time where there are as many workgroups as half the CUs anyway (16 groups of 16384 x 2048 x 1024: 16 chunks
-// 202 us, 4 chunks 139).
-TnPlan tn_plan(int64_t m, int32_t kdim, int32_t nout, bool direct) {
+TnPlan tn_plan(int64_t m, int32_t groups, int32_t kdim, int32_t nout, int32_t dtype, int32_t prec, int ways) {
   TnPlan p{};
-  p.tile = kdim <= 64 || nout <= 64 ? kTile64 : direct && kdim >= 256 && nout >= 256 ? kDirect256 : kTile128;
+  // (a chunk of 512 rows or a group is what a workgroup has at least)
+  const int64_t pairs = groups > m / 512 + 1 ? groups : m / 512 + 1;
+  p.tile = choose_tile(dtype, prec, ways, kdim, 0, nout, pairs, m / pairs, false);
   p.row_tiles = ceil_div(kdim, grouped_tile_rows(p.tile));
   p.col_tiles = ceil_div(nout, grouped_tile_cols(p.tile));
-  const int64_t tiles = p.row_tiles * p.col_tiles, rare = m / (direct ? 8192 : 2048);
+  const int64_t tiles = p.row_tiles * p.col_tiles, rare = m / (p.tile == kDirect256 ? 8192 : 640);
   int64_t chunks = 512 / tiles < rare ? 512 / tiles : rare;
   if (chunks < 128 / tiles) chunks = 128 / tiles;
   if (chunks > ceil_div(m, 256)) chunks = ceil_div(m, 256);
@@ -70,27 +122,43 @@ TnPlan tn_plan(int64_t m, int32_t kdim, int32_t nout, bool direct) {
   p.chunks = ceil_div(m > 0 ? m : 1, p.chunk);
   return p;
 }
-size_t tn_ws_bytes(int64_t m, int32_t kdim, int32_t nout) {
-  const int64_t a = tn_plan(m, kdim, nout, false).chunks, b = tn_plan(m, kdim, nout, true).chunks, chunks = a > b ? a : b;
+// Room for the plan of any types and modes
+size_t tn_ws_bytes(int64_t m, int32_t groups, int32_t kdim, int32_t nout) {
+  int64_t chunks = 0;
+  auto most = [&](int32_t dtype, int32_t prec, int ways) {
+    const int64_t c = tn_plan(m, groups, kdim, nout, dtype, prec, ways).chunks;
+    chunks = c > chunks ? c : chunks;
+  };
+  most(SAGNN_BF16, SAGNN_GEMM_FP32, kAny);
+  most(SAGNN_BF16, SAGNN_GEMM_FP32, kDirect);
+  for (int32_t prec : {SAGNN_GEMM_FP32, SAGNN_GEMM_BF16, SAGNN_GEMM_FP32_BF16X3}) {
+    most(SAGNN_F32, prec, kAny);
+    most(SAGNN_F32, prec, kStaged);
+  }
   return chunks > 1 ? (size_t)(2 * chunks) * kdim * nout * 4 : 0;
 }
 
 int launch_tn(const GroupedArgs& g, int32_t dtype, int32_t prec, hipStream_t s) {
   GroupedArgs a = g;
-  const TnPlan p = tn_plan(a.m, a.kdim, a.nout, dtype == SAGNN_BF16 && direct_rows(a.X, a.ldx, a.kdim) && direct_rows(a.G, a.ldg, a.nout) &&
-                                                    aligned16(a.dW) && aligned16(a.partial));
+  const bool direct = dtype == SAGNN_BF16 && direct_rows(a.X, a.ldx, a.kdim) && direct_rows(a.G, a.ldg, a.nout) && aligned16(a.dW) && aligned16(a.partial);
+  const bool staged = dtype == SAGNN_F32 && a.ldx <= kStagedLd && a.ldg <= kStagedLd;
+  const TnPlan p = tn_plan(a.m, a.groups, a.kdim, a.nout, dtype, prec, direct ? kDirect : staged ? kStaged : kAny);
   a.chunk = p.chunk;
   a.row_tiles = (int32_t)p.row_tiles;
   a.col_tiles = (int32_t)p.col_tiles;
-  const int64_t blocks = (p.chunks + a.groups) * p.row_tiles * p.col_tiles;
+  int64_t pairs = p.chunks + a.groups;
+  a.pairs = (int32_t)pairs;
+  if (pairs >= kManyPairs) pairs = round_up((size_t)pairs, 8);
+  const int64_t blocks = pairs * p.row_tiles * p.col_tiles;
   if (blocks > INT32_MAX) return SAGNN_EINVAL;
   const int rc = dtype == SAGNN_BF16 ? grouped_tn_bf16(a, p.tile, blocks, s)
                  : prec == SAGNN_GEMM_FP32 ? grouped_tn_fp32(a, p.tile, blocks, s)
                  : prec == SAGNN_GEMM_BF16 ? grouped_tn_fp32_bf16(a, p.tile, blocks, s) : grouped_tn_fp32_bf16x3(a, p.tile, blocks, s);
   if (rc != SAGNN_OK || p.chunks == 1) return rc;
-  int64_t wide = ceil_div((int64_t)a.kdim * a.nout, 256);
+  const bool four = ((int64_t)a.kdim * a.nout & 3) == 0 && aligned16(a.dW) && aligned16(a.partial);
+  int64_t wide = ceil_div((int64_t)a.kdim * a.nout, four ? 1024 : 256);
   if (wide > 1024) wide = 1024;
-  grouped_join_kernel<<<dim3((uint32_t)wide, (uint32_t)a.groups), 256, 0, s>>>(a);
+  grouped_join_kernel<<<dim3((uint32_t)wide, (uint32_t)a.groups), 256, 0, s>>>(a, four);
   SAGNN_LAUNCH_CHECK();
   return SAGNN_OK;
 }
@@ -118,7 +186,7 @@ SAGNN_EXPORT int grouped_gemm_act(int32_t dtype, const void* d_X, int64_t ldx, c
 SAGNN_EXPORT int grouped_gemm_bwd_workspace_bytes(int64_t m, int32_t n_groups, int32_t kdim, int32_t nout, size_t* bytes) {
   using namespace sagnn;
   if (!bytes || !valid(SAGNN_F32, SAGNN_GEMM_FP32, m, n_groups, kdim, nout)) return SAGNN_EINVAL;
-  *bytes = tn_ws_bytes(m, kdim, nout);
+  *bytes = tn_ws_bytes(m, n_groups, kdim, nout);
   return SAGNN_OK;
 }
 
@@ -134,8 +202,8 @@ SAGNN_EXPORT int grouped_gemm_bwd(int32_t dtype, const void* d_X, int64_t ldx, c
   for (const void* p : {d_X, d_W, d_G, d_mask, (const void*)d_dX})
     if (!element_aligned(p, dtype)) return SAGNN_EINVAL;
   if (!element_aligned(d_off, SAGNN_F32) || !element_aligned(d_dW, SAGNN_F32) || !element_aligned(d_ws, SAGNN_F32)) return SAGNN_EINVAL;
-  if (d_dW && ws_bytes < tn_ws_bytes(m, kdim, nout)) return SAGNN_ECAPACITY;
-  if (d_dW && !d_ws && tn_ws_bytes(m, kdim, nout) > 0) return SAGNN_EINVAL;
+  if (d_dW && ws_bytes < tn_ws_bytes(m, n_groups, kdim, nout)) return SAGNN_ECAPACITY;
+  if (d_dW && !d_ws && tn_ws_bytes(m, n_groups, kdim, nout) > 0) return SAGNN_EINVAL;
   hipStream_t s = (hipStream_t)stream;
   GroupedArgs a{};
   a.off = d_off; a.groups = n_groups; a.m = m;
