@@ -640,11 +640,13 @@ int grouped_gemm_bwd(int32_t dtype, const void* d_X, int64_t ldx, const void* d_
  * may be NULL) are fp32.  mean and rstd are outputs forward and inputs backward.  Mean and variance are summed in 64 bits.
  * Orders of sums are fixed: the same bits every time.  Any C up to SAGNN_NORM_MAX_WIDTH, n_groups <= SAGNN_NORM_MAX_GROUPS,
  * any leading dimensions not below C, tensors aligned to their element.  Y may be X, dX may be G or X.
- * d_ws: group_norm_workspace_bytes() bytes (serves both directions), 16-byte aligned.
+ * d_ws: group_norm_workspace_bytes() bytes, 16-byte aligned; NULL where that is 0 (forward over short segments).  ld: the largest
+ * leading dimension of the call, backward: 0 or 1.
  */
 #define SAGNN_NORM_MAX_WIDTH 16384
 #define SAGNN_NORM_MAX_GROUPS 1024
-int group_norm_workspace_bytes(int64_t m, int32_t n_seg, int32_t C, int32_t n_groups, size_t* bytes);
+int group_norm_workspace_bytes(int32_t dtype, int64_t m, int32_t n_seg, int64_t max_rows, int32_t C, int32_t n_groups,
+                               int64_t ld, int32_t backward, size_t* bytes);
 int group_norm_act_fwd(int32_t dtype, const void* d_X, int64_t ldx, const int32_t* d_seg, int32_t n_seg,
                        int64_t max_rows, int64_t m, int32_t C, int32_t n_groups, const float* d_gamma,
                        const float* d_beta, double eps, int32_t act, void* d_Y, int64_t ldy, float* d_mean,

@@ -163,7 +163,7 @@ def lib():
         L.grouped_gemm_act.argtypes = [i32, vp, i64, vp, i64, i64, i32, vp, i32, i64, i32, i32, i32, i32, vp, i64, vp, i64, vp]
         L.grouped_gemm_bwd_workspace_bytes.argtypes = [i64, i32, i32, i32, psz]
         L.grouped_gemm_bwd.argtypes = [i32, vp, i64, vp, i64, i64, vp, i32, i64, i32, i32, i32, vp, i64, vp, i64, vp, i64, vp, vp, sz, vp]
-        L.group_norm_workspace_bytes.argtypes = [i64, i32, i32, i32, psz]
+        L.group_norm_workspace_bytes.argtypes = [i32, i64, i32, i64, i32, i32, i64, i32, psz]
         L.group_norm_act_fwd.argtypes = [i32, vp, i64, vp, i32, i64, i64, i32, i32, vp, vp, f64, i32, vp, i64, vp, vp, vp, sz, vp]
         L.group_norm_act_bwd.argtypes = [i32, vp, i64, vp, i64, vp, i32, i64, i64, i32, i32, vp, vp, i32, vp, vp, vp, i64, vp, vp, vp,
                                          sz, vp]
@@ -712,7 +712,8 @@ def _typed(t: torch.Tensor, name: str, dtype=None):
     """A row-major matrix of fp32 or bfloat16 (of `dtype` where that is given), possibly a column slice of a wider one."""
     if not t.is_cuda:
         raise ValueError(f"{name} must be a CUDA/HIP tensor (there is no CPU path)")
-    if t.dim() != 2 or t.dtype not in _DTYPE or (dtype is not None and t.dtype is not dtype):
+    kind = t.dtype
+    if t.dim() != 2 or (kind not in _DTYPE if dtype is None else kind is not dtype):
         raise ValueError(f"{name}: expected a 2-D tensor of " + (str(dtype) if dtype is not None else "float32 or bfloat16"))
     if not t.is_contiguous() and t.shape[0] > 1 and t.shape[1] > 0 and ((t.shape[1] > 1 and t.stride(1) != 1) or t.stride(0) < t.shape[1]):
         raise ValueError(f"{name}: rows must be contiguous (unit stride inside a row) and must not overlap")
@@ -720,7 +721,7 @@ def _typed(t: torch.Tensor, name: str, dtype=None):
 
 
 def _shape(t: torch.Tensor, shape, name: str):
-    if tuple(t.shape) != tuple(shape):
+    if t.shape != shape:
         raise ValueError(f"{name}: expected {tuple(shape)}, got {tuple(t.shape)}")
     return t
 
@@ -761,10 +762,11 @@ def grouped_gemm_act(X, W, off, transW=False, prec=GEMM_FP32, act=ACT_IDENTITY, 
         _shape(_typed(mask, "mask", X.dtype), (m, nout), "mask")
     if out is None:
         out = torch.empty((m, nout), dtype=X.dtype, device=X.device)
-    _shape(_typed(out, "out", X.dtype), (m, nout), "out")
-    _check(_calls().grouped_gemm_act(_DTYPE[X.dtype], _ptr(X), _ld(X), _ptr(W), ldw, stride_w, int(transW), _ptr(off), types, m, kdim,
-                                     nout, prec, act, _ptr(mask), _ld(mask) if mask is not None else 0, _ptr(out), _ld(out), _stream()),
-           "grouped_gemm_act")
+    else:
+        _shape(_typed(out, "out", X.dtype), (m, nout), "out")
+    _check(_calls().grouped_gemm_act(_DTYPE[X.dtype], X.data_ptr(), _ld(X), W.data_ptr(), ldw, stride_w, int(transW), off.data_ptr(), types,
+                                     m, kdim, nout, prec, act, _ptr(mask), _ld(mask) if mask is not None else 0, out.data_ptr(), _ld(out),
+                                     _stream()), "grouped_gemm_act")
     return out
 
 
@@ -795,16 +797,21 @@ def grouped_gemm_bwd(X, W, off, G, mask=None, prec=GEMM_FP32, want_dx=True, want
     return dX, dW
 
 
-def _norm_args(X, groups, gamma, beta, seg, n_seg):
+def _norm_args(X, groups, gamma, beta, seg, n_seg, out):
+    """What both directions check; and out's place where it is not given."""
     X = _typed(X, "X")
-    m, c = X.shape
+    shape = X.shape
     if seg is not None:
-        seg = _offsets(seg, "seg")
-        n_seg = seg.numel() - 1
-    for name, t in (("gamma", gamma), ("beta", beta)):
-        if t is not None:
-            _shape(_dev(t, torch.float32, name), (c,), name)
-    return X, m, c, seg, n_seg, _ws(_bytes_of("group_norm_workspace_bytes", m, n_seg, c, groups), X.device)
+        n_seg = _offsets(seg, "seg").numel() - 1
+    if gamma is not None:
+        _shape(_dev(gamma, torch.float32, "gamma"), shape[1:], "gamma")
+    if beta is not None:
+        _shape(_dev(beta, torch.float32, "beta"), shape[1:], "beta")
+    if out is None:
+        out = torch.empty(shape, dtype=X.dtype, device=X.device)
+    else:
+        _shape(_typed(out, "out", X.dtype), shape, "out")
+    return *shape, n_seg, out, _ld(X), _ld(out)
 
 
 def group_norm_act(X, groups, gamma=None, beta=None, seg=None, n_seg=1, max_rows=0, eps=1e-5, act=ACT_IDENTITY, out=None):
@@ -812,30 +819,30 @@ def group_norm_act(X, groups, gamma=None, beta=None, seg=None, n_seg=1, max_rows
     segment and each of `groups` groups of channels.  seg: int32 on the device, one more than there are segments (rows behind
     the last are zeros in Y), or None for n_seg segments of equal length; max_rows: rows of the longest one where it is known.
     Returns (Y, mean, rstd), the last two float32, segments x groups."""
-    X, m, c, seg, n_seg, ws = _norm_args(X, groups, gamma, beta, seg, n_seg)
-    if out is None:
-        out = torch.empty((m, c), dtype=X.dtype, device=X.device)
-    _shape(_typed(out, "out", X.dtype), (m, c), "out")
-    mean, rstd = torch.empty((2, n_seg, groups), dtype=torch.float32, device=X.device).unbind()
-    _check(_calls().group_norm_act_fwd(_DTYPE[X.dtype], _ptr(X), _ld(X), _ptr(seg), n_seg, max_rows, m, c, groups, _ptr(gamma), _ptr(beta),
-                                       eps, act, _ptr(out), _ld(out), _ptr(mean), _ptr(rstd), _ptr(ws), ws.numel(), _stream()),
+    m, c, n_seg, out, ldx, ldy = _norm_args(X, groups, gamma, beta, seg, n_seg, out)
+    kind, dev = _DTYPE[X.dtype], X.device
+    need = _bytes_of("group_norm_workspace_bytes", kind, m, n_seg, max_rows, c, groups, max(ldx, ldy), 0)
+    ws = _ws(need, dev) if need else None
+    mean, rstd = torch.empty((2, n_seg, groups), dtype=torch.float32, device=dev).unbind()
+    _check(_calls().group_norm_act_fwd(kind, X.data_ptr(), ldx, _ptr(seg), n_seg, max_rows, m, c, groups, _ptr(gamma), _ptr(beta),
+                                       eps, act, out.data_ptr(), ldy, mean.data_ptr(), rstd.data_ptr(), _ptr(ws), need, _stream()),
            "group_norm_act_fwd")
     return out, mean, rstd
 
 
 def group_norm_act_bwd(X, G, mean, rstd, groups, gamma=None, beta=None, seg=None, n_seg=1, max_rows=0, act=ACT_IDENTITY, out=None):
     """Gradients of group_norm_act for G = dLoss/dY, with the mean and rstd that it returned.  Returns (dX, dgamma, dbeta)."""
-    X, m, c, seg, n_seg, ws = _norm_args(X, groups, gamma, beta, seg, n_seg)
+    m, c, n_seg, out, ldx, lddx = _norm_args(X, groups, gamma, beta, seg, n_seg, out)
     _shape(_typed(G, "G", X.dtype), (m, c), "G")
     for name, t in (("mean", mean), ("rstd", rstd)):
         _shape(_dev(t, torch.float32, name), (n_seg, groups), name)
-    if out is None:
-        out = torch.empty((m, c), dtype=X.dtype, device=X.device)
-    _shape(_typed(out, "out", X.dtype), (m, c), "out")
-    dgamma, dbeta = torch.empty((2, c), dtype=torch.float32, device=X.device).unbind()
-    _check(_calls().group_norm_act_bwd(_DTYPE[X.dtype], _ptr(X), _ld(X), _ptr(G), _ld(G), _ptr(seg), n_seg, max_rows, m, c, groups,
-                                       _ptr(gamma), _ptr(beta), act, _ptr(mean), _ptr(rstd), _ptr(out), _ld(out), _ptr(dgamma), _ptr(dbeta),
-                                       _ptr(ws), ws.numel(), _stream()), "group_norm_act_bwd")
+    kind, dev, ldg = _DTYPE[X.dtype], X.device, _ld(G)
+    need = _bytes_of("group_norm_workspace_bytes", kind, m, n_seg, max_rows, c, groups, max(ldx, ldg, lddx), 1)
+    ws = _ws(need, dev) if need else None
+    dgamma, dbeta = torch.empty((2, c), dtype=torch.float32, device=dev).unbind()
+    _check(_calls().group_norm_act_bwd(kind, X.data_ptr(), ldx, G.data_ptr(), ldg, _ptr(seg), n_seg, max_rows, m, c, groups, _ptr(gamma),
+                                       _ptr(beta), act, mean.data_ptr(), rstd.data_ptr(), out.data_ptr(), lddx, dgamma.data_ptr(),
+                                       dbeta.data_ptr(), _ptr(ws), need, _stream()), "group_norm_act_bwd")
     return out, dgamma, dbeta
 
 

@@ -778,7 +778,8 @@ int vector_of(int32_t dtype, int32_t C) {
 
 struct NormPlan { int64_t chunk, chunks; size_t parts, sums, rows, total; };
 constexpr int kMostStripes = 2048;
-NormPlan norm_plan(int64_t m, int32_t segments, int32_t C, int32_t groups) {
+// Segments in parts: chunks of rows, and where the sums lie
+NormPlan norm_plan(int64_t m, int32_t segments, int32_t C, int32_t groups, bool backward) {
   NormPlan p{};
   // 2048 workgroups fill the chip; a chunk has eight rows of 256 threads or more
   int64_t least = ceil_div(8 * 2048, C);
@@ -789,9 +790,10 @@ NormPlan norm_plan(int64_t m, int32_t segments, int32_t C, int32_t groups) {
   size_t off = 0;
   auto take = [&](size_t bytes) { const size_t o = off; off += round_up(bytes, 256); return o; };
   p.parts = take((size_t)(p.chunks + segments) * groups * sizeof(double2));
-  p.sums = take((size_t)segments * groups * sizeof(float2));
-  p.rows = take((size_t)(segments < kMostStripes && segments > p.chunks ? segments : p.chunks > kMostStripes || segments < kMostStripes ? p.chunks : kMostStripes) *
-                C * sizeof(float2));
+  if (backward) {
+    p.sums = take((size_t)segments * groups * sizeof(float2));
+    p.rows = take((size_t)p.chunks * C * sizeof(float2));
+  }
   p.total = off;
   return p;
 }
@@ -823,6 +825,27 @@ size_t whole_lds(const WholePlan& w, int32_t D, int v, bool backward) {
   return ((size_t)(w.slab / D) + (size_t)w.threads * (D % v == 0 ? 1 : v)) * sizeof(double2) + (backward ? (size_t)w.threads * v * sizeof(float2) : 0);
 }
 
+// How a call is carried out, and what it needs for that
+struct NormForm { WholePlan whole; NormPlan parts; int64_t table; size_t bytes; };
+NormForm norm_form(int32_t dtype, int64_t m, int32_t segments, int64_t max_rows, int32_t C, int32_t groups, int64_t ld, bool backward) {
+  NormForm f{};
+  const int32_t D = C / groups;
+  const int size = dtype == SAGNN_BF16 ? 2 : 4;
+  int v = vector_of(dtype, C);
+  if (backward && v * size > 8) v /= 2;
+  if (m > 0 && ld <= kWholeLd) f.whole = whole_plan(m, max_rows, C, D, v, size, !backward ? kKept : D % v == 0 ? kKeptBackward : kKeptBackward / 2);
+  if (((int64_t)segments + 16) * f.whole.slabs > INT32_MAX) f.whole.slab = 0;
+  if (f.whole.slab) {
+    f.table = segments < kMostStripes ? segments : kMostStripes;
+    f.bytes = backward ? round_up((size_t)f.table * C * sizeof(float2), 256) : 0;
+  } else {
+    f.parts = norm_plan(m, segments, C, groups, backward);
+    f.table = m > 0 ? f.parts.chunks : 0;
+    f.bytes = f.parts.total;
+  }
+  return f;
+}
+
 template <typename F>
 int by_act(int32_t act, F f) {
   if (act == SAGNN_ACT_RELU) return f(std::integral_constant<int, SAGNN_ACT_RELU>{});
@@ -852,11 +875,12 @@ bool aligned_to(const void* p, uintptr_t bytes) { return (reinterpret_cast<uintp
 }  // namespace
 }  // namespace sagnn
 
-SAGNN_EXPORT int group_norm_workspace_bytes(int64_t m, int32_t n_seg, int32_t C, int32_t n_groups, size_t* bytes) {
+SAGNN_EXPORT int group_norm_workspace_bytes(int32_t dtype, int64_t m, int32_t n_seg, int64_t max_rows, int32_t C, int32_t n_groups,
+                                            int64_t ld, int32_t backward, size_t* bytes) {
   using namespace sagnn;
   static const int32_t some = 0;
-  if (!bytes || !valid(SAGNN_F32, &some, n_seg, m, C, n_groups, SAGNN_ACT_IDENTITY)) return SAGNN_EINVAL;
-  *bytes = norm_plan(m, n_seg, C, n_groups).total;
+  if (!bytes || !valid(dtype, &some, n_seg, m, C, n_groups, SAGNN_ACT_IDENTITY) || max_rows < 0 || ld < C || (backward & ~1)) return SAGNN_EINVAL;
+  *bytes = norm_form(dtype, m, n_seg, max_rows, C, n_groups, ld, backward != 0).bytes;
   return SAGNN_OK;
 }
 
@@ -866,31 +890,30 @@ SAGNN_EXPORT int group_norm_act_fwd(int32_t dtype, const void* d_X, int64_t ldx,
                                     void* stream) {
   using namespace sagnn;
   if (!valid(dtype, d_seg, n_seg, m, C, n_groups, act) || max_rows < 0 || ldx < C || ldy < C || !(eps >= 0.) || eps > 1e30) return SAGNN_EINVAL;
-  if (!d_mean || !d_rstd || !d_ws || (m > 0 && (!d_X || !d_Y))) return SAGNN_EINVAL;
+  if (!d_mean || !d_rstd || (m > 0 && (!d_X || !d_Y))) return SAGNN_EINVAL;
   const uintptr_t size = dtype == SAGNN_BF16 ? 2 : 4;
   if (!aligned_to(d_X, size) || !aligned_to(d_Y, size) || !aligned_to(d_seg, 4) || !aligned_to(d_gamma, 4) || !aligned_to(d_beta, 4) ||
       !aligned_to(d_mean, 4) || !aligned_to(d_rstd, 4) || !aligned_to(d_ws, 16))
     return SAGNN_EINVAL;
-  const NormPlan p = norm_plan(m, n_seg, C, n_groups);
-  if (ws_bytes < p.total) return SAGNN_ECAPACITY;
+  const NormForm f = norm_form(dtype, m, n_seg, max_rows, C, n_groups, ldx > ldy ? ldx : ldy, false);
+  const NormPlan& p = f.parts;
+  const WholePlan& w = f.whole;
+  if (f.bytes > 0 && !d_ws) return SAGNN_EINVAL;
+  if (ws_bytes < f.bytes) return SAGNN_ECAPACITY;
   NormArgs a{};
   a.X = d_X; a.ldx = ldx; a.Y = d_Y; a.ldy = ldy; a.seg = d_seg; a.segments = n_seg; a.each = m / n_seg; a.m = m; a.C = C; a.groups = n_groups;
   a.D = C / n_groups; a.gamma = d_gamma; a.beta = d_beta; a.mean = d_mean; a.rstd = d_rstd; a.eps = eps; a.act = act;
-  a.chunk = p.chunk; a.chunks = p.chunks; a.parts = (double2*)((char*)d_ws + p.parts);
+  a.chunk = p.chunk; a.chunks = p.chunks; a.parts = (double2*)((char*)d_ws + p.parts); a.slab = w.slab;
   hipStream_t s = (hipStream_t)stream;
   return by_act(act, [&](auto A) { return by_vector(dtype, vector_of(dtype, C), [&](auto V, auto zero) {
     constexpr int v = decltype(V)::value, ACT = decltype(A)::value;
     using S = decltype(zero);
-    const WholePlan w = whole_plan(m, max_rows, C, a.D, v, sizeof(S), kKept);
-    if (w.slab && m > 0 && ldx <= kWholeLd && ldy <= kWholeLd) {
-      a.slab = w.slab;
-      const int64_t blocks = ((int64_t)n_seg + (d_seg ? 16 : 0)) * w.slabs;       // (rows behind the last segment)
-      if (blocks <= INT32_MAX) {
-        if (a.D % v == 0) norm_whole_kernel<S, v, 1, ACT><<<dim3((uint32_t)blocks), (uint32_t)w.threads, whole_lds(w, a.D, v, false), s>>>(a, w.slabs);
-        else norm_whole_kernel<S, v, v, ACT><<<dim3((uint32_t)blocks), (uint32_t)w.threads, whole_lds(w, a.D, v, false), s>>>(a, w.slabs);
-        SAGNN_LAUNCH_CHECK();
-        return (int)SAGNN_OK;
-      }
+    if (w.slab) {
+      const dim3 grid((uint32_t)(n_seg + (d_seg ? 16 : 0)) * w.slabs);            // (sixteen for the rows behind the last segment)
+      if (a.D % v == 0) norm_whole_kernel<S, v, 1, ACT><<<grid, (uint32_t)w.threads, whole_lds(w, a.D, v, false), s>>>(a, w.slabs);
+      else norm_whole_kernel<S, v, v, ACT><<<grid, (uint32_t)w.threads, whole_lds(w, a.D, v, false), s>>>(a, w.slabs);
+      SAGNN_LAUNCH_CHECK();
+      return (int)SAGNN_OK;
     }
     if (m > 0) {
       norm_sum_kernel<S, v><<<dim3((uint32_t)p.chunks), kThreads, (size_t)n_groups * 16 + kThreads * v * 16, s>>>(a);
@@ -912,30 +935,30 @@ SAGNN_EXPORT int group_norm_act_bwd(int32_t dtype, const void* d_X, int64_t ldx,
                                     float* d_dgamma, float* d_dbeta, void* d_ws, size_t ws_bytes, void* stream) {
   using namespace sagnn;
   if (!valid(dtype, d_seg, n_seg, m, C, n_groups, act) || max_rows < 0 || ldx < C || ldg < C || lddx < C) return SAGNN_EINVAL;
-  if (!d_mean || !d_rstd || !d_ws || (m > 0 && (!d_X || !d_G || !d_dX))) return SAGNN_EINVAL;
+  if (!d_mean || !d_rstd || (m > 0 && (!d_X || !d_G || !d_dX))) return SAGNN_EINVAL;
   const uintptr_t size = dtype == SAGNN_BF16 ? 2 : 4;
   if (!aligned_to(d_X, size) || !aligned_to(d_G, size) || !aligned_to(d_dX, size) || !aligned_to(d_seg, 4) || !aligned_to(d_gamma, 4) ||
       !aligned_to(d_beta, 4) || !aligned_to(d_mean, 4) || !aligned_to(d_rstd, 4) || !aligned_to(d_dgamma, 4) || !aligned_to(d_dbeta, 4) ||
       !aligned_to(d_ws, 16))
     return SAGNN_EINVAL;
-  const NormPlan p = norm_plan(m, n_seg, C, n_groups);
-  if (ws_bytes < p.total) return SAGNN_ECAPACITY;
+  const NormForm f = norm_form(dtype, m, n_seg, max_rows, C, n_groups, ldx > ldg ? (ldx > lddx ? ldx : lddx) : (ldg > lddx ? ldg : lddx), true);
+  const NormPlan& p = f.parts;
+  const WholePlan& w = f.whole;
+  if (!d_ws && f.bytes > 0) return SAGNN_EINVAL;
+  if (ws_bytes < f.bytes) return SAGNN_ECAPACITY;
   NormArgs a{};
   a.X = d_X; a.ldx = ldx; a.G = d_G; a.ldg = ldg; a.Y = d_dX; a.ldy = lddx; a.seg = d_seg; a.segments = n_seg; a.each = m / n_seg; a.m = m;
   a.C = C; a.groups = n_groups; a.D = C / n_groups; a.gamma = d_gamma; a.beta = d_beta; a.mean = const_cast<float*>(d_mean);
   a.rstd = const_cast<float*>(d_rstd); a.act = act; a.dgamma = d_dgamma; a.dbeta = d_dbeta; a.chunk = p.chunk; a.chunks = p.chunks;
   a.parts = (double2*)((char*)d_ws + p.parts); a.sums = (float2*)((char*)d_ws + p.sums); a.rows = (float2*)((char*)d_ws + p.rows);
-  a.table = m > 0 ? p.chunks : 0;
+  a.table = f.table; a.slab = w.slab;
   hipStream_t s = (hipStream_t)stream;
   return by_act(act, [&](auto A) { return by_vector(dtype, vector_of(dtype, C), [&](auto V, auto zero) {
     constexpr int v = decltype(V)::value, ACT = decltype(A)::value;
     using S = decltype(zero);
     const int32_t wide = (int32_t)ceil_div(C, 16);
     constexpr int u = v * sizeof(S) > 8 ? v / 2 : v;
-    const WholePlan w = whole_plan(m, max_rows, C, a.D, u, sizeof(S), a.D % u == 0 ? kKeptBackward : kKeptBackward / 2);
-    if (w.slab && m > 0 && ldx <= kWholeLd && ldg <= kWholeLd && lddx <= kWholeLd) {
-      a.slab = w.slab;
-      a.table = n_seg < kMostStripes ? n_seg : kMostStripes;
+    if (w.slab) {
       const size_t lds = whole_lds(w, a.D, u, true);
       const dim3 grid((uint32_t)(a.table * w.slabs));
       if (a.D % u == 0) norm_bwd_whole_kernel<S, u, 1, ACT><<<grid, (uint32_t)w.threads, lds, s>>>(a, w.slabs);

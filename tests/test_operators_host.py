@@ -72,7 +72,7 @@ FWD_NORM = dict(dtype=0, X=P, ldx=24, seg=P, n_seg=4, max_rows=0, m=100, C=24, g
     {"dtype": 2}, {"n_seg": 0}, {"n_seg": -1}, {"max_rows": -1}, {"m": -1}, {"m": 1 << 31}, {"C": 0}, {"C": 16385, "ldx": 16385, "ldy": 16385, "groups": 1},
     {"groups": 0}, {"groups": 5}, {"groups": 1025, "C": 2050, "ldx": 2050, "ldy": 2050}, {"eps": -1e-5}, {"eps": float("nan")},
     {"eps": float("inf")}, {"act": 3}, {"act": -1}, {"ldx": 23}, {"ldy": 23}, {"X": None}, {"Y": None}, {"mean": None}, {"rstd": None},
-    {"ws": None}, {"seg": None, "n_seg": 7}, {"X": P + 2}, {"Y": P + 1}, {"gamma": P + 2}, {"beta": P + 1}, {"mean": P + 2}, {"rstd": P + 2},
+    {"m": 500_000, "ws": None}, {"seg": None, "n_seg": 7}, {"X": P + 2}, {"Y": P + 1}, {"gamma": P + 2}, {"beta": P + 1}, {"mean": P + 2}, {"rstd": P + 2},
     {"ws": P + 8}, {"seg": P + 2}, {"n_seg": 1 << 27},
 ])
 def test_group_norm_act_fwd_refuses(change):
@@ -95,12 +95,22 @@ def test_group_norm_act_bwd_refuses(change):
 def test_group_norm_needs_its_workspace():
     b = ctypes.c_size_t(0)
     query = sagnn.lib().group_norm_workspace_bytes
-    assert query(100, 4, 24, 3, ctypes.byref(b)) == 0 and b.value > 0
-    assert call("group_norm_act_fwd", FWD_NORM, ws_bytes=b.value - 1) == ECAPACITY
-    assert call("group_norm_act_bwd", BWD_NORM, ws_bytes=b.value - 1) == ECAPACITY
-    for bad in ((-1, 4, 24, 3), (100, 0, 24, 3), (100, 4, 25, 3), (100, 4, 24, 0), (100, 4, 0, 1)):
-        assert query(*bad, ctypes.byref(b)) == EINVAL
-    assert query(100, 4, 24, 3, None) == EINVAL
+    good = dict(dtype=0, m=500_000, n_seg=4, max_rows=0, C=24, groups=3, ld=24, backward=0)
+
+    def size(**change):
+        assert query(*{**good, **change}.values(), ctypes.byref(b)) == 0
+        return b.value
+
+    assert call("group_norm_act_fwd", FWD_NORM, m=500_000, ws_bytes=size() - 1) == ECAPACITY
+    assert call("group_norm_act_fwd", FWD_NORM, m=500_000, ws=None) == EINVAL
+    assert size(backward=1) > size() > 0
+    assert call("group_norm_act_bwd", BWD_NORM, m=500_000, ws_bytes=size(dtype=1, backward=1) - 1) == ECAPACITY
+    # short segments: none forward, gamma's and beta's sums backward; what lies far apart goes the other way
+    assert size(max_rows=100) == 0 and size(max_rows=100, backward=1) > 0 and size(max_rows=100, ld=1 << 20) > 0
+    assert call("group_norm_act_bwd", BWD_NORM, m=500_000, max_rows=100, ws_bytes=size(dtype=1, backward=1, max_rows=100) - 1) == ECAPACITY
+    for bad in ({"m": -1}, {"n_seg": 0}, {"C": 25}, {"groups": 0}, {"C": 0}, {"dtype": 2}, {"max_rows": -1}, {"ld": 23}, {"backward": 2}):
+        assert query(*{**good, **bad}.values(), ctypes.byref(b)) == EINVAL, bad
+    assert query(*good.values(), None) == EINVAL
 
 
 def grad_rows(*rows):
