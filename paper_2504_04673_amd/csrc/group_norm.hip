@@ -27,6 +27,7 @@ struct NormArgs {
   float* dgamma; float* dbeta;
   int64_t chunk, chunks;             // rows of a chunk, chunks
   int64_t table;                     // rows of `rows`
+  bool joined;                       // the workgroups that write join the parts of their segments, each for itself
   int32_t slab;                      // channels of a workgroup, where it takes whole segments
   double2* parts;                    // (chunks + segments) x groups
   float2* sums;                      // backward, segments x groups: the two sums over a group, divided by its size
@@ -256,6 +257,7 @@ __global__ __launch_bounds__(kThreads) void norm_sum_kernel(const NormArgs a) {
 __device__ __forceinline__ double2 join_parts(const NormArgs& a, int32_t b, int32_t g, int64_t lo, int64_t hi) {
   double2 s = make_double2(0., 0.);
   if (hi > lo)
+#pragma unroll 4
     for (int64_t c = lo / a.chunk + (threadIdx.x & 63); c <= (hi - 1) / a.chunk; c += 64) {
       const double2 p = a.parts[(c + b) * a.groups + g];
       s.x += p.x;
@@ -268,18 +270,40 @@ __device__ __forceinline__ double2 join_parts(const NormArgs& a, int32_t b, int3
   return s;
 }
 
+// Mean and reciprocal deviation of n values by their sums
+__device__ __forceinline__ float2 moments(const NormArgs& a, double2 s, int64_t rows) {
+  const double n = rows > 0 ? (double)rows * a.D : 1.;
+  const double mean = s.x / n, var = s.y / n - mean * mean;
+  return make_float2((float)mean, (float)(1. / sqrt((var < 0. ? 0. : var) + a.eps)));
+}
+// Backward: the two sums over the group's size
+__device__ __forceinline__ float2 means(const NormArgs& a, double2 s, int64_t rows) {
+  const double n = rows > 0 ? (double)rows * a.D : 1.;
+  return make_float2((float)(s.x / n), (float)(s.y / n));
+}
+
 __global__ __launch_bounds__(kThreads) void norm_join_kernel(const NormArgs a) {
   const int64_t at = (int64_t)blockIdx.x * (kThreads / 64) + (threadIdx.x >> 6);
   if (at >= (int64_t)a.segments * a.groups) return;
   const int32_t b = (int32_t)(at / a.groups), g = (int32_t)(at % a.groups);
   const int64_t lo = seg_row(a, b), hi = seg_row(a, b + 1);
-  const double2 s = join_parts(a, b, g, lo, hi);
+  const float2 s = moments(a, join_parts(a, b, g, lo, hi), hi - lo);
   if ((threadIdx.x & 63) == 0) {
-    const double n = hi > lo ? (double)(hi - lo) * a.D : 1.;
-    const double mean = s.x / n, var = s.y / n - mean * mean;
-    a.mean[at] = (float)mean;
-    a.rstd[at] = (float)(1. / sqrt((var < 0. ? 0. : var) + a.eps));
+    a.mean[at] = s.x;
+    a.rstd[at] = s.y;
   }
+}
+
+// The same inside a workgroup that writes rows of segment b: of(sums, rows) of each group into `out`
+template <typename F>
+__device__ __forceinline__ void join_here(const NormArgs& a, int32_t b, float2* out, F of) {
+  const int64_t lo = seg_row(a, b), hi = seg_row(a, b + 1);
+  __syncthreads();
+  for (int32_t g = threadIdx.x >> 6; g < a.groups; g += kThreads / 64) {
+    const float2 s = of(join_parts(a, b, g, lo, hi), hi - lo);
+    if ((threadIdx.x & 63) == 0) out[g] = s;
+  }
+  __syncthreads();
 }
 
 // What a vector's channels make of its values: z = scale x + shift, (x - mean) rstd = rstd x + base.  (A mean far from zero costs
@@ -293,6 +317,16 @@ struct Channel {
       const int64_t g = (int64_t)b * a.groups + (ch + i) / a.D;
       rstd[i] = a.rstd[g];
       base[i] = a.mean[g];
+    }
+    affine(a, ch);
+  }
+  // (of a vector's groups, N = V)
+  __device__ __forceinline__ void read(const NormArgs& a, const float2* moments, int ch) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const float2 m = moments[(ch + i) / a.D];
+      base[i] = m.x;
+      rstd[i] = m.y;
     }
     affine(a, ch);
   }
@@ -312,9 +346,27 @@ template <typename S, int V, int ACT>
 __global__ __launch_bounds__(kThreads) void norm_write_kernel(const NormArgs a) {
   const S* X = reinterpret_cast<const S*>(a.X);
   S* Y = reinterpret_cast<S*>(a.Y);
+  extern __shared__ __attribute__((aligned(16))) char smem[];
+  float2* here = reinterpret_cast<float2*>(smem);
+  if (a.joined && blockIdx.x == 0)                          // (segments without rows are nobody's)
+    for (int b = 0; b < a.segments; ++b)
+      if (seg_row(a, b + 1) <= seg_row(a, b))
+        for (int g = threadIdx.x; g < a.groups; g += kThreads) {
+          const float2 s = moments(a, make_double2(0., 0.), 0);
+          a.mean[b * a.groups + g] = s.x;
+          a.rstd[b * a.groups + g] = s.y;
+        }
   // (last chunk first: what was read last is still in the caches)
   each_part(a, a.chunks - 1 - blockIdx.x, [&](int32_t b, int64_t r0, int64_t r1) {
     const bool none = b < 0 || b >= a.segments;
+    if (a.joined && !none) {
+      join_here(a, b, here, [&](double2 s, int64_t rows) { return moments(a, s, rows); });
+      if (r0 == seg_row(a, b))
+        for (int g = threadIdx.x; g < a.groups; g += kThreads) {
+          a.mean[b * a.groups + g] = here[g].x;
+          a.rstd[b * a.groups + g] = here[g].y;
+        }
+    }
     for (int vec0 = 0; vec0 * V < a.C; vec0 += kThreads) {
       const Lay l = lay<V>(a, vec0);
       if (l.ty >= l.rows) continue;
@@ -324,7 +376,8 @@ __global__ __launch_bounds__(kThreads) void norm_write_kernel(const NormArgs a) 
         continue;
       }
       Channel<V, V> k;
-      k.read(a, b, ch);
+      if (a.joined) k.read(a, here, ch);
+      else k.read(a, b, ch);
       each_row<4>(r0 + l.ty, r1, l.rows, [&](int64_t r) { return fetch<S, V>(X + r * a.ldx + ch); }, [&](int64_t r, const Whole<S, V>& w) {
         float y[V];
 #pragma unroll
@@ -405,47 +458,52 @@ __global__ __launch_bounds__(kThreads) void norm_bwd_sum_kernel(const NormArgs a
     for (int x = threadIdx.x; x < a.C; x += kThreads) a.rows[c * a.C + x] = make_float2(0.f, 0.f);
 }
 
-// Workgroups below `wide`: sixteen channels of gamma and beta each, 64 rows of the table at a time; the others: a segment and group
-// for each wavefront.  (With a row of 64 channels for each of four wavefronts 1037 rows took 67 us.)
+// Sixteen channels of gamma and beta: the rows of the table, THREADS / 16 at a time.  (With 64 channels for four wavefronts 1037
+// rows took 67 us.)
+template <int THREADS>
+__device__ __forceinline__ void join_rows(const NormArgs& a, int32_t block) {
+  __shared__ double2 sm[THREADS / 64][16];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int ch = block * 16 + (threadIdx.x & 15);
+  double2 s = make_double2(0., 0.);
+  if (ch < a.C) {
+    const float2* p = a.rows + ch;
+#pragma unroll 8
+    for (int64_t c = threadIdx.x >> 4; c < a.table; c += THREADS / 16) {
+      const float2 v = p[c * a.C];
+      s.x += v.x;
+      s.y += v.y;
+    }
+  }
+  for (int d = 16; d < 64; d *= 2) {
+    s.x += __shfl_xor(s.x, d);
+    s.y += __shfl_xor(s.y, d);
+  }
+  if (lane < 16) sm[wave][lane] = s;
+  __syncthreads();
+  if (threadIdx.x < 16 && ch < a.C) {
+    for (int w = 1; w < THREADS / 64; ++w) {
+      s.x += sm[w][lane].x;
+      s.y += sm[w][lane].y;
+    }
+    if (a.dgamma) a.dgamma[ch] = (float)s.x;
+    if (a.dbeta) a.dbeta[ch] = (float)s.y;
+  }
+}
+
+// Workgroups below `wide` join the rows of the table, the others a segment and group for each wavefront.
 constexpr int kJoinThreads = 1024;
 __global__ __launch_bounds__(kJoinThreads) void norm_bwd_join_kernel(const NormArgs a, int32_t wide) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   if ((int)blockIdx.x < wide) {
-    __shared__ double2 sm[kJoinThreads / 64][16];
-    const int ch = (int)blockIdx.x * 16 + (threadIdx.x & 15);
-    double2 s = make_double2(0., 0.);
-    if (ch < a.C) {
-      const float2* p = a.rows + ch;
-#pragma unroll 8
-      for (int64_t c = threadIdx.x >> 4; c < a.table; c += kJoinThreads / 16) {
-        const float2 v = p[c * a.C];
-        s.x += v.x;
-        s.y += v.y;
-      }
-    }
-    for (int d = 16; d < 64; d *= 2) {
-      s.x += __shfl_xor(s.x, d);
-      s.y += __shfl_xor(s.y, d);
-    }
-    if (lane < 16) sm[wave][lane] = s;
-    __syncthreads();
-    if (threadIdx.x < 16 && ch < a.C) {
-      for (int w = 1; w < kJoinThreads / 64; ++w) {
-        s.x += sm[w][lane].x;
-        s.y += sm[w][lane].y;
-      }
-      if (a.dgamma) a.dgamma[ch] = (float)s.x;
-      if (a.dbeta) a.dbeta[ch] = (float)s.y;
-    }
+    join_rows<kJoinThreads>(a, (int32_t)blockIdx.x);
     return;
   }
-  const int64_t at = (int64_t)(blockIdx.x - wide) * (kJoinThreads / 64) + wave;
+  const int64_t at = (int64_t)(blockIdx.x - wide) * (kJoinThreads / 64) + (threadIdx.x >> 6);
   if (at >= (int64_t)a.segments * a.groups) return;
   const int32_t b = (int32_t)(at / a.groups), g = (int32_t)(at % a.groups);
   const int64_t lo = seg_row(a, b), hi = seg_row(a, b + 1);
-  const double2 s = join_parts(a, b, g, lo, hi);
-  const double n = hi > lo ? (double)(hi - lo) * a.D : 1.;
-  if (lane == 0) a.sums[at] = make_float2((float)(s.x / n), (float)(s.y / n));
+  const float2 s = means(a, join_parts(a, b, g, lo, hi), hi - lo);
+  if ((threadIdx.x & 63) == 0) a.sums[at] = s;
 }
 
 // dx = h gamma rstd - rstd s1 - rstd s2 (rstd x + base) = h scale + tilt x + level, s1 and s2 the means of the group's sums
@@ -459,9 +517,15 @@ __global__ __launch_bounds__(kThreads) void norm_bwd_write_kernel(const NormArgs
   const S* X = reinterpret_cast<const S*>(a.X);
   const S* G = reinterpret_cast<const S*>(a.G);
   S* Y = reinterpret_cast<S*>(a.Y);
-  // (last chunk first: what was read last is still in the caches)
+  extern __shared__ __attribute__((aligned(16))) char smem[];
+  float2* here = reinterpret_cast<float2*>(smem);
+  if ((int64_t)blockIdx.x >= a.chunks) {                    // (where there is no launch between for it)
+    join_rows<kThreads>(a, (int32_t)(blockIdx.x - a.chunks));
+    return;
+  }
   each_part(a, a.chunks - 1 - blockIdx.x, [&](int32_t b, int64_t r0, int64_t r1) {
     const bool none = b < 0 || b >= a.segments;
+    if (a.joined && !none) join_here(a, b, here, [&](double2 s, int64_t rows) { return means(a, s, rows); });
     for (int vec0 = 0; vec0 * V < a.C; vec0 += kThreads) {
       const Lay l = lay<V>(a, vec0);
       if (l.ty >= l.rows) continue;
@@ -474,7 +538,7 @@ __global__ __launch_bounds__(kThreads) void norm_bwd_write_kernel(const NormArgs
       k.read(a, b, ch);
       float tilt[V], level[V];
 #pragma unroll
-      for (int i = 0; i < V; ++i) input_line(k.rstd[i], k.base[i], a.sums[(int64_t)b * a.groups + (ch + i) / a.D], tilt[i], level[i]);
+      for (int i = 0; i < V; ++i) input_line(k.rstd[i], k.base[i], a.joined ? here[(ch + i) / a.D] : a.sums[(int64_t)b * a.groups + (ch + i) / a.D], tilt[i], level[i]);
       each_row<2>(r0 + l.ty, r1, l.rows, [&](int64_t r) { return Two<S, V>{fetch<S, V>(X + r * a.ldx + ch), fetch<S, V>(G + r * a.ldg + ch)}; },
                   [&](int64_t r, const Two<S, V>& w) {
         float y[V];
@@ -813,8 +877,8 @@ WholePlan whole_plan(int64_t m, int64_t max_rows, int32_t C, int32_t D, int v, i
   const int64_t all = ceil_div(C, unit);
   if (units > all) units = all;
   units = ceil_div(all, ceil_div(all, units));              // slabs of like width
-  // less than a cache line of a row for each workgroup reads lines twice
-  if (units < all && units * unit * size < 128) return w;
+  // less than a cache line of a row for each workgroup reads lines twice: where the L2s do not have them the second time
+  if (units < all && units * unit * size < 128 && m * C * size > (4 << 20)) return w;
   w.slab = (int32_t)(units * unit);
   w.slabs = (int32_t)ceil_div(C, w.slab);
   const int64_t vectors = rows * (w.slab / v);
@@ -826,7 +890,7 @@ size_t whole_lds(const WholePlan& w, int32_t D, int v, bool backward) {
 }
 
 // How a call is carried out, and what it needs for that
-struct NormForm { WholePlan whole; NormPlan parts; int64_t table; size_t bytes; };
+struct NormForm { WholePlan whole; NormPlan parts; int64_t table; bool joined; size_t bytes; };
 NormForm norm_form(int32_t dtype, int64_t m, int32_t segments, int64_t max_rows, int32_t C, int32_t groups, int64_t ld, bool backward) {
   NormForm f{};
   const int32_t D = C / groups;
@@ -842,6 +906,9 @@ NormForm norm_form(int32_t dtype, int64_t m, int32_t segments, int64_t max_rows,
     f.parts = norm_plan(m, segments, C, groups, backward);
     f.table = m > 0 ? f.parts.chunks : 0;
     f.bytes = f.parts.total;
+    // A launch less, some ten microseconds, where every workgroup can join its segments' parts: 128 KB of them at most, and few
+    // segments (170003 x 100, four groups, backward 84 -> 68 us; 2 M x 256 in 32 groups would read 134 MB of sums for it).
+    f.joined = m > 0 && segments <= 64 && f.parts.chunks * groups <= 8192;
   }
   return f;
 }
@@ -903,7 +970,7 @@ SAGNN_EXPORT int group_norm_act_fwd(int32_t dtype, const void* d_X, int64_t ldx,
   NormArgs a{};
   a.X = d_X; a.ldx = ldx; a.Y = d_Y; a.ldy = ldy; a.seg = d_seg; a.segments = n_seg; a.each = m / n_seg; a.m = m; a.C = C; a.groups = n_groups;
   a.D = C / n_groups; a.gamma = d_gamma; a.beta = d_beta; a.mean = d_mean; a.rstd = d_rstd; a.eps = eps; a.act = act;
-  a.chunk = p.chunk; a.chunks = p.chunks; a.parts = (double2*)((char*)d_ws + p.parts); a.slab = w.slab;
+  a.chunk = p.chunk; a.chunks = p.chunks; a.parts = (double2*)((char*)d_ws + p.parts); a.slab = w.slab; a.joined = f.joined;
   hipStream_t s = (hipStream_t)stream;
   return by_act(act, [&](auto A) { return by_vector(dtype, vector_of(dtype, C), [&](auto V, auto zero) {
     constexpr int v = decltype(V)::value, ACT = decltype(A)::value;
@@ -919,10 +986,12 @@ SAGNN_EXPORT int group_norm_act_fwd(int32_t dtype, const void* d_X, int64_t ldx,
       norm_sum_kernel<S, v><<<dim3((uint32_t)p.chunks), kThreads, (size_t)n_groups * 16 + kThreads * v * 16, s>>>(a);
       SAGNN_LAUNCH_CHECK();
     }
-    norm_join_kernel<<<dim3((uint32_t)ceil_div((int64_t)n_seg * n_groups, kThreads / 64)), kThreads, 0, s>>>(a);
-    SAGNN_LAUNCH_CHECK();
+    if (!a.joined) {
+      norm_join_kernel<<<dim3((uint32_t)ceil_div((int64_t)n_seg * n_groups, kThreads / 64)), kThreads, 0, s>>>(a);
+      SAGNN_LAUNCH_CHECK();
+    }
     if (m > 0) {
-      norm_write_kernel<S, v, ACT><<<dim3((uint32_t)p.chunks), kThreads, 0, s>>>(a);
+      norm_write_kernel<S, v, ACT><<<dim3((uint32_t)p.chunks), kThreads, (size_t)n_groups * sizeof(float2), s>>>(a);
       SAGNN_LAUNCH_CHECK();
     }
     return (int)SAGNN_OK;
@@ -951,7 +1020,7 @@ SAGNN_EXPORT int group_norm_act_bwd(int32_t dtype, const void* d_X, int64_t ldx,
   a.C = C; a.groups = n_groups; a.D = C / n_groups; a.gamma = d_gamma; a.beta = d_beta; a.mean = const_cast<float*>(d_mean);
   a.rstd = const_cast<float*>(d_rstd); a.act = act; a.dgamma = d_dgamma; a.dbeta = d_dbeta; a.chunk = p.chunk; a.chunks = p.chunks;
   a.parts = (double2*)((char*)d_ws + p.parts); a.sums = (float2*)((char*)d_ws + p.sums); a.rows = (float2*)((char*)d_ws + p.rows);
-  a.table = f.table; a.slab = w.slab;
+  a.table = f.table; a.slab = w.slab; a.joined = f.joined;
   hipStream_t s = (hipStream_t)stream;
   return by_act(act, [&](auto A) { return by_vector(dtype, vector_of(dtype, C), [&](auto V, auto zero) {
     constexpr int v = decltype(V)::value, ACT = decltype(A)::value;
@@ -972,10 +1041,12 @@ SAGNN_EXPORT int group_norm_act_bwd(int32_t dtype, const void* d_X, int64_t ldx,
       norm_bwd_sum_kernel<S, v, ACT><<<dim3((uint32_t)p.chunks), kThreads, (size_t)n_groups * 16 + kThreads * v * 16, s>>>(a);
       SAGNN_LAUNCH_CHECK();
     }
-    norm_bwd_join_kernel<<<dim3((uint32_t)(wide + ceil_div((int64_t)n_seg * n_groups, kJoinThreads / 64))), kJoinThreads, 0, s>>>(a, wide);
-    SAGNN_LAUNCH_CHECK();
+    if (!a.joined) {
+      norm_bwd_join_kernel<<<dim3((uint32_t)(wide + ceil_div((int64_t)n_seg * n_groups, kJoinThreads / 64))), kJoinThreads, 0, s>>>(a, wide);
+      SAGNN_LAUNCH_CHECK();
+    }
     if (m > 0) {
-      norm_bwd_write_kernel<S, v, ACT><<<dim3((uint32_t)p.chunks), kThreads, 0, s>>>(a);
+      norm_bwd_write_kernel<S, v, ACT><<<dim3((uint32_t)(p.chunks + (a.joined ? wide : 0))), kThreads, (size_t)n_groups * sizeof(float2), s>>>(a);
       SAGNN_LAUNCH_CHECK();
     }
     return (int)SAGNN_OK;

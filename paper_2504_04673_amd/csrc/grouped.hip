@@ -55,7 +55,7 @@ struct TileCost { double rate, ends; };
 TileCost tile_cost(int32_t dtype, int32_t prec, int tile) {
   static constexpr TileCost fp32[kGroupedTiles] = {{1., 48}, {.98, 24}, {.91, 12}, {.95, 8}, {.85, 16}, {0, 0}, {0, 0}, {0, 0}};
   static constexpr TileCost rounded[kGroupedTiles] = {{1., 128}, {.76, 128}, {.62, 32}, {.49, 8}, {.25, 16}, {0, 0}, {1.08, 160}, {1.08, 160}};
-  static constexpr TileCost split[kGroupedTiles] = {{1., 33}, {.87, 24}, {.67, 8}, {.76, 8}, {.65, 8}, {0, 0}, {1.18, 54}, {1.18, 54}};
+  static constexpr TileCost split[kGroupedTiles] = {{1., 48}, {.87, 24}, {.67, 8}, {.76, 8}, {.65, 8}, {0, 0}, {1.18, 54}, {1.18, 54}};
   static constexpr TileCost bf16[kGroupedTiles] = {{1., 128}, {.81, 128}, {.66, 32}, {.66, 32}, {.39, 32}, {1.69, 350}, {0, 0}, {0, 0}};
   return dtype == SAGNN_BF16 ? bf16[tile] : prec == SAGNN_GEMM_FP32 ? fp32[tile] : prec == SAGNN_GEMM_BF16 ? rounded[tile] : split[tile];
 }
