@@ -167,12 +167,12 @@ struct TileLoad {
 
   // the tile at `base` (leading dimension ld), of which `rows` rows and `sum` of the summed index are there (both
   // may exceed the tile; at least one of each).  Zeros beyond `sum`; rows beyond `rows` are zeros or any row's.
-  __device__ __forceinline__ void load(const S* __restrict__ base, int64_t ld, int rows, int sum) {
+  __device__ __forceinline__ void load(const S* __restrict__ base, int64_t ld, int rows, int sum, int tid) {
     const int outer_end = TR ? sum : rows, inner_end = TR ? rows : sum;
     if (inner_end >= Shape::kInner && (!TR || sum >= BK)) {
 #pragma unroll
       for (int u = 0; u < N; ++u) {
-        const int w = threadIdx.x + u * THREADS;
+        const int w = tid + u * THREADS;
         int o = w / kPerRow;
         if (!TR) o = o < outer_end ? o : outer_end - 1;
         const S* p = base + (int64_t)o * ld + (w % kPerRow) * V;
@@ -183,7 +183,7 @@ struct TileLoad {
     }
 #pragma unroll
     for (int u = 0; u < N; ++u) {
-      const int w = threadIdx.x + u * THREADS, o = w / kPerRow, i = (w % kPerRow) * V;
+      const int w = tid + u * THREADS, o = w / kPerRow, i = (w % kPerRow) * V;
       const int there = o < outer_end ? inner_end - i : 0;
       const S* p = base + (int64_t)o * ld + i;
       if (there >= V) {
@@ -195,10 +195,10 @@ struct TileLoad {
     }
   }
 
-  __device__ __forceinline__ void store(char* smem) const {
+  __device__ __forceinline__ void store(char* smem, int tid) const {
 #pragma unroll
     for (int u = 0; u < N; ++u) {
-      const int w = threadIdx.x + u * THREADS, at = (w / kPerRow) * Shape::kPitch + (w % kPerRow) * V;
+      const int w = tid + u * THREADS, at = (w / kPerRow) * Shape::kPitch + (w % kPerRow) * V;
       if constexpr (PREC == SAGNN_GEMM_FP32) {
         *reinterpret_cast<Vec*>(reinterpret_cast<float*>(smem) + at) = v[u];
       } else if constexpr (sizeof(S) == 2) {
@@ -241,10 +241,10 @@ __device__ __forceinline__ bf16x8 tile_operand(const __bf16* tile, int row0, int
 
 // acc += A B over one staged step.  The workgroup's WM x WN wavefronts own TM x TN tiles of 32 x 32 each.
 template <int PREC, bool TRA, bool TRB, int WM, int WN, int TM, int TN, int BK>
-__device__ __forceinline__ void tile_multiply(const char* sa, const char* sb, floatx16 (&acc)[TM][TN]) {
+__device__ __forceinline__ void tile_multiply(const char* sa, const char* sb, floatx16 (&acc)[TM][TN], int tid) {
   using SA = TileShape<PREC, TRA, WM * TM * 32, BK>;
   using SB = TileShape<PREC, TRB, WN * TN * 32, BK>;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int lane = tid & 63, wave = tid >> 6;
   const int ra = (wave / WN) * TM * 32, rb = (wave % WN) * TN * 32;
   if constexpr (PREC == SAGNN_GEMM_FP32) {
     const float* A = reinterpret_cast<const float*>(sa);
@@ -274,7 +274,7 @@ __device__ __forceinline__ void tile_multiply(const char* sa, const char* sb, fl
         for (int tm = 0; tm < TM; ++tm)
 #pragma unroll
           for (int tn = 0; tn < TN; ++tn)
-            acc[tm][tn] = __builtin_amdgcn_mfma_f32_32x32x2f32(x[tm][i], y[tn][i], acc[tm][tn], 0, 0, 0);
+            acc[tm][tn] = __builtin_amdgcn_mfma_f32_32x32x2f32(y[tn][i], x[tm][i], acc[tm][tn], 0, 0, 0);
     }
   } else {
     const __bf16* A = reinterpret_cast<const __bf16*>(sa);
@@ -298,7 +298,7 @@ __device__ __forceinline__ void tile_multiply(const char* sa, const char* sb, fl
         for (int tm = 0; tm < TM; ++tm)
 #pragma unroll
           for (int tn = 0; tn < TN; ++tn)
-            acc[tm][tn] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x[pair[s][0]][tm], y[pair[s][1]][tn], acc[tm][tn], 0, 0, 0);
+            acc[tm][tn] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(y[pair[s][1]][tn], x[pair[s][0]][tm], acc[tm][tn], 0, 0, 0);
     }
   }
 }
@@ -320,35 +320,65 @@ __device__ __forceinline__ void tile_product(const S* A, int64_t lda, int rows, 
       for (int v = 0; v < 16; ++v) acc[tm][tn][v] = 0.f;
   if (sum <= 0) return;
   auto left = [&](int64_t k) { return (int)(sum - k < BK ? sum - k : BK); };
-  la.load(A, lda, rows, left(0));
-  lb.load(B, ldb, cols, left(0));
+  const int tid = threadIdx.x;
+  la.load(A, lda, rows, left(0), tid);
+  lb.load(B, ldb, cols, left(0), tid);
   for (int64_t k = 0; k < sum; k += BK) {
-    la.store(smem);
-    lb.store(smem + SA::kBytes);
+    la.store(smem, tid);
+    lb.store(smem + SA::kBytes, tid);
     __syncthreads();
     if (k + BK < sum) {
-      la.load(A + (k + BK) * (TRA ? lda : 1), lda, rows, left(k + BK));
-      lb.load(B + (k + BK) * (TRB ? ldb : 1), ldb, cols, left(k + BK));
+      la.load(A + (k + BK) * (TRA ? lda : 1), lda, rows, left(k + BK), tid);
+      lb.load(B + (k + BK) * (TRB ? ldb : 1), ldb, cols, left(k + BK), tid);
     }
-    tile_multiply<PREC, TRA, TRB, WM, WN, TM, TN, BK>(smem, smem + SA::kBytes, acc);
+    tile_multiply<PREC, TRA, TRB, WM, WN, TM, TN, BK>(smem, smem + SA::kBytes, acc, tid);
     __syncthreads();
   }
 }
 
-// f(row, column, sum) of the values that a lane holds, rows and columns relative to the workgroup's tile
+// f(row, column, sums) of what a lane holds, four neighbouring columns of a row at a time (the products are taken transposed for
+// that), relative to the workgroup's tile
 template <int WM, int WN, int TM, int TN, typename F>
-__device__ __forceinline__ void tile_each(floatx16 (&acc)[TM][TN], F f) {
+__device__ __forceinline__ void tile_fours(floatx16 (&acc)[TM][TN], F f) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
 #pragma unroll
   for (int tm = 0; tm < TM; ++tm)
 #pragma unroll
-    for (int v = 0; v < 16; ++v)
+    for (int tn = 0; tn < TN; ++tn)
 #pragma unroll
-      for (int tn = 0; tn < TN; ++tn) {
-        float y = acc[tm][tn][v];
-        f(((wave / WN) * TM + tm) * 32 + 8 * (v / 4) + 4 * (lane >> 5) + v % 4, ((wave % WN) * TN + tn) * 32 + (lane & 31), y);
-        acc[tm][tn][v] = y;
+      for (int v = 0; v < 16; v += 4) {
+        float y[4] = {acc[tm][tn][v], acc[tm][tn][v + 1], acc[tm][tn][v + 2], acc[tm][tn][v + 3]};
+        f(((wave / WN) * TM + tm) * 32 + (lane & 31), ((wave % WN) * TN + tn) * 32 + 2 * v + 4 * (lane >> 5), y);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) acc[tm][tn][v + i] = y[i];
       }
+}
+// Four values at p, of which `there` are inside (any alignment)
+template <typename S>
+struct __attribute__((packed)) Four { S x[4]; };
+template <typename S>
+__device__ __forceinline__ void store_four(S* p, const float (&y)[4], int there) {
+  if (there >= 4) {
+    struct __attribute__((aligned(sizeof(S) * 4))) Whole { S x[4]; } w = {(S)y[0], (S)y[1], (S)y[2], (S)y[3]};
+    __builtin_memcpy(reinterpret_cast<Four<S>*>(p), &w, sizeof(w));
+  } else {
+#pragma unroll
+    for (int i = 0; i < 3; ++i)
+      if (i < there) p[i] = (S)y[i];
+  }
+}
+template <typename S>
+__device__ __forceinline__ void mask_four(const S* p, float (&y)[4], int there) {
+  if (there >= 4) {
+    struct __attribute__((aligned(sizeof(S) * 4))) Whole { S x[4]; } w;
+    __builtin_memcpy(&w, reinterpret_cast<const Four<S>*>(p), sizeof(w));
+#pragma unroll
+    for (int i = 0; i < 4; ++i) y[i] = (float)w.x[i] > 0.f ? y[i] : 0.f;
+  } else {
+#pragma unroll
+    for (int i = 0; i < 3; ++i)
+      if (i < there) y[i] = (float)p[i] > 0.f ? y[i] : 0.f;
+  }
 }
 
 // Results of a tile at row r0, column c0 -> Y, through activation and mask
@@ -358,13 +388,13 @@ __device__ __forceinline__ void tile_store(const GroupedArgs& a, int64_t r0, int
   const bool relu = a.act == SAGNN_ACT_RELU;
   if (a.mask) {                                 // (all loads ahead of the stores, which the compiler could not pass)
     const S* mask = reinterpret_cast<const S*>(a.mask) + r0 * a.ldmask + c0;
-    tile_each<WM, WN, TM, TN>(acc, [&](int r, int c, float& y) {
-      const S z = mask[(int64_t)(r < rows ? r : rows - 1) * a.ldmask + (c < cols ? c : cols - 1)];
-      y = (float)z > 0.f ? y : 0.f;
-    });
+    tile_fours<WM, WN, TM, TN>(acc, [&](int r, int c, float (&y)[4]) { if (r < rows) mask_four(mask + (int64_t)r * a.ldmask + c, y, cols - c); });
   }
-  tile_each<WM, WN, TM, TN>(acc, [&](int r, int c, float& y) {
-    if (r < rows && c < cols) Y[(int64_t)r * a.ldy + c] = (S)(relu && y < 0.f ? 0.f : y);
+  tile_fours<WM, WN, TM, TN>(acc, [&](int r, int c, float (&y)[4]) {
+    if (relu)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) y[i] = y[i] < 0.f ? 0.f : y[i];
+    if (r < rows) store_four(Y + (int64_t)r * a.ldy + c, y, cols - c);
   });
 }
 
@@ -384,6 +414,76 @@ __global__ __launch_bounds__(WM * WN * 64) void grouped_kernel(const GroupedArgs
   tile_store<S, WM, WN, TM, TN>(a, t.r0, c0, rows, cols, acc);
 }
 
+// Few rows of a group, or few tiles for the CUs: a workgroup's wavefronts share the summed index of one tile of 32 rows instead of
+// the tile, each through a part of LDS of its own, and their sums are added in LDS at the end.  Bound by the chain of
+// loads of a wavefront, which is WAVES times shorter (3 rows, 2211 x 228 of 28 groups: 70 us by 32 x 128, 19 this way; 44 columns' gradient for
+// 1000 rows of 46 groups, 1066 deep: 36 and 12).
+template <typename S, int PREC, bool WT, int TN, int WAVES, int BK>
+__global__ __launch_bounds__(WAVES * 64) void grouped_thin_kernel(const GroupedArgs a) {
+  constexpr int BN = TN * 32, kRow = BN + 4;
+  using SA = TileShape<PREC, false, 32, BK>;
+  using SB = TileShape<PREC, !WT, BN, BK>;
+  constexpr int kOwn = SA::kBytes + SB::kBytes, kSums = 32 * kRow * 4;
+  __shared__ __attribute__((aligned(16))) char smem[WAVES * (kOwn > kSums ? kOwn : kSums)];
+  GroupTile t;
+  int32_t col;
+  if (!grouped_find<32>(a, t, col)) return;
+  const int64_t c0 = (int64_t)col * BN;
+  const int rows = (int)(t.end - t.r0 < 32 ? t.end - t.r0 : 32), cols = (int)(a.nout - c0 < BN ? a.nout - c0 : BN);
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const S* X = reinterpret_cast<const S*>(a.X) + t.r0 * a.ldx;
+  const S* W = reinterpret_cast<const S*>(a.W) + (t.g < a.groups ? t.g * a.stride_w : 0) + c0 * (WT ? a.ldw : 1);
+  floatx16 acc[1][TN];
+#pragma unroll
+  for (int tn = 0; tn < TN; ++tn)
+#pragma unroll
+    for (int v = 0; v < 16; ++v) acc[0][tn][v] = 0.f;
+  TileLoad<S, PREC, false, 32, BK, 64> la;
+  TileLoad<S, PREC, !WT, BN, BK, 64> lb;
+  const int sum = t.g < a.groups ? a.kdim : 0;
+  char* own = smem + wave * kOwn;
+  auto load = [&](int k) {
+    la.load(X + k, a.ldx, rows, sum - k < BK ? sum - k : BK, lane);
+    lb.load(W + (int64_t)k * (WT ? 1 : a.ldw), a.ldw, cols, sum - k < BK ? sum - k : BK, lane);
+  };
+  int k = wave * BK;
+  if (k < sum) load(k);
+  for (; k < sum; k += WAVES * BK) {
+    la.store(own, lane);
+    lb.store(own + SA::kBytes, lane);
+    asm volatile("" ::: "memory");                // (a wavefront's own LDS accesses are in order)
+    if (k + WAVES * BK < sum) load(k + WAVES * BK);
+    tile_multiply<PREC, false, !WT, 1, 1, 1, TN, BK>(own, own + SA::kBytes, acc, lane);
+    asm volatile("" ::: "memory");
+  }
+  __syncthreads();
+  float* sums = reinterpret_cast<float*>(smem);
+#pragma unroll
+  for (int tn = 0; tn < TN; ++tn)
+#pragma unroll
+    for (int v = 0; v < 16; v += 4)
+      *reinterpret_cast<float4*>(sums + (wave * 32 + (lane & 31)) * kRow + tn * 32 + 2 * v + 4 * (lane >> 5)) =
+          make_float4(acc[0][tn][v], acc[0][tn][v + 1], acc[0][tn][v + 2], acc[0][tn][v + 3]);
+  __syncthreads();
+  S* Y = reinterpret_cast<S*>(a.Y) + t.r0 * a.ldy + c0;
+  const S* mask = a.mask ? reinterpret_cast<const S*>(a.mask) + t.r0 * a.ldmask + c0 : nullptr;
+  for (int u = threadIdx.x; u < 32 * (BN / 4); u += WAVES * 64) {
+    const int r = u / (BN / 4), c = u % (BN / 4) * 4;
+    if (r >= rows || c >= cols) continue;
+    float y[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int w = 0; w < WAVES; ++w) {
+      const float4 x = *reinterpret_cast<const float4*>(sums + (w * 32 + r) * kRow + c);
+      y[0] += x.x; y[1] += x.y; y[2] += x.z; y[3] += x.w;
+    }
+    if (a.act == SAGNN_ACT_RELU)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) y[i] = y[i] < 0.f ? 0.f : y[i];
+    if (mask) mask_four(mask + (int64_t)r * a.ldmask + c, y, cols - c);
+    store_four(Y + (int64_t)r * a.ldy + c, y, cols - c);
+  }
+}
+
 template <typename S, int PREC, int WM, int WN, int TM, int TN, int BK>
 __global__ __launch_bounds__(WM * WN * 64) void grouped_tn_kernel(const GroupedArgs a) {
   constexpr int BM = WM * TM * 32, BN = WN * TN * 32;
@@ -397,19 +497,18 @@ __global__ __launch_bounds__(WM * WN * 64) void grouped_tn_kernel(const GroupedA
   tile_product<S, PREC, true, true, WM, WN, TM, TN, BK>(reinterpret_cast<const S*>(a.X) + p.r0 * a.ldx + k0, a.ldx, rows,
                                                         reinterpret_cast<const S*>(a.G) + p.r0 * a.ldg + c0, a.ldg, cols, p.r1 - p.r0, smem, acc);
   float* out = (p.cut ? a.partial + grouped_partial_slot(p) * a.kdim * a.nout : a.dW + (int64_t)p.g * a.kdim * a.nout) + k0 * a.nout + c0;
-  tile_each<WM, WN, TM, TN>(acc, [&](int r, int c, float& y) {
-    if (r < rows && c < cols) out[(int64_t)r * a.nout + c] = y;
-  });
+  tile_fours<WM, WN, TM, TN>(acc, [&](int r, int c, float (&y)[4]) { if (r < rows) store_four(out + (int64_t)r * a.nout + c, y, cols - c); });
 }
 
+constexpr int kThinCols = 32;
 // Tiles that a launch can take, rows of X (of W for the weight gradient) by columns
-enum GroupedTile { kTile128, kTile128x64, kTile128x32, kTile64, kTile32x128, kDirect256, kStaged256x128, kStaged128x256, kGroupedTiles };
+enum GroupedTile { kTile128, kTile128x64, kTile128x32, kTile64, kTile32x128, kDirect256, kStaged256x128, kStaged128x256, kThin, kGroupedTiles };
 inline int grouped_tile_rows(int tile) {
-  constexpr int rows[kGroupedTiles] = {128, 128, 128, 64, 32, 256, 256, 128};
+  constexpr int rows[kGroupedTiles] = {128, 128, 128, 64, 32, 256, 256, 128, 32};
   return rows[tile];
 }
 inline int grouped_tile_cols(int tile) {
-  constexpr int cols[kGroupedTiles] = {128, 64, 32, 64, 128, 256, 128, 256};
+  constexpr int cols[kGroupedTiles] = {128, 64, 32, 64, 128, 256, 128, 256, kThinCols};
   return cols[tile];
 }
 
@@ -430,6 +529,7 @@ int grouped_launch(const GroupedArgs& a, int tile, int64_t blocks, hipStream_t s
   else if (tile == kTile128x64) grouped_kernel<S, PREC, WT, 2, 2, 2, 1, BK><<<grid, block, 0, s>>>(a);
   else if (tile == kTile128x32) grouped_kernel<S, PREC, WT, 4, 1, 1, 1, BK><<<grid, block, 0, s>>>(a);
   else if (tile == kTile64) grouped_kernel<S, PREC, WT, 2, 2, 1, 1, BK><<<grid, block, 0, s>>>(a);
+  else if (tile == kThin) grouped_thin_kernel<S, PREC, WT, kThinCols / 32, 8, BK == 32 && PREC != SAGNN_GEMM_FP32 ? 16 : BK><<<grid, 512, 0, s>>>(a);
   else grouped_kernel<S, PREC, WT, 1, 4, 1, 1, BK><<<grid, block, 0, s>>>(a);
   SAGNN_LAUNCH_CHECK();
   return SAGNN_OK;

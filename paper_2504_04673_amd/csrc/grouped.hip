@@ -53,10 +53,10 @@ enum { kAny = 0, kDirect = 1, kStaged = 2 };
 // beginning and end are worth.  Small tiles are several to a CU, which hides both; the large ones are alone there.
 struct TileCost { double rate, ends; };
 TileCost tile_cost(int32_t dtype, int32_t prec, int tile) {
-  static constexpr TileCost fp32[kGroupedTiles] = {{1., 48}, {.98, 24}, {.91, 12}, {.95, 8}, {.85, 16}, {0, 0}, {0, 0}, {0, 0}};
-  static constexpr TileCost rounded[kGroupedTiles] = {{1., 128}, {.76, 128}, {.62, 32}, {.49, 8}, {.25, 16}, {0, 0}, {1.08, 160}, {1.08, 160}};
-  static constexpr TileCost split[kGroupedTiles] = {{1., 48}, {.87, 24}, {.67, 8}, {.76, 8}, {.65, 8}, {0, 0}, {1.18, 54}, {1.18, 54}};
-  static constexpr TileCost bf16[kGroupedTiles] = {{1., 128}, {.81, 128}, {.66, 32}, {.66, 32}, {.39, 32}, {1.69, 350}, {0, 0}, {0, 0}};
+  static constexpr TileCost fp32[kGroupedTiles] = {{1., 48}, {.98, 24}, {.91, 12}, {.95, 8}, {.85, 16}, {0, 0}, {0, 0}, {0, 0}, {.78, 200}};
+  static constexpr TileCost rounded[kGroupedTiles] = {{1., 128}, {.76, 128}, {.62, 32}, {.49, 8}, {.25, 16}, {0, 0}, {1.08, 160}, {1.08, 160}, {.18, 200}};
+  static constexpr TileCost split[kGroupedTiles] = {{1., 48}, {.87, 24}, {.67, 8}, {.76, 8}, {.65, 8}, {0, 0}, {1.18, 54}, {1.18, 54}, {.46, 200}};
+  static constexpr TileCost bf16[kGroupedTiles] = {{1., 128}, {.81, 128}, {.66, 32}, {.66, 32}, {.39, 32}, {1.69, 200}, {0, 0}, {0, 0}, {.26, 200}};
   return dtype == SAGNN_BF16 ? bf16[tile] : prec == SAGNN_GEMM_FP32 ? fp32[tile] : prec == SAGNN_GEMM_BF16 ? rounded[tile] : split[tile];
 }
 
@@ -69,6 +69,7 @@ int choose_tile(int32_t dtype, int32_t prec, int ways, int64_t rows, int64_t par
   for (int tile = 0; tile < kGroupedTiles; ++tile) {
     const TileCost c = tile_cost(dtype, prec, tile);
     if (c.rate == 0 || (tile == kDirect256 && !(ways & kDirect)) || ((tile == kStaged256x128 || tile == kStaged128x256) && !(ways & kStaged))) continue;
+    if (tile == kThin && !whole) continue;
     const int64_t h = grouped_tile_rows(tile), w = grouped_tile_cols(tile);
     const int64_t tiles = (ceil_div(rows, h) + (parts < rows ? parts : rows) / 2) * ceil_div(cols, w) * times;
     const double turns = tiles <= 256 ? 1.25 : whole && tiles < 4 * 256 ? (double)ceil_div(tiles, 256) : tiles / 256.;

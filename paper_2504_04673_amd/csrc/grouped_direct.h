@@ -1,10 +1,10 @@
 // The grouped products of bfloat16 tensors whose rows begin on 16 bytes: operands go from memory into LDS without
 // passing through registers, several steps ahead of the matrix cores.
 //
-// Bound: the matrix cores where every weight meets a few hundred rows, the weights' traffic below that.  A wavefront owns
-// up to 128 x 128 of the result (256 accumulators a lane), since LDS has to deliver (rows + columns) of a wavefront's tile
-// for rows x columns of work: 64 bytes a cycle and CU at 128 x 128, twice that at 64 x 64, which is all LDS has.  Four
-// steps of 32 are in flight, so that a load has three steps' arithmetic to arrive.
+// Bound: the matrix cores where every weight meets a few hundred rows, the weights' traffic below that.  A workgroup owns 256 x 256 of
+// the result, eight wavefronts of 128 x 64: LDS has to deliver (rows + columns) of a wavefront's tile for rows x columns of
+// work, 96 bytes a cycle and CU at 128 x 64, 128 at 64 x 64.  Two wavefronts share a SIMD, so that one's products fill the
+// other's waits.  Four steps of 32 are in flight, so that a load has three steps' arithmetic to arrive.
 #pragma once
 #include "grouped.h"
 
@@ -98,8 +98,8 @@ struct DirectOperand {
 // acc[tm][tn] = (A B)^T tile by tile, over all steps: a lane holds four neighbouring columns of one row at a time.
 //
 // Two instructions' worth of operands: one is multiplied while the other is read.  What a wavefront issues besides its products
-// stands singly between them: a row of LDS reads or loads holds up the wavefront, and with it the matrix core, since there
-// is one wavefront for each (8192^3: 1950 cycles a step that way, 1450 this way; its products take 1024).
+// stands singly between them: a row of LDS reads or loads holds up the wavefront, and with it the matrix core (8192^3 in
+// wavefronts of 128 x 128: 1950 cycles a step that way, 1450 this way; its products take 1024).
 template <bool TRA, bool TRB, int WM, int WN, int TM, int TN>
 __device__ __forceinline__ void direct_product(const __bf16* A, int64_t lda, int rows, const __bf16* B, int64_t ldb, int cols, int64_t total,
                                                char* smem, floatx16 (&acc)[TM][TN]) {

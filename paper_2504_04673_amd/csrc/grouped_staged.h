@@ -148,7 +148,7 @@ __device__ __forceinline__ void staged_product(const float* A, int64_t lda, int 
 #pragma unroll
       for (int i = 0; i < kProducts; ++i) {
         const int s = i / (TM * TN) + 6 - kTerms, tm = i / TN % TM, tn = i % TN;
-        acc[tm][tn] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x[turn][pair[s][0]][tm], y[turn][pair[s][1]][tn], acc[tm][tn], 0, 0, 0);
+        acc[tm][tn] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(y[turn][pair[s][1]][tn], x[turn][pair[s][0]][tm], acc[tm][tn], 0, 0, 0);
         __builtin_amdgcn_sched_barrier(0);
         // behind the barrier the next step is there, and nobody reads this one any more
         if (turn == 1 && i == 0) asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
@@ -200,9 +200,7 @@ __global__ __launch_bounds__(WM * WN * 64) void grouped_staged_tn_kernel(const G
   staged_product<PREC, true, true, WM, WN, 2, 2>(reinterpret_cast<const float*>(a.X) + p.r0 * a.ldx + k0, a.ldx, rows,
                                                  reinterpret_cast<const float*>(a.G) + p.r0 * a.ldg + c0, a.ldg, cols, p.r1 - p.r0, smem, acc);
   float* out = (p.cut ? a.partial + grouped_partial_slot(p) * a.kdim * a.nout : a.dW + (int64_t)p.g * a.kdim * a.nout) + k0 * a.nout + c0;
-  tile_each<WM, WN, 2, 2>(acc, [&](int r, int c, float& y) {
-    if (r < rows && c < cols) out[(int64_t)r * a.nout + c] = y;
-  });
+  tile_fours<WM, WN, 2, 2>(acc, [&](int r, int c, float (&y)[4]) { if (r < rows) store_four(out + (int64_t)r * a.nout + c, y, cols - c); });
 }
 
 template <int PREC, int WM, int WN>
