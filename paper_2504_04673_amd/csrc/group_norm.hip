@@ -150,6 +150,34 @@ __device__ __forceinline__ Lay lay(const NormArgs& a, int vec0) {
   return l;
 }
 
+// As many neighbouring lanes to each of `groups` as `threads` threads have, a power of two up to 64; and their sum
+__device__ __forceinline__ int lanes_each(int groups, int threads) {
+  int lanes = 64;
+  while (lanes > 1 && threads / lanes < groups) lanes /= 2;
+  return lanes;
+}
+__device__ __forceinline__ void add_lanes(double2& s, int lanes) {
+  for (int d = lanes / 2; d; d /= 2) {
+    s.x += __shfl_xor(s.x, d);
+    s.y += __shfl_xor(s.y, d);
+  }
+}
+
+// Rows of `width` pairs in LDS, one behind the other, added into the first, by halves.  All threads call it; ends with a barrier.
+template <typename P>
+__device__ __forceinline__ void add_rows(P* sm, int rows, int width, int threads) {
+  __syncthreads();
+  while (rows > 1) {
+    const int half = (rows + 1) / 2;
+    for (int i = threadIdx.x; i < (rows - half) * width; i += threads) {
+      const P a = sm[i], b = sm[half * width + i];
+      sm[i] = P{a.x + b.x, a.y + b.y};
+    }
+    __syncthreads();
+    rows = half;
+  }
+}
+
 // Sums p[], q[] per thread and channel of a slab -> per group of channels, added to acc[group].  All threads call it.
 template <int V>
 __device__ __forceinline__ void to_groups(const NormArgs& a, const Lay& l, int c0, const double (&p)[V], const double (&q)[V], double2* sm,
@@ -159,41 +187,19 @@ __device__ __forceinline__ void to_groups(const NormArgs& a, const Lay& l, int c
   if (l.ty < l.rows)
 #pragma unroll
     for (int i = 0; i < V; ++i) sm[(l.ty * l.per_row + l.tx) * V + i] = make_double2(p[i], q[i]);
-  __syncthreads();
-  for (int c = threadIdx.x; c < width; c += kThreads) {
-    double2 s = sm[c];
-    for (int y = 1; y < l.rows; ++y) {
-      s.x += sm[y * width + c].x;
-      s.y += sm[y * width + c].y;
-    }
-    sm[c] = s;
-  }
-  __syncthreads();
-  const int g0 = c0 / a.D, g1 = (c0 + width - 1) / a.D;
-  if (a.D <= 16) {
-    for (int g = g0 + threadIdx.x; g <= g1; g += kThreads) {
-      double2 s = acc[g];
-      for (int c = g * a.D < c0 ? c0 : g * a.D; c < (g + 1) * a.D && c < c0 + width; ++c) {
+  add_rows(sm, l.rows, width, kThreads);
+  const int g0 = c0 / a.D, g1 = (c0 + width - 1) / a.D, lanes = lanes_each(g1 - g0 + 1, kThreads);
+  for (int g = g0 + threadIdx.x / lanes; g - (int)(threadIdx.x / lanes) <= g1; g += kThreads / lanes) {
+    double2 s = make_double2(0., 0.);
+    if (g <= g1)
+      for (int c = (g * a.D < c0 ? c0 : g * a.D) + threadIdx.x % lanes; c < (g + 1) * a.D && c < c0 + width; c += lanes) {
         s.x += sm[c - c0].x;
         s.y += sm[c - c0].y;
       }
-      acc[g] = s;
-    }
-  } else {
-    for (int g = g0 + (threadIdx.x >> 6); g <= g1; g += kThreads / 64) {
-      double2 s = make_double2(0., 0.);
-      for (int c = (g * a.D < c0 ? c0 : g * a.D) + (threadIdx.x & 63); c < (g + 1) * a.D && c < c0 + width; c += 64) {
-        s.x += sm[c - c0].x;
-        s.y += sm[c - c0].y;
-      }
-      for (int d = 32; d; d >>= 1) {
-        s.x += __shfl_xor(s.x, d);
-        s.y += __shfl_xor(s.y, d);
-      }
-      if ((threadIdx.x & 63) == 0) {
-        acc[g].x += s.x;
-        acc[g].y += s.y;
-      }
+    add_lanes(s, lanes);
+    if (g <= g1 && threadIdx.x % lanes == 0) {
+      acc[g].x += s.x;
+      acc[g].y += s.y;
     }
   }
 }
@@ -253,20 +259,18 @@ __global__ __launch_bounds__(kThreads) void norm_sum_kernel(const NormArgs a) {
   });
 }
 
-// Parts of a segment and group, added in their order (a lane every 64th, then the lanes)
-__device__ __forceinline__ double2 join_parts(const NormArgs& a, int32_t b, int32_t g, int64_t lo, int64_t hi) {
+// Parts of a segment and group, added by `lanes` neighbouring lanes: each every lanes-th, then the lanes
+__device__ __forceinline__ double2 join_parts(const NormArgs& a, int32_t b, int32_t g, int64_t lo, int64_t hi, int lanes) {
   double2 s = make_double2(0., 0.);
-  if (hi > lo)
+  if (hi > lo) {
 #pragma unroll 4
-    for (int64_t c = lo / a.chunk + (threadIdx.x & 63); c <= (hi - 1) / a.chunk; c += 64) {
+    for (int64_t c = lo / a.chunk + threadIdx.x % lanes; c <= (hi - 1) / a.chunk; c += lanes) {
       const double2 p = a.parts[(c + b) * a.groups + g];
       s.x += p.x;
       s.y += p.y;
     }
-  for (int d = 32; d; d >>= 1) {
-    s.x += __shfl_xor(s.x, d);
-    s.y += __shfl_xor(s.y, d);
   }
+  add_lanes(s, lanes);
   return s;
 }
 
@@ -287,7 +291,7 @@ __global__ __launch_bounds__(kThreads) void norm_join_kernel(const NormArgs a) {
   if (at >= (int64_t)a.segments * a.groups) return;
   const int32_t b = (int32_t)(at / a.groups), g = (int32_t)(at % a.groups);
   const int64_t lo = seg_row(a, b), hi = seg_row(a, b + 1);
-  const float2 s = moments(a, join_parts(a, b, g, lo, hi), hi - lo);
+  const float2 s = moments(a, join_parts(a, b, g, lo, hi, 64), hi - lo);
   if ((threadIdx.x & 63) == 0) {
     a.mean[at] = s.x;
     a.rstd[at] = s.y;
@@ -299,9 +303,10 @@ template <typename F>
 __device__ __forceinline__ void join_here(const NormArgs& a, int32_t b, float2* out, F of) {
   const int64_t lo = seg_row(a, b), hi = seg_row(a, b + 1);
   __syncthreads();
-  for (int32_t g = threadIdx.x >> 6; g < a.groups; g += kThreads / 64) {
-    const float2 s = of(join_parts(a, b, g, lo, hi), hi - lo);
-    if ((threadIdx.x & 63) == 0) out[g] = s;
+  const int lanes = lanes_each(a.groups, kThreads), first = threadIdx.x / lanes;
+  for (int32_t g = first; g - first < a.groups; g += kThreads / lanes) {      // (all lanes stay for the sums)
+    const float2 s = of(join_parts(a, b, g, lo, g < a.groups ? hi : lo, lanes), hi - lo);
+    if (g < a.groups && threadIdx.x % lanes == 0) out[g] = s;
   }
   __syncthreads();
 }
@@ -434,13 +439,9 @@ __global__ __launch_bounds__(kThreads) void norm_bwd_sum_kernel(const NormArgs a
       if (l.ty < l.rows)
 #pragma unroll
         for (int i = 0; i < V; ++i) sf[(l.ty * l.per_row + l.tx) * V + i] = make_float2(q[i], p[i]);
-      __syncthreads();
+      add_rows(sf, l.rows, width, kThreads);
       for (int x = threadIdx.x; x < width; x += kThreads) {
         float2 s = sf[x];
-        for (int y = 1; y < l.rows; ++y) {
-          s.x += sf[y * width + x].x;
-          s.y += sf[y * width + x].y;
-        }
         float2* out = a.rows + c * a.C + vec0 * V + x;
         if (!first) {
           s.x += out->x;
@@ -502,7 +503,7 @@ __global__ __launch_bounds__(kJoinThreads) void norm_bwd_join_kernel(const NormA
   if (at >= (int64_t)a.segments * a.groups) return;
   const int32_t b = (int32_t)(at / a.groups), g = (int32_t)(at % a.groups);
   const int64_t lo = seg_row(a, b), hi = seg_row(a, b + 1);
-  const float2 s = means(a, join_parts(a, b, g, lo, hi), hi - lo);
+  const float2 s = means(a, join_parts(a, b, g, lo, hi, 64), hi - lo);
   if ((threadIdx.x & 63) == 0) a.sums[at] = s;
 }
 
@@ -586,8 +587,7 @@ __device__ __forceinline__ void team_groups(const NormArgs& a, const Team& t, co
     __syncthreads();
     const int each = t.rows * (a.D / V);                    // (a group's sums lie one behind the other)
     // as many lanes to a group as there are; a power of two, so that they join by shuffles
-    int lanes = 64;
-    while (lanes > 1 && (int)blockDim.x / lanes < groups) lanes /= 2;
+    const int lanes = lanes_each(groups, blockDim.x);
     for (int g0 = 0; g0 < groups; g0 += (int)blockDim.x / lanes) {
       const int g = g0 + (int)threadIdx.x / lanes;
       double2 v = make_double2(0., 0.);
@@ -596,10 +596,7 @@ __device__ __forceinline__ void team_groups(const NormArgs& a, const Team& t, co
           v.x += sm[g * each + i].x;
           v.y += sm[g * each + i].y;
         }
-      for (int d = lanes / 2; d; d /= 2) {
-        v.x += __shfl_xor(v.x, d);
-        v.y += __shfl_xor(v.y, d);
-      }
+      add_lanes(v, lanes);
       if (g < groups && threadIdx.x % lanes == 0) out[g] = v;
     }
   } else {
@@ -614,10 +611,7 @@ __device__ __forceinline__ void team_groups(const NormArgs& a, const Team& t, co
         v.x += x.x;
         v.y += x.y;
       }
-      for (int d = 32; d; d /= 2) {
-        v.x += __shfl_xor(v.x, d);
-        v.y += __shfl_xor(v.y, d);
-      }
+      add_lanes(v, 64);
       if (lane == 0) out[g] = v;
     }
   }
@@ -821,16 +815,21 @@ __global__ __launch_bounds__(kMostTeam, 4) void norm_bwd_whole_kernel(const Norm
   team_zeros<S, V>(a, t, stripe, stripes);
   // this workgroup's row of the table of gamma's and beta's sums
   __syncthreads();
-  const float2* of = reinterpret_cast<const float2*>(sm + blockDim.x * N);
-  for (int c = threadIdx.x; c < t.width; c += blockDim.x) {
-    float2 s = make_float2(0.f, 0.f);
-    for (int y = 0; y < t.rows; ++y) {
-      const float2 v = of[(c % V) * blockDim.x + y * t.per_row + c / V];
-      s.x += v.x;
-      s.y += v.y;
-    }
-    a.rows[stripe * a.C + t.c0 + c] = s;
+  for (int rows = t.rows; rows > 1;) {                      // by halves: a thread adds what the one `half` rows below it has
+    const int half = (rows + 1) / 2;
+    if (t.ty + half < rows)
+#pragma unroll
+      for (int i = 0; i < V; ++i) {
+        const float2 v = all[i * blockDim.x + half * t.per_row];
+        all[i * blockDim.x].x += v.x;
+        all[i * blockDim.x].y += v.y;
+      }
+    __syncthreads();
+    rows = half;
   }
+  if (t.ty == 0)
+#pragma unroll
+    for (int i = 0; i < V; ++i) a.rows[stripe * a.C + ch + i] = all[i * blockDim.x];
 }
 
 // Values that a thread takes at a time: what 16 bytes hold, and a divisor of the width
@@ -843,13 +842,15 @@ int vector_of(int32_t dtype, int32_t C) {
 struct NormPlan { int64_t chunk, chunks; size_t parts, sums, rows, total; };
 constexpr int kMostStripes = 2048;
 // Segments in parts: chunks of rows, and where the sums lie
-NormPlan norm_plan(int64_t m, int32_t segments, int32_t C, int32_t groups, bool backward) {
+NormPlan norm_plan(int32_t dtype, int64_t m, int32_t segments, int32_t C, int32_t groups, bool backward) {
   NormPlan p{};
-  // 2048 workgroups fill the chip; a chunk has eight rows of 256 threads or more
-  int64_t least = ceil_div(8 * 2048, C);
-  if (least < 8) least = 8;
-  p.chunk = ceil_div(m > 0 ? m : 1, 2048);
-  if (p.chunk < least) p.chunk = least;
+  // 2048 workgroups fill the chip, half of them with matrices in the caches, whose parts are joined by every workgroup; but
+  // each thread has four vectors of a value or more (14530 x 8 by chunks of 2048 rows 38 us, of 512 22)
+  const int64_t vectors = ceil_div(m * C, dtype == SAGNN_BF16 ? 8 : 4);
+  int64_t chunks = vectors / (4 * kThreads);
+  const int64_t most = vectors > (1 << 23) ? 2048 : 1024;
+  chunks = chunks < 1 ? 1 : chunks > most ? most : chunks;
+  p.chunk = ceil_div(m > 0 ? m : 1, chunks);
   p.chunks = ceil_div(m > 0 ? m : 1, p.chunk);
   size_t off = 0;
   auto take = [&](size_t bytes) { const size_t o = off; off += round_up(bytes, 256); return o; };
@@ -864,7 +865,7 @@ NormPlan norm_plan(int64_t m, int32_t segments, int32_t C, int32_t groups, bool 
 
 // Whole segments: channels of a workgroup (0: not that way), workgroups beside one another, threads
 struct WholePlan { int32_t slab, slabs, threads; };
-WholePlan whole_plan(int64_t m, int64_t max_rows, int32_t C, int32_t D, int v, int size, int kept) {
+WholePlan whole_plan(int64_t m, int32_t segments, int64_t max_rows, int32_t C, int32_t D, int v, int size, int kept, bool backward) {
   WholePlan w{};
   int64_t rows = max_rows > 0 && max_rows < m ? max_rows : m;
   if (rows < 1) rows = 1;
@@ -879,9 +880,17 @@ WholePlan whole_plan(int64_t m, int64_t max_rows, int32_t C, int32_t D, int v, i
   units = ceil_div(all, ceil_div(all, units));              // slabs of like width
   // less than a cache line of a row for each workgroup reads lines twice: where the L2s do not have them the second time
   if (units < all && units * unit * size < 128 && m * C * size > (4 << 20)) return w;
+  // Few workgroups: narrower slabs where the matrix is in the L2s; and where each has still much to do, chunks share it better (three
+  // segments of 415 x 896, backward: 84 workgroups 43 us, chunks 24, narrower slabs 17.5).
+  const int64_t one = rows * (unit / v);
+  if (segments * ceil_div(C, units * unit) < 256 && m * C * size <= (4 << 20)) {
+    const int64_t narrow = one < kMostTeam ? kMostTeam / one : 1;
+    if (narrow < units) units = narrow;
+  }
+  const int64_t vectors = one * units;
+  if (segments * ceil_div(C, units * unit) < 128 && vectors > kMostTeam * (backward ? 4 : 8)) return w;
   w.slab = (int32_t)(units * unit);
   w.slabs = (int32_t)ceil_div(C, w.slab);
-  const int64_t vectors = rows * (w.slab / v);
   w.threads = vectors <= 64 * 4 && w.slab / v <= 64 ? 64 : vectors <= 256 * 4 && w.slab / v <= 256 ? 256 : kMostTeam;
   return w;
 }
@@ -897,13 +906,13 @@ NormForm norm_form(int32_t dtype, int64_t m, int32_t segments, int64_t max_rows,
   const int size = dtype == SAGNN_BF16 ? 2 : 4;
   int v = vector_of(dtype, C);
   if (backward && v * size > 8) v /= 2;
-  if (m > 0 && ld <= kWholeLd) f.whole = whole_plan(m, max_rows, C, D, v, size, !backward ? kKept : D % v == 0 ? kKeptBackward : kKeptBackward / 2);
+  if (m > 0 && ld <= kWholeLd) f.whole = whole_plan(m, segments, max_rows, C, D, v, size, !backward ? kKept : D % v == 0 ? kKeptBackward : kKeptBackward / 2, backward);
   if (((int64_t)segments + 16) * f.whole.slabs > INT32_MAX) f.whole.slab = 0;
   if (f.whole.slab) {
     f.table = segments < kMostStripes ? segments : kMostStripes;
     f.bytes = backward ? round_up((size_t)f.table * C * sizeof(float2), 256) : 0;
   } else {
-    f.parts = norm_plan(m, segments, C, groups, backward);
+    f.parts = norm_plan(dtype, m, segments, C, groups, backward);
     f.table = m > 0 ? f.parts.chunks : 0;
     f.bytes = f.parts.total;
     // A launch less, some ten microseconds, where every workgroup can join its segments' parts: 128 KB of them at most, and few
