@@ -47,12 +47,14 @@ __device__ __forceinline__ int32_t grouped_tiles(const GroupedArgs& a, int32_t g
   hi = g < a.groups ? grouped_row(a.off, g + 1, a.m) : (g == a.groups ? a.m : 0);
   return hi > lo ? (int32_t)((hi - lo + BM - 1) / BM) : 0;
 }
-__device__ __forceinline__ int32_t wave_sums(int32_t x) {     // of the lanes up to each
+// Sums of the lanes up to each, `most` at the most: ascending offsets have no more tiles than that, and others cannot wrap it.
+__device__ __forceinline__ int32_t wave_sums(int32_t x, int32_t most) {
   const int lane = threadIdx.x & 63;
+  if (x > most) x = most;
 #pragma unroll
   for (int d = 1; d < 64; d *= 2) {
     const int32_t y = __shfl_up(x, d);
-    if (lane >= d) x += y;
+    if (lane >= d) x = x < most - y ? x + y : most;
   }
   return x;
 }
@@ -62,23 +64,24 @@ __device__ __forceinline__ int32_t wave_sums(int32_t x) {     // of the lanes up
 // the launch's size, the last XCDs got the missing ones: 8192^3 in five rounds instead of four).  Every wavefront looks
 // for itself: 64 groups a round, a scan over the lanes.  False: no tile.
 template <int BM>
-__device__ __forceinline__ bool grouped_find(const GroupedArgs& a, GroupTile& found, int32_t& col) {
+__device__ __forceinline__ bool grouped_find(const GroupedArgs& a, int32_t block, GroupTile& found, int32_t& col) {
   const int lane = threadIdx.x & 63;
   int64_t lo, hi;
-  int32_t tiles = grouped_tiles<BM>(a, lane, lo, hi), upto = wave_sums(tiles);
+  int32_t tiles = grouped_tiles<BM>(a, lane, lo, hi), upto = wave_sums(tiles, a.row_tiles);
   int32_t total = __builtin_amdgcn_readlane(upto, 63);
   for (int32_t g0 = 64; g0 <= a.groups; g0 += 64) {
     int64_t l, h;
-    total += __builtin_amdgcn_readlane(wave_sums(grouped_tiles<BM>(a, g0 + lane, l, h)), 63);
+    const int32_t more = __builtin_amdgcn_readlane(wave_sums(grouped_tiles<BM>(a, g0 + lane, l, h), a.row_tiles), 63);
+    total = more < a.row_tiles - total ? total + more : a.row_tiles;
   }
-  if ((int64_t)blockIdx.x >= (int64_t)total * a.col_tiles) return false;
-  const int32_t id = xcd_run(blockIdx.x, total * a.col_tiles), t = id / a.col_tiles;
+  if (block >= total * a.col_tiles) return false;          // (row_tiles * col_tiles is the launch's size)
+  const int32_t id = xcd_run(block, total * a.col_tiles), t = id / a.col_tiles;
   col = id % a.col_tiles;
   int32_t before = 0;
   for (int32_t g0 = 0; g0 <= a.groups; g0 += 64) {
     if (g0) {
       tiles = grouped_tiles<BM>(a, g0 + lane, lo, hi);
-      upto = wave_sums(tiles);
+      upto = wave_sums(tiles, a.row_tiles);
     }
     const uint64_t past = __ballot(before + upto > t);
     if (past) {
@@ -99,11 +102,11 @@ __device__ __forceinline__ bool grouped_find(const GroupedArgs& a, GroupTile& fo
 // names it; not every number does.  Rows [r0, r1) of the pair that p names; cut: the group has rows in other chunks.
 constexpr int32_t kManyPairs = 32;
 struct GroupPart { int32_t g; int64_t r0, r1; int32_t c; bool cut, first; };
-__device__ __forceinline__ bool grouped_part(const GroupedArgs& a, GroupPart& part, int32_t& tile) {
+__device__ __forceinline__ bool grouped_part(const GroupedArgs& a, int32_t id, GroupPart& part, int32_t& tile) {
   const int lane = threadIdx.x & 63;
   // Tiles of a pair read the same rows.  Many pairs: an XCD has all tiles of every eighth; few: a run of the tiles of each.
   // (The last pairs may not be there, so that the XCDs share them in any case.)
-  const int32_t tiles = a.row_tiles * a.col_tiles, id = (int32_t)blockIdx.x;
+  const int32_t tiles = a.row_tiles * a.col_tiles;
   int32_t p = id / tiles;
   tile = id % tiles;
   if (a.pairs >= kManyPairs) {
@@ -404,7 +407,7 @@ __global__ __launch_bounds__(WM * WN * 64) void grouped_kernel(const GroupedArgs
   __shared__ __attribute__((aligned(16))) char smem[TileShape<PREC, false, BM, BK>::kBytes + TileShape<PREC, !WT, BN, BK>::kBytes];
   GroupTile t;
   int32_t col;
-  if (!grouped_find<BM>(a, t, col)) return;
+  if (!grouped_find<BM>(a, (int32_t)blockIdx.x, t, col)) return;
   const int64_t c0 = (int64_t)col * BN;
   const int rows = (int)(t.end - t.r0 < BM ? t.end - t.r0 : BM), cols = (int)(a.nout - c0 < BN ? a.nout - c0 : BN);
   floatx16 acc[TM][TN];
@@ -427,7 +430,7 @@ __global__ __launch_bounds__(WAVES * 64) void grouped_thin_kernel(const GroupedA
   __shared__ __attribute__((aligned(16))) char smem[WAVES * (kOwn > kSums ? kOwn : kSums)];
   GroupTile t;
   int32_t col;
-  if (!grouped_find<32>(a, t, col)) return;
+  if (!grouped_find<32>(a, (int32_t)blockIdx.x, t, col)) return;
   const int64_t c0 = (int64_t)col * BN;
   const int rows = (int)(t.end - t.r0 < 32 ? t.end - t.r0 : 32), cols = (int)(a.nout - c0 < BN ? a.nout - c0 : BN);
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -490,7 +493,7 @@ __global__ __launch_bounds__(WM * WN * 64) void grouped_tn_kernel(const GroupedA
   __shared__ __attribute__((aligned(16))) char smem[TileShape<PREC, true, BM, BK>::kBytes + TileShape<PREC, true, BN, BK>::kBytes];
   GroupPart p;
   int32_t tile;
-  if (!grouped_part(a, p, tile)) return;
+  if (!grouped_part(a, (int32_t)blockIdx.x, p, tile)) return;
   const int64_t k0 = (int64_t)(tile / a.col_tiles) * BM, c0 = (int64_t)(tile % a.col_tiles) * BN;
   const int rows = (int)(a.kdim - k0 < BM ? a.kdim - k0 : BM), cols = (int)(a.nout - c0 < BN ? a.nout - c0 : BN);
   floatx16 acc[TM][TN];
@@ -521,6 +524,7 @@ SAGNN_GROUPED_MODE(fp32_bf16)
 SAGNN_GROUPED_MODE(fp32_bf16x3)
 SAGNN_GROUPED_MODE(bf16)
 #undef SAGNN_GROUPED_MODE
+int grouped_bwd_bf16(const GroupedArgs& rows, int64_t rows_blocks, const GroupedArgs& tn, int64_t tn_blocks, hipStream_t s);
 
 template <typename S, int PREC, int BK, bool WT>
 int grouped_launch(const GroupedArgs& a, int tile, int64_t blocks, hipStream_t s) {

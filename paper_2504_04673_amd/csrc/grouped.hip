@@ -82,8 +82,9 @@ int choose_tile(int32_t dtype, int32_t prec, int ways, int64_t rows, int64_t par
   return best;
 }
 
-int launch_rows(const GroupedArgs& g, int32_t dtype, int32_t prec, bool trans_w, hipStream_t s) {
-  GroupedArgs a = g;
+// Tile and workgroups of the product (fills in a's tiles); < 0 workgroups: more than a launch has
+struct Launch { int tile; int64_t blocks; };
+Launch plan_rows(GroupedArgs& a, int32_t dtype, int32_t prec) {
   int ways = kAny;
   if (dtype == SAGNN_BF16) {
     if (direct_rows(a.X, a.ldx, a.kdim) && direct_rows(a.W, a.ldw, a.nout) && a.stride_w % 8 == 0 && direct_rows(a.Y, a.ldy, 0) &&
@@ -96,10 +97,14 @@ int launch_rows(const GroupedArgs& g, int32_t dtype, int32_t prec, bool trans_w,
   a.row_tiles = (int32_t)(a.m / grouped_tile_rows(tile) + a.groups + 1);
   a.col_tiles = (int32_t)ceil_div(a.nout, grouped_tile_cols(tile));
   const int64_t blocks = (int64_t)a.row_tiles * a.col_tiles;
-  if (blocks > INT32_MAX) return SAGNN_EINVAL;
-  if (dtype == SAGNN_BF16) return grouped_bf16(a, tile, trans_w, blocks, s);
-  return prec == SAGNN_GEMM_FP32 ? grouped_fp32(a, tile, trans_w, blocks, s)
-         : prec == SAGNN_GEMM_BF16 ? grouped_fp32_bf16(a, tile, trans_w, blocks, s) : grouped_fp32_bf16x3(a, tile, trans_w, blocks, s);
+  return {tile, blocks <= INT32_MAX ? blocks : -1};
+}
+
+int launch_rows(const GroupedArgs& a, Launch l, int32_t dtype, int32_t prec, bool trans_w, hipStream_t s) {
+  if (dtype == SAGNN_BF16) return grouped_bf16(a, l.tile, trans_w, l.blocks, s);
+  return prec == SAGNN_GEMM_FP32 ? grouped_fp32(a, l.tile, trans_w, l.blocks, s)
+         : prec == SAGNN_GEMM_BF16 ? grouped_fp32_bf16(a, l.tile, trans_w, l.blocks, s)
+                                   : grouped_fp32_bf16x3(a, l.tile, trans_w, l.blocks, s);
 }
 
 // The weight gradient's tiles and chunks of rows.  Chunks fill the chip where the matrices are small or one group has most rows (170003 x 128 x 128
@@ -139,8 +144,7 @@ size_t tn_ws_bytes(int64_t m, int32_t groups, int32_t kdim, int32_t nout) {
   return chunks > 1 ? (size_t)(2 * chunks) * kdim * nout * 4 : 0;
 }
 
-int launch_tn(const GroupedArgs& g, int32_t dtype, int32_t prec, hipStream_t s) {
-  GroupedArgs a = g;
+Launch plan_weights(GroupedArgs& a, int32_t dtype, int32_t prec) {
   const bool direct = dtype == SAGNN_BF16 && direct_rows(a.X, a.ldx, a.kdim) && direct_rows(a.G, a.ldg, a.nout) && aligned16(a.dW) && aligned16(a.partial);
   const bool staged = dtype == SAGNN_F32 && a.ldx <= kStagedLd && a.ldg <= kStagedLd;
   const TnPlan p = tn_plan(a.m, a.groups, a.kdim, a.nout, dtype, prec, direct ? kDirect : staged ? kStaged : kAny);
@@ -151,11 +155,18 @@ int launch_tn(const GroupedArgs& g, int32_t dtype, int32_t prec, hipStream_t s) 
   a.pairs = (int32_t)pairs;
   if (pairs >= kManyPairs) pairs = round_up((size_t)pairs, 8);
   const int64_t blocks = pairs * p.row_tiles * p.col_tiles;
-  if (blocks > INT32_MAX) return SAGNN_EINVAL;
-  const int rc = dtype == SAGNN_BF16 ? grouped_tn_bf16(a, p.tile, blocks, s)
-                 : prec == SAGNN_GEMM_FP32 ? grouped_tn_fp32(a, p.tile, blocks, s)
-                 : prec == SAGNN_GEMM_BF16 ? grouped_tn_fp32_bf16(a, p.tile, blocks, s) : grouped_tn_fp32_bf16x3(a, p.tile, blocks, s);
-  if (rc != SAGNN_OK || p.chunks == 1) return rc;
+  return {p.tile, blocks <= INT32_MAX ? blocks : -1};
+}
+
+int launch_weights(const GroupedArgs& a, Launch l, int32_t dtype, int32_t prec, hipStream_t s) {
+  return dtype == SAGNN_BF16 ? grouped_tn_bf16(a, l.tile, l.blocks, s)
+         : prec == SAGNN_GEMM_FP32 ? grouped_tn_fp32(a, l.tile, l.blocks, s)
+         : prec == SAGNN_GEMM_BF16 ? grouped_tn_fp32_bf16(a, l.tile, l.blocks, s) : grouped_tn_fp32_bf16x3(a, l.tile, l.blocks, s);
+}
+
+// The groups whose rows lie in several chunks
+int join_weights(const GroupedArgs& a, hipStream_t s) {
+  if (a.m <= a.chunk) return SAGNN_OK;
   const bool four = ((int64_t)a.kdim * a.nout & 3) == 0 && aligned16(a.dW) && aligned16(a.partial);
   int64_t wide = ceil_div((int64_t)a.kdim * a.nout, four ? 1024 : 256);
   if (wide > 1024) wide = 1024;
@@ -181,7 +192,9 @@ SAGNN_EXPORT int grouped_gemm_act(int32_t dtype, const void* d_X, int64_t ldx, c
   GroupedArgs a{};
   a.X = d_X; a.ldx = ldx; a.W = d_W; a.ldw = ldw; a.stride_w = stride_w; a.off = d_off; a.groups = n_groups;
   a.m = m; a.kdim = kdim; a.nout = nout; a.act = act; a.mask = d_mask; a.ldmask = ldmask; a.Y = d_Y; a.ldy = ldy;
-  return launch_rows(a, dtype, prec, transW != 0, (hipStream_t)stream);
+  const Launch l = plan_rows(a, dtype, prec);
+  if (l.blocks < 0) return SAGNN_EINVAL;
+  return launch_rows(a, l, dtype, prec, transW != 0, (hipStream_t)stream);
 }
 
 SAGNN_EXPORT int grouped_gemm_bwd_workspace_bytes(int64_t m, int32_t n_groups, int32_t kdim, int32_t nout, size_t* bytes) {
@@ -206,17 +219,26 @@ SAGNN_EXPORT int grouped_gemm_bwd(int32_t dtype, const void* d_X, int64_t ldx, c
   if (d_dW && ws_bytes < tn_ws_bytes(m, n_groups, kdim, nout)) return SAGNN_ECAPACITY;
   if (d_dW && !d_ws && tn_ws_bytes(m, n_groups, kdim, nout) > 0) return SAGNN_EINVAL;
   hipStream_t s = (hipStream_t)stream;
-  GroupedArgs a{};
-  a.off = d_off; a.groups = n_groups; a.m = m;
+  GroupedArgs x{}, w{};
+  Launch lx{0, 0}, lw{0, 0};
   if (d_dX && m > 0) {       // (G W^T: the stored W read as the transposed one of a product with kdim and nout exchanged)
-    a.X = d_G; a.ldx = ldg; a.W = d_W; a.ldw = ldw; a.stride_w = stride_w; a.kdim = nout; a.nout = kdim;
-    a.mask = d_mask; a.ldmask = ldmask; a.Y = d_dX; a.ldy = lddx;
-    const int rc = launch_rows(a, dtype, prec, true, s);
-    if (rc != SAGNN_OK) return rc;
+    x.off = d_off; x.groups = n_groups; x.m = m;
+    x.X = d_G; x.ldx = ldg; x.W = d_W; x.ldw = ldw; x.stride_w = stride_w; x.kdim = nout; x.nout = kdim;
+    x.mask = d_mask; x.ldmask = ldmask; x.Y = d_dX; x.ldy = lddx;
+    lx = plan_rows(x, dtype, prec);
   }
   if (d_dW) {
-    a.X = d_X; a.ldx = ldx; a.G = d_G; a.ldg = ldg; a.kdim = kdim; a.nout = nout; a.dW = d_dW; a.partial = (float*)d_ws;
-    return launch_tn(a, dtype, prec, s);
+    w.off = d_off; w.groups = n_groups; w.m = m;
+    w.X = d_X; w.ldx = ldx; w.G = d_G; w.ldg = ldg; w.kdim = kdim; w.nout = nout; w.dW = d_dW; w.partial = (float*)d_ws;
+    lw = plan_weights(w, dtype, prec);
   }
-  return SAGNN_OK;
+  if (lx.blocks < 0 || lw.blocks < 0) return SAGNN_EINVAL;
+  int rc = SAGNN_OK;
+  if (lx.blocks > 0 && lw.blocks > 0 && lx.tile == kDirect256 && lw.tile == kDirect256 && lx.blocks + lw.blocks <= INT32_MAX) {
+    rc = grouped_bwd_bf16(x, lx.blocks, w, lw.blocks, s);
+  } else {
+    if (d_dX && m > 0) rc = launch_rows(x, lx, dtype, prec, true, s);
+    if (rc == SAGNN_OK && d_dW) rc = launch_weights(w, lw, dtype, prec, s);
+  }
+  return rc == SAGNN_OK && d_dW ? join_weights(w, s) : rc;
 }

@@ -20,4 +20,9 @@ int grouped_tn_bf16(const GroupedArgs& a, int tile, int64_t blocks, hipStream_t 
   }
   return grouped_tn_launch<__bf16, SAGNN_GEMM_BF16, 64>(a, tile, blocks, s);
 }
+int grouped_bwd_bf16(const GroupedArgs& rows, int64_t rows_blocks, const GroupedArgs& tn, int64_t tn_blocks, hipStream_t s) {
+  grouped_direct_bwd_kernel<4, 4, 2><<<dim3((uint32_t)(rows_blocks + tn_blocks)), 512, 0, s>>>(rows, tn, (int32_t)tn_blocks);
+  SAGNN_LAUNCH_CHECK();
+  return SAGNN_OK;
+}
 }  // namespace sagnn
