@@ -861,6 +861,10 @@ def _rows_in_python(grads, out):
 _rows = None
 
 
+def _listed(grads):
+    return grads if isinstance(grads, (list, tuple)) else list(grads)
+
+
 def _grad_list(grads, out=None):
     """struct sagnn_grad of the C header for each tensor, one behind the other."""
     global _rows
@@ -885,6 +889,7 @@ def _grad_ws(n, device):
 
 def grad_global_norm(grads):
     """The 2-norm over all tensors of the list, a float32 tensor of one element on the device."""
+    grads = _listed(grads)
     rows, n = _grad_list(grads)
     ws, norm = _grad_ws(n, grads[0].device if n else "cuda")
     _check(_calls().grad_global_norm(rows, n, _ptr(norm), _ptr(ws), ws.numel(), _stream()), "grad_global_norm")
@@ -894,6 +899,7 @@ def grad_global_norm(grads):
 def grad_clip_norm(grads, max_norm: float, norm=None, out=None):
     """Scales the tensors of the list by min(1, max_norm / norm), in place or into `out` (tensors like them).  norm: what
     grad_global_norm returned, perhaps joined across processes; None computes it.  Returns the norm (on the device)."""
+    grads = _listed(grads)
     rows, n = _grad_list(grads, out)
     if norm is not None:
         _shape(_dev(norm, torch.float32, "norm"), (1,), "norm")

@@ -10,24 +10,46 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kMaxBlocks = 1024;     // workgroups of a launch that sums, and the sums that it leaves
-constexpr int kListed = 120;         // tensors that one launch takes: they travel as its arguments (4 KB at most)
+constexpr int kListBytes = 3840;     // of a launch's arguments (4 KB at most), in which the tensors travel
 // Values that a workgroup takes at a time: so many that kMaxBlocks workgroups have one each, within these bounds.  (More
 // workgroups are more sums for each of them to join: 2 x 10 M values, 2048 workgroups 8.5 us to sum and 16.7 to scale, 1024 8.9 and
 // 14.7, 512 10.1 and 14.1; half a billion 188 and 361, 186 and 358, 212 and 352.)
 constexpr int kLeastPiece = 2048, kMostPiece = 16384;
 
+// Tensors of one launch.  Addresses have 48 bits and a tensor's end 15, so that a launch takes 318 tensors, or 212 with places for
+// results (211 tensors as 24 bytes each, two launches to sum and two to scale: 51 us in place of 41).
+template <bool OUT>
 struct List {
-  const void* in[kListed];
-  void* out[kListed];
-  int32_t first[kListed + 1];        // pieces before the tensor
-  uint32_t last[kListed];            // values of its last piece
-  uint8_t bf16[kListed];
+  static constexpr int kMost = (kListBytes - 16) / (OUT ? 18 : 12), kAddresses = OUT ? 2 * kMost : kMost;
+  int32_t first[kMost + 1];          // pieces before the tensor
+  uint32_t low[kAddresses];          // of the tensors, then of their results
+  uint16_t high[kAddresses];
+  uint16_t end[kMost];               // (values of its last piece - 1) * 2 + whether they are bfloat16
   int32_t count, piece;              // tensors, values of a piece
+
+  void add(const sagnn_grad& h) {
+    const int64_t pieces = ceil_div(h.n, piece);
+    const void* at[2] = {h.d_in, h.d_out};
+    for (int i = 0; i < (OUT ? 2 : 1); ++i) {
+      low[i * kMost + count] = (uint32_t)(uintptr_t)at[i];
+      high[i * kMost + count] = (uint16_t)((uintptr_t)at[i] >> 32);
+    }
+    end[count] = (uint16_t)((h.n - (pieces - 1) * piece - 1) * 2 + (h.dtype == SAGNN_BF16));
+    first[count + 1] = first[count] + (int32_t)pieces;
+    ++count;
+  }
+  __device__ __forceinline__ char* in(int t) const { return reinterpret_cast<char*>((uint64_t)high[t] << 32 | low[t]); }
+  __device__ __forceinline__ char* out(int t) const { return in(OUT ? kMost + t : t); }
+  __device__ __forceinline__ bool bf16(int t) const { return end[t] & 1; }
+  // values of a piece
+  __device__ __forceinline__ int values(int t, int32_t p) const { return p + 1 == first[t + 1] ? (end[t] >> 1) + 1 : piece; }
 };
-static_assert(sizeof(List) <= 3800, "arguments of a launch");
+static_assert(kMostPiece <= 32768, "a tensor's end has 15 bits");
+static_assert(sizeof(List<false>) <= kListBytes && sizeof(List<true>) <= kListBytes, "arguments of a launch");
 
 // Tensor of a piece, by the pieces before each (64 tensors a round)
-__device__ __forceinline__ int find_tensor(const List& l, int32_t piece) {
+template <bool OUT>
+__device__ __forceinline__ int find_tensor(const List<OUT>& l, int32_t piece) {
   const int lane = threadIdx.x & 63;
   int count = 0;
   for (int t0 = 0; t0 < l.count; t0 += 64) {
@@ -106,14 +128,14 @@ __device__ __forceinline__ double block_sum(double s) {
   return s;
 }
 
-__global__ __launch_bounds__(kThreads) void grad_sum_kernel(const List l, double* __restrict__ sums) {
+__global__ __launch_bounds__(kThreads) void grad_sum_kernel(const List<false> l, double* __restrict__ sums) {
   double s = 0.;
   for (int32_t piece = blockIdx.x; piece < l.first[l.count]; piece += gridDim.x) {
     const int t = find_tensor(l, piece);
     const int32_t at = piece - l.first[t];
-    const int n = piece + 1 == l.first[t + 1] ? (int)l.last[t] : l.piece;
-    s += l.bf16[t] ? sum_piece(reinterpret_cast<const __bf16*>(l.in[t]) + (int64_t)at * l.piece, n)
-                   : sum_piece(reinterpret_cast<const float*>(l.in[t]) + (int64_t)at * l.piece, n);
+    const int n = l.values(t, piece);
+    s += l.bf16(t) ? sum_piece(reinterpret_cast<const __bf16*>(l.in(t)) + (int64_t)at * l.piece, n)
+                   : sum_piece(reinterpret_cast<const float*>(l.in(t)) + (int64_t)at * l.piece, n);
   }
   s = block_sum(s);
   if (threadIdx.x == 0) sums[blockIdx.x] = s;
@@ -131,50 +153,46 @@ __global__ __launch_bounds__(kThreads) void grad_norm_kernel(const double* __res
 }
 
 // Pieces in the order opposite to grad_sum_kernel's: what was read last is still in the caches.
-__global__ __launch_bounds__(kThreads) void grad_scale_kernel(const List l, const double* __restrict__ sums, int count, const float* __restrict__ given,
-                                                              double max_norm, float* __restrict__ norm) {
+template <bool OUT>
+__global__ __launch_bounds__(kThreads) void grad_scale_kernel(const List<OUT> l, const double* __restrict__ sums, int count,
+                                                              const float* __restrict__ given, double max_norm, float* __restrict__ norm) {
   const double n = given ? (double)*given : norm_of(sums, count);
   if (norm && blockIdx.x == 0 && threadIdx.x == 0) *norm = (float)n;
   const double ratio = max_norm / n;                 // (norm 0: infinite; NaN stays NaN)
   const float c = ratio > 1. ? 1.f : (float)ratio;
   for (int32_t piece = l.first[l.count] - 1 - (int32_t)blockIdx.x; piece >= 0; piece -= gridDim.x) {
     const int t = find_tensor(l, piece);
-    if (c == 1.f && l.in[t] == l.out[t]) continue;   // (nothing changes)
+    if (c == 1.f && l.in(t) == l.out(t)) continue;   // (nothing changes)
     const int64_t at = (int64_t)(piece - l.first[t]) * l.piece;
-    const int k = piece + 1 == l.first[t + 1] ? (int)l.last[t] : l.piece;
-    if (l.bf16[t]) scale_piece(reinterpret_cast<const __bf16*>(l.in[t]) + at, reinterpret_cast<__bf16*>(l.out[t]) + at, k, c);
-    else scale_piece(reinterpret_cast<const float*>(l.in[t]) + at, reinterpret_cast<float*>(l.out[t]) + at, k, c);
+    const int k = l.values(t, piece);
+    if (l.bf16(t)) scale_piece(reinterpret_cast<const __bf16*>(l.in(t)) + at, reinterpret_cast<__bf16*>(l.out(t)) + at, k, c);
+    else scale_piece(reinterpret_cast<const float*>(l.in(t)) + at, reinterpret_cast<float*>(l.out(t)) + at, k, c);
   }
 }
 
 int grid_of(int64_t pieces) { return (int)(pieces < kMaxBlocks ? pieces : kMaxBlocks); }
 
 // The tensors in lists of one launch each: f(list, pieces)
-template <typename F>
+template <bool OUT, typename F>
 int each_list(const sagnn_grad* h, int32_t n, F f) {
   for (int32_t i = 0; i < n;) {
-    List l;
+    List<OUT> l;
     l.count = 0;
     l.first[0] = 0;
     int64_t values = 0;
     int32_t end = i;
-    for (int32_t c = 0; end < n && c < kListed; ++end) {
+    int32_t tensors = 0;
+    for (; end < n && tensors < List<OUT>::kMost; ++end) {
       if (h[end].n == 0) continue;
-      if (c > 0 && values + h[end].n > (int64_t)kLeastPiece * (1 << 30)) break;
+      if (tensors > 0 && values + h[end].n > (int64_t)kLeastPiece * (1 << 30)) break;
       values += h[end].n;
-      ++c;
+      ++tensors;
     }
     const int64_t each = (int64_t)round_up((size_t)ceil_div(values > 0 ? values : 1, kMaxBlocks), kLeastPiece);
     l.piece = (int32_t)(each < kMostPiece ? each : kMostPiece);
     for (; i < end; ++i) {
       if (h[i].n == 0) continue;
-      const int64_t pieces = ceil_div(h[i].n, l.piece);
-      l.in[l.count] = h[i].d_in;
-      l.out[l.count] = h[i].d_out;
-      l.last[l.count] = (uint32_t)(h[i].n - (pieces - 1) * l.piece);
-      l.bf16[l.count] = h[i].dtype == SAGNN_BF16;
-      l.first[l.count + 1] = l.first[l.count] + (int32_t)pieces;
-      ++l.count;
+      l.add(h[i]);
     }
     if (!l.count) continue;
     const int rc = f(l, (int64_t)l.first[l.count]);
@@ -192,6 +210,7 @@ int check(const sagnn_grad* h, int32_t n, bool written) {
     const uintptr_t size = h[i].dtype == SAGNN_BF16 ? 2 : 4;
     if ((h[i].dtype != SAGNN_F32 && h[i].dtype != SAGNN_BF16) || h[i].n < 0 || h[i].n > ((int64_t)1 << 40)) return SAGNN_EINVAL;
     if (h[i].n == 0) continue;
+    if ((uintptr_t)h[i].d_in >> 48 || (written && (uintptr_t)h[i].d_out >> 48)) return SAGNN_EINVAL;
     if (!h[i].d_in || ((uintptr_t)h[i].d_in & (size - 1))) return SAGNN_EINVAL;
     if (written && (!h[i].d_out || ((uintptr_t)h[i].d_out & (size - 1)))) return SAGNN_EINVAL;
   }
@@ -218,12 +237,12 @@ int check(const sagnn_grad* h, int32_t n, bool written) {
   return shared ? SAGNN_EINVAL : SAGNN_OK;
 }
 
-size_t ws_bytes_of(int32_t n) { return sizeof(double) * kMaxBlocks * (size_t)(ceil_div(n > 0 ? n : 1, kListed) + 1); }
+size_t ws_bytes_of(int32_t n) { return sizeof(double) * kMaxBlocks * (size_t)(ceil_div(n > 0 ? n : 1, List<false>::kMost) + 1); }
 
 // Sums of all tensors into `sums`; how many there are
 int launch_sums(const sagnn_grad* h, int32_t n, double* sums, int* count, hipStream_t s) {
   *count = 0;
-  return each_list(h, n, [&](const List& l, int64_t pieces) {
+  return each_list<false>(h, n, [&](const List<false>& l, int64_t pieces) {
     const int grid = grid_of(pieces);
     grad_sum_kernel<<<dim3((uint32_t)grid), kThreads, 0, s>>>(l, sums + *count);
     SAGNN_LAUNCH_CHECK();
@@ -232,13 +251,20 @@ int launch_sums(const sagnn_grad* h, int32_t n, double* sums, int* count, hipStr
   });
 }
 
-int launch_scale(const sagnn_grad* h, int32_t n, const double* sums, int count, const float* given, double max_norm, float* norm, hipStream_t s) {
-  return each_list(h, n, [&](const List& l, int64_t pieces) {
-    grad_scale_kernel<<<dim3((uint32_t)grid_of(pieces)), kThreads, 0, s>>>(l, sums, count, given, max_norm, norm);
+template <bool OUT>
+int launch_scale_as(const sagnn_grad* h, int32_t n, const double* sums, int count, const float* given, double max_norm, float* norm, hipStream_t s) {
+  return each_list<OUT>(h, n, [&](const List<OUT>& l, int64_t pieces) {
+    grad_scale_kernel<OUT><<<dim3((uint32_t)grid_of(pieces)), kThreads, 0, s>>>(l, sums, count, given, max_norm, norm);
     SAGNN_LAUNCH_CHECK();
     norm = nullptr;
     return (int)SAGNN_OK;
   });
+}
+int launch_scale(const sagnn_grad* h, int32_t n, const double* sums, int count, const float* given, double max_norm, float* norm, hipStream_t s) {
+  bool out = false;
+  for (int32_t i = 0; i < n; ++i) out |= h[i].n > 0 && h[i].d_in != h[i].d_out;
+  return out ? launch_scale_as<true>(h, n, sums, count, given, max_norm, norm, s)
+             : launch_scale_as<false>(h, n, sums, count, given, max_norm, norm, s);
 }
 
 }  // namespace

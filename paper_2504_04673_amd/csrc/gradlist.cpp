@@ -1,5 +1,5 @@
 // A list of gradient tensors as struct sagnn_grad of the C header: address, address of the result, values, type.  Asked for one by
-// one from Python these are ten questions a tensor at 70 ns each: 211 tensors 170 us, this way 4, of 48 for their clipping.
+// one from Python these are ten questions a tensor at 70 ns each: 211 tensors 170 us, this way 4, of 41 for their clipping.
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <cstring>

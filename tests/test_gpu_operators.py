@@ -13,6 +13,7 @@ import pytest
 import torch
 
 import paper_2504_04673_amd as sagnn
+from paper_2504_04673_amd import binding
 
 pytestmark = pytest.mark.gpu
 U = 2.0 ** -24
@@ -454,6 +455,48 @@ def test_clipping(sizes, kinds, shift):
         whole = [t.clone() for t in grads]
         sagnn.grad_clip_norm(whole, ratio * norm64)
         assert all(torch.equal(a, b) for a, b in zip(whole, out))
+
+
+@pytest.mark.parametrize("count", [211, 212, 213, 318, 319, 640])
+def test_clipping_of_as_many_tensors_as_a_launch_takes_and_more(count):
+    g = gen(count)
+    sizes = [(i * 37) % 301 + 1 if i % 11 else 0 for i in range(count + count // 10)]       # (a tensor of no values takes no place)
+    grads = tensors(g, sizes, [F, B, F])
+    norm64 = sum(float(t.double().square().sum()) for t in grads) ** 0.5
+    out, whole = [torch.empty_like(t) for t in grads], [t.clone() for t in grads]
+    half = [w if i % 2 else torch.empty_like(w) for i, w in enumerate(whole)]               # (some in place, some not)
+    norm = sagnn.grad_clip_norm(grads, 0.5 * norm64, out=out)
+    assert abs(float(norm) - norm64) <= 2 * U * norm64
+    for t, o in zip(grads, out):
+        ref = t.double() * 0.5
+        close(o, ref, 4 * U * ref.abs() + rounding(t.dtype, ref) + 1e-45, "out")
+    sagnn.grad_clip_norm([w if i % 2 else t for i, (w, t) in enumerate(zip(whole, grads))], 0.5 * norm64, out=half)
+    assert all(torch.equal(a, b) for a, b in zip(half, out))
+    whole = [t.clone() for t in grads]
+    sagnn.grad_clip_norm(tuple(whole), 0.5 * norm64)
+    assert all(torch.equal(a, b) for a, b in zip(whole, out))
+
+
+def test_lists_of_gradients_are_read_alike_in_both_ways():
+    g = gen(3)
+    grads = tensors(g, [5, 0, 300, 17], [F, B], 1)
+    out = [torch.empty_like(t) for t in grads]
+    ext = binding._extension("_gradlist", binding._build.GRADLIST)
+    assert ext is not None
+    for o in (None, out, grads):
+        assert ext.rows(grads, o) == binding._rows_in_python(grads, o)
+    assert ext.rows([], None) == binding._rows_in_python([], None) == b""
+    t = grads[0]
+    wrong = [([t.double()], None), ([t.cpu()], None), ([normal(g, 4, 6)[:, 1:3]], None), ([t], []), ([t], out[:2]), ([t], [t.cpu()]),
+             ([t], [out[0][1:]]), ([t], [out[0].bfloat16()]), ([normal(g, 4, 6)], [normal(g, 6, 4).t()])]
+    for rows in (ext.rows, binding._rows_in_python):
+        for a in wrong:
+            with pytest.raises(ValueError):
+                rows(*a)
+    with pytest.raises(ValueError):
+        ext.rows([1], None)
+    for call in (lambda: sagnn.grad_global_norm(x for x in grads), lambda: sagnn.grad_clip_norm((x.clone() for x in grads), 1.0)):
+        assert float(call()) == pytest.approx(float(sagnn.grad_global_norm(grads)), rel=1e-6)
 
 
 def test_clipping_writes_nothing_beside_its_tensors():

@@ -133,6 +133,7 @@ def test_clipping_refuses():
     for row in ([0, P, 9, 0], [P, 0, 9, 0], [P, P, -1, 0], [P, P, 9, 2], [P, P, 9, -1], [P + 2, P, 9, 0], [P, P + 2, 9, 0], [P + 1, P, 9, 1],
                 [P, P, 1 << 50, 0]):
         assert clip(grad_rows(row)) == EINVAL, row
+    assert clip(grad_rows([1 << 48, 1 << 48, 9, 0])) == EINVAL and clip(grad_rows([P, 1 << 48, 9, 0])) == EINVAL
     # what is written is shared: a tensor twice, one inside another, an output over another's input, over half of its own
     for rows in ([[P, P, 10, 0], [P, P, 10, 0]], [[P, P, 1000, 0], [P + 8, P + 8, 10, 0]], [[P, P, 10, 0], [P + 400, P + 36, 10, 0]],
                  [[P, P + 4, 10, 0]], [[P, P + (1 << 16), 10, 1], [P + 64, P + (1 << 16) + 18, 10, 1]],
