@@ -128,6 +128,26 @@ def test_gradients_of_ragged_groups(sizes, mode):
 
 
 @pytest.mark.parametrize("mode", ["fp32", "x3", "rounded", "bf16"])
+@pytest.mark.parametrize("sizes", [[37, 0, 20], [9000, 5000, 71]], ids=lambda s: f"{sum(s)}")
+def test_masks_of_every_width_in_four(sizes, mode):
+    dtype = torch.bfloat16 if mode == "bf16" else torch.float32
+    off, m = offsets(sizes), sum(sizes)
+    for n in (1, 2, 3, 4, 5, 6, 7, 30, 33, 66, 127, 129, 131, 259):
+        g = gen(n)
+        X, W = normal(g, m, 24, dtype=dtype), normal(g, len(sizes), 24, n, dtype=dtype)
+        wide = normal(g, m, n + 3, dtype=dtype)             # (rows that begin anywhere, and what lies beside them would pass other values)
+        mask = wide[:, 1:n + 1]
+        mask[::7] = float("nan")
+        mask[1::7] = 0.0
+        mask[2::7] = float("inf")
+        Y = sagnn.grouped_gemm_act(X, W, off, mask=mask, prec=PREC[mode])
+        ref, terms = plain_product(X, W, off, False, mode)
+        ref = torch.where(mask > 0, ref, 0.0)
+        close(Y, ref, 1e-5 * terms + rounding(dtype, ref) + 1e-30, f"{n} columns")
+        assert not Y[~(mask > 0)].any()
+
+
+@pytest.mark.parametrize("mode", ["fp32", "x3", "rounded", "bf16"])
 @pytest.mark.parametrize("m,types,k,n", [(4100, 3, 512, 384), (3000, 2, 320, 576), (1500, 5, 1024, 136), (2600, 1, 264, 1544)])
 def test_products_that_fill_large_tiles(m, types, k, n, mode):
     """Widths and groups of several of the largest tiles and a part of one in each direction."""
