@@ -894,6 +894,8 @@ WholePlan whole_plan(int64_t m, int32_t segments, int64_t max_rows, int32_t C, i
   w.threads = vectors <= 64 * 4 && w.slab / v <= 64 ? 64 : vectors <= 256 * 4 && w.slab / v <= 256 ? 256 : kMostTeam;
   return w;
 }
+// Forward: eight values only where they are of one group.  Of several, 512 threads' sums of them are 64 KB of LDS and the groups' more.
+constexpr int whole_vector(int v, int D) { return v > 4 && D % v ? 4 : v; }
 size_t whole_lds(const WholePlan& w, int32_t D, int v, bool backward) {
   return ((size_t)(w.slab / D) + (size_t)w.threads * (D % v == 0 ? 1 : v)) * sizeof(double2) + (backward ? (size_t)w.threads * v * sizeof(float2) : 0);
 }
@@ -906,6 +908,7 @@ NormForm norm_form(int32_t dtype, int64_t m, int32_t segments, int64_t max_rows,
   const int size = dtype == SAGNN_BF16 ? 2 : 4;
   int v = vector_of(dtype, C);
   if (backward && v * size > 8) v /= 2;
+  if (!backward) v = whole_vector(v, D);
   if (m > 0 && ld <= kWholeLd) f.whole = whole_plan(m, segments, max_rows, C, D, v, size, !backward ? kKept : D % v == 0 ? kKeptBackward : kKeptBackward / 2, backward);
   if (((int64_t)segments + 16) * f.whole.slabs > INT32_MAX) f.whole.slab = 0;
   if (f.whole.slab) {
@@ -986,8 +989,11 @@ SAGNN_EXPORT int group_norm_act_fwd(int32_t dtype, const void* d_X, int64_t ldx,
     using S = decltype(zero);
     if (w.slab) {
       const dim3 grid((uint32_t)(n_seg + (d_seg ? 16 : 0)) * w.slabs);            // (sixteen for the rows behind the last segment)
-      if (a.D % v == 0) norm_whole_kernel<S, v, 1, ACT><<<grid, (uint32_t)w.threads, whole_lds(w, a.D, v, false), s>>>(a, w.slabs);
-      else norm_whole_kernel<S, v, v, ACT><<<grid, (uint32_t)w.threads, whole_lds(w, a.D, v, false), s>>>(a, w.slabs);
+      constexpr int u = v > 4 ? 4 : v;
+      const size_t lds = whole_lds(w, a.D, whole_vector(v, a.D), false);
+      if (a.D % v == 0) norm_whole_kernel<S, v, 1, ACT><<<grid, (uint32_t)w.threads, lds, s>>>(a, w.slabs);
+      else if (a.D % u == 0) norm_whole_kernel<S, u, 1, ACT><<<grid, (uint32_t)w.threads, lds, s>>>(a, w.slabs);
+      else norm_whole_kernel<S, u, u, ACT><<<grid, (uint32_t)w.threads, lds, s>>>(a, w.slabs);
       SAGNN_LAUNCH_CHECK();
       return (int)SAGNN_OK;
     }

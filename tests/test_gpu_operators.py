@@ -334,6 +334,31 @@ def test_norm_of_ragged_segments(sizes, dtype):
 
 
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("rows", [1, 12, 40, 300])
+@pytest.mark.parametrize("c,groups", [(1000, 250), (4096, 1024), (1024, 1024), (1000, 8), (16384, 4), (528, 44)])
+def test_norm_of_many_and_of_wide_groups(c, groups, rows, dtype):
+    g = gen(c + rows)
+    X, G = normal(g, 3 * rows, c, dtype=dtype), normal(g, 3 * rows, c, dtype=dtype)
+    known = rows if rows < 300 else 0
+    x, h = (t.double().view(3, rows, groups, -1) for t in (X, G))
+    n = rows * (c // groups)
+    mean = x.mean((1, 3), keepdim=True)
+    rstd = ((x - mean).square().mean((1, 3), keepdim=True) + 1e-2).rsqrt()
+    xh = (x - mean) * rstd
+    size = (x.abs() + mean.abs()) * rstd
+    Y, m32, r32 = sagnn.group_norm_act(X, groups, n_seg=3, max_rows=known, eps=1e-2)
+    close(Y, xh.view_as(X), 2.0 ** -20 * size.view_as(X) + 1.01 * rounding(dtype, xh.view_as(X)) + 1e-30, "y")
+    dX, dgamma, dbeta = sagnn.group_norm_act_bwd(X, G, m32, r32, groups, torch.ones(c, device="cuda"), torch.zeros(c, device="cuda"), n_seg=3,
+                                                 max_rows=known)
+    s1, s2 = h.mean((1, 3), keepdim=True), (h * xh).mean((1, 3), keepdim=True)
+    dx = (rstd * (h - s1 - xh * s2)).view_as(X)
+    a1, a2 = h.abs().mean((1, 3), keepdim=True), (h.abs() * size).mean((1, 3), keepdim=True)
+    close(dX, dx, 1e-5 * (rstd * (h.abs() + a1 + size * a2)).view_as(X) + 1.01 * rounding(dtype, dx) + 1e-30, "dx")
+    close(dgamma, (h * xh).sum((0, 1)).flatten(), 1e-5 * (h.abs() * size).sum((0, 1)).flatten() + 1e-30, "dgamma")
+    close(dbeta, h.sum((0, 1)).flatten(), 1e-5 * h.abs().sum((0, 1)).flatten() + 1e-30, "dbeta")
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
 @pytest.mark.parametrize("n_seg,rows,c,groups", [(1, 1, 4, 1), (6, 50, 64, 4), (2, 1025, 48, 16), (300, 1, 128, 1), (1, 20000, 320, 32)])
 def test_norm_of_equal_segments_is_that_of_their_offsets(n_seg, rows, c, groups, dtype):
     g = gen(rows)
