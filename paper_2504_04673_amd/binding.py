@@ -761,12 +761,12 @@ def grouped_gemm_act(X, W, off, transW=False, prec=GEMM_FP32, act=ACT_IDENTITY, 
     if mask is not None:
         _shape(_typed(mask, "mask", X.dtype), (m, nout), "mask")
     if out is None:
-        out = torch.empty((m, nout), dtype=X.dtype, device=X.device)
+        out, ldy = X.new_empty((m, nout)), nout
     else:
-        _shape(_typed(out, "out", X.dtype), (m, nout), "out")
-    _check(_calls().grouped_gemm_act(_DTYPE[X.dtype], X.data_ptr(), _ld(X), W.data_ptr(), ldw, stride_w, int(transW), off.data_ptr(), types,
-                                     m, kdim, nout, prec, act, _ptr(mask), _ld(mask) if mask is not None else 0, out.data_ptr(), _ld(out),
-                                     _stream()), "grouped_gemm_act")
+        ldy = _ld(_shape(_typed(out, "out", X.dtype), (m, nout), "out"))
+    _check(_calls().grouped_gemm_act(_DTYPE[X.dtype], X.data_ptr(), kdim if X.is_contiguous() else _ld(X), W.data_ptr(), ldw, stride_w,
+                                     int(transW), off.data_ptr(), types, m, kdim, nout, prec, act, _ptr(mask),
+                                     _ld(mask) if mask is not None else 0, out.data_ptr(), ldy, _stream()), "grouped_gemm_act")
     return out
 
 
@@ -786,11 +786,12 @@ def grouped_gemm_bwd(X, W, off, G, mask=None, prec=GEMM_FP32, want_dx=True, want
         raise ValueError("the gradient of W needs X")
     if mask is not None:
         _shape(_typed(mask, "mask", G.dtype), (m, kdim), "mask")
-    dX = torch.empty((m, kdim), dtype=G.dtype, device=G.device) if want_dx else None
+    dX = G.new_empty((m, kdim)) if want_dx else None
     dW = ws = None
     if want_dw:
-        dW = torch.empty((types, kdim, nout), dtype=torch.float32, device=G.device)
-        ws = _ws(_bytes_of("grouped_gemm_bwd_workspace_bytes", m, types, kdim, nout), G.device)
+        dW = G.new_empty((types, kdim, nout), dtype=torch.float32)
+        need = _bytes_of("grouped_gemm_bwd_workspace_bytes", m, types, kdim, nout)
+        ws = _ws(need, G.device) if need else None
     _check(_calls().grouped_gemm_bwd(_DTYPE[G.dtype], _ptr(X), _ld(X) if X is not None else kdim, _ptr(W), ldw, stride_w, _ptr(off), types,
                                      m, kdim, nout, prec, _ptr(G), _ld(G), _ptr(mask), _ld(mask) if mask is not None else 0, _ptr(dX), kdim,
                                      _ptr(dW), _ptr(ws), ws.numel() if ws is not None else 0, _stream()), "grouped_gemm_bwd")
@@ -807,11 +808,12 @@ def _norm_args(X, groups, gamma, beta, seg, n_seg, out):
         _shape(_dev(gamma, torch.float32, "gamma"), shape[1:], "gamma")
     if beta is not None:
         _shape(_dev(beta, torch.float32, "beta"), shape[1:], "beta")
+    whole = X.is_contiguous()
     if out is None:
-        out = torch.empty(shape, dtype=X.dtype, device=X.device)
+        out, ldo = torch.empty_like(X) if whole else X.new_empty(shape), shape[1]
     else:
-        _shape(_typed(out, "out", X.dtype), shape, "out")
-    return *shape, n_seg, out, _ld(X), _ld(out)
+        ldo = _ld(_shape(_typed(out, "out", X.dtype), shape, "out"))
+    return *shape, n_seg, out, shape[1] if whole else _ld(X), ldo
 
 
 def group_norm_act(X, groups, gamma=None, beta=None, seg=None, n_seg=1, max_rows=0, eps=1e-5, act=ACT_IDENTITY, out=None):
@@ -823,7 +825,8 @@ def group_norm_act(X, groups, gamma=None, beta=None, seg=None, n_seg=1, max_rows
     kind, dev = _DTYPE[X.dtype], X.device
     need = _bytes_of("group_norm_workspace_bytes", kind, m, n_seg, max_rows, c, groups, max(ldx, ldy), 0)
     ws = _ws(need, dev) if need else None
-    mean, rstd = torch.empty((2, n_seg, groups), dtype=torch.float32, device=dev).unbind()
+    mean = X.new_empty((n_seg, groups), dtype=torch.float32)
+    rstd = torch.empty_like(mean)
     _check(_calls().group_norm_act_fwd(kind, X.data_ptr(), ldx, _ptr(seg), n_seg, max_rows, m, c, groups, _ptr(gamma), _ptr(beta),
                                        eps, act, out.data_ptr(), ldy, mean.data_ptr(), rstd.data_ptr(), _ptr(ws), need, _stream()),
            "group_norm_act_fwd")
@@ -839,7 +842,8 @@ def group_norm_act_bwd(X, G, mean, rstd, groups, gamma=None, beta=None, seg=None
     kind, dev, ldg = _DTYPE[X.dtype], X.device, _ld(G)
     need = _bytes_of("group_norm_workspace_bytes", kind, m, n_seg, max_rows, c, groups, max(ldx, ldg, lddx), 1)
     ws = _ws(need, dev) if need else None
-    dgamma, dbeta = torch.empty((2, c), dtype=torch.float32, device=dev).unbind()
+    dgamma = X.new_empty(c, dtype=torch.float32)
+    dbeta = torch.empty_like(dgamma)
     _check(_calls().group_norm_act_bwd(kind, X.data_ptr(), ldx, G.data_ptr(), ldg, _ptr(seg), n_seg, max_rows, m, c, groups, _ptr(gamma),
                                        _ptr(beta), act, mean.data_ptr(), rstd.data_ptr(), out.data_ptr(), lddx, dgamma.data_ptr(),
                                        dbeta.data_ptr(), _ptr(ws), need, _stream()), "group_norm_act_bwd")
