@@ -829,7 +829,15 @@ __global__ __launch_bounds__(kMostTeam, 4) void norm_bwd_whole_kernel(const Norm
   }
   if (t.ty == 0)
 #pragma unroll
-    for (int i = 0; i < V; ++i) a.rows[stripe * a.C + ch + i] = all[i * blockDim.x];
+    for (int i = 0; i < V; ++i) {
+      const float2 v = all[i * blockDim.x];
+      if (stripes > 1) {
+        a.rows[stripe * a.C + ch + i] = v;
+      } else {                                              // (the only row: nothing to join)
+        if (a.dgamma) a.dgamma[ch + i] = v.x;
+        if (a.dbeta) a.dbeta[ch + i] = v.y;
+      }
+    }
 }
 
 // Values that a thread takes at a time: what 16 bytes hold, and a divisor of the width
@@ -913,7 +921,7 @@ NormForm norm_form(int32_t dtype, int64_t m, int32_t segments, int64_t max_rows,
   if (((int64_t)segments + 16) * f.whole.slabs > INT32_MAX) f.whole.slab = 0;
   if (f.whole.slab) {
     f.table = segments < kMostStripes ? segments : kMostStripes;
-    f.bytes = backward ? round_up((size_t)f.table * C * sizeof(float2), 256) : 0;
+    f.bytes = backward && f.table > 1 ? round_up((size_t)f.table * C * sizeof(float2), 256) : 0;
   } else {
     f.parts = norm_plan(dtype, m, segments, C, groups, backward);
     f.table = m > 0 ? f.parts.chunks : 0;
@@ -1048,8 +1056,10 @@ SAGNN_EXPORT int group_norm_act_bwd(int32_t dtype, const void* d_X, int64_t ldx,
       if (a.D % u == 0) norm_bwd_whole_kernel<S, u, 1, ACT><<<grid, (uint32_t)w.threads, lds, s>>>(a, w.slabs);
       else norm_bwd_whole_kernel<S, u, u, ACT><<<grid, (uint32_t)w.threads, lds, s>>>(a, w.slabs);
       SAGNN_LAUNCH_CHECK();
-      norm_bwd_join_kernel<<<dim3((uint32_t)wide), kJoinThreads, 0, s>>>(a, wide);
-      SAGNN_LAUNCH_CHECK();
+      if (a.table > 1) {
+        norm_bwd_join_kernel<<<dim3((uint32_t)wide), kJoinThreads, 0, s>>>(a, wide);
+        SAGNN_LAUNCH_CHECK();
+      }
       return (int)SAGNN_OK;
     }
     if (m > 0) {
