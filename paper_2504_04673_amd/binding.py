@@ -791,7 +791,7 @@ def grouped_gemm_bwd(X, W, off, G, mask=None, prec=GEMM_FP32, want_dx=True, want
     if want_dw:
         dW = G.new_empty((types, kdim, nout), dtype=torch.float32)
         need = _bytes_of("grouped_gemm_bwd_workspace_bytes", m, types, kdim, nout)
-        ws = _ws(need, G.device) if need else None
+        ws = G.new_empty(need, dtype=torch.uint8) if need else None
     _check(_calls().grouped_gemm_bwd(_DTYPE[G.dtype], _ptr(X), _ld(X) if X is not None else kdim, _ptr(W), ldw, stride_w, _ptr(off), types,
                                      m, kdim, nout, prec, _ptr(G), _ld(G), _ptr(mask), _ld(mask) if mask is not None else 0, _ptr(dX), kdim,
                                      _ptr(dW), _ptr(ws), ws.numel() if ws is not None else 0, _stream()), "grouped_gemm_bwd")
@@ -822,9 +822,9 @@ def group_norm_act(X, groups, gamma=None, beta=None, seg=None, n_seg=1, max_rows
     the last are zeros in Y), or None for n_seg segments of equal length; max_rows: rows of the longest one where it is known.
     Returns (Y, mean, rstd), the last two float32, segments x groups."""
     m, c, n_seg, out, ldx, ldy = _norm_args(X, groups, gamma, beta, seg, n_seg, out)
-    kind, dev = _DTYPE[X.dtype], X.device
+    kind = _DTYPE[X.dtype]
     need = _bytes_of("group_norm_workspace_bytes", kind, m, n_seg, max_rows, c, groups, max(ldx, ldy), 0)
-    ws = _ws(need, dev) if need else None
+    ws = X.new_empty(need, dtype=torch.uint8) if need else None
     mean = X.new_empty((n_seg, groups), dtype=torch.float32)
     rstd = torch.empty_like(mean)
     _check(_calls().group_norm_act_fwd(kind, X.data_ptr(), ldx, _ptr(seg), n_seg, max_rows, m, c, groups, _ptr(gamma), _ptr(beta),
@@ -839,9 +839,9 @@ def group_norm_act_bwd(X, G, mean, rstd, groups, gamma=None, beta=None, seg=None
     _shape(_typed(G, "G", X.dtype), (m, c), "G")
     for name, t in (("mean", mean), ("rstd", rstd)):
         _shape(_dev(t, torch.float32, name), (n_seg, groups), name)
-    kind, dev, ldg = _DTYPE[X.dtype], X.device, _ld(G)
+    kind, ldg = _DTYPE[X.dtype], _ld(G)
     need = _bytes_of("group_norm_workspace_bytes", kind, m, n_seg, max_rows, c, groups, max(ldx, ldg, lddx), 1)
-    ws = _ws(need, dev) if need else None
+    ws = X.new_empty(need, dtype=torch.uint8) if need else None
     dgamma = X.new_empty(c, dtype=torch.float32)
     dbeta = torch.empty_like(dgamma)
     _check(_calls().group_norm_act_bwd(kind, X.data_ptr(), ldx, G.data_ptr(), ldg, _ptr(seg), n_seg, max_rows, m, c, groups, _ptr(gamma),
@@ -887,16 +887,18 @@ def _bytes_of(query: str, *sizes) -> int:
     return b.value
 
 
-def _grad_ws(n, device):
-    return _ws(_bytes_of("grad_norm_workspace_bytes", n), device), torch.empty(1, dtype=torch.float32, device=device)
+def _grad_ws(grads, n):
+    """Room for the sums, how much that is, and the norm's place."""
+    like, need = grads[0] if n else torch.empty(0, device="cuda"), _bytes_of("grad_norm_workspace_bytes", n)
+    return like.new_empty(need, dtype=torch.uint8), need, like.new_empty(1, dtype=torch.float32)
 
 
 def grad_global_norm(grads):
     """The 2-norm over all tensors of the list, a float32 tensor of one element on the device."""
     grads = _listed(grads)
     rows, n = _grad_list(grads)
-    ws, norm = _grad_ws(n, grads[0].device if n else "cuda")
-    _check(_calls().grad_global_norm(rows, n, _ptr(norm), _ptr(ws), ws.numel(), _stream()), "grad_global_norm")
+    ws, need, norm = _grad_ws(grads, n)
+    _check(_calls().grad_global_norm(rows, n, norm.data_ptr(), ws.data_ptr(), need, _stream()), "grad_global_norm")
     return norm
 
 
@@ -909,6 +911,6 @@ def grad_clip_norm(grads, max_norm: float, norm=None, out=None):
         _shape(_dev(norm, torch.float32, "norm"), (1,), "norm")
         _check(_calls().grad_scale_to_norm(rows, n, max_norm, _ptr(norm), _stream()), "grad_scale_to_norm")
         return norm
-    ws, norm = _grad_ws(n, grads[0].device if n else "cuda")
-    _check(_calls().grad_clip_norm(rows, n, max_norm, _ptr(norm), _ptr(ws), ws.numel(), _stream()), "grad_clip_norm")
+    ws, need, norm = _grad_ws(grads, n)
+    _check(_calls().grad_clip_norm(rows, n, max_norm, norm.data_ptr(), ws.data_ptr(), need, _stream()), "grad_clip_norm")
     return norm
