@@ -822,6 +822,8 @@ def group_norm_act(X, groups, gamma=None, beta=None, seg=None, n_seg=1, max_rows
     the last are zeros in Y), or None for n_seg segments of equal length; max_rows: rows of the longest one where it is known.
     Returns (Y, mean, rstd), the last two float32, segments x groups."""
     m, c, n_seg, out, ldx, ldy = _norm_args(X, groups, gamma, beta, seg, n_seg, out)
+    if seg is None and not max_rows and n_seg > 1:
+        max_rows = m // n_seg
     kind = _DTYPE[X.dtype]
     need = _bytes_of("group_norm_workspace_bytes", kind, m, n_seg, max_rows, c, groups, max(ldx, ldy), 0)
     ws = X.new_empty(need, dtype=torch.uint8) if need else None
@@ -836,6 +838,8 @@ def group_norm_act(X, groups, gamma=None, beta=None, seg=None, n_seg=1, max_rows
 def group_norm_act_bwd(X, G, mean, rstd, groups, gamma=None, beta=None, seg=None, n_seg=1, max_rows=0, act=ACT_IDENTITY, out=None):
     """Gradients of group_norm_act for G = dLoss/dY, with the mean and rstd that it returned.  Returns (dX, dgamma, dbeta)."""
     m, c, n_seg, out, ldx, lddx = _norm_args(X, groups, gamma, beta, seg, n_seg, out)
+    if seg is None and not max_rows and n_seg > 1:
+        max_rows = m // n_seg
     _shape(_typed(G, "G", X.dtype), (m, c), "G")
     for name, t in (("mean", mean), ("rstd", rstd)):
         _shape(_dev(t, torch.float32, name), (n_seg, groups), name)
