@@ -1,5 +1,5 @@
 """A graph network over vertices of several types, trained on one GPU: every layer aggregates (sparse product), multiplies by
-the weights of the vertex's type, normalises over the vertices of each graph of the batch and applies ReLU; the last one ends
+the weights of the vertex's type, normalises over the vertices of each type and applies ReLU; the last one ends
 with the product.  All of it, gradients and clipping included, runs in the library's kernels; torch holds the tensors, takes
 the loss's gradient and subtracts.
 
@@ -7,7 +7,7 @@ the loss's gradient and subtracts.
 
     python -m paper_2504_04673_amd.typed_gcn [--vertices N] [--types K] [--steps S]
 
-makes a synthetic batch of graphs with random types, orders its vertices by type (spmm_perm_from_labels) and prints the loss,
+makes a random graph with random types, orders its vertices by type (spmm_perm_from_labels) and prints the loss,
 the gradients' norm and the time of each step.
 """
 from __future__ import annotations
