@@ -249,9 +249,16 @@ def _mat(t: torch.Tensor, name: str):
         raise ValueError(f"{name} must be a CUDA/HIP tensor (there is no CPU path)")
     if t.dtype is not torch.float32 or t.dim() != 2:
         raise ValueError(f"{name}: expected a 2-D float32 tensor")
-    if not t.is_contiguous() and t.shape[0] > 1 and t.shape[1] > 0 and (t.stride(1) != 1 or t.stride(0) < t.shape[1]):
-        raise ValueError(f"{name}: rows must be contiguous (unit stride inside a row)")
+    if not t.is_contiguous() and not _rows_apart(t):
+        raise ValueError(f"{name}: rows must be contiguous (unit stride inside a row) and must not overlap")
     return t
+
+
+def _rows_apart(t: torch.Tensor) -> bool:
+    """Whether a matrix (with elements) lies row by row.  A row's own stride is asked for however many rows there are, a
+    single one too; what lies between rows only where there are two."""
+    n, f = t.shape
+    return (f == 1 or t.stride(1) == 1) and (n == 1 or t.stride(0) >= f)
 
 
 def _ld(t: torch.Tensor) -> int:
@@ -715,7 +722,7 @@ def _typed(t: torch.Tensor, name: str, dtype=None):
     kind = t.dtype
     if t.dim() != 2 or (kind not in _DTYPE if dtype is None else kind is not dtype):
         raise ValueError(f"{name}: expected a 2-D tensor of " + (str(dtype) if dtype is not None else "float32 or bfloat16"))
-    if not t.is_contiguous() and t.shape[0] > 1 and t.shape[1] > 0 and ((t.shape[1] > 1 and t.stride(1) != 1) or t.stride(0) < t.shape[1]):
+    if not t.is_contiguous() and not _rows_apart(t):
         raise ValueError(f"{name}: rows must be contiguous (unit stride inside a row) and must not overlap")
     return t
 
