@@ -34,6 +34,9 @@ inline int hip_fail(hipError_t e) {
 inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 inline size_t round_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
 inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+// Workgroups of `threads` along a launch's x: the runtime counts threads there in 32 bits, and more than they hold are not
+// started, without an error
+constexpr int64_t most_blocks(int threads) { return ((int64_t(1) << 32) - 1) / threads; }
 
 // --- SpMM workspace geometry (host and device agree through these) -----------------------
 // Chunks of the nonzero-splitting schedule: about T entries each, T a multiple of 16.  Long enough that what a

@@ -27,6 +27,7 @@ struct NormArgs {
   float* dgamma; float* dbeta;
   int64_t chunk, chunks;             // rows of a chunk, chunks
   int64_t table;                     // rows of `rows`
+  int64_t first;                     // forward, whole segments: segments of the launches before this one
   bool joined;                       // the workgroups that write join the parts of their segments, each for itself
   int32_t slab;                      // channels of a workgroup, where it takes whole segments
   double2* parts;                    // (chunks + segments) x groups
@@ -286,15 +287,18 @@ __device__ __forceinline__ float2 means(const NormArgs& a, double2 s, int64_t ro
   return make_float2((float)(s.x / n), (float)(s.y / n));
 }
 
+// Workgroups that join the parts of segments and groups, one for each wavefront, in turn beyond that
+constexpr int64_t kMostJoins = 1 << 20;
 __global__ __launch_bounds__(kThreads) void norm_join_kernel(const NormArgs a) {
-  const int64_t at = (int64_t)blockIdx.x * (kThreads / 64) + (threadIdx.x >> 6);
-  if (at >= (int64_t)a.segments * a.groups) return;
-  const int32_t b = (int32_t)(at / a.groups), g = (int32_t)(at % a.groups);
-  const int64_t lo = seg_row(a, b), hi = seg_row(a, b + 1);
-  const float2 s = moments(a, join_parts(a, b, g, lo, hi, 64), hi - lo);
-  if ((threadIdx.x & 63) == 0) {
-    a.mean[at] = s.x;
-    a.rstd[at] = s.y;
+  for (int64_t at = (int64_t)blockIdx.x * (kThreads / 64) + (threadIdx.x >> 6); at < (int64_t)a.segments * a.groups;
+       at += (int64_t)gridDim.x * (kThreads / 64)) {
+    const int32_t b = (int32_t)(at / a.groups), g = (int32_t)(at % a.groups);
+    const int64_t lo = seg_row(a, b), hi = seg_row(a, b + 1);
+    const float2 s = moments(a, join_parts(a, b, g, lo, hi, 64), hi - lo);
+    if ((threadIdx.x & 63) == 0) {
+      a.mean[at] = s.x;
+      a.rstd[at] = s.y;
+    }
   }
 }
 
@@ -499,12 +503,13 @@ __global__ __launch_bounds__(kJoinThreads) void norm_bwd_join_kernel(const NormA
     join_rows<kJoinThreads>(a, (int32_t)blockIdx.x);
     return;
   }
-  const int64_t at = (int64_t)(blockIdx.x - wide) * (kJoinThreads / 64) + (threadIdx.x >> 6);
-  if (at >= (int64_t)a.segments * a.groups) return;
-  const int32_t b = (int32_t)(at / a.groups), g = (int32_t)(at % a.groups);
-  const int64_t lo = seg_row(a, b), hi = seg_row(a, b + 1);
-  const float2 s = means(a, join_parts(a, b, g, lo, hi, 64), hi - lo);
-  if ((threadIdx.x & 63) == 0) a.sums[at] = s;
+  for (int64_t at = (int64_t)(blockIdx.x - wide) * (kJoinThreads / 64) + (threadIdx.x >> 6); at < (int64_t)a.segments * a.groups;
+       at += (int64_t)(gridDim.x - wide) * (kJoinThreads / 64)) {
+    const int32_t b = (int32_t)(at / a.groups), g = (int32_t)(at % a.groups);
+    const int64_t lo = seg_row(a, b), hi = seg_row(a, b + 1);
+    const float2 s = means(a, join_parts(a, b, g, lo, hi, 64), hi - lo);
+    if ((threadIdx.x & 63) == 0) a.sums[at] = s;
+  }
 }
 
 // dx = h gamma rstd - rstd s1 - rstd s2 (rstd x + base) = h scale + tilt x + level, s1 and s2 the means of the group's sums
@@ -633,13 +638,14 @@ __device__ __forceinline__ Whole<S, V> fetch_at(const void* row, uint32_t lane) 
   return fetch<S, V>(reinterpret_cast<const S*>(reinterpret_cast<const char*>(row) + lane));
 }
 
+constexpr int kBehind = 16;                // workgroups of a slab for the rows behind the last segment
 template <typename S, int V, int N, int ACT>
 __global__ __launch_bounds__(kMostTeam) void norm_whole_kernel(const NormArgs a, int32_t slabs) {
   extern __shared__ __attribute__((aligned(16))) char smem[];
   const Team t = team<V>(a, (int)(blockIdx.x % slabs));
-  const int64_t b = blockIdx.x / slabs, blocks = gridDim.x / slabs;
+  const int64_t b = a.first + blockIdx.x / slabs;
   if (b >= a.segments) {
-    team_zeros<S, V>(a, t, b - a.segments, blocks - a.segments);
+    team_zeros<S, V>(a, t, b - a.segments, kBehind);
     return;
   }
   double2* sums = reinterpret_cast<double2*>(smem);
@@ -918,7 +924,6 @@ NormForm norm_form(int32_t dtype, int64_t m, int32_t segments, int64_t max_rows,
   if (backward && v * size > 8) v /= 2;
   if (!backward) v = whole_vector(v, D);
   if (m > 0 && ld <= kWholeLd) f.whole = whole_plan(m, segments, max_rows, C, D, v, size, !backward ? kKept : D % v == 0 ? kKeptBackward : kKeptBackward / 2, backward);
-  if (((int64_t)segments + 16) * f.whole.slabs > INT32_MAX) f.whole.slab = 0;
   if (f.whole.slab) {
     f.table = segments < kMostStripes ? segments : kMostStripes;
     f.bytes = backward && f.table > 1 ? round_up((size_t)f.table * C * sizeof(float2), 256) : 0;
@@ -996,13 +1001,16 @@ SAGNN_EXPORT int group_norm_act_fwd(int32_t dtype, const void* d_X, int64_t ldx,
     constexpr int v = decltype(V)::value, ACT = decltype(A)::value;
     using S = decltype(zero);
     if (w.slab) {
-      const dim3 grid((uint32_t)(n_seg + (d_seg ? 16 : 0)) * w.slabs);            // (sixteen for the rows behind the last segment)
+      const int64_t blocks = (int64_t)n_seg + (d_seg ? kBehind : 0), most = most_blocks(w.threads) / w.slabs;
       constexpr int u = v > 4 ? 4 : v;
       const size_t lds = whole_lds(w, a.D, whole_vector(v, a.D), false);
-      if (a.D % v == 0) norm_whole_kernel<S, v, 1, ACT><<<grid, (uint32_t)w.threads, lds, s>>>(a, w.slabs);
-      else if (a.D % u == 0) norm_whole_kernel<S, u, 1, ACT><<<grid, (uint32_t)w.threads, lds, s>>>(a, w.slabs);
-      else norm_whole_kernel<S, u, u, ACT><<<grid, (uint32_t)w.threads, lds, s>>>(a, w.slabs);
-      SAGNN_LAUNCH_CHECK();
+      for (a.first = 0; a.first < blocks; a.first += most) {
+        const dim3 grid((uint32_t)((blocks - a.first < most ? blocks - a.first : most) * w.slabs));
+        if (a.D % v == 0) norm_whole_kernel<S, v, 1, ACT><<<grid, (uint32_t)w.threads, lds, s>>>(a, w.slabs);
+        else if (a.D % u == 0) norm_whole_kernel<S, u, 1, ACT><<<grid, (uint32_t)w.threads, lds, s>>>(a, w.slabs);
+        else norm_whole_kernel<S, u, u, ACT><<<grid, (uint32_t)w.threads, lds, s>>>(a, w.slabs);
+        SAGNN_LAUNCH_CHECK();
+      }
       return (int)SAGNN_OK;
     }
     if (m > 0) {
@@ -1010,7 +1018,8 @@ SAGNN_EXPORT int group_norm_act_fwd(int32_t dtype, const void* d_X, int64_t ldx,
       SAGNN_LAUNCH_CHECK();
     }
     if (!a.joined) {
-      norm_join_kernel<<<dim3((uint32_t)ceil_div((int64_t)n_seg * n_groups, kThreads / 64)), kThreads, 0, s>>>(a);
+      const int64_t joins = ceil_div((int64_t)n_seg * n_groups, kThreads / 64);
+      norm_join_kernel<<<dim3((uint32_t)(joins < kMostJoins ? joins : kMostJoins)), kThreads, 0, s>>>(a);
       SAGNN_LAUNCH_CHECK();
     }
     if (m > 0) {
@@ -1067,7 +1076,8 @@ SAGNN_EXPORT int group_norm_act_bwd(int32_t dtype, const void* d_X, int64_t ldx,
       SAGNN_LAUNCH_CHECK();
     }
     if (!a.joined) {
-      norm_bwd_join_kernel<<<dim3((uint32_t)(wide + ceil_div((int64_t)n_seg * n_groups, kJoinThreads / 64))), kJoinThreads, 0, s>>>(a, wide);
+      const int64_t joins = ceil_div((int64_t)n_seg * n_groups, kJoinThreads / 64);
+      norm_bwd_join_kernel<<<dim3((uint32_t)(wide + (joins < kMostJoins ? joins : kMostJoins))), kJoinThreads, 0, s>>>(a, wide);
       SAGNN_LAUNCH_CHECK();
     }
     if (m > 0) {

@@ -21,6 +21,7 @@ struct GroupedArgs {
   int64_t chunk;                                 // weight gradient: rows that one workgroup sums at most
   int32_t row_tiles, col_tiles;                  // of the launch
   int32_t pairs;                                 // weight gradient: numbers of pairs of a chunk and a group
+  int32_t first;                                 // workgroups of the launches before this one
 };
 
 // Rows of group g as the kernels see them: whatever d_off holds, they lie inside [0, m).
@@ -445,7 +446,7 @@ __global__ __launch_bounds__(WM * WN * 64) void grouped_kernel(const GroupedArgs
   __shared__ __attribute__((aligned(16))) char smem[TileShape<PREC, false, BM, BK>::kBytes + TileShape<PREC, !WT, BN, BK>::kBytes];
   GroupTile t;
   int32_t col;
-  if (!grouped_find<BM>(a, (int32_t)blockIdx.x, t, col)) return;
+  if (!grouped_find<BM>(a, a.first + (int32_t)blockIdx.x, t, col)) return;
   const int64_t c0 = (int64_t)col * BN;
   const int rows = (int)(t.end - t.r0 < BM ? t.end - t.r0 : BM), cols = (int)(a.nout - c0 < BN ? a.nout - c0 : BN);
   floatx16 acc[TM][TN];
@@ -468,7 +469,7 @@ __global__ __launch_bounds__(WAVES * 64) void grouped_thin_kernel(const GroupedA
   __shared__ __attribute__((aligned(16))) char smem[WAVES * (kOwn > kSums ? kOwn : kSums)];
   GroupTile t;
   int32_t col;
-  if (!grouped_find<32>(a, (int32_t)blockIdx.x, t, col)) return;
+  if (!grouped_find<32>(a, a.first + (int32_t)blockIdx.x, t, col)) return;
   const int64_t c0 = (int64_t)col * BN;
   const int rows = (int)(t.end - t.r0 < 32 ? t.end - t.r0 : 32), cols = (int)(a.nout - c0 < BN ? a.nout - c0 : BN);
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -531,7 +532,7 @@ __global__ __launch_bounds__(WM * WN * 64) void grouped_tn_kernel(const GroupedA
   __shared__ __attribute__((aligned(16))) char smem[TileShape<PREC, true, BM, BK>::kBytes + TileShape<PREC, true, BN, BK>::kBytes];
   GroupPart p;
   int32_t tile;
-  if (!grouped_part(a, (int32_t)blockIdx.x, p, tile)) return;
+  if (!grouped_part(a, a.first + (int32_t)blockIdx.x, p, tile)) return;
   const int64_t k0 = (int64_t)(tile / a.col_tiles) * BM, c0 = (int64_t)(tile % a.col_tiles) * BN;
   const int rows = (int)(a.kdim - k0 < BM ? a.kdim - k0 : BM), cols = (int)(a.nout - c0 < BN ? a.nout - c0 : BN);
   floatx16 acc[TM][TN];
@@ -553,7 +554,7 @@ inline int grouped_tile_cols(int tile) {
   return cols[tile];
 }
 
-// one launch of `blocks` workgroups; per operand mode (and storage type)
+// a product of `blocks` workgroups; per operand mode (and storage type)
 #define SAGNN_GROUPED_MODE(name)                                                                                       \
   int grouped_##name(const GroupedArgs& a, int tile, bool trans_w, int64_t blocks, hipStream_t s);                      \
   int grouped_tn_##name(const GroupedArgs& a, int tile, int64_t blocks, hipStream_t s);
@@ -564,28 +565,40 @@ SAGNN_GROUPED_MODE(bf16)
 #undef SAGNN_GROUPED_MODE
 int grouped_bwd_bf16(const GroupedArgs& rows, int64_t rows_blocks, const GroupedArgs& tn, int64_t tn_blocks, hipStream_t s);
 
-template <typename S, int PREC, int BK, bool WT>
-int grouped_launch(const GroupedArgs& a, int tile, int64_t blocks, hipStream_t s) {
-  const dim3 grid((uint32_t)blocks), block(256);
-  if (tile == kTile128) grouped_kernel<S, PREC, WT, 2, 2, 2, 2, BK><<<grid, block, 0, s>>>(a);
-  else if (tile == kTile128x64) grouped_kernel<S, PREC, WT, 2, 2, 2, 1, BK><<<grid, block, 0, s>>>(a);
-  else if (tile == kTile128x32) grouped_kernel<S, PREC, WT, 4, 1, 1, 1, BK><<<grid, block, 0, s>>>(a);
-  else if (tile == kTile64) grouped_kernel<S, PREC, WT, 2, 2, 1, 1, BK><<<grid, block, 0, s>>>(a);
-  else if (tile == kThin) grouped_thin_kernel<S, PREC, WT, kThinCols / 32, 8, BK == 32 && PREC != SAGNN_GEMM_FP32 ? 16 : BK><<<grid, 512, 0, s>>>(a);
-  else grouped_kernel<S, PREC, WT, 1, 4, 1, 1, BK><<<grid, block, 0, s>>>(a);
-  SAGNN_LAUNCH_CHECK();
+// `blocks` workgroups: launch(arguments, grid), several times where they are more than one launch takes
+template <typename F>
+int grouped_launches(GroupedArgs a, int64_t blocks, int threads, F launch) {
+  const int64_t most = most_blocks(threads) / 8 * 8;        // (the XCDs are dealt to in turn)
+  for (int64_t b = 0; b < blocks; b += most) {
+    a.first = (int32_t)b;
+    launch(a, dim3((uint32_t)(blocks - b < most ? blocks - b : most)));
+    SAGNN_LAUNCH_CHECK();
+  }
   return SAGNN_OK;
 }
+
+template <typename S, int PREC, int BK, bool WT>
+int grouped_launch(const GroupedArgs& args, int tile, int64_t blocks, hipStream_t s) {
+  const dim3 block(256);
+  return grouped_launches(args, blocks, tile == kThin ? 512 : 256, [&](const GroupedArgs& a, dim3 grid) {
+    if (tile == kTile128) grouped_kernel<S, PREC, WT, 2, 2, 2, 2, BK><<<grid, block, 0, s>>>(a);
+    else if (tile == kTile128x64) grouped_kernel<S, PREC, WT, 2, 2, 2, 1, BK><<<grid, block, 0, s>>>(a);
+    else if (tile == kTile128x32) grouped_kernel<S, PREC, WT, 4, 1, 1, 1, BK><<<grid, block, 0, s>>>(a);
+    else if (tile == kTile64) grouped_kernel<S, PREC, WT, 2, 2, 1, 1, BK><<<grid, block, 0, s>>>(a);
+    else if (tile == kThin) grouped_thin_kernel<S, PREC, WT, kThinCols / 32, 8, BK == 32 && PREC != SAGNN_GEMM_FP32 ? 16 : BK><<<grid, 512, 0, s>>>(a);
+    else grouped_kernel<S, PREC, WT, 1, 4, 1, 1, BK><<<grid, block, 0, s>>>(a);
+  });
+}
 template <typename S, int PREC, int BK>
-int grouped_tn_launch(const GroupedArgs& a, int tile, int64_t blocks, hipStream_t s) {
-  const dim3 grid((uint32_t)blocks), block(256);
-  if (tile == kTile128) grouped_tn_kernel<S, PREC, 2, 2, 2, 2, BK><<<grid, block, 0, s>>>(a);
-  else if (tile == kTile128x64) grouped_tn_kernel<S, PREC, 2, 2, 2, 1, BK><<<grid, block, 0, s>>>(a);
-  else if (tile == kTile128x32) grouped_tn_kernel<S, PREC, 4, 1, 1, 1, BK><<<grid, block, 0, s>>>(a);
-  else if (tile == kTile64) grouped_tn_kernel<S, PREC, 2, 2, 1, 1, BK><<<grid, block, 0, s>>>(a);
-  else grouped_tn_kernel<S, PREC, 1, 4, 1, 1, BK><<<grid, block, 0, s>>>(a);
-  SAGNN_LAUNCH_CHECK();
-  return SAGNN_OK;
+int grouped_tn_launch(const GroupedArgs& args, int tile, int64_t blocks, hipStream_t s) {
+  const dim3 block(256);
+  return grouped_launches(args, blocks, 256, [&](const GroupedArgs& a, dim3 grid) {
+    if (tile == kTile128) grouped_tn_kernel<S, PREC, 2, 2, 2, 2, BK><<<grid, block, 0, s>>>(a);
+    else if (tile == kTile128x64) grouped_tn_kernel<S, PREC, 2, 2, 2, 1, BK><<<grid, block, 0, s>>>(a);
+    else if (tile == kTile128x32) grouped_tn_kernel<S, PREC, 4, 1, 1, 1, BK><<<grid, block, 0, s>>>(a);
+    else if (tile == kTile64) grouped_tn_kernel<S, PREC, 2, 2, 1, 1, BK><<<grid, block, 0, s>>>(a);
+    else grouped_tn_kernel<S, PREC, 1, 4, 1, 1, BK><<<grid, block, 0, s>>>(a);
+  });
 }
 
 }  // namespace sagnn

@@ -234,7 +234,7 @@ SAGNN_EXPORT int grouped_gemm_bwd(int32_t dtype, const void* d_X, int64_t ldx, c
   }
   if (lx.blocks < 0 || lw.blocks < 0) return SAGNN_EINVAL;
   int rc = SAGNN_OK;
-  if (lx.blocks > 0 && lw.blocks > 0 && lx.tile == kDirect256 && lw.tile == kDirect256 && lx.blocks + lw.blocks <= INT32_MAX) {
+  if (lx.blocks > 0 && lw.blocks > 0 && lx.tile == kDirect256 && lw.tile == kDirect256 && lx.blocks + lw.blocks <= most_blocks(512)) {
     rc = grouped_bwd_bf16(x, lx.blocks, w, lw.blocks, s);
   } else {
     if (d_dX && m > 0) rc = launch_rows(x, lx, dtype, prec, true, s);

@@ -317,12 +317,12 @@ __device__ __forceinline__ void direct_tn_tile(const GroupedArgs& a, int32_t blo
 template <bool WT, int WN, int TM, int TN>
 __global__ __launch_bounds__(2 * WN * 64) void grouped_direct_kernel(const GroupedArgs a) {
   __shared__ __attribute__((aligned(1024))) char smem[direct_lds(2 * TM * 32, WN * TN * 32, WN)];
-  direct_rows_tile<WT, WN, TM, TN>(a, (int32_t)blockIdx.x, smem);
+  direct_rows_tile<WT, WN, TM, TN>(a, a.first + (int32_t)blockIdx.x, smem);
 }
 template <int WN, int TM, int TN>
 __global__ __launch_bounds__(2 * WN * 64) void grouped_direct_tn_kernel(const GroupedArgs a) {
   __shared__ __attribute__((aligned(1024))) char smem[direct_lds(2 * TM * 32, WN * TN * 32, WN)];
-  direct_tn_tile<WN, TM, TN>(a, (int32_t)blockIdx.x, smem);
+  direct_tn_tile<WN, TM, TN>(a, a.first + (int32_t)blockIdx.x, smem);
 }
 // Both gradients of a product in one launch, whose last tiles leave CUs idle once instead of twice: first `tn_blocks` for the weights,
 // whose tiles are the long ones, then those for the rows (16384 x 2048 x 1024 in 16 uneven groups: 107 + 118 us as two launches, 203 as one).

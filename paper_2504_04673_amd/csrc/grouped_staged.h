@@ -175,7 +175,7 @@ __global__ __launch_bounds__(WM * WN * 64) void grouped_staged_kernel(const Grou
   __shared__ __attribute__((aligned(1024))) char smem[2 * (OA::kBytes + OB::kBytes)];
   GroupTile t;
   int32_t col;
-  if (!grouped_find<BM>(a, (int32_t)blockIdx.x, t, col)) return;
+  if (!grouped_find<BM>(a, a.first + (int32_t)blockIdx.x, t, col)) return;
   const int64_t c0 = (int64_t)col * BN;
   const int rows = (int)(t.end - t.r0 < BM ? t.end - t.r0 : BM), cols = (int)(a.nout - c0 < BN ? a.nout - c0 : BN);
   const float* W = reinterpret_cast<const float*>(a.W) + (t.g < a.groups ? t.g * a.stride_w : 0) + c0 * (WT ? a.ldw : 1);
@@ -193,7 +193,7 @@ __global__ __launch_bounds__(WM * WN * 64) void grouped_staged_tn_kernel(const G
   __shared__ __attribute__((aligned(1024))) char smem[2 * (OA::kBytes + OB::kBytes)];
   GroupPart p;
   int32_t tile;
-  if (!grouped_part(a, (int32_t)blockIdx.x, p, tile)) return;
+  if (!grouped_part(a, a.first + (int32_t)blockIdx.x, p, tile)) return;
   const int64_t k0 = (int64_t)(tile / a.col_tiles) * BM, c0 = (int64_t)(tile % a.col_tiles) * BN;
   const int rows = (int)(a.kdim - k0 < BM ? a.kdim - k0 : BM), cols = (int)(a.nout - c0 < BN ? a.nout - c0 : BN);
   floatx16 acc[2][2];
@@ -205,16 +205,15 @@ __global__ __launch_bounds__(WM * WN * 64) void grouped_staged_tn_kernel(const G
 
 template <int PREC, int WM, int WN>
 int grouped_staged_launch(const GroupedArgs& a, bool trans_w, int64_t blocks, hipStream_t s) {
-  if (trans_w) grouped_staged_kernel<PREC, true, WM, WN><<<dim3((uint32_t)blocks), WM * WN * 64, 0, s>>>(a);
-  else grouped_staged_kernel<PREC, false, WM, WN><<<dim3((uint32_t)blocks), WM * WN * 64, 0, s>>>(a);
-  SAGNN_LAUNCH_CHECK();
-  return SAGNN_OK;
+  return grouped_launches(a, blocks, WM * WN * 64, [&](const GroupedArgs& part, dim3 grid) {
+    if (trans_w) grouped_staged_kernel<PREC, true, WM, WN><<<grid, WM * WN * 64, 0, s>>>(part);
+    else grouped_staged_kernel<PREC, false, WM, WN><<<grid, WM * WN * 64, 0, s>>>(part);
+  });
 }
 template <int PREC, int WM, int WN>
 int grouped_staged_tn_launch(const GroupedArgs& a, int64_t blocks, hipStream_t s) {
-  grouped_staged_tn_kernel<PREC, WM, WN><<<dim3((uint32_t)blocks), WM * WN * 64, 0, s>>>(a);
-  SAGNN_LAUNCH_CHECK();
-  return SAGNN_OK;
+  return grouped_launches(a, blocks, WM * WN * 64,
+                          [&](const GroupedArgs& part, dim3 grid) { grouped_staged_tn_kernel<PREC, WM, WN><<<grid, WM * WN * 64, 0, s>>>(part); });
 }
 
 }  // namespace sagnn
