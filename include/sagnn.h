@@ -637,7 +637,8 @@ int grouped_gemm_bwd(int32_t dtype, const void* d_X, int64_t ldx, const void* d_
  * each.  Segments may be empty (mean 0, rstd 1 / sqrt(eps)).  Rows behind the last segment: zeros in Y and dX, no part
  * of any sum.  max_rows: rows of the longest segment if the caller knows it, 0 if not; it only chooses between forms.
  * dtype: type of X, Y, G, dX; gamma, beta (each may be NULL: 1, 0), mean, rstd (n_seg x n_groups), dgamma, dbeta (each
- * may be NULL) are fp32.  mean and rstd are outputs forward and inputs backward.  Mean and variance are summed in 64 bits.
+ * may be NULL) are fp32.  mean and rstd are outputs forward and inputs backward.  Mean and variance are summed in 64 bits, of
+ * values less the segment's and group's first; (x - mean) is formed before anything is multiplied, with the mean as it is stored.
  * Orders of sums are fixed: the same bits every time.  Any C up to SAGNN_NORM_MAX_WIDTH, n_groups <= SAGNN_NORM_MAX_GROUPS,
  * any leading dimensions not below C, tensors aligned to their element.  Y may be X, dX may be G or X.
  * d_ws: group_norm_workspace_bytes() bytes, 16-byte aligned; NULL where that is 0 (short segments forward, a single

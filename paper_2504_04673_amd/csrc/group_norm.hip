@@ -31,6 +31,7 @@ struct NormArgs {
   bool joined;                       // the workgroups that write join the parts of their segments, each for itself
   int32_t slab;                      // channels of a workgroup, where it takes whole segments
   double2* parts;                    // (chunks + segments) x groups
+  float* pivots;                     // forward, segments x groups: what the sums of parts are taken from
   float2* sums;                      // backward, segments x groups: the two sums over a group, divided by its size
   float2* rows;                      // backward, table x C: sums of h xh and h over the rows of a chunk (of some segments)
 };
@@ -226,7 +227,17 @@ __device__ __forceinline__ float act_gradient(float g, float z) {
   return g;
 }
 
-// Sum and sum of squares of a part, in 64 bits: whatever the mean is against the deviation, their difference holds.
+// What the sums over a segment and group are taken from: its first value.  Squares of what is left of the mean besides the deviation would cost
+// the variance its digits: their sum is (1 + ((mean - pivot) / deviation)^2) n variances, and a value of n is at most n^(1/2) deviations
+// from their mean, so that of 53 bits log2(n) are lost at worst, and two or three where the first value is no outlier.  (0 where it is
+// not finite: the mean then is infinite or a NaN as the sum is.)
+template <typename S>
+__device__ __forceinline__ float pivot_of(const NormArgs& a, int64_t row, int c) {
+  const float x = (float)reinterpret_cast<const S*>(a.X)[row * a.ldx + c / a.D * a.D];
+  return __builtin_isfinite(x) ? x : 0.f;
+}
+
+// Sum and sum of squares of a part, from the segment's pivots, in 64 bits
 template <typename S, int V>
 __global__ __launch_bounds__(kThreads) void norm_sum_kernel(const NormArgs a) {
   extern __shared__ __attribute__((aligned(16))) char smem[];
@@ -236,18 +247,25 @@ __global__ __launch_bounds__(kThreads) void norm_sum_kernel(const NormArgs a) {
   const int64_t c = blockIdx.x;
   each_part(a, c, [&](int32_t b, int64_t r0, int64_t r1) {
     if (b < 0 || b >= a.segments) return;
-    for (int g = threadIdx.x; g < a.groups; g += kThreads) acc[g] = make_double2(0., 0.);
+    const int64_t lo = seg_row(a, b);
+    for (int g = threadIdx.x; g < a.groups; g += kThreads) {
+      acc[g] = make_double2(0., 0.);
+      if (r0 == lo) a.pivots[(int64_t)b * a.groups + g] = pivot_of<S>(a, lo, g * a.D);
+    }
     for (int vec0 = 0; vec0 * V < a.C; vec0 += kThreads) {
       const Lay l = lay<V>(a, vec0);
       const int ch = (vec0 + l.tx) * V;
-      double p[V], q[V];
+      double p[V], q[V], from[V];
 #pragma unroll
-      for (int i = 0; i < V; ++i) p[i] = q[i] = 0.;
+      for (int i = 0; i < V; ++i) {
+        p[i] = q[i] = 0.;
+        from[i] = pivot_of<S>(a, lo, ch + i);
+      }
       if (l.ty < l.rows)
         each_row<4>(r0 + l.ty, r1, l.rows, [&](int64_t r) { return fetch<S, V>(X + r * a.ldx + ch); }, [&](int64_t, const Whole<S, V>& w) {
 #pragma unroll
           for (int i = 0; i < V; ++i) {
-            const double d = (float)w.x[i];
+            const double d = (double)(float)w.x[i] - from[i];
             p[i] += d;
             q[i] = fma(d, d, q[i]);
           }
@@ -275,11 +293,11 @@ __device__ __forceinline__ double2 join_parts(const NormArgs& a, int32_t b, int3
   return s;
 }
 
-// Mean and reciprocal deviation of n values by their sums
-__device__ __forceinline__ float2 moments(const NormArgs& a, double2 s, int64_t rows) {
+// Mean and reciprocal deviation of n values by their sums from a pivot
+__device__ __forceinline__ float2 moments(const NormArgs& a, double2 s, int64_t rows, double pivot) {
   const double n = rows > 0 ? (double)rows * a.D : 1.;
   const double mean = s.x / n, var = s.y / n - mean * mean;
-  return make_float2((float)mean, (float)(1. / sqrt((var < 0. ? 0. : var) + a.eps)));
+  return make_float2((float)(pivot + mean), (float)(1. / sqrt((var < 0. ? 0. : var) + a.eps)));
 }
 // Backward: the two sums over the group's size
 __device__ __forceinline__ float2 means(const NormArgs& a, double2 s, int64_t rows) {
@@ -294,7 +312,7 @@ __global__ __launch_bounds__(kThreads) void norm_join_kernel(const NormArgs a) {
        at += (int64_t)gridDim.x * (kThreads / 64)) {
     const int32_t b = (int32_t)(at / a.groups), g = (int32_t)(at % a.groups);
     const int64_t lo = seg_row(a, b), hi = seg_row(a, b + 1);
-    const float2 s = moments(a, join_parts(a, b, g, lo, hi, 64), hi - lo);
+    const float2 s = moments(a, join_parts(a, b, g, lo, hi, 64), hi - lo, hi > lo ? a.pivots[at] : 0.f);
     if ((threadIdx.x & 63) == 0) {
       a.mean[at] = s.x;
       a.rstd[at] = s.y;
@@ -302,30 +320,33 @@ __global__ __launch_bounds__(kThreads) void norm_join_kernel(const NormArgs a) {
   }
 }
 
-// The same inside a workgroup that writes rows of segment b: of(sums, rows) of each group into `out`
+// The same inside a workgroup that writes rows of segment b: of(sums, rows, group) of each group into `out`
 template <typename F>
 __device__ __forceinline__ void join_here(const NormArgs& a, int32_t b, float2* out, F of) {
   const int64_t lo = seg_row(a, b), hi = seg_row(a, b + 1);
   __syncthreads();
   const int lanes = lanes_each(a.groups, kThreads), first = threadIdx.x / lanes;
   for (int32_t g = first; g - first < a.groups; g += kThreads / lanes) {      // (all lanes stay for the sums)
-    const float2 s = of(join_parts(a, b, g, lo, g < a.groups ? hi : lo, lanes), hi - lo);
-    if (g < a.groups && threadIdx.x % lanes == 0) out[g] = s;
+    const double2 s = join_parts(a, b, g, lo, g < a.groups ? hi : lo, lanes);
+    if (g < a.groups && threadIdx.x % lanes == 0) out[g] = of(s, hi - lo, g);
   }
   __syncthreads();
 }
 
-// What a vector's channels make of its values: z = scale x + shift, (x - mean) rstd = rstd x + base.  (A mean far from zero costs
-// the digits that its own rounding costs.)  N: groups that a vector can have, 1 where a group is whole vectors, else V.
+// What a vector's channels make of its values: d = x - mean, z = scale d + beta, (x - mean) rstd = rstd d.  The mean is taken off before
+// anything is multiplied: values equal to it give beta, and a mean far from zero costs what its own rounding costs and no more.
+// N: groups that a vector can have, 1 where a group is whole vectors, else V.
 template <int V, int N>
 struct Channel {
-  float scale[V], shift[V], rstd[N], base[N];
+  float scale[V], beta[V], rstd[N], mean[N];
+  __device__ __forceinline__ float off(float x, int i) const { return x - mean[i % N]; }
+  __device__ __forceinline__ float z(float d, int i) const { return fmaf(d, scale[i], beta[i]); }
   __device__ __forceinline__ void read(const NormArgs& a, int32_t b, int ch) {
 #pragma unroll
     for (int i = 0; i < N; ++i) {
       const int64_t g = (int64_t)b * a.groups + (ch + i) / a.D;
       rstd[i] = a.rstd[g];
-      base[i] = a.mean[g];
+      mean[i] = a.mean[g];
     }
     affine(a, ch);
   }
@@ -334,20 +355,17 @@ struct Channel {
 #pragma unroll
     for (int i = 0; i < N; ++i) {
       const float2 m = moments[(ch + i) / a.D];
-      base[i] = m.x;
+      mean[i] = m.x;
       rstd[i] = m.y;
     }
     affine(a, ch);
   }
-  // `base` holds the mean
   __device__ __forceinline__ void affine(const NormArgs& a, int ch) {
 #pragma unroll
     for (int i = 0; i < V; ++i) {
       scale[i] = (a.gamma ? a.gamma[ch + i] : 1.f) * rstd[i % N];
-      shift[i] = fmaf(-base[i % N], scale[i], a.beta ? a.beta[ch + i] : 0.f);
+      beta[i] = a.beta ? a.beta[ch + i] : 0.f;
     }
-#pragma unroll
-    for (int i = 0; i < N; ++i) base[i] = -base[i] * rstd[i];
   }
 };
 
@@ -361,7 +379,7 @@ __global__ __launch_bounds__(kThreads) void norm_write_kernel(const NormArgs a) 
     for (int b = 0; b < a.segments; ++b)
       if (seg_row(a, b + 1) <= seg_row(a, b))
         for (int g = threadIdx.x; g < a.groups; g += kThreads) {
-          const float2 s = moments(a, make_double2(0., 0.), 0);
+          const float2 s = moments(a, make_double2(0., 0.), 0, 0.);
           a.mean[b * a.groups + g] = s.x;
           a.rstd[b * a.groups + g] = s.y;
         }
@@ -369,7 +387,7 @@ __global__ __launch_bounds__(kThreads) void norm_write_kernel(const NormArgs a) 
   each_part(a, a.chunks - 1 - blockIdx.x, [&](int32_t b, int64_t r0, int64_t r1) {
     const bool none = b < 0 || b >= a.segments;
     if (a.joined && !none) {
-      join_here(a, b, here, [&](double2 s, int64_t rows) { return moments(a, s, rows); });
+      join_here(a, b, here, [&](double2 s, int64_t rows, int32_t g) { return moments(a, s, rows, a.pivots[(int64_t)b * a.groups + g]); });
       if (r0 == seg_row(a, b))
         for (int g = threadIdx.x; g < a.groups; g += kThreads) {
           a.mean[b * a.groups + g] = here[g].x;
@@ -390,7 +408,7 @@ __global__ __launch_bounds__(kThreads) void norm_write_kernel(const NormArgs a) 
       each_row<4>(r0 + l.ty, r1, l.rows, [&](int64_t r) { return fetch<S, V>(X + r * a.ldx + ch); }, [&](int64_t r, const Whole<S, V>& w) {
         float y[V];
 #pragma unroll
-        for (int i = 0; i < V; ++i) y[i] = act_value<ACT>(fmaf((float)w.x[i], k.scale[i], k.shift[i]));
+        for (int i = 0; i < V; ++i) y[i] = act_value<ACT>(k.z(k.off((float)w.x[i], i), i));
         store<S, V>(Y + r * a.ldy + ch, y);
       });
     }
@@ -423,9 +441,9 @@ __global__ __launch_bounds__(kThreads) void norm_bwd_sum_kernel(const NormArgs a
                     [&](int64_t, const Two<S, V>& w) {
 #pragma unroll
           for (int i = 0; i < V; ++i) {
-            const float x = (float)w.a.x[i], h = act_gradient<ACT>((float)w.b.x[i], fmaf(x, k.scale[i], k.shift[i]));
+            const float d = k.off((float)w.a.x[i], i), h = act_gradient<ACT>((float)w.b.x[i], k.z(d, i));
             p[i] += h;
-            q[i] = fmaf(h, fmaf(x, k.rstd[i], k.base[i]), q[i]);
+            q[i] = fmaf(h, d * k.rstd[i], q[i]);
           }
         });
 #pragma unroll
@@ -512,10 +530,10 @@ __global__ __launch_bounds__(kJoinThreads) void norm_bwd_join_kernel(const NormA
   }
 }
 
-// dx = h gamma rstd - rstd s1 - rstd s2 (rstd x + base) = h scale + tilt x + level, s1 and s2 the means of the group's sums
-__device__ __forceinline__ void input_line(float rstd, float base, float2 s, float& tilt, float& level) {
+// dx = h gamma rstd - rstd s1 - rstd s2 xh = h scale + tilt d + level, s1 and s2 the means of the group's sums
+__device__ __forceinline__ void input_line(float rstd, float2 s, float& tilt, float& level) {
   tilt = -rstd * s.y * rstd;
-  level = -rstd * fmaf(s.y, base, s.x);
+  level = -rstd * s.x;
 }
 
 template <typename S, int V, int ACT>
@@ -531,7 +549,7 @@ __global__ __launch_bounds__(kThreads) void norm_bwd_write_kernel(const NormArgs
   }
   each_part(a, a.chunks - 1 - blockIdx.x, [&](int32_t b, int64_t r0, int64_t r1) {
     const bool none = b < 0 || b >= a.segments;
-    if (a.joined && !none) join_here(a, b, here, [&](double2 s, int64_t rows) { return means(a, s, rows); });
+    if (a.joined && !none) join_here(a, b, here, [&](double2 s, int64_t rows, int32_t) { return means(a, s, rows); });
     for (int vec0 = 0; vec0 * V < a.C; vec0 += kThreads) {
       const Lay l = lay<V>(a, vec0);
       if (l.ty >= l.rows) continue;
@@ -544,14 +562,14 @@ __global__ __launch_bounds__(kThreads) void norm_bwd_write_kernel(const NormArgs
       k.read(a, b, ch);
       float tilt[V], level[V];
 #pragma unroll
-      for (int i = 0; i < V; ++i) input_line(k.rstd[i], k.base[i], a.joined ? here[(ch + i) / a.D] : a.sums[(int64_t)b * a.groups + (ch + i) / a.D], tilt[i], level[i]);
+      for (int i = 0; i < V; ++i) input_line(k.rstd[i], a.joined ? here[(ch + i) / a.D] : a.sums[(int64_t)b * a.groups + (ch + i) / a.D], tilt[i], level[i]);
       each_row<2>(r0 + l.ty, r1, l.rows, [&](int64_t r) { return Two<S, V>{fetch<S, V>(X + r * a.ldx + ch), fetch<S, V>(G + r * a.ldg + ch)}; },
                   [&](int64_t r, const Two<S, V>& w) {
         float y[V];
 #pragma unroll
         for (int i = 0; i < V; ++i) {
-          const float x = (float)w.a.x[i], h = act_gradient<ACT>((float)w.b.x[i], fmaf(x, k.scale[i], k.shift[i]));
-          y[i] = fmaf(h, k.scale[i], fmaf(x, tilt[i], level[i]));
+          const float d = k.off((float)w.a.x[i], i), h = act_gradient<ACT>((float)w.b.x[i], k.z(d, i));
+          y[i] = fmaf(h, k.scale[i], fmaf(d, tilt[i], level[i]));
         }
         store<S, V>(Y + r * a.ldy + ch, y);
       });
@@ -664,13 +682,16 @@ __global__ __launch_bounds__(kMostTeam) void norm_whole_kernel(const NormArgs a,
 #pragma unroll
     for (int n = 0; n < kKept; ++n) kept[n] = fetch_at<S, V>(x_row(0), at + (n < there ? n * step : 0));
   }
-  double p[N], q[N];
+  double p[N], q[N], from[N];
 #pragma unroll
-  for (int i = 0; i < N; ++i) p[i] = q[i] = 0.;
+  for (int i = 0; i < N; ++i) {
+    p[i] = q[i] = 0.;
+    from[i] = mine ? pivot_of<S>(a, lo, ch + i) : 0.f;
+  }
   auto add = [&](const Whole<S, V>& w) {
 #pragma unroll
     for (int i = 0; i < V; ++i) {
-      const double d = (float)w.x[i];
+      const double d = (double)(float)w.x[i] - from[i % N];
       p[i % N] += d;
       q[i % N] = fma(d, d, q[i % N]);
     }
@@ -682,14 +703,12 @@ __global__ __launch_bounds__(kMostTeam) void norm_whole_kernel(const NormArgs a,
   }
   for (int64_t n = kKept; n < mine; ++n) add(fetch_at<S, V>(x_row(n), vx));
   team_groups<V, N>(a, t, p, q, sm, sums);
-  const double n_values = hi > lo ? (double)(hi - lo) * a.D : 1.;
-  for (int g = threadIdx.x; g < t.width / a.D; g += blockDim.x) {
-    const double mean = sums[g].x / n_values, var = sums[g].y / n_values - mean * mean;
-    const float m = (float)mean, r = (float)(1. / sqrt((var < 0. ? 0. : var) + a.eps));
+  for (int g = threadIdx.x; g < t.width / a.D; g += blockDim.x) {     // (nobody writes rows before the barrier)
+    const float2 s = moments(a, sums[g], hi - lo, hi > lo ? pivot_of<S>(a, lo, t.c0 + g * a.D) : 0.f);
     const int64_t at = b * a.groups + t.c0 / a.D + g;
-    a.mean[at] = m;
-    a.rstd[at] = r;
-    sums[g] = make_double2(m, r);
+    a.mean[at] = s.x;
+    a.rstd[at] = s.y;
+    sums[g] = make_double2(s.x, s.y);
   }
   __syncthreads();
   if (mine == 0) return;
@@ -697,14 +716,14 @@ __global__ __launch_bounds__(kMostTeam) void norm_whole_kernel(const NormArgs a,
 #pragma unroll
   for (int i = 0; i < N; ++i) {
     const double2 s = sums[(t.tx * V + i) / a.D];
-    k.base[i] = (float)s.x;
+    k.mean[i] = (float)s.x;
     k.rstd[i] = (float)s.y;
   }
   k.affine(a, ch);
   auto put = [&](int64_t n, const Whole<S, V>& w) {
     float y[V];
 #pragma unroll
-    for (int i = 0; i < V; ++i) y[i] = act_value<ACT>(fmaf((float)w.x[i], k.scale[i], k.shift[i]));
+    for (int i = 0; i < V; ++i) y[i] = act_value<ACT>(k.z(k.off((float)w.x[i], i), i));
     store<S, V>(reinterpret_cast<S*>(y_row(n) + vy), y);
   };
 #pragma unroll
@@ -763,9 +782,9 @@ __global__ __launch_bounds__(kMostTeam, 4) void norm_bwd_whole_kernel(const Norm
       auto add = [&](const Whole<S, V>& w, Whole<S, V>& g) {
 #pragma unroll
         for (int i = 0; i < V; ++i) {
-          const float v = (float)w.x[i], y = act_gradient<ACT>((float)g.x[i], fmaf(v, k.scale[i], k.shift[i]));
+          const float d = k.off((float)w.x[i], i), y = act_gradient<ACT>((float)g.x[i], k.z(d, i));
           p[i] += y;
-          q[i] = fmaf(y, fmaf(v, k.rstd[i % N], k.base[i % N]), q[i]);
+          q[i] = fmaf(y, d * k.rstd[i % N], q[i]);
           if (kExact) g.x[i] = (S)y;
         }
       };
@@ -798,14 +817,14 @@ __global__ __launch_bounds__(kMostTeam, 4) void norm_bwd_whole_kernel(const Norm
 #pragma unroll
     for (int i = 0; i < N; ++i) {
       const double2 v = sums[(t.tx * V + i) / a.D];
-      input_line(k.rstd[i], k.base[i], make_float2((float)(v.x * n_values), (float)(v.y * n_values)), tilt[i], level[i]);
+      input_line(k.rstd[i], make_float2((float)(v.x * n_values), (float)(v.y * n_values)), tilt[i], level[i]);
     }
     auto put = [&](int64_t n, const Whole<S, V>& w, const Whole<S, V>& g, bool done) {
       float y[V];
 #pragma unroll
       for (int i = 0; i < V; ++i) {
-        const float v = (float)w.x[i], d = done ? (float)g.x[i] : act_gradient<ACT>((float)g.x[i], fmaf(v, k.scale[i], k.shift[i]));
-        y[i] = fmaf(d, k.scale[i], fmaf(v, tilt[i % N], level[i % N]));
+        const float d = k.off((float)w.x[i], i), h = done ? (float)g.x[i] : act_gradient<ACT>((float)g.x[i], k.z(d, i));
+        y[i] = fmaf(h, k.scale[i], fmaf(d, tilt[i % N], level[i % N]));
       }
       store<S, V>(reinterpret_cast<S*>(y_row(n) + vy), y);
     };
@@ -853,7 +872,7 @@ int vector_of(int32_t dtype, int32_t C) {
   return v;
 }
 
-struct NormPlan { int64_t chunk, chunks; size_t parts, sums, rows, total; };
+struct NormPlan { int64_t chunk, chunks; size_t parts, pivots, sums, rows, total; };
 constexpr int kMostStripes = 2048;
 // Segments in parts: chunks of rows, and where the sums lie
 NormPlan norm_plan(int32_t dtype, int64_t m, int32_t segments, int32_t C, int32_t groups, bool backward) {
@@ -872,6 +891,8 @@ NormPlan norm_plan(int32_t dtype, int64_t m, int32_t segments, int32_t C, int32_
   if (backward) {
     p.sums = take((size_t)segments * groups * sizeof(float2));
     p.rows = take((size_t)p.chunks * C * sizeof(float2));
+  } else {
+    p.pivots = take((size_t)segments * groups * sizeof(float));
   }
   p.total = off;
   return p;
@@ -995,7 +1016,7 @@ SAGNN_EXPORT int group_norm_act_fwd(int32_t dtype, const void* d_X, int64_t ldx,
   NormArgs a{};
   a.X = d_X; a.ldx = ldx; a.Y = d_Y; a.ldy = ldy; a.seg = d_seg; a.segments = n_seg; a.each = m / n_seg; a.m = m; a.C = C; a.groups = n_groups;
   a.D = C / n_groups; a.gamma = d_gamma; a.beta = d_beta; a.mean = d_mean; a.rstd = d_rstd; a.eps = eps; a.act = act;
-  a.chunk = p.chunk; a.chunks = p.chunks; a.parts = (double2*)((char*)d_ws + p.parts); a.slab = w.slab; a.joined = f.joined;
+  a.chunk = p.chunk; a.chunks = p.chunks; a.parts = (double2*)((char*)d_ws + p.parts); a.pivots = (float*)((char*)d_ws + p.pivots); a.slab = w.slab; a.joined = f.joined;
   hipStream_t s = (hipStream_t)stream;
   return by_act(act, [&](auto A) { return by_vector(dtype, vector_of(dtype, C), [&](auto V, auto zero) {
     constexpr int v = decltype(V)::value, ACT = decltype(A)::value;
