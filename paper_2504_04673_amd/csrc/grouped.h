@@ -22,7 +22,37 @@ struct GroupedArgs {
   int32_t row_tiles, col_tiles;                  // of the launch
   int32_t pairs;                                 // weight gradient: numbers of pairs of a chunk and a group
   int32_t first;                                 // workgroups of the launches before this one
+  int32_t run;                                   // of the summed index that one set of sums takes (grouped_run)
 };
+
+// Sums of equal terms: every addition of a serial run may round the same way, by up to half a unit in the last place of a sum that
+// grows to its end, which makes n/3 2^-24 of the whole for n additions; and the matrix cores cut off what an addend has below the sum's last
+// place.  1e-5 is 168 2^-24.  Measured, the worst of millions of pairs of values: fp32 instructions 0.34 2^-24 a term; three terms 197 2^-24 for 1024
+// terms and 542 for 4096 (the small products are cut first); bfloat16 0 up to 2048, where a sum of products of 16 bits begins to need
+// more than 24, 128 for 4096, 192 for 6144.  A longer sum is cut into runs, which are added in turn; a run and the runs together stay below 168.
+enum { kRunFp32 = 480, kRunTerms = 768, kRunBf16 = 5120 };       // a sum up to here is one run
+// The longest run of a sum of `sum`, and the longest sum
+inline int32_t grouped_run(int32_t prec, int64_t sum) {
+  if (prec == SAGNN_GEMM_FP32) return sum <= kRunFp32 ? kRunFp32 : sum <= 96 * 384 ? 384 : 256;
+  if (prec == SAGNN_GEMM_FP32_BF16X3) return sum <= kRunTerms ? kRunTerms : 512;
+  return sum <= kRunBf16 ? kRunBf16 : 4096;
+}
+inline int64_t grouped_sum_most(int32_t prec) {
+  return prec == SAGNN_GEMM_FP32 ? 192 * 256 : prec == SAGNN_GEMM_FP32_BF16X3 ? 160 * 512 : 96 * 4096;
+}
+// Runs of like length, whole steps of every kernel
+__device__ __forceinline__ int32_t run_length(int32_t sum, int32_t run) {
+  if (sum <= run) return run;
+  const int32_t runs = (sum + run - 1) / run;
+  return ((sum + runs - 1) / runs + 63) & ~63;
+}
+// This thread's number, anew in each turn of a loop: addresses that follow from it are worked out where they are used and take no registers beside
+// the products.
+__device__ __forceinline__ int this_thread() {
+  int t = threadIdx.x;
+  asm volatile("" : "+v"(t));
+  return t;
+}
 
 // Rows of group g as the kernels see them: whatever d_off holds, they lie inside [0, m).
 __device__ __forceinline__ int64_t grouped_row(const int32_t* __restrict__ off, int32_t g, int64_t m) {
@@ -229,8 +259,7 @@ typedef short short4v __attribute__((ext_vector_type(4)));
 // A lane has row lane % 32 and the eight sums of its half.  TR: two transposing reads; sixteen lanes read four rows of
 // 32 bytes, and each gets a column of four.
 template <typename Shape, bool TR>
-__device__ __forceinline__ bf16x8 tile_operand(const __bf16* tile, int row0, int k0) {
-  const int lane = threadIdx.x & 63;
+__device__ __forceinline__ bf16x8 tile_operand(const __bf16* tile, int row0, int k0, int lane) {
   if constexpr (!TR) {
     return *reinterpret_cast<const bf16x8*>(tile + (row0 + (lane & 31)) * Shape::kPitch + k0 + (lane >> 5) * 8);
   } else {
@@ -290,9 +319,9 @@ __device__ __forceinline__ void tile_multiply(const char* sa, const char* sb, fl
 #pragma unroll
       for (int q = 0; q < P; ++q) {
 #pragma unroll
-        for (int t = 0; t < TM; ++t) x[q][t] = tile_operand<SA, TRA>(A + q * SA::kPlane, ra + t * 32, k);
+        for (int t = 0; t < TM; ++t) x[q][t] = tile_operand<SA, TRA>(A + q * SA::kPlane, ra + t * 32, k, lane);
 #pragma unroll
-        for (int t = 0; t < TN; ++t) y[q][t] = tile_operand<SB, TRB>(B + q * SB::kPlane, rb + t * 32, k);
+        for (int t = 0; t < TN; ++t) y[q][t] = tile_operand<SB, TRB>(B + q * SB::kPlane, rb + t * 32, k, lane);
       }
       // split mode: the six products down to 2^-16 of the leading one, smallest first
       constexpr int pair[6][2] = {{2, 0}, {0, 2}, {1, 1}, {1, 0}, {0, 1}, {0, 0}};
@@ -308,10 +337,10 @@ __device__ __forceinline__ void tile_multiply(const char* sa, const char* sb, fl
 }
 
 // acc = A B over `sum` of the summed index: a step of both operands is loaded into registers while the one before it
-// is multiplied out of LDS.
-template <typename S, int PREC, bool TRA, bool TRB, int WM, int WN, int TM, int TN, int BK>
+// is multiplied out of LDS.  LONG: runs of `run` at most, which are added in registers of their own.
+template <typename S, int PREC, bool TRA, bool TRB, int WM, int WN, int TM, int TN, int BK, bool LONG>
 __device__ __forceinline__ void tile_product(const S* A, int64_t lda, int rows, const S* B, int64_t ldb, int cols, int64_t sum,
-                                             char* smem, floatx16 (&acc)[TM][TN]) {
+                                             char* smem, floatx16 (&acc)[TM][TN], int32_t run) {
   constexpr int THREADS = WM * WN * 64;
   using SA = TileShape<PREC, TRA, WM * TM * 32, BK>;
   TileLoad<S, PREC, TRA, WM * TM * 32, BK, THREADS> la;
@@ -327,16 +356,48 @@ __device__ __forceinline__ void tile_product(const S* A, int64_t lda, int rows, 
   const int tid = threadIdx.x;
   la.load(A, lda, rows, left(0), tid);
   lb.load(B, ldb, cols, left(0), tid);
-  for (int64_t k = 0; k < sum; k += BK) {
-    la.store(smem, tid);
-    lb.store(smem + SA::kBytes, tid);
-    __syncthreads();
-    if (k + BK < sum) {
-      la.load(A + (k + BK) * (TRA ? lda : 1), lda, rows, left(k + BK), tid);
-      lb.load(B + (k + BK) * (TRB ? ldb : 1), ldb, cols, left(k + BK), tid);
+  if constexpr (!LONG) {
+    for (int64_t k = 0; k < sum; k += BK) {
+      la.store(smem, tid);
+      lb.store(smem + SA::kBytes, tid);
+      __syncthreads();
+      if (k + BK < sum) {
+        la.load(A + (k + BK) * (TRA ? lda : 1), lda, rows, left(k + BK), tid);
+        lb.load(B + (k + BK) * (TRB ? ldb : 1), ldb, cols, left(k + BK), tid);
+      }
+      tile_multiply<PREC, TRA, TRB, WM, WN, TM, TN, BK>(smem, smem + SA::kBytes, acc, tid);
+      __syncthreads();
     }
-    tile_multiply<PREC, TRA, TRB, WM, WN, TM, TN, BK>(smem, smem + SA::kBytes, acc, tid);
-    __syncthreads();
+  } else {                                        // (the same steps, run by run)
+    run = run_length((int32_t)sum, run);
+    floatx16 all[TM][TN];
+#pragma unroll
+    for (int i = 0; i < TM * TN; ++i) all[i / TN][i % TN] = acc[i / TN][i % TN];
+#pragma unroll 1
+    for (int32_t k = 0; k < sum; k += run) {
+#pragma unroll
+      for (int tm = 0; tm < TM; ++tm)
+#pragma unroll
+        for (int tn = 0; tn < TN; ++tn)
+#pragma unroll
+          for (int v = 0; v < 16; ++v) acc[tm][tn][v] = 0.f;
+      const int64_t end = k + run < sum ? k + run : sum;
+      for (int64_t at = k; at < end; at += BK) {
+        la.store(smem, tid);
+        lb.store(smem + SA::kBytes, tid);
+        __syncthreads();
+        if (at + BK < sum) {
+          la.load(A + (at + BK) * (TRA ? lda : 1), lda, rows, left(at + BK), tid);
+          lb.load(B + (at + BK) * (TRB ? ldb : 1), ldb, cols, left(at + BK), tid);
+        }
+        tile_multiply<PREC, TRA, TRB, WM, WN, TM, TN, BK>(smem, smem + SA::kBytes, acc, tid);
+        __syncthreads();
+      }
+#pragma unroll
+      for (int i = 0; i < TM * TN; ++i) all[i / TN][i % TN] += acc[i / TN][i % TN];
+    }
+#pragma unroll
+    for (int i = 0; i < TM * TN; ++i) acc[i / TN][i % TN] = all[i / TN][i % TN];
   }
 }
 
@@ -440,8 +501,10 @@ __device__ __forceinline__ void tile_store(const GroupedArgs& a, int64_t r0, int
   });
 }
 
-template <typename S, int PREC, bool WT, int WM, int WN, int TM, int TN, int BK>
-__global__ __launch_bounds__(WM * WN * 64) void grouped_kernel(const GroupedArgs a) {
+// LONG, here and below: a sum of several runs.  (Two workgroups on a CU are worth the registers that they have to give up for it; not the
+// wide steps of operands that are rounded on the way, whose sums would be spilled.)
+template <typename S, int PREC, bool WT, int WM, int WN, int TM, int TN, int BK, bool LONG>
+__global__ __launch_bounds__(WM * WN * 64, LONG && !(sizeof(S) == 4 && PREC == SAGNN_GEMM_BF16) ? 2 : 1) void grouped_kernel(const GroupedArgs a) {
   constexpr int BM = WM * TM * 32, BN = WN * TN * 32;
   __shared__ __attribute__((aligned(16))) char smem[TileShape<PREC, false, BM, BK>::kBytes + TileShape<PREC, !WT, BN, BK>::kBytes];
   GroupTile t;
@@ -451,8 +514,8 @@ __global__ __launch_bounds__(WM * WN * 64) void grouped_kernel(const GroupedArgs
   const int rows = (int)(t.end - t.r0 < BM ? t.end - t.r0 : BM), cols = (int)(a.nout - c0 < BN ? a.nout - c0 : BN);
   floatx16 acc[TM][TN];
   const S* W = reinterpret_cast<const S*>(a.W) + (t.g < a.groups ? t.g * a.stride_w : 0) + c0 * (WT ? a.ldw : 1);
-  tile_product<S, PREC, false, !WT, WM, WN, TM, TN, BK>(reinterpret_cast<const S*>(a.X) + t.r0 * a.ldx, a.ldx, rows, W, a.ldw, cols,
-                                                        t.g < a.groups ? a.kdim : 0, smem, acc);
+  tile_product<S, PREC, false, !WT, WM, WN, TM, TN, BK, LONG>(reinterpret_cast<const S*>(a.X) + t.r0 * a.ldx, a.ldx, rows, W, a.ldw, cols,
+                                                              t.g < a.groups ? a.kdim : 0, smem, acc, a.run);
   tile_store<S, WM, WN, TM, TN>(a, t.r0, c0, rows, cols, acc);
 }
 
@@ -472,62 +535,78 @@ __global__ __launch_bounds__(WAVES * 64) void grouped_thin_kernel(const GroupedA
   if (!grouped_find<32>(a, a.first + (int32_t)blockIdx.x, t, col)) return;
   const int64_t c0 = (int64_t)col * BN;
   const int rows = (int)(t.end - t.r0 < 32 ? t.end - t.r0 : 32), cols = (int)(a.nout - c0 < BN ? a.nout - c0 : BN);
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const S* X = reinterpret_cast<const S*>(a.X) + t.r0 * a.ldx;
   const S* W = reinterpret_cast<const S*>(a.W) + (t.g < a.groups ? t.g * a.stride_w : 0) + c0 * (WT ? a.ldw : 1);
-  floatx16 acc[1][TN];
-#pragma unroll
-  for (int tn = 0; tn < TN; ++tn)
-#pragma unroll
-    for (int v = 0; v < 16; ++v) acc[0][tn][v] = 0.f;
   TileLoad<S, PREC, false, 32, BK, 64> la;
   TileLoad<S, PREC, !WT, BN, BK, 64> lb;
   const int sum = t.g < a.groups ? a.kdim : 0;
   char* own = smem + wave * kOwn;
-  auto load = [&](int k) {
-    la.load(X + k, a.ldx, rows, sum - k < BK ? sum - k : BK, lane);
-    lb.load(W + (int64_t)k * (WT ? 1 : a.ldw), a.ldw, cols, sum - k < BK ? sum - k : BK, lane);
-  };
-  int k = wave * BK;
-  if (k < sum) load(k);
-  for (; k < sum; k += WAVES * BK) {
-    la.store(own, lane);
-    lb.store(own + SA::kBytes, lane);
-    asm volatile("" ::: "memory");                // (a wavefront's own LDS accesses are in order)
-    if (k + WAVES * BK < sum) load(k + WAVES * BK);
-    tile_multiply<PREC, false, !WT, 1, 1, 1, TN, BK>(own, own + SA::kBytes, acc, lane);
-    asm volatile("" ::: "memory");
-  }
-  __syncthreads();
   float* sums = reinterpret_cast<float*>(smem);
-#pragma unroll
-  for (int tn = 0; tn < TN; ++tn)
-#pragma unroll
-    for (int v = 0; v < 16; v += 4)
-      *reinterpret_cast<float4*>(sums + (wave * 32 + (lane & 31)) * kRow + tn * 32 + 2 * v + 4 * (lane >> 5)) =
-          make_float4(acc[0][tn][v], acc[0][tn][v + 1], acc[0][tn][v + 2], acc[0][tn][v + 3]);
-  __syncthreads();
   S* Y = reinterpret_cast<S*>(a.Y) + t.r0 * a.ldy + c0;
   const S* mask = a.mask ? reinterpret_cast<const S*>(a.mask) + t.r0 * a.ldmask + c0 : nullptr;
-  for (int u = threadIdx.x; u < 32 * (BN / 4); u += WAVES * 64) {
-    const int r = u / (BN / 4), c = u % (BN / 4) * 4;
-    if (r >= rows || c >= cols) continue;
-    float y[4] = {0.f, 0.f, 0.f, 0.f};
+  // a run of each wavefront at a time (bfloat16 results: there is one only)
+  const int32_t each = sizeof(S) == 4 ? WAVES * run_length((sum + WAVES - 1) / WAVES, a.run) : sum;
+#pragma unroll 1
+  for (int32_t from = 0;; from += each) {
+    const bool last = sum - from <= each;
+    const int end = last ? sum : from + each;
+    const int tid = this_thread(), lane = tid & 63;
+    auto load = [&](int k) {
+      la.load(X + k, a.ldx, rows, end - k < BK ? end - k : BK, lane);
+      lb.load(W + (int64_t)k * (WT ? 1 : a.ldw), a.ldw, cols, end - k < BK ? end - k : BK, lane);
+    };
+    floatx16 acc[1][TN];
 #pragma unroll
-    for (int w = 0; w < WAVES; ++w) {
-      const float4 x = *reinterpret_cast<const float4*>(sums + (w * 32 + r) * kRow + c);
-      y[0] += x.x; y[1] += x.y; y[2] += x.z; y[3] += x.w;
+    for (int tn = 0; tn < TN; ++tn)
+#pragma unroll
+      for (int v = 0; v < 16; ++v) acc[0][tn][v] = 0.f;
+    int k = from + wave * BK;
+    if (k < end) load(k);
+    for (; k < end; k += WAVES * BK) {
+      la.store(own, lane);
+      lb.store(own + SA::kBytes, lane);
+      asm volatile("" ::: "memory");                // (a wavefront's own LDS accesses are in order)
+      if (k + WAVES * BK < end) load(k + WAVES * BK);
+      tile_multiply<PREC, false, !WT, 1, 1, 1, TN, BK>(own, own + SA::kBytes, acc, lane);
+      asm volatile("" ::: "memory");
     }
-    if (a.act == SAGNN_ACT_RELU)
+    __syncthreads();
 #pragma unroll
-      for (int i = 0; i < 4; ++i) y[i] = y[i] < 0.f ? 0.f : y[i];
-    if (mask) mask_four(mask + (int64_t)r * a.ldmask + c, y, cols - c);
-    store_four(Y + (int64_t)r * a.ldy + c, y, cols - c);
+    for (int tn = 0; tn < TN; ++tn)
+#pragma unroll
+      for (int v = 0; v < 16; v += 4)
+        *reinterpret_cast<float4*>(sums + (wave * 32 + (lane & 31)) * kRow + tn * 32 + 2 * v + 4 * (lane >> 5)) =
+            make_float4(acc[0][tn][v], acc[0][tn][v + 1], acc[0][tn][v + 2], acc[0][tn][v + 3]);
+    __syncthreads();
+    for (int u = tid; u < 32 * (BN / 4); u += WAVES * 64) {
+      const int r = u / (BN / 4), c = u % (BN / 4) * 4;
+      if (r >= rows || c >= cols) continue;
+      float y[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int w = 0; w < WAVES; ++w) {
+        const float4 x = *reinterpret_cast<const float4*>(sums + (w * 32 + r) * kRow + c);
+        y[0] += x.x; y[1] += x.y; y[2] += x.z; y[3] += x.w;
+      }
+      S* to = Y + (int64_t)r * a.ldy + c;
+      if constexpr (sizeof(S) == 4)
+        if (from > 0)
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            if (c + i < cols) y[i] += to[i];
+      if (last && a.act == SAGNN_ACT_RELU)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) y[i] = y[i] < 0.f ? 0.f : y[i];
+      if (last && mask) mask_four(mask + (int64_t)r * a.ldmask + c, y, cols - c);
+      store_four(to, y, cols - c);
+    }
+    if (last) break;
+    __syncthreads();                              // (the sums lie where the next run's operands do)
   }
 }
 
-template <typename S, int PREC, int WM, int WN, int TM, int TN, int BK>
-__global__ __launch_bounds__(WM * WN * 64) void grouped_tn_kernel(const GroupedArgs a) {
+template <typename S, int PREC, int WM, int WN, int TM, int TN, int BK, bool LONG>
+__global__ __launch_bounds__(WM * WN * 64, LONG && !(sizeof(S) == 4 && PREC == SAGNN_GEMM_BF16) ? 2 : 1) void grouped_tn_kernel(const GroupedArgs a) {
   constexpr int BM = WM * TM * 32, BN = WN * TN * 32;
   __shared__ __attribute__((aligned(16))) char smem[TileShape<PREC, true, BM, BK>::kBytes + TileShape<PREC, true, BN, BK>::kBytes];
   GroupPart p;
@@ -536,9 +615,9 @@ __global__ __launch_bounds__(WM * WN * 64) void grouped_tn_kernel(const GroupedA
   const int64_t k0 = (int64_t)(tile / a.col_tiles) * BM, c0 = (int64_t)(tile % a.col_tiles) * BN;
   const int rows = (int)(a.kdim - k0 < BM ? a.kdim - k0 : BM), cols = (int)(a.nout - c0 < BN ? a.nout - c0 : BN);
   floatx16 acc[TM][TN];
-  tile_product<S, PREC, true, true, WM, WN, TM, TN, BK>(reinterpret_cast<const S*>(a.X) + p.r0 * a.ldx + k0, a.ldx, rows,
-                                                        reinterpret_cast<const S*>(a.G) + p.r0 * a.ldg + c0, a.ldg, cols, p.r1 - p.r0, smem, acc);
   float* out = (p.cut ? a.partial + grouped_partial_slot(p) * a.kdim * a.nout : a.dW + (int64_t)p.g * a.kdim * a.nout) + k0 * a.nout + c0;
+  tile_product<S, PREC, true, true, WM, WN, TM, TN, BK, LONG>(reinterpret_cast<const S*>(a.X) + p.r0 * a.ldx + k0, a.ldx, rows,
+                                                              reinterpret_cast<const S*>(a.G) + p.r0 * a.ldg + c0, a.ldg, cols, p.r1 - p.r0, smem, acc, a.run);
   tile_fours<WM, WN, TM, TN>(acc, [&](int r, int c, float (&y)[4]) { if (r < rows) store_four(out + (int64_t)r * a.nout + c, y, cols - c); });
 }
 
@@ -577,27 +656,37 @@ int grouped_launches(GroupedArgs a, int64_t blocks, int threads, F launch) {
   return SAGNN_OK;
 }
 
+template <typename S, int PREC, int BK, bool WT, bool LONG>
+void grouped_launch_as(const GroupedArgs& a, int tile, dim3 grid, hipStream_t s) {
+  const dim3 block(256);
+  if (tile == kTile128) grouped_kernel<S, PREC, WT, 2, 2, 2, 2, BK, LONG><<<grid, block, 0, s>>>(a);
+  else if (tile == kTile128x64) grouped_kernel<S, PREC, WT, 2, 2, 2, 1, BK, LONG><<<grid, block, 0, s>>>(a);
+  else if (tile == kTile128x32) grouped_kernel<S, PREC, WT, 4, 1, 1, 1, BK, LONG><<<grid, block, 0, s>>>(a);
+  else if (tile == kTile64) grouped_kernel<S, PREC, WT, 2, 2, 1, 1, BK, LONG><<<grid, block, 0, s>>>(a);
+  else grouped_kernel<S, PREC, WT, 1, 4, 1, 1, BK, LONG><<<grid, block, 0, s>>>(a);
+}
 template <typename S, int PREC, int BK, bool WT>
 int grouped_launch(const GroupedArgs& args, int tile, int64_t blocks, hipStream_t s) {
-  const dim3 block(256);
   return grouped_launches(args, blocks, tile == kThin ? 512 : 256, [&](const GroupedArgs& a, dim3 grid) {
-    if (tile == kTile128) grouped_kernel<S, PREC, WT, 2, 2, 2, 2, BK><<<grid, block, 0, s>>>(a);
-    else if (tile == kTile128x64) grouped_kernel<S, PREC, WT, 2, 2, 2, 1, BK><<<grid, block, 0, s>>>(a);
-    else if (tile == kTile128x32) grouped_kernel<S, PREC, WT, 4, 1, 1, 1, BK><<<grid, block, 0, s>>>(a);
-    else if (tile == kTile64) grouped_kernel<S, PREC, WT, 2, 2, 1, 1, BK><<<grid, block, 0, s>>>(a);
-    else if (tile == kThin) grouped_thin_kernel<S, PREC, WT, kThinCols / 32, 8, BK == 32 && PREC != SAGNN_GEMM_FP32 ? 16 : BK><<<grid, 512, 0, s>>>(a);
-    else grouped_kernel<S, PREC, WT, 1, 4, 1, 1, BK><<<grid, block, 0, s>>>(a);
+    if (tile == kThin) grouped_thin_kernel<S, PREC, WT, kThinCols / 32, 8, BK == 32 && PREC != SAGNN_GEMM_FP32 ? 16 : BK><<<grid, 512, 0, s>>>(a);
+    else if (a.kdim > a.run) grouped_launch_as<S, PREC, BK, WT, true>(a, tile, grid, s);
+    else grouped_launch_as<S, PREC, BK, WT, false>(a, tile, grid, s);
   });
+}
+template <typename S, int PREC, int BK, bool LONG>
+void grouped_tn_launch_as(const GroupedArgs& a, int tile, dim3 grid, hipStream_t s) {
+  const dim3 block(256);
+  if (tile == kTile128) grouped_tn_kernel<S, PREC, 2, 2, 2, 2, BK, LONG><<<grid, block, 0, s>>>(a);
+  else if (tile == kTile128x64) grouped_tn_kernel<S, PREC, 2, 2, 2, 1, BK, LONG><<<grid, block, 0, s>>>(a);
+  else if (tile == kTile128x32) grouped_tn_kernel<S, PREC, 4, 1, 1, 1, BK, LONG><<<grid, block, 0, s>>>(a);
+  else if (tile == kTile64) grouped_tn_kernel<S, PREC, 2, 2, 1, 1, BK, LONG><<<grid, block, 0, s>>>(a);
+  else grouped_tn_kernel<S, PREC, 1, 4, 1, 1, BK, LONG><<<grid, block, 0, s>>>(a);
 }
 template <typename S, int PREC, int BK>
 int grouped_tn_launch(const GroupedArgs& args, int tile, int64_t blocks, hipStream_t s) {
-  const dim3 block(256);
   return grouped_launches(args, blocks, 256, [&](const GroupedArgs& a, dim3 grid) {
-    if (tile == kTile128) grouped_tn_kernel<S, PREC, 2, 2, 2, 2, BK><<<grid, block, 0, s>>>(a);
-    else if (tile == kTile128x64) grouped_tn_kernel<S, PREC, 2, 2, 2, 1, BK><<<grid, block, 0, s>>>(a);
-    else if (tile == kTile128x32) grouped_tn_kernel<S, PREC, 4, 1, 1, 1, BK><<<grid, block, 0, s>>>(a);
-    else if (tile == kTile64) grouped_tn_kernel<S, PREC, 2, 2, 1, 1, BK><<<grid, block, 0, s>>>(a);
-    else grouped_tn_kernel<S, PREC, 1, 4, 1, 1, BK><<<grid, block, 0, s>>>(a);
+    if (a.chunk > a.run) grouped_tn_launch_as<S, PREC, BK, true>(a, tile, grid, s);
+    else grouped_tn_launch_as<S, PREC, BK, false>(a, tile, grid, s);
   });
 }
 

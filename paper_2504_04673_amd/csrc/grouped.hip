@@ -5,7 +5,7 @@
 namespace sagnn {
 namespace {
 
-// dW[g] = the sum of its parts, chunks ascending; a group of one part was written by the product itself.
+// dW[g] = the sum of its parts, chunks ascending, in 64 bits (there may be thousands); a group of one part was written by the product itself.
 __global__ __launch_bounds__(256) void grouped_join_kernel(const GroupedArgs a, bool four) {
   const int32_t g = blockIdx.y;
   const int64_t lo = grouped_row(a.off, g, a.m), hi = grouped_row(a.off, g + 1, a.m), size = (int64_t)a.kdim * a.nout;
@@ -14,21 +14,22 @@ __global__ __launch_bounds__(256) void grouped_join_kernel(const GroupedArgs a, 
   if (c0 == c1) return;
   if (four) {                                 // (a multiple of four, and aligned so)
     for (int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4; i < size; i += (int64_t)gridDim.x * 1024) {
-      float4 sum = *reinterpret_cast<const float4*>(a.partial + (2 * c0 + 1) * size + i);
+      const float4 head = *reinterpret_cast<const float4*>(a.partial + (2 * c0 + 1) * size + i);
+      double sum[4] = {head.x, head.y, head.z, head.w};
 #pragma unroll 4
       for (int64_t c = c0 + 1; c <= c1; ++c) {
         const float4 x = *reinterpret_cast<const float4*>(a.partial + 2 * c * size + i);
-        sum.x += x.x; sum.y += x.y; sum.z += x.z; sum.w += x.w;
+        sum[0] += x.x; sum[1] += x.y; sum[2] += x.z; sum[3] += x.w;
       }
-      *reinterpret_cast<float4*>(a.dW + g * size + i) = sum;
+      *reinterpret_cast<float4*>(a.dW + g * size + i) = make_float4((float)sum[0], (float)sum[1], (float)sum[2], (float)sum[3]);
     }
     return;
   }
   for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < size; i += (int64_t)gridDim.x * 256) {
-    float sum = a.partial[(2 * c0 + 1) * size + i];
+    double sum = a.partial[(2 * c0 + 1) * size + i];
 #pragma unroll 8
     for (int64_t c = c0 + 1; c <= c1; ++c) sum += a.partial[2 * c * size + i];
-    a.dW[g * size + i] = sum;
+    a.dW[g * size + i] = (float)sum;
   }
 }
 
@@ -62,7 +63,8 @@ TileCost tile_cost(int32_t dtype, int32_t prec, int tile) {
 
 // The tile with the least cost: `rows` rows in `parts` ragged parts by `cols` columns, `times` over, `sum` of the summed index.  Tiles are
 // whole, so each part leaves half a tile empty; a launch lasts as long as its fullest CU; and a tile alone on a CU waits for its
-// loads.
+// loads.  `whole`: a product of rows.  Bfloat16 results are no place for the sum of several runs, which the largest tiles and the thin ones would
+// need.
 int choose_tile(int32_t dtype, int32_t prec, int ways, int64_t rows, int64_t parts, int64_t cols, int64_t times, int64_t sum, bool whole) {
   int best = kTile128;
   double least = 1e300;
@@ -70,6 +72,7 @@ int choose_tile(int32_t dtype, int32_t prec, int ways, int64_t rows, int64_t par
     const TileCost c = tile_cost(dtype, prec, tile);
     if (c.rate == 0 || (tile == kDirect256 && !(ways & kDirect)) || ((tile == kStaged256x128 || tile == kStaged128x256) && !(ways & kStaged))) continue;
     if (tile == kThin && !whole) continue;
+    if (whole && dtype == SAGNN_BF16 && ((tile == kDirect256 && sum > kRunBf16) || (tile == kThin && sum > 8 * kRunBf16))) continue;
     const int64_t h = grouped_tile_rows(tile), w = grouped_tile_cols(tile);
     const int64_t tiles = (ceil_div(rows, h) + (parts < rows ? parts : rows) / 2) * ceil_div(cols, w) * times;
     const double turns = tiles <= 256 ? 1.25 : whole && tiles < 4 * 256 ? (double)ceil_div(tiles, 256) : tiles / 256.;
@@ -94,6 +97,7 @@ Launch plan_rows(GroupedArgs& a, int32_t dtype, int32_t prec) {
     ways = kStaged;
   }
   const int tile = choose_tile(dtype, prec, ways, a.m, a.groups, a.nout, 1, a.kdim, true);
+  a.run = grouped_run(dtype == SAGNN_BF16 ? SAGNN_GEMM_BF16 : prec, tile == kThin ? ceil_div(a.kdim, 8) : a.kdim);
   a.row_tiles = (int32_t)(a.m / grouped_tile_rows(tile) + a.groups + 1);
   a.col_tiles = (int32_t)ceil_div(a.nout, grouped_tile_cols(tile));
   const int64_t blocks = (int64_t)a.row_tiles * a.col_tiles;
@@ -110,7 +114,7 @@ int launch_rows(const GroupedArgs& a, Launch l, int32_t dtype, int32_t prec, boo
 // The weight gradient's tiles and chunks of rows.  Chunks fill the chip where the matrices are small or one group has most rows (170003 x 128 x 128
 // in 4 groups, three terms: 83 chunks 95 us, 256 chunks 62); but a group that a chunk's end cuts costs its matrix written twice, read
 // twice and written once more, so a chunk has 640 rows or more, and 8192 where the arithmetic is fastest (16 groups of 16384 x
-// 2048 x 1024, bfloat16: 16 chunks 191 us, 4 chunks 106), but never fewer than as many as give half the CUs work.
+// 2048 x 1024, bfloat16: 16 chunks 191 us, 4 chunks 106), but never fewer than as many as give half the CUs work, or as its sums' runs ask for.
 struct TnPlan { int tile; int64_t row_tiles, col_tiles, chunk, chunks; };
 TnPlan tn_plan(int64_t m, int32_t groups, int32_t kdim, int32_t nout, int32_t dtype, int32_t prec, int ways) {
   TnPlan p{};
@@ -123,6 +127,8 @@ TnPlan tn_plan(int64_t m, int32_t groups, int32_t kdim, int32_t nout, int32_t dt
   int64_t chunks = 512 / tiles < rare ? 512 / tiles : rare;
   if (chunks < 128 / tiles) chunks = 128 / tiles;
   if (chunks > ceil_div(m, 256)) chunks = ceil_div(m, 256);
+  const int64_t longest = grouped_sum_most(dtype == SAGNN_BF16 ? SAGNN_GEMM_BF16 : prec);
+  if (chunks < ceil_div(m, longest)) chunks = ceil_div(m, longest);
   if (chunks < 1) chunks = 1;
   p.chunk = round_up((size_t)ceil_div(m > 0 ? m : 1, chunks), 64);
   p.chunks = ceil_div(m > 0 ? m : 1, p.chunk);
@@ -149,6 +155,7 @@ Launch plan_weights(GroupedArgs& a, int32_t dtype, int32_t prec) {
   const bool staged = dtype == SAGNN_F32 && a.ldx <= kStagedLd && a.ldg <= kStagedLd;
   const TnPlan p = tn_plan(a.m, a.groups, a.kdim, a.nout, dtype, prec, direct ? kDirect : staged ? kStaged : kAny);
   a.chunk = p.chunk;
+  a.run = grouped_run(dtype == SAGNN_BF16 ? SAGNN_GEMM_BF16 : prec, p.chunk);
   a.row_tiles = (int32_t)p.row_tiles;
   a.col_tiles = (int32_t)p.col_tiles;
   int64_t pairs = p.chunks + a.groups;

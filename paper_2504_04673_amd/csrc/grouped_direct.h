@@ -38,8 +38,7 @@ struct DirectOperand {
   uint32_t at[kLoads];   // of this lane, from the corner
   int inner;             // first of its eight elements inside a row (every load's)
 
-  __device__ __forceinline__ void init(const __bf16* corner, int64_t ld, int rows, int total) {
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  __device__ __forceinline__ void init(const __bf16* corner, int64_t ld, int rows, int total, int lane, int wave) {
     base = reinterpret_cast<const char*>(corner);
     step = TR ? kStep * ld * 2 : kUnit * kStep * 2;
     left = ((int64_t)((TR ? total : rows) - 1) * ld + (TR ? rows : total)) * 2;
@@ -58,13 +57,13 @@ struct DirectOperand {
   // Load j of the next unit, whose first step has place `stage` in the ring at `ring`; zeros beyond the operand.
   // By hand: with the compiler's own instruction every transposing read waits for all loads.  No register is written; vmcnt
   // counts the loads, and direct_product waits for them ahead of the barrier behind which their bytes are read.
-  __device__ __forceinline__ void load(uint32_t ring, int stage, int j) const {
+  __device__ __forceinline__ void load(uint32_t ring, int stage, int j, int wave) const {
     typedef uint32_t uint4v __attribute__((ext_vector_type(4)));
     const int64_t bytes = sum > 0 ? left : 0;
     const uint64_t b = reinterpret_cast<uint64_t>(base);
     const uint4v rsrc = {(uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)b), (uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)(b >> 32)) & 0xffff,
                          (uint32_t)__builtin_amdgcn_readfirstlane(bytes < 0x7fffffff ? (uint32_t)bytes : 0x7fffffffu), 0x00027000u};
-    const uint32_t own = ring + stage * kStageBytes + (__builtin_amdgcn_readfirstlane(threadIdx.x >> 6) * kLoads + j) * 1024;
+    const uint32_t own = ring + stage * kStageBytes + (wave * kLoads + j) * 1024;
     // (two instructions of a wavefront are eight rows apart, and every other one is swizzled differently)
     const int in = (j & 1) ? inner ^ 16 : inner;
     const uint32_t v = !TR && in >= sum ? 0x80000000u : at[j];
@@ -76,8 +75,7 @@ struct DirectOperand {
     sum -= kUnit * kStep;
   }
   // Operand of one 32 x 32 x 16 instruction: 32 rows from row0, 16 of the step from k0 (0 or 16)
-  static __device__ __forceinline__ bf16x8 read(const char* ring, int stage, int row0, int k0) {
-    const int lane = threadIdx.x & 63;
+  static __device__ __forceinline__ bf16x8 read(const char* ring, int stage, int row0, int k0, int lane) {
     if constexpr (!TR) {
       const int r = row0 + (lane & 31);
       return *reinterpret_cast<const bf16x8*>(ring + (stage & 2) * kStageBytes + (stage & 1) * 512 + (r >> 3) * 1024 + (r & 7) * 64 +
@@ -108,7 +106,7 @@ __device__ __forceinline__ void direct_product(const __bf16* A, int64_t lda, int
   using OB = DirectOperand<TRB, BN, WM * WN>;
   // loads a wavefront issues for each step, and for each two
   constexpr int kSingle = (TRA ? OA::kLoads : 0) + (TRB ? OB::kLoads : 0), kDouble = (TRA ? 0 : OA::kLoads) + (TRB ? 0 : OB::kLoads);
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int tid = this_thread(), lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int ra = (wave / WN) * TM * 32, rb = (wave % WN) * TN * 32;
 #pragma unroll
   for (int tm = 0; tm < TM; ++tm)
@@ -119,19 +117,19 @@ __device__ __forceinline__ void direct_product(const __bf16* A, int64_t lda, int
   if (total <= 0) return;
   OA oa;
   OB ob;
-  oa.init(A, lda, rows, (int)total);
-  ob.init(B, ldb, cols, (int)total);
+  oa.init(A, lda, rows, (int)total, lane, wave);
+  ob.init(B, ldb, cols, (int)total, lane, wave);
   const uint32_t lds_a = (uint32_t)reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) char*)smem), lds_b = lds_a + OA::kBytes;
   const char* ring_a = smem;
   const char* ring_b = smem + OA::kBytes;
   // loads of a single step, of two: the j-th into the place of `stage`
   auto load_single = [&](int stage, int j) {
-    if (TRA && j < OA::kLoads) oa.load(lds_a, stage, j);
-    else ob.load(lds_b, stage, TRA ? j - OA::kLoads : j);
+    if (TRA && j < OA::kLoads) oa.load(lds_a, stage, j, wave);
+    else ob.load(lds_b, stage, TRA ? j - OA::kLoads : j, wave);
   };
   auto load_double = [&](int stage, int j) {
-    if (!TRA && j < OA::kLoads) oa.load(lds_a, stage, j);
-    else ob.load(lds_b, stage, !TRA ? j - OA::kLoads : j);
+    if (!TRA && j < OA::kLoads) oa.load(lds_a, stage, j, wave);
+    else ob.load(lds_b, stage, !TRA ? j - OA::kLoads : j, wave);
   };
   auto advance_single = [&] { if (TRA) oa.advance(); if (TRB) ob.advance(); };
   auto advance_double = [&] { if (!TRA) oa.advance(); if (!TRB) ob.advance(); };
@@ -147,9 +145,9 @@ __device__ __forceinline__ void direct_product(const __bf16* A, int64_t lda, int
   }
   bf16x8 xa[2][TM], xb[2][TN];
   auto read = [&](int slot, int stage, int k0, int i) {       // in the order of use
-    if (i == 0) xa[slot][0] = OA::read(ring_a, stage, ra, k0);
-    else if (i <= TN) xb[slot][i - 1] = OB::read(ring_b, stage, rb + (i - 1) * 32, k0);
-    else xa[slot][i - TN] = OA::read(ring_a, stage, ra + (i - TN) * 32, k0);
+    if (i == 0) xa[slot][0] = OA::read(ring_a, stage, ra, k0, lane);
+    else if (i <= TN) xb[slot][i - 1] = OB::read(ring_b, stage, rb + (i - 1) * 32, k0, lane);
+    else xa[slot][i - TN] = OA::read(ring_a, stage, ra + (i - TN) * 32, k0, lane);
   };
   constexpr int kProducts = TM * TN, kReads = TM + TN;
   auto multiply = [&](int slot, int i) {
@@ -296,22 +294,34 @@ __device__ __forceinline__ void direct_tn_tile(const GroupedArgs& a, int32_t blo
   const int64_t k0 = (int64_t)(tile / a.col_tiles) * BM, c0 = (int64_t)(tile % a.col_tiles) * BN;
   const int rows = (int)(a.kdim - k0 < BM ? a.kdim - k0 : BM), cols = (int)(a.nout - c0 < BN ? a.nout - c0 : BN);
   floatx16 acc[TM][TN];
-  direct_product<true, true, 2, WN, TM, TN>(reinterpret_cast<const __bf16*>(a.X) + p.r0 * a.ldx + k0, a.ldx, rows,
-                                           reinterpret_cast<const __bf16*>(a.G) + p.r0 * a.ldg + c0, a.ldg, cols, p.r1 - p.r0, smem, acc);
   float* out = (p.cut ? a.partial + grouped_partial_slot(p) * a.kdim * a.nout : a.dW + (int64_t)p.g * a.kdim * a.nout) + k0 * a.nout + c0;
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int ra = (wave / WN) * TM * 32 + (lane & 31), rb = (wave % WN) * TN * 32 + 4 * (lane >> 5);
+  const __bf16 *X = reinterpret_cast<const __bf16*>(a.X) + p.r0 * a.ldx + k0, *G = reinterpret_cast<const __bf16*>(a.G) + p.r0 * a.ldg + c0;
+  const int32_t sum = (int32_t)(p.r1 - p.r0), each = run_length(sum, a.run);
+#pragma unroll 1
+  for (int32_t from = 0;; from += each) {
+    const bool last = sum - from <= each;
+    direct_product<true, true, 2, WN, TM, TN>(X + from * a.ldx, a.ldx, rows, G + from * a.ldg, a.ldg, cols, last ? sum - from : each, smem, acc);
+    const int tid = this_thread(), lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int ra = (wave / WN) * TM * 32 + (lane & 31), rb = (wave % WN) * TN * 32 + 4 * (lane >> 5);
 #pragma unroll
-  for (int tm = 0; tm < TM; ++tm)
+    for (int tm = 0; tm < TM; ++tm) {
+      // (nout is a multiple of 8: four columns are there or not)
+      float* row = out + (int64_t)(ra + tm * 32) * a.nout + rb;
+      if (from > 0 && ra + tm * 32 < rows && rb < cols) {      // (on top of the runs before, which are where they will be: no registers are left for them)
+        float4 before[TN][4];
 #pragma unroll
-    for (int tn = 0; tn < TN; ++tn)
+        for (int i = 0; i < TN * 4; ++i) before[i / 4][i % 4] = *reinterpret_cast<const float4*>(row + (rb + i * 8 < cols ? i * 8 : 0));
 #pragma unroll
-      for (int v = 0; v < 16; v += 4) {
-        const int r = ra + tm * 32, c = rb + tn * 32 + 2 * v;
-        if (r < rows && c < cols)       // (nout is a multiple of 8: four columns are there or not)
-          *reinterpret_cast<float4*>(out + (int64_t)r * a.nout + c) =
-              make_float4(acc[tm][tn][v], acc[tm][tn][v + 1], acc[tm][tn][v + 2], acc[tm][tn][v + 3]);
+        for (int i = 0; i < TN * 16; ++i) acc[tm][i / 16][i % 16] += reinterpret_cast<const float*>(&before[i / 16][i % 16 / 4])[i % 4];
       }
+#pragma unroll
+      for (int i = 0; i < TN * 4; ++i)
+        if (ra + tm * 32 < rows && rb + i * 8 < cols)
+          *reinterpret_cast<float4*>(row + i * 8) =
+              make_float4(acc[tm][i / 4][i % 4 * 4], acc[tm][i / 4][i % 4 * 4 + 1], acc[tm][i / 4][i % 4 * 4 + 2], acc[tm][i / 4][i % 4 * 4 + 3]);
+    }
+    if (last) break;
+  }
 }
 
 template <bool WT, int WN, int TM, int TN>

@@ -94,10 +94,11 @@ struct StagedOperand {
 };
 
 // acc = A B over the summed index; the workgroup's WM x WN wavefronts own TM x TN tiles of 32 x 32 each.  Step t is multiplied out of
-// one place in LDS while step t + 1 is converted into the other and step t + 2 loaded.
-template <int PREC, bool TRA, bool TRB, int WM, int WN, int TM, int TN>
+// one place in LDS while step t + 1 is converted into the other and step t + 2 loaded.  LONG: runs of `run` at most, which are added in registers of
+// their own.
+template <int PREC, bool TRA, bool TRB, int WM, int WN, int TM, int TN, bool LONG>
 __device__ __forceinline__ void staged_product(const float* A, int64_t lda, int rows, const float* B, int64_t ldb, int cols, int64_t total,
-                                               char* smem, floatx16 (&acc)[TM][TN]) {
+                                               char* smem, floatx16 (&acc)[TM][TN], int32_t run) {
   constexpr int THREADS = WM * WN * 64;
   using OA = StagedOperand<PREC, TRA, WM * TM * 32, THREADS>;
   using OB = StagedOperand<PREC, TRB, WN * TN * 32, THREADS>;
@@ -138,6 +139,13 @@ __device__ __forceinline__ void staged_product(const float* A, int64_t lda, int 
   };
 #pragma unroll
   for (int i = 0; i < kReads; ++i) read(0, smem, 0, i);
+  [[maybe_unused]] floatx16 all[TM][TN];
+  [[maybe_unused]] int left = 0;                  // steps of the run
+  if constexpr (LONG) {
+    run = left = run_length((int32_t)total, run) / kStagedStep;
+#pragma unroll
+    for (int i = 0; i < TM * TN; ++i) all[i / TN][i % TN] = acc[i / TN][i % TN];
+  }
   for (int t = 0; t < steps; ++t) {
     char *tile = smem + at * kBuffer, *other = smem + (at ^ 1) * kBuffer;
 #pragma unroll
@@ -163,11 +171,24 @@ __device__ __forceinline__ void staged_product(const float* A, int64_t lda, int 
     }
     oa.advance(); ob.advance();
     at ^= 1;
+    if constexpr (LONG)
+      if (--left == 0) {
+        left = run;
+#pragma unroll
+        for (int i = 0; i < TM * TN; ++i) {
+          all[i / TN][i % TN] += acc[i / TN][i % TN];
+#pragma unroll
+          for (int v = 0; v < 16; ++v) acc[i / TN][i % TN][v] = 0.f;
+        }
+      }
   }
+  if constexpr (LONG)
+#pragma unroll
+    for (int i = 0; i < TM * TN; ++i) acc[i / TN][i % TN] += all[i / TN][i % TN];
 }
 
 // Tiles of WM x WN wavefronts, 64 x 64 each
-template <int PREC, bool WT, int WM, int WN>
+template <int PREC, bool WT, int WM, int WN, bool LONG>
 __global__ __launch_bounds__(WM * WN * 64) void grouped_staged_kernel(const GroupedArgs a) {
   constexpr int BM = WM * 64, BN = WN * 64, THREADS = WM * WN * 64;
   using OA = StagedOperand<PREC, false, BM, THREADS>;
@@ -180,12 +201,12 @@ __global__ __launch_bounds__(WM * WN * 64) void grouped_staged_kernel(const Grou
   const int rows = (int)(t.end - t.r0 < BM ? t.end - t.r0 : BM), cols = (int)(a.nout - c0 < BN ? a.nout - c0 : BN);
   const float* W = reinterpret_cast<const float*>(a.W) + (t.g < a.groups ? t.g * a.stride_w : 0) + c0 * (WT ? a.ldw : 1);
   floatx16 acc[2][2];
-  staged_product<PREC, false, !WT, WM, WN, 2, 2>(reinterpret_cast<const float*>(a.X) + t.r0 * a.ldx, a.ldx, rows, W, a.ldw, cols,
-                                                 t.g < a.groups ? a.kdim : 0, smem, acc);
+  staged_product<PREC, false, !WT, WM, WN, 2, 2, LONG>(reinterpret_cast<const float*>(a.X) + t.r0 * a.ldx, a.ldx, rows, W, a.ldw, cols,
+                                                       t.g < a.groups ? a.kdim : 0, smem, acc, a.run);
   tile_store<float, WM, WN, 2, 2>(a, t.r0, c0, rows, cols, acc);
 }
 
-template <int PREC, int WM, int WN>
+template <int PREC, int WM, int WN, bool LONG>
 __global__ __launch_bounds__(WM * WN * 64) void grouped_staged_tn_kernel(const GroupedArgs a) {
   constexpr int BM = WM * 64, BN = WN * 64, THREADS = WM * WN * 64;
   using OA = StagedOperand<PREC, true, BM, THREADS>;
@@ -197,8 +218,8 @@ __global__ __launch_bounds__(WM * WN * 64) void grouped_staged_tn_kernel(const G
   const int64_t k0 = (int64_t)(tile / a.col_tiles) * BM, c0 = (int64_t)(tile % a.col_tiles) * BN;
   const int rows = (int)(a.kdim - k0 < BM ? a.kdim - k0 : BM), cols = (int)(a.nout - c0 < BN ? a.nout - c0 : BN);
   floatx16 acc[2][2];
-  staged_product<PREC, true, true, WM, WN, 2, 2>(reinterpret_cast<const float*>(a.X) + p.r0 * a.ldx + k0, a.ldx, rows,
-                                                 reinterpret_cast<const float*>(a.G) + p.r0 * a.ldg + c0, a.ldg, cols, p.r1 - p.r0, smem, acc);
+  staged_product<PREC, true, true, WM, WN, 2, 2, LONG>(reinterpret_cast<const float*>(a.X) + p.r0 * a.ldx + k0, a.ldx, rows,
+                                                       reinterpret_cast<const float*>(a.G) + p.r0 * a.ldg + c0, a.ldg, cols, p.r1 - p.r0, smem, acc, a.run);
   float* out = (p.cut ? a.partial + grouped_partial_slot(p) * a.kdim * a.nout : a.dW + (int64_t)p.g * a.kdim * a.nout) + k0 * a.nout + c0;
   tile_fours<WM, WN, 2, 2>(acc, [&](int r, int c, float (&y)[4]) { if (r < rows) store_four(out + (int64_t)r * a.nout + c, y, cols - c); });
 }
@@ -206,14 +227,19 @@ __global__ __launch_bounds__(WM * WN * 64) void grouped_staged_tn_kernel(const G
 template <int PREC, int WM, int WN>
 int grouped_staged_launch(const GroupedArgs& a, bool trans_w, int64_t blocks, hipStream_t s) {
   return grouped_launches(a, blocks, WM * WN * 64, [&](const GroupedArgs& part, dim3 grid) {
-    if (trans_w) grouped_staged_kernel<PREC, true, WM, WN><<<grid, WM * WN * 64, 0, s>>>(part);
-    else grouped_staged_kernel<PREC, false, WM, WN><<<grid, WM * WN * 64, 0, s>>>(part);
+    const bool several = part.kdim > part.run;
+    if (trans_w && several) grouped_staged_kernel<PREC, true, WM, WN, true><<<grid, WM * WN * 64, 0, s>>>(part);
+    else if (trans_w) grouped_staged_kernel<PREC, true, WM, WN, false><<<grid, WM * WN * 64, 0, s>>>(part);
+    else if (several) grouped_staged_kernel<PREC, false, WM, WN, true><<<grid, WM * WN * 64, 0, s>>>(part);
+    else grouped_staged_kernel<PREC, false, WM, WN, false><<<grid, WM * WN * 64, 0, s>>>(part);
   });
 }
 template <int PREC, int WM, int WN>
 int grouped_staged_tn_launch(const GroupedArgs& a, int64_t blocks, hipStream_t s) {
-  return grouped_launches(a, blocks, WM * WN * 64,
-                          [&](const GroupedArgs& part, dim3 grid) { grouped_staged_tn_kernel<PREC, WM, WN><<<grid, WM * WN * 64, 0, s>>>(part); });
+  return grouped_launches(a, blocks, WM * WN * 64, [&](const GroupedArgs& part, dim3 grid) {
+    if (part.chunk > part.run) grouped_staged_tn_kernel<PREC, WM, WN, true><<<grid, WM * WN * 64, 0, s>>>(part);
+    else grouped_staged_tn_kernel<PREC, WM, WN, false><<<grid, WM * WN * 64, 0, s>>>(part);
+  });
 }
 
 }  // namespace sagnn
