@@ -88,6 +88,12 @@ static PyObject* bind(PyObject* self, PyObject* args) {
   (void)self;
   if (!PyArg_ParseTuple(args, "Ks#O", &address, &kinds, &n, &error)) return NULL;
   if (!address || n > MOST) return PyErr_Format(PyExc_ValueError, "no address, or more than %d parameters", MOST);
+  int doubles = 0;
+  for (Py_ssize_t i = 0; i < n; ++i) {
+    if (kinds[i] != 'p' && kinds[i] != 'i' && kinds[i] != 'd') return PyErr_Format(PyExc_ValueError, "parameter %zd: p, i or d expected", i + 1);
+    doubles += kinds[i] == 'd';
+  }
+  if (doubles > 1) return PyErr_Format(PyExc_ValueError, "%d doubles, one at most", doubles);
   Bound* b = (Bound*)malloc(sizeof(Bound));
   if (!b) return PyErr_NoMemory();
   b->fn = (Fn)(uintptr_t)address;
