@@ -114,7 +114,7 @@ def lib():
     global _lib
     if _lib is None:
         if not os.path.exists(_build.LIB):
-            _build.build_hip()
+            _build.build_all()
         L = ctypes.CDLL(_build.LIB)
         i64, i32, u32, vp, sz = (ctypes.c_int64, ctypes.c_int32, ctypes.c_uint32, ctypes.c_void_p,
                                  ctypes.c_size_t)

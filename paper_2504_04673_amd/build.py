@@ -83,6 +83,12 @@ def build_hip(verbose: bool = False, incremental: bool = False, jobs: int = 8) -
         if os.path.exists(MARSHAL):
             os.remove(MARSHAL)                # (of another source)
         warnings.warn(f"calls go through ctypes: {e}")
+    return LIB
+
+
+def build_all(verbose: bool = False, incremental: bool = False) -> str:
+    """The library, the calls into it and the lists of tensors: everything that binding.py loads."""
+    build_hip(verbose, incremental)
     try:
         build_gradlist(verbose)
     except (OSError, RuntimeError) as e:      # no C++ compiler: binding.py asks the tensors one by one
