@@ -883,8 +883,8 @@ def _listed(grads):
 def _grad_list(grads, out=None):
     """struct sagnn_grad of the C header for each tensor, one behind the other."""
     global _rows
-    if _rows is None:                      # csrc/gradlist.cpp, or the same in Python where it is not built
-        ext = _extension("_gradlist", _build.GRADLIST)
+    if _rows is None:                      # csrc/gradlist.cpp, or the same in Python where it is not built for this torch
+        ext = _extension("_gradlist", _build.GRADLIST) if _build.gradlist_fits() else None
         _rows = ext.rows if ext else _rows_in_python
     rows = _rows(grads, out)
     return rows, len(rows) // 32

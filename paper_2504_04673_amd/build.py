@@ -48,7 +48,16 @@ def marshal_stale() -> bool:
 
 
 def gradlist_stale() -> bool:
-    return not os.path.exists(GRADLIST) or os.path.getmtime(GRADLIST_SOURCE) > os.path.getmtime(GRADLIST)
+    return not gradlist_fits() or os.path.getmtime(GRADLIST_SOURCE) > os.path.getmtime(GRADLIST)
+
+
+def gradlist_fits() -> bool:
+    """Whether the lists of tensors are built, and against the torch that is here: asked of the file, before it is loaded."""
+    if not os.path.exists(GRADLIST):
+        return False
+    import torch
+    with open(GRADLIST, "rb") as f:
+        return f"sagnn_gradlist_torch={torch.__version__}\0".encode() in f.read()
 
 
 def _run(cmd, verbose):
@@ -118,5 +127,6 @@ def build_gradlist(verbose: bool = False) -> str:
     import torch
     from torch.utils.cpp_extension import include_paths
     libs = os.path.join(os.path.dirname(torch.__file__), "lib")
-    return _build_extension([os.environ.get("CXX", "g++"), "-O2", "-std=c++17", GRADLIST_SOURCE, *["-I" + i for i in include_paths()],
+    return _build_extension([os.environ.get("CXX", "g++"), "-O2", "-std=c++17", f'-DSAGNN_TORCH="{torch.__version__}"', GRADLIST_SOURCE,
+                             *["-I" + i for i in include_paths()],
                              "-L" + libs, "-lc10", "-ltorch_cpu", "-ltorch_python"], GRADLIST, verbose)

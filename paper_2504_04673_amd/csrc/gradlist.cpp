@@ -5,6 +5,9 @@
 #include <cstring>
 #include <exception>
 
+// The torch that this is compiled against, found in the file before it is loaded: another one's tensors may lie otherwise.
+extern "C" __attribute__((used)) const char sagnn_gradlist_torch[] = "sagnn_gradlist_torch=" SAGNN_TORCH;
+
 namespace {
 
 struct Row { int64_t in, out, n, dtype; };

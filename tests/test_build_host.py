@@ -2,6 +2,7 @@
 import os
 
 import pytest
+import torch
 
 from paper_2504_04673_amd import binding, build
 
@@ -38,4 +39,15 @@ def test_lists_are_built_whole_or_not_at_all(elsewhere, monkeypatch):
 def test_lists_are_read_in_python_where_they_are_not_built(monkeypatch, tmp_path):
     monkeypatch.setattr(binding, "_rows", None)
     monkeypatch.setattr(build, "GRADLIST", str(tmp_path / "none"))
+    assert binding._grad_list([]) == (b"", 0) and binding._rows is binding._rows_in_python
+
+
+def test_lists_built_for_another_torch_are_out_of_date_and_not_loaded(elsewhere, monkeypatch):
+    assert not build.gradlist_fits()
+    build.build_gradlist()
+    assert build.gradlist_fits() and not build.gradlist_stale()
+    monkeypatch.setattr(torch, "__version__", "2.1")               # (a prefix of 2.10 among others)
+    assert not build.gradlist_fits() and build.gradlist_stale()
+    monkeypatch.setattr(binding, "_rows", None)
+    monkeypatch.setattr(binding, "_extension", lambda *a: pytest.fail("loaded"))
     assert binding._grad_list([]) == (b"", 0) and binding._rows is binding._rows_in_python
