@@ -67,7 +67,7 @@ struct DirectOperand {
     // (two instructions of a wavefront are eight rows apart, and every other one is swizzled differently)
     const int in = (j & 1) ? inner ^ 16 : inner;
     const uint32_t v = !TR && in >= sum ? 0x80000000u : at[j];
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(own), "v"(v), "s"(rsrc) : "memory");
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(own), "v"(v), "s"(rsrc) : "memory", "m0");
   }
   __device__ __forceinline__ void advance() {
     base += step;
