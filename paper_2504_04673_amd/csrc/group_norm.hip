@@ -219,7 +219,7 @@ __device__ __forceinline__ float act_value(float z) {
 // g act'(z)
 template <int ACT>
 __device__ __forceinline__ float act_gradient(float g, float z) {
-  if (ACT == SAGNN_ACT_RELU) return z > 0.f ? g : g == g ? 0.f : g;      // (0 times a NaN)
+  if (ACT == SAGNN_ACT_RELU) return z > 0.f ? g : 0.f * g;               // (a NaN for a NaN or an infinity)
   if (ACT == SAGNN_ACT_SILU) {
     const float t = sigmoid(z);
     return g * fmaf(z * t, 1.f - t, t);

@@ -148,3 +148,21 @@ def test_gradient_along_directions_that_the_group_takes_out(dtype):
             # stretching: eps keeps 1e-5 rstd^2 of it
             left = (d * xh).sum((0, 2)).abs()
             assert bool((left <= noise(xh.abs()) + 4e-5 * rstd[b].double().square() * (d.abs() * xh.abs()).sum((0, 2))).all())
+
+
+@pytest.mark.parametrize("dtype", [F, B])
+@pytest.mark.parametrize("value", [float("inf"), float("-inf"), float("nan")])
+@pytest.mark.parametrize("rows,known", [(40, 40), (700, 1), (4000, 0)])
+def test_gradients_that_are_not_finite_where_relu_is_flat(rows, known, value, dtype):
+    """0 times an infinity is a NaN: an overflow in the gradient is not hidden by ReLU."""
+    seg, X, G, gamma, beta = inputs([rows, 30], 16, dtype, sagnn.ACT_RELU, 4, rows)
+    z = reference(X, G, 4, gamma, beta, seg, 0)["z"]
+    at = int((z[:rows, 5] < -0.5).nonzero()[0])
+    G[at, 5] = value
+    _, mean, rstd = sagnn.group_norm_act(X, 4, gamma, beta, seg=seg, max_rows=known, act=sagnn.ACT_RELU)
+    dX, dgamma, dbeta = sagnn.group_norm_act_bwd(X, G, mean, rstd, 4, gamma, beta, seg=seg, max_rows=known, act=sagnn.ACT_RELU)
+    bad = torch.zeros(X.shape, dtype=torch.bool, device="cuda")
+    bad[:rows, 4:8] = True
+    assert torch.equal(dX.isnan(), bad)
+    for t in (dgamma, dbeta):
+        assert torch.equal(t.isnan(), torch.arange(16, device="cuda") == 5)
