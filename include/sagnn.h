@@ -641,7 +641,8 @@ int grouped_gemm_bwd(int32_t dtype, const void* d_X, int64_t ldx, const void* d_
  * may be NULL) are fp32.  mean and rstd are outputs forward and inputs backward.  Mean and variance are summed in 64 bits, of
  * values less the segment's and group's first; (x - mean) is formed before anything is multiplied, with the mean as it is stored.
  * Orders of sums are fixed: the same bits every time.  Any C up to SAGNN_NORM_MAX_WIDTH, n_groups <= SAGNN_NORM_MAX_GROUPS,
- * any leading dimensions not below C, tensors aligned to their element.  Y may be X, dX may be G or X.
+ * any leading dimensions not below C, tensors aligned to their element.  Y may be X, dX may be G or X, in the same place and with the same leading
+ * dimension, or lie beside it in wider rows; other overlaps are refused.
  * d_ws: group_norm_workspace_bytes() bytes, 16-byte aligned; NULL where that is 0 (short segments forward, a single
  * one backward).  ld: the largest
  * leading dimension of the call, backward: 0 or 1.

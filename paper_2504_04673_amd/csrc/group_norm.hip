@@ -983,6 +983,17 @@ bool valid(int32_t dtype, const int32_t* d_seg, int32_t n_seg, int64_t m, int32_
          groups <= SAGNN_NORM_MAX_GROUPS && C % groups == 0 && (int64_t)n_seg * groups <= INT32_MAX && act >= SAGNN_ACT_IDENTITY && act <= SAGNN_ACT_SILU &&
          (d_seg || m % n_seg == 0);
 }
+// Whether an output of m rows lies over an operand otherwise than in its own place: rows of the same length apart may be each other's, or
+// columns beside each other
+bool tangled(const void* out, int64_t ldo, const void* in, int64_t ldi, int64_t m, int32_t C, uintptr_t size) {
+  if (m == 0) return false;
+  const uintptr_t o = reinterpret_cast<uintptr_t>(out), i = reinterpret_cast<uintptr_t>(in);
+  const uintptr_t o1 = o + ((uintptr_t)(m - 1) * ldo + C) * size, i1 = i + ((uintptr_t)(m - 1) * ldi + C) * size;
+  if (o1 <= i || i1 <= o || (o == i && (ldo == ldi || m == 1))) return false;
+  if (ldo != ldi || m == 1) return true;
+  const uintptr_t apart = (o > i ? o - i : i - o) % ((uintptr_t)ldo * size);
+  return apart < C * size || (uintptr_t)ldo * size - apart < C * size;
+}
 bool aligned_to(const void* p, uintptr_t bytes) { return (reinterpret_cast<uintptr_t>(p) & (bytes - 1)) == 0; }
 
 }  // namespace
@@ -1008,6 +1019,7 @@ SAGNN_EXPORT int group_norm_act_fwd(int32_t dtype, const void* d_X, int64_t ldx,
   if (!aligned_to(d_X, size) || !aligned_to(d_Y, size) || !aligned_to(d_seg, 4) || !aligned_to(d_gamma, 4) || !aligned_to(d_beta, 4) ||
       !aligned_to(d_mean, 4) || !aligned_to(d_rstd, 4) || !aligned_to(d_ws, 16))
     return SAGNN_EINVAL;
+  if (tangled(d_Y, ldy, d_X, ldx, m, C, size)) return SAGNN_EINVAL;
   const NormForm f = norm_form(dtype, m, n_seg, max_rows, C, n_groups, ldx > ldy ? ldx : ldy, false);
   const NormPlan& p = f.parts;
   const WholePlan& w = f.whole;
@@ -1063,6 +1075,7 @@ SAGNN_EXPORT int group_norm_act_bwd(int32_t dtype, const void* d_X, int64_t ldx,
       !aligned_to(d_beta, 4) || !aligned_to(d_mean, 4) || !aligned_to(d_rstd, 4) || !aligned_to(d_dgamma, 4) || !aligned_to(d_dbeta, 4) ||
       !aligned_to(d_ws, 16))
     return SAGNN_EINVAL;
+  if (tangled(d_dX, lddx, d_X, ldx, m, C, size) || tangled(d_dX, lddx, d_G, ldg, m, C, size)) return SAGNN_EINVAL;
   const NormForm f = norm_form(dtype, m, n_seg, max_rows, C, n_groups, ldx > ldg ? (ldx > lddx ? ldx : lddx) : (ldg > lddx ? ldg : lddx), true);
   const NormPlan& p = f.parts;
   const WholePlan& w = f.whole;
