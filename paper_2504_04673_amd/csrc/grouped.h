@@ -354,51 +354,39 @@ __device__ __forceinline__ void tile_product(const S* A, int64_t lda, int rows, 
   if (sum <= 0) return;
   auto left = [&](int64_t k) { return (int)(sum - k < BK ? sum - k : BK); };
   const int tid = threadIdx.x;
-  la.load(A, lda, rows, left(0), tid);
-  lb.load(B, ldb, cols, left(0), tid);
-  if constexpr (!LONG) {
-    for (int64_t k = 0; k < sum; k += BK) {
-      la.store(smem, tid);
-      lb.store(smem + SA::kBytes, tid);
-      __syncthreads();
-      if (k + BK < sum) {
-        la.load(A + (k + BK) * (TRA ? lda : 1), lda, rows, left(k + BK), tid);
-        lb.load(B + (k + BK) * (TRB ? ldb : 1), ldb, cols, left(k + BK), tid);
-      }
-      tile_multiply<PREC, TRA, TRB, WM, WN, TM, TN, BK>(smem, smem + SA::kBytes, acc, tid);
-      __syncthreads();
-    }
-  } else {                                        // (the same steps, run by run)
-    run = run_length((int32_t)sum, run);
-    floatx16 all[TM][TN];
+  [[maybe_unused]] floatx16 all[TM][TN];
+  [[maybe_unused]] int64_t until = 0;             // end of the run
+  if constexpr (LONG) {
+    until = run = run_length((int32_t)sum, run);
 #pragma unroll
     for (int i = 0; i < TM * TN; ++i) all[i / TN][i % TN] = acc[i / TN][i % TN];
-#pragma unroll 1
-    for (int32_t k = 0; k < sum; k += run) {
-#pragma unroll
-      for (int tm = 0; tm < TM; ++tm)
-#pragma unroll
-        for (int tn = 0; tn < TN; ++tn)
-#pragma unroll
-          for (int v = 0; v < 16; ++v) acc[tm][tn][v] = 0.f;
-      const int64_t end = k + run < sum ? k + run : sum;
-      for (int64_t at = k; at < end; at += BK) {
-        la.store(smem, tid);
-        lb.store(smem + SA::kBytes, tid);
-        __syncthreads();
-        if (at + BK < sum) {
-          la.load(A + (at + BK) * (TRA ? lda : 1), lda, rows, left(at + BK), tid);
-          lb.load(B + (at + BK) * (TRB ? ldb : 1), ldb, cols, left(at + BK), tid);
-        }
-        tile_multiply<PREC, TRA, TRB, WM, WN, TM, TN, BK>(smem, smem + SA::kBytes, acc, tid);
-        __syncthreads();
-      }
-#pragma unroll
-      for (int i = 0; i < TM * TN; ++i) all[i / TN][i % TN] += acc[i / TN][i % TN];
-    }
-#pragma unroll
-    for (int i = 0; i < TM * TN; ++i) acc[i / TN][i % TN] = all[i / TN][i % TN];
   }
+  la.load(A, lda, rows, left(0), tid);
+  lb.load(B, ldb, cols, left(0), tid);
+  for (int64_t k = 0; k < sum; k += BK) {
+    la.store(smem, tid);
+    lb.store(smem + SA::kBytes, tid);
+    __syncthreads();
+    if (k + BK < sum) {
+      la.load(A + (k + BK) * (TRA ? lda : 1), lda, rows, left(k + BK), tid);
+      lb.load(B + (k + BK) * (TRB ? ldb : 1), ldb, cols, left(k + BK), tid);
+    }
+    tile_multiply<PREC, TRA, TRB, WM, WN, TM, TN, BK>(smem, smem + SA::kBytes, acc, tid);
+    __syncthreads();
+    if constexpr (LONG)                           // (as a loop around this one it cost 16 % where it costs 4: 1024 x 1024, three terms)
+      if (k + BK >= until) {
+        until += run;
+#pragma unroll
+        for (int i = 0; i < TM * TN; ++i) {
+          all[i / TN][i % TN] += acc[i / TN][i % TN];
+#pragma unroll
+          for (int v = 0; v < 16; ++v) acc[i / TN][i % TN][v] = 0.f;
+        }
+      }
+  }
+  if constexpr (LONG)
+#pragma unroll
+    for (int i = 0; i < TM * TN; ++i) acc[i / TN][i % TN] += all[i / TN][i % TN];
 }
 
 // f(row, column, sums) of what a lane holds, four neighbouring columns of a row at a time (the products are taken transposed for
