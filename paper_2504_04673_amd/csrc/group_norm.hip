@@ -231,10 +231,10 @@ __device__ __forceinline__ float act_gradient(float g, float z) {
 // the variance its digits: their sum is (1 + ((mean - pivot) / deviation)^2) n variances, and a value of n is at most n^(1/2) deviations
 // from their mean, so that of 53 bits log2(n) are lost at worst, and two or three where the first value is no outlier.  (0 where it is
 // not finite: the mean then is infinite or a NaN as the sum is.)
+__device__ __forceinline__ float finite(float x) { return __builtin_isfinite(x) ? x : 0.f; }
 template <typename S>
 __device__ __forceinline__ float pivot_of(const NormArgs& a, int64_t row, int c) {
-  const float x = (float)reinterpret_cast<const S*>(a.X)[row * a.ldx + c / a.D * a.D];
-  return __builtin_isfinite(x) ? x : 0.f;
+  return finite((float)reinterpret_cast<const S*>(a.X)[row * a.ldx + c / a.D * a.D]);
 }
 
 // Sum and sum of squares of a part, from the segment's pivots, in 64 bits
@@ -657,8 +657,9 @@ __device__ __forceinline__ Whole<S, V> fetch_at(const void* row, uint32_t lane) 
 }
 
 constexpr int kBehind = 16;                // workgroups of a slab for the rows behind the last segment
+// (Vectors of several groups: six wavefronts to a SIMD are worth two registers.  1 M x 100, four groups, 20000 segments: 230 us, with five 269.)
 template <typename S, int V, int N, int ACT>
-__global__ __launch_bounds__(kMostTeam) void norm_whole_kernel(const NormArgs a, int32_t slabs) {
+__global__ __launch_bounds__(kMostTeam, N > 1 ? 6 : 1) void norm_whole_kernel(const NormArgs a, int32_t slabs) {
   extern __shared__ __attribute__((aligned(16))) char smem[];
   const Team t = team<V>(a, (int)(blockIdx.x % slabs));
   const int64_t b = a.first + blockIdx.x / slabs;
@@ -668,6 +669,7 @@ __global__ __launch_bounds__(kMostTeam) void norm_whole_kernel(const NormArgs a,
   }
   double2* sums = reinterpret_cast<double2*>(smem);
   double2* sm = sums + a.slab / a.D;
+  float* pivots = reinterpret_cast<float*>(sm + blockDim.x * N);
   const int64_t lo = seg_row(a, b), hi = seg_row(a, b + 1);
   const int ch = t.c0 + t.tx * V;
   // rows lo + ty + n * t.rows: a lane's part of the address does not change
@@ -682,11 +684,14 @@ __global__ __launch_bounds__(kMostTeam) void norm_whole_kernel(const NormArgs a,
 #pragma unroll
     for (int n = 0; n < kKept; ++n) kept[n] = fetch_at<S, V>(x_row(0), at + (n < there ? n * step : 0));
   }
+  const int groups = t.width / a.D;
+  for (int g = threadIdx.x; g < groups; g += blockDim.x) pivots[g] = hi > lo ? finite((float)x_row(0)[t.c0 + g * a.D]) : 0.f;
+  __syncthreads();
   double p[N], q[N], from[N];
 #pragma unroll
   for (int i = 0; i < N; ++i) {
     p[i] = q[i] = 0.;
-    from[i] = mine ? pivot_of<S>(a, lo, ch + i) : 0.f;
+    from[i] = t.ty < t.rows ? pivots[(t.tx * V + i) / a.D] : 0.f;
   }
   auto add = [&](const Whole<S, V>& w) {
 #pragma unroll
@@ -703,8 +708,8 @@ __global__ __launch_bounds__(kMostTeam) void norm_whole_kernel(const NormArgs a,
   }
   for (int64_t n = kKept; n < mine; ++n) add(fetch_at<S, V>(x_row(n), vx));
   team_groups<V, N>(a, t, p, q, sm, sums);
-  for (int g = threadIdx.x; g < t.width / a.D; g += blockDim.x) {     // (nobody writes rows before the barrier)
-    const float2 s = moments(a, sums[g], hi - lo, hi > lo ? pivot_of<S>(a, lo, t.c0 + g * a.D) : 0.f);
+  for (int g = threadIdx.x; g < groups; g += blockDim.x) {
+    const float2 s = moments(a, sums[g], hi - lo, pivots[g]);
     const int64_t at = b * a.groups + t.c0 / a.D + g;
     a.mean[at] = s.x;
     a.rstd[at] = s.y;
@@ -932,7 +937,8 @@ WholePlan whole_plan(int64_t m, int32_t segments, int64_t max_rows, int32_t C, i
 // Forward: eight values only where they are of one group.  Of several, 512 threads' sums of them are 64 KB of LDS and the groups' more.
 constexpr int whole_vector(int v, int D) { return v > 4 && D % v ? 4 : v; }
 size_t whole_lds(const WholePlan& w, int32_t D, int v, bool backward) {
-  return ((size_t)(w.slab / D) + (size_t)w.threads * (D % v == 0 ? 1 : v)) * sizeof(double2) + (backward ? (size_t)w.threads * v * sizeof(float2) : 0);
+  return ((size_t)(w.slab / D) + (size_t)w.threads * (D % v == 0 ? 1 : v)) * sizeof(double2) +
+         (backward ? (size_t)w.threads * v * sizeof(float2) : (size_t)(w.slab / D) * sizeof(float));
 }
 
 // How a call is carried out, and what it needs for that
