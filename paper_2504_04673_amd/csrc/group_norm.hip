@@ -14,6 +14,9 @@ namespace sagnn {
 namespace {
 
 constexpr int kThreads = 256;
+// Terms of the gradients' sums that a thread adds up in 32 bits, one after the other: equal ones may round the same way, n/3 2^-24 of
+// their sum for n
+constexpr int64_t kSerial = 384;
 
 struct NormArgs {
   const void* X; int64_t ldx;
@@ -33,7 +36,11 @@ struct NormArgs {
   double2* parts;                    // (chunks + segments) x groups
   float* pivots;                     // forward, segments x groups: what the sums of parts are taken from
   float2* sums;                      // backward, segments x groups: the two sums over a group, divided by its size
-  float2* rows;                      // backward, table x C: sums of h xh and h over the rows of a chunk (of some segments)
+  // backward, table x C: sums of h xh and h, over the rows of a chunk (double2: as many are added up as it has segments) or over some
+  // whole segments (float2)
+  void* rows;
+  template <typename Sum>
+  __device__ __forceinline__ Sum* row_of(int64_t at) const { return reinterpret_cast<Sum*>(rows) + at * C; }
 };
 
 template <typename S, int V>
@@ -463,8 +470,8 @@ __global__ __launch_bounds__(kThreads) void norm_bwd_sum_kernel(const NormArgs a
         for (int i = 0; i < V; ++i) sf[(l.ty * l.per_row + l.tx) * V + i] = make_float2(q[i], p[i]);
       add_rows(sf, l.rows, width, kThreads);
       for (int x = threadIdx.x; x < width; x += kThreads) {
-        float2 s = sf[x];
-        float2* out = a.rows + c * a.C + vec0 * V + x;
+        double2 s = make_double2(sf[x].x, sf[x].y);
+        double2* out = a.row_of<double2>(c) + vec0 * V + x;
         if (!first) {
           s.x += out->x;
           s.y += out->y;
@@ -478,22 +485,22 @@ __global__ __launch_bounds__(kThreads) void norm_bwd_sum_kernel(const NormArgs a
     __syncthreads();
   });
   if (first)
-    for (int x = threadIdx.x; x < a.C; x += kThreads) a.rows[c * a.C + x] = make_float2(0.f, 0.f);
+    for (int x = threadIdx.x; x < a.C; x += kThreads) a.row_of<double2>(c)[x] = make_double2(0., 0.);
 }
 
 // Sixteen channels of gamma and beta: the rows of the table, THREADS / 16 at a time.  (With 64 channels for four wavefronts 1037
 // rows took 67 us.)
-template <int THREADS>
+template <int THREADS, typename Sum>
 __device__ __forceinline__ void join_rows(const NormArgs& a, int32_t block) {
   __shared__ double2 sm[THREADS / 64][16];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int ch = block * 16 + (threadIdx.x & 15);
   double2 s = make_double2(0., 0.);
   if (ch < a.C) {
-    const float2* p = a.rows + ch;
+    const Sum* p = a.row_of<Sum>(0) + ch;
 #pragma unroll 8
     for (int64_t c = threadIdx.x >> 4; c < a.table; c += THREADS / 16) {
-      const float2 v = p[c * a.C];
+      const Sum v = p[c * a.C];
       s.x += v.x;
       s.y += v.y;
     }
@@ -516,9 +523,10 @@ __device__ __forceinline__ void join_rows(const NormArgs& a, int32_t block) {
 
 // Workgroups below `wide` join the rows of the table, the others a segment and group for each wavefront.
 constexpr int kJoinThreads = 1024;
+template <typename Sum>
 __global__ __launch_bounds__(kJoinThreads) void norm_bwd_join_kernel(const NormArgs a, int32_t wide) {
   if ((int)blockIdx.x < wide) {
-    join_rows<kJoinThreads>(a, (int32_t)blockIdx.x);
+    join_rows<kJoinThreads, Sum>(a, (int32_t)blockIdx.x);
     return;
   }
   for (int64_t at = (int64_t)(blockIdx.x - wide) * (kJoinThreads / 64) + (threadIdx.x >> 6); at < (int64_t)a.segments * a.groups;
@@ -544,7 +552,7 @@ __global__ __launch_bounds__(kThreads) void norm_bwd_write_kernel(const NormArgs
   extern __shared__ __attribute__((aligned(16))) char smem[];
   float2* here = reinterpret_cast<float2*>(smem);
   if ((int64_t)blockIdx.x >= a.chunks) {                    // (where there is no launch between for it)
-    join_rows<kThreads>(a, (int32_t)(blockIdx.x - a.chunks));
+    join_rows<kThreads, double2>(a, (int32_t)(blockIdx.x - a.chunks));
     return;
   }
   each_part(a, a.chunks - 1 - blockIdx.x, [&](int32_t b, int64_t r0, int64_t r1) {
@@ -739,7 +747,9 @@ __global__ __launch_bounds__(kMostTeam, N > 1 ? 6 : 1) void norm_whole_kernel(co
   for (int64_t n = kKept; n < mine; ++n) put(n, fetch_at<S, V>(x_row(n), vx));
 }
 
-// Backward: workgroups take segments in turn and keep gamma's and beta's sums until their last one.
+// Backward: workgroups take segments in turn and keep gamma's and beta's sums until their last one.  Segments longer than the caller said,
+// more than a workgroup keeps, come behind the others, in a loop of their own: beside them it would cost registers that are not
+// there (a loop over further rows inside the first one: 476 us of 1 M x 256 with SiLU became 507 to 570).
 template <typename S, int V, int N, int ACT>
 __global__ __launch_bounds__(kMostTeam, 4) void norm_bwd_whole_kernel(const NormArgs a, int32_t slabs) {
   extern __shared__ __attribute__((aligned(16))) char smem[];
@@ -757,21 +767,45 @@ __global__ __launch_bounds__(kMostTeam, 4) void norm_bwd_whole_kernel(const Norm
   const int ch = t.c0 + t.tx * V;
   const uint32_t vx = (uint32_t)((t.ty * a.ldx + ch) * sizeof(S)), vg = (uint32_t)((t.ty * a.ldg + ch) * sizeof(S)),
                  vy = (uint32_t)((t.ty * a.ldy + ch) * sizeof(S));
+  auto x_row = [&](int64_t r) { return reinterpret_cast<const S*>(a.X) + r * a.ldx; };
+  auto g_row = [&](int64_t r) { return reinterpret_cast<const S*>(a.G) + r * a.ldg; };
+  auto y_row = [&](int64_t r) { return reinterpret_cast<char*>(reinterpret_cast<S*>(a.Y) + r * a.ldy); };
+  // rows lo + ty + n * t.rows are this thread's
+  auto rows_of = [&](int64_t rows) { return t.ty < t.rows && rows > t.ty ? (rows - t.ty + t.rows - 1) / t.rows : 0; };
+  auto lines = [&](int64_t rows, const Channel<V, N>& k, float (&tilt)[N], float (&level)[N]) {
+    const double n_values = 1. / ((double)rows * a.D);
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const double2 v = sums[(t.tx * V + i) / a.D];
+      input_line(k.rstd[i], make_float2((float)(v.x * n_values), (float)(v.y * n_values)), tilt[i], level[i]);
+    }
+  };
+  auto put = [&](int64_t r, const Channel<V, N>& k, const float (&tilt)[N], const float (&level)[N], const Whole<S, V>& w, const Whole<S, V>& g, bool done) {
+    float y[V];
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+      const float d = k.off((float)w.x[i], i), h = done ? (float)g.x[i] : act_gradient<ACT>((float)g.x[i], k.z(d, i));
+      y[i] = fmaf(h, k.scale[i], fmaf(d, tilt[i % N], level[i % N]));
+    }
+    store<S, V>(reinterpret_cast<S*>(y_row(r) + vy), y);
+  };
+  bool longer = false;
   for (int64_t b = stripe; b < a.segments; b += stripes) {
     const int64_t lo = seg_row(a, b), hi = seg_row(a, b + 1);
-    auto x_row = [&](int64_t n) { return reinterpret_cast<const S*>(a.X) + (lo + n * t.rows) * a.ldx; };
-    auto g_row = [&](int64_t n) { return reinterpret_cast<const S*>(a.G) + (lo + n * t.rows) * a.ldg; };
-    auto y_row = [&](int64_t n) { return reinterpret_cast<char*>(reinterpret_cast<S*>(a.Y) + (lo + n * t.rows) * a.ldy); };
-    const int64_t mine = t.ty < t.rows && hi - lo > t.ty ? (hi - lo - t.ty + t.rows - 1) / t.rows : 0;
-    const int there = mine < K ? (int)mine : K;
+    if (hi <= lo) continue;
+    if (hi - lo > (int64_t)K * t.rows) {
+      longer = true;
+      continue;
+    }
+    const int there = (int)rows_of(hi - lo);
     Whole<S, V> x[K], h[K];
-    if (hi > lo) {
+    {
       const uint32_t step_x = (uint32_t)(t.rows * a.ldx * sizeof(S)), step_g = (uint32_t)(t.rows * a.ldg * sizeof(S)),
-                     at_x = mine ? vx : (uint32_t)(ch * sizeof(S)), at_g = mine ? vg : (uint32_t)(ch * sizeof(S));
+                     at_x = there ? vx : (uint32_t)(ch * sizeof(S)), at_g = there ? vg : (uint32_t)(ch * sizeof(S));
 #pragma unroll
       for (int n = 0; n < K; ++n) {
-        x[n] = fetch_at<S, V>(x_row(0), at_x + (n < there ? n * step_x : 0));
-        h[n] = fetch_at<S, V>(g_row(0), at_g + (n < there ? n * step_g : 0));
+        x[n] = fetch_at<S, V>(x_row(lo), at_x + (n < there ? n * step_x : 0));
+        h[n] = fetch_at<S, V>(g_row(lo), at_g + (n < there ? n * step_g : 0));
         __builtin_amdgcn_sched_barrier(0);                  // (addresses one after the other)
       }
     }
@@ -784,25 +818,19 @@ __global__ __launch_bounds__(kMostTeam, 4) void norm_bwd_whole_kernel(const Norm
       float p[V], q[V];
 #pragma unroll
       for (int i = 0; i < V; ++i) p[i] = q[i] = 0.f;
-      auto add = [&](const Whole<S, V>& w, Whole<S, V>& g) {
-#pragma unroll
-        for (int i = 0; i < V; ++i) {
-          const float d = k.off((float)w.x[i], i), y = act_gradient<ACT>((float)g.x[i], k.z(d, i));
-          p[i] += y;
-          q[i] = fmaf(y, d * k.rstd[i % N], q[i]);
-          if (kExact) g.x[i] = (S)y;
-        }
-      };
 #pragma unroll
       for (int n = 0; n < K; ++n) {
         keep(x[n]);
         keep(h[n]);
-        if (n < there) add(x[n], h[n]);
+        if (n < there)
+#pragma unroll
+          for (int i = 0; i < V; ++i) {
+            const float d = k.off((float)x[n].x[i], i), y = act_gradient<ACT>((float)h[n].x[i], k.z(d, i));
+            p[i] += y;
+            q[i] = fmaf(y, d * k.rstd[i % N], q[i]);
+            if (kExact) h[n].x[i] = (S)y;
+          }
         __builtin_amdgcn_sched_barrier(0);                 // (one vector's temporaries at a time)
-      }
-      for (int64_t n = K; n < mine; ++n) {
-        Whole<S, V> g = fetch_at<S, V>(g_row(n), vg);
-        add(fetch_at<S, V>(x_row(n), vx), g);
       }
 #pragma unroll
       for (int i = 0; i < V; ++i) {
@@ -816,32 +844,54 @@ __global__ __launch_bounds__(kMostTeam, 4) void norm_bwd_whole_kernel(const Norm
       }
     }
     team_groups<V, N>(a, t, dp, dq, sm, sums);
-    const double n_values = hi > lo ? 1. / ((double)(hi - lo) * a.D) : 1.;
-    if (mine == 0) continue;
+    if (there == 0) continue;
     float tilt[N], level[N];
-#pragma unroll
-    for (int i = 0; i < N; ++i) {
-      const double2 v = sums[(t.tx * V + i) / a.D];
-      input_line(k.rstd[i], make_float2((float)(v.x * n_values), (float)(v.y * n_values)), tilt[i], level[i]);
-    }
-    auto put = [&](int64_t n, const Whole<S, V>& w, const Whole<S, V>& g, bool done) {
-      float y[V];
-#pragma unroll
-      for (int i = 0; i < V; ++i) {
-        const float d = k.off((float)w.x[i], i), h = done ? (float)g.x[i] : act_gradient<ACT>((float)g.x[i], k.z(d, i));
-        y[i] = fmaf(h, k.scale[i], fmaf(d, tilt[i % N], level[i % N]));
-      }
-      store<S, V>(reinterpret_cast<S*>(y_row(n) + vy), y);
-    };
+    lines(hi - lo, k, tilt, level);
 #pragma unroll
     for (int n = 0; n < K; ++n) {
       keep(x[n]);
       keep(h[n]);
-      if (n < there) put(n, x[n], h[n], kExact);
+      if (n < there) put(lo + (int64_t)n * t.rows, k, tilt, level, x[n], h[n], kExact);
       __builtin_amdgcn_sched_barrier(0);
     }
-    for (int64_t n = K; n < mine; ++n) put(n, fetch_at<S, V>(x_row(n), vx), fetch_at<S, V>(g_row(n), vg), false);
   }
+  if (longer)
+#pragma unroll 1
+    for (int64_t b = stripe; b < a.segments; b += stripes) {
+      const int64_t lo = seg_row(a, b), hi = seg_row(a, b + 1);
+      if (hi - lo <= (int64_t)K * t.rows) continue;
+      const int64_t mine = rows_of(hi - lo);
+      Channel<V, N> k;
+      k.read(a, (int32_t)b, ch);
+      double p[V], q[V], dp[N], dq[N];                     // (there may be any number of rows)
+#pragma unroll
+      for (int i = 0; i < V; ++i) p[i] = q[i] = 0.;
+      for (int64_t n = 0; n < mine; ++n) {
+        const Whole<S, V> w = fetch_at<S, V>(x_row(lo + n * t.rows), vx), g = fetch_at<S, V>(g_row(lo + n * t.rows), vg);
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+          const float d = k.off((float)w.x[i], i), y = act_gradient<ACT>((float)g.x[i], k.z(d, i));
+          p[i] += y;
+          q[i] = fma((double)y, (double)(d * k.rstd[i % N]), q[i]);
+        }
+      }
+#pragma unroll
+      for (int i = 0; i < N; ++i) dp[i] = dq[i] = 0.;
+#pragma unroll
+      for (int i = 0; i < V; ++i) {
+        all[i * blockDim.x].x += (float)q[i];
+        all[i * blockDim.x].y += (float)p[i];
+        const float gamma = a.gamma ? a.gamma[ch + i] : 1.f;
+        dp[i % N] += p[i] * gamma;
+        dq[i % N] += q[i] * gamma;
+      }
+      team_groups<V, N>(a, t, dp, dq, sm, sums);
+      if (mine == 0) continue;
+      float tilt[N], level[N];
+      lines(hi - lo, k, tilt, level);
+      for (int64_t n = 0; n < mine; ++n)
+        put(lo + n * t.rows, k, tilt, level, fetch_at<S, V>(x_row(lo + n * t.rows), vx), fetch_at<S, V>(g_row(lo + n * t.rows), vg), false);
+    }
   team_zeros<S, V>(a, t, stripe, stripes);
   // this workgroup's row of the table of gamma's and beta's sums
   __syncthreads();
@@ -862,7 +912,7 @@ __global__ __launch_bounds__(kMostTeam, 4) void norm_bwd_whole_kernel(const Norm
     for (int i = 0; i < V; ++i) {
       const float2 v = all[i * blockDim.x];
       if (stripes > 1) {
-        a.rows[stripe * a.C + ch + i] = v;
+        a.row_of<float2>(stripe)[ch + i] = v;
       } else {                                              // (the only row: nothing to join)
         if (a.dgamma) a.dgamma[ch + i] = v.x;
         if (a.dbeta) a.dbeta[ch + i] = v.y;
@@ -889,13 +939,17 @@ NormPlan norm_plan(int32_t dtype, int64_t m, int32_t segments, int32_t C, int32_
   const int64_t most = vectors > (1 << 23) ? 2048 : 1024;
   chunks = chunks < 1 ? 1 : chunks > most ? most : chunks;
   p.chunk = ceil_div(m > 0 ? m : 1, chunks);
+  if (backward) {
+    const int64_t per_row = C / vector_of(dtype, C), serial = kSerial * (per_row < kThreads ? kThreads / per_row : 1);
+    if (p.chunk > serial) p.chunk = serial;
+  }
   p.chunks = ceil_div(m > 0 ? m : 1, p.chunk);
   size_t off = 0;
   auto take = [&](size_t bytes) { const size_t o = off; off += round_up(bytes, 256); return o; };
   p.parts = take((size_t)(p.chunks + segments) * groups * sizeof(double2));
   if (backward) {
     p.sums = take((size_t)segments * groups * sizeof(float2));
-    p.rows = take((size_t)p.chunks * C * sizeof(float2));
+    p.rows = take((size_t)p.chunks * C * sizeof(double2));
   } else {
     p.pivots = take((size_t)segments * groups * sizeof(float));
   }
@@ -953,6 +1007,8 @@ NormForm norm_form(int32_t dtype, int64_t m, int32_t segments, int64_t max_rows,
   if (m > 0 && ld <= kWholeLd) f.whole = whole_plan(m, segments, max_rows, C, D, v, size, !backward ? kKept : D % v == 0 ? kKeptBackward : kKeptBackward / 2, backward);
   if (f.whole.slab) {
     f.table = segments < kMostStripes ? segments : kMostStripes;
+    if (f.table < segments / kSerial) f.table = segments / kSerial;
+    if (f.table > most_blocks(f.whole.threads) / f.whole.slabs) f.table = most_blocks(f.whole.threads) / f.whole.slabs;
     f.bytes = backward && f.table > 1 ? round_up((size_t)f.table * C * sizeof(float2), 256) : 0;
   } else {
     f.parts = norm_plan(dtype, m, segments, C, groups, backward);
@@ -1091,7 +1147,7 @@ SAGNN_EXPORT int group_norm_act_bwd(int32_t dtype, const void* d_X, int64_t ldx,
   a.X = d_X; a.ldx = ldx; a.G = d_G; a.ldg = ldg; a.Y = d_dX; a.ldy = lddx; a.seg = d_seg; a.segments = n_seg; a.each = m / n_seg; a.m = m;
   a.C = C; a.groups = n_groups; a.D = C / n_groups; a.gamma = d_gamma; a.beta = d_beta; a.mean = const_cast<float*>(d_mean);
   a.rstd = const_cast<float*>(d_rstd); a.act = act; a.dgamma = d_dgamma; a.dbeta = d_dbeta; a.chunk = p.chunk; a.chunks = p.chunks;
-  a.parts = (double2*)((char*)d_ws + p.parts); a.sums = (float2*)((char*)d_ws + p.sums); a.rows = (float2*)((char*)d_ws + p.rows);
+  a.parts = (double2*)((char*)d_ws + p.parts); a.sums = (float2*)((char*)d_ws + p.sums); a.rows = (char*)d_ws + p.rows;
   a.table = f.table; a.slab = w.slab; a.joined = f.joined;
   hipStream_t s = (hipStream_t)stream;
   return by_act(act, [&](auto A) { return by_vector(dtype, vector_of(dtype, C), [&](auto V, auto zero) {
@@ -1106,7 +1162,7 @@ SAGNN_EXPORT int group_norm_act_bwd(int32_t dtype, const void* d_X, int64_t ldx,
       else norm_bwd_whole_kernel<S, u, u, ACT><<<grid, (uint32_t)w.threads, lds, s>>>(a, w.slabs);
       SAGNN_LAUNCH_CHECK();
       if (a.table > 1) {
-        norm_bwd_join_kernel<<<dim3((uint32_t)wide), kJoinThreads, 0, s>>>(a, wide);
+        norm_bwd_join_kernel<float2><<<dim3((uint32_t)wide), kJoinThreads, 0, s>>>(a, wide);
         SAGNN_LAUNCH_CHECK();
       }
       return (int)SAGNN_OK;
@@ -1117,7 +1173,7 @@ SAGNN_EXPORT int group_norm_act_bwd(int32_t dtype, const void* d_X, int64_t ldx,
     }
     if (!a.joined) {
       const int64_t joins = ceil_div((int64_t)n_seg * n_groups, kJoinThreads / 64);
-      norm_bwd_join_kernel<<<dim3((uint32_t)(wide + (joins < kMostJoins ? joins : kMostJoins))), kJoinThreads, 0, s>>>(a, wide);
+      norm_bwd_join_kernel<double2><<<dim3((uint32_t)(wide + (joins < kMostJoins ? joins : kMostJoins))), kJoinThreads, 0, s>>>(a, wide);
       SAGNN_LAUNCH_CHECK();
     }
     if (m > 0) {
