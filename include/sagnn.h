@@ -60,7 +60,7 @@ enum {
 
 #define SAGNN_ACT_IDENTITY 0
 #define SAGNN_ACT_RELU 1
-#define SAGNN_ACT_SILU 2 /* z / (1 + exp(-z)); group_norm_act_fwd / _bwd only */
+#define SAGNN_ACT_SILU 2 /* z / (1 + exp(-z)), the exponential to (4 + |z|) 2^-24 of itself; group_norm_act_fwd / _bwd only */
 
 #define SAGNN_F32 0  /* storage types of the calls that take one */
 #define SAGNN_BF16 1
@@ -636,11 +636,13 @@ int grouped_gemm_bwd(int32_t dtype, const void* d_X, int64_t ldx, const void* d_
  *
  * d_seg (device, n_seg+1 int32, ascending, d_seg[0] = 0, d_seg[n_seg] <= m) or NULL for n_seg segments of m / n_seg rows
  * each.  Segments may be empty (mean 0, rstd 1 / sqrt(eps)).  Rows behind the last segment: zeros in Y and dX, no part
- * of any sum.  max_rows: rows of the longest segment if the caller knows it, 0 if not; it only chooses between forms.
+ * of any sum.  max_rows: rows of the longest segment if the caller knows it (m / n_seg where d_seg is NULL), 0 if not; it only chooses
+ * between forms, in one of which a workgroup has a whole segment: a value below the true one is slow, not wrong.
  * dtype: type of X, Y, G, dX; gamma, beta (each may be NULL: 1, 0), mean, rstd (n_seg x n_groups), dgamma, dbeta (each
  * may be NULL) are fp32.  mean and rstd are outputs forward and inputs backward.  Mean and variance are summed in 64 bits, of
  * values less the segment's and group's first; (x - mean) is formed before anything is multiplied, with the mean as it is stored.
- * Orders of sums are fixed: the same bits every time.  Any C up to SAGNN_NORM_MAX_WIDTH, n_groups <= SAGNN_NORM_MAX_GROUPS,
+ * The gradients' sums are runs of fp32 short enough to err by less than 1e-5 of the sum of their terms' absolute values, joined in 64
+ * bits.  Orders of sums are fixed: the same bits every time.  Any C up to SAGNN_NORM_MAX_WIDTH, n_groups <= SAGNN_NORM_MAX_GROUPS,
  * any leading dimensions not below C, tensors aligned to their element.  Y may be X, dX may be G or X, in the same place and with the same leading
  * dimension, or lie beside it in wider rows; other overlaps are refused.
  * d_ws: group_norm_workspace_bytes() bytes, 16-byte aligned; NULL where that is 0 (short segments forward, a single

@@ -26,7 +26,7 @@ struct NormArgs {
   int64_t m; int32_t C, groups, D;   // D = C / groups
   const float* gamma; const float* beta;
   float* mean; float* rstd;          // segments x groups: outputs forward, inputs backward
-  double eps; int32_t act;
+  double eps;
   float* dgamma; float* dbeta;
   int64_t chunk, chunks;             // rows of a chunk, chunks
   int64_t table;                     // rows of `rows`
@@ -213,7 +213,8 @@ __device__ __forceinline__ void to_groups(const NormArgs& a, const Lay& l, int c
   }
 }
 
-// 1 / (1 + exp(-z)) by the machine's exponential and reciprocal (an ulp each); a division in its place is ten instructions.
+// 1 / (1 + exp(-z)) by the machine's exponential and reciprocal (an ulp each; the exponent's own rounding makes |z| 2^-24 of the exponential); a
+// division in its place is ten instructions.
 __device__ __forceinline__ float sigmoid(float z) {
   return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(z * -1.44269504f));
 }
@@ -1089,7 +1090,7 @@ SAGNN_EXPORT int group_norm_act_fwd(int32_t dtype, const void* d_X, int64_t ldx,
   if (ws_bytes < f.bytes) return SAGNN_ECAPACITY;
   NormArgs a{};
   a.X = d_X; a.ldx = ldx; a.Y = d_Y; a.ldy = ldy; a.seg = d_seg; a.segments = n_seg; a.each = m / n_seg; a.m = m; a.C = C; a.groups = n_groups;
-  a.D = C / n_groups; a.gamma = d_gamma; a.beta = d_beta; a.mean = d_mean; a.rstd = d_rstd; a.eps = eps; a.act = act;
+  a.D = C / n_groups; a.gamma = d_gamma; a.beta = d_beta; a.mean = d_mean; a.rstd = d_rstd; a.eps = eps;
   a.chunk = p.chunk; a.chunks = p.chunks; a.parts = (double2*)((char*)d_ws + p.parts); a.pivots = (float*)((char*)d_ws + p.pivots); a.slab = w.slab; a.joined = f.joined;
   hipStream_t s = (hipStream_t)stream;
   return by_act(act, [&](auto A) { return by_vector(dtype, vector_of(dtype, C), [&](auto V, auto zero) {
@@ -1146,7 +1147,7 @@ SAGNN_EXPORT int group_norm_act_bwd(int32_t dtype, const void* d_X, int64_t ldx,
   NormArgs a{};
   a.X = d_X; a.ldx = ldx; a.G = d_G; a.ldg = ldg; a.Y = d_dX; a.ldy = lddx; a.seg = d_seg; a.segments = n_seg; a.each = m / n_seg; a.m = m;
   a.C = C; a.groups = n_groups; a.D = C / n_groups; a.gamma = d_gamma; a.beta = d_beta; a.mean = const_cast<float*>(d_mean);
-  a.rstd = const_cast<float*>(d_rstd); a.act = act; a.dgamma = d_dgamma; a.dbeta = d_dbeta; a.chunk = p.chunk; a.chunks = p.chunks;
+  a.rstd = const_cast<float*>(d_rstd); a.dgamma = d_dgamma; a.dbeta = d_dbeta; a.chunk = p.chunk; a.chunks = p.chunks;
   a.parts = (double2*)((char*)d_ws + p.parts); a.sums = (float2*)((char*)d_ws + p.sums); a.rows = (char*)d_ws + p.rows;
   a.table = f.table; a.slab = w.slab; a.joined = f.joined;
   hipStream_t s = (hipStream_t)stream;
