@@ -604,7 +604,8 @@ int spmm_volume_stats(const int64_t* h_counts, int32_t P, int32_t f, int32_t ele
  * dtype: SAGNN_F32 or SAGNN_BF16, the type of X, W, G, mask, Y and dX; dW is fp32.  prec: as in dense_gemm_act for
  * fp32 tensors, SAGNN_GEMM_FP32 for bfloat16 ones (whose products are exact).  All sums are fp32 (the parts of a type's dW are
  * added in 64 bits), their order is a fixed function of the arguments and d_off: the same bits every time.  Long sums are cut into
- * runs, so that they err by less than 1e-5 of the sum of their terms' absolute values, equal terms included.  Results are rounded once.
+ * runs, so that they err by less than 1e-5 of the sum of their terms' absolute values, equal terms included (bfloat16 results, whose
+ * own rounding is 2e-3: by less than 4e-5 where kdim is above 5120).  Results are rounded once.
  * Any widths up to SAGNN_GROUPED_MAX_WIDTH, any leading dimensions not below the width, pointers aligned to their
  * element; tensors with 16-byte aligned rows are read faster.  n_groups <= SAGNN_GROUPED_MAX.  Outputs must not overlap
  * inputs.  d_ws of grouped_gemm_bwd: grouped_gemm_bwd_workspace_bytes() bytes, 4-byte aligned, needed for dW only.

@@ -31,6 +31,9 @@ struct GroupedArgs {
 // terms and 542 for 4096 (the small products are cut first); bfloat16 0 up to 2048, where a sum of products of 16 bits begins to need
 // more than 24, 128 for 4096, 192 for 6144.  A longer sum is cut into runs, which are added in turn; a run and the runs together stay below 168.
 enum { kRunFp32 = 480, kRunTerms = 768, kRunBf16 = 5120 };       // a sum up to here is one run
+// Bfloat16 results that the tile without room for a second set of sums makes: one run up to here, which errs by 512 2^-24 at most, a sixtieth of the
+// result's own rounding (8192^3 876 us; in runs, by a smaller tile, 1578).
+constexpr int64_t kRunRounded = 16384;
 // The longest run of a sum of `sum`, and the longest sum
 inline int32_t grouped_run(int32_t prec, int64_t sum) {
   if (prec == SAGNN_GEMM_FP32) return sum <= kRunFp32 ? kRunFp32 : sum <= 96 * 384 ? 384 : 256;

@@ -63,7 +63,7 @@ TileCost tile_cost(int32_t dtype, int32_t prec, int tile) {
 
 // The tile with the least cost: `rows` rows in `parts` ragged parts by `cols` columns, `times` over, `sum` of the summed index.  Tiles are
 // whole, so each part leaves half a tile empty; a launch lasts as long as its fullest CU; and a tile alone on a CU waits for its
-// loads.  `whole`: a product of rows.  Bfloat16 results are no place for the sum of several runs, which the largest tiles and the thin ones would
+// loads.  `whole`: a product of rows.  Bfloat16 results are no place for the sum of several runs, which the largest tile and the thin one would
 // need.
 int choose_tile(int32_t dtype, int32_t prec, int ways, int64_t rows, int64_t parts, int64_t cols, int64_t times, int64_t sum, bool whole) {
   int best = kTile128;
@@ -72,7 +72,7 @@ int choose_tile(int32_t dtype, int32_t prec, int ways, int64_t rows, int64_t par
     const TileCost c = tile_cost(dtype, prec, tile);
     if (c.rate == 0 || (tile == kDirect256 && !(ways & kDirect)) || ((tile == kStaged256x128 || tile == kStaged128x256) && !(ways & kStaged))) continue;
     if (tile == kThin && !whole) continue;
-    if (whole && dtype == SAGNN_BF16 && ((tile == kDirect256 && sum > kRunBf16) || (tile == kThin && sum > 8 * kRunBf16))) continue;
+    if (whole && dtype == SAGNN_BF16 && ((tile == kDirect256 && sum > kRunRounded) || (tile == kThin && sum > 8 * kRunBf16))) continue;
     const int64_t h = grouped_tile_rows(tile), w = grouped_tile_cols(tile);
     const int64_t tiles = (ceil_div(rows, h) + (parts < rows ? parts : rows) / 2) * ceil_div(cols, w) * times;
     const double turns = tiles <= 256 ? 1.25 : whole && tiles < 4 * 256 ? (double)ceil_div(tiles, 256) : tiles / 256.;
