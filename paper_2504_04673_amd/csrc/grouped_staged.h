@@ -3,9 +3,10 @@
 //
 // Bound: the matrix cores (six products for each of the split mode) and beside them the conversion, some seven instructions for each
 // staged value, which a wavefront does between its products: those leave it seven issue slots each.  256 x 128 converts a
-// quarter less than 128 x 128.  8192 x 4096 x 4096, three terms: 1330 us, 207 TFLOP/s, six times that on the matrix cores, the
-// rate of the library's bfloat16 product; rounded 530 us.  (grouped.h's tiles of 128 x 128: 1550 and 600.  With fp32 instructions, 133 TFLOP/s in
-// either, there is nothing to gain.)
+// quarter less than 128 x 128.  8192 x 4096 x 4096, three terms: 1340 to 1380 us, some 202 TFLOP/s, six times that on the matrix cores, the
+// rate of the library's bfloat16 product.  Rounded 530 to 590 us, dX 700, less than half of that rate: one conversion for two
+// values, but the same loads through registers, LDS writes and barriers for a sixth of the products.  (grouped.h's tiles of 128 x 128: 1550
+// and 600.  With fp32 instructions, 133 TFLOP/s in either, there is nothing to gain.)
 #pragma once
 #include "grouped.h"
 
