@@ -64,6 +64,7 @@ enum {
 
 #define SAGNN_F32 0  /* storage types of the calls that take one */
 #define SAGNN_BF16 1
+#define SAGNN_E4M3 2 /* rows of 8 bits (OCP e4m3, largest 448): rms_norm_fwd's output and what spmm_pack_rows_e4m3 reads */
 
 #define SAGNN_GEMM_FP32 0 /* fp32 operands, fp32 MFMA                          */
 #define SAGNN_GEMM_BF16 1 /* operands rounded to bfloat16 (RNE), fp32 accumulate */
@@ -690,6 +691,54 @@ int grad_global_norm(const sagnn_grad* h_grads, int32_t n, float* d_norm, void* 
 int grad_clip_norm(const sagnn_grad* h_grads, int32_t n, double max_norm, float* d_norm, void* d_ws, size_t ws_bytes,
                    void* stream);
 int grad_scale_to_norm(const sagnn_grad* h_grads, int32_t n, double max_norm, const float* d_norm, void* stream);
+
+/* ---------------------------------------------------------------------------------------
+ * Dropout with a residual:  Y[r, c] = R[r, c] + (kept(r, c) ? X[r, c] 65536 / (65536 - drop) : 0)      R may be NULL: 0
+ *
+ * drop: 65536ths of the values that fall, 0 to 65536 (all of them; 0: none).  The mask is stored nowhere.  It is a function of seed, offset, row and
+ * column alone, not of C, leading dimensions or the launch: ten rounds of Philox-4x32 (Salmon et al., 2011) under the key (seed's
+ * low word, high word) of the counter (c / 8, row0 + r, offset's low word, high word) give four words, and value c takes the
+ * (c % 8)-th half of them, low halves first; it is kept where that is >= drop.  So the ranks that share a matrix's rows get the whole matrix's mask by
+ * row0, the number of the call's first row, and the gradient is the same call on dY without R.  offset: the number of a step, say; d_offset (device, may be NULL) is
+ * added to it when the kernel runs, so that a captured graph whose steps count it up draws anew each time it is replayed.  row0 + m <= 2^32.
+ * A value that falls is 0 whatever it was.  One rounding to the type.  m x C matrices of dtype, any C up to SAGNN_NORM_MAX_WIDTH, any leading
+ * dimensions not below it, aligned to their element.  Y may be X or R, in the same place and with the same leading dimension, or lie beside them in wider rows;
+ * other overlaps are refused.
+ */
+int dropout_add(int32_t dtype, const void* d_X, int64_t ldx, const void* d_R, int64_t ldr, int64_t m, int32_t C, int32_t drop, uint64_t seed,
+                uint64_t offset, const uint64_t* d_offset, int64_t row0, void* d_Y, int64_t ldy, void* stream);
+
+/* ---------------------------------------------------------------------------------------
+ * Root-mean-square norm of a residual sum:
+ *
+ *   S = R + drop(X)                              R may be NULL (0), drop 0: S = X; dropout as in dropout_add, arguments too
+ *   rstd = 1 / sqrt(sum over a row of s^2 / C + eps),  Y = S rstd gamma[c]
+ *
+ * and backward, with G = dLoss/dY, D = the gradient that S has from elsewhere (may be NULL: 0), xh = S rstd:
+ *   dR = rstd (G gamma - xh sum(G gamma xh) / C) + D,  dX = drop(dR),  dgamma[c] = sum over rows of G xh
+ *
+ * out_type: dtype, or SAGNN_E4M3: Y holds rows of 8 bits (ldy in bytes) and d_scale one float for each, Y = d_scale[r] q:
+ * d_scale[r] = max |y| / 448, q = y / d_scale[r] rounded to nearest even.  A row whose scale would be below 2^-126 has scale 0 and zeros.  A NaN stays one.
+ * Y is made of the sum before that is rounded for S.  Squares are summed in 64 bits.  d_S, d_rstd: outputs, may be NULL (S for the next residual
+ * and both for the backward pass); gamma, rstd, dgamma are fp32, gamma may be NULL (1).  Backward d_S is an input (the X of the forward call where nothing was added or
+ * dropped); d_dX, d_dR, d_dgamma may be NULL each.  Sums of gradients are runs of fp32 of 384 terms at most, joined in 64 bits; their order is fixed: the same bits
+ * every time.  S may be X or R, Y too, dX and dR any operand, in the same place and with the same leading dimension, or lie
+ * beside it in wider rows; two outputs in one place and other overlaps are refused (rows of 8 bits: any).
+ * d_ws: rms_norm_bwd_workspace_bytes() bytes, 4-byte aligned, needed for dgamma only, NULL where that is 0.
+ */
+int rms_norm_fwd(int32_t dtype, const void* d_X, int64_t ldx, const void* d_R, int64_t ldr, int64_t m, int32_t C, const float* d_gamma, double eps,
+                 int32_t drop, uint64_t seed, uint64_t offset, const uint64_t* d_offset, int64_t row0, int32_t out_type, void* d_Y, int64_t ldy,
+                 float* d_scale, void* d_S, int64_t lds, float* d_rstd, void* stream);
+int rms_norm_bwd_workspace_bytes(int64_t m, int32_t C, size_t* bytes);
+int rms_norm_bwd(int32_t dtype, const void* d_S, int64_t lds, const void* d_G, int64_t ldg, const void* d_D, int64_t ldd, int64_t m, int32_t C,
+                 const float* d_gamma, const float* d_rstd, int32_t drop, uint64_t seed, uint64_t offset, const uint64_t* d_offset, int64_t row0,
+                 void* d_dX, int64_t lddx, void* d_dR, int64_t lddr, float* d_dgamma, void* d_ws, size_t ws_bytes, void* stream);
+
+/* Rows of 8 bits, gathered and widened: out[i, :] = d_scale[rows[i]] Q[rows[i], :], out_type SAGNN_F32 or SAGNN_BF16; Q is n x C bytes
+ * (ldq), d_scale n floats.  Step 2 of the path for rows that are kept or were sent in 8 bits: a quarter of the bytes of spmm_pack_rows are read.
+ * d_rows NULL: the first N rows.  A row number outside [0, n) gives zeros.  Any C up to SAGNN_NORM_MAX_WIDTH. */
+int spmm_pack_rows_e4m3(const void* d_Q, int64_t ldq, const float* d_scale, int64_t n, int32_t C, const int32_t* d_rows, int64_t N, int32_t out_type,
+                        void* d_out, int64_t ldo, void* stream);
 
 #ifdef __cplusplus
 }

@@ -14,7 +14,7 @@ import torch
 from . import build as _build
 
 ACT_IDENTITY, ACT_RELU, ACT_SILU = 0, 1, 2
-F32, BF16 = 0, 1
+F32, BF16, E4M3 = 0, 1, 2
 GEMM_FP32, GEMM_BF16, GEMM_FP32_BF16X3 = 0, 1, 2
 PLAN_VALIDATE, PLAN_OBLIVIOUS, PLAN_MULTIPASS = 1, 2, 4
 
@@ -30,6 +30,7 @@ EXPORTS = [
     "grouped_gemm_act", "grouped_gemm_bwd_workspace_bytes", "grouped_gemm_bwd",
     "group_norm_workspace_bytes", "group_norm_act_fwd", "group_norm_act_bwd",
     "grad_norm_workspace_bytes", "grad_global_norm", "grad_clip_norm", "grad_scale_to_norm",
+    "dropout_add", "rms_norm_fwd", "rms_norm_bwd_workspace_bytes", "rms_norm_bwd", "spmm_pack_rows_e4m3",
 ]
 
 
@@ -171,6 +172,12 @@ def lib():
         L.grad_global_norm.argtypes = [vp, i32, vp, vp, sz, vp]
         L.grad_clip_norm.argtypes = [vp, i32, f64, vp, vp, sz, vp]
         L.grad_scale_to_norm.argtypes = [vp, i32, f64, vp, vp]
+        u64 = ctypes.c_uint64
+        L.dropout_add.argtypes = [i32, vp, i64, vp, i64, i64, i32, i32, u64, u64, vp, i64, vp, i64, vp]
+        L.rms_norm_fwd.argtypes = [i32, vp, i64, vp, i64, i64, i32, vp, f64, i32, u64, u64, vp, i64, i32, vp, i64, vp, vp, i64, vp, vp]
+        L.rms_norm_bwd_workspace_bytes.argtypes = [i64, i32, psz]
+        L.rms_norm_bwd.argtypes = [i32, vp, i64, vp, i64, vp, i64, i64, i32, vp, vp, i32, u64, u64, vp, i64, vp, i64, vp, i64, vp, vp, sz, vp]
+        L.spmm_pack_rows_e4m3.argtypes = [vp, i64, vp, i64, i32, vp, i64, i32, vp, i64, vp]
         for name in EXPORTS[3:]:
             getattr(L, name).restype = ctypes.c_int
         _lib = L
@@ -185,7 +192,7 @@ _bound = None
 # the calls of a step: integers and pointers, and one double at most
 STEP_CALLS = ("spmm_plan_needed_rows", "spmm_pack_rows", "spmm_csr_tallskinny", "dense_gemm_act", "gcn_layer_fwd", "gcn_layer_bwd",
               "grouped_gemm_act", "grouped_gemm_bwd", "group_norm_act_fwd", "group_norm_act_bwd", "grad_global_norm", "grad_clip_norm",
-              "grad_scale_to_norm")
+              "grad_scale_to_norm", "dropout_add", "rms_norm_fwd", "rms_norm_bwd", "spmm_pack_rows_e4m3")
 _KIND = {ctypes.c_void_p: "p", ctypes.c_double: "d"}
 
 
@@ -925,3 +932,123 @@ def grad_clip_norm(grads, max_norm: float, norm=None, out=None):
     ws, need, norm = _grad_ws(grads, n)
     _check(_calls().grad_clip_norm(rows, n, max_norm, norm.data_ptr(), ws.data_ptr(), need, _stream()), "grad_clip_norm")
     return norm
+
+
+def _drop_args(p, seed, offset, row0):
+    """Dropout as the library takes it: 65536ths, and the offset's two parts."""
+    if not 0.0 <= p <= 1.0:
+        raise ValueError(f"p: expected a probability, got {p}")
+    d_offset = None
+    if isinstance(offset, torch.Tensor):
+        if offset.numel() != 1:
+            raise ValueError("offset: expected one element")
+        d_offset, offset = _dev(offset, torch.int64, "offset").data_ptr(), 0
+    if not (0 <= seed < 1 << 64 and 0 <= offset < 1 << 64):
+        raise ValueError("seed and offset: expected 64 bits without a sign")
+    return int(p * 65536 + 0.5), seed, offset, d_offset, row0
+
+
+def _here(t, name="X"):
+    """A tensor on the device whose current stream the call goes to: a launch elsewhere would neither wait for it nor be waited for."""
+    if t.is_cuda and t.get_device() != torch._C._cuda_getDevice():
+        raise ValueError(f"{name}: lies on {t.device}, which is not the current device")
+    return t
+
+
+def _like(t, X, name):
+    """A matrix like X, or None: its address and leading dimension."""
+    if t is None:
+        return None, 0
+    t = _here(_shape(_typed(t, name, X.dtype), X.shape, name), name)
+    return t.data_ptr(), _ld(t)
+
+
+def dropout_add(X, p: float, seed: int, offset=0, residual=None, row0: int = 0, out=None):
+    """Y = residual + dropout(X): each value is kept with probability 1 - p (to 2^-17) and divided by that, or 0.  The mask is a function of
+    seed, offset, row0 + row and column; the gradient for X is the same call on dY without a residual, with the same seed, offset and row0.
+    offset: an integer, or an int64 tensor of one element on the device that is read when the kernel runs (a captured graph counts it up).
+    row0: the first row's number in the whole matrix where ranks share its rows.  X: m x C, float32 or bfloat16; residual like it."""
+    X = _here(_typed(X, "X"))
+    m, c = X.shape
+    if out is None:
+        out = X.new_empty((m, c))
+    r, ldr = _like(residual, X, "residual")
+    y, ldy = _like(out, X, "out")
+    _check(_calls().dropout_add(_DTYPE[X.dtype], X.data_ptr(), _ld(X), r, ldr, m, c, *_drop_args(p, seed, offset, row0), y, ldy, _stream()), "dropout_add")
+    return out
+
+
+def _gamma(gamma, X):
+    return None if gamma is None else _shape(_dev(gamma, torch.float32, "gamma"), X.shape[1:], "gamma").data_ptr()
+
+
+def _rms_norm(X, gamma, residual, eps, p, seed, offset, row0, kind, out, scale, out_sum):
+    X = _here(X)
+    m, c = X.shape
+    added = residual is not None or p > 0.0
+    if not added and out_sum is not None:
+        raise ValueError("out_sum: nothing is added or dropped, the sum is X")
+    S = None if not added else X.new_empty((m, c)) if out_sum is None else out_sum
+    rstd = X.new_empty(m, dtype=torch.float32)
+    r, ldr = _like(residual, X, "residual")
+    s, lds = _like(S, X, "out_sum")
+    _check(_calls().rms_norm_fwd(_DTYPE[X.dtype], X.data_ptr(), _ld(X), r, ldr, m, c, _gamma(gamma, X), eps, *_drop_args(p, seed, offset, row0),
+                                 kind, out.data_ptr(), _ld(out), _ptr(scale), s, lds, rstd.data_ptr(), _stream()), "rms_norm_fwd")
+    return S if added else X, rstd
+
+
+def rms_norm(X, gamma=None, residual=None, eps: float = 1e-6, p: float = 0.0, seed: int = 0, offset=0, row0: int = 0, out=None, out_sum=None):
+    """Root-mean-square norm of the rows of S = residual + dropout(X) (dropout_add's p, seed, offset, row0): Y = S rstd gamma,
+    rstd = (mean(S^2) + eps)^-1/2.  X: m x C, float32 or bfloat16, residual like it; gamma: C, float32.  Returns (Y, S, rstd), S being X itself
+    where nothing is added or dropped, rstd float32; out_sum may be the residual, which is updated in place then."""
+    X = _typed(X, "X")
+    out = X.new_empty(X.shape) if out is None else _shape(_typed(out, "out", X.dtype), X.shape, "out")
+    S, rstd = _rms_norm(X, gamma, residual, eps, p, seed, offset, row0, _DTYPE[X.dtype], out, None, out_sum)
+    return out, S, rstd
+
+
+def rms_norm_e4m3(X, gamma=None, residual=None, eps: float = 1e-6, p: float = 0.0, seed: int = 0, offset=0, row0: int = 0, out_sum=None):
+    """rms_norm with rows of 8 bits: Y[r, :] = scale[r] Q[r, :], Q torch.float8_e4m3fn, scale float32.  Returns (Q, scale, S, rstd).
+    spmm_pack_rows_e4m3 reads them."""
+    X = _typed(X, "X")
+    Q, scale = X.new_empty(X.shape, dtype=torch.float8_e4m3fn), X.new_empty(X.shape[0], dtype=torch.float32)
+    S, rstd = _rms_norm(X, gamma, residual, eps, p, seed, offset, row0, E4M3, Q, scale, out_sum)
+    return Q, scale, S, rstd
+
+
+def rms_norm_bwd(S, G, rstd, gamma=None, grad_sum=None, p: float = 0.0, seed: int = 0, offset=0, row0: int = 0, want_dx=True, want_dgamma=True):
+    """Gradients of rms_norm for G = dLoss/dY, with the S and rstd that it returned; grad_sum: the gradient that S has from elsewhere (the
+    next residual).  Returns (dX, dR, dgamma): dX = dropout(dR), or dR itself where nothing was dropped; None for what is not wanted."""
+    S = _here(_typed(S, "S"), "S")
+    m, c = S.shape
+    g, ldg = _like(G, S, "G")
+    if g is None:
+        raise ValueError("G is needed")
+    d, ldd = _like(grad_sum, S, "grad_sum")
+    _shape(_dev(rstd, torch.float32, "rstd"), (m,), "rstd")
+    drop = _drop_args(p, seed, offset, row0)
+    dR = S.new_empty((m, c))
+    dX = S.new_empty((m, c)) if want_dx and drop[0] else None
+    dgamma = S.new_empty(c, dtype=torch.float32) if want_dgamma else None
+    need = _bytes_of("rms_norm_bwd_workspace_bytes", m, c) if want_dgamma else 0
+    ws = S.new_empty(need, dtype=torch.uint8) if need else None
+    _check(_calls().rms_norm_bwd(_DTYPE[S.dtype], S.data_ptr(), _ld(S), g, ldg, d, ldd, m, c, _gamma(gamma, S), rstd.data_ptr(), *drop, _ptr(dX), c,
+                                 dR.data_ptr(), c, _ptr(dgamma), _ptr(ws), need, _stream()), "rms_norm_bwd")
+    return (dX if drop[0] else dR) if want_dx else None, dR, dgamma
+
+
+def spmm_pack_rows_e4m3(Q, scale, rows=None, dtype=torch.float32, out=None):
+    """out[i, :] = scale[rows[i]] Q[rows[i], :] for rows of 8 bits (rms_norm_e4m3's), widened to float32 or bfloat16; rows: int32, None: all of
+    them.  A row number out of range gives zeros."""
+    Q = _here(_typed(Q, "Q", torch.float8_e4m3fn), "Q")
+    n, c = Q.shape
+    _shape(_dev(scale, torch.float32, "scale"), (n,), "scale")
+    if rows is not None and _dev(rows, torch.int32, "rows").dim() != 1:
+        raise ValueError("rows: expected a vector")
+    N = n if rows is None else rows.numel()
+    if out is None:
+        out = Q.new_empty((N, c), dtype=dtype)
+    out = _shape(_typed(out, "out"), (N, c), "out")
+    _check(_calls().spmm_pack_rows_e4m3(Q.data_ptr(), _ld(Q), scale.data_ptr(), n, c, _ptr(rows), N, _DTYPE[out.dtype], out.data_ptr(), _ld(out),
+                                        _stream()), "spmm_pack_rows_e4m3")
+    return out

@@ -37,6 +37,18 @@ inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 // Workgroups of `threads` along a launch's x: the runtime counts threads there in 32 bits, and more than they hold are not
 // started, without an error
 constexpr int64_t most_blocks(int threads) { return ((int64_t(1) << 32) - 1) / threads; }
+// Whether an output of m rows lies over an operand otherwise than in its own place: rows of the same length apart may be each other's, or
+// columns beside each other
+inline bool tangled(const void* out, int64_t ldo, const void* in, int64_t ldi, int64_t m, int32_t C, uintptr_t size) {
+  if (m == 0) return false;
+  const uintptr_t o = reinterpret_cast<uintptr_t>(out), i = reinterpret_cast<uintptr_t>(in);
+  const uintptr_t o1 = o + ((uintptr_t)(m - 1) * ldo + C) * size, i1 = i + ((uintptr_t)(m - 1) * ldi + C) * size;
+  if (o1 <= i || i1 <= o || (o == i && (ldo == ldi || m == 1))) return false;
+  if (ldo != ldi || m == 1) return true;
+  const uintptr_t apart = (o > i ? o - i : i - o) % ((uintptr_t)ldo * size);
+  return apart < C * size || (uintptr_t)ldo * size - apart < C * size;
+}
+inline bool aligned_to(const void* p, uintptr_t bytes) { return (reinterpret_cast<uintptr_t>(p) & (bytes - 1)) == 0; }
 
 // --- SpMM workspace geometry (host and device agree through these) -----------------------
 // Chunks of the nonzero-splitting schedule: about T entries each, T a multiple of 16.  Long enough that what a

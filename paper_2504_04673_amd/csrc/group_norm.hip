@@ -1046,19 +1046,6 @@ bool valid(int32_t dtype, const int32_t* d_seg, int32_t n_seg, int64_t m, int32_
          groups <= SAGNN_NORM_MAX_GROUPS && C % groups == 0 && (int64_t)n_seg * groups <= INT32_MAX && act >= SAGNN_ACT_IDENTITY && act <= SAGNN_ACT_SILU &&
          (d_seg || m % n_seg == 0);
 }
-// Whether an output of m rows lies over an operand otherwise than in its own place: rows of the same length apart may be each other's, or
-// columns beside each other
-bool tangled(const void* out, int64_t ldo, const void* in, int64_t ldi, int64_t m, int32_t C, uintptr_t size) {
-  if (m == 0) return false;
-  const uintptr_t o = reinterpret_cast<uintptr_t>(out), i = reinterpret_cast<uintptr_t>(in);
-  const uintptr_t o1 = o + ((uintptr_t)(m - 1) * ldo + C) * size, i1 = i + ((uintptr_t)(m - 1) * ldi + C) * size;
-  if (o1 <= i || i1 <= o || (o == i && (ldo == ldi || m == 1))) return false;
-  if (ldo != ldi || m == 1) return true;
-  const uintptr_t apart = (o > i ? o - i : i - o) % ((uintptr_t)ldo * size);
-  return apart < C * size || (uintptr_t)ldo * size - apart < C * size;
-}
-bool aligned_to(const void* p, uintptr_t bytes) { return (reinterpret_cast<uintptr_t>(p) & (bytes - 1)) == 0; }
-
 }  // namespace
 }  // namespace sagnn
 
