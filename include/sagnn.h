@@ -740,6 +740,33 @@ int rms_norm_bwd(int32_t dtype, const void* d_S, int64_t lds, const void* d_G, i
 int spmm_pack_rows_e4m3(const void* d_Q, int64_t ldq, const float* d_scale, int64_t n, int32_t C, const int32_t* d_rows, int64_t N, int32_t out_type,
                         void* d_out, int64_t ldo, void* stream);
 
+/* ---------------------------------------------------------------------------------------
+ * Softmax cross entropy over the classes of a linear layer, the logits not kept.  With Z = H W + bias (m x n_classes, nowhere in memory):
+ *
+ *   lse[r] = log(sum over classes of exp(Z[r, c])),  loss[r] = lse[r] - Z[r, labels[r]]
+ *
+ * and backward, with g[r] = grad_all * (d_grad ? d_grad[r] : 1) = dLoss/d(loss[r]), P[r, c] = g[r] (exp(Z[r, c] - lse[r]) - [c == labels[r]]):
+ *   dH = P W^T,  dW = H^T P,  dbias[c] = sum over rows of P[r, c]
+ *
+ * H is m x kdim (ldh), W is kdim x n_classes (ldw), or with transW = 1 n_classes x kdim, a table of the classes' vectors.  d_bias (n_classes) may be NULL.
+ * A label outside [0, n_classes) says that the row has none: its loss is 0, its row of dH zeros, and it is no part of dW and dbias, whatever its H holds; its lse is that of the formula.
+ * dtype: type of H, W, dH and dW; bias, loss, lse, grad and dbias are fp32.  dW is dense and laid out like W.  prec: as in grouped_gemm_act.  Sums are fp32 or more, cut into runs as
+ * there, their order fixed: the same bits every time.  Backward the classes are taken in pieces; a piece's P is rounded to dtype once, ahead of
+ * its products (bfloat16: each term of dH and dW by 2^-8 of itself at most, which their own rounding exceeds; dbias is summed of what is not
+ * rounded).  Infinite and NaN logits give what the formula gives: a bias of -inf takes a class out.
+ * Any kdim up to SAGNN_GROUPED_MAX_WIDTH, n_classes up to SAGNN_XENT_MAX_CLASSES, any leading dimensions not below the width, tensors aligned to their element; rows that begin on 16
+ * bytes are read faster.  d_dH, d_dW, d_dbias may be NULL each.  Outputs must not overlap inputs or each other.  Nothing is waited for.
+ * d_ws: softmax_xent_workspace_bytes() bytes, 16-byte aligned; NULL where that is 0 (forward, few classes).
+ */
+#define SAGNN_XENT_MAX_CLASSES 16777216
+int softmax_xent_workspace_bytes(int32_t dtype, int64_t m, int32_t kdim, int32_t n_classes, int32_t prec, int32_t backward, size_t* bytes);
+int softmax_xent_fwd(int32_t dtype, const void* d_H, int64_t ldh, const void* d_W, int64_t ldw, int32_t transW, const float* d_bias,
+                     const int32_t* d_labels, int64_t m, int32_t kdim, int32_t n_classes, int32_t prec, float* d_loss, float* d_lse, void* d_ws,
+                     size_t ws_bytes, void* stream);
+int softmax_xent_bwd(int32_t dtype, const void* d_H, int64_t ldh, const void* d_W, int64_t ldw, int32_t transW, const float* d_bias,
+                     const int32_t* d_labels, const float* d_lse, const float* d_grad, double grad_all, int64_t m, int32_t kdim, int32_t n_classes,
+                     int32_t prec, void* d_dH, int64_t lddh, void* d_dW, float* d_dbias, void* d_ws, size_t ws_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

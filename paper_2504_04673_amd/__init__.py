@@ -12,6 +12,6 @@ from .binding import (  # noqa: F401
     ColBlocks, spmm_split_colblocks, spmm_stage_loop, spmm_volume_stats, spmm_csr_transpose,
     spmm_perm_from_labels, spmm_csr_permute_symmetric,
     grouped_gemm_act, grouped_gemm_bwd, group_norm_act, group_norm_act_bwd, grad_global_norm, grad_clip_norm,
-    dropout_add, rms_norm, rms_norm_e4m3, rms_norm_bwd, spmm_pack_rows_e4m3,
+    dropout_add, rms_norm, rms_norm_e4m3, rms_norm_bwd, spmm_pack_rows_e4m3, softmax_xent, softmax_xent_bwd,
     ACT_IDENTITY, ACT_RELU, ACT_SILU, GEMM_FP32, GEMM_BF16, GEMM_FP32_BF16X3, PLAN_VALIDATE, PLAN_OBLIVIOUS, PLAN_MULTIPASS,
 )

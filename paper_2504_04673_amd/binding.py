@@ -31,6 +31,7 @@ EXPORTS = [
     "group_norm_workspace_bytes", "group_norm_act_fwd", "group_norm_act_bwd",
     "grad_norm_workspace_bytes", "grad_global_norm", "grad_clip_norm", "grad_scale_to_norm",
     "dropout_add", "rms_norm_fwd", "rms_norm_bwd_workspace_bytes", "rms_norm_bwd", "spmm_pack_rows_e4m3",
+    "softmax_xent_workspace_bytes", "softmax_xent_fwd", "softmax_xent_bwd",
 ]
 
 
@@ -178,6 +179,9 @@ def lib():
         L.rms_norm_bwd_workspace_bytes.argtypes = [i64, i32, psz]
         L.rms_norm_bwd.argtypes = [i32, vp, i64, vp, i64, vp, i64, i64, i32, vp, vp, i32, u64, u64, vp, i64, vp, i64, vp, i64, vp, vp, sz, vp]
         L.spmm_pack_rows_e4m3.argtypes = [vp, i64, vp, i64, i32, vp, i64, i32, vp, i64, vp]
+        L.softmax_xent_workspace_bytes.argtypes = [i32, i64, i32, i32, i32, i32, psz]
+        L.softmax_xent_fwd.argtypes = [i32, vp, i64, vp, i64, i32, vp, vp, i64, i32, i32, i32, vp, vp, vp, sz, vp]
+        L.softmax_xent_bwd.argtypes = [i32, vp, i64, vp, i64, i32, vp, vp, vp, vp, f64, i64, i32, i32, i32, vp, i64, vp, vp, vp, sz, vp]
         for name in EXPORTS[3:]:
             getattr(L, name).restype = ctypes.c_int
         _lib = L
@@ -192,7 +196,8 @@ _bound = None
 # the calls of a step: integers and pointers, and one double at most
 STEP_CALLS = ("spmm_plan_needed_rows", "spmm_pack_rows", "spmm_csr_tallskinny", "dense_gemm_act", "gcn_layer_fwd", "gcn_layer_bwd",
               "grouped_gemm_act", "grouped_gemm_bwd", "group_norm_act_fwd", "group_norm_act_bwd", "grad_global_norm", "grad_clip_norm",
-              "grad_scale_to_norm", "dropout_add", "rms_norm_fwd", "rms_norm_bwd", "spmm_pack_rows_e4m3")
+              "grad_scale_to_norm", "dropout_add", "rms_norm_fwd", "rms_norm_bwd", "spmm_pack_rows_e4m3",
+              "softmax_xent_fwd", "softmax_xent_bwd")
 _KIND = {ctypes.c_void_p: "p", ctypes.c_double: "d"}
 
 
@@ -1052,3 +1057,47 @@ def spmm_pack_rows_e4m3(Q, scale, rows=None, dtype=torch.float32, out=None):
     _check(_calls().spmm_pack_rows_e4m3(Q.data_ptr(), _ld(Q), scale.data_ptr(), n, c, _ptr(rows), N, _DTYPE[out.dtype], out.data_ptr(), _ld(out),
                                         _stream()), "spmm_pack_rows_e4m3")
     return out
+
+
+def _xent_args(H, W, labels, bias, transW):
+    """What both directions check: H's rows and width, the classes, and the pointers that lead both calls."""
+    H = _here(_typed(H, "H"), "H")
+    W = _here(_typed(W, "W", H.dtype), "W")
+    m, k = H.shape
+    n = W.shape[0 if transW else 1]
+    _shape(W, (n, k) if transW else (k, n), "W")
+    _shape(_here(_dev(labels, torch.int32, "labels"), "labels"), (m,), "labels")
+    if bias is not None:
+        _shape(_here(_dev(bias, torch.float32, "bias"), "bias"), (n,), "bias")
+    return m, k, n, (_DTYPE[H.dtype], H.data_ptr(), _ld(H), W.data_ptr(), _ld(W), int(transW), _ptr(bias), labels.data_ptr())
+
+
+def softmax_xent(H, W, labels, bias=None, transW=False, prec=GEMM_FP32):
+    """Softmax cross entropy over the classes of the logits H W + bias, which are not kept: loss[r] = lse[r] - logit[r, labels[r]], lse the
+    logarithm of the row's sum of exponentials.  H: m x kdim, W: kdim x classes (classes x kdim with transW), float32 or bfloat16; labels: m, int32,
+    one outside the classes (-1, say) for a row that has none: loss 0; bias: classes, float32.  Returns (loss, lse), float32."""
+    m, k, n, args = _xent_args(H, W, labels, bias, transW)
+    need = _bytes_of("softmax_xent_workspace_bytes", args[0], m, k, n, prec, 0)
+    ws = H.new_empty(need, dtype=torch.uint8) if need else None
+    loss = H.new_empty(m, dtype=torch.float32)
+    lse = torch.empty_like(loss)
+    _check(_calls().softmax_xent_fwd(*args, m, k, n, prec, loss.data_ptr(), lse.data_ptr(), _ptr(ws), need, _stream()), "softmax_xent_fwd")
+    return loss, lse
+
+
+def softmax_xent_bwd(H, W, labels, lse, grad=1.0, bias=None, transW=False, prec=GEMM_FP32, want_dh=True, want_dw=True):
+    """Gradients of softmax_xent with the lse that it returned; grad: dLoss/d(loss), a number for all rows (one over how many labels there are, for
+    their mean) or m, float32.  Returns (dH, dW, dbias), the first two in H's type, dbias float32; None for what is not wanted or not there."""
+    m, k, n, args = _xent_args(H, W, labels, bias, transW)
+    _shape(_here(_dev(lse, torch.float32, "lse"), "lse"), (m,), "lse")
+    rows = isinstance(grad, torch.Tensor)
+    if rows:
+        _shape(_here(_dev(grad, torch.float32, "grad"), "grad"), (m,), "grad")
+    need = _bytes_of("softmax_xent_workspace_bytes", args[0], m, k, n, prec, 1)
+    ws = H.new_empty(need, dtype=torch.uint8)
+    dH = H.new_empty((m, k)) if want_dh else None
+    dW = H.new_empty(W.shape) if want_dw else None
+    dbias = None if bias is None or not want_dw else torch.empty_like(bias)
+    _check(_calls().softmax_xent_bwd(*args, lse.data_ptr(), grad.data_ptr() if rows else None, 1.0 if rows else grad, m, k, n, prec, _ptr(dH), k, _ptr(dW),
+                                     _ptr(dbias), ws.data_ptr(), need, _stream()), "softmax_xent_bwd")
+    return dH, dW, dbias

@@ -624,6 +624,11 @@ inline int grouped_tile_cols(int tile) {
   return cols[tile];
 }
 
+// What a tile costs: how well it feeds the matrix cores (rates of 8192 x 4096 x 4096, 128 x 128 = 1), and how much of the summed index its
+// beginning and end are worth.  Small tiles are several to a CU, which hides both; the large ones are alone there.
+struct TileCost { double rate, ends; };
+TileCost tile_cost(int32_t dtype, int32_t prec, int tile);
+
 // a product of `blocks` workgroups; per operand mode (and storage type)
 #define SAGNN_GROUPED_MODE(name)                                                                                       \
   int grouped_##name(const GroupedArgs& a, int tile, bool trans_w, int64_t blocks, hipStream_t s);                      \

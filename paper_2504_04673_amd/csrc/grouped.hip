@@ -3,6 +3,15 @@
 #include "grouped.h"
 
 namespace sagnn {
+
+TileCost tile_cost(int32_t dtype, int32_t prec, int tile) {
+  static constexpr TileCost fp32[kGroupedTiles] = {{1., 48}, {.98, 24}, {.91, 12}, {.95, 8}, {.85, 16}, {0, 0}, {0, 0}, {0, 0}, {.78, 200}};
+  static constexpr TileCost rounded[kGroupedTiles] = {{1., 128}, {.76, 128}, {.62, 32}, {.49, 8}, {.25, 16}, {0, 0}, {1.08, 160}, {1.08, 160}, {.18, 200}};
+  static constexpr TileCost split[kGroupedTiles] = {{1., 48}, {.87, 24}, {.67, 8}, {.76, 8}, {.65, 8}, {0, 0}, {1.18, 54}, {1.18, 54}, {.46, 200}};
+  static constexpr TileCost bf16[kGroupedTiles] = {{1., 128}, {.81, 128}, {.66, 32}, {.66, 32}, {.39, 32}, {1.69, 200}, {0, 0}, {0, 0}, {.26, 200}};
+  return dtype == SAGNN_BF16 ? bf16[tile] : prec == SAGNN_GEMM_FP32 ? fp32[tile] : prec == SAGNN_GEMM_BF16 ? rounded[tile] : split[tile];
+}
+
 namespace {
 
 // dW[g] = the sum of its parts, chunks ascending, in 64 bits (there may be thousands); a group of one part was written by the product itself.
@@ -49,17 +58,6 @@ constexpr int64_t kStagedLd = 1 << 20;     // (offsets inside a tile of 256 rows
 
 // Which tiles an operation can have: through registers any (staged: fp32 tensors), straight into LDS bfloat16 ones
 enum { kAny = 0, kDirect = 1, kStaged = 2 };
-
-// What a tile costs: how well it feeds the matrix cores (rates of 8192 x 4096 x 4096, 128 x 128 = 1), and how much of the summed index its
-// beginning and end are worth.  Small tiles are several to a CU, which hides both; the large ones are alone there.
-struct TileCost { double rate, ends; };
-TileCost tile_cost(int32_t dtype, int32_t prec, int tile) {
-  static constexpr TileCost fp32[kGroupedTiles] = {{1., 48}, {.98, 24}, {.91, 12}, {.95, 8}, {.85, 16}, {0, 0}, {0, 0}, {0, 0}, {.78, 200}};
-  static constexpr TileCost rounded[kGroupedTiles] = {{1., 128}, {.76, 128}, {.62, 32}, {.49, 8}, {.25, 16}, {0, 0}, {1.08, 160}, {1.08, 160}, {.18, 200}};
-  static constexpr TileCost split[kGroupedTiles] = {{1., 48}, {.87, 24}, {.67, 8}, {.76, 8}, {.65, 8}, {0, 0}, {1.18, 54}, {1.18, 54}, {.46, 200}};
-  static constexpr TileCost bf16[kGroupedTiles] = {{1., 128}, {.81, 128}, {.66, 32}, {.66, 32}, {.39, 32}, {1.69, 200}, {0, 0}, {0, 0}, {.26, 200}};
-  return dtype == SAGNN_BF16 ? bf16[tile] : prec == SAGNN_GEMM_FP32 ? fp32[tile] : prec == SAGNN_GEMM_BF16 ? rounded[tile] : split[tile];
-}
 
 // The tile with the least cost: `rows` rows in `parts` ragged parts by `cols` columns, `times` over, `sum` of the summed index.  Tiles are
 // whole, so each part leaves half a tile empty; a launch lasts as long as its fullest CU; and a tile alone on a CU waits for its

@@ -1,0 +1,363 @@
+// Softmax cross entropy over the classes of a linear layer: entry points, plans, and what stands between the products of xent.h.
+//
+// Forward, tiles of the logits live in registers: each leaves a maximum and a sum for each of its rows, and a second launch joins a row's.
+// Backward the classes are cut into pieces.  A piece's logits are multiplied anew, become P = g (softmax - one-hot) in the epilogue and are stored
+// in the operands' type; dH takes P W^T of piece after piece, dW and the bias's gradient are the piece's own.  2 m k n operations forward
+// and 6 backward, of which 2 are the price of a memory of one piece.
+// Rows without a label are no part of any of it: a vertex in three has one, often one in a hundred.  Those with one are listed first and their
+// features copied, so that the products are as long as the list, and a NaN in a row that has none meets nothing.
+#include <initializer_list>
+#include <type_traits>
+
+#include "xent.h"
+
+namespace sagnn {
+namespace {
+
+constexpr int kListBlocks = 4096;                 // of rows, at most
+constexpr int kListThreads = 256;
+// Bytes of P at a time, about: a piece that the memory-side cache holds would be smaller, but dH's sums are read and written once for each.
+constexpr int64_t kPieceBytes = int64_t(512) << 20;
+// The widest piece: sums of dH stay one run of bfloat16 products (kRunRounded), and a workspace's rows below 2^16 bytes
+constexpr int32_t kPieceMost = 16384;
+
+__device__ __forceinline__ bool known(int32_t label, int32_t classes) { return label >= 0 && label < classes; }
+
+// Rows with a label in each block of `each` rows
+__global__ __launch_bounds__(kListThreads) void label_count_kernel(const int32_t* __restrict__ labels, int64_t m, int64_t each, int32_t classes,
+                                                                   int32_t* __restrict__ counts) {
+  __shared__ int32_t room[kListThreads / 64];
+  const int64_t end = (blockIdx.x + 1) * each < m ? (blockIdx.x + 1) * each : m;
+  int32_t n = 0;
+  for (int64_t r = blockIdx.x * each + threadIdx.x; r < end; r += kListThreads) n += known(labels[r], classes);
+  for (int d = 1; d < 64; d *= 2) n += __shfl_xor(n, d);
+  if ((threadIdx.x & 63) == 0) room[threadIdx.x >> 6] = n;
+  __syncthreads();
+  if (threadIdx.x == 0) counts[blockIdx.x] = room[0] + room[1] + room[2] + room[3];
+}
+
+// map[i] = row of the i-th label; H's rows one behind the other in rows of ldc values (zeros behind the k there are); zeros in dH's rows without
+// one.  bounds = {0, how many}.
+template <typename T>
+__global__ __launch_bounds__(kListThreads) void label_list_kernel(const int32_t* __restrict__ labels, int64_t m, int64_t each, int32_t classes,
+                                                                  const int32_t* __restrict__ counts, int32_t* __restrict__ map, int32_t* __restrict__ bounds,
+                                                                  const T* __restrict__ H, int64_t ldh, int32_t k, T* __restrict__ rows, int64_t ldc,
+                                                                  T* __restrict__ dH, int64_t lddh) {
+  __shared__ int32_t room[kListThreads / 64];
+  __shared__ int32_t place[kListThreads];          // of a row of the round: its number in the list, or -1
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  int32_t before = 0;
+  for (int b = threadIdx.x; b < (int)blockIdx.x; b += kListThreads) before += counts[b];
+  for (int d = 1; d < 64; d *= 2) before += __shfl_xor(before, d);
+  if (lane == 0) room[wave] = before;
+  __syncthreads();
+  before = room[0] + room[1] + room[2] + room[3];
+  const int64_t end = (blockIdx.x + 1) * each < m ? (blockIdx.x + 1) * each : m;
+  for (int64_t r0 = blockIdx.x * each; r0 < end; r0 += kListThreads) {
+    const int64_t r = r0 + threadIdx.x;
+    const bool in = r < end && known(labels[r], classes);
+    const uint64_t all = __ballot(in);
+    __syncthreads();
+    if (lane == 0) room[wave] = __popcll(all);
+    __syncthreads();
+    int32_t at = before + __popcll(all & ((1ull << lane) - 1));
+    for (int w = 0; w < wave; ++w) at += room[w];
+    place[threadIdx.x] = in ? at : -1;
+    if (in) map[at] = (int32_t)r;
+    before += room[0] + room[1] + room[2] + room[3];
+    __syncthreads();
+    // a wavefront a row
+    const int n = end - r0 < kListThreads ? (int)(end - r0) : kListThreads;
+    for (int i = wave; i < n; i += kListThreads / 64) {
+      const int32_t to = place[i];
+      if (to >= 0)
+        for (int c = lane; c < ldc; c += 64) rows[to * ldc + c] = c < k ? H[(r0 + i) * ldh + c] : (T)0.f;
+      else if (dH)
+        for (int c = lane; c < k; c += 64) dH[(r0 + i) * lddh + c] = (T)0.f;
+    }
+  }
+  if (blockIdx.x == gridDim.x - 1 && threadIdx.x == 0) {
+    bounds[0] = 0;
+    bounds[1] = before;
+  }
+}
+
+// lse and loss of a row from its tiles of columns: 64 rows a workgroup, four threads to each
+__global__ __launch_bounds__(256) void xent_join_kernel(const float2* __restrict__ stats, const float* __restrict__ z_label, int64_t m, int32_t tiles,
+                                                        const int32_t* __restrict__ labels, int32_t classes, float* __restrict__ loss, float* __restrict__ lse) {
+  __shared__ float2 room[256];
+  const int64_t r = (int64_t)blockIdx.x * 64 + (threadIdx.x & 63);
+  float most = -INFINITY, sum = 0.f;
+  if (r < m)
+    for (int t = threadIdx.x >> 6; t < tiles; t += 4) {
+      const float2 p = stats[t * m + r];
+      join_stats(most, sum, p.x, p.y);
+    }
+  room[threadIdx.x] = make_float2(most, sum);
+  __syncthreads();
+  if (threadIdx.x >= 64 || r >= m) return;
+#pragma unroll
+  for (int t = 1; t < 4; ++t) join_stats(most, sum, room[t * 64 + threadIdx.x].x, room[t * 64 + threadIdx.x].y);
+  const float l = lse_of(most, sum);
+  lse[r] = l;
+  loss[r] = known(labels[r], classes) ? l - z_label[r] : 0.f;
+}
+
+// The bias's gradient: sums over the row tiles, in 64 bits
+__global__ __launch_bounds__(256) void xent_bias_kernel(const float* __restrict__ parts, const int32_t* __restrict__ bounds, int32_t tile_rows, int32_t cols,
+                                                        float* __restrict__ dbias) {
+  __shared__ double room[256];
+  const int c = blockIdx.x * 16 + (threadIdx.x & 15);
+  const int32_t tiles = (bounds[1] + tile_rows - 1) / tile_rows;
+  double sum = 0.;
+  if (c < cols)
+#pragma unroll 4
+    for (int t = threadIdx.x >> 4; t < tiles; t += 16) sum += (double)parts[(int64_t)t * cols + c];
+  room[threadIdx.x] = sum;
+  __syncthreads();
+  if (threadIdx.x < 16 && c < cols) {
+#pragma unroll
+    for (int p = 1; p < 16; ++p) sum += room[p * 16 + threadIdx.x];
+    dbias[c] = (float)sum;
+  }
+}
+
+// A piece's dW from fp32 into its place
+template <typename T>
+__global__ __launch_bounds__(256) void xent_weights_kernel(const float* __restrict__ from, int64_t rows, int32_t cols, T* __restrict__ to, int64_t ldt) {
+  const int64_t fours = (cols + 3) / 4, all = rows * fours;
+  for (int64_t i = blockIdx.x * 256ll + threadIdx.x; i < all; i += gridDim.x * 256ll) {
+    const int64_t r = i / fours;
+    const int c = (int)(i - r * fours) * 4;
+    float y[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) y[e] = c + e < cols ? from[r * cols + c + e] : 0.f;
+    store_four(to + r * ldt + c, y, cols - c);
+  }
+}
+
+// ------------------------------------------------------------------------------------------
+
+bool valid(int32_t dtype, int32_t transW, int64_t m, int32_t kdim, int32_t classes, int32_t prec) {
+  return (dtype == SAGNN_F32 || (dtype == SAGNN_BF16 && prec == SAGNN_GEMM_FP32)) && prec >= SAGNN_GEMM_FP32 && prec <= SAGNN_GEMM_FP32_BF16X3 &&
+         !(transW & ~1) && m >= 0 && m <= INT32_MAX && kdim >= 1 && kdim <= SAGNN_GROUPED_MAX_WIDTH && classes >= 1 && classes <= SAGNN_XENT_MAX_CLASSES &&
+         ceil_div(m, 32) * ceil_div(classes, 32) <= INT32_MAX;
+}
+
+int32_t products(int32_t dtype, int32_t prec) { return dtype == SAGNN_BF16 ? SAGNN_GEMM_BF16 : prec; }
+
+// Tile of a product: m rows by cols, `sum` deep
+int pick_tile(int32_t dtype, int32_t prec, int64_t m, int64_t cols, int64_t sum) {
+  int best = kTile128;
+  double least = 1e300;
+  for (int tile : {kTile128, kTile128x64, kTile32x128}) {
+    const TileCost c = tile_cost(dtype, prec, tile);
+    const int64_t h = grouped_tile_rows(tile), w = grouped_tile_cols(tile), tiles = ceil_div(m, h) * ceil_div(cols, w);
+    const double turns = tiles <= 256 ? 1.25 : tiles < 4 * 256 ? (double)ceil_div(tiles, 256) : tiles / 256.;
+    const double cost = turns * h * w * (sum + c.ends) / c.rate;
+    if (cost < least) {
+      least = cost;
+      best = tile;
+    }
+  }
+  return best;
+}
+
+int launch(const XentArgs& args, int32_t dtype, int32_t prec, int tile, bool trans_w, hipStream_t s) {
+  XentArgs a = args;
+  a.run = grouped_run(products(dtype, prec), a.sum);
+  a.col_tiles = (int32_t)ceil_div(a.cols, grouped_tile_cols(tile));
+  if (dtype == SAGNN_BF16) return xent_bf16(a, tile, trans_w, s);
+  return prec == SAGNN_GEMM_FP32 ? xent_fp32(a, tile, trans_w, s) : prec == SAGNN_GEMM_BF16 ? xent_fp32_bf16(a, tile, trans_w, s) : xent_fp32_bf16x3(a, tile, trans_w, s);
+}
+
+struct Room {
+  size_t off = 0;
+  size_t take(size_t bytes) { const size_t o = off; off += round_up(bytes, 256); return o; }
+};
+
+struct FwdPlan { int tile; int32_t col_tiles; size_t stats, z_label, total; };
+FwdPlan fwd_plan(int32_t dtype, int32_t prec, int64_t m, int32_t kdim, int32_t classes) {
+  FwdPlan p{};
+  p.tile = pick_tile(dtype, prec, m, classes, kdim);
+  p.col_tiles = (int32_t)ceil_div(classes, grouped_tile_cols(p.tile));
+  if (p.col_tiles > 1) {
+    Room room;
+    p.stats = room.take((size_t)m * p.col_tiles * sizeof(float2));
+    p.z_label = room.take((size_t)m * sizeof(float));
+    p.total = room.off;
+  }
+  return p;
+}
+
+struct BwdPlan {
+  int32_t piece, pieces;                     // classes of a piece
+  int64_t ldp, ldc;                          // of P, of the listed rows
+  size_t map, bounds, counts, rows, P, sums, weights, parts, bias, parts_bytes, total;
+};
+BwdPlan bwd_plan(int32_t dtype, int32_t prec, int64_t m, int32_t kdim, int32_t classes) {
+  BwdPlan p{};
+  const int64_t size = dtype == SAGNN_BF16 ? 2 : 4, rows = m > 0 ? m : 1;
+  int64_t most = kPieceBytes / (rows * size) / 256 * 256;
+  most = most < 256 ? 256 : most > kPieceMost ? kPieceMost : most;
+  p.pieces = (int32_t)ceil_div(classes, most);
+  p.piece = p.pieces == 1 ? classes : (int32_t)round_up((size_t)ceil_div(classes, p.pieces), 256);
+  p.pieces = (int32_t)ceil_div(classes, p.piece);
+  p.ldp = (int64_t)round_up((size_t)p.piece, 8);
+  p.ldc = (int64_t)round_up((size_t)kdim, 8);
+  // dW's products, in either order, of a whole piece and of the last (which may be cut into more parts)
+  for (int32_t n : {p.piece, classes - (p.pieces - 1) * p.piece}) {
+    size_t one = 0, two = 0;
+    grouped_gemm_bwd_workspace_bytes(m, 1, kdim, n, &one);
+    grouped_gemm_bwd_workspace_bytes(m, 1, n, kdim, &two);
+    p.parts_bytes = one > p.parts_bytes ? one : p.parts_bytes;
+    p.parts_bytes = two > p.parts_bytes ? two : p.parts_bytes;
+  }
+  Room room;
+  p.map = room.take((size_t)rows * 4);
+  p.bounds = room.take(8);
+  p.counts = room.take(kListBlocks * 4);
+  p.rows = room.take((size_t)rows * p.ldc * size);
+  p.P = room.take((size_t)rows * p.ldp * size);
+  p.sums = room.take(p.pieces > 1 ? (size_t)rows * kdim * 4 : 0);
+  p.weights = room.take((size_t)p.piece * kdim * 4);
+  p.parts = room.take(p.parts_bytes);
+  p.bias = room.take((size_t)ceil_div(rows, 32) * p.piece * 4);
+  p.total = room.off;
+  return p;
+}
+
+template <typename T>
+int list_labels(const BwdPlan& p, char* ws, const int32_t* labels, int64_t m, int32_t classes, const void* H, int64_t ldh, int32_t k, void* dH, int64_t lddh,
+                hipStream_t s) {
+  int64_t each = ceil_div(m, kListBlocks);
+  if (each < kListThreads) each = kListThreads;
+  const uint32_t blocks = (uint32_t)ceil_div(m > 0 ? m : 1, each);
+  int32_t *counts = (int32_t*)(ws + p.counts), *map = (int32_t*)(ws + p.map), *bounds = (int32_t*)(ws + p.bounds);
+  label_count_kernel<<<dim3(blocks), kListThreads, 0, s>>>(labels, m, each, classes, counts);
+  SAGNN_LAUNCH_CHECK();
+  label_list_kernel<T><<<dim3(blocks), kListThreads, 0, s>>>(labels, m, each, classes, counts, map, bounds, (const T*)H, ldh, k, (T*)(ws + p.rows), p.ldc,
+                                                            (T*)dH, lddh);
+  SAGNN_LAUNCH_CHECK();
+  return SAGNN_OK;
+}
+
+bool element_aligned(const void* p, int32_t dtype) { return aligned_to(p, dtype == SAGNN_BF16 ? 2 : 4); }
+// Two ranges of bytes have nothing in common
+bool clear_of(const void* p, size_t bytes_p, const void* q, size_t bytes_q) {
+  const uintptr_t a = reinterpret_cast<uintptr_t>(p), b = reinterpret_cast<uintptr_t>(q);
+  return !p || !q || !bytes_p || !bytes_q || a + bytes_p <= b || b + bytes_q <= a;
+}
+size_t reach(int64_t rows, int64_t ld, int64_t cols, size_t size) { return rows > 0 ? ((size_t)(rows - 1) * ld + cols) * size : 0; }
+
+}  // namespace
+}  // namespace sagnn
+
+SAGNN_EXPORT int softmax_xent_workspace_bytes(int32_t dtype, int64_t m, int32_t kdim, int32_t n_classes, int32_t prec, int32_t backward, size_t* bytes) {
+  using namespace sagnn;
+  if (!bytes || !valid(dtype, 0, m, kdim, n_classes, prec) || (backward & ~1)) return SAGNN_EINVAL;
+  *bytes = backward ? bwd_plan(dtype, prec, m, kdim, n_classes).total : fwd_plan(dtype, prec, m, kdim, n_classes).total;
+  return SAGNN_OK;
+}
+
+SAGNN_EXPORT int softmax_xent_fwd(int32_t dtype, const void* d_H, int64_t ldh, const void* d_W, int64_t ldw, int32_t transW, const float* d_bias,
+                                  const int32_t* d_labels, int64_t m, int32_t kdim, int32_t n_classes, int32_t prec, float* d_loss, float* d_lse,
+                                  void* d_ws, size_t ws_bytes, void* stream) {
+  using namespace sagnn;
+  if (!valid(dtype, transW, m, kdim, n_classes, prec) || ldh < kdim || ldw < (transW ? kdim : n_classes)) return SAGNN_EINVAL;
+  if (m == 0) return SAGNN_OK;
+  if (!d_H || !d_W || !d_labels || !d_loss || !d_lse || !element_aligned(d_H, dtype) || !element_aligned(d_W, dtype) || !aligned_to(d_bias, 4) ||
+      !aligned_to(d_labels, 4) || !aligned_to(d_loss, 4) || !aligned_to(d_lse, 4) || !aligned_to(d_ws, 16))
+    return SAGNN_EINVAL;
+  const size_t size = dtype == SAGNN_BF16 ? 2 : 4, h = reach(m, ldh, kdim, size), w = transW ? reach(n_classes, ldw, kdim, size) : reach(kdim, ldw, n_classes, size);
+  for (const float* out : {d_loss, d_lse})
+    if (!clear_of(out, m * 4, d_H, h) || !clear_of(out, m * 4, d_W, w) || !clear_of(out, m * 4, d_labels, m * 4) || !clear_of(out, m * 4, d_bias, (size_t)n_classes * 4))
+      return SAGNN_EINVAL;
+  if (!clear_of(d_loss, m * 4, d_lse, m * 4)) return SAGNN_EINVAL;
+  const FwdPlan p = fwd_plan(dtype, prec, m, kdim, n_classes);
+  if (p.total > 0 && !d_ws) return SAGNN_EINVAL;
+  if (ws_bytes < p.total) return SAGNN_ECAPACITY;
+  XentArgs a{};
+  a.X = d_H; a.ldx = ldh; a.W = d_W; a.ldw = ldw; a.m = m; a.cols = n_classes; a.sum = kdim; a.mode = kXentStats; a.bias = d_bias; a.labels = d_labels;
+  a.classes = n_classes; a.loss = d_loss; a.lse = d_lse;
+  if (p.total > 0) {
+    a.stats = (float2*)((char*)d_ws + p.stats);
+    a.z_label = (float*)((char*)d_ws + p.z_label);
+  }
+  hipStream_t s = (hipStream_t)stream;
+  const int rc = launch(a, dtype, prec, p.tile, transW != 0, s);
+  if (rc != SAGNN_OK || p.total == 0) return rc;
+  xent_join_kernel<<<dim3((uint32_t)ceil_div(m, 64)), 256, 0, s>>>(a.stats, a.z_label, m, p.col_tiles, d_labels, n_classes, d_loss, d_lse);
+  SAGNN_LAUNCH_CHECK();
+  return SAGNN_OK;
+}
+
+SAGNN_EXPORT int softmax_xent_bwd(int32_t dtype, const void* d_H, int64_t ldh, const void* d_W, int64_t ldw, int32_t transW, const float* d_bias,
+                                  const int32_t* d_labels, const float* d_lse, const float* d_grad, double grad_all, int64_t m, int32_t kdim,
+                                  int32_t n_classes, int32_t prec, void* d_dH, int64_t lddh, void* d_dW, float* d_dbias, void* d_ws, size_t ws_bytes,
+                                  void* stream) {
+  using namespace sagnn;
+  if (!valid(dtype, transW, m, kdim, n_classes, prec) || ldh < kdim || ldw < (transW ? kdim : n_classes) || (d_dH && lddh < kdim)) return SAGNN_EINVAL;
+  if (!d_W || (m > 0 && (!d_H || !d_labels || !d_lse)) || !element_aligned(d_H, dtype) || !element_aligned(d_W, dtype) || !aligned_to(d_bias, 4) ||
+      !aligned_to(d_labels, 4) || !aligned_to(d_lse, 4) || !aligned_to(d_grad, 4) || !element_aligned(d_dH, dtype) || !element_aligned(d_dW, dtype) ||
+      !aligned_to(d_dbias, 4) || !aligned_to(d_ws, 16))
+    return SAGNN_EINVAL;
+  const size_t size = dtype == SAGNN_BF16 ? 2 : 4;
+  {
+    const struct { const void* p; size_t bytes; } in[] = {{d_H, reach(m, ldh, kdim, size)}, {d_W, transW ? reach(n_classes, ldw, kdim, size) : reach(kdim, ldw, n_classes, size)},
+                                                          {d_bias, (size_t)n_classes * 4}, {d_labels, (size_t)m * 4}, {d_lse, (size_t)m * 4}, {d_grad, (size_t)m * 4}};
+    const struct { const void* p; size_t bytes; } out[] = {{d_dH, reach(m, lddh, kdim, size)}, {d_dW, (size_t)n_classes * kdim * size}, {d_dbias, (size_t)n_classes * 4}};
+    for (int o = 0; o < 3; ++o) {
+      for (const auto& i : in)
+        if (!clear_of(out[o].p, out[o].bytes, i.p, i.bytes)) return SAGNN_EINVAL;
+      for (int q = 0; q < o; ++q)
+        if (!clear_of(out[o].p, out[o].bytes, out[q].p, out[q].bytes)) return SAGNN_EINVAL;
+    }
+  }
+  const BwdPlan p = bwd_plan(dtype, prec, m, kdim, n_classes);
+  if (!d_ws) return SAGNN_EINVAL;
+  if (ws_bytes < p.total) return SAGNN_ECAPACITY;
+  char* ws = (char*)d_ws;
+  hipStream_t s = (hipStream_t)stream;
+  int rc = dtype == SAGNN_BF16 ? list_labels<__bf16>(p, ws, d_labels, m, n_classes, d_H, ldh, kdim, d_dH, lddh, s)
+                               : list_labels<float>(p, ws, d_labels, m, n_classes, d_H, ldh, kdim, d_dH, lddh, s);
+  const int32_t* bounds = (const int32_t*)(ws + p.bounds);
+  for (int32_t at = 0; at < n_classes && rc == SAGNN_OK; at += p.piece) {
+    const int32_t n = n_classes - at < p.piece ? n_classes - at : p.piece;
+    XentArgs a{};
+    a.X = ws + p.rows; a.ldx = p.ldc; a.W = (const char*)d_W + (size_t)at * (transW ? ldw : 1) * size; a.ldw = ldw; a.m = m; a.count = bounds + 1;
+    a.cols = n; a.sum = kdim; a.mode = kXentGrads; a.bias = d_bias ? d_bias + at : nullptr; a.labels = d_labels; a.class0 = at; a.classes = n_classes;
+    a.map = (const int32_t*)(ws + p.map); a.row_lse = d_lse; a.grad = d_grad; a.grad_all = (float)grad_all; a.P = ws + p.P; a.ldp = p.ldp;
+    a.stored = (int32_t)round_up((size_t)n, 8); a.bias_parts = d_dbias ? (float*)(ws + p.bias) : nullptr;
+    const int tile = pick_tile(dtype, prec, m, n, kdim);
+    if (m > 0) rc = launch(a, dtype, prec, tile, transW != 0, s);
+    if (rc == SAGNN_OK && d_dbias) {
+      xent_bias_kernel<<<dim3((uint32_t)ceil_div(n, 16)), 256, 0, s>>>(a.bias_parts, bounds, grouped_tile_rows(tile), n, d_dbias + at);
+      SAGNN_LAUNCH_CHECK();
+    }
+    if (rc == SAGNN_OK && d_dH && m > 0) {
+      XentArgs b{};
+      b.X = a.P; b.ldx = p.ldp; b.W = a.W; b.ldw = ldw; b.m = m; b.count = a.count; b.cols = kdim; b.sum = n; b.mode = kXentRows; b.map = a.map;
+      b.sums = (float*)(ws + p.sums); b.add = at > 0; b.last = at + n == n_classes; b.out = d_dH; b.ldo = lddh;
+      rc = launch(b, dtype, prec, pick_tile(dtype, prec, m, kdim, n), transW == 0, s);
+    }
+    if (rc == SAGNN_OK && d_dW) {
+      // (fp32 weights whose piece lies in one place are written there)
+      const bool there = dtype == SAGNN_F32 && (transW || p.pieces == 1);
+      float* dW = there ? (float*)d_dW + (size_t)at * (transW ? kdim : 1) : (float*)(ws + p.weights);
+      rc = transW ? grouped_gemm_bwd(dtype, a.P, p.ldp, nullptr, 0, 0, bounds, 1, m, n, kdim, prec, a.X, p.ldc, nullptr, 0, nullptr, 0, dW, ws + p.parts, p.parts_bytes, stream)
+                  : grouped_gemm_bwd(dtype, a.X, p.ldc, nullptr, 0, 0, bounds, 1, m, kdim, n, prec, a.P, p.ldp, nullptr, 0, nullptr, 0, dW, ws + p.parts, p.parts_bytes, stream);
+      if (rc == SAGNN_OK && !there) {
+        const int64_t rows = transW ? n : kdim, ldt = transW ? kdim : n_classes;
+        const int32_t cols = transW ? kdim : n;
+        const int64_t blocks = ceil_div(rows * ceil_div(cols, 4), 256);
+        const dim3 grid((uint32_t)(blocks < 4096 ? blocks : 4096));
+        const size_t first = (size_t)at * (transW ? kdim : 1);
+        if (dtype == SAGNN_BF16) xent_weights_kernel<__bf16><<<grid, 256, 0, s>>>(dW, rows, cols, (__bf16*)d_dW + first, ldt);
+        else xent_weights_kernel<float><<<grid, 256, 0, s>>>(dW, rows, cols, (float*)d_dW + first, ldt);
+        SAGNN_LAUNCH_CHECK();
+      }
+    }
+  }
+  return rc;
+}

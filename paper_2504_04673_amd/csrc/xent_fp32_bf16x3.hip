@@ -1,0 +1,6 @@
+// The products of xent.h: fp32 tensors, operands as three bfloat16 terms.
+#include "xent.h"
+
+namespace sagnn {
+int xent_fp32_bf16x3(const XentArgs& a, int tile, bool trans_w, hipStream_t s) { return xent_small<float, SAGNN_GEMM_FP32_BF16X3, 32>(a, tile, trans_w, s); }
+}  // namespace sagnn
