@@ -23,7 +23,7 @@ SOURCES = ["api.hip", "pack.hip", "plan.hip", "spmm.hip", "spmm_flat.hip", "spmm
            "grouped_fp32_bf16x3.hip", "grouped_bf16.hip", "group_norm.hip", "grad_norm.hip", "row_norm.hip", "xent.hip", "xent_fp32.hip", "xent_fp32_bf16.hip",
            "xent_fp32_bf16x3.hip", "xent_bf16.hip"]
 HEADERS = [os.path.join(CSRC, "common.h"), os.path.join(CSRC, "rowload.h"), os.path.join(CSRC, "rows.h"), os.path.join(CSRC, "gemm.h"),
-           os.path.join(CSRC, "gemm_nn.h"), os.path.join(CSRC, "grouped.h"), os.path.join(CSRC, "grouped_direct.h"), os.path.join(CSRC, "grouped_staged.h"), os.path.join(CSRC, "xent.h"), os.path.join(INCLUDE, "sagnn.h")]
+           os.path.join(CSRC, "gemm_nn.h"), os.path.join(CSRC, "grouped.h"), os.path.join(CSRC, "grouped_direct.h"), os.path.join(CSRC, "grouped_staged.h"), os.path.join(CSRC, "xent.h"), os.path.join(CSRC, "xent_staged.h"), os.path.join(INCLUDE, "sagnn.h")]
 
 HIPCC_FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-fvisibility=hidden",

@@ -93,14 +93,15 @@ struct DirectOperand {
   }
 };
 
-// acc[tm][tn] = (A B)^T tile by tile, over all steps: a lane holds four neighbouring columns of one row at a time.
+// acc[tm][tn] = (A B)^T tile by tile, over all steps: a lane holds four neighbouring columns of one row at a time.  total_b: B's length of the
+// summed index where A's, padded with zeros, is longer.
 //
 // Two instructions' worth of operands: one is multiplied while the other is read.  What a wavefront issues besides its products
 // stands singly between them: a row of LDS reads or loads holds up the wavefront, and with it the matrix core (8192^3 in
 // wavefronts of 128 x 128: 1950 cycles a step that way, 1450 this way; its products take 1024).
 template <bool TRA, bool TRB, int WM, int WN, int TM, int TN>
 __device__ __forceinline__ void direct_product(const __bf16* A, int64_t lda, int rows, const __bf16* B, int64_t ldb, int cols, int64_t total,
-                                               char* smem, floatx16 (&acc)[TM][TN]) {
+                                               char* smem, floatx16 (&acc)[TM][TN], int64_t total_b = 0) {
   constexpr int BM = WM * TM * 32, BN = WN * TN * 32;
   using OA = DirectOperand<TRA, BM, WM * WN>;
   using OB = DirectOperand<TRB, BN, WM * WN>;
@@ -118,7 +119,7 @@ __device__ __forceinline__ void direct_product(const __bf16* A, int64_t lda, int
   OA oa;
   OB ob;
   oa.init(A, lda, rows, (int)total, lane, wave);
-  ob.init(B, ldb, cols, (int)total, lane, wave);
+  ob.init(B, ldb, cols, (int)(total_b ? total_b : total), lane, wave);
   const uint32_t lds_a = (uint32_t)reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) char*)smem), lds_b = lds_a + OA::kBytes;
   const char* ring_a = smem;
   const char* ring_b = smem + OA::kBytes;

@@ -17,6 +17,8 @@ struct XentArgs {
   int64_t m;                                 // rows at most
   const int32_t* count;                      // how many there are, on the device; NULL: m
   int32_t cols, sum, run, mode;
+  int32_t padded;                            // X's columns with zeros behind `sum`
+  bool wide;                                 // results in rows that begin on 16 bytes, whole eights of them
   int32_t col_tiles; int64_t first;          // of the launch
   // stats, grads
   const float* bias; const int32_t* labels;  // bias of the first column on, or NULL
@@ -27,9 +29,11 @@ struct XentArgs {
   const int32_t* map; const float* row_lse; const float* grad; float grad_all;
   void* P; int64_t ldp; int32_t stored;      // columns that are stored, zeros behind `cols`
   float* bias_parts;                         // row tiles x cols, or NULL
-  // rows
-  float* sums; bool add, last;               // between pieces of the classes: m x cols
-  void* out; int64_t ldo;                    // rows by `map`
+  // rows: `splits` shares of the summed index, `share` of it each, with sums of their own, splits x m x cols, added to from piece to piece of the
+  // classes; or, of one piece and one share, the result, rows by `map`
+  int32_t splits, share;
+  float* sums; bool add;
+  void* out; int64_t ldo;
 };
 
 // LDS of the epilogues: maxima, sums and the label's z of every row; sums of every column
@@ -46,13 +50,14 @@ struct SmallProduct {
   static constexpr int kOperands = TileShape<PREC, false, WM * TM * 32, BK>::kBytes + TileShape<PREC, TRB, WN * TN * 32, BK>::kBytes;
   static constexpr int kLds = kOperands > xent_lds(WM, WN, TM, TN) ? kOperands : xent_lds(WM, WN, TM, TN);
   static constexpr bool kTransW = !TRB;
-  static __device__ __forceinline__ void run(const S* A, int64_t lda, int rows, const S* B, int64_t ldb, int cols, int64_t sum, char* smem,
-                                             floatx16 (&acc)[TM][TN], int32_t run) {
-    tile_product<S, PREC, false, TRB, WM, WN, TM, TN, BK, LONG>(A, lda, rows, B, ldb, cols, sum, smem, acc, run);
+  static constexpr bool kTurned = false;
+  static __device__ __forceinline__ void run(const XentArgs& a, const S* A, int rows, const S* B, int cols, int sum, int, char* smem, floatx16 (&acc)[TM][TN]) {
+    tile_product<S, PREC, false, TRB, WM, WN, TM, TN, BK, LONG>(A, a.ldx, rows, B, a.ldw, cols, sum, smem, acc, a.run);
   }
 };
 
-// Class weights of e^x: x log2(e) is rounded, so the result is good to (1 + |x|) 2^-23
+// e^x.  (x - y is formed first, exact where it matters: y's product taken off in one operation saves one of five, and overflows
+// for the type's lowest values, which serve as masks.)
 __device__ __forceinline__ float exp_of(float x) { return __builtin_amdgcn_exp2f(x * 1.44269504088896341f); }
 
 // log of a sum of exponentials that is kept as (what is taken off, sum).  Nothing is taken off an infinite maximum: a row of -inf has a sum
@@ -66,53 +71,70 @@ __device__ __forceinline__ void join_stats(float& most, float& sum, float most2,
 }
 __device__ __forceinline__ float lse_of(float most, float sum) { return shift_of(most) + logf(sum); }
 
-// z = acc + bias in place, -inf behind the last column
+// Column, in the tile, of a lane's value v of its tile tn
 template <typename C>
-__device__ __forceinline__ void add_bias(const XentArgs& a, int64_t c0, int cols, floatx16 (&acc)[C::TM][C::TN], float behind) {
+__device__ __forceinline__ int column_of(int tn, int v) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  return ((wave % C::WN) * C::TN + tn) * 32 + 8 * (v / 4) + 4 * (lane >> 5) + v % 4;
+}
+// Biases of a lane's columns
+template <typename C, bool WHOLE>
+__device__ __forceinline__ void load_bias(const XentArgs& a, int64_t c0, int cols, float (&b)[C::TN][16]) {
 #pragma unroll
   for (int tn = 0; tn < C::TN; ++tn)
 #pragma unroll
-    for (int v = 0; v < 16; ++v) {
-      const int c = ((wave % C::WN) * C::TN + tn) * 32 + 8 * (v / 4) + 4 * (lane >> 5) + v % 4;
-      const bool in = c < cols;
-      const float b = a.bias && in ? a.bias[c0 + c] : 0.f;
+    for (int v = 0; v < 16; v += 4) {
+      const int c = column_of<C>(tn, v);
+      float x[4] = {0.f, 0.f, 0.f, 0.f};
+      if (a.bias) {
+        if (WHOLE || c + 4 <= cols) __builtin_memcpy(x, reinterpret_cast<const Four<float>*>(a.bias + c0 + c), 16);
+        else
 #pragma unroll
-      for (int tm = 0; tm < C::TM; ++tm) acc[tm][tn][v] = in ? acc[tm][tn][v] + b : behind;
+          for (int i = 0; i < 3; ++i)
+            if (c + i < cols) x[i] = a.bias[c0 + c + i];
+      }
+#pragma unroll
+      for (int i = 0; i < 4; ++i) b[tn][v + i] = x[i];
     }
 }
 
-template <typename C>
+// The epilogues take a lane's sums row by row and leave them as they are.  WHOLE: a tile without ends of the matrix, which asks nothing for each value.
+template <typename C, bool WHOLE>
 __device__ __forceinline__ void xent_stats(const XentArgs& a, int64_t r0, int32_t col, int64_t c0, int rows, int cols, char* smem,
-                                           floatx16 (&acc)[C::TM][C::TN]) {
+                                           const floatx16 (&acc)[C::TM][C::TN]) {
   constexpr int BM = C::WM * C::TM * 32;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  add_bias<C>(a, c0, cols, acc, -INFINITY);
+  float b[C::TN][16];
+  load_bias<C, WHOLE>(a, c0, cols, b);
   float2* place = reinterpret_cast<float2*>(smem);           // [WN][BM]
   float* z_label = reinterpret_cast<float*>(place + C::WN * BM);
 #pragma unroll
   for (int tm = 0; tm < C::TM; ++tm) {
     const int r = ((wave / C::WN) * C::TM + tm) * 32 + (lane & 31);
-    const int64_t label = (r < rows ? (int64_t)a.labels[r0 + r] : -1) - c0;          // column of this tile, or outside it
-    float most = -INFINITY;
+    // the label as a number of this lane's columns
+    const int64_t label = (WHOLE || r < rows ? (int64_t)a.labels[r0 + r] : -1) - c0, far = label - column_of<C>(0, 0);
+    const int near = far >= 0 && far < C::TN * 32 && label < cols ? (int)far : -1;
+    auto z = [&](int tn, int v) { return WHOLE || column_of<C>(tn, v) < cols ? acc[tm][tn][v] + b[tn][v] : -INFINITY; };
+    float most = -INFINITY, own = 0.f;
+    bool here = false;
 #pragma unroll
     for (int tn = 0; tn < C::TN; ++tn)
 #pragma unroll
       for (int v = 0; v < 16; ++v) {
-        const int c = ((wave % C::WN) * C::TN + tn) * 32 + 8 * (v / 4) + 4 * (lane >> 5) + v % 4;
-        most = fmaxf(most, acc[tm][tn][v]);
-        if (c == label && c < cols) {
-          if (a.stats) a.z_label[r0 + r] = acc[tm][tn][v];
-          else z_label[r] = acc[tm][tn][v];
-        }
+        const float x = z(tn, v);
+        most = fmaxf(most, x);
+        const bool hit = near == tn * 32 + 8 * (v / 4) + v % 4;
+        own = hit ? x : own;
+        here |= hit;
       }
+    if (here) (a.stats ? a.z_label + r0 : z_label)[r] = own;
     most = fmaxf(most, __shfl_xor(most, 32));
     const float s = shift_of(most);
     float sum = 0.f;
 #pragma unroll
     for (int tn = 0; tn < C::TN; ++tn)
 #pragma unroll
-      for (int v = 0; v < 16; ++v) sum += exp_of(acc[tm][tn][v] - s);
+      for (int v = 0; v < 16; ++v) sum += exp_of(z(tn, v) - s);
     sum += __shfl_xor(sum, 32);
     if (lane < 32) place[(wave % C::WN) * BM + r] = make_float2(most, sum);
   }
@@ -144,71 +166,128 @@ __device__ __forceinline__ float sixteen_sum(float x) {
   return x;
 }
 
+// Bfloat16 results of a large tile -> memory: every wavefront turns its own through LDS (rows of 16 bytes more than they have, against the
+// banks), so that a lane stores eight neighbouring columns.
 template <typename C>
+struct Turn {
+  static constexpr int kPitch = C::TN * 32 * 2 + 16, kPerRow = C::TN * 4;
+  static __device__ __forceinline__ char* own(char* smem) { return smem + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) * (C::TM * 32 * kPitch); }
+  static __device__ __forceinline__ void put(char* smem, int tm, int tn, int v, const float (&y)[4]) {
+    const int lane = threadIdx.x & 63;
+    bf16x4 w;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) w[i] = (__bf16)y[i];
+    *reinterpret_cast<bf16x4*>(own(smem) + (tm * 32 + (lane & 31)) * kPitch + (tn * 32 + 2 * v + 4 * (lane >> 5)) * 2) = w;
+  }
+  // at(row): offset of a row; `cols` whole eights
+  template <typename F>
+  static __device__ __forceinline__ void store(char* smem, __bf16* out, int rows, int cols, F at) {
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int ra = (wave / C::WN) * C::TM * 32, rb = (wave % C::WN) * C::TN * 32;
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");      // (its own writes only)
+#pragma unroll 4
+    for (int u = lane; u < C::TM * 32 * kPerRow; u += 64) {
+      const int r = u / kPerRow, c = u % kPerRow * 8;
+      if (ra + r < rows && rb + c < cols)
+        *reinterpret_cast<bf16x8*>(out + at(ra + r) + rb + c) = *reinterpret_cast<const bf16x8*>(own(smem) + r * kPitch + c * 2);
+    }
+  }
+};
+
+template <typename C, bool WHOLE>
 __device__ __forceinline__ void xent_grads(const XentArgs& a, int64_t r0, int64_t row_tile, int64_t c0, int rows, int cols, char* smem,
-                                           floatx16 (&acc)[C::TM][C::TN]) {
+                                           const floatx16 (&acc)[C::TM][C::TN]) {
+  using S = typename C::S;
   constexpr int BN = C::WN * C::TN * 32;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  add_bias<C>(a, c0, cols, acc, -INFINITY);
+  float b[C::TN][16], sums[C::TN][16];
+  load_bias<C, WHOLE>(a, c0, cols, b);
+#pragma unroll
+  for (int tn = 0; tn < C::TN; ++tn)
+#pragma unroll
+    for (int v = 0; v < 16; ++v) sums[tn][v] = 0.f;
+  S* P = reinterpret_cast<S*>(a.P) + r0 * a.ldp + c0;
+  const int stored = a.stored - c0 < BN ? (int)(a.stored - c0) : BN;
 #pragma unroll
   for (int tm = 0; tm < C::TM; ++tm) {
     const int r = ((wave / C::WN) * C::TM + tm) * 32 + (lane & 31);
-    const bool in = r < rows;
+    const bool in = WHOLE || r < rows;
     const int64_t row = in ? a.map[r0 + r] : 0;
     const float lse = in ? a.row_lse[row] : 0.f, g = in ? a.grad_all * (a.grad ? a.grad[row] : 1.f) : 0.f;
-    const int64_t label = in ? (int64_t)a.labels[row] - a.class0 - c0 : -1;
+    const int64_t far = (in ? (int64_t)a.labels[row] - a.class0 : -1) - c0 - column_of<C>(0, 0);
+    const int near = far >= 0 && far < C::TN * 32 ? (int)far : -1;
 #pragma unroll
     for (int tn = 0; tn < C::TN; ++tn)
 #pragma unroll
-      for (int v = 0; v < 16; ++v) {
-        const int c = ((wave % C::WN) * C::TN + tn) * 32 + 8 * (v / 4) + 4 * (lane >> 5) + v % 4;
-        const float p = exp_of(acc[tm][tn][v] - lse) - (c == label ? 1.f : 0.f);
-        acc[tm][tn][v] = in && c < cols ? p * g : 0.f;
+      for (int v = 0; v < 16; v += 4) {
+        float y[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          y[i] = exp_of(acc[tm][tn][v + i] + b[tn][v + i] - lse) * g - (near == tn * 32 + 2 * v + i ? g : 0.f);
+          if (!WHOLE) y[i] = in && column_of<C>(tn, v + i) < cols ? y[i] : 0.f;
+          sums[tn][v + i] += y[i];
+        }
+        if constexpr (C::kTurned) Turn<C>::put(smem, tm, tn, v, y);
+        else if (in) store_four(P + (int64_t)r * a.ldp + column_of<C>(tn, v), y, stored - column_of<C>(tn, v));
       }
   }
-  if (a.bias_parts) {                             // sums over the rows, of what is not rounded yet
-    float* place = reinterpret_cast<float*>(smem);           // [WM][2][BN]
+  if constexpr (C::kTurned) Turn<C>::store(smem, P, rows, stored, [&](int r) { return r * a.ldp; });
+  if (!a.bias_parts) return;
+  // sums over the rows, of what is not rounded
+  __syncthreads();
+  float* place = reinterpret_cast<float*>(smem);             // [WM][2][BN]
 #pragma unroll
-    for (int tn = 0; tn < C::TN; ++tn)
+  for (int tn = 0; tn < C::TN; ++tn)
 #pragma unroll
-      for (int v = 0; v < 16; ++v) {
-        float x = 0.f;
-#pragma unroll
-        for (int tm = 0; tm < C::TM; ++tm) x += acc[tm][tn][v];
-        x = sixteen_sum(x);
-        if ((lane & 15) == 0)
-          place[((wave / C::WN) * 2 + ((lane >> 4) & 1)) * BN + ((wave % C::WN) * C::TN + tn) * 32 + 8 * (v / 4) + 4 * (lane >> 5) + v % 4] = x;
-      }
-    __syncthreads();
-    for (int c = threadIdx.x; c < cols; c += C::kThreads) {
-      float x = 0.f;
-#pragma unroll
-      for (int w = 0; w < 2 * C::WM; ++w) x += place[w * BN + c];
-      a.bias_parts[row_tile * a.cols + c0 + c] = x;
+    for (int v = 0; v < 16; ++v) {
+      const float x = sixteen_sum(sums[tn][v]);
+      if ((lane & 15) == 0) place[((wave / C::WN) * 2 + ((lane >> 4) & 1)) * BN + column_of<C>(tn, v)] = x;
     }
-    __syncthreads();
+  __syncthreads();
+  for (int c = threadIdx.x; c < cols; c += C::kThreads) {
+    float x = 0.f;
+#pragma unroll
+    for (int w = 0; w < 2 * C::WM; ++w) x += place[w * BN + c];
+    a.bias_parts[row_tile * a.cols + c0 + c] = x;
   }
-  using S = typename C::S;
-  S* P = reinterpret_cast<S*>(a.P) + r0 * a.ldp + c0;
-  const int stored = a.stored - c0 < BN ? (int)(a.stored - c0) : BN;
-  tile_fours<C::WM, C::WN, C::TM, C::TN>(acc, [&](int r, int c, float (&y)[4]) {
-    if (r < rows) store_four(P + (int64_t)r * a.ldp + c, y, stored - c);
-  });
 }
 
 template <typename C>
-__device__ __forceinline__ void xent_rows(const XentArgs& a, int64_t r0, int64_t c0, int rows, int cols, floatx16 (&acc)[C::TM][C::TN]) {
+__device__ __forceinline__ void xent_rows(const XentArgs& a, int32_t split, int64_t r0, int64_t c0, int rows, int cols, char* smem, floatx16 (&acc)[C::TM][C::TN]) {
   using S = typename C::S;
-  float* sums = a.sums + r0 * a.cols + c0;
-  S* out = reinterpret_cast<S*>(a.out) + c0;
-  tile_fours<C::WM, C::WN, C::TM, C::TN>(acc, [&](int r, int c, float (&y)[4]) {
-    if (r >= rows) return;
-    if (a.add)
+  if (!a.sums) {
+    S* out = reinterpret_cast<S*>(a.out) + c0;
+    if constexpr (C::kTurned)
+      if (a.wide) {
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
-        if (c + i < cols) y[i] += sums[(int64_t)r * a.cols + c + i];
-    if (a.last) store_four(out + (int64_t)a.map[r0 + r] * a.ldo + c, y, cols - c);
-    else store_four(sums + (int64_t)r * a.cols + c, y, cols - c);
+        for (int i = 0; i < C::TM * C::TN * 4; ++i) {
+          const int tm = i / (C::TN * 4), tn = i / 4 % C::TN, v = i % 4 * 4;
+          const float y[4] = {acc[tm][tn][v], acc[tm][tn][v + 1], acc[tm][tn][v + 2], acc[tm][tn][v + 3]};
+          Turn<C>::put(smem, tm, tn, v, y);
+        }
+        Turn<C>::store(smem, out, rows, cols, [&](int r) { return (int64_t)a.map[r0 + r] * a.ldo; });
+        return;
+      }
+    tile_fours<C::WM, C::WN, C::TM, C::TN>(acc, [&](int r, int c, float (&y)[4]) { if (r < rows) store_four(out + (int64_t)a.map[r0 + r] * a.ldo + c, y, cols - c); });
+    return;
+  }
+  float* sums = a.sums + (split * a.m + r0) * a.cols + c0;
+  tile_fours<C::WM, C::WN, C::TM, C::TN>(acc, [&](int r, int c, float (&y)[4]) {
+    float* to = sums + (int64_t)r * a.cols + c;
+    if (r >= rows) return;
+    if (a.add) {
+      if (c + 4 <= cols) {
+        float x[4];
+        __builtin_memcpy(x, reinterpret_cast<const Four<float>*>(to), 16);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) y[i] += x[i];
+      } else {
+#pragma unroll
+        for (int i = 0; i < 3; ++i)
+          if (c + i < cols) y[i] += to[i];
+      }
+    }
+    store_four(to, y, cols - c);
   });
 }
 
@@ -219,22 +298,31 @@ __global__ __launch_bounds__(C::kThreads) void xent_kernel(const XentArgs a) {
   constexpr int BM = C::WM * C::TM * 32, BN = C::WN * C::TN * 32;
   __shared__ __attribute__((aligned(1024))) char smem[C::kLds];
   const int64_t m = a.count ? (*a.count < 0 ? 0 : *a.count > a.m ? a.m : *a.count) : a.m;
-  const int32_t row_tiles = (int32_t)((m + BM - 1) / BM);
-  const int64_t block = a.first + blockIdx.x, total = (int64_t)row_tiles * a.col_tiles;
+  const int32_t row_tiles = (int32_t)((m + BM - 1) / BM), tiles = row_tiles * a.col_tiles;
+  const int64_t block = a.first + blockIdx.x, total = (int64_t)tiles * a.splits;
   if (block >= total) return;
-  const int32_t id = xcd_run((int32_t)block, (int32_t)total), band = id / (kXentBand * a.col_tiles), in = id - band * kXentBand * a.col_tiles;
+  int32_t id = xcd_run((int32_t)block, (int32_t)total);
+  const int32_t split = id / tiles;
+  id -= split * tiles;
+  const int32_t band = id / (kXentBand * a.col_tiles), in = id - band * kXentBand * a.col_tiles;
   const int32_t high = row_tiles - band * kXentBand < kXentBand ? row_tiles - band * kXentBand : kXentBand;
   const int32_t row = band * kXentBand + in % high, col = in / high;
   const int64_t r0 = (int64_t)row * BM, c0 = (int64_t)col * BN;
   const int rows = (int)(m - r0 < BM ? m - r0 : BM), cols = (int)(a.cols - c0 < BN ? a.cols - c0 : BN);
+  const int32_t from = split * a.share, sum = a.sum - from < a.share ? a.sum - from : a.share, padded = a.sum - from <= a.share ? a.padded - from : a.share;
   using S = typename C::S;
   floatx16 acc[C::TM][C::TN];
-  C::run(reinterpret_cast<const S*>(a.X) + r0 * a.ldx, a.ldx, rows, reinterpret_cast<const S*>(a.W) + c0 * (C::kTransW ? a.ldw : 1), a.ldw, cols, a.sum,
-         smem, acc, a.run);
+  C::run(a, reinterpret_cast<const S*>(a.X) + r0 * a.ldx + from, rows,
+         reinterpret_cast<const S*>(a.W) + c0 * (C::kTransW ? a.ldw : 1) + (int64_t)from * (C::kTransW ? 1 : a.ldw), cols, sum, padded, smem, acc);
   __syncthreads();
-  if (a.mode == kXentStats) xent_stats<C>(a, r0, col, c0, rows, cols, smem, acc);
-  else if (a.mode == kXentGrads) xent_grads<C>(a, r0, row, c0, rows, cols, smem, acc);
-  else xent_rows<C>(a, r0, c0, rows, cols, acc);
+  const bool whole = rows == BM && cols == BN;
+  if (a.mode == kXentStats) {
+    if (whole) xent_stats<C, true>(a, r0, col, c0, rows, cols, smem, acc);
+    else xent_stats<C, false>(a, r0, col, c0, rows, cols, smem, acc);
+  } else if (a.mode == kXentGrads) {
+    if (whole) xent_grads<C, true>(a, r0, row, c0, rows, cols, smem, acc);
+    else xent_grads<C, false>(a, r0, row, c0, rows, cols, smem, acc);
+  } else xent_rows<C>(a, split, r0, c0, rows, cols, smem, acc);
 }
 
 #define SAGNN_XENT_MODE(name) int xent_##name(const XentArgs& a, int tile, bool trans_w, hipStream_t s);
@@ -246,7 +334,7 @@ SAGNN_XENT_MODE(bf16)
 
 template <typename C>
 int xent_launch(const XentArgs& args, hipStream_t s) {
-  const int64_t blocks = ceil_div(args.m, C::WM * C::TM * 32) * args.col_tiles, most = most_blocks(C::kThreads) / 8 * 8;
+  const int64_t blocks = ceil_div(args.m, C::WM * C::TM * 32) * args.col_tiles * args.splits, most = most_blocks(C::kThreads) / 8 * 8;
   XentArgs a = args;
   for (a.first = 0; a.first < blocks; a.first += most) {
     xent_kernel<C><<<dim3((uint32_t)(blocks - a.first < most ? blocks - a.first : most)), C::kThreads, 0, s>>>(a);
@@ -262,7 +350,7 @@ int xent_small_as(const XentArgs& a, int tile, hipStream_t s) {
 }
 template <typename S, int PREC, int BK>
 int xent_small(const XentArgs& a, int tile, bool trans_w, hipStream_t s) {
-  const bool several = a.sum > a.run;
+  const bool several = a.share > a.run;
   if (trans_w) return several ? xent_small_as<S, PREC, BK, false, true>(a, tile, s) : xent_small_as<S, PREC, BK, false, false>(a, tile, s);
   return several ? xent_small_as<S, PREC, BK, true, true>(a, tile, s) : xent_small_as<S, PREC, BK, true, false>(a, tile, s);
 }

@@ -9,6 +9,7 @@
 #include <initializer_list>
 #include <type_traits>
 
+#include "rows.h"
 #include "xent.h"
 
 namespace sagnn {
@@ -18,8 +19,9 @@ constexpr int kListBlocks = 4096;                 // of rows, at most
 constexpr int kListThreads = 256;
 // Bytes of P at a time, about: a piece that the memory-side cache holds would be smaller, but dH's sums are read and written once for each.
 constexpr int64_t kPieceBytes = int64_t(512) << 20;
-// The widest piece: sums of dH stay one run of bfloat16 products (kRunRounded), and a workspace's rows below 2^16 bytes
-constexpr int32_t kPieceMost = 16384;
+// Classes of a piece, and pieces, which dH's sums are added over in turn
+constexpr int64_t kSumBytes = int64_t(512) << 20;
+constexpr int32_t kPieceLeast = 1024, kPieceMost = 16384, kPiecesMost = 384;
 
 __device__ __forceinline__ bool known(int32_t label, int32_t classes) { return label >= 0 && label < classes; }
 
@@ -42,7 +44,7 @@ template <typename T>
 __global__ __launch_bounds__(kListThreads) void label_list_kernel(const int32_t* __restrict__ labels, int64_t m, int64_t each, int32_t classes,
                                                                   const int32_t* __restrict__ counts, int32_t* __restrict__ map, int32_t* __restrict__ bounds,
                                                                   const T* __restrict__ H, int64_t ldh, int32_t k, T* __restrict__ rows, int64_t ldc,
-                                                                  T* __restrict__ dH, int64_t lddh) {
+                                                                  T* __restrict__ dH, int64_t lddh, int lanes) {
   __shared__ int32_t room[kListThreads / 64];
   __shared__ int32_t place[kListThreads];          // of a row of the round: its number in the list, or -1
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -66,14 +68,17 @@ __global__ __launch_bounds__(kListThreads) void label_list_kernel(const int32_t*
     if (in) map[at] = (int32_t)r;
     before += room[0] + room[1] + room[2] + room[3];
     __syncthreads();
-    // a wavefront a row
-    const int n = end - r0 < kListThreads ? (int)(end - r0) : kListThreads;
-    for (int i = wave; i < n; i += kListThreads / 64) {
+    // `lanes` of them to a row
+    const int n = end - r0 < kListThreads ? (int)(end - r0) : kListThreads, own = threadIdx.x & (lanes - 1);
+    for (int i = threadIdx.x / lanes; i < n; i += kListThreads / lanes) {
       const int32_t to = place[i];
       if (to >= 0)
-        for (int c = lane; c < ldc; c += 64) rows[to * ldc + c] = c < k ? H[(r0 + i) * ldh + c] : (T)0.f;
+        for (int c = own * 8; c < ldc; c += lanes * 8) {
+          const auto w = load_eight(H + (r0 + i) * ldh + c, k - c);
+          *reinterpret_cast<TightRun<T, 8>*>(rows + to * ldc + c) = w;
+        }
       else if (dH)
-        for (int c = lane; c < k; c += 64) dH[(r0 + i) * lddh + c] = (T)0.f;
+        for (int c = own * 8; c < k; c += lanes * 8) store_eight(dH + (r0 + i) * lddh + c, {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f}, k - c);
     }
   }
   if (blockIdx.x == gridDim.x - 1 && threadIdx.x == 0) {
@@ -82,22 +87,24 @@ __global__ __launch_bounds__(kListThreads) void label_list_kernel(const int32_t*
   }
 }
 
-// lse and loss of a row from its tiles of columns: 64 rows a workgroup, four threads to each
+// lse and loss of a row from its tiles of columns: 2^log_rows rows a workgroup, its other threads share their tiles
 __global__ __launch_bounds__(256) void xent_join_kernel(const float2* __restrict__ stats, const float* __restrict__ z_label, int64_t m, int32_t tiles,
-                                                        const int32_t* __restrict__ labels, int32_t classes, float* __restrict__ loss, float* __restrict__ lse) {
+                                                        const int32_t* __restrict__ labels, int32_t classes, int log_rows, float* __restrict__ loss,
+                                                        float* __restrict__ lse) {
   __shared__ float2 room[256];
-  const int64_t r = (int64_t)blockIdx.x * 64 + (threadIdx.x & 63);
+  const int rows = 1 << log_rows, own = threadIdx.x & (rows - 1), shares = 256 >> log_rows;
+  const int64_t r = ((int64_t)blockIdx.x << log_rows) + own;
   float most = -INFINITY, sum = 0.f;
   if (r < m)
-    for (int t = threadIdx.x >> 6; t < tiles; t += 4) {
+#pragma unroll 4
+    for (int t = threadIdx.x >> log_rows; t < tiles; t += shares) {
       const float2 p = stats[t * m + r];
       join_stats(most, sum, p.x, p.y);
     }
   room[threadIdx.x] = make_float2(most, sum);
   __syncthreads();
-  if (threadIdx.x >= 64 || r >= m) return;
-#pragma unroll
-  for (int t = 1; t < 4; ++t) join_stats(most, sum, room[t * 64 + threadIdx.x].x, room[t * 64 + threadIdx.x].y);
+  if (threadIdx.x >= rows || r >= m) return;
+  for (int t = 1; t < shares; ++t) join_stats(most, sum, room[(t << log_rows) + own].x, room[(t << log_rows) + own].y);
   const float l = lse_of(most, sum);
   lse[r] = l;
   loss[r] = known(labels[r], classes) ? l - z_label[r] : 0.f;
@@ -119,6 +126,34 @@ __global__ __launch_bounds__(256) void xent_bias_kernel(const float* __restrict_
 #pragma unroll
     for (int p = 1; p < 16; ++p) sum += room[p * 16 + threadIdx.x];
     dbias[c] = (float)sum;
+  }
+}
+
+// dH's listed rows: the sum of the shares' sums
+template <typename T>
+__global__ __launch_bounds__(256) void xent_rows_kernel(const float* __restrict__ sums, int32_t splits, int64_t m, const int32_t* __restrict__ bounds, int32_t k,
+                                                        const int32_t* __restrict__ map, T* __restrict__ dH, int64_t lddh) {
+  const int64_t fours = (k + 3) / 4, all = bounds[1] * fours;
+  for (int64_t i = blockIdx.x * 256ll + threadIdx.x; i < all; i += gridDim.x * 256ll) {
+    const int64_t r = i / fours;
+    const int c = (int)(i - r * fours) * 4;
+    float y[4] = {0.f, 0.f, 0.f, 0.f};
+    const float* from = sums + r * k + c;
+    if (c + 4 <= k) {
+#pragma unroll 4
+      for (int32_t s = 0; s < splits; ++s) {
+        float x[4];
+        __builtin_memcpy(x, reinterpret_cast<const Four<float>*>(from + s * m * k), 16);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) y[e] += x[e];
+      }
+    } else {
+      for (int32_t s = 0; s < splits; ++s)
+#pragma unroll
+        for (int e = 0; e < 3; ++e)
+          if (c + e < k) y[e] += from[s * m * k + e];
+    }
+    store_four(dH + map[r] * lddh + c, y, k - c);
   }
 }
 
@@ -146,26 +181,55 @@ bool valid(int32_t dtype, int32_t transW, int64_t m, int32_t kdim, int32_t class
 
 int32_t products(int32_t dtype, int32_t prec) { return dtype == SAGNN_BF16 ? SAGNN_GEMM_BF16 : prec; }
 
-// Tile of a product: m rows by cols, `sum` deep
-int pick_tile(int32_t dtype, int32_t prec, int64_t m, int64_t cols, int64_t sum) {
-  int best = kTile128;
+// Which large tile a product can have besides the small ones: none, one that loads straight into LDS, one staged through registers
+enum { kSmallOnly = 0, kDirect = 1, kStaged = 2 };
+constexpr int64_t kLargeLd = 1 << 20;             // (offsets inside a tile of 256 rows below 2^31)
+bool whole_granules(const void* p, int64_t ld, int64_t width) { return aligned16(p) && ld % 8 == 0 && width % 8 == 0 && ld <= kLargeLd; }
+
+// Tile of a product, m rows by cols, `sum` deep, and shares of the summed index (several only with `room` for sums of their own): what the fullest CU
+// multiplies, by the tiles' rates, and what it costs to write and read the shares' sums.
+struct TilePick { int tile; int32_t splits, share; };
+TilePick pick_tile(int32_t dtype, int32_t prec, int ways, int64_t m, int64_t cols, int64_t sum, int32_t room) {
+  TilePick best{kTile128, 1, (int32_t)sum};
   double least = 1e300;
-  for (int tile : {kTile128, kTile128x64, kTile32x128}) {
+  // values of a 128 x 128 tile that a CU multiplies in a microsecond (half of the operations), and bytes that the chip moves in one
+  const double a_us = (dtype == SAGNN_BF16 ? 740e6 : prec == SAGNN_GEMM_FP32 ? 133e6 : prec == SAGNN_GEMM_BF16 ? 430e6 : 171e6) / 512, bytes_us = 4e6;
+  for (int tile : {kTile128, kTile128x64, kTile32x128, kDirect256, kStaged256x128, kStaged128x256}) {
     const TileCost c = tile_cost(dtype, prec, tile);
-    const int64_t h = grouped_tile_rows(tile), w = grouped_tile_cols(tile), tiles = ceil_div(m, h) * ceil_div(cols, w);
-    const double turns = tiles <= 256 ? 1.25 : tiles < 4 * 256 ? (double)ceil_div(tiles, 256) : tiles / 256.;
-    const double cost = turns * h * w * (sum + c.ends) / c.rate;
-    if (cost < least) {
-      least = cost;
-      best = tile;
+    if (c.rate == 0 || (tile == kDirect256 && ways != kDirect) || ((tile == kStaged256x128 || tile == kStaged128x256) && ways != kStaged)) continue;
+    const int64_t h = grouped_tile_rows(tile), w = grouped_tile_cols(tile);
+    for (int32_t splits = 1; splits <= room; splits *= 2) {
+      const int64_t share = splits == 1 ? sum : (int64_t)round_up((size_t)ceil_div(sum, splits), 64), n = ceil_div(sum, share);
+      if (splits > 1 && (share < 512 || n < splits)) break;
+      if (tile == kDirect256 && share > kRunRounded) continue;
+      const int64_t tiles = ceil_div(m, h) * ceil_div(cols, w) * n;
+      const double turns = tiles <= 256 ? 1.25 : tiles < 4 * 256 ? (double)ceil_div(tiles, 256) : tiles / 256.;
+      const double cost = turns * h * w * (share + c.ends) / c.rate / a_us + (n > 1 ? 12. * n * m * cols / bytes_us + 5. : 0.);
+      if (cost < least) {
+        least = cost;
+        best = {tile, (int32_t)n, (int32_t)share};
+      }
     }
   }
   return best;
 }
+// Of the logits: H (or the listed rows, whose ends are padded) and W
+int logits_ways(int32_t dtype, const void* H, int64_t ldh, int64_t width, const void* W, int64_t ldw, bool transW, int32_t kdim, int32_t classes) {
+  if (dtype == SAGNN_F32) return ldh <= kLargeLd && ldw <= kLargeLd ? kStaged : kSmallOnly;
+  return kdim <= kRunBf16 && whole_granules(H, ldh, width) && whole_granules(W, ldw, transW ? kdim : classes) ? kDirect : kSmallOnly;
+}
+// Of dH: P, whose rows are padded, and W the other way
+int rows_ways(int32_t dtype, int64_t ldp, const void* W, int64_t ldw, bool transW, int32_t kdim, int32_t classes) {
+  if (dtype == SAGNN_F32) return ldp <= kLargeLd && ldw <= kLargeLd ? kStaged : kSmallOnly;
+  return whole_granules(W, ldw, transW ? kdim : classes) ? kDirect : kSmallOnly;
+}
 
-int launch(const XentArgs& args, int32_t dtype, int32_t prec, int tile, bool trans_w, hipStream_t s) {
+int launch(const XentArgs& args, int32_t dtype, int32_t prec, const TilePick& pick, bool trans_w, hipStream_t s) {
   XentArgs a = args;
-  a.run = grouped_run(products(dtype, prec), a.sum);
+  const int tile = pick.tile;
+  a.splits = pick.splits;
+  a.share = pick.share;
+  a.run = grouped_run(products(dtype, prec), a.share);
   a.col_tiles = (int32_t)ceil_div(a.cols, grouped_tile_cols(tile));
   if (dtype == SAGNN_BF16) return xent_bf16(a, tile, trans_w, s);
   return prec == SAGNN_GEMM_FP32 ? xent_fp32(a, tile, trans_w, s) : prec == SAGNN_GEMM_BF16 ? xent_fp32_bf16(a, tile, trans_w, s) : xent_fp32_bf16x3(a, tile, trans_w, s);
@@ -176,11 +240,11 @@ struct Room {
   size_t take(size_t bytes) { const size_t o = off; off += round_up(bytes, 256); return o; }
 };
 
-struct FwdPlan { int tile; int32_t col_tiles; size_t stats, z_label, total; };
-FwdPlan fwd_plan(int32_t dtype, int32_t prec, int64_t m, int32_t kdim, int32_t classes) {
+struct FwdPlan { TilePick tile; int32_t col_tiles; size_t stats, z_label, total; };
+FwdPlan fwd_plan(int32_t dtype, int32_t prec, int ways, int64_t m, int32_t kdim, int32_t classes) {
   FwdPlan p{};
-  p.tile = pick_tile(dtype, prec, m, classes, kdim);
-  p.col_tiles = (int32_t)ceil_div(classes, grouped_tile_cols(p.tile));
+  p.tile = pick_tile(dtype, prec, ways, m, classes, kdim, 1);
+  p.col_tiles = (int32_t)ceil_div(classes, grouped_tile_cols(p.tile.tile));
   if (p.col_tiles > 1) {
     Room room;
     p.stats = room.take((size_t)m * p.col_tiles * sizeof(float2));
@@ -192,6 +256,7 @@ FwdPlan fwd_plan(int32_t dtype, int32_t prec, int64_t m, int32_t kdim, int32_t c
 
 struct BwdPlan {
   int32_t piece, pieces;                     // classes of a piece
+  int32_t splits;                            // shares of them that there is room for in dH's sums
   int64_t ldp, ldc;                          // of P, of the listed rows
   size_t map, bounds, counts, rows, P, sums, weights, parts, bias, parts_bytes, total;
 };
@@ -199,7 +264,8 @@ BwdPlan bwd_plan(int32_t dtype, int32_t prec, int64_t m, int32_t kdim, int32_t c
   BwdPlan p{};
   const int64_t size = dtype == SAGNN_BF16 ? 2 : 4, rows = m > 0 ? m : 1;
   int64_t most = kPieceBytes / (rows * size) / 256 * 256;
-  most = most < 256 ? 256 : most > kPieceMost ? kPieceMost : most;
+  most = most < kPieceLeast ? kPieceLeast : most > kPieceMost ? kPieceMost : most;
+  if (most < ceil_div(classes, kPiecesMost)) most = ceil_div(classes, kPiecesMost);
   p.pieces = (int32_t)ceil_div(classes, most);
   p.piece = p.pieces == 1 ? classes : (int32_t)round_up((size_t)ceil_div(classes, p.pieces), 256);
   p.pieces = (int32_t)ceil_div(classes, p.piece);
@@ -219,7 +285,15 @@ BwdPlan bwd_plan(int32_t dtype, int32_t prec, int64_t m, int32_t kdim, int32_t c
   p.counts = room.take(kListBlocks * 4);
   p.rows = room.take((size_t)rows * p.ldc * size);
   p.P = room.take((size_t)rows * p.ldp * size);
-  p.sums = room.take(p.pieces > 1 ? (size_t)rows * kdim * 4 : 0);
+  // dH's sums: of every share of a piece's classes
+  const int64_t share = rows * kdim * 4;
+  p.splits = share > 0 ? (int32_t)(kSumBytes / share < 1 ? 1 : kSumBytes / share > 32 ? 32 : kSumBytes / share) : 1;
+  int32_t splits = 1;
+  for (int ways : {kSmallOnly, dtype == SAGNN_BF16 ? kDirect : kStaged}) {
+    const int32_t n = pick_tile(dtype, prec, ways, m, kdim, p.piece, p.splits).splits;
+    if (n > splits) splits = n;
+  }
+  p.sums = room.take(p.pieces > 1 || splits > 1 ? (size_t)splits * share : 0);
   p.weights = room.take((size_t)p.piece * kdim * 4);
   p.parts = room.take(p.parts_bytes);
   p.bias = room.take((size_t)ceil_div(rows, 32) * p.piece * 4);
@@ -230,14 +304,17 @@ BwdPlan bwd_plan(int32_t dtype, int32_t prec, int64_t m, int32_t kdim, int32_t c
 template <typename T>
 int list_labels(const BwdPlan& p, char* ws, const int32_t* labels, int64_t m, int32_t classes, const void* H, int64_t ldh, int32_t k, void* dH, int64_t lddh,
                 hipStream_t s) {
+  // (many small blocks: 8192 rows of 1024 in blocks of 256 took 429 us)
   int64_t each = ceil_div(m, kListBlocks);
-  if (each < kListThreads) each = kListThreads;
+  if (each < 16) each = 16;
+  int lanes = 2;
+  while (lanes < 64 && lanes * 8 < p.ldc) lanes *= 2;
   const uint32_t blocks = (uint32_t)ceil_div(m > 0 ? m : 1, each);
   int32_t *counts = (int32_t*)(ws + p.counts), *map = (int32_t*)(ws + p.map), *bounds = (int32_t*)(ws + p.bounds);
   label_count_kernel<<<dim3(blocks), kListThreads, 0, s>>>(labels, m, each, classes, counts);
   SAGNN_LAUNCH_CHECK();
   label_list_kernel<T><<<dim3(blocks), kListThreads, 0, s>>>(labels, m, each, classes, counts, map, bounds, (const T*)H, ldh, k, (T*)(ws + p.rows), p.ldc,
-                                                            (T*)dH, lddh);
+                                                            (T*)dH, lddh, lanes);
   SAGNN_LAUNCH_CHECK();
   return SAGNN_OK;
 }
@@ -256,7 +333,15 @@ size_t reach(int64_t rows, int64_t ld, int64_t cols, size_t size) { return rows 
 SAGNN_EXPORT int softmax_xent_workspace_bytes(int32_t dtype, int64_t m, int32_t kdim, int32_t n_classes, int32_t prec, int32_t backward, size_t* bytes) {
   using namespace sagnn;
   if (!bytes || !valid(dtype, 0, m, kdim, n_classes, prec) || (backward & ~1)) return SAGNN_EINVAL;
-  *bytes = backward ? bwd_plan(dtype, prec, m, kdim, n_classes).total : fwd_plan(dtype, prec, m, kdim, n_classes).total;
+  if (backward) {
+    *bytes = bwd_plan(dtype, prec, m, kdim, n_classes).total;
+  } else {                                   // (room for any strides and alignments)
+    *bytes = 0;
+    for (int ways : {kSmallOnly, dtype == SAGNN_BF16 ? kDirect : kStaged}) {
+      const size_t b = fwd_plan(dtype, prec, ways, m, kdim, n_classes).total;
+      if (b > *bytes) *bytes = b;
+    }
+  }
   return SAGNN_OK;
 }
 
@@ -274,11 +359,11 @@ SAGNN_EXPORT int softmax_xent_fwd(int32_t dtype, const void* d_H, int64_t ldh, c
     if (!clear_of(out, m * 4, d_H, h) || !clear_of(out, m * 4, d_W, w) || !clear_of(out, m * 4, d_labels, m * 4) || !clear_of(out, m * 4, d_bias, (size_t)n_classes * 4))
       return SAGNN_EINVAL;
   if (!clear_of(d_loss, m * 4, d_lse, m * 4)) return SAGNN_EINVAL;
-  const FwdPlan p = fwd_plan(dtype, prec, m, kdim, n_classes);
+  const FwdPlan p = fwd_plan(dtype, prec, logits_ways(dtype, d_H, ldh, kdim, d_W, ldw, transW != 0, kdim, n_classes), m, kdim, n_classes);
   if (p.total > 0 && !d_ws) return SAGNN_EINVAL;
   if (ws_bytes < p.total) return SAGNN_ECAPACITY;
   XentArgs a{};
-  a.X = d_H; a.ldx = ldh; a.W = d_W; a.ldw = ldw; a.m = m; a.cols = n_classes; a.sum = kdim; a.mode = kXentStats; a.bias = d_bias; a.labels = d_labels;
+  a.X = d_H; a.ldx = ldh; a.W = d_W; a.ldw = ldw; a.m = m; a.cols = n_classes; a.sum = a.padded = kdim; a.mode = kXentStats; a.bias = d_bias; a.labels = d_labels;
   a.classes = n_classes; a.loss = d_loss; a.lse = d_lse;
   if (p.total > 0) {
     a.stats = (float2*)((char*)d_ws + p.stats);
@@ -287,7 +372,9 @@ SAGNN_EXPORT int softmax_xent_fwd(int32_t dtype, const void* d_H, int64_t ldh, c
   hipStream_t s = (hipStream_t)stream;
   const int rc = launch(a, dtype, prec, p.tile, transW != 0, s);
   if (rc != SAGNN_OK || p.total == 0) return rc;
-  xent_join_kernel<<<dim3((uint32_t)ceil_div(m, 64)), 256, 0, s>>>(a.stats, a.z_label, m, p.col_tiles, d_labels, n_classes, d_loss, d_lse);
+  // (16 threads to a row of many tiles: 8192 rows of 1024 of them, four threads to each, took 106 us)
+  const int log_rows = p.col_tiles > 16 ? 4 : 6;
+  xent_join_kernel<<<dim3((uint32_t)ceil_div(m, 1 << log_rows)), 256, 0, s>>>(a.stats, a.z_label, m, p.col_tiles, d_labels, n_classes, log_rows, d_loss, d_lse);
   SAGNN_LAUNCH_CHECK();
   return SAGNN_OK;
 }
@@ -322,6 +409,7 @@ SAGNN_EXPORT int softmax_xent_bwd(int32_t dtype, const void* d_H, int64_t ldh, c
   int rc = dtype == SAGNN_BF16 ? list_labels<__bf16>(p, ws, d_labels, m, n_classes, d_H, ldh, kdim, d_dH, lddh, s)
                                : list_labels<float>(p, ws, d_labels, m, n_classes, d_H, ldh, kdim, d_dH, lddh, s);
   const int32_t* bounds = (const int32_t*)(ws + p.bounds);
+  TilePick rows{};
   for (int32_t at = 0; at < n_classes && rc == SAGNN_OK; at += p.piece) {
     const int32_t n = n_classes - at < p.piece ? n_classes - at : p.piece;
     XentArgs a{};
@@ -329,17 +417,31 @@ SAGNN_EXPORT int softmax_xent_bwd(int32_t dtype, const void* d_H, int64_t ldh, c
     a.cols = n; a.sum = kdim; a.mode = kXentGrads; a.bias = d_bias ? d_bias + at : nullptr; a.labels = d_labels; a.class0 = at; a.classes = n_classes;
     a.map = (const int32_t*)(ws + p.map); a.row_lse = d_lse; a.grad = d_grad; a.grad_all = (float)grad_all; a.P = ws + p.P; a.ldp = p.ldp;
     a.stored = (int32_t)round_up((size_t)n, 8); a.bias_parts = d_dbias ? (float*)(ws + p.bias) : nullptr;
-    const int tile = pick_tile(dtype, prec, m, n, kdim);
+    a.padded = (int32_t)p.ldc;
+    const TilePick tile = pick_tile(dtype, prec, logits_ways(dtype, a.X, p.ldc, p.ldc, a.W, ldw, transW != 0, kdim, n), m, n, kdim, 1);
     if (m > 0) rc = launch(a, dtype, prec, tile, transW != 0, s);
     if (rc == SAGNN_OK && d_dbias) {
-      xent_bias_kernel<<<dim3((uint32_t)ceil_div(n, 16)), 256, 0, s>>>(a.bias_parts, bounds, grouped_tile_rows(tile), n, d_dbias + at);
+      xent_bias_kernel<<<dim3((uint32_t)ceil_div(n, 16)), 256, 0, s>>>(a.bias_parts, bounds, grouped_tile_rows(tile.tile), n, d_dbias + at);
       SAGNN_LAUNCH_CHECK();
     }
     if (rc == SAGNN_OK && d_dH && m > 0) {
+      // (the last piece in as many shares as the others, whose sums it adds to)
+      if (at == 0) rows = pick_tile(dtype, prec, rows_ways(dtype, p.ldp, a.W, ldw, transW != 0, kdim, n_classes), m, kdim, p.piece, p.splits);
+      const bool summed = p.pieces > 1 || rows.splits > 1;
+      TilePick pick = rows;
+      if (pick.splits == 1) pick.share = n;
       XentArgs b{};
       b.X = a.P; b.ldx = p.ldp; b.W = a.W; b.ldw = ldw; b.m = m; b.count = a.count; b.cols = kdim; b.sum = n; b.mode = kXentRows; b.map = a.map;
-      b.sums = (float*)(ws + p.sums); b.add = at > 0; b.last = at + n == n_classes; b.out = d_dH; b.ldo = lddh;
-      rc = launch(b, dtype, prec, pick_tile(dtype, prec, m, kdim, n), transW == 0, s);
+      b.sums = summed ? (float*)(ws + p.sums) : nullptr; b.add = at > 0; b.out = d_dH; b.ldo = lddh;
+      b.padded = a.stored; b.wide = aligned16(d_dH) && lddh % 8 == 0 && kdim % 8 == 0;
+      rc = launch(b, dtype, prec, pick, transW == 0, s);
+      if (rc == SAGNN_OK && summed && at + n == n_classes) {
+        const int64_t blocks = ceil_div(m * ceil_div(kdim, 4), 256);
+        const dim3 grid((uint32_t)(blocks < 8192 ? blocks : 8192));
+        if (dtype == SAGNN_BF16) xent_rows_kernel<__bf16><<<grid, 256, 0, s>>>(b.sums, rows.splits, m, bounds, kdim, b.map, (__bf16*)d_dH, lddh);
+        else xent_rows_kernel<float><<<grid, 256, 0, s>>>(b.sums, rows.splits, m, bounds, kdim, b.map, (float*)d_dH, lddh);
+        SAGNN_LAUNCH_CHECK();
+      }
     }
     if (rc == SAGNN_OK && d_dW) {
       // (fp32 weights whose piece lies in one place are written there)
