@@ -198,11 +198,12 @@ TilePick pick_tile(int32_t dtype, int32_t prec, int ways, int64_t m, int64_t col
     const TileCost c = tile_cost(dtype, prec, tile);
     if (c.rate == 0 || (tile == kDirect256 && ways != kDirect) || ((tile == kStaged256x128 || tile == kStaged128x256) && ways != kStaged)) continue;
     const int64_t h = grouped_tile_rows(tile), w = grouped_tile_cols(tile);
-    for (int32_t splits = 1; splits <= room; splits *= 2) {
+    const int64_t whole = ceil_div(m, h) * ceil_div(cols, w);
+    for (int32_t splits = 1; splits <= room && (splits == 1 || whole * splits < 4 * 256); ++splits) {
       const int64_t share = splits == 1 ? sum : (int64_t)round_up((size_t)ceil_div(sum, splits), 64), n = ceil_div(sum, share);
-      if (splits > 1 && (share < 512 || n < splits)) break;
+      if (splits > 1 && share < 512) break;
       if (tile == kDirect256 && share > kRunRounded) continue;
-      const int64_t tiles = ceil_div(m, h) * ceil_div(cols, w) * n;
+      const int64_t tiles = whole * n;
       const double turns = tiles <= 256 ? 1.25 : tiles < 4 * 256 ? (double)ceil_div(tiles, 256) : tiles / 256.;
       const double cost = turns * h * w * (share + c.ends) / c.rate / a_us + (n > 1 ? 12. * n * m * cols / bytes_us + 5. : 0.);
       if (cost < least) {
