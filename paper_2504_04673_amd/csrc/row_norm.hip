@@ -38,6 +38,13 @@ __device__ __forceinline__ T team_join(T x, T* place, F join) {
   return y;
 }
 
+// 1 / sqrt(x) in 64 bits: the instruction's estimate, good to 2^-23 or so, and a Newton step.  Of zero and infinity the estimate is the result.
+__device__ __forceinline__ float root_inverse(double x) {
+  const double r = __builtin_amdgcn_rsq(x), e = __builtin_fma(-x * r, r, 1.);
+  const double better = __builtin_fma(0.5 * r, e, r);
+  return (float)(e == e ? better : r);
+}
+
 struct RowArgs {
   const void* X; int64_t ldx;        // backward: the sums S
   const void* R; int64_t ldr;        // residual, or NULL; backward: gradient of S from elsewhere
@@ -66,9 +73,9 @@ __global__ __launch_bounds__(kThreads) void dropout_kernel(const RowArgs a) {
     T* y = reinterpret_cast<T*>(a.Y) + r * a.ldy;
     for (int e = lane; e < a.eights; e += a.lanes) {
       const int there = a.C - e * 8;
-      const auto w = load_eight(x + e * 8, there);
+      const auto w = load_eight(x + e * 8, there, a.C);
       TightRun<T, 8> z;
-      if constexpr (RES) z = load_eight(res + e * 8, there);
+      if constexpr (RES) z = load_eight(res + e * 8, there, a.C);
       float v[8];
 #pragma unroll
       for (int i = 0; i < 8; ++i) v[i] = (float)w.x[i];
@@ -91,6 +98,19 @@ __global__ __launch_bounds__(TEAM == 64 ? kThreads : TEAM) void rms_norm_kernel(
   const int L = kWide ? TEAM : a.lanes, lane = kWide ? threadIdx.x : threadIdx.x & (L - 1);
   const int64_t per = kWide ? 1 : kThreads / L, slot = kWide ? 0 : threadIdx.x / L;
   const uint64_t offset = drop_offset(a.drop);
+  float gamma[V][8];
+#pragma unroll
+  for (int v = 0; v < V; ++v) {
+    const int e = v * L + lane, there = a.C - e * 8;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) gamma[v][i] = 1.f;
+    if (a.gamma && there > 0) {
+      const auto c = load_eight(a.gamma + e * 8, there, a.C);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) gamma[v][i] = c.x[i];
+    }
+  }
+  const double per_value = 1. / a.C;
   for (int64_t r = blockIdx.x * per + slot; r < a.m; r += gridDim.x * per) {      // (all lanes of a row together)
     float s[V][8];
     double squares = 0.;
@@ -100,12 +120,12 @@ __global__ __launch_bounds__(TEAM == 64 ? kThreads : TEAM) void rms_norm_kernel(
 #pragma unroll
       for (int i = 0; i < 8; ++i) s[v][i] = 0.f;
       if (there <= 0) continue;
-      const auto w = load_eight(reinterpret_cast<const T*>(a.X) + r * a.ldx + e * 8, there);
+      const auto w = load_eight(reinterpret_cast<const T*>(a.X) + r * a.ldx + e * 8, there, a.C);
 #pragma unroll
       for (int i = 0; i < 8; ++i) s[v][i] = (float)w.x[i];
       if (a.drop.cut) drop_eight(a.drop, offset, (uint32_t)r, (uint32_t)e, s[v]);
       if (a.R) {
-        const auto z = load_eight(reinterpret_cast<const T*>(a.R) + r * a.ldr + e * 8, there);
+        const auto z = load_eight(reinterpret_cast<const T*>(a.R) + r * a.ldr + e * 8, there, a.C);
 #pragma unroll
         for (int i = 0; i < 8; ++i) s[v][i] += (float)z.x[i];
       }
@@ -115,7 +135,7 @@ __global__ __launch_bounds__(TEAM == 64 ? kThreads : TEAM) void rms_norm_kernel(
     }
     if constexpr (kWide) squares = team_join<TEAM>(squares, room, [](double x, double y) { return x + y; });
     else squares = lanes_sum(squares, L);
-    const float rstd = (float)(1. / sqrt(squares / a.C + a.eps));
+    const float rstd = root_inverse(squares * per_value + a.eps);
     if (a.rstd && lane == 0) a.rstd[r] = rstd;
     float most = 0.f;
 #pragma unroll
@@ -123,12 +143,7 @@ __global__ __launch_bounds__(TEAM == 64 ? kThreads : TEAM) void rms_norm_kernel(
       const int e = v * L + lane, there = a.C - e * 8;
       if (there <= 0) continue;
 #pragma unroll
-      for (int i = 0; i < 8; ++i) s[v][i] *= rstd;
-      if (a.gamma) {
-        const auto g = load_eight(a.gamma + e * 8, there);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) s[v][i] *= g.x[i];
-      }
+      for (int i = 0; i < 8; ++i) s[v][i] = s[v][i] * rstd * gamma[v][i];
       if constexpr (EIGHT)
 #pragma unroll
         for (int i = 0; i < 8; ++i) most = fmaxf(most, fabsf(s[v][i]));
@@ -170,6 +185,18 @@ __global__ __launch_bounds__(TEAM == 64 ? kThreads : TEAM) void rms_norm_bwd_ker
   const int L = kWide ? TEAM : a.lanes, lane = kWide ? threadIdx.x : threadIdx.x & (L - 1);
   const int64_t per = kWide ? 1 : kThreads / L, slot = kWide ? 0 : threadIdx.x / L;
   const uint64_t offset = drop_offset(a.drop);
+  float gamma[V][8];
+#pragma unroll
+  for (int v = 0; v < V; ++v) {
+    const int e = v * L + lane, there = a.C - e * 8;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) gamma[v][i] = 1.f;
+    if (a.gamma && there > 0) {
+      const auto c = load_eight(a.gamma + e * 8, there, a.C);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) gamma[v][i] = c.x[i];
+    }
+  }
   const float per_value = 1.f / a.C;
   float sums[V][8];
 #pragma unroll
@@ -183,19 +210,16 @@ __global__ __launch_bounds__(TEAM == 64 ? kThreads : TEAM) void rms_norm_bwd_ker
     for (int v = 0; v < V; ++v) {
       const int e = v * L + lane, there = a.C - e * 8;
       if (there <= 0) continue;
-      const auto w = load_eight(reinterpret_cast<const T*>(a.X) + r * a.ldx + e * 8, there);
-      const auto z = load_eight(reinterpret_cast<const T*>(a.G) + r * a.ldg + e * 8, there);
+      const auto w = load_eight(reinterpret_cast<const T*>(a.X) + r * a.ldx + e * 8, there, a.C);
+      const auto z = load_eight(reinterpret_cast<const T*>(a.G) + r * a.ldg + e * 8, there, a.C);
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
         x[v][i] = (float)w.x[i] * rstd;
         g[v][i] = (float)z.x[i];
         sums[v][i] += g[v][i] * x[v][i];
       }
-      if (a.gamma) {
-        const auto c = load_eight(a.gamma + e * 8, there);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) g[v][i] *= c.x[i];
-      }
+      for (int i = 0; i < 8; ++i) g[v][i] *= gamma[v][i];
 #pragma unroll
       for (int i = 0; i < 8; ++i) dot += g[v][i] * x[v][i];
     }
@@ -209,7 +233,7 @@ __global__ __launch_bounds__(TEAM == 64 ? kThreads : TEAM) void rms_norm_bwd_ker
 #pragma unroll
       for (int i = 0; i < 8; ++i) g[v][i] = rstd * (g[v][i] - x[v][i] * dot);
       if (a.R) {
-        const auto d = load_eight(reinterpret_cast<const T*>(a.R) + r * a.ldr + e * 8, there);
+        const auto d = load_eight(reinterpret_cast<const T*>(a.R) + r * a.ldr + e * 8, there, a.C);
 #pragma unroll
         for (int i = 0; i < 8; ++i) g[v][i] += (float)d.x[i];
       }
@@ -276,7 +300,7 @@ __global__ __launch_bounds__(kThreads) void unpack_rows_kernel(const uint8_t* __
       const int there = C - e * 8;
       float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
       if (in) {
-        from_e4m3(load_bytes(Q + r * ldq + e * 8, there), v);
+        from_e4m3(load_bytes(Q + r * ldq + e * 8, there, C), v);
 #pragma unroll
         for (int k = 0; k < 8; ++k) v[k] *= s;
       }

@@ -74,7 +74,7 @@ __global__ __launch_bounds__(kListThreads) void label_list_kernel(const int32_t*
       const int32_t to = place[i];
       if (to >= 0)
         for (int c = own * 8; c < ldc; c += lanes * 8) {
-          const auto w = load_eight(H + (r0 + i) * ldh + c, k - c);
+          const auto w = load_eight(H + (r0 + i) * ldh + c, k - c, k);
           *reinterpret_cast<TightRun<T, 8>*>(rows + to * ldc + c) = w;
         }
       else if (dH)
