@@ -316,11 +316,15 @@ int lanes_of(int32_t eights, int most) {
   while (l < eights && l < most) l *= 2;
   return l;
 }
-// Workgroups for m rows, `per` of them each at a time: the chip is full with 2048
-int64_t workgroups(int64_t m, int64_t per) {
+// Workgroups for m rows, `per` of them each at a time, `most` at the most
+dim3 workgroups(int64_t m, int64_t per, int64_t most) {
   const int64_t n = ceil_div(m, per);
-  return n < 2048 ? n : 2048;
+  return dim3((uint32_t)(n < most ? n : most));
 }
+// How many workgroups are best is measured: dropout (2 M x 256 bfloat16 and a residual) 574 us with the 2048 that the chip holds, 613 with 4096, 511 with
+// one for every few rows; the norm, whose workgroups keep their scale (1 M x 256), 495 with what the chip holds, 394 with 8192, 372 with 32768, 402
+// with one for every few rows; the gather (0.8 M of 2 M rows of 256) 118, 124 with 16384 and 143 with one for every few.
+constexpr int64_t kDropGroups = 4000000, kNormGroups = 32768, kPackGroups = 2048;
 
 // How a row is spread: V turns of eight values over `team` threads (64: lanes of a wavefront)
 struct RowForm { int turns, team; };
@@ -348,8 +352,10 @@ int64_t bwd_workgroups(int64_t m, int32_t C) {
   const int32_t eights = (C + 7) / 8;
   const RowForm f = row_form(eights);
   const int64_t per = f.team == 64 ? kThreads / lanes_of(eights, 64) : 1;
+  // as many as the chip holds at once (by their registers)
+  const int64_t most = f.team == 64 ? (f.turns == 1 ? 6 : f.turns == 2 ? 4 : 2) * 256 : f.team == 256 ? 1024 : 256;
   int64_t n = ceil_div(m, per * 8);
-  if (n > 2048) n = 2048;
+  if (n > most) n = most;
   if (n < ceil_div(m, per * kSerial)) n = ceil_div(m, per * kSerial);
   return n < 1 ? 1 : n;
 }
@@ -390,7 +396,7 @@ SAGNN_EXPORT int dropout_add(int32_t dtype, const void* d_X, int64_t ldx, const 
   if (!d_X || !d_Y || !aligned_to(d_X, size) || !aligned_to(d_R, size) || !aligned_to(d_Y, size)) return SAGNN_EINVAL;
   if (!in_place(d_Y, ldy, d_X, ldx, m, C, size) || !in_place(d_Y, ldy, d_R, ldr, m, C, size)) return SAGNN_EINVAL;
   a.X = d_X; a.ldx = ldx; a.R = d_R; a.ldr = ldr; a.m = m; a.C = C; a.eights = (C + 7) / 8; a.lanes = lanes_of(a.eights, 64); a.Y = d_Y; a.ldy = ldy;
-  const dim3 grid((uint32_t)workgroups(m, kThreads / a.lanes));
+  const dim3 grid = workgroups(m, kThreads / a.lanes, kDropGroups);
   hipStream_t s = (hipStream_t)stream;
   if (dtype == SAGNN_BF16 && d_R) dropout_kernel<__bf16, true><<<grid, kThreads, 0, s>>>(a);
   else if (dtype == SAGNN_BF16) dropout_kernel<__bf16, false><<<grid, kThreads, 0, s>>>(a);
@@ -423,7 +429,7 @@ SAGNN_EXPORT int rms_norm_fwd(int32_t dtype, const void* d_X, int64_t ldx, const
   const RowForm f = row_form(a.eights);
   return by_form(f, [&](auto turns, auto team) {
     constexpr int V = decltype(turns)::value, TEAM = decltype(team)::value, kGroup = TEAM == 64 ? kThreads : TEAM;
-    const dim3 grid((uint32_t)workgroups(m, TEAM == 64 ? kThreads / a.lanes : 1));
+    const dim3 grid = workgroups(m, TEAM == 64 ? kThreads / a.lanes : 1, kNormGroups);
     hipStream_t s = (hipStream_t)stream;
     if (dtype == SAGNN_BF16 && eight) rms_norm_kernel<__bf16, V, TEAM, true><<<grid, kGroup, 0, s>>>(a);
     else if (dtype == SAGNN_BF16) rms_norm_kernel<__bf16, V, TEAM, false><<<grid, kGroup, 0, s>>>(a);
@@ -489,7 +495,7 @@ SAGNN_EXPORT int spmm_pack_rows_e4m3(const void* d_Q, int64_t ldq, const float* 
   const uintptr_t q = reinterpret_cast<uintptr_t>(d_Q), o = reinterpret_cast<uintptr_t>(d_out);
   if (n > 0 && q < o + ((uintptr_t)(N - 1) * ldo + C) * size && o < q + (uintptr_t)(n - 1) * ldq + C) return SAGNN_EINVAL;
   const int32_t eights = (C + 7) / 8, lanes = lanes_of(eights, 64);
-  const dim3 grid((uint32_t)workgroups(N, kThreads / lanes));
+  const dim3 grid = workgroups(N, kThreads / lanes, kPackGroups);
   hipStream_t s = (hipStream_t)stream;
   const uint8_t* Q = reinterpret_cast<const uint8_t*>(d_Q);
   if (out_type == SAGNN_BF16) unpack_rows_kernel<__bf16><<<grid, kThreads, 0, s>>>(Q, ldq, d_scale, n, C, eights, lanes, d_rows, N, reinterpret_cast<__bf16*>(d_out), ldo);
