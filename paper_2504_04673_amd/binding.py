@@ -960,12 +960,31 @@ def _here(t, name="X"):
     return t
 
 
+def _lead(X, name="X", dtype=None):
+    """A matrix on the current device: its address, leading dimension and rows and columns."""
+    if X.is_cuda and X.is_contiguous() and X.dim() == 2 and (X.dtype in _DTYPE if dtype is None else X.dtype is dtype) and X.get_device() == torch._C._cuda_getDevice():
+        m, c = X.shape
+        return X.data_ptr(), c, m, c
+    _here(_typed(X, name, dtype), name)
+    return X.data_ptr(), _ld(X), *X.shape
+
+
 def _like(t, X, name):
     """A matrix like X, or None: its address and leading dimension."""
     if t is None:
         return None, 0
-    t = _here(_shape(_typed(t, name, X.dtype), X.shape, name), name)
+    if t.dtype is X.dtype and t.shape == X.shape and t.is_contiguous() and t.get_device() == X.get_device():
+        return t.data_ptr(), X.shape[1]
+    _here(_shape(_typed(t, name, X.dtype), X.shape, name), name)
     return t.data_ptr(), _ld(t)
+
+
+def _vector(t, n, name, dtype=torch.float32):
+    """A vector of n values on the current device, or None: its address."""
+    if t is None:
+        return None
+    _here(_shape(_dev(t, dtype, name), (n,), name), name)
+    return t.data_ptr()
 
 
 def dropout_add(X, p: float, seed: int, offset=0, residual=None, row0: int = 0, out=None):
@@ -973,71 +992,69 @@ def dropout_add(X, p: float, seed: int, offset=0, residual=None, row0: int = 0, 
     seed, offset, row0 + row and column; the gradient for X is the same call on dY without a residual, with the same seed, offset and row0.
     offset: an integer, or an int64 tensor of one element on the device that is read when the kernel runs (a captured graph counts it up).
     row0: the first row's number in the whole matrix where ranks share its rows.  X: m x C, float32 or bfloat16; residual like it."""
-    X = _here(_typed(X, "X"))
-    m, c = X.shape
+    x, ldx, m, c = _lead(X)
+    y, ldy = _like(out, X, "out")
     if out is None:
         out = X.new_empty((m, c))
+        y, ldy = out.data_ptr(), c
     r, ldr = _like(residual, X, "residual")
-    y, ldy = _like(out, X, "out")
-    _check(_calls().dropout_add(_DTYPE[X.dtype], X.data_ptr(), _ld(X), r, ldr, m, c, *_drop_args(p, seed, offset, row0), y, ldy, _stream()), "dropout_add")
+    _check(_calls().dropout_add(_DTYPE[X.dtype], x, ldx, r, ldr, m, c, *_drop_args(p, seed, offset, row0), y, ldy, _stream()), "dropout_add")
     return out
 
 
-def _gamma(gamma, X):
-    return None if gamma is None else _shape(_dev(gamma, torch.float32, "gamma"), X.shape[1:], "gamma").data_ptr()
-
-
-def _rms_norm(X, gamma, residual, eps, p, seed, offset, row0, kind, out, scale, out_sum):
-    X = _here(X)
-    m, c = X.shape
-    added = residual is not None or p > 0.0
-    if not added and out_sum is not None:
+def _rms_norm(X, lead, gamma, residual, eps, p, seed, offset, row0, kind, y, ldy, scale, out_sum):
+    x, ldx, m, c = lead
+    S, s, lds = X, None, 0
+    if residual is not None or p > 0.0:
+        S = X.new_empty((m, c)) if out_sum is None else out_sum
+        s, lds = _like(S, X, "out_sum")
+    elif out_sum is not None:
         raise ValueError("out_sum: nothing is added or dropped, the sum is X")
-    S = None if not added else X.new_empty((m, c)) if out_sum is None else out_sum
     rstd = X.new_empty(m, dtype=torch.float32)
     r, ldr = _like(residual, X, "residual")
-    s, lds = _like(S, X, "out_sum")
-    _check(_calls().rms_norm_fwd(_DTYPE[X.dtype], X.data_ptr(), _ld(X), r, ldr, m, c, _gamma(gamma, X), eps, *_drop_args(p, seed, offset, row0),
-                                 kind, out.data_ptr(), _ld(out), _ptr(scale), s, lds, rstd.data_ptr(), _stream()), "rms_norm_fwd")
-    return S if added else X, rstd
+    _check(_calls().rms_norm_fwd(_DTYPE[X.dtype], x, ldx, r, ldr, m, c, _vector(gamma, c, "gamma"), eps, *_drop_args(p, seed, offset, row0),
+                                 kind, y, ldy, scale, s, lds, rstd.data_ptr(), _stream()), "rms_norm_fwd")
+    return S, rstd
 
 
 def rms_norm(X, gamma=None, residual=None, eps: float = 1e-6, p: float = 0.0, seed: int = 0, offset=0, row0: int = 0, out=None, out_sum=None):
     """Root-mean-square norm of the rows of S = residual + dropout(X) (dropout_add's p, seed, offset, row0): Y = S rstd gamma,
     rstd = (mean(S^2) + eps)^-1/2.  X: m x C, float32 or bfloat16, residual like it; gamma: C, float32.  Returns (Y, S, rstd), S being X itself
     where nothing is added or dropped, rstd float32; out_sum may be the residual, which is updated in place then."""
-    X = _typed(X, "X")
-    out = X.new_empty(X.shape) if out is None else _shape(_typed(out, "out", X.dtype), X.shape, "out")
-    S, rstd = _rms_norm(X, gamma, residual, eps, p, seed, offset, row0, _DTYPE[X.dtype], out, None, out_sum)
+    lead = _lead(X)
+    if out is None:
+        out = X.new_empty(lead[2:])
+        y, ldy = out.data_ptr(), lead[3]
+    else:
+        y, ldy = _like(out, X, "out")
+    S, rstd = _rms_norm(X, lead, gamma, residual, eps, p, seed, offset, row0, _DTYPE[X.dtype], y, ldy, None, out_sum)
     return out, S, rstd
 
 
 def rms_norm_e4m3(X, gamma=None, residual=None, eps: float = 1e-6, p: float = 0.0, seed: int = 0, offset=0, row0: int = 0, out_sum=None):
     """rms_norm with rows of 8 bits: Y[r, :] = scale[r] Q[r, :], Q torch.float8_e4m3fn, scale float32.  Returns (Q, scale, S, rstd).
     spmm_pack_rows_e4m3 reads them."""
-    X = _typed(X, "X")
-    Q, scale = X.new_empty(X.shape, dtype=torch.float8_e4m3fn), X.new_empty(X.shape[0], dtype=torch.float32)
-    S, rstd = _rms_norm(X, gamma, residual, eps, p, seed, offset, row0, E4M3, Q, scale, out_sum)
+    lead = _lead(X)
+    Q, scale = X.new_empty(lead[2:], dtype=torch.float8_e4m3fn), X.new_empty(lead[2], dtype=torch.float32)
+    S, rstd = _rms_norm(X, lead, gamma, residual, eps, p, seed, offset, row0, E4M3, Q.data_ptr(), lead[3], scale.data_ptr(), out_sum)
     return Q, scale, S, rstd
 
 
 def rms_norm_bwd(S, G, rstd, gamma=None, grad_sum=None, p: float = 0.0, seed: int = 0, offset=0, row0: int = 0, want_dx=True, want_dgamma=True):
     """Gradients of rms_norm for G = dLoss/dY, with the S and rstd that it returned; grad_sum: the gradient that S has from elsewhere (the
     next residual).  Returns (dX, dR, dgamma): dX = dropout(dR), or dR itself where nothing was dropped; None for what is not wanted."""
-    S = _here(_typed(S, "S"), "S")
-    m, c = S.shape
+    s, lds, m, c = _lead(S, "S")
     g, ldg = _like(G, S, "G")
     if g is None:
         raise ValueError("G is needed")
     d, ldd = _like(grad_sum, S, "grad_sum")
-    _shape(_dev(rstd, torch.float32, "rstd"), (m,), "rstd")
     drop = _drop_args(p, seed, offset, row0)
     dR = S.new_empty((m, c))
     dX = S.new_empty((m, c)) if want_dx and drop[0] else None
     dgamma = S.new_empty(c, dtype=torch.float32) if want_dgamma else None
     need = _bytes_of("rms_norm_bwd_workspace_bytes", m, c) if want_dgamma else 0
     ws = S.new_empty(need, dtype=torch.uint8) if need else None
-    _check(_calls().rms_norm_bwd(_DTYPE[S.dtype], S.data_ptr(), _ld(S), g, ldg, d, ldd, m, c, _gamma(gamma, S), rstd.data_ptr(), *drop, _ptr(dX), c,
+    _check(_calls().rms_norm_bwd(_DTYPE[S.dtype], s, lds, g, ldg, d, ldd, m, c, _vector(gamma, c, "gamma"), _vector(rstd, m, "rstd"), *drop, _ptr(dX), c,
                                  dR.data_ptr(), c, _ptr(dgamma), _ptr(ws), need, _stream()), "rms_norm_bwd")
     return (dX if drop[0] else dR) if want_dx else None, dR, dgamma
 
@@ -1045,31 +1062,29 @@ def rms_norm_bwd(S, G, rstd, gamma=None, grad_sum=None, p: float = 0.0, seed: in
 def spmm_pack_rows_e4m3(Q, scale, rows=None, dtype=torch.float32, out=None):
     """out[i, :] = scale[rows[i]] Q[rows[i], :] for rows of 8 bits (rms_norm_e4m3's), widened to float32 or bfloat16; rows: int32, None: all of
     them.  A row number out of range gives zeros."""
-    Q = _here(_typed(Q, "Q", torch.float8_e4m3fn), "Q")
-    n, c = Q.shape
-    _shape(_dev(scale, torch.float32, "scale"), (n,), "scale")
-    if rows is not None and _dev(rows, torch.int32, "rows").dim() != 1:
-        raise ValueError("rows: expected a vector")
+    q, ldq, n, c = _lead(Q, "Q", torch.float8_e4m3fn)
     N = n if rows is None else rows.numel()
+    at = _vector(rows, N, "rows", torch.int32)
     if out is None:
-        out = Q.new_empty((N, c), dtype=dtype)
-    out = _shape(_typed(out, "out"), (N, c), "out")
-    _check(_calls().spmm_pack_rows_e4m3(Q.data_ptr(), _ld(Q), scale.data_ptr(), n, c, _ptr(rows), N, _DTYPE[out.dtype], out.data_ptr(), _ld(out),
-                                        _stream()), "spmm_pack_rows_e4m3")
+        out, o, ldo = Q.new_empty((N, c), dtype=dtype), None, c
+        _typed(out, "dtype")
+    else:
+        o, ldo, *shape = _lead(out, "out")
+        if shape != [N, c]:
+            raise ValueError(f"out: expected {(N, c)}, got {tuple(out.shape)}")
+    _check(_calls().spmm_pack_rows_e4m3(q, ldq, _vector(scale, n, "scale"), n, c, at, N, _DTYPE[out.dtype], o or out.data_ptr(), ldo, _stream()),
+           "spmm_pack_rows_e4m3")
     return out
 
 
 def _xent_args(H, W, labels, bias, transW):
     """What both directions check: H's rows and width, the classes, and the pointers that lead both calls."""
-    H = _here(_typed(H, "H"), "H")
-    W = _here(_typed(W, "W", H.dtype), "W")
-    m, k = H.shape
-    n = W.shape[0 if transW else 1]
-    _shape(W, (n, k) if transW else (k, n), "W")
-    _shape(_here(_dev(labels, torch.int32, "labels"), "labels"), (m,), "labels")
-    if bias is not None:
-        _shape(_here(_dev(bias, torch.float32, "bias"), "bias"), (n,), "bias")
-    return m, k, n, (_DTYPE[H.dtype], H.data_ptr(), _ld(H), W.data_ptr(), _ld(W), int(transW), _ptr(bias), labels.data_ptr())
+    h, ldh, m, k = _lead(H, "H")
+    w, ldw, *shape = _lead(W, "W", H.dtype)
+    n = shape[0 if transW else 1]
+    if shape != ([n, k] if transW else [k, n]):
+        raise ValueError(f"W: expected {k} {'columns' if transW else 'rows'}, got {tuple(W.shape)}")
+    return m, k, n, (_DTYPE[H.dtype], h, ldh, w, ldw, int(transW), _vector(bias, n, "bias"), _vector(labels, m, "labels", torch.int32))
 
 
 def softmax_xent(H, W, labels, bias=None, transW=False, prec=GEMM_FP32):
@@ -1089,15 +1104,12 @@ def softmax_xent_bwd(H, W, labels, lse, grad=1.0, bias=None, transW=False, prec=
     """Gradients of softmax_xent with the lse that it returned; grad: dLoss/d(loss), a number for all rows (one over how many labels there are, for
     their mean) or m, float32.  Returns (dH, dW, dbias), the first two in H's type, dbias float32; None for what is not wanted or not there."""
     m, k, n, args = _xent_args(H, W, labels, bias, transW)
-    _shape(_here(_dev(lse, torch.float32, "lse"), "lse"), (m,), "lse")
     rows = isinstance(grad, torch.Tensor)
-    if rows:
-        _shape(_here(_dev(grad, torch.float32, "grad"), "grad"), (m,), "grad")
     need = _bytes_of("softmax_xent_workspace_bytes", args[0], m, k, n, prec, 1)
     ws = H.new_empty(need, dtype=torch.uint8)
     dH = H.new_empty((m, k)) if want_dh else None
     dW = H.new_empty(W.shape) if want_dw else None
     dbias = None if bias is None or not want_dw else torch.empty_like(bias)
-    _check(_calls().softmax_xent_bwd(*args, lse.data_ptr(), grad.data_ptr() if rows else None, 1.0 if rows else grad, m, k, n, prec, _ptr(dH), k, _ptr(dW),
+    _check(_calls().softmax_xent_bwd(*args, _vector(lse, m, "lse"), _vector(grad, m, "grad") if rows else None, 1.0 if rows else grad, m, k, n, prec, _ptr(dH), k, _ptr(dW),
                                      _ptr(dbias), ws.data_ptr(), need, _stream()), "softmax_xent_bwd")
     return dH, dW, dbias
