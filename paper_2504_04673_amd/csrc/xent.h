@@ -98,6 +98,20 @@ __device__ __forceinline__ void load_bias(const XentArgs& a, int64_t c0, int col
     }
 }
 
+// Whether a lane has the column `near`, counted from its first (half of the columns are those of the lane 32 away)
+template <typename C>
+__device__ __forceinline__ bool ours(int near) { return near >= 0 && (near & 4) == 0; }
+// Of a lane's values the one of its column `near`
+template <typename C>
+__device__ __forceinline__ float value_at(const floatx16 (&acc)[C::TN], const float (&b)[C::TN][16], int near) {
+  float x = 0.f;
+#pragma unroll
+  for (int tn = 0; tn < C::TN; ++tn)
+#pragma unroll
+    for (int v = 0; v < 16; ++v) x = near == tn * 32 + 8 * (v / 4) + v % 4 ? acc[tn][v] + b[tn][v] : x;
+  return x;
+}
+
 // The epilogues take a lane's sums row by row and leave them as they are.  WHOLE: a tile without ends of the matrix, which asks nothing for each value.
 template <typename C, bool WHOLE>
 __device__ __forceinline__ void xent_stats(const XentArgs& a, int64_t r0, int32_t col, int64_t c0, int rows, int cols, char* smem,
@@ -115,19 +129,16 @@ __device__ __forceinline__ void xent_stats(const XentArgs& a, int64_t r0, int32_
     const int64_t label = (WHOLE || r < rows ? (int64_t)a.labels[r0 + r] : -1) - c0, far = label - column_of<C>(0, 0);
     const int near = far >= 0 && far < C::TN * 32 && label < cols ? (int)far : -1;
     auto z = [&](int tn, int v) { return WHOLE || column_of<C>(tn, v) < cols ? acc[tm][tn][v] + b[tn][v] : -INFINITY; };
-    float most = -INFINITY, own = 0.f;
-    bool here = false;
+    const bool here = ours<C>(near);
+    if (__any(here)) {                              // (few wavefronts of many classes)
+      const float own = value_at<C>(acc[tm], b, near);
+      if (here) (a.stats ? a.z_label + r0 : z_label)[r] = own;
+    }
+    float most = -INFINITY;
 #pragma unroll
     for (int tn = 0; tn < C::TN; ++tn)
 #pragma unroll
-      for (int v = 0; v < 16; ++v) {
-        const float x = z(tn, v);
-        most = fmaxf(most, x);
-        const bool hit = near == tn * 32 + 8 * (v / 4) + v % 4;
-        own = hit ? x : own;
-        here |= hit;
-      }
-    if (here) (a.stats ? a.z_label + r0 : z_label)[r] = own;
+      for (int v = 0; v < 16; ++v) most = fmaxf(most, z(tn, v));
     most = fmaxf(most, __shfl_xor(most, 32));
     const float s = shift_of(most);
     float sum = 0.f;
@@ -179,6 +190,11 @@ struct Turn {
     for (int i = 0; i < 4; ++i) w[i] = (__bf16)y[i];
     *reinterpret_cast<bf16x4*>(own(smem) + (tm * 32 + (lane & 31)) * kPitch + (tn * 32 + 2 * v + 4 * (lane >> 5)) * 2) = w;
   }
+  // the value of a lane's row in its column `near`
+  static __device__ __forceinline__ void put_one(char* smem, int tm, int near, float p) {
+    const int lane = threadIdx.x & 63;
+    *reinterpret_cast<__bf16*>(own(smem) + (tm * 32 + (lane & 31)) * kPitch + (near + 4 * (lane >> 5)) * 2) = (__bf16)p;
+  }
   // at(row): offset of a row; `cols` whole eights
   template <typename F>
   static __device__ __forceinline__ void store(char* smem, __bf16* out, int rows, int cols, F at) {
@@ -215,7 +231,7 @@ __device__ __forceinline__ void xent_grads(const XentArgs& a, int64_t r0, int64_
     const int64_t row = in ? a.map[r0 + r] : 0;
     const float lse = in ? a.row_lse[row] : 0.f, g = in ? a.grad_all * (a.grad ? a.grad[row] : 1.f) : 0.f;
     const int64_t far = (in ? (int64_t)a.labels[row] - a.class0 : -1) - c0 - column_of<C>(0, 0);
-    const int near = far >= 0 && far < C::TN * 32 ? (int)far : -1;
+    const int near = far >= 0 && far < C::TN * 32 && far + column_of<C>(0, 0) < cols ? (int)far : -1;
 #pragma unroll
     for (int tn = 0; tn < C::TN; ++tn)
 #pragma unroll
@@ -223,13 +239,25 @@ __device__ __forceinline__ void xent_grads(const XentArgs& a, int64_t r0, int64_
         float y[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          y[i] = exp_of(acc[tm][tn][v + i] + b[tn][v + i] - lse) * g - (near == tn * 32 + 2 * v + i ? g : 0.f);
+          y[i] = exp_of(acc[tm][tn][v + i] + b[tn][v + i] - lse) * g;
           if (!WHOLE) y[i] = in && column_of<C>(tn, v + i) < cols ? y[i] : 0.f;
           sums[tn][v + i] += y[i];
         }
         if constexpr (C::kTurned) Turn<C>::put(smem, tm, tn, v, y);
         else if (in) store_four(P + (int64_t)r * a.ldp + column_of<C>(tn, v), y, stored - column_of<C>(tn, v));
       }
+    const bool here = ours<C>(near);
+    if (__any(here)) {                              // the label's own value, over what was stored
+      const float p = exp_of(value_at<C>(acc[tm], b, near) - lse) * g - g;
+#pragma unroll
+      for (int tn = 0; tn < C::TN; ++tn)
+#pragma unroll
+        for (int v = 0; v < 16; ++v) sums[tn][v] -= near == tn * 32 + 8 * (v / 4) + v % 4 ? g : 0.f;
+      if (here) {
+        if constexpr (C::kTurned) Turn<C>::put_one(smem, tm, near, p);
+        else P[(int64_t)r * a.ldp + column_of<C>(0, 0) + near] = (S)p;
+      }
+    }
   }
   if constexpr (C::kTurned) Turn<C>::store(smem, P, rows, stored, [&](int r) { return r * a.ldp; });
   if (!a.bias_parts) return;
@@ -293,8 +321,9 @@ __device__ __forceinline__ void xent_rows(const XentArgs& a, int32_t split, int6
 
 // Tiles in bands of eight rows of them, rows fastest, so that the tiles that an XCD has at a time share both operands' rows
 constexpr int kXentBand = 8;
-template <typename C>
-__global__ __launch_bounds__(C::kThreads) void xent_kernel(const XentArgs a) {
+// (a kernel for each mode: in one for all of them the longest epilogue's registers were the products', 170 k x 128 of 172 classes 298 us for 262)
+template <typename C, int MODE>
+__global__ __launch_bounds__(C::kThreads, 2) void xent_kernel(const XentArgs a) {
   constexpr int BM = C::WM * C::TM * 32, BN = C::WN * C::TN * 32;
   __shared__ __attribute__((aligned(1024))) char smem[C::kLds];
   const int64_t m = a.count ? (*a.count < 0 ? 0 : *a.count > a.m ? a.m : *a.count) : a.m;
@@ -316,10 +345,10 @@ __global__ __launch_bounds__(C::kThreads) void xent_kernel(const XentArgs a) {
          reinterpret_cast<const S*>(a.W) + c0 * (C::kTransW ? a.ldw : 1) + (int64_t)from * (C::kTransW ? 1 : a.ldw), cols, sum, padded, smem, acc);
   __syncthreads();
   const bool whole = rows == BM && cols == BN;
-  if (a.mode == kXentStats) {
+  if constexpr (MODE == kXentStats) {
     if (whole) xent_stats<C, true>(a, r0, col, c0, rows, cols, smem, acc);
     else xent_stats<C, false>(a, r0, col, c0, rows, cols, smem, acc);
-  } else if (a.mode == kXentGrads) {
+  } else if constexpr (MODE == kXentGrads) {
     if (whole) xent_grads<C, true>(a, r0, row, c0, rows, cols, smem, acc);
     else xent_grads<C, false>(a, r0, row, c0, rows, cols, smem, acc);
   } else xent_rows<C>(a, split, r0, c0, rows, cols, smem, acc);
@@ -337,7 +366,10 @@ int xent_launch(const XentArgs& args, hipStream_t s) {
   const int64_t blocks = ceil_div(args.m, C::WM * C::TM * 32) * args.col_tiles * args.splits, most = most_blocks(C::kThreads) / 8 * 8;
   XentArgs a = args;
   for (a.first = 0; a.first < blocks; a.first += most) {
-    xent_kernel<C><<<dim3((uint32_t)(blocks - a.first < most ? blocks - a.first : most)), C::kThreads, 0, s>>>(a);
+    const dim3 grid((uint32_t)(blocks - a.first < most ? blocks - a.first : most));
+    if (a.mode == kXentStats) xent_kernel<C, kXentStats><<<grid, C::kThreads, 0, s>>>(a);
+    else if (a.mode == kXentGrads) xent_kernel<C, kXentGrads><<<grid, C::kThreads, 0, s>>>(a);
+    else xent_kernel<C, kXentRows><<<grid, C::kThreads, 0, s>>>(a);
     SAGNN_LAUNCH_CHECK();
   }
   return SAGNN_OK;

@@ -21,7 +21,7 @@ constexpr int kListThreads = 256;
 constexpr int64_t kPieceBytes = int64_t(512) << 20;
 // Classes of a piece, and pieces, which dH's sums are added over in turn
 constexpr int64_t kSumBytes = int64_t(512) << 20;
-constexpr int32_t kPieceLeast = 1024, kPieceMost = 16384, kPiecesMost = 384;
+constexpr int32_t kPieceLeast = 1024, kPieceMost = 32768, kPiecesMost = 384;
 
 __device__ __forceinline__ bool known(int32_t label, int32_t classes) { return label >= 0 && label < classes; }
 
