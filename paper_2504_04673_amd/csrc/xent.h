@@ -321,37 +321,157 @@ __device__ __forceinline__ void xent_rows(const XentArgs& a, int32_t split, int6
 
 // Tiles in bands of eight rows of them, rows fastest, so that the tiles that an XCD has at a time share both operands' rows
 constexpr int kXentBand = 8;
+struct XentTile { int64_t r0, c0; int32_t row, col, split, rows, cols, from, sum, padded; };
+template <int BM, int BN>
+__device__ __forceinline__ bool xent_find(const XentArgs& a, XentTile& t) {
+  const int64_t m = a.count ? (*a.count < 0 ? 0 : *a.count > a.m ? a.m : *a.count) : a.m;
+  const int32_t row_tiles = (int32_t)((m + BM - 1) / BM), tiles = row_tiles * a.col_tiles;
+  const int64_t block = a.first + blockIdx.x, total = (int64_t)tiles * a.splits;
+  if (block >= total) return false;
+  int32_t id = xcd_run((int32_t)block, (int32_t)total);
+  t.split = id / tiles;
+  id -= t.split * tiles;
+  const int32_t band = id / (kXentBand * a.col_tiles), in = id - band * kXentBand * a.col_tiles;
+  const int32_t high = row_tiles - band * kXentBand < kXentBand ? row_tiles - band * kXentBand : kXentBand;
+  t.row = band * kXentBand + in % high;
+  t.col = in / high;
+  t.r0 = (int64_t)t.row * BM;
+  t.c0 = (int64_t)t.col * BN;
+  t.rows = (int)(m - t.r0 < BM ? m - t.r0 : BM);
+  t.cols = (int)(a.cols - t.c0 < BN ? a.cols - t.c0 : BN);
+  t.from = t.split * a.share;
+  t.sum = a.sum - t.from < a.share ? a.sum - t.from : a.share;
+  t.padded = a.sum - t.from <= a.share ? a.padded - t.from : a.share;
+  return true;
+}
 // (a kernel for each mode: in one for all of them the longest epilogue's registers were the products', 170 k x 128 of 172 classes 298 us for 262)
 template <typename C, int MODE>
 __global__ __launch_bounds__(C::kThreads, 2) void xent_kernel(const XentArgs a) {
   constexpr int BM = C::WM * C::TM * 32, BN = C::WN * C::TN * 32;
   __shared__ __attribute__((aligned(1024))) char smem[C::kLds];
-  const int64_t m = a.count ? (*a.count < 0 ? 0 : *a.count > a.m ? a.m : *a.count) : a.m;
-  const int32_t row_tiles = (int32_t)((m + BM - 1) / BM), tiles = row_tiles * a.col_tiles;
-  const int64_t block = a.first + blockIdx.x, total = (int64_t)tiles * a.splits;
-  if (block >= total) return;
-  int32_t id = xcd_run((int32_t)block, (int32_t)total);
-  const int32_t split = id / tiles;
-  id -= split * tiles;
-  const int32_t band = id / (kXentBand * a.col_tiles), in = id - band * kXentBand * a.col_tiles;
-  const int32_t high = row_tiles - band * kXentBand < kXentBand ? row_tiles - band * kXentBand : kXentBand;
-  const int32_t row = band * kXentBand + in % high, col = in / high;
-  const int64_t r0 = (int64_t)row * BM, c0 = (int64_t)col * BN;
-  const int rows = (int)(m - r0 < BM ? m - r0 : BM), cols = (int)(a.cols - c0 < BN ? a.cols - c0 : BN);
-  const int32_t from = split * a.share, sum = a.sum - from < a.share ? a.sum - from : a.share, padded = a.sum - from <= a.share ? a.padded - from : a.share;
+  XentTile t;
+  if (!xent_find<BM, BN>(a, t)) return;
   using S = typename C::S;
   floatx16 acc[C::TM][C::TN];
-  C::run(a, reinterpret_cast<const S*>(a.X) + r0 * a.ldx + from, rows,
-         reinterpret_cast<const S*>(a.W) + c0 * (C::kTransW ? a.ldw : 1) + (int64_t)from * (C::kTransW ? 1 : a.ldw), cols, sum, padded, smem, acc);
+  C::run(a, reinterpret_cast<const S*>(a.X) + t.r0 * a.ldx + t.from, t.rows,
+         reinterpret_cast<const S*>(a.W) + t.c0 * (C::kTransW ? a.ldw : 1) + (int64_t)t.from * (C::kTransW ? 1 : a.ldw), t.cols, t.sum, t.padded, smem, acc);
   __syncthreads();
-  const bool whole = rows == BM && cols == BN;
+  const bool whole = t.rows == BM && t.cols == BN;
   if constexpr (MODE == kXentStats) {
-    if (whole) xent_stats<C, true>(a, r0, col, c0, rows, cols, smem, acc);
-    else xent_stats<C, false>(a, r0, col, c0, rows, cols, smem, acc);
+    if (whole) xent_stats<C, true>(a, t.r0, t.col, t.c0, t.rows, t.cols, smem, acc);
+    else xent_stats<C, false>(a, t.r0, t.col, t.c0, t.rows, t.cols, smem, acc);
   } else if constexpr (MODE == kXentGrads) {
-    if (whole) xent_grads<C, true>(a, r0, row, c0, rows, cols, smem, acc);
-    else xent_grads<C, false>(a, r0, row, c0, rows, cols, smem, acc);
-  } else xent_rows<C>(a, split, r0, c0, rows, cols, smem, acc);
+    if (whole) xent_grads<C, true>(a, t.r0, t.row, t.c0, t.rows, t.cols, smem, acc);
+    else xent_grads<C, false>(a, t.r0, t.row, t.c0, t.rows, t.cols, smem, acc);
+  } else xent_rows<C>(a, t.split, t.r0, t.c0, t.rows, t.cols, smem, acc);
+}
+
+// Few rows, or few tiles for the CUs: tiles of 32 x 32, whose summed index the eight wavefronts of a workgroup share, each through LDS of its own.
+// Bound by a wavefront's chain of loads, which is eight times shorter; and where a few rows meet many classes, by the weights' bytes, of which more are on
+// their way (2 rows of 1831 by 39483 classes, fp32: 32 x 128 took 137 us, 2.1 TB/s).  A thread ends with two neighbouring columns of a row.
+constexpr int kThinWaves = 8;
+template <typename S, int PREC, bool TRB, int BK, int MODE>
+__global__ __launch_bounds__(kThinWaves * 64) void xent_thin_kernel(const XentArgs a) {
+  using SA = TileShape<PREC, false, 32, BK>;
+  using SB = TileShape<PREC, TRB, 32, BK>;
+  constexpr int kRow = 36, kSums = 32 * kRow * 4, kOwn = SA::kBytes + SB::kBytes > kSums ? SA::kBytes + SB::kBytes : kSums;
+  __shared__ __attribute__((aligned(16))) char smem[kThinWaves * kOwn];
+  XentTile t;
+  if (!xent_find<32, 32>(a, t)) return;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const S* X = reinterpret_cast<const S*>(a.X) + t.r0 * a.ldx + t.from;
+  const S* W = reinterpret_cast<const S*>(a.W) + t.c0 * (TRB ? 1 : a.ldw) + (int64_t)t.from * (TRB ? a.ldw : 1);
+  TileLoad<S, PREC, false, 32, BK, 64> la;
+  TileLoad<S, PREC, TRB, 32, BK, 64> lb;
+  char* own = smem + wave * kOwn;
+  float* sums = reinterpret_cast<float*>(smem);
+  const int r = tid >> 4, c = (tid & 15) * 2;
+  float y[2] = {0.f, 0.f};
+  // a run of each wavefront at a time
+  const int each = kThinWaves * run_length((t.sum + kThinWaves - 1) / kThinWaves, a.run);
+#pragma unroll 1
+  for (int from = 0; from < t.sum; from += each) {
+    const int end = t.sum - from <= each ? t.sum : from + each;
+    auto load = [&](int k) {
+      la.load(X + k, a.ldx, t.rows, end - k < BK ? end - k : BK, lane);
+      lb.load(W + (int64_t)k * (TRB ? a.ldw : 1), a.ldw, t.cols, end - k < BK ? end - k : BK, lane);
+    };
+    floatx16 acc[1][1];
+#pragma unroll
+    for (int v = 0; v < 16; ++v) acc[0][0][v] = 0.f;
+    int k = from + wave * BK;
+    if (k < end) load(k);
+    for (; k < end; k += kThinWaves * BK) {
+      la.store(own, lane);
+      lb.store(own + SA::kBytes, lane);
+      asm volatile("" ::: "memory");                // (a wavefront's own LDS accesses are in order)
+      if (k + kThinWaves * BK < end) load(k + kThinWaves * BK);
+      tile_multiply<PREC, false, TRB, 1, 1, 1, 1, BK>(own, own + SA::kBytes, acc, lane);
+      asm volatile("" ::: "memory");
+    }
+    __syncthreads();
+#pragma unroll
+    for (int v = 0; v < 16; v += 4)
+      *reinterpret_cast<float4*>(sums + (wave * 32 + (lane & 31)) * kRow + 2 * v + 4 * (lane >> 5)) =
+          make_float4(acc[0][0][v], acc[0][0][v + 1], acc[0][0][v + 2], acc[0][0][v + 3]);
+    __syncthreads();
+    float all[2] = {0.f, 0.f};
+#pragma unroll
+    for (int w = 0; w < kThinWaves; ++w) {
+      const float2 x = *reinterpret_cast<const float2*>(sums + (w * 32 + r) * kRow + c);
+      all[0] += x.x; all[1] += x.y;
+    }
+    y[0] += all[0]; y[1] += all[1];
+    __syncthreads();                              // (the sums lie where the next run's operands do)
+  }
+  const bool in = r < t.rows;
+  if constexpr (MODE == kXentRows) {
+    float* to = a.sums ? a.sums + (t.split * a.m + t.r0 + r) * a.cols + t.c0 + c : nullptr;
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+      if (in && c + i < t.cols) {
+        if (!to) reinterpret_cast<S*>(a.out)[(int64_t)a.map[t.r0 + r] * a.ldo + t.c0 + c + i] = (S)y[i];
+        else to[i] = a.add ? to[i] + y[i] : y[i];
+      }
+    return;
+  }
+  const int64_t row = !in ? 0 : MODE == kXentGrads ? (int64_t)a.map[t.r0 + r] : t.r0 + r;
+  const int64_t label = (in ? (int64_t)a.labels[row] - a.class0 : -1) - t.c0;
+#pragma unroll
+  for (int i = 0; i < 2; ++i) y[i] = c + i < t.cols ? y[i] + (a.bias ? a.bias[t.c0 + c + i] : 0.f) : -INFINITY;
+  if constexpr (MODE == kXentStats) {
+    float most = fmaxf(y[0], y[1]);
+    for (int d = 1; d < 16; d *= 2) most = fmaxf(most, __shfl_xor(most, d));
+    const float s = shift_of(most), sum = sixteen_sum(exp_of(y[0] - s) + exp_of(y[1] - s));
+    const bool here = label >= 0 && label < t.cols && (label & ~1) == c;
+    const float z = sixteen_sum(here ? y[label & 1] : 0.f);                   // (all other lanes' are zeros)
+    if (!in) return;
+    if (a.stats) {
+      if (here) a.z_label[row] = y[label & 1];
+      if ((tid & 15) == 0) a.stats[(int64_t)t.col * a.m + row] = make_float2(most, sum);
+    } else if ((tid & 15) == 0) {
+      const float lse = lse_of(most, sum);
+      a.lse[row] = lse;
+      a.loss[row] = label >= 0 && label < a.classes ? lse - z : 0.f;
+    }
+  } else {
+    const float lse = in ? a.row_lse[row] : 0.f, g = in ? a.grad_all * (a.grad ? a.grad[row] : 1.f) : 0.f;
+    S* P = reinterpret_cast<S*>(a.P) + (t.r0 + r) * a.ldp + t.c0;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      y[i] = in && c + i < t.cols ? exp_of(y[i] - lse) * g - (label == c + i ? g : 0.f) : 0.f;
+      if (in && t.c0 + c + i < a.stored) P[c + i] = (S)y[i];
+    }
+    if (!a.bias_parts) return;
+    *reinterpret_cast<float2*>(sums + r * kRow + c) = make_float2(y[0], y[1]);
+    __syncthreads();
+    if (tid < t.cols) {
+      float x = 0.f;
+#pragma unroll 8
+      for (int i = 0; i < 32; ++i) x += sums[i * kRow + tid];
+      a.bias_parts[(int64_t)t.row * a.cols + t.c0 + tid] = x;
+    }
+  }
 }
 
 #define SAGNN_XENT_MODE(name) int xent_##name(const XentArgs& a, int tile, bool trans_w, hipStream_t s);
@@ -361,18 +481,31 @@ SAGNN_XENT_MODE(fp32_bf16x3)
 SAGNN_XENT_MODE(bf16)
 #undef SAGNN_XENT_MODE
 
-template <typename C>
-int xent_launch(const XentArgs& args, hipStream_t s) {
-  const int64_t blocks = ceil_div(args.m, C::WM * C::TM * 32) * args.col_tiles * args.splits, most = most_blocks(C::kThreads) / 8 * 8;
-  XentArgs a = args;
+// launch(arguments, grid), several times where there are more tiles of `rows` rows than one launch takes
+template <typename F>
+int xent_launches(XentArgs a, int rows, int threads, F launch) {
+  const int64_t blocks = ceil_div(a.m, rows) * a.col_tiles * a.splits, most = most_blocks(threads) / 8 * 8;
   for (a.first = 0; a.first < blocks; a.first += most) {
-    const dim3 grid((uint32_t)(blocks - a.first < most ? blocks - a.first : most));
-    if (a.mode == kXentStats) xent_kernel<C, kXentStats><<<grid, C::kThreads, 0, s>>>(a);
-    else if (a.mode == kXentGrads) xent_kernel<C, kXentGrads><<<grid, C::kThreads, 0, s>>>(a);
-    else xent_kernel<C, kXentRows><<<grid, C::kThreads, 0, s>>>(a);
+    launch(a, dim3((uint32_t)(blocks - a.first < most ? blocks - a.first : most)));
     SAGNN_LAUNCH_CHECK();
   }
   return SAGNN_OK;
+}
+template <typename C>
+int xent_launch(const XentArgs& args, hipStream_t s) {
+  return xent_launches(args, C::WM * C::TM * 32, C::kThreads, [&](const XentArgs& a, dim3 grid) {
+    if (a.mode == kXentStats) xent_kernel<C, kXentStats><<<grid, C::kThreads, 0, s>>>(a);
+    else if (a.mode == kXentGrads) xent_kernel<C, kXentGrads><<<grid, C::kThreads, 0, s>>>(a);
+    else xent_kernel<C, kXentRows><<<grid, C::kThreads, 0, s>>>(a);
+  });
+}
+template <typename S, int PREC, int BK, bool TRB>
+int xent_thin(const XentArgs& args, hipStream_t s) {
+  return xent_launches(args, 32, kThinWaves * 64, [&](const XentArgs& a, dim3 grid) {
+    if (a.mode == kXentStats) xent_thin_kernel<S, PREC, TRB, BK, kXentStats><<<grid, kThinWaves * 64, 0, s>>>(a);
+    else if (a.mode == kXentGrads) xent_thin_kernel<S, PREC, TRB, BK, kXentGrads><<<grid, kThinWaves * 64, 0, s>>>(a);
+    else xent_thin_kernel<S, PREC, TRB, BK, kXentRows><<<grid, kThinWaves * 64, 0, s>>>(a);
+  });
 }
 template <typename S, int PREC, int BK, bool TRB, bool LONG>
 int xent_small_as(const XentArgs& a, int tile, hipStream_t s) {
@@ -383,6 +516,8 @@ int xent_small_as(const XentArgs& a, int tile, hipStream_t s) {
 template <typename S, int PREC, int BK>
 int xent_small(const XentArgs& a, int tile, bool trans_w, hipStream_t s) {
   const bool several = a.share > a.run;
+  constexpr int kThinStep = BK == 32 && PREC != SAGNN_GEMM_FP32 ? 16 : BK;
+  if (tile == kThin) return trans_w ? xent_thin<S, PREC, kThinStep, false>(a, s) : xent_thin<S, PREC, kThinStep, true>(a, s);
   if (trans_w) return several ? xent_small_as<S, PREC, BK, false, true>(a, tile, s) : xent_small_as<S, PREC, BK, false, false>(a, tile, s);
   return several ? xent_small_as<S, PREC, BK, true, true>(a, tile, s) : xent_small_as<S, PREC, BK, true, false>(a, tile, s);
 }

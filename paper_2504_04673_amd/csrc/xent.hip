@@ -194,7 +194,7 @@ TilePick pick_tile(int32_t dtype, int32_t prec, int ways, int64_t m, int64_t col
   double least = 1e300;
   // values of a 128 x 128 tile that a CU multiplies in a microsecond (half of the operations), and bytes that the chip moves in one
   const double a_us = (dtype == SAGNN_BF16 ? 740e6 : prec == SAGNN_GEMM_FP32 ? 133e6 : prec == SAGNN_GEMM_BF16 ? 430e6 : 171e6) / 512, bytes_us = 4e6;
-  for (int tile : {kTile128, kTile128x64, kTile32x128, kDirect256, kStaged256x128, kStaged128x256}) {
+  for (int tile : {kTile128, kTile128x64, kTile32x128, kThin, kDirect256, kStaged256x128, kStaged128x256}) {
     const TileCost c = tile_cost(dtype, prec, tile);
     if (c.rate == 0 || (tile == kDirect256 && ways != kDirect) || ((tile == kStaged256x128 || tile == kStaged128x256) && ways != kStaged)) continue;
     const int64_t h = grouped_tile_rows(tile), w = grouped_tile_cols(tile);
@@ -230,7 +230,7 @@ int launch(const XentArgs& args, int32_t dtype, int32_t prec, const TilePick& pi
   const int tile = pick.tile;
   a.splits = pick.splits;
   a.share = pick.share;
-  a.run = grouped_run(products(dtype, prec), a.share);
+  a.run = grouped_run(products(dtype, prec), tile == kThin ? ceil_div(a.share, kThinWaves) : a.share);
   a.col_tiles = (int32_t)ceil_div(a.cols, grouped_tile_cols(tile));
   if (dtype == SAGNN_BF16) return xent_bf16(a, tile, trans_w, s);
   return prec == SAGNN_GEMM_FP32 ? xent_fp32(a, tile, trans_w, s) : prec == SAGNN_GEMM_BF16 ? xent_fp32_bf16(a, tile, trans_w, s) : xent_fp32_bf16x3(a, tile, trans_w, s);
