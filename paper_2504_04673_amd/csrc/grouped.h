@@ -23,6 +23,22 @@ struct GroupedArgs {
   int32_t pairs;                                 // weight gradient: numbers of pairs of a chunk and a group
   int32_t first;                                 // workgroups of the launches before this one
   int32_t run;                                   // of the summed index that one set of sums takes (grouped_run)
+  const int32_t* listed;                         // weight gradient, may be NULL: where *listed is m, X and G lie elsewhere:
+  const void* X2; int64_t ldx2;
+  const void* G2; int64_t ldg2;
+};
+// The operands of a weight gradient
+template <typename S>
+struct GroupedSides {
+  const S *X, *G;
+  int64_t ldx, ldg;
+  __device__ __forceinline__ explicit GroupedSides(const GroupedArgs& a) {
+    const bool other = a.listed && *a.listed == a.m;
+    X = reinterpret_cast<const S*>(other ? a.X2 : a.X);
+    G = reinterpret_cast<const S*>(other ? a.G2 : a.G);
+    ldx = other ? a.ldx2 : a.ldx;
+    ldg = other ? a.ldg2 : a.ldg;
+  }
 };
 
 // Sums of equal terms: every addition of a serial run may round the same way, by up to half a unit in the last place of a sum that
@@ -607,8 +623,9 @@ __global__ __launch_bounds__(WM * WN * 64, LONG && !(sizeof(S) == 4 && PREC == S
   const int rows = (int)(a.kdim - k0 < BM ? a.kdim - k0 : BM), cols = (int)(a.nout - c0 < BN ? a.nout - c0 : BN);
   floatx16 acc[TM][TN];
   float* out = (p.cut ? a.partial + grouped_partial_slot(p) * a.kdim * a.nout : a.dW + (int64_t)p.g * a.kdim * a.nout) + k0 * a.nout + c0;
-  tile_product<S, PREC, true, true, WM, WN, TM, TN, BK, LONG>(reinterpret_cast<const S*>(a.X) + p.r0 * a.ldx + k0, a.ldx, rows,
-                                                              reinterpret_cast<const S*>(a.G) + p.r0 * a.ldg + c0, a.ldg, cols, p.r1 - p.r0, smem, acc, a.run);
+  const GroupedSides<S> in(a);
+  tile_product<S, PREC, true, true, WM, WN, TM, TN, BK, LONG>(in.X + p.r0 * in.ldx + k0, in.ldx, rows, in.G + p.r0 * in.ldg + c0, in.ldg, cols, p.r1 - p.r0,
+                                                              smem, acc, a.run);
   tile_fours<WM, WN, TM, TN>(acc, [&](int r, int c, float (&y)[4]) { if (r < rows) store_four(out + (int64_t)r * a.nout + c, y, cols - c); });
 }
 
@@ -628,6 +645,9 @@ inline int grouped_tile_cols(int tile) {
 // beginning and end are worth.  Small tiles are several to a CU, which hides both; the large ones are alone there.
 struct TileCost { double rate, ends; };
 TileCost tile_cost(int32_t dtype, int32_t prec, int tile);
+
+// dW of grouped_gemm_bwd for arguments that are filled in but for the launch's; ws: as much as it says
+int grouped_weights(const GroupedArgs& a, int32_t dtype, int32_t prec, hipStream_t s);
 
 // a product of `blocks` workgroups; per operand mode (and storage type)
 #define SAGNN_GROUPED_MODE(name)                                                                                       \

@@ -181,6 +181,14 @@ int join_weights(const GroupedArgs& a, hipStream_t s) {
 }
 
 }  // namespace
+
+int grouped_weights(const GroupedArgs& args, int32_t dtype, int32_t prec, hipStream_t s) {
+  GroupedArgs a = args;
+  const Launch l = plan_weights(a, dtype, prec);
+  if (l.blocks < 0) return SAGNN_EINVAL;
+  const int rc = launch_weights(a, l, dtype, prec, s);
+  return rc == SAGNN_OK ? join_weights(a, s) : rc;
+}
 }  // namespace sagnn
 
 SAGNN_EXPORT int grouped_gemm_act(int32_t dtype, const void* d_X, int64_t ldx, const void* d_W, int64_t ldw, int64_t stride_w,

@@ -296,12 +296,13 @@ __device__ __forceinline__ void direct_tn_tile(const GroupedArgs& a, int32_t blo
   const int rows = (int)(a.kdim - k0 < BM ? a.kdim - k0 : BM), cols = (int)(a.nout - c0 < BN ? a.nout - c0 : BN);
   floatx16 acc[TM][TN];
   float* out = (p.cut ? a.partial + grouped_partial_slot(p) * a.kdim * a.nout : a.dW + (int64_t)p.g * a.kdim * a.nout) + k0 * a.nout + c0;
-  const __bf16 *X = reinterpret_cast<const __bf16*>(a.X) + p.r0 * a.ldx + k0, *G = reinterpret_cast<const __bf16*>(a.G) + p.r0 * a.ldg + c0;
+  const GroupedSides<__bf16> in(a);
+  const __bf16 *X = in.X + p.r0 * in.ldx + k0, *G = in.G + p.r0 * in.ldg + c0;
   const int32_t sum = (int32_t)(p.r1 - p.r0), each = run_length(sum, a.run);
 #pragma unroll 1
   for (int32_t from = 0;; from += each) {
     const bool last = sum - from <= each;
-    direct_product<true, true, 2, WN, TM, TN>(X + from * a.ldx, a.ldx, rows, G + from * a.ldg, a.ldg, cols, last ? sum - from : each, smem, acc);
+    direct_product<true, true, 2, WN, TM, TN>(X + from * in.ldx, in.ldx, rows, G + from * in.ldg, in.ldg, cols, last ? sum - from : each, smem, acc);
     const int tid = this_thread(), lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int ra = (wave / WN) * TM * 32 + (lane & 31), rb = (wave % WN) * TN * 32 + 4 * (lane >> 5);
 #pragma unroll

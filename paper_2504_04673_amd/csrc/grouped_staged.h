@@ -219,8 +219,9 @@ __global__ __launch_bounds__(WM * WN * 64) void grouped_staged_tn_kernel(const G
   const int64_t k0 = (int64_t)(tile / a.col_tiles) * BM, c0 = (int64_t)(tile % a.col_tiles) * BN;
   const int rows = (int)(a.kdim - k0 < BM ? a.kdim - k0 : BM), cols = (int)(a.nout - c0 < BN ? a.nout - c0 : BN);
   floatx16 acc[2][2];
-  staged_product<PREC, true, true, WM, WN, 2, 2, LONG>(reinterpret_cast<const float*>(a.X) + p.r0 * a.ldx + k0, a.ldx, rows,
-                                                       reinterpret_cast<const float*>(a.G) + p.r0 * a.ldg + c0, a.ldg, cols, p.r1 - p.r0, smem, acc, a.run);
+  const GroupedSides<float> in(a);
+  staged_product<PREC, true, true, WM, WN, 2, 2, LONG>(in.X + p.r0 * in.ldx + k0, in.ldx, rows, in.G + p.r0 * in.ldg + c0, in.ldg, cols, p.r1 - p.r0, smem, acc,
+                                                       a.run);
   float* out = (p.cut ? a.partial + grouped_partial_slot(p) * a.kdim * a.nout : a.dW + (int64_t)p.g * a.kdim * a.nout) + k0 * a.nout + c0;
   tile_fours<WM, WN, 2, 2>(acc, [&](int r, int c, float (&y)[4]) { if (r < rows) store_four(out + (int64_t)r * a.nout + c, y, cols - c); });
 }

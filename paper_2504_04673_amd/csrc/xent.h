@@ -16,6 +16,7 @@ struct XentArgs {
   const void* W; int64_t ldw;                // sum x cols, or cols x sum
   int64_t m;                                 // rows at most
   const int32_t* count;                      // how many there are, on the device; NULL: m
+  const void* all; int64_t ldall;            // may be NULL: what X is where *count is m
   int32_t cols, sum, run, mode;
   int32_t padded;                            // X's columns with zeros behind `sum`
   bool wide;                                 // results in rows that begin on 16 bytes, whole eights of them
@@ -51,8 +52,8 @@ struct SmallProduct {
   static constexpr int kLds = kOperands > xent_lds(WM, WN, TM, TN) ? kOperands : xent_lds(WM, WN, TM, TN);
   static constexpr bool kTransW = !TRB;
   static constexpr bool kTurned = false;
-  static __device__ __forceinline__ void run(const XentArgs& a, const S* A, int rows, const S* B, int cols, int sum, int, char* smem, floatx16 (&acc)[TM][TN]) {
-    tile_product<S, PREC, false, TRB, WM, WN, TM, TN, BK, LONG>(A, a.ldx, rows, B, a.ldw, cols, sum, smem, acc, a.run);
+  static __device__ __forceinline__ void run(const XentArgs& a, const S* A, int64_t lda, int rows, const S* B, int cols, int sum, int, char* smem, floatx16 (&acc)[TM][TN]) {
+    tile_product<S, PREC, false, TRB, WM, WN, TM, TN, BK, LONG>(A, lda, rows, B, a.ldw, cols, sum, smem, acc, a.run);
   }
 };
 
@@ -321,6 +322,9 @@ __device__ __forceinline__ void xent_rows(const XentArgs& a, int32_t split, int6
 
 // Tiles in bands of eight rows of them, rows fastest, so that the tiles that an XCD has at a time share both operands' rows
 constexpr int kXentBand = 8;
+// X as it is for this call
+struct XentRows { const void* X; int64_t ld; };
+__device__ __forceinline__ XentRows xent_x(const XentArgs& a) { return a.all && *a.count == a.m ? XentRows{a.all, a.ldall} : XentRows{a.X, a.ldx}; }
 struct XentTile { int64_t r0, c0; int32_t row, col, split, rows, cols, from, sum, padded; };
 template <int BM, int BN>
 __device__ __forceinline__ bool xent_find(const XentArgs& a, XentTile& t) {
@@ -353,7 +357,8 @@ __global__ __launch_bounds__(C::kThreads, 2) void xent_kernel(const XentArgs a) 
   if (!xent_find<BM, BN>(a, t)) return;
   using S = typename C::S;
   floatx16 acc[C::TM][C::TN];
-  C::run(a, reinterpret_cast<const S*>(a.X) + t.r0 * a.ldx + t.from, t.rows,
+  const XentRows x = xent_x(a);
+  C::run(a, reinterpret_cast<const S*>(x.X) + t.r0 * x.ld + t.from, x.ld, t.rows,
          reinterpret_cast<const S*>(a.W) + t.c0 * (C::kTransW ? a.ldw : 1) + (int64_t)t.from * (C::kTransW ? 1 : a.ldw), t.cols, t.sum, t.padded, smem, acc);
   __syncthreads();
   const bool whole = t.rows == BM && t.cols == BN;
@@ -379,7 +384,8 @@ __global__ __launch_bounds__(kThinWaves * 64) void xent_thin_kernel(const XentAr
   XentTile t;
   if (!xent_find<32, 32>(a, t)) return;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const S* X = reinterpret_cast<const S*>(a.X) + t.r0 * a.ldx + t.from;
+  const XentRows x = xent_x(a);
+  const S* X = reinterpret_cast<const S*>(x.X) + t.r0 * x.ld + t.from;
   const S* W = reinterpret_cast<const S*>(a.W) + t.c0 * (TRB ? 1 : a.ldw) + (int64_t)t.from * (TRB ? a.ldw : 1);
   TileLoad<S, PREC, false, 32, BK, 64> la;
   TileLoad<S, PREC, TRB, 32, BK, 64> lb;
@@ -393,7 +399,7 @@ __global__ __launch_bounds__(kThinWaves * 64) void xent_thin_kernel(const XentAr
   for (int from = 0; from < t.sum; from += each) {
     const int end = t.sum - from <= each ? t.sum : from + each;
     auto load = [&](int k) {
-      la.load(X + k, a.ldx, t.rows, end - k < BK ? end - k : BK, lane);
+      la.load(X + k, x.ld, t.rows, end - k < BK ? end - k : BK, lane);
       lb.load(W + (int64_t)k * (TRB ? a.ldw : 1), a.ldw, t.cols, end - k < BK ? end - k : BK, lane);
     };
     floatx16 acc[1][1];

@@ -15,7 +15,7 @@
 namespace sagnn {
 namespace {
 
-constexpr int kListBlocks = 4096;                 // of rows, at most
+constexpr int kListBlocks = 1024;                 // of rows, at most (each reads all their counts)
 constexpr int kListThreads = 256;
 // Bytes of P at a time, about: a piece that the memory-side cache holds would be smaller, but dH's sums are read and written once for each.
 constexpr int64_t kPieceBytes = int64_t(512) << 20;
@@ -38,22 +38,33 @@ __global__ __launch_bounds__(kListThreads) void label_count_kernel(const int32_t
   if (threadIdx.x == 0) counts[blockIdx.x] = room[0] + room[1] + room[2] + room[3];
 }
 
-// map[i] = row of the i-th label; H's rows one behind the other in rows of ldc values (zeros behind the k there are); zeros in dH's rows without
-// one.  bounds = {0, how many}.
+// map[i] = row of the i-th label; H's rows one behind the other in rows of ldc values (zeros behind the k there are), unless every row has one and
+// `needed` is not set: then H itself will do; zeros in dH's rows without one.  bounds = {0, how many}.
 template <typename T>
 __global__ __launch_bounds__(kListThreads) void label_list_kernel(const int32_t* __restrict__ labels, int64_t m, int64_t each, int32_t classes,
                                                                   const int32_t* __restrict__ counts, int32_t* __restrict__ map, int32_t* __restrict__ bounds,
                                                                   const T* __restrict__ H, int64_t ldh, int32_t k, T* __restrict__ rows, int64_t ldc,
-                                                                  T* __restrict__ dH, int64_t lddh, int lanes) {
+                                                                  T* __restrict__ dH, int64_t lddh, int lanes, bool needed) {
   __shared__ int32_t room[kListThreads / 64];
   __shared__ int32_t place[kListThreads];          // of a row of the round: its number in the list, or -1
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  int32_t before = 0;
-  for (int b = threadIdx.x; b < (int)blockIdx.x; b += kListThreads) before += counts[b];
-  for (int d = 1; d < 64; d *= 2) before += __shfl_xor(before, d);
-  if (lane == 0) room[wave] = before;
+  int32_t before = 0, every = 0;                   // before this block; all
+  for (int b = threadIdx.x; b < (int)gridDim.x; b += kListThreads) {
+    const int32_t n = counts[b];
+    every += n;
+    before += b < (int)blockIdx.x ? n : 0;
+  }
+  for (int d = 1; d < 64; d *= 2) {
+    before += __shfl_xor(before, d);
+    every += __shfl_xor(every, d);
+  }
+  if (lane == 0) {
+    room[wave] = before;
+    place[wave] = every;
+  }
   __syncthreads();
   before = room[0] + room[1] + room[2] + room[3];
+  every = place[0] + place[1] + place[2] + place[3];
   const int64_t end = (blockIdx.x + 1) * each < m ? (blockIdx.x + 1) * each : m;
   for (int64_t r0 = blockIdx.x * each; r0 < end; r0 += kListThreads) {
     const int64_t r = r0 + threadIdx.x;
@@ -72,6 +83,7 @@ __global__ __launch_bounds__(kListThreads) void label_list_kernel(const int32_t*
     const int n = end - r0 < kListThreads ? (int)(end - r0) : kListThreads, own = threadIdx.x & (lanes - 1);
     for (int i = threadIdx.x / lanes; i < n; i += kListThreads / lanes) {
       const int32_t to = place[i];
+      if (to >= 0 && !needed && every == m) break;
       if (to >= 0)
         for (int c = own * 8; c < ldc; c += lanes * 8) {
           const auto w = load_eight(H + (r0 + i) * ldh + c, k - c, k);
@@ -189,7 +201,8 @@ bool whole_granules(const void* p, int64_t ld, int64_t width) { return aligned16
 // Tile of a product, m rows by cols, `sum` deep, and shares of the summed index (several only with `room` for sums of their own): what the fullest CU
 // multiplies, by the tiles' rates, and what it costs to write and read the shares' sums.
 struct TilePick { int tile; int32_t splits, share; };
-TilePick pick_tile(int32_t dtype, int32_t prec, int ways, int64_t m, int64_t cols, int64_t sum, int32_t room) {
+// joined: several tiles of columns cost a launch more.
+TilePick pick_tile(int32_t dtype, int32_t prec, int ways, int64_t m, int64_t cols, int64_t sum, int32_t room, bool joined = false) {
   TilePick best{kTile128, 1, (int32_t)sum};
   double least = 1e300;
   // values of a 128 x 128 tile that a CU multiplies in a microsecond (half of the operations), and bytes that the chip moves in one
@@ -205,7 +218,7 @@ TilePick pick_tile(int32_t dtype, int32_t prec, int ways, int64_t m, int64_t col
       if (tile == kDirect256 && share > kRunRounded) continue;
       const int64_t tiles = whole * n;
       const double turns = tiles <= 256 ? 1.25 : tiles < 4 * 256 ? (double)ceil_div(tiles, 256) : tiles / 256.;
-      const double cost = turns * h * w * (share + c.ends) / c.rate / a_us + (n > 1 ? 12. * n * m * cols / bytes_us + 5. : 0.);
+      const double cost = turns * h * w * (share + c.ends) / c.rate / a_us + (n > 1 ? 12. * n * m * cols / bytes_us + 5. : 0.) + (joined && cols > w ? 5. : 0.);
       if (cost < least) {
         least = cost;
         best = {tile, (int32_t)n, (int32_t)share};
@@ -244,7 +257,7 @@ struct Room {
 struct FwdPlan { TilePick tile; int32_t col_tiles; size_t stats, z_label, total; };
 FwdPlan fwd_plan(int32_t dtype, int32_t prec, int ways, int64_t m, int32_t kdim, int32_t classes) {
   FwdPlan p{};
-  p.tile = pick_tile(dtype, prec, ways, m, classes, kdim, 1);
+  p.tile = pick_tile(dtype, prec, ways, m, classes, kdim, 1, true);
   p.col_tiles = (int32_t)ceil_div(classes, grouped_tile_cols(p.tile.tile));
   if (p.col_tiles > 1) {
     Room room;
@@ -304,7 +317,7 @@ BwdPlan bwd_plan(int32_t dtype, int32_t prec, int64_t m, int32_t kdim, int32_t c
 
 template <typename T>
 int list_labels(const BwdPlan& p, char* ws, const int32_t* labels, int64_t m, int32_t classes, const void* H, int64_t ldh, int32_t k, void* dH, int64_t lddh,
-                hipStream_t s) {
+                bool needed, hipStream_t s) {
   // (many small blocks: 8192 rows of 1024 in blocks of 256 took 429 us)
   int64_t each = ceil_div(m, kListBlocks);
   if (each < 16) each = 16;
@@ -315,7 +328,7 @@ int list_labels(const BwdPlan& p, char* ws, const int32_t* labels, int64_t m, in
   label_count_kernel<<<dim3(blocks), kListThreads, 0, s>>>(labels, m, each, classes, counts);
   SAGNN_LAUNCH_CHECK();
   label_list_kernel<T><<<dim3(blocks), kListThreads, 0, s>>>(labels, m, each, classes, counts, map, bounds, (const T*)H, ldh, k, (T*)(ws + p.rows), p.ldc,
-                                                            (T*)dH, lddh, lanes);
+                                                            (T*)dH, lddh, lanes, needed);
   SAGNN_LAUNCH_CHECK();
   return SAGNN_OK;
 }
@@ -407,15 +420,18 @@ SAGNN_EXPORT int softmax_xent_bwd(int32_t dtype, const void* d_H, int64_t ldh, c
   if (ws_bytes < p.total) return SAGNN_ECAPACITY;
   char* ws = (char*)d_ws;
   hipStream_t s = (hipStream_t)stream;
-  int rc = dtype == SAGNN_BF16 ? list_labels<__bf16>(p, ws, d_labels, m, n_classes, d_H, ldh, kdim, d_dH, lddh, s)
-                               : list_labels<float>(p, ws, d_labels, m, n_classes, d_H, ldh, kdim, d_dH, lddh, s);
+  // Where every row has a label H itself is taken, if it lies as well as the copy would (617 k x 1344 of 50 classes, three terms, all labelled: 5.8 ms
+  // with the copy).  Only the device knows.
+  const bool itself = dtype == SAGNN_BF16 ? whole_granules(d_H, ldh, kdim) : ldh <= kLargeLd;
+  int rc = dtype == SAGNN_BF16 ? list_labels<__bf16>(p, ws, d_labels, m, n_classes, d_H, ldh, kdim, d_dH, lddh, !itself, s)
+                               : list_labels<float>(p, ws, d_labels, m, n_classes, d_H, ldh, kdim, d_dH, lddh, !itself, s);
   const int32_t* bounds = (const int32_t*)(ws + p.bounds);
   TilePick rows{};
   for (int32_t at = 0; at < n_classes && rc == SAGNN_OK; at += p.piece) {
     const int32_t n = n_classes - at < p.piece ? n_classes - at : p.piece;
     XentArgs a{};
     a.X = ws + p.rows; a.ldx = p.ldc; a.W = (const char*)d_W + (size_t)at * (transW ? ldw : 1) * size; a.ldw = ldw; a.m = m; a.count = bounds + 1;
-    a.cols = n; a.sum = kdim; a.mode = kXentGrads; a.bias = d_bias ? d_bias + at : nullptr; a.labels = d_labels; a.class0 = at; a.classes = n_classes;
+    a.all = itself ? d_H : nullptr; a.ldall = ldh; a.cols = n; a.sum = kdim; a.mode = kXentGrads; a.bias = d_bias ? d_bias + at : nullptr; a.labels = d_labels; a.class0 = at; a.classes = n_classes;
     a.map = (const int32_t*)(ws + p.map); a.row_lse = d_lse; a.grad = d_grad; a.grad_all = (float)grad_all; a.P = ws + p.P; a.ldp = p.ldp;
     a.stored = (int32_t)round_up((size_t)n, 8); a.bias_parts = d_dbias ? (float*)(ws + p.bias) : nullptr;
     a.padded = (int32_t)p.ldc;
@@ -448,8 +464,16 @@ SAGNN_EXPORT int softmax_xent_bwd(int32_t dtype, const void* d_H, int64_t ldh, c
       // (fp32 weights whose piece lies in one place are written there)
       const bool there = dtype == SAGNN_F32 && (transW || p.pieces == 1);
       float* dW = there ? (float*)d_dW + (size_t)at * (transW ? kdim : 1) : (float*)(ws + p.weights);
-      rc = transW ? grouped_gemm_bwd(dtype, a.P, p.ldp, nullptr, 0, 0, bounds, 1, m, n, kdim, prec, a.X, p.ldc, nullptr, 0, nullptr, 0, dW, ws + p.parts, p.parts_bytes, stream)
-                  : grouped_gemm_bwd(dtype, a.X, p.ldc, nullptr, 0, 0, bounds, 1, m, kdim, n, prec, a.P, p.ldp, nullptr, 0, nullptr, 0, dW, ws + p.parts, p.parts_bytes, stream);
+      GroupedArgs w{};
+      w.off = bounds; w.groups = 1; w.m = m; w.dW = dW; w.partial = (float*)(ws + p.parts);
+      w.X = transW ? a.P : a.X; w.ldx = transW ? p.ldp : p.ldc; w.kdim = transW ? n : kdim;
+      w.G = transW ? a.X : a.P; w.ldg = transW ? p.ldc : p.ldp; w.nout = transW ? kdim : n;
+      if (itself) {
+        w.listed = bounds + 1;
+        w.X2 = transW ? a.P : d_H; w.ldx2 = transW ? p.ldp : ldh;
+        w.G2 = transW ? d_H : a.P; w.ldg2 = transW ? ldh : p.ldp;
+      }
+      rc = grouped_weights(w, dtype, prec, s);
       if (rc == SAGNN_OK && !there) {
         const int64_t rows = transW ? n : kdim, ldt = transW ? kdim : n_classes;
         const int32_t cols = transW ? kdim : n;

@@ -10,8 +10,8 @@ struct DirectProduct {
   static constexpr int WM = 2, WN = 4, TM = 4, TN = 2, kThreads = 512;
   static constexpr int kLds = direct_lds(256, 256, WN) > xent_lds(WM, WN, TM, TN) ? direct_lds(256, 256, WN) : xent_lds(WM, WN, TM, TN);
   static constexpr bool kTransW = !TRB, kTurned = true;
-  static __device__ __forceinline__ void run(const XentArgs& a, const S* A, int rows, const S* B, int cols, int sum, int padded, char* smem, floatx16 (&acc)[TM][TN]) {
-    direct_product<false, TRB, WM, WN, TM, TN>(A, a.ldx, rows, B, a.ldw, cols, padded, smem, acc, sum);
+  static __device__ __forceinline__ void run(const XentArgs& a, const S* A, int64_t lda, int rows, const S* B, int cols, int sum, int padded, char* smem, floatx16 (&acc)[TM][TN]) {
+    direct_product<false, TRB, WM, WN, TM, TN>(A, lda, rows, B, a.ldw, cols, padded, smem, acc, sum);
   }
 };
 }  // namespace

@@ -12,8 +12,8 @@ struct StagedProduct {
   static constexpr int kOperands = 2 * (StagedOperand<PREC, false, WM * 64, kThreads>::kBytes + StagedOperand<PREC, TRB, WN * 64, kThreads>::kBytes);
   static constexpr int kLds = kOperands > xent_lds(WM, WN, TM, TN) ? kOperands : xent_lds(WM, WN, TM, TN);
   static constexpr bool kTransW = !TRB, kTurned = false;
-  static __device__ __forceinline__ void run(const XentArgs& a, const S* A, int rows, const S* B, int cols, int sum, int, char* smem, floatx16 (&acc)[TM][TN]) {
-    staged_product<PREC, false, TRB, WM, WN, TM, TN, LONG>(A, a.ldx, rows, B, a.ldw, cols, sum, smem, acc, a.run);
+  static __device__ __forceinline__ void run(const XentArgs& a, const S* A, int64_t lda, int rows, const S* B, int cols, int sum, int, char* smem, floatx16 (&acc)[TM][TN]) {
+    staged_product<PREC, false, TRB, WM, WN, TM, TN, LONG>(A, lda, rows, B, a.ldw, cols, sum, smem, acc, a.run);
   }
 };
 

@@ -80,7 +80,7 @@ def inputs(seed, m, k, n, dtype, trans, biased, labelled, strided):
 @pytest.mark.parametrize("m,k,n", SHAPES)
 def test_loss_and_gradients(m, k, n, mode):
     dtype = torch.bfloat16 if mode == "bf16" else torch.float32
-    for i, (trans, biased, labelled, strided) in enumerate([(False, True, 1.0, False), (True, False, 0.4, False), (True, True, 0.7, True), (False, False, 0.5, True)]):
+    for i, (trans, biased, labelled, strided) in enumerate([(False, True, 1.0, False), (True, False, 0.4, False), (True, True, 0.7, True), (False, False, 0.5, True), (False, True, 1.0, True)]):
         H, W, labels, bias = inputs(m + k + n + i, m, k, n, dtype, trans, biased, labelled, strided)
         g = 1.0 / m if i % 2 else normal(gen(i), m, scale=1.0 / m)
         what = f"case {i}"
