@@ -5,10 +5,13 @@ the loss's gradient and subtracts.
 
     T = A H,  Z[r] = T[r] W[type(r)],  H' = ReLU(group_norm(Z))
 
-    python -m paper_2504_04673_amd.typed_gcn [--vertices N] [--types K] [--steps S]
+    python -m paper_2504_04673_amd.typed_gcn [--vertices N] [--types K] [--steps S] [--classes C]
 
 makes a random graph with random types, orders its vertices by type (spmm_perm_from_labels) and prints the loss,
-the gradients' norm and the time of each step.
+the gradients' norm and the time of each step.  With --classes the network is a deeper one, of residual blocks that are normalised row by row,
+and learns classes of its vertices, two in five of which have a label:
+
+    Y = rms_norm(S),  S' = S + dropout(ReLU((A Y) W1[type]) W2[type]),  loss = cross entropy of softmax(Y' head + bias)
 """
 from __future__ import annotations
 
@@ -106,6 +109,89 @@ class TypedGCN:
         return diff.square().mean(), norm
 
 
+class TypedResidualGCN:
+    """Residual blocks of one width over the types of `graph`, each with a hidden layer, and a linear classifier behind the last.  The sum that
+    the blocks add to is normalised row by row where a block reads it; p: share of a block's values that fall while training, p_in: of the features'.
+    Masks are drawn from (seed, step), so that a step's backward pass needs none of them."""
+
+    def __init__(self, graph: TypedGraph, width, hidden, blocks, classes, p=0.1, p_in=0.0, prec=sagnn.GEMM_FP32, seed=0):
+        self.graph, self.p, self.p_in, self.prec, self.seed = graph, p, p_in, prec, seed
+        dev, types = graph.off.device, graph.off.numel() - 1
+        gen = torch.Generator(device=dev).manual_seed(seed)
+
+        def normal(*shape, scale):
+            return torch.randn(shape, generator=gen, device=dev) * scale
+
+        self.W1 = [normal(types, width, hidden, scale=width ** -0.5) for _ in range(blocks)]
+        self.W2 = [normal(types, hidden, width, scale=(hidden * blocks) ** -0.5) for _ in range(blocks)]
+        self.gamma = [torch.ones(width, device=dev) for _ in range(blocks + 1)]
+        self.head, self.bias = normal(classes, width, scale=width ** -0.5), torch.zeros(classes, device=dev)
+        self.ws = graph.prepare(width)
+
+    def parameters(self):
+        return [*self.W1, *self.W2, *self.gamma, self.head, self.bias]
+
+    def forward(self, H, step=0, training=True):
+        """The last block's normalised rows, and what the backward pass needs.  step: an integer, or an int64 tensor of one element on the device
+        (a captured graph counts it up)."""
+        p = self.p if training else 0.0
+        if training and self.p_in:
+            H = sagnn.dropout_add(H, self.p_in, self.seed, step)
+        Y, S, rstd = sagnn.rms_norm(H, self.gamma[0])
+        kept = [(S, rstd, None, None)]
+        for i, (W1, W2) in enumerate(zip(self.W1, self.W2)):
+            T = self.graph.multiply(Y, self.ws)
+            U = sagnn.grouped_gemm_act(T, W1, self.graph.off, prec=self.prec, act=sagnn.ACT_RELU)
+            Z = sagnn.grouped_gemm_act(U, W2, self.graph.off, prec=self.prec)
+            Y, S, rstd = sagnn.rms_norm(Z, self.gamma[i + 1], residual=S, p=p, seed=self.seed + 1 + i, offset=step)
+            kept.append((S, rstd, T, U))
+        return Y, kept
+
+    def backward(self, G, kept, step=0, dhead=None, dbias=None):
+        """Gradients in the order of parameters(), from G = dLoss/dY and those of the classifier."""
+        n = len(self.W1)
+        dW1, dW2, dgamma, dS = [None] * n, [None] * n, [None] * (n + 1), None
+        for i in reversed(range(n)):
+            S, rstd, T, U = kept[i + 1]
+            dZ, dS, dgamma[i + 1] = sagnn.rms_norm_bwd(S, G, rstd, self.gamma[i + 1], grad_sum=dS, p=self.p, seed=self.seed + 1 + i, offset=step)
+            dU, dW2[i] = sagnn.grouped_gemm_bwd(U, self.W2[i], self.graph.off, dZ, mask=U, prec=self.prec)
+            dT, dW1[i] = sagnn.grouped_gemm_bwd(T, self.W1[i], self.graph.off, dU, prec=self.prec)
+            G = self.graph.multiply(dT, self.ws)
+        S, rstd = kept[0][:2]
+        dgamma[0] = sagnn.rms_norm_bwd(S, G, rstd, self.gamma[0], grad_sum=dS, want_dx=False)[2]
+        return [*dW1, *dW2, *dgamma, dhead, dbias]
+
+    def gradients(self, H, labels, count, step=0):
+        """Loss of each row and the gradients of the mean over the `count` rows that have a label."""
+        Y, kept = self.forward(H, step)
+        loss, lse = sagnn.softmax_xent(Y, self.head, labels, bias=self.bias, transW=True, prec=self.prec)
+        G, dhead, dbias = sagnn.softmax_xent_bwd(Y, self.head, labels, lse, 1.0 / count, bias=self.bias, transW=True, prec=self.prec)
+        return loss, self.backward(G, kept, step, dhead, dbias)
+
+    def step(self, H, labels, count, step=0, rate=0.5, max_norm=1.0):
+        """One step of gradient descent.  labels: int32, outside the classes for a row that has none.  Returns (mean loss over the rows that have
+        one, norm of the gradients before they were clipped), both on the device."""
+        loss, grads = self.gradients(H, labels, count, step)
+        norm = sagnn.grad_clip_norm(grads, max_norm)
+        for q, g in zip(self.parameters(), grads):
+            q.sub_(g, alpha=rate)
+        return loss.sum() / count, norm
+
+    def rows_e4m3(self, H):
+        """What the network makes of every vertex, in rows of 8 bits and a scale each (spmm_pack_rows_e4m3 gathers them)."""
+        kept = self.forward(H, training=False)[1]
+        return sagnn.rms_norm_e4m3(kept[-1][0], self.gamma[-1])[:2]
+
+
+def synthetic_classes(n, n_types, f, classes, degree=8, seed=0):
+    """synthetic's graph and features, and a class for two vertices in five (-1 for the others): (graph, H, labels, how many)."""
+    graph, H, target = synthetic(n, n_types, f, classes, degree, seed)
+    gen = torch.Generator(device="cuda").manual_seed(seed + 2)
+    labelled = torch.rand(n, generator=gen, device="cuda") < 0.4
+    labels = torch.where(labelled, target.argmax(1), -1).int()
+    return graph, H, labels, int(labelled.sum())
+
+
 def synthetic(n, n_types, f, f_out, degree=8, seed=0):
     """A random graph with random types on the GPU, its rows ordered by type: (graph, H, target)."""
     from . import synth
@@ -125,7 +211,17 @@ def main():
     ap.add_argument("--vertices", type=int, default=100_000)
     ap.add_argument("--types", type=int, default=8)
     ap.add_argument("--steps", type=int, default=20)
+    ap.add_argument("--classes", type=int, default=0)
     args = ap.parse_args()
+    if args.classes:
+        graph, H, labels, count = synthetic_classes(args.vertices, args.types, 128, args.classes)
+        net = TypedResidualGCN(graph, 128, 256, 3, args.classes)
+        for step in range(args.steps):
+            t = time.perf_counter()
+            loss, norm = net.step(H, labels, count, step)
+            loss, norm = float(loss), float(norm)
+            print(f"step {step}: loss {loss:.5f}, norm {norm:.5f}, {(time.perf_counter() - t) * 1e3:.2f} ms", flush=True)
+        return
     graph, H, target = synthetic(args.vertices, args.types, 64, 16)
     net = TypedGCN(graph, (64, 128, 128, 16))
     for step in range(args.steps):
