@@ -17,6 +17,7 @@ namespace {
 
 constexpr int kListBlocks = 1024;                 // of rows, at most (each reads all their counts)
 constexpr int kListThreads = 256;
+constexpr int kListFew = 4096;                    // rows whose labels every block counts itself, a launch less
 // Bytes of P at a time, about: a piece that the memory-side cache holds would be smaller, but dH's sums are read and written once for each.
 constexpr int64_t kPieceBytes = int64_t(512) << 20;
 // Classes of a piece, and pieces, which dH's sums are added over in turn
@@ -39,21 +40,33 @@ __global__ __launch_bounds__(kListThreads) void label_count_kernel(const int32_t
 }
 
 // map[i] = row of the i-th label; H's rows one behind the other in rows of ldc values (zeros behind the k there are), unless every row has one and
-// `needed` is not set: then H itself will do; zeros in dH's rows without one.  bounds = {0, how many}.
+// `needed` is not set: then H itself will do; zeros in dH's rows without one, and in `clear`.  bounds = {0, how many}.  counts NULL: few rows, whose labels each
+// block counts itself.
 template <typename T>
 __global__ __launch_bounds__(kListThreads) void label_list_kernel(const int32_t* __restrict__ labels, int64_t m, int64_t each, int32_t classes,
                                                                   const int32_t* __restrict__ counts, int32_t* __restrict__ map, int32_t* __restrict__ bounds,
                                                                   const T* __restrict__ H, int64_t ldh, int32_t k, T* __restrict__ rows, int64_t ldc,
-                                                                  T* __restrict__ dH, int64_t lddh, int lanes, bool needed) {
+                                                                  T* __restrict__ dH, int64_t lddh, int lanes, bool needed, float* __restrict__ clear,
+                                                                  int32_t n_clear) {
   __shared__ int32_t room[kListThreads / 64];
   __shared__ int32_t place[kListThreads];          // of a row of the round: its number in the list, or -1
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   int32_t before = 0, every = 0;                   // before this block; all
-  for (int b = threadIdx.x; b < (int)gridDim.x; b += kListThreads) {
-    const int32_t n = counts[b];
-    every += n;
-    before += b < (int)blockIdx.x ? n : 0;
+  if (counts) {
+    for (int b = threadIdx.x; b < (int)gridDim.x; b += kListThreads) {
+      const int32_t n = counts[b];
+      every += n;
+      before += b < (int)blockIdx.x ? n : 0;
+    }
+  } else {
+    for (int r = threadIdx.x; r < (int)m; r += kListThreads) {
+      const int32_t n = known(labels[r], classes);
+      every += n;
+      before += r < (int)blockIdx.x * (int)each ? n : 0;
+    }
   }
+  if (clear)
+    for (int64_t i = (int64_t)blockIdx.x * kListThreads + threadIdx.x; i < n_clear; i += (int64_t)gridDim.x * kListThreads) clear[i] = 0.f;
   for (int d = 1; d < 64; d *= 2) {
     before += __shfl_xor(before, d);
     every += __shfl_xor(every, d);
@@ -171,14 +184,14 @@ __global__ __launch_bounds__(256) void xent_rows_kernel(const float* __restrict_
 
 // A piece's dW from fp32 into its place
 template <typename T>
-__global__ __launch_bounds__(256) void xent_weights_kernel(const float* __restrict__ from, int64_t rows, int32_t cols, T* __restrict__ to, int64_t ldt) {
+__global__ __launch_bounds__(256) void xent_weights_kernel(const float* __restrict__ from, int64_t ldf, int64_t rows, int32_t cols, T* __restrict__ to, int64_t ldt) {
   const int64_t fours = (cols + 3) / 4, all = rows * fours;
   for (int64_t i = blockIdx.x * 256ll + threadIdx.x; i < all; i += gridDim.x * 256ll) {
     const int64_t r = i / fours;
     const int c = (int)(i - r * fours) * 4;
     float y[4];
 #pragma unroll
-    for (int e = 0; e < 4; ++e) y[e] = c + e < cols ? from[r * cols + c + e] : 0.f;
+    for (int e = 0; e < 4; ++e) y[e] = c + e < cols ? from[r * ldf + c + e] : 0.f;
     store_four(to + r * ldt + c, y, cols - c);
   }
 }
@@ -268,6 +281,10 @@ FwdPlan fwd_plan(int32_t dtype, int32_t prec, int ways, int64_t m, int32_t kdim,
   return p;
 }
 
+// dW's products have the listed rows' and P's ends in them, zeros, so that bfloat16 ones go straight into LDS whatever the widths are: they end in a place
+// of their own anyway
+int32_t padded_width(int32_t dtype, int32_t width) { return dtype == SAGNN_BF16 ? (int32_t)round_up((size_t)width, 8) : width; }
+
 struct BwdPlan {
   int32_t piece, pieces;                     // classes of a piece
   int32_t splits;                            // shares of them that there is room for in dH's sums
@@ -286,10 +303,11 @@ BwdPlan bwd_plan(int32_t dtype, int32_t prec, int64_t m, int32_t kdim, int32_t c
   p.ldp = (int64_t)round_up((size_t)p.piece, 8);
   p.ldc = (int64_t)round_up((size_t)kdim, 8);
   // dW's products, in either order, of a whole piece and of the last (which may be cut into more parts)
+  const int32_t kw = padded_width(dtype, kdim);
   for (int32_t n : {p.piece, classes - (p.pieces - 1) * p.piece}) {
     size_t one = 0, two = 0;
-    grouped_gemm_bwd_workspace_bytes(m, 1, kdim, n, &one);
-    grouped_gemm_bwd_workspace_bytes(m, 1, n, kdim, &two);
+    grouped_gemm_bwd_workspace_bytes(m, 1, kw, padded_width(dtype, n), &one);
+    grouped_gemm_bwd_workspace_bytes(m, 1, padded_width(dtype, n), kw, &two);
     p.parts_bytes = one > p.parts_bytes ? one : p.parts_bytes;
     p.parts_bytes = two > p.parts_bytes ? two : p.parts_bytes;
   }
@@ -308,7 +326,7 @@ BwdPlan bwd_plan(int32_t dtype, int32_t prec, int64_t m, int32_t kdim, int32_t c
     if (n > splits) splits = n;
   }
   p.sums = room.take(p.pieces > 1 || splits > 1 ? (size_t)splits * share : 0);
-  p.weights = room.take((size_t)p.piece * kdim * 4);
+  p.weights = room.take((size_t)padded_width(dtype, p.piece) * kw * 4);
   p.parts = room.take(p.parts_bytes);
   p.bias = room.take((size_t)ceil_div(rows, 32) * p.piece * 4);
   p.total = room.off;
@@ -317,7 +335,7 @@ BwdPlan bwd_plan(int32_t dtype, int32_t prec, int64_t m, int32_t kdim, int32_t c
 
 template <typename T>
 int list_labels(const BwdPlan& p, char* ws, const int32_t* labels, int64_t m, int32_t classes, const void* H, int64_t ldh, int32_t k, void* dH, int64_t lddh,
-                bool needed, hipStream_t s) {
+                bool needed, float* clear, int32_t n_clear, hipStream_t s) {
   // (many small blocks: 8192 rows of 1024 in blocks of 256 took 429 us)
   int64_t each = ceil_div(m, kListBlocks);
   if (each < 16) each = 16;
@@ -325,10 +343,14 @@ int list_labels(const BwdPlan& p, char* ws, const int32_t* labels, int64_t m, in
   while (lanes < 64 && lanes * 8 < p.ldc) lanes *= 2;
   const uint32_t blocks = (uint32_t)ceil_div(m > 0 ? m : 1, each);
   int32_t *counts = (int32_t*)(ws + p.counts), *map = (int32_t*)(ws + p.map), *bounds = (int32_t*)(ws + p.bounds);
-  label_count_kernel<<<dim3(blocks), kListThreads, 0, s>>>(labels, m, each, classes, counts);
-  SAGNN_LAUNCH_CHECK();
+  if (m <= kListFew) {
+    counts = nullptr;
+  } else {
+    label_count_kernel<<<dim3(blocks), kListThreads, 0, s>>>(labels, m, each, classes, counts);
+    SAGNN_LAUNCH_CHECK();
+  }
   label_list_kernel<T><<<dim3(blocks), kListThreads, 0, s>>>(labels, m, each, classes, counts, map, bounds, (const T*)H, ldh, k, (T*)(ws + p.rows), p.ldc,
-                                                            (T*)dH, lddh, lanes, needed);
+                                                            (T*)dH, lddh, lanes, needed, clear, n_clear);
   SAGNN_LAUNCH_CHECK();
   return SAGNN_OK;
 }
@@ -423,8 +445,15 @@ SAGNN_EXPORT int softmax_xent_bwd(int32_t dtype, const void* d_H, int64_t ldh, c
   // Where every row has a label H itself is taken, if it lies as well as the copy would (617 k x 1344 of 50 classes, three terms, all labelled: 5.8 ms
   // with the copy).  Only the device knows.
   const bool itself = dtype == SAGNN_BF16 ? whole_granules(d_H, ldh, kdim) : ldh <= kLargeLd;
-  int rc = dtype == SAGNN_BF16 ? list_labels<__bf16>(p, ws, d_labels, m, n_classes, d_H, ldh, kdim, d_dH, lddh, !itself, s)
-                               : list_labels<float>(p, ws, d_labels, m, n_classes, d_H, ldh, kdim, d_dH, lddh, !itself, s);
+  // The bias's gradient of one tile of rows is its sums: written there, over zeros for the case that there is no such row
+  auto logits = [&](const void* W, int32_t n) {
+    return pick_tile(dtype, prec, logits_ways(dtype, ws + p.rows, p.ldc, p.ldc, W, ldw, transW != 0, kdim, n), m, n, kdim, 1);
+  };
+  const int32_t last = n_classes - (p.pieces - 1) * p.piece;
+  const bool direct_bias = d_dbias && m <= grouped_tile_rows(logits(d_W, p.piece).tile) && m <= grouped_tile_rows(logits(d_W, last).tile);
+  float* clear = direct_bias ? d_dbias : nullptr;
+  int rc = dtype == SAGNN_BF16 ? list_labels<__bf16>(p, ws, d_labels, m, n_classes, d_H, ldh, kdim, d_dH, lddh, !itself, clear, n_classes, s)
+                               : list_labels<float>(p, ws, d_labels, m, n_classes, d_H, ldh, kdim, d_dH, lddh, !itself, clear, n_classes, s);
   const int32_t* bounds = (const int32_t*)(ws + p.bounds);
   TilePick rows{};
   for (int32_t at = 0; at < n_classes && rc == SAGNN_OK; at += p.piece) {
@@ -433,11 +462,11 @@ SAGNN_EXPORT int softmax_xent_bwd(int32_t dtype, const void* d_H, int64_t ldh, c
     a.X = ws + p.rows; a.ldx = p.ldc; a.W = (const char*)d_W + (size_t)at * (transW ? ldw : 1) * size; a.ldw = ldw; a.m = m; a.count = bounds + 1;
     a.all = itself ? d_H : nullptr; a.ldall = ldh; a.cols = n; a.sum = kdim; a.mode = kXentGrads; a.bias = d_bias ? d_bias + at : nullptr; a.labels = d_labels; a.class0 = at; a.classes = n_classes;
     a.map = (const int32_t*)(ws + p.map); a.row_lse = d_lse; a.grad = d_grad; a.grad_all = (float)grad_all; a.P = ws + p.P; a.ldp = p.ldp;
-    a.stored = (int32_t)round_up((size_t)n, 8); a.bias_parts = d_dbias ? (float*)(ws + p.bias) : nullptr;
+    a.stored = (int32_t)round_up((size_t)n, 8); a.bias_parts = direct_bias ? d_dbias + at : d_dbias ? (float*)(ws + p.bias) : nullptr;
     a.padded = (int32_t)p.ldc;
-    const TilePick tile = pick_tile(dtype, prec, logits_ways(dtype, a.X, p.ldc, p.ldc, a.W, ldw, transW != 0, kdim, n), m, n, kdim, 1);
+    const TilePick tile = logits(a.W, n);
     if (m > 0) rc = launch(a, dtype, prec, tile, transW != 0, s);
-    if (rc == SAGNN_OK && d_dbias) {
+    if (rc == SAGNN_OK && d_dbias && !direct_bias) {
       xent_bias_kernel<<<dim3((uint32_t)ceil_div(n, 16)), 256, 0, s>>>(a.bias_parts, bounds, grouped_tile_rows(tile.tile), n, d_dbias + at);
       SAGNN_LAUNCH_CHECK();
     }
@@ -466,8 +495,9 @@ SAGNN_EXPORT int softmax_xent_bwd(int32_t dtype, const void* d_H, int64_t ldh, c
       float* dW = there ? (float*)d_dW + (size_t)at * (transW ? kdim : 1) : (float*)(ws + p.weights);
       GroupedArgs w{};
       w.off = bounds; w.groups = 1; w.m = m; w.dW = dW; w.partial = (float*)(ws + p.parts);
-      w.X = transW ? a.P : a.X; w.ldx = transW ? p.ldp : p.ldc; w.kdim = transW ? n : kdim;
-      w.G = transW ? a.X : a.P; w.ldg = transW ? p.ldc : p.ldp; w.nout = transW ? kdim : n;
+      const int32_t kw = padded_width(dtype, kdim), nw = padded_width(dtype, n);
+      w.X = transW ? a.P : a.X; w.ldx = transW ? p.ldp : p.ldc; w.kdim = transW ? nw : kw;
+      w.G = transW ? a.X : a.P; w.ldg = transW ? p.ldc : p.ldp; w.nout = transW ? kw : nw;
       if (itself) {
         w.listed = bounds + 1;
         w.X2 = transW ? a.P : d_H; w.ldx2 = transW ? p.ldp : ldh;
@@ -480,8 +510,8 @@ SAGNN_EXPORT int softmax_xent_bwd(int32_t dtype, const void* d_H, int64_t ldh, c
         const int64_t blocks = ceil_div(rows * ceil_div(cols, 4), 256);
         const dim3 grid((uint32_t)(blocks < 4096 ? blocks : 4096));
         const size_t first = (size_t)at * (transW ? kdim : 1);
-        if (dtype == SAGNN_BF16) xent_weights_kernel<__bf16><<<grid, 256, 0, s>>>(dW, rows, cols, (__bf16*)d_dW + first, ldt);
-        else xent_weights_kernel<float><<<grid, 256, 0, s>>>(dW, rows, cols, (float*)d_dW + first, ldt);
+        if (dtype == SAGNN_BF16) xent_weights_kernel<__bf16><<<grid, 256, 0, s>>>(dW, w.nout, rows, cols, (__bf16*)d_dW + first, ldt);
+        else xent_weights_kernel<float><<<grid, 256, 0, s>>>(dW, w.nout, rows, cols, (float*)d_dW + first, ldt);
         SAGNN_LAUNCH_CHECK();
       }
     }

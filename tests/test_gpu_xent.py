@@ -123,6 +123,8 @@ def test_rows_without_a_label_meet_nothing(dtype, n):
     loss, lse = sagnn.softmax_xent(clean, W, none)
     dH, dW, dbias = sagnn.softmax_xent_bwd(H, W, none, lse, 0.01, bias=bias)
     assert not loss.any() and not dH.any() and not dW.any() and not dbias.any()
+    few = sagnn.softmax_xent_bwd(H[:5], W, none[:5], lse[:5], 0.01, bias=bias)
+    assert not any(t.any() for t in few)
     z = clean[:0]
     loss, lse = sagnn.softmax_xent(z, W, labels[:0])
     dH, dW, dbias = sagnn.softmax_xent_bwd(z, W, labels[:0], lse, bias=bias)
