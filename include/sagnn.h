@@ -756,7 +756,9 @@ int spmm_pack_rows_e4m3(const void* d_Q, int64_t ldq, const float* d_scale, int6
  * rounded).  Infinite and NaN logits give what the formula gives: a bias of -inf takes a class out.
  * Any kdim up to SAGNN_GROUPED_MAX_WIDTH, n_classes up to SAGNN_XENT_MAX_CLASSES, any leading dimensions not below the width, tensors aligned to their element; rows that begin on 16
  * bytes are read faster.  d_dH, d_dW, d_dbias may be NULL each.  Outputs must not overlap inputs or each other.  Nothing is waited for.
- * d_ws: softmax_xent_workspace_bytes() bytes, 16-byte aligned; NULL where that is 0 (forward, few classes).
+ * d_ws: softmax_xent_workspace_bytes() bytes, 16-byte aligned; NULL where that is 0 (forward, few classes).  Forward it is 8 bytes for each row and some 128
+ * to 256 classes; backward a copy of H, P of a piece (512 MB, or all classes' or 1024 classes' where those are fewer or more), sums of dH in fp32 where there
+ * are several pieces, a piece's dW in fp32.
  */
 #define SAGNN_XENT_MAX_CLASSES 16777216
 int softmax_xent_workspace_bytes(int32_t dtype, int64_t m, int32_t kdim, int32_t n_classes, int32_t prec, int32_t backward, size_t* bytes);

@@ -25,6 +25,7 @@ constexpr int kListFew = 4096;                    // rows whose labels every blo
 // (8192 x 1024 x 131072 bfloat16: pieces of 4096 classes 10.8 ms, 8192 13.0, 16384 9.04, 32768 8.78, 65536 8.6 to 8.9)
 constexpr int64_t kPieceBytes = int64_t(512) << 20;
 constexpr int32_t kPieceLeast = 1024, kPieceMost = 32768;
+constexpr int64_t kLeastBytes = int64_t(4) << 30;   // of P in pieces of kPieceLeast; beyond that, tens of millions of rows, they are narrower
 // Pieces at most: dH's sums are added over them in turn, in 32 bits
 constexpr int32_t kPiecesMost = 384;
 // Bytes of the sums of dH's shares
@@ -302,7 +303,8 @@ BwdPlan bwd_plan(int32_t dtype, int32_t prec, int64_t m, int32_t kdim, int32_t c
   BwdPlan p{};
   const int64_t size = dtype == SAGNN_BF16 ? 2 : 4, rows = m > 0 ? m : 1;
   int64_t most = kPieceBytes / (rows * size) / 256 * 256;
-  most = most < kPieceLeast ? kPieceLeast : most > kPieceMost ? kPieceMost : most;
+  const int32_t least = rows * size * kPieceLeast <= kLeastBytes ? kPieceLeast : 256;
+  most = most < least ? least : most > kPieceMost ? kPieceMost : most;
   if (most < ceil_div(classes, kPiecesMost)) most = ceil_div(classes, kPiecesMost);
   p.pieces = (int32_t)ceil_div(classes, most);
   p.piece = p.pieces == 1 ? classes : (int32_t)round_up((size_t)ceil_div(classes, p.pieces), 256);
@@ -311,12 +313,14 @@ BwdPlan bwd_plan(int32_t dtype, int32_t prec, int64_t m, int32_t kdim, int32_t c
   p.ldc = (int64_t)round_up((size_t)kdim, 8);
   // dW's products, in either order, of a whole piece and of the last (which may be cut into more parts)
   const int32_t kw = padded_width(dtype, kdim);
-  for (int32_t n : {p.piece, classes - (p.pieces - 1) * p.piece}) {
+  const int32_t last = classes - (p.pieces - 1) * p.piece;
+  for (int32_t n : {p.piece, last}) {
     size_t one = 0, two = 0;
     grouped_gemm_bwd_workspace_bytes(m, 1, kw, padded_width(dtype, n), &one);
     grouped_gemm_bwd_workspace_bytes(m, 1, padded_width(dtype, n), kw, &two);
     p.parts_bytes = one > p.parts_bytes ? one : p.parts_bytes;
     p.parts_bytes = two > p.parts_bytes ? two : p.parts_bytes;
+    if (last == p.piece) break;
   }
   Room room;
   p.map = room.take((size_t)rows * 4);

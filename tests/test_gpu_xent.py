@@ -256,3 +256,23 @@ def test_weights_behind_four_gigabytes():
     assert torch.all((dW[-100:].double() - want).abs() <= (2.0 ** -7 + 2e-3) * (p.abs().t().contiguous() @ H.double().abs()) + 1e-6)
     want = p @ W[-100:].double()
     assert torch.all((dH.double() - want).abs() <= (2.0 ** -7 + 2e-3) * (p.abs() @ W[-100:].double().abs()) + 1e-6)
+
+
+def test_so_many_rows_that_pieces_are_narrower():
+    """2.2 million rows by 1200 classes: P of 1024 classes would be more than 4 GiB.  Against the same call on a few of the rows."""
+    m, k, n = 2_200_000, 8, 1200
+    H, W, labels, bias = inputs(3, m, k, n, torch.bfloat16, True, True, 0.5, False)
+    loss, lse = sagnn.softmax_xent(H, W, labels, bias=bias, transW=True)
+    dH, dW, dbias = sagnn.softmax_xent_bwd(H, W, labels, lse, 1e-3, bias=bias, transW=True)
+    few = slice(m - 300, m)
+    ref = Plain(H[few], W, labels[few], bias, True, 1e-3, "bf16")
+    close(lse[few], ref.lse, ref.lse_bound, "lse")
+    close(loss[few], ref.loss, ref.loss_bound, "loss")
+    close(dH[few], ref.dH, ref.dH_bound, "dH")
+    # sums over all rows in parts of 64 bits
+    want, bound, wb, bb = 0.0, 0.0, 0.0, 0.0
+    for a in range(0, m, 100_000):
+        part = Plain(H[a:a + 100_000], W, labels[a:a + 100_000], bias, True, 1e-3, "bf16")
+        want, bound, wb, bb = want + part.dW, bound + part.dW_bound, wb + part.dbias, bb + part.dbias_bound
+    close(dW, want, bound, "dW")
+    close(dbias, wb, bb, "dbias")
