@@ -480,6 +480,17 @@ __global__ __launch_bounds__(kThinWaves * 64) void xent_thin_kernel(const XentAr
   }
 }
 
+// dW of bfloat16 tensors, rounded once where it belongs: out (rows x cols) = A^T B over the listed rows.  A and B are H and P in either order, both in rows on 16
+// bytes whose ends are padded with zeros; where *count is m, the other two.
+struct XentWeightArgs {
+  const void *A, *B, *A2, *B2;
+  int64_t lda, ldb, lda2, ldb2;
+  const int32_t* count; int64_t m;
+  int32_t rows, cols, row_tiles, col_tiles;
+  void* out; int64_t ldo; bool wide;
+};
+int xent_weights_bf16(const XentWeightArgs& a, hipStream_t s);
+
 #define SAGNN_XENT_MODE(name) int xent_##name(const XentArgs& a, int tile, bool trans_w, hipStream_t s);
 SAGNN_XENT_MODE(fp32)
 SAGNN_XENT_MODE(fp32_bf16)

@@ -191,7 +191,7 @@ __global__ __launch_bounds__(256) void xent_rows_kernel(const float* __restrict_
 
 // A piece's dW from fp32 into its place
 template <typename T>
-__global__ __launch_bounds__(256) void xent_weights_kernel(const float* __restrict__ from, int64_t ldf, int64_t rows, int32_t cols, T* __restrict__ to, int64_t ldt) {
+__global__ __launch_bounds__(256) void xent_convert_kernel(const float* __restrict__ from, int64_t ldf, int64_t rows, int32_t cols, T* __restrict__ to, int64_t ldt) {
   const int64_t fours = (cols + 3) / 4, all = rows * fours;
   for (int64_t i = blockIdx.x * 256ll + threadIdx.x; i < all; i += gridDim.x * 256ll) {
     const int64_t r = i / fours;
@@ -293,11 +293,20 @@ FwdPlan fwd_plan(int32_t dtype, int32_t prec, int ways, int64_t m, int32_t kdim,
 // of their own anyway
 int32_t padded_width(int32_t dtype, int32_t width) { return dtype == SAGNN_BF16 ? (int32_t)round_up((size_t)width, 8) : width; }
 
+// Whether dW (bfloat16) is made by tiles over all rows, rounded where it belongs, or in chunks of rows through fp32, which are joined and converted: by what each
+// takes, the first in whole turns of the CUs (microseconds; 0.027 a row of a tile, at the large tile's rate), the second with its bytes and launches.
+bool whole_weights(int32_t dtype, int64_t m, int32_t kdim, int32_t classes) {
+  const int64_t tiles = ceil_div(kdim, 256) * ceil_div(classes, 256);
+  if (dtype != SAGNN_BF16 || m > kRunRounded || tiles > INT32_MAX) return false;
+  const double one = .027 * (m + 200);
+  return one * ceil_div(tiles, 256) <= one * tiles / 256. + 12. + 12. * kdim * classes / 4e6;
+}
+
 struct BwdPlan {
   int32_t piece, pieces;                     // classes of a piece
   int32_t splits;                            // shares of them that there is room for in dH's sums
   int64_t ldp, ldc;                          // of P, of the listed rows
-  size_t map, bounds, counts, rows, P, sums, weights, parts, bias, parts_bytes, total;
+  size_t map, bounds, counts, rows, P, sums, weights, parts, bias, weights_bytes, parts_bytes, total;
 };
 BwdPlan bwd_plan(int32_t dtype, int32_t prec, int64_t m, int32_t kdim, int32_t classes) {
   BwdPlan p{};
@@ -315,6 +324,8 @@ BwdPlan bwd_plan(int32_t dtype, int32_t prec, int64_t m, int32_t kdim, int32_t c
   const int32_t kw = padded_width(dtype, kdim);
   const int32_t last = classes - (p.pieces - 1) * p.piece;
   for (int32_t n : {p.piece, last}) {
+    if (whole_weights(dtype, m, kdim, n)) continue;
+    p.weights_bytes = (size_t)padded_width(dtype, p.piece) * kw * 4;
     size_t one = 0, two = 0;
     grouped_gemm_bwd_workspace_bytes(m, 1, kw, padded_width(dtype, n), &one);
     grouped_gemm_bwd_workspace_bytes(m, 1, padded_width(dtype, n), kw, &two);
@@ -337,7 +348,7 @@ BwdPlan bwd_plan(int32_t dtype, int32_t prec, int64_t m, int32_t kdim, int32_t c
     if (n > splits) splits = n;
   }
   p.sums = room.take(p.pieces > 1 || splits > 1 ? (size_t)splits * share : 0);
-  p.weights = room.take((size_t)padded_width(dtype, p.piece) * kw * 4);
+  p.weights = room.take(p.weights_bytes);
   p.parts = room.take(p.parts_bytes);
   p.bias = room.take((size_t)ceil_div(rows, 32) * p.piece * 4);
   p.total = room.off;
@@ -500,7 +511,18 @@ SAGNN_EXPORT int softmax_xent_bwd(int32_t dtype, const void* d_H, int64_t ldh, c
         SAGNN_LAUNCH_CHECK();
       }
     }
-    if (rc == SAGNN_OK && d_dW) {
+    if (rc == SAGNN_OK && d_dW && whole_weights(dtype, m, kdim, n)) {
+      XentWeightArgs w{};
+      const void* whole = itself ? d_H : a.X;
+      const int64_t ldwhole = itself ? ldh : p.ldc;
+      w.A = transW ? a.P : a.X; w.lda = transW ? p.ldp : p.ldc; w.A2 = transW ? a.P : whole; w.lda2 = transW ? p.ldp : ldwhole;
+      w.B = transW ? a.X : a.P; w.ldb = transW ? p.ldc : p.ldp; w.B2 = transW ? whole : a.P; w.ldb2 = transW ? ldwhole : p.ldp;
+      w.count = bounds + 1; w.m = m; w.rows = transW ? n : kdim; w.cols = transW ? kdim : n;
+      w.row_tiles = (int32_t)ceil_div(w.rows, 256); w.col_tiles = (int32_t)ceil_div(w.cols, 256);
+      w.ldo = transW ? kdim : n_classes; w.out = (__bf16*)d_dW + (size_t)at * (transW ? kdim : 1);
+      w.wide = aligned16(w.out) && w.ldo % 8 == 0 && w.cols % 8 == 0;
+      rc = xent_weights_bf16(w, s);
+    } else if (rc == SAGNN_OK && d_dW) {
       // (fp32 weights whose piece lies in one place are written there)
       const bool there = dtype == SAGNN_F32 && (transW || p.pieces == 1);
       float* dW = there ? (float*)d_dW + (size_t)at * (transW ? kdim : 1) : (float*)(ws + p.weights);
@@ -521,8 +543,8 @@ SAGNN_EXPORT int softmax_xent_bwd(int32_t dtype, const void* d_H, int64_t ldh, c
         const int64_t blocks = ceil_div(rows * ceil_div(cols, 4), 256);
         const dim3 grid((uint32_t)(blocks < 4096 ? blocks : 4096));
         const size_t first = (size_t)at * (transW ? kdim : 1);
-        if (dtype == SAGNN_BF16) xent_weights_kernel<__bf16><<<grid, 256, 0, s>>>(dW, w.nout, rows, cols, (__bf16*)d_dW + first, ldt);
-        else xent_weights_kernel<float><<<grid, 256, 0, s>>>(dW, w.nout, rows, cols, (float*)d_dW + first, ldt);
+        if (dtype == SAGNN_BF16) xent_convert_kernel<__bf16><<<grid, 256, 0, s>>>(dW, w.nout, rows, cols, (__bf16*)d_dW + first, ldt);
+        else xent_convert_kernel<float><<<grid, 256, 0, s>>>(dW, w.nout, rows, cols, (float*)d_dW + first, ldt);
         SAGNN_LAUNCH_CHECK();
       }
     }
