@@ -43,15 +43,49 @@ constexpr int xent_lds(int wm, int wn, int tm, int tn) {
   return rows > cols ? rows : cols;
 }
 
+// Bfloat16 results of a tile -> memory: every wavefront turns its own through LDS (rows of 16 bytes more than they have, against the
+// banks), so that a lane stores eight neighbouring columns
+// (four at a time, as the products leave them, 2 M x 128 results of 47 classes took 324 us).
+template <typename C>
+struct Turn {
+  static constexpr int kPitch = C::TN * 32 * 2 + 16, kPerRow = C::TN * 4;
+  static __device__ __forceinline__ char* own(char* smem) { return smem + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) * (C::TM * 32 * kPitch); }
+  static __device__ __forceinline__ void put(char* smem, int tm, int tn, int v, const float (&y)[4]) {
+    const int lane = threadIdx.x & 63;
+    bf16x4 w;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) w[i] = (__bf16)y[i];
+    *reinterpret_cast<bf16x4*>(own(smem) + (tm * 32 + (lane & 31)) * kPitch + (tn * 32 + 2 * v + 4 * (lane >> 5)) * 2) = w;
+  }
+  // the value of a lane's row in its column `near`
+  static __device__ __forceinline__ void put_one(char* smem, int tm, int near, float p) {
+    const int lane = threadIdx.x & 63;
+    *reinterpret_cast<__bf16*>(own(smem) + (tm * 32 + (lane & 31)) * kPitch + (near + 4 * (lane >> 5)) * 2) = (__bf16)p;
+  }
+  // at(row): offset of a row; `cols` whole eights
+  template <typename F>
+  static __device__ __forceinline__ void store(char* smem, __bf16* out, int rows, int cols, F at) {
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int ra = (wave / C::WN) * C::TM * 32, rb = (wave % C::WN) * C::TN * 32;
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");      // (its own writes only)
+#pragma unroll 4
+    for (int u = lane; u < C::TM * 32 * kPerRow; u += 64) {
+      const int r = u / kPerRow, c = u % kPerRow * 8;
+      if (ra + r < rows && rb + c < cols)
+        *reinterpret_cast<bf16x8*>(out + at(ra + r) + rb + c) = *reinterpret_cast<const bf16x8*>(own(smem) + r * kPitch + c * 2);
+    }
+  }
+};
+
 // The products of grouped.h, grouped_direct.h and grouped_staged.h by one name
 template <typename S_, int PREC, bool TRB, int WM_, int WN_, int TM_, int TN_, int BK, bool LONG>
 struct SmallProduct {
   using S = S_;
   static constexpr int WM = WM_, WN = WN_, TM = TM_, TN = TN_, kThreads = WM * WN * 64;
   static constexpr int kOperands = TileShape<PREC, false, WM * TM * 32, BK>::kBytes + TileShape<PREC, TRB, WN * TN * 32, BK>::kBytes;
-  static constexpr int kLds = kOperands > xent_lds(WM, WN, TM, TN) ? kOperands : xent_lds(WM, WN, TM, TN);
-  static constexpr bool kTransW = !TRB;
-  static constexpr bool kTurned = false;
+  static constexpr bool kTransW = !TRB, kTurned = sizeof(S) == 2;
+  static constexpr int kResults = kTurned ? WM * WN * TM * 32 * (TN * 64 + 16) : 0;
+  static constexpr int kRest = kResults > xent_lds(WM, WN, TM, TN) ? kResults : xent_lds(WM, WN, TM, TN), kLds = kOperands > kRest ? kOperands : kRest;
   static __device__ __forceinline__ void run(const XentArgs& a, const S* A, int64_t lda, int rows, const S* B, int cols, int sum, int, char* smem, floatx16 (&acc)[TM][TN]) {
     tile_product<S, PREC, false, TRB, WM, WN, TM, TN, BK, LONG>(A, lda, rows, B, a.ldw, cols, sum, smem, acc, a.run);
   }
@@ -177,39 +211,6 @@ __device__ __forceinline__ float sixteen_sum(float x) {
   x += moved(x, std::integral_constant<int, 0x140>{});       // the other eight of sixteen
   return x;
 }
-
-// Bfloat16 results of a large tile -> memory: every wavefront turns its own through LDS (rows of 16 bytes more than they have, against the
-// banks), so that a lane stores eight neighbouring columns.
-template <typename C>
-struct Turn {
-  static constexpr int kPitch = C::TN * 32 * 2 + 16, kPerRow = C::TN * 4;
-  static __device__ __forceinline__ char* own(char* smem) { return smem + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) * (C::TM * 32 * kPitch); }
-  static __device__ __forceinline__ void put(char* smem, int tm, int tn, int v, const float (&y)[4]) {
-    const int lane = threadIdx.x & 63;
-    bf16x4 w;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) w[i] = (__bf16)y[i];
-    *reinterpret_cast<bf16x4*>(own(smem) + (tm * 32 + (lane & 31)) * kPitch + (tn * 32 + 2 * v + 4 * (lane >> 5)) * 2) = w;
-  }
-  // the value of a lane's row in its column `near`
-  static __device__ __forceinline__ void put_one(char* smem, int tm, int near, float p) {
-    const int lane = threadIdx.x & 63;
-    *reinterpret_cast<__bf16*>(own(smem) + (tm * 32 + (lane & 31)) * kPitch + (near + 4 * (lane >> 5)) * 2) = (__bf16)p;
-  }
-  // at(row): offset of a row; `cols` whole eights
-  template <typename F>
-  static __device__ __forceinline__ void store(char* smem, __bf16* out, int rows, int cols, F at) {
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int ra = (wave / C::WN) * C::TM * 32, rb = (wave % C::WN) * C::TN * 32;
-    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");      // (its own writes only)
-#pragma unroll 4
-    for (int u = lane; u < C::TM * 32 * kPerRow; u += 64) {
-      const int r = u / kPerRow, c = u % kPerRow * 8;
-      if (ra + r < rows && rb + c < cols)
-        *reinterpret_cast<bf16x8*>(out + at(ra + r) + rb + c) = *reinterpret_cast<const bf16x8*>(own(smem) + r * kPitch + c * 2);
-    }
-  }
-};
 
 template <typename C, bool WHOLE>
 __device__ __forceinline__ void xent_grads(const XentArgs& a, int64_t r0, int64_t row_tile, int64_t c0, int rows, int cols, char* smem,
