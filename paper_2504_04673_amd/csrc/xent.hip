@@ -7,8 +7,8 @@
 // Rows without a label are no part of the gradients: a vertex in three has one, often one in a hundred.  Those with one are listed first and their
 // features copied (where all have one, taken as they lie), so that the products are as long as the list, and a NaN in a row that has none meets nothing.
 //
-// Bound by the matrix cores where features are wide: 8192 x 1024 x 131072 bfloat16 forward 2.1 ms (1050 TFLOP/s), a step 8.7 ms, 1010 TFLOP/s of what is
-// multiplied; with narrow features by the epilogues' vector instructions, in three terms by the conversion: 170 k x 128 x 172, two in five labelled, 262 us.
+// Bound by the matrix cores where features are wide: 8192 x 1024 x 131072 bfloat16 forward 2.1 ms (1040 TFLOP/s), a step 8.2 to 8.3 ms, 1060 TFLOP/s of what
+// is multiplied; with narrow features by the epilogues' vector instructions, in three terms by the conversion: 170 k x 128 x 172, two in five labelled, 262 us.
 #include <initializer_list>
 #include <type_traits>
 
