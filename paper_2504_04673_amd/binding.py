@@ -947,7 +947,7 @@ def _drop_args(p, seed, offset, row0):
     if isinstance(offset, torch.Tensor):
         if offset.numel() != 1:
             raise ValueError("offset: expected one element")
-        d_offset, offset = _dev(offset, torch.int64, "offset").data_ptr(), 0
+        d_offset, offset = _here(_dev(offset, torch.int64, "offset"), "offset").data_ptr(), 0
     if not (0 <= seed < 1 << 64 and 0 <= offset < 1 << 64):
         raise ValueError("seed and offset: expected 64 bits without a sign")
     return int(p * 65536 + 0.5), seed, offset, d_offset, row0
