@@ -231,6 +231,9 @@ bool whole_granules(const void* p, int64_t ld, int64_t width) { return aligned16
 // Tile of a product, m rows by cols, `sum` deep, and shares of the summed index (several only with `room` for sums of their own): what the fullest CU
 // multiplies, by the tiles' rates, and what it costs to write and read the shares' sums.
 struct TilePick { int tile; int32_t splits, share; };
+// What the 256 x 256 tile's epilogue costs, in rows of the summed index: with exponentials in it and one workgroup on a CU more than a plain product's 200
+// (a step of 170 k x 128 x 172 in bfloat16 took 205 us with 200, 167 with 300; 8192 x 128 x 65536, which keeps the tile, 1594; with 400, without it, 1660).
+constexpr double kDirectEnds = 300;
 // joined: several tiles of columns cost a launch more.  (The staged tiles' rates 0.8 and 1.4 times as high: 170 k x 128 x 172 in three terms 308 and 267 us
 // for 266, 4099 x 200 x 54321 2.67 and 2.92 ms for 2.67.)
 TilePick pick_tile(int32_t dtype, int32_t prec, int ways, int64_t m, int64_t cols, int64_t sum, int32_t room, bool joined = false) {
@@ -239,7 +242,8 @@ TilePick pick_tile(int32_t dtype, int32_t prec, int ways, int64_t m, int64_t col
   // values of a 128 x 128 tile that a CU multiplies in a microsecond (half of the operations), and bytes that the chip moves in one
   const double a_us = (dtype == SAGNN_BF16 ? 740e6 : prec == SAGNN_GEMM_FP32 ? 133e6 : prec == SAGNN_GEMM_BF16 ? 430e6 : 171e6) / 512, bytes_us = 4e6;
   for (int tile : {kTile128, kTile128x64, kTile32x128, kThin, kDirect256, kStaged256x128, kStaged128x256}) {
-    const TileCost c = tile_cost(dtype, prec, tile);
+    TileCost c = tile_cost(dtype, prec, tile);
+    if (tile == kDirect256) c.ends = kDirectEnds;
     if (c.rate == 0 || (tile == kDirect256 && ways != kDirect) || ((tile == kStaged256x128 || tile == kStaged128x256) && ways != kStaged)) continue;
     const int64_t h = grouped_tile_rows(tile), w = grouped_tile_cols(tile);
     const int64_t whole = ceil_div(m, h) * ceil_div(cols, w);
