@@ -14,6 +14,7 @@ import pytest
 import torch
 
 import paper_2504_04673_amd as sagnn
+from paper_2504_04673_amd import binding
 from tests.philox import kept
 
 pytestmark = pytest.mark.gpu
@@ -342,3 +343,14 @@ def test_rows_behind_two_gigabytes():
     few = sagnn.rms_norm_bwd(X[-3:], Y[-3:], rstd[-3:].contiguous())
     assert torch.equal(dX[-3:], few[0])
     close(dgamma, few[2].double(), 1e-5 * (Y[-3:].double() * X[-3:].double() * rstd[-3:, None].double()).abs().sum(0) + 1e-37, "dgamma")
+
+
+def test_tensors_of_another_device_are_refused(monkeypatch):
+    """The current device is asked for on the host: where it is another than the tensors', nothing is launched."""
+    x, v, n = torch.zeros(4, 8, device="cuda"), torch.zeros(4, device="cuda"), torch.zeros(1, dtype=torch.int64, device="cuda")
+    monkeypatch.setattr(torch._C, "_cuda_getDevice", lambda: 1 + x.get_device())
+    for f in (lambda: sagnn.dropout_add(x, 0.1, 0), lambda: sagnn.rms_norm(x), lambda: sagnn.rms_norm_e4m3(x), lambda: sagnn.rms_norm_bwd(x, x, v),
+              lambda: sagnn.spmm_pack_rows_e4m3(x.to(torch.float8_e4m3fn), v), lambda: sagnn.softmax_xent(x, x, v.int(), transW=True),
+              lambda: binding._drop_args(0.5, 0, n, 0)):
+        with pytest.raises(ValueError, match="current device"):
+            f()
