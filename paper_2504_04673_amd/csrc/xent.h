@@ -3,13 +3,14 @@
 //
 //   stats   tiles of z = H W + b leave a maximum, a sum of exponentials above it and the label's z for each row and tile of columns
 //   grads   tiles of z become P = g (exp(z - lse) - [class == label]), stored in the operands' type, and column sums of it
+//   two     the same in two bfloat16 terms, the value and what its rounding leaves, in neighbouring rows
 //   rows    dH (+)= P W^T
 #pragma once
 #include "grouped.h"
 
 namespace sagnn {
 
-enum XentMode { kXentStats, kXentGrads, kXentRows };
+enum XentMode { kXentStats, kXentGrads, kXentTwo, kXentRows };
 
 struct XentArgs {
   const void* X; int64_t ldx;                // rows x sum
@@ -28,6 +29,7 @@ struct XentArgs {
   float* loss; float* lse;                   // the results
   // grads; the rows are `map`'s
   const int32_t* map; const float* row_lse; const float* grad; float grad_all;
+  float scale;                               // what is not in P (bfloat16: the factor of all rows), of dbias and the results
   void* P; int64_t ldp; int32_t stored;      // columns that are stored, zeros behind `cols`
   float* bias_parts;                         // row tiles x cols, or NULL
   // rows: `splits` shares of the summed index, `share` of it each, with sums of their own, splits x m x cols, added to from piece to piece of the
@@ -76,6 +78,12 @@ struct Turn {
     }
   }
 };
+
+// What the rounding of a value leaves (nothing of an infinity or NaN)
+__device__ __forceinline__ float rest_of(float x) {
+  const float high = (float)(__bf16)x;
+  return __builtin_fabsf(high) < INFINITY ? x - high : 0.f;
+}
 
 // The products of grouped.h, grouped_direct.h and grouped_staged.h by one name
 template <typename S_, int PREC, bool TRB, int WM_, int WN_, int TM_, int TN_, int BK, bool LONG>
@@ -212,7 +220,7 @@ __device__ __forceinline__ float sixteen_sum(float x) {
   return x;
 }
 
-template <typename C, bool WHOLE>
+template <typename C, bool WHOLE, bool TWO>
 __device__ __forceinline__ void xent_grads(const XentArgs& a, int64_t r0, int64_t row_tile, int64_t c0, int rows, int cols, char* smem,
                                            const floatx16 (&acc)[C::TM][C::TN]) {
   using S = typename C::S;
@@ -224,7 +232,9 @@ __device__ __forceinline__ void xent_grads(const XentArgs& a, int64_t r0, int64_
   for (int tn = 0; tn < C::TN; ++tn)
 #pragma unroll
     for (int v = 0; v < 16; ++v) sums[tn][v] = 0.f;
-  S* P = reinterpret_cast<S*>(a.P) + r0 * a.ldp + c0;
+  constexpr bool kTurned = C::kTurned && !TWO;
+  const int64_t ldp = TWO ? 2 * a.ldp : a.ldp;
+  S* P = reinterpret_cast<S*>(a.P) + r0 * ldp + c0;
   const int stored = a.stored - c0 < BN ? (int)(a.stored - c0) : BN;
 #pragma unroll
   for (int tm = 0; tm < C::TM; ++tm) {
@@ -245,8 +255,13 @@ __device__ __forceinline__ void xent_grads(const XentArgs& a, int64_t r0, int64_
           if (!WHOLE) y[i] = in && column_of<C>(tn, v + i) < cols ? y[i] : 0.f;
           sums[tn][v + i] += y[i];
         }
-        if constexpr (C::kTurned) Turn<C>::put(smem, tm, tn, v, y);
-        else if (in) store_four(P + (int64_t)r * a.ldp + column_of<C>(tn, v), y, stored - column_of<C>(tn, v));
+        if constexpr (kTurned) Turn<C>::put(smem, tm, tn, v, y);
+        else if (in) store_four(P + r * ldp + column_of<C>(tn, v), y, stored - column_of<C>(tn, v));
+        if constexpr (TWO)
+          if (in) {
+            const float rest[4] = {rest_of(y[0]), rest_of(y[1]), rest_of(y[2]), rest_of(y[3])};
+            store_four(P + r * ldp + a.ldp + column_of<C>(tn, v), rest, stored - column_of<C>(tn, v));
+          }
       }
     const bool here = ours<C>(near);
     if (__any(here)) {                              // the label's own value, over what was stored
@@ -256,12 +271,13 @@ __device__ __forceinline__ void xent_grads(const XentArgs& a, int64_t r0, int64_
 #pragma unroll
         for (int v = 0; v < 16; ++v) sums[tn][v] -= near == tn * 32 + 8 * (v / 4) + v % 4 ? g : 0.f;
       if (here) {
-        if constexpr (C::kTurned) Turn<C>::put_one(smem, tm, near, p);
-        else P[(int64_t)r * a.ldp + column_of<C>(0, 0) + near] = (S)p;
+        if constexpr (kTurned) Turn<C>::put_one(smem, tm, near, p);
+        else P[r * ldp + column_of<C>(0, 0) + near] = (S)p;
+        if constexpr (TWO) P[r * ldp + a.ldp + column_of<C>(0, 0) + near] = (S)rest_of(p);
       }
     }
   }
-  if constexpr (C::kTurned) Turn<C>::store(smem, P, rows, stored, [&](int r) { return r * a.ldp; });
+  if constexpr (kTurned) Turn<C>::store(smem, P, rows, stored, [&](int r) { return r * ldp; });
   if (!a.bias_parts) return;
   // sums over the rows, of what is not rounded
   __syncthreads();
@@ -278,7 +294,7 @@ __device__ __forceinline__ void xent_grads(const XentArgs& a, int64_t r0, int64_
     float x = 0.f;
 #pragma unroll
     for (int w = 0; w < 2 * C::WM; ++w) x += place[w * BN + c];
-    a.bias_parts[row_tile * a.cols + c0 + c] = x;
+    a.bias_parts[row_tile * a.cols + c0 + c] = x * a.scale;
   }
 }
 
@@ -292,13 +308,18 @@ __device__ __forceinline__ void xent_rows(const XentArgs& a, int32_t split, int6
 #pragma unroll
         for (int i = 0; i < C::TM * C::TN * 4; ++i) {
           const int tm = i / (C::TN * 4), tn = i / 4 % C::TN, v = i % 4 * 4;
-          const float y[4] = {acc[tm][tn][v], acc[tm][tn][v + 1], acc[tm][tn][v + 2], acc[tm][tn][v + 3]};
+          const float y[4] = {acc[tm][tn][v] * a.scale, acc[tm][tn][v + 1] * a.scale, acc[tm][tn][v + 2] * a.scale, acc[tm][tn][v + 3] * a.scale};
           Turn<C>::put(smem, tm, tn, v, y);
         }
         Turn<C>::store(smem, out, rows, cols, [&](int r) { return (int64_t)a.map[r0 + r] * a.ldo; });
         return;
       }
-    tile_fours<C::WM, C::WN, C::TM, C::TN>(acc, [&](int r, int c, float (&y)[4]) { if (r < rows) store_four(out + (int64_t)a.map[r0 + r] * a.ldo + c, y, cols - c); });
+    tile_fours<C::WM, C::WN, C::TM, C::TN>(acc, [&](int r, int c, float (&y)[4]) {
+      if (r >= rows) return;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) y[i] *= a.scale;
+      store_four(out + (int64_t)a.map[r0 + r] * a.ldo + c, y, cols - c);
+    });
     return;
   }
   float* sums = a.sums + (split * a.m + r0) * a.cols + c0;
@@ -366,9 +387,9 @@ __global__ __launch_bounds__(C::kThreads, 2) void xent_kernel(const XentArgs a) 
   if constexpr (MODE == kXentStats) {
     if (whole) xent_stats<C, true>(a, t.r0, t.col, t.c0, t.rows, t.cols, smem, acc);
     else xent_stats<C, false>(a, t.r0, t.col, t.c0, t.rows, t.cols, smem, acc);
-  } else if constexpr (MODE == kXentGrads) {
-    if (whole) xent_grads<C, true>(a, t.r0, t.row, t.c0, t.rows, t.cols, smem, acc);
-    else xent_grads<C, false>(a, t.r0, t.row, t.c0, t.rows, t.cols, smem, acc);
+  } else if constexpr (MODE == kXentGrads || MODE == kXentTwo) {
+    if (whole) xent_grads<C, true, MODE == kXentTwo>(a, t.r0, t.row, t.c0, t.rows, t.cols, smem, acc);
+    else xent_grads<C, false, MODE == kXentTwo>(a, t.r0, t.row, t.c0, t.rows, t.cols, smem, acc);
   } else xent_rows<C>(a, t.split, t.r0, t.c0, t.rows, t.cols, smem, acc);
 }
 
@@ -437,12 +458,12 @@ __global__ __launch_bounds__(kThinWaves * 64) void xent_thin_kernel(const XentAr
 #pragma unroll
     for (int i = 0; i < 2; ++i)
       if (in && c + i < t.cols) {
-        if (!to) reinterpret_cast<S*>(a.out)[(int64_t)a.map[t.r0 + r] * a.ldo + t.c0 + c + i] = (S)y[i];
+        if (!to) reinterpret_cast<S*>(a.out)[(int64_t)a.map[t.r0 + r] * a.ldo + t.c0 + c + i] = (S)(y[i] * a.scale);
         else to[i] = a.add ? to[i] + y[i] : y[i];
       }
     return;
   }
-  const int64_t row = !in ? 0 : MODE == kXentGrads ? (int64_t)a.map[t.r0 + r] : t.r0 + r;
+  const int64_t row = !in ? 0 : MODE != kXentStats ? (int64_t)a.map[t.r0 + r] : t.r0 + r;
   const int64_t label = (in ? (int64_t)a.labels[row] - a.class0 : -1) - t.c0;
 #pragma unroll
   for (int i = 0; i < 2; ++i) y[i] = c + i < t.cols ? y[i] + (a.bias ? a.bias[t.c0 + c + i] : 0.f) : -INFINITY;
@@ -463,11 +484,14 @@ __global__ __launch_bounds__(kThinWaves * 64) void xent_thin_kernel(const XentAr
     }
   } else {
     const float lse = in ? a.row_lse[row] : 0.f, g = in ? a.grad_all * (a.grad ? a.grad[row] : 1.f) : 0.f;
-    S* P = reinterpret_cast<S*>(a.P) + (t.r0 + r) * a.ldp + t.c0;
+    S* P = reinterpret_cast<S*>(a.P) + (t.r0 + r) * (MODE == kXentTwo ? 2 * a.ldp : a.ldp) + t.c0;
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
       y[i] = in && c + i < t.cols ? exp_of(y[i] - lse) * g - (label == c + i ? g : 0.f) : 0.f;
-      if (in && t.c0 + c + i < a.stored) P[c + i] = (S)y[i];
+      if (in && t.c0 + c + i < a.stored) {
+        P[c + i] = (S)y[i];
+        if constexpr (MODE == kXentTwo) P[a.ldp + c + i] = (S)rest_of(y[i]);
+      }
     }
     if (!a.bias_parts) return;
     *reinterpret_cast<float2*>(sums + r * kRow + c) = make_float2(y[0], y[1]);
@@ -476,7 +500,7 @@ __global__ __launch_bounds__(kThinWaves * 64) void xent_thin_kernel(const XentAr
       float x = 0.f;
 #pragma unroll 8
       for (int i = 0; i < 32; ++i) x += sums[i * kRow + tid];
-      a.bias_parts[(int64_t)t.row * a.cols + t.c0 + tid] = x;
+      a.bias_parts[(int64_t)t.row * a.cols + t.c0 + tid] = x * a.scale;
     }
   }
 }
@@ -489,6 +513,7 @@ struct XentWeightArgs {
   const int32_t* count; int64_t m;
   int32_t rows, cols, row_tiles, col_tiles;
   void* out; int64_t ldo; bool wide;
+  float scale;                               // of the result
 };
 int xent_weights_bf16(const XentWeightArgs& a, hipStream_t s);
 
@@ -512,6 +537,11 @@ int xent_launches(XentArgs a, int rows, int threads, F launch) {
 template <typename C>
 int xent_launch(const XentArgs& args, hipStream_t s) {
   return xent_launches(args, C::WM * C::TM * 32, C::kThreads, [&](const XentArgs& a, dim3 grid) {
+    if constexpr (sizeof(typename C::S) == 2)
+      if (a.mode == kXentTwo) {
+        xent_kernel<C, kXentTwo><<<grid, C::kThreads, 0, s>>>(a);
+        return;
+      }
     if (a.mode == kXentStats) xent_kernel<C, kXentStats><<<grid, C::kThreads, 0, s>>>(a);
     else if (a.mode == kXentGrads) xent_kernel<C, kXentGrads><<<grid, C::kThreads, 0, s>>>(a);
     else xent_kernel<C, kXentRows><<<grid, C::kThreads, 0, s>>>(a);
@@ -520,6 +550,11 @@ int xent_launch(const XentArgs& args, hipStream_t s) {
 template <typename S, int PREC, int BK, bool TRB>
 int xent_thin(const XentArgs& args, hipStream_t s) {
   return xent_launches(args, 32, kThinWaves * 64, [&](const XentArgs& a, dim3 grid) {
+    if constexpr (sizeof(S) == 2)
+      if (a.mode == kXentTwo) {
+        xent_thin_kernel<S, PREC, TRB, BK, kXentTwo><<<grid, kThinWaves * 64, 0, s>>>(a);
+        return;
+      }
     if (a.mode == kXentStats) xent_thin_kernel<S, PREC, TRB, BK, kXentStats><<<grid, kThinWaves * 64, 0, s>>>(a);
     else if (a.mode == kXentGrads) xent_thin_kernel<S, PREC, TRB, BK, kXentGrads><<<grid, kThinWaves * 64, 0, s>>>(a);
     else xent_thin_kernel<S, PREC, TRB, BK, kXentRows><<<grid, kThinWaves * 64, 0, s>>>(a);

@@ -28,6 +28,12 @@ constexpr int32_t kPieceLeast = 1024, kPieceMost = 32768;
 constexpr int64_t kLeastBytes = int64_t(4) << 30;   // of P in pieces of kPieceLeast; beyond that, tens of millions of rows, they are narrower
 // Pieces at most: dH's sums are added over them in turn, in 32 bits
 constexpr int32_t kPiecesMost = 384;
+// Rows up to which a bfloat16 P is kept in two terms, the value and what its rounding leaves, each of them a row of dH's and dW's products: they meet 2^-16 of P,
+// not 2^-8.  Of more rows those roundings average out against the results' own; of few one of them decides (a row's label outweighs its other classes), and
+// the gradients were up to three times as far off as by their own rounding.  The weights' bytes bound these products where rows are few
+// (a step, with one term and with two: 1 x 256 x 50000 72 and 77 us, 16 x 1024 x 131072 343 and 358, 128 x 4096 x 131072 1395 and 1675, 512 x 256 x 32768 112 and 148).
+// With a weight of its own every row's label is rounded elsewhere, which averages out later: 758 rows, half of them labelled, of 2 classes 0.0025 against 0.0017.
+constexpr int64_t kTwoTerms = 512, kTwoTermsWeighted = 1024;
 // Bytes of the sums of dH's shares
 constexpr int64_t kSumBytes = int64_t(512) << 20;
 
@@ -47,12 +53,12 @@ __global__ __launch_bounds__(kListThreads) void label_count_kernel(const int32_t
 }
 
 // map[i] = row of the i-th label; H's rows one behind the other in rows of ldc values (zeros behind the k there are), unless every row has one and
-// `needed` is not set: then H itself will do; zeros in dH's rows without one, and in `clear`.  bounds = {0, how many}.  counts NULL: few rows, whose labels each
-// block counts itself.
+// `needed` is not set: then H itself will do; each as often as P has terms; zeros in dH's rows without one, and in `clear`.  bounds = {0, how many, 0, how many
+// rows of terms}.  counts NULL: few rows, whose labels each block counts itself.
 template <typename T>
 __global__ __launch_bounds__(kListThreads) void label_list_kernel(const int32_t* __restrict__ labels, int64_t m, int64_t each, int32_t classes,
                                                                   const int32_t* __restrict__ counts, int32_t* __restrict__ map, int32_t* __restrict__ bounds,
-                                                                  const T* __restrict__ H, int64_t ldh, int32_t k, T* __restrict__ rows, int64_t ldc,
+                                                                  const T* __restrict__ H, int64_t ldh, int32_t k, T* __restrict__ rows, int64_t ldc, int terms,
                                                                   T* __restrict__ dH, int64_t lddh, int lanes, bool needed, float* __restrict__ clear,
                                                                   int32_t n_clear) {
   __shared__ int32_t room[kListThreads / 64];
@@ -107,7 +113,7 @@ __global__ __launch_bounds__(kListThreads) void label_list_kernel(const int32_t*
       if (to >= 0)
         for (int c = own * 8; c < ldc; c += lanes * 8) {
           const auto w = load_eight(H + (r0 + i) * ldh + c, k - c, k);
-          *reinterpret_cast<TightRun<T, 8>*>(rows + to * ldc + c) = w;
+          for (int e = 0; e < terms; ++e) *reinterpret_cast<TightRun<T, 8>*>(rows + ((int64_t)to * terms + e) * ldc + c) = w;
         }
       else if (dH)
         for (int c = own * 8; c < k; c += lanes * 8) store_eight(dH + (r0 + i) * lddh + c, {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f}, k - c);
@@ -116,6 +122,8 @@ __global__ __launch_bounds__(kListThreads) void label_list_kernel(const int32_t*
   if (blockIdx.x == gridDim.x - 1 && threadIdx.x == 0) {
     bounds[0] = 0;
     bounds[1] = before;
+    bounds[2] = 0;
+    bounds[3] = before * terms;
   }
 }
 
@@ -171,44 +179,50 @@ __global__ __launch_bounds__(kBiasThreads) void xent_bias_kernel(const float* __
   }
 }
 
-// dH's listed rows: the sum of the shares' sums
+// dH's listed rows: the sum of the shares' sums, m rows each, of a row's terms
 template <typename T>
-__global__ __launch_bounds__(256) void xent_rows_kernel(const float* __restrict__ sums, int32_t splits, int64_t m, const int32_t* __restrict__ bounds, int32_t k,
+__global__ __launch_bounds__(256) void xent_rows_kernel(const float* __restrict__ sums, int32_t splits, int64_t m, int terms, float scale, const int32_t* __restrict__ bounds, int32_t k,
                                                         const int32_t* __restrict__ map, T* __restrict__ dH, int64_t lddh) {
   const int64_t fours = (k + 3) / 4, all = bounds[1] * fours;
   for (int64_t i = blockIdx.x * 256ll + threadIdx.x; i < all; i += gridDim.x * 256ll) {
     const int64_t r = i / fours;
     const int c = (int)(i - r * fours) * 4;
     float y[4] = {0.f, 0.f, 0.f, 0.f};
-    const float* from = sums + r * k + c;
+    const float* from = sums + r * terms * k + c;
+    const int32_t parts = splits * terms;
+    auto part = [&](int32_t p) { return from + (terms == 2 ? (p >> 1) * m * k + (p & 1) * k : p * m * k); };
     if (c + 4 <= k) {
 #pragma unroll 4
-      for (int32_t s = 0; s < splits; ++s) {
+      for (int32_t s = 0; s < parts; ++s) {
         float x[4];
-        __builtin_memcpy(x, reinterpret_cast<const Four<float>*>(from + s * m * k), 16);
+        __builtin_memcpy(x, reinterpret_cast<const Four<float>*>(part(s)), 16);
 #pragma unroll
         for (int e = 0; e < 4; ++e) y[e] += x[e];
       }
     } else {
-      for (int32_t s = 0; s < splits; ++s)
+      for (int32_t s = 0; s < parts; ++s)
 #pragma unroll
         for (int e = 0; e < 3; ++e)
-          if (c + e < k) y[e] += from[s * m * k + e];
+          if (c + e < k) y[e] += part(s)[e];
     }
+#pragma unroll
+    for (int e = 0; e < 4; ++e) y[e] *= scale;
     store_four(dH + map[r] * lddh + c, y, k - c);
   }
 }
 
-// A piece's dW from fp32 into its place
+// A piece's dW from fp32 into its place (no rows: zeros, whatever the scale is)
 template <typename T>
-__global__ __launch_bounds__(256) void xent_convert_kernel(const float* __restrict__ from, int64_t ldf, int64_t rows, int32_t cols, T* __restrict__ to, int64_t ldt) {
+__global__ __launch_bounds__(256) void xent_convert_kernel(const float* __restrict__ from, int64_t ldf, int64_t rows, int32_t cols, float factor,
+                                                           const int32_t* __restrict__ bounds, T* __restrict__ to, int64_t ldt) {
+  const float scale = bounds[1] > 0 ? factor : 0.f;
   const int64_t fours = (cols + 3) / 4, all = rows * fours;
   for (int64_t i = blockIdx.x * 256ll + threadIdx.x; i < all; i += gridDim.x * 256ll) {
     const int64_t r = i / fours;
     const int c = (int)(i - r * fours) * 4;
     float y[4];
 #pragma unroll
-    for (int e = 0; e < 4; ++e) y[e] = c + e < cols ? from[r * ldf + c + e] : 0.f;
+    for (int e = 0; e < 4; ++e) y[e] = c + e < cols ? from[r * ldf + c + e] * scale : 0.f;
     store_four(to + r * ldt + c, y, cols - c);
   }
 }
@@ -317,13 +331,16 @@ bool whole_weights(int32_t dtype, int64_t m, int32_t kdim, int32_t classes) {
 }
 
 struct BwdPlan {
+  int32_t terms;                             // of P
   int32_t piece, pieces;                     // classes of a piece
   int32_t splits;                            // shares of them that there is room for in dH's sums
   int64_t ldp, ldc;                          // of P, of the listed rows
   size_t map, bounds, counts, rows, P, sums, weights, parts, bias, weights_bytes, parts_bytes, total;
 };
-BwdPlan bwd_plan(int32_t dtype, int32_t prec, int64_t m, int32_t kdim, int32_t classes) {
+int32_t terms_of(int32_t dtype, int64_t m, bool weighted) { return dtype == SAGNN_BF16 && m <= (weighted ? kTwoTermsWeighted : kTwoTerms) ? 2 : 1; }
+BwdPlan bwd_plan(int32_t dtype, int32_t prec, int32_t terms, int64_t m, int32_t kdim, int32_t classes) {
   BwdPlan p{};
+  p.terms = terms;
   const int64_t size = dtype == SAGNN_BF16 ? 2 : 4, rows = m > 0 ? m : 1;
   int64_t most = kPieceBytes / (rows * size) / 256 * 256;
   const int32_t least = rows * size * kPieceLeast <= kLeastBytes ? kPieceLeast : 256;
@@ -338,30 +355,30 @@ BwdPlan bwd_plan(int32_t dtype, int32_t prec, int64_t m, int32_t kdim, int32_t c
   const int32_t kw = padded_width(dtype, kdim);
   const int32_t last = classes - (p.pieces - 1) * p.piece;
   for (int32_t n : {p.piece, last}) {
-    if (whole_weights(dtype, m, kdim, n)) continue;
+    if (whole_weights(dtype, m * p.terms, kdim, n)) continue;
     p.weights_bytes = (size_t)padded_width(dtype, p.piece) * kw * 4;
     size_t one = 0, two = 0;
-    grouped_gemm_bwd_workspace_bytes(m, 1, kw, padded_width(dtype, n), &one);
-    grouped_gemm_bwd_workspace_bytes(m, 1, padded_width(dtype, n), kw, &two);
+    grouped_gemm_bwd_workspace_bytes(m * p.terms, 1, kw, padded_width(dtype, n), &one);
+    grouped_gemm_bwd_workspace_bytes(m * p.terms, 1, padded_width(dtype, n), kw, &two);
     p.parts_bytes = one > p.parts_bytes ? one : p.parts_bytes;
     p.parts_bytes = two > p.parts_bytes ? two : p.parts_bytes;
     if (last == p.piece) break;
   }
   Room room;
   p.map = room.take((size_t)rows * 4);
-  p.bounds = room.take(8);
+  p.bounds = room.take(16);
   p.counts = room.take(kListBlocks * 4);
-  p.rows = room.take((size_t)rows * p.ldc * size);
-  p.P = room.take((size_t)rows * p.ldp * size);
+  p.rows = room.take((size_t)rows * p.terms * p.ldc * size);
+  p.P = room.take((size_t)rows * p.terms * p.ldp * size);
   // dH's sums: of every share of a piece's classes
-  const int64_t share = rows * kdim * 4;
+  const int64_t share = rows * p.terms * kdim * 4;
   p.splits = share > 0 ? (int32_t)(kSumBytes / share < 1 ? 1 : kSumBytes / share > 32 ? 32 : kSumBytes / share) : 1;
   int32_t splits = 1;
   for (int ways : {kSmallOnly, dtype == SAGNN_BF16 ? kDirect : kStaged}) {
-    const int32_t n = pick_tile(dtype, prec, ways, m, kdim, p.piece, p.splits).splits;
+    const int32_t n = pick_tile(dtype, prec, ways, m * p.terms, kdim, p.piece, p.splits).splits;
     if (n > splits) splits = n;
   }
-  p.sums = room.take(p.pieces > 1 || splits > 1 ? (size_t)splits * share : 0);
+  p.sums = room.take(p.pieces > 1 || splits > 1 || p.terms > 1 ? (size_t)splits * share : 0);
   p.weights = room.take(p.weights_bytes);
   p.parts = room.take(p.parts_bytes);
   p.bias = room.take((size_t)ceil_div(rows, 32) * p.piece * 4);
@@ -385,7 +402,7 @@ int list_labels(const BwdPlan& p, char* ws, const int32_t* labels, int64_t m, in
     label_count_kernel<<<dim3(blocks), kListThreads, 0, s>>>(labels, m, each, classes, counts);
     SAGNN_LAUNCH_CHECK();
   }
-  label_list_kernel<T><<<dim3(blocks), kListThreads, 0, s>>>(labels, m, each, classes, counts, map, bounds, (const T*)H, ldh, k, (T*)(ws + p.rows), p.ldc,
+  label_list_kernel<T><<<dim3(blocks), kListThreads, 0, s>>>(labels, m, each, classes, counts, map, bounds, (const T*)H, ldh, k, (T*)(ws + p.rows), p.ldc, p.terms,
                                                             (T*)dH, lddh, lanes, needed, clear, n_clear);
   SAGNN_LAUNCH_CHECK();
   return SAGNN_OK;
@@ -406,7 +423,11 @@ SAGNN_EXPORT int softmax_xent_workspace_bytes(int32_t dtype, int64_t m, int32_t 
   using namespace sagnn;
   if (!bytes || !valid(dtype, 0, m, kdim, n_classes, prec) || (backward & ~1)) return SAGNN_EINVAL;
   if (backward) {
-    *bytes = bwd_plan(dtype, prec, m, kdim, n_classes).total;
+    *bytes = 0;                              // (for either kind of gradient)
+    for (bool weighted : {false, true}) {
+      const size_t b = bwd_plan(dtype, prec, terms_of(dtype, m, weighted), m, kdim, n_classes).total;
+      if (b > *bytes) *bytes = b;
+    }
   } else {                                   // (room for any strides and alignments)
     *bytes = 0;
     for (int ways : {kSmallOnly, dtype == SAGNN_BF16 ? kDirect : kStaged}) {
@@ -473,17 +494,17 @@ SAGNN_EXPORT int softmax_xent_bwd(int32_t dtype, const void* d_H, int64_t ldh, c
         if (!clear_of(out[o].p, out[o].bytes, out[q].p, out[q].bytes)) return SAGNN_EINVAL;
     }
   }
-  const BwdPlan p = bwd_plan(dtype, prec, m, kdim, n_classes);
+  const BwdPlan p = bwd_plan(dtype, prec, terms_of(dtype, m, d_grad != nullptr), m, kdim, n_classes);
   if (!d_ws) return SAGNN_EINVAL;
   if (ws_bytes < p.total) return SAGNN_ECAPACITY;
   char* ws = (char*)d_ws;
   hipStream_t s = (hipStream_t)stream;
   // Where every row has a label H itself is taken, if it lies as well as the copy would (617 k x 1344 of 50 classes, three terms, all labelled: 5.8 ms
   // with the copy).  Only the device knows.
-  const bool itself = dtype == SAGNN_BF16 ? whole_granules(d_H, ldh, kdim) : ldh <= kLargeLd;
+  const bool itself = p.terms == 1 && (dtype == SAGNN_BF16 ? whole_granules(d_H, ldh, kdim) : ldh <= kLargeLd);
   // The bias's gradient of one tile of rows is its sums: written there, over zeros for the case that there is no such row
   auto logits = [&](const void* W, int32_t n) {
-    return pick_tile(dtype, prec, logits_ways(dtype, ws + p.rows, p.ldc, p.ldc, W, ldw, transW != 0, kdim, n), m, n, kdim, 1);
+    return pick_tile(dtype, prec, logits_ways(dtype, ws + p.rows, p.ldc * p.terms, p.ldc, W, ldw, transW != 0, kdim, n), m, n, kdim, 1);
   };
   const int32_t last = n_classes - (p.pieces - 1) * p.piece;
   const bool direct_bias = d_dbias && m <= grouped_tile_rows(logits(d_W, p.piece).tile) && m <= grouped_tile_rows(logits(d_W, last).tile);
@@ -491,13 +512,17 @@ SAGNN_EXPORT int softmax_xent_bwd(int32_t dtype, const void* d_H, int64_t ldh, c
   int rc = dtype == SAGNN_BF16 ? list_labels<__bf16>(p, ws, d_labels, m, n_classes, d_H, ldh, kdim, d_dH, lddh, !itself, clear, n_classes, s)
                                : list_labels<float>(p, ws, d_labels, m, n_classes, d_H, ldh, kdim, d_dH, lddh, !itself, clear, n_classes, s);
   const int32_t* bounds = (const int32_t*)(ws + p.bounds);
+  const int32_t* term_bounds = bounds + (p.terms == 2 ? 2 : 0);
+  const int64_t terms = m * p.terms;
+  // A factor of all rows is no part of a bfloat16 P: its rounding would be one for most labels' terms and shift all gradients by up to 2^-8
+  const float scale = dtype == SAGNN_BF16 ? (float)grad_all : 1.f;
   TilePick rows{};
   for (int32_t at = 0; at < n_classes && rc == SAGNN_OK; at += p.piece) {
     const int32_t n = n_classes - at < p.piece ? n_classes - at : p.piece;
     XentArgs a{};
-    a.X = ws + p.rows; a.ldx = p.ldc; a.W = (const char*)d_W + (size_t)at * (transW ? ldw : 1) * size; a.ldw = ldw; a.m = m; a.count = bounds + 1;
-    a.all = itself ? d_H : nullptr; a.ldall = ldh; a.cols = n; a.sum = kdim; a.mode = kXentGrads; a.bias = d_bias ? d_bias + at : nullptr; a.labels = d_labels; a.class0 = at; a.classes = n_classes;
-    a.map = (const int32_t*)(ws + p.map); a.row_lse = d_lse; a.grad = d_grad; a.grad_all = (float)grad_all; a.P = ws + p.P; a.ldp = p.ldp;
+    a.X = ws + p.rows; a.ldx = p.ldc * p.terms; a.W = (const char*)d_W + (size_t)at * (transW ? ldw : 1) * size; a.ldw = ldw; a.m = m; a.count = bounds + 1;
+    a.all = itself ? d_H : nullptr; a.ldall = ldh; a.cols = n; a.sum = kdim; a.mode = p.terms == 2 ? kXentTwo : kXentGrads; a.bias = d_bias ? d_bias + at : nullptr; a.labels = d_labels; a.class0 = at; a.classes = n_classes;
+    a.map = (const int32_t*)(ws + p.map); a.row_lse = d_lse; a.grad = d_grad; a.grad_all = dtype == SAGNN_BF16 ? 1.f : (float)grad_all; a.scale = scale; a.P = ws + p.P; a.ldp = p.ldp;
     a.stored = (int32_t)round_up((size_t)n, 8); a.bias_parts = direct_bias ? d_dbias + at : d_dbias ? (float*)(ws + p.bias) : nullptr;
     a.padded = (int32_t)p.ldc;
     const TilePick tile = logits(a.W, n);
@@ -511,30 +536,30 @@ SAGNN_EXPORT int softmax_xent_bwd(int32_t dtype, const void* d_H, int64_t ldh, c
     }
     if (rc == SAGNN_OK && d_dH && m > 0) {
       // (the last piece in as many shares as the others, whose sums it adds to)
-      if (at == 0) rows = pick_tile(dtype, prec, rows_ways(dtype, p.ldp, a.W, ldw, transW != 0, kdim, n_classes), m, kdim, p.piece, p.splits);
-      const bool summed = p.pieces > 1 || rows.splits > 1;
+      if (at == 0) rows = pick_tile(dtype, prec, rows_ways(dtype, p.ldp, a.W, ldw, transW != 0, kdim, n_classes), terms, kdim, p.piece, p.splits);
+      const bool summed = p.pieces > 1 || rows.splits > 1 || p.terms > 1;
       TilePick pick = rows;
       if (pick.splits == 1) pick.share = n;
       XentArgs b{};
-      b.X = a.P; b.ldx = p.ldp; b.W = a.W; b.ldw = ldw; b.m = m; b.count = a.count; b.cols = kdim; b.sum = n; b.mode = kXentRows; b.map = a.map;
+      b.X = a.P; b.ldx = p.ldp; b.W = a.W; b.ldw = ldw; b.m = terms; b.count = term_bounds + 1; b.scale = scale; b.cols = kdim; b.sum = n; b.mode = kXentRows; b.map = a.map;
       b.sums = summed ? (float*)(ws + p.sums) : nullptr; b.add = at > 0; b.out = d_dH; b.ldo = lddh;
       b.padded = a.stored; b.wide = aligned16(d_dH) && lddh % 8 == 0 && kdim % 8 == 0;
       rc = launch(b, dtype, prec, pick, transW == 0, s);
       if (rc == SAGNN_OK && summed && at + n == n_classes) {
         const int64_t blocks = ceil_div(m * ceil_div(kdim, 4), 256);
         const dim3 grid((uint32_t)(blocks < 8192 ? blocks : 8192));
-        if (dtype == SAGNN_BF16) xent_rows_kernel<__bf16><<<grid, 256, 0, s>>>(b.sums, rows.splits, m, bounds, kdim, b.map, (__bf16*)d_dH, lddh);
-        else xent_rows_kernel<float><<<grid, 256, 0, s>>>(b.sums, rows.splits, m, bounds, kdim, b.map, (float*)d_dH, lddh);
+        if (dtype == SAGNN_BF16) xent_rows_kernel<__bf16><<<grid, 256, 0, s>>>(b.sums, rows.splits, terms, p.terms, scale, bounds, kdim, b.map, (__bf16*)d_dH, lddh);
+        else xent_rows_kernel<float><<<grid, 256, 0, s>>>(b.sums, rows.splits, terms, p.terms, scale, bounds, kdim, b.map, (float*)d_dH, lddh);
         SAGNN_LAUNCH_CHECK();
       }
     }
-    if (rc == SAGNN_OK && d_dW && whole_weights(dtype, m, kdim, n)) {
+    if (rc == SAGNN_OK && d_dW && whole_weights(dtype, terms, kdim, n)) {
       XentWeightArgs w{};
       const void* whole = itself ? d_H : a.X;
       const int64_t ldwhole = itself ? ldh : p.ldc;
-      w.A = transW ? a.P : a.X; w.lda = transW ? p.ldp : p.ldc; w.A2 = transW ? a.P : whole; w.lda2 = transW ? p.ldp : ldwhole;
+      w.scale = scale; w.A = transW ? a.P : a.X; w.lda = transW ? p.ldp : p.ldc; w.A2 = transW ? a.P : whole; w.lda2 = transW ? p.ldp : ldwhole;
       w.B = transW ? a.X : a.P; w.ldb = transW ? p.ldc : p.ldp; w.B2 = transW ? whole : a.P; w.ldb2 = transW ? ldwhole : p.ldp;
-      w.count = bounds + 1; w.m = m; w.rows = transW ? n : kdim; w.cols = transW ? kdim : n;
+      w.count = term_bounds + 1; w.m = terms; w.rows = transW ? n : kdim; w.cols = transW ? kdim : n;
       w.row_tiles = (int32_t)ceil_div(w.rows, 256); w.col_tiles = (int32_t)ceil_div(w.cols, 256);
       w.ldo = transW ? kdim : n_classes; w.out = (__bf16*)d_dW + (size_t)at * (transW ? kdim : 1);
       w.wide = aligned16(w.out) && w.ldo % 8 == 0 && w.cols % 8 == 0;
@@ -544,7 +569,7 @@ SAGNN_EXPORT int softmax_xent_bwd(int32_t dtype, const void* d_H, int64_t ldh, c
       const bool there = dtype == SAGNN_F32 && (transW || p.pieces == 1);
       float* dW = there ? (float*)d_dW + (size_t)at * (transW ? kdim : 1) : (float*)(ws + p.weights);
       GroupedArgs w{};
-      w.off = bounds; w.groups = 1; w.m = m; w.dW = dW; w.partial = (float*)(ws + p.parts);
+      w.off = term_bounds; w.groups = 1; w.m = terms; w.dW = dW; w.partial = (float*)(ws + p.parts);
       const int32_t kw = padded_width(dtype, kdim), nw = padded_width(dtype, n);
       w.X = transW ? a.P : a.X; w.ldx = transW ? p.ldp : p.ldc; w.kdim = transW ? nw : kw;
       w.G = transW ? a.X : a.P; w.ldg = transW ? p.ldc : p.ldp; w.nout = transW ? kw : nw;
@@ -560,8 +585,8 @@ SAGNN_EXPORT int softmax_xent_bwd(int32_t dtype, const void* d_H, int64_t ldh, c
         const int64_t blocks = ceil_div(rows * ceil_div(cols, 4), 256);
         const dim3 grid((uint32_t)(blocks < 4096 ? blocks : 4096));
         const size_t first = (size_t)at * (transW ? kdim : 1);
-        if (dtype == SAGNN_BF16) xent_convert_kernel<__bf16><<<grid, 256, 0, s>>>(dW, w.nout, rows, cols, (__bf16*)d_dW + first, ldt);
-        else xent_convert_kernel<float><<<grid, 256, 0, s>>>(dW, w.nout, rows, cols, (float*)d_dW + first, ldt);
+        if (dtype == SAGNN_BF16) xent_convert_kernel<__bf16><<<grid, 256, 0, s>>>(dW, w.nout, rows, cols, scale, bounds, (__bf16*)d_dW + first, ldt);
+        else xent_convert_kernel<float><<<grid, 256, 0, s>>>(dW, w.nout, rows, cols, scale, bounds, (float*)d_dW + first, ldt);
         SAGNN_LAUNCH_CHECK();
       }
     }

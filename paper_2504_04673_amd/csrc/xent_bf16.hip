@@ -16,7 +16,7 @@ struct DirectProduct {
 };
 
 // Tiles of 256 x 256 over all listed rows.  Bound by the matrix cores (8192 rows, 1024 by 32768 classes: 430 us, 1279 TFLOP/s), by the weights' bytes where rows
-// are few (128 rows of 4096 by 131072 classes: a step 1394 us, through fp32 and a conversion 2487).
+// are few (128 rows of 4096 by 131072 classes, P in one term: a step 1394 us, through fp32 and a conversion 2487).
 struct WeightTile {
   static constexpr int WM = 2, WN = 4, TM = 4, TN = 2;
 };
@@ -36,17 +36,23 @@ __global__ __launch_bounds__(512) void xent_weights_kernel(const XentWeightArgs 
   direct_product<true, true, C::WM, C::WN, C::TM, C::TN>(A, lda, (rows + 7) & ~7, B, ldb, (cols + 7) & ~7, count < a.m ? count : a.m, smem, acc);
   __syncthreads();
   __bf16* out = reinterpret_cast<__bf16*>(a.out) + (int64_t)r0 * a.ldo + c0;
+  const float scale = count > 0 ? a.scale : 0.f;              // (no rows: zeros, whatever it is)
   if (a.wide) {
 #pragma unroll
     for (int i = 0; i < C::TM * C::TN * 4; ++i) {
       const int tm = i / (C::TN * 4), tn = i / 4 % C::TN, v = i % 4 * 4;
-      const float y[4] = {acc[tm][tn][v], acc[tm][tn][v + 1], acc[tm][tn][v + 2], acc[tm][tn][v + 3]};
+      const float y[4] = {acc[tm][tn][v] * scale, acc[tm][tn][v + 1] * scale, acc[tm][tn][v + 2] * scale, acc[tm][tn][v + 3] * scale};
       Turn<C>::put(smem, tm, tn, v, y);
     }
     Turn<C>::store(smem, out, rows, cols, [&](int r) { return r * a.ldo; });
     return;
   }
-  tile_fours<C::WM, C::WN, C::TM, C::TN>(acc, [&](int r, int c, float (&y)[4]) { if (r < rows) store_four(out + r * a.ldo + c, y, cols - c); });
+  tile_fours<C::WM, C::WN, C::TM, C::TN>(acc, [&](int r, int c, float (&y)[4]) {
+    if (r >= rows) return;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) y[i] *= scale;
+    store_four(out + r * a.ldo + c, y, cols - c);
+  });
 }
 }  // namespace
 

@@ -276,3 +276,56 @@ def test_so_many_rows_that_pieces_are_narrower():
         want, bound, wb, bb = want + part.dW, bound + part.dW_bound, wb + part.dbias, bb + part.dbias_bound
     close(dW, want, bound, "dW")
     close(dbias, wb, bb, "dbias")
+
+
+def unrounded(H, W, labels, g, bias=None):
+    """Gradients in 64 bits, and the sums of their terms' absolute values."""
+    h, w = H.double(), W.double()
+    P = torch.softmax(h @ w + (0 if bias is None else bias.double()), 1)
+    P.scatter_add_(1, labels.long()[:, None], torch.full_like(P[:, :1], -1.0))
+    P *= g.double()[:, None] if isinstance(g, torch.Tensor) else g
+    wt, ht = w.t().contiguous(), h.t().contiguous()
+    return P @ wt, ht @ P, P.abs() @ wt.abs(), ht.abs() @ P.abs()
+
+
+@pytest.mark.parametrize("weights", [False, True])
+@pytest.mark.parametrize("m,k,n", [(1, 24, 3), (1, 64, 2), (2, 40, 900), (9, 128, 47), (33, 100, 172), (130, 64, 2), (257, 16, 40000), (512, 264, 130)])
+def test_few_bfloat16_rows_meet_one_rounding(m, k, n, weights):
+    """P in two terms errs by 2^-16 of itself (what a rounding leaves is 2^-8 of it at most, and is rounded by 2^-8 of that); all else as with fp32 operands, 4e-5 for the sums,
+    the result's rounding 2^-8 and the factor's 2 u."""
+    H, W, labels, bias = inputs(m + k + n, m, k, n, torch.bfloat16, False, True, 1.0, False)
+    g = normal(gen(m), m).abs() + 0.1 if weights else 1.0 + 2.0 ** -8
+    _, lse = sagnn.softmax_xent(H, W, labels, bias=bias)
+    dH, dW, _ = sagnn.softmax_xent_bwd(H, W, labels, lse, g, bias=bias)
+    ref = Plain(H, W, labels, bias, False, g, "fp32")
+    rH, rW, aH, aW = unrounded(H, W, labels, g, bias)
+    close(dH, rH, ref.dH_bound + (3e-5 + 2.0 ** -16) * 1.001 * aH + (2.0 ** -8 + 2 * U) * rH.abs(), "dH")
+    close(dW, rW, ref.dW_bound + (3e-5 + 2.0 ** -16) * 1.001 * aW + (2.0 ** -8 + 2 * U) * rW.abs(), "dW")
+
+
+@pytest.mark.parametrize("m,k,n", [(600, 72, 4096), (3000, 100, 1024), (2500, 512, 8192)])
+def test_a_factor_of_all_rows_is_not_rounded(m, k, n):
+    """W of zeros, or H of zeros: p = 1 / n, a power of two, and P is off by 1 / n in the label's place at most; sums 4e-5, the result's rounding 2^-8.  The factor 1 + 2^-8, halfway
+    between two bfloat16 values, would be off by 2^-8 more in every term."""
+    H, W, labels, _ = inputs(m, m, k, n, torch.bfloat16, False, False, 1.0, False)
+    g = 1.0 + 2.0 ** -8
+    for h, w in ((H, torch.zeros_like(W)), (torch.zeros_like(H), W)):
+        _, lse = sagnn.softmax_xent(h, w, labels)
+        dH, dW, _ = sagnn.softmax_xent_bwd(h, w, labels, lse, g)
+        rH, rW, aH, aW = unrounded(h, w, labels, g)
+        close(dH, rH, 2.0 ** -8 * rH.abs() + (1.0 / n + 6e-5) * aH, "dH")
+        close(dW, rW, 2.0 ** -8 * rW.abs() + (1.0 / n + 6e-5) * aW, "dW")
+
+
+@pytest.mark.parametrize("m", [70, 700])
+def test_no_labelled_row_whatever_the_factor(m):
+    H, W, labels, bias = inputs(m, m, 40, 300, torch.bfloat16, False, True, 1.0, False)
+    labels.fill_(-1)
+    _, lse = sagnn.softmax_xent(H, W, labels, bias=bias)
+    for g in (float("inf"), float("nan")):
+        assert not any(t.any() for t in sagnn.softmax_xent_bwd(H, W, labels, lse, g, bias=bias))
+
+
+@pytest.mark.parametrize("m,k,n", [(758, 512, 2), (1024, 72, 300)])
+def test_weighted_bfloat16_rows_meet_one_rounding(m, k, n):
+    test_few_bfloat16_rows_meet_one_rounding(m, k, n, True)
