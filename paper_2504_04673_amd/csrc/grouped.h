@@ -648,6 +648,8 @@ TileCost tile_cost(int32_t dtype, int32_t prec, int tile);
 
 // dW of grouped_gemm_bwd for arguments that are filled in but for the launch's; ws: as much as it says
 int grouped_weights(const GroupedArgs& a, int32_t dtype, int32_t prec, hipStream_t s);
+// Bytes of its `partial`, of one group of m rows, for any types and modes
+size_t grouped_weights_bytes(int64_t m, int32_t kdim, int32_t nout);
 
 // a product of `blocks` workgroups; per operand mode (and storage type)
 #define SAGNN_GROUPED_MODE(name)                                                                                       \

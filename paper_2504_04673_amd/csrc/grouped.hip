@@ -182,6 +182,8 @@ int join_weights(const GroupedArgs& a, hipStream_t s) {
 
 }  // namespace
 
+size_t grouped_weights_bytes(int64_t m, int32_t kdim, int32_t nout) { return tn_ws_bytes(m, 1, kdim, nout); }
+
 int grouped_weights(const GroupedArgs& args, int32_t dtype, int32_t prec, hipStream_t s) {
   GroupedArgs a = args;
   const Launch l = plan_weights(a, dtype, prec);

@@ -28,12 +28,14 @@ struct XentArgs {
   float2* stats; float* z_label;             // col_tiles x m; m.  Or, with one tile of columns, NULL and
   float* loss; float* lse;                   // the results
   // grads; the rows are `map`'s
-  const int32_t* map; const float* row_lse; const float* grad; float grad_all;
+  const int32_t* map; const float* row_lse; float grad_all;
+  const float* grad;                         // weights of the rows, or NULL; of the results of `rows` too
+  bool outside;                              // they are no part of P
   float scale;                               // what is not in P (bfloat16: the factor of all rows), of dbias and the results
   void* P; int64_t ldp; int32_t stored;      // columns that are stored, zeros behind `cols`
   float* bias_parts;                         // row tiles x cols, or NULL
   // rows: `splits` shares of the summed index, `share` of it each, with sums of their own, splits x m x cols, added to from piece to piece of the
-  // classes; or, of one piece and one share, the result, rows by `map`
+  // classes; or, of one piece and one share, the result, rows by `map`, times `scale` and `grad`
   int32_t splits, share;
   float* sums; bool add;
   void* out; int64_t ldo;
@@ -241,7 +243,8 @@ __device__ __forceinline__ void xent_grads(const XentArgs& a, int64_t r0, int64_
     const int r = ((wave / C::WN) * C::TM + tm) * 32 + (lane & 31);
     const bool in = WHOLE || r < rows;
     const int64_t row = in ? a.map[r0 + r] : 0;
-    const float lse = in ? a.row_lse[row] : 0.f, g = in ? a.grad_all * (a.grad ? a.grad[row] : 1.f) : 0.f;
+    const float lse = in ? a.row_lse[row] : 0.f, own = in && a.grad ? a.grad[row] : 1.f, all = in ? a.grad_all * own : 0.f;
+    const float g = a.outside ? a.grad_all : all, rest = a.outside ? own : 1.f;          // the factor in P, and that of the bias's terms
     const int64_t far = (in ? (int64_t)a.labels[row] - a.class0 : -1) - c0 - column_of<C>(0, 0);
     const int near = far >= 0 && far < C::TN * 32 && far + column_of<C>(0, 0) < cols ? (int)far : -1;
 #pragma unroll
@@ -253,14 +256,14 @@ __device__ __forceinline__ void xent_grads(const XentArgs& a, int64_t r0, int64_
         for (int i = 0; i < 4; ++i) {
           y[i] = exp_of(acc[tm][tn][v + i] + b[tn][v + i] - lse) * g;
           if (!WHOLE) y[i] = in && column_of<C>(tn, v + i) < cols ? y[i] : 0.f;
-          sums[tn][v + i] += y[i];
+          sums[tn][v + i] += y[i] * rest;
         }
         if constexpr (kTurned) Turn<C>::put(smem, tm, tn, v, y);
         else if (in) store_four(P + r * ldp + column_of<C>(tn, v), y, stored - column_of<C>(tn, v));
         if constexpr (TWO)
           if (in) {
-            const float rest[4] = {rest_of(y[0]), rest_of(y[1]), rest_of(y[2]), rest_of(y[3])};
-            store_four(P + r * ldp + a.ldp + column_of<C>(tn, v), rest, stored - column_of<C>(tn, v));
+            const float low[4] = {rest_of(y[0]), rest_of(y[1]), rest_of(y[2]), rest_of(y[3])};
+            store_four(P + r * ldp + a.ldp + column_of<C>(tn, v), low, stored - column_of<C>(tn, v));
           }
       }
     const bool here = ours<C>(near);
@@ -269,7 +272,7 @@ __device__ __forceinline__ void xent_grads(const XentArgs& a, int64_t r0, int64_
 #pragma unroll
       for (int tn = 0; tn < C::TN; ++tn)
 #pragma unroll
-        for (int v = 0; v < 16; ++v) sums[tn][v] -= near == tn * 32 + 8 * (v / 4) + v % 4 ? g : 0.f;
+        for (int v = 0; v < 16; ++v) sums[tn][v] -= near == tn * 32 + 8 * (v / 4) + v % 4 ? all : 0.f;
       if (here) {
         if constexpr (kTurned) Turn<C>::put_one(smem, tm, near, p);
         else P[r * ldp + column_of<C>(0, 0) + near] = (S)p;
@@ -303,22 +306,28 @@ __device__ __forceinline__ void xent_rows(const XentArgs& a, int32_t split, int6
   using S = typename C::S;
   if (!a.sums) {
     S* out = reinterpret_cast<S*>(a.out) + c0;
+#pragma unroll
+    for (int tm = 0; tm < C::TM; ++tm) {
+      const int r = ((threadIdx.x >> 6) / C::WN * C::TM + tm) * 32 + (threadIdx.x & 31);
+      const float factor = a.grad && r < rows ? a.scale * a.grad[a.map[r0 + r]] : a.scale;
+#pragma unroll
+      for (int tn = 0; tn < C::TN; ++tn)
+#pragma unroll
+        for (int v = 0; v < 16; ++v) acc[tm][tn][v] *= factor;
+    }
     if constexpr (C::kTurned)
       if (a.wide) {
 #pragma unroll
         for (int i = 0; i < C::TM * C::TN * 4; ++i) {
           const int tm = i / (C::TN * 4), tn = i / 4 % C::TN, v = i % 4 * 4;
-          const float y[4] = {acc[tm][tn][v] * a.scale, acc[tm][tn][v + 1] * a.scale, acc[tm][tn][v + 2] * a.scale, acc[tm][tn][v + 3] * a.scale};
+          const float y[4] = {acc[tm][tn][v], acc[tm][tn][v + 1], acc[tm][tn][v + 2], acc[tm][tn][v + 3]};
           Turn<C>::put(smem, tm, tn, v, y);
         }
         Turn<C>::store(smem, out, rows, cols, [&](int r) { return (int64_t)a.map[r0 + r] * a.ldo; });
         return;
       }
     tile_fours<C::WM, C::WN, C::TM, C::TN>(acc, [&](int r, int c, float (&y)[4]) {
-      if (r >= rows) return;
-#pragma unroll
-      for (int i = 0; i < 4; ++i) y[i] *= a.scale;
-      store_four(out + (int64_t)a.map[r0 + r] * a.ldo + c, y, cols - c);
+      if (r < rows) store_four(out + (int64_t)a.map[r0 + r] * a.ldo + c, y, cols - c);
     });
     return;
   }
@@ -455,10 +464,12 @@ __global__ __launch_bounds__(kThinWaves * 64) void xent_thin_kernel(const XentAr
   const bool in = r < t.rows;
   if constexpr (MODE == kXentRows) {
     float* to = a.sums ? a.sums + (t.split * a.m + t.r0 + r) * a.cols + t.c0 + c : nullptr;
+    const int64_t row = in && !to ? (int64_t)a.map[t.r0 + r] : 0;
+    const float factor = a.grad && in && !to ? a.scale * a.grad[row] : a.scale;
 #pragma unroll
     for (int i = 0; i < 2; ++i)
       if (in && c + i < t.cols) {
-        if (!to) reinterpret_cast<S*>(a.out)[(int64_t)a.map[t.r0 + r] * a.ldo + t.c0 + c + i] = (S)(y[i] * a.scale);
+        if (!to) reinterpret_cast<S*>(a.out)[row * a.ldo + t.c0 + c + i] = (S)(y[i] * factor);
         else to[i] = a.add ? to[i] + y[i] : y[i];
       }
     return;
@@ -483,7 +494,8 @@ __global__ __launch_bounds__(kThinWaves * 64) void xent_thin_kernel(const XentAr
       a.loss[row] = label >= 0 && label < a.classes ? lse - z : 0.f;
     }
   } else {
-    const float lse = in ? a.row_lse[row] : 0.f, g = in ? a.grad_all * (a.grad ? a.grad[row] : 1.f) : 0.f;
+    const float lse = in ? a.row_lse[row] : 0.f, own = in && a.grad ? a.grad[row] : 1.f, all = in ? a.grad_all * own : 0.f;
+    const float g = a.outside ? a.grad_all : all, rest = a.outside ? own : 1.f;
     S* P = reinterpret_cast<S*>(a.P) + (t.r0 + r) * (MODE == kXentTwo ? 2 * a.ldp : a.ldp) + t.c0;
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
@@ -494,7 +506,7 @@ __global__ __launch_bounds__(kThinWaves * 64) void xent_thin_kernel(const XentAr
       }
     }
     if (!a.bias_parts) return;
-    *reinterpret_cast<float2*>(sums + r * kRow + c) = make_float2(y[0], y[1]);
+    *reinterpret_cast<float2*>(sums + r * kRow + c) = make_float2(y[0] * rest, y[1] * rest);
     __syncthreads();
     if (tid < t.cols) {
       float x = 0.f;

@@ -29,10 +29,13 @@ constexpr int64_t kLeastBytes = int64_t(4) << 30;   // of P in pieces of kPieceL
 // Pieces at most: dH's sums are added over them in turn, in 32 bits
 constexpr int32_t kPiecesMost = 384;
 // Rows up to which a bfloat16 P is kept in two terms, the value and what its rounding leaves, each of them a row of dH's and dW's products: they meet 2^-16 of P,
-// not 2^-8.  Of more rows those roundings average out against the results' own; of few one of them decides (a row's label outweighs its other classes), and
-// the gradients were up to three times as far off as by their own rounding.  The weights' bytes bound these products where rows are few
+// not 2^-8.  Of more rows those roundings add to the results' own as errors of other sign (1.05 to 1.3 times in the norm, 2000 to 2 classes); of few one of them decides (a row's
+// label outweighs its other classes), and the gradients were up to three times as far off as by their own rounding.  The weights' bytes bound these products where rows are few
 // (a step, with one term and with two: 1 x 256 x 50000 72 and 77 us, 16 x 1024 x 131072 343 and 358, 128 x 4096 x 131072 1395 and 1675, 512 x 256 x 32768 112 and 148).
-// With a weight of its own every row's label is rounded elsewhere, which averages out later: 758 rows, half of them labelled, of 2 classes 0.0025 against 0.0017.
+// Beyond that weights of the rows are no part of P: equal ones would round most labels' terms alike and shift all gradients by up to 2^-8 (3000 x 256 x 2000, weights of 1 + 2^-8:
+// 0.0040 against 64 bits, the results' own rounding being 0.0017, 0.0017 this way; random weights 0.0022 and 0.0017).  dH's rows are multiplied by them
+// afterwards; dW sums over the rows, so that they are on the other operand, two terms of weighted H beside each other in twice the columns (a step with weights,
+// in P and this way: 2 M x 128 x 47 970 and 1380 us, 170 k x 128 x 172 168 and 193, 8192 x 128 x 65536 1610 and 1727, 8192 x 1024 x 131072 8.05 and 10.5 ms).
 constexpr int64_t kTwoTerms = 512, kTwoTermsWeighted = 1024;
 // Bytes of the sums of dH's shares
 constexpr int64_t kSumBytes = int64_t(512) << 20;
@@ -54,13 +57,14 @@ __global__ __launch_bounds__(kListThreads) void label_count_kernel(const int32_t
 
 // map[i] = row of the i-th label; H's rows one behind the other in rows of ldc values (zeros behind the k there are), unless every row has one and
 // `needed` is not set: then H itself will do; each as often as P has terms; zeros in dH's rows without one, and in `clear`.  bounds = {0, how many, 0, how many
-// rows of terms}.  counts NULL: few rows, whose labels each block counts itself.
-template <typename T>
+// rows of terms}.  counts NULL: few rows, whose labels each block counts itself.  `weighted`, if so: the rows, rounded to bfloat16 as the products
+// take them, times `weights`, each in two bfloat16 terms of ldc values beside each other.
+template <typename T, bool WEIGHTED>
 __global__ __launch_bounds__(kListThreads) void label_list_kernel(const int32_t* __restrict__ labels, int64_t m, int64_t each, int32_t classes,
                                                                   const int32_t* __restrict__ counts, int32_t* __restrict__ map, int32_t* __restrict__ bounds,
                                                                   const T* __restrict__ H, int64_t ldh, int32_t k, T* __restrict__ rows, int64_t ldc, int terms,
                                                                   T* __restrict__ dH, int64_t lddh, int lanes, bool needed, float* __restrict__ clear,
-                                                                  int32_t n_clear) {
+                                                                  int32_t n_clear, const float* __restrict__ weights, T* __restrict__ weighted) {
   __shared__ int32_t room[kListThreads / 64];
   __shared__ int32_t place[kListThreads];          // of a row of the round: its number in the list, or -1
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -109,12 +113,29 @@ __global__ __launch_bounds__(kListThreads) void label_list_kernel(const int32_t*
     const int n = end - r0 < kListThreads ? (int)(end - r0) : kListThreads, own = threadIdx.x & (lanes - 1);
     for (int i = threadIdx.x / lanes; i < n; i += kListThreads / lanes) {
       const int32_t to = place[i];
-      if (to >= 0 && !needed && every == m) break;
-      if (to >= 0)
+      const bool copied = needed || every != m;
+      if (to >= 0 && !copied && !WEIGHTED) break;
+      if (to >= 0) {
+        float g = 1.f;
+        if constexpr (WEIGHTED) g = weights[r0 + i];
         for (int c = own * 8; c < ldc; c += lanes * 8) {
           const auto w = load_eight(H + (r0 + i) * ldh + c, k - c, k);
-          for (int e = 0; e < terms; ++e) *reinterpret_cast<TightRun<T, 8>*>(rows + ((int64_t)to * terms + e) * ldc + c) = w;
+          if (copied)
+            for (int e = 0; e < terms; ++e) *reinterpret_cast<TightRun<T, 8>*>(rows + ((int64_t)to * terms + e) * ldc + c) = w;
+          if constexpr (WEIGHTED) {
+            TightRun<T, 8> high, low;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+              const float x = (float)(__bf16)w.x[e] * g;
+              high.x[e] = (T)(__bf16)x;
+              low.x[e] = (T)rest_of(x);
+            }
+            T* to_w = weighted + (int64_t)to * 2 * ldc + c;
+            *reinterpret_cast<TightRun<T, 8>*>(to_w) = high;
+            *reinterpret_cast<TightRun<T, 8>*>(to_w + ldc) = low;
+          }
         }
+      }
       else if (dH)
         for (int c = own * 8; c < k; c += lanes * 8) store_eight(dH + (r0 + i) * lddh + c, {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f}, k - c);
     }
@@ -179,10 +200,10 @@ __global__ __launch_bounds__(kBiasThreads) void xent_bias_kernel(const float* __
   }
 }
 
-// dH's listed rows: the sum of the shares' sums, m rows each, of a row's terms
+// dH's listed rows: the sum of the shares' sums, m rows each, of a row's terms, times its weight (grad, may be NULL)
 template <typename T>
-__global__ __launch_bounds__(256) void xent_rows_kernel(const float* __restrict__ sums, int32_t splits, int64_t m, int terms, float scale, const int32_t* __restrict__ bounds, int32_t k,
-                                                        const int32_t* __restrict__ map, T* __restrict__ dH, int64_t lddh) {
+__global__ __launch_bounds__(256) void xent_rows_kernel(const float* __restrict__ sums, int32_t splits, int64_t m, int terms, float scale, const float* __restrict__ grad,
+                                                        const int32_t* __restrict__ bounds, int32_t k, const int32_t* __restrict__ map, T* __restrict__ dH, int64_t lddh) {
   const int64_t fours = (k + 3) / 4, all = bounds[1] * fours;
   for (int64_t i = blockIdx.x * 256ll + threadIdx.x; i < all; i += gridDim.x * 256ll) {
     const int64_t r = i / fours;
@@ -205,15 +226,18 @@ __global__ __launch_bounds__(256) void xent_rows_kernel(const float* __restrict_
         for (int e = 0; e < 3; ++e)
           if (c + e < k) y[e] += part(s)[e];
     }
+    const int64_t row = map[r];
+    const float factor = grad ? scale * grad[row] : scale;
 #pragma unroll
-    for (int e = 0; e < 4; ++e) y[e] *= scale;
-    store_four(dH + map[r] * lddh + c, y, k - c);
+    for (int e = 0; e < 4; ++e) y[e] *= factor;
+    store_four(dH + row * lddh + c, y, k - c);
   }
 }
 
-// A piece's dW from fp32 into its place (no rows: zeros, whatever the scale is)
+// A piece's dW from fp32 into its place (no rows: zeros, whatever the scale is).  second: how far behind a value the rest of it is that weighted rows' second
+// terms make; 0: there is none
 template <typename T>
-__global__ __launch_bounds__(256) void xent_convert_kernel(const float* __restrict__ from, int64_t ldf, int64_t rows, int32_t cols, float factor,
+__global__ __launch_bounds__(256) void xent_convert_kernel(const float* __restrict__ from, int64_t ldf, int64_t second, int64_t rows, int32_t cols, float factor,
                                                            const int32_t* __restrict__ bounds, T* __restrict__ to, int64_t ldt) {
   const float scale = bounds[1] > 0 ? factor : 0.f;
   const int64_t fours = (cols + 3) / 4, all = rows * fours;
@@ -222,7 +246,10 @@ __global__ __launch_bounds__(256) void xent_convert_kernel(const float* __restri
     const int c = (int)(i - r * fours) * 4;
     float y[4];
 #pragma unroll
-    for (int e = 0; e < 4; ++e) y[e] = c + e < cols ? from[r * ldf + c + e] * scale : 0.f;
+    for (int e = 0; e < 4; ++e) {
+      const float* x = from + r * ldf + c + e;
+      y[e] = c + e < cols ? (second ? x[0] + x[second] : x[0]) * scale : 0.f;
+    }
     store_four(to + r * ldt + c, y, cols - c);
   }
 }
@@ -332,15 +359,17 @@ bool whole_weights(int32_t dtype, int64_t m, int32_t kdim, int32_t classes) {
 
 struct BwdPlan {
   int32_t terms;                             // of P
+  bool outside;                              // the rows' weights are no part of P: dH's rows are multiplied by them, and dW's product takes weighted rows of H
   int32_t piece, pieces;                     // classes of a piece
   int32_t splits;                            // shares of them that there is room for in dH's sums
   int64_t ldp, ldc;                          // of P, of the listed rows
-  size_t map, bounds, counts, rows, P, sums, weights, parts, bias, weights_bytes, parts_bytes, total;
+  size_t map, bounds, counts, rows, weighted, P, sums, weights, parts, bias, weights_bytes, parts_bytes, total;
 };
 int32_t terms_of(int32_t dtype, int64_t m, bool weighted) { return dtype == SAGNN_BF16 && m <= (weighted ? kTwoTermsWeighted : kTwoTerms) ? 2 : 1; }
-BwdPlan bwd_plan(int32_t dtype, int32_t prec, int32_t terms, int64_t m, int32_t kdim, int32_t classes) {
+BwdPlan bwd_plan(int32_t dtype, int32_t prec, bool weighted, int64_t m, int32_t kdim, int32_t classes) {
   BwdPlan p{};
-  p.terms = terms;
+  p.terms = terms_of(dtype, m, weighted);
+  p.outside = weighted && p.terms == 1 && products(dtype, prec) == SAGNN_GEMM_BF16;
   const int64_t size = dtype == SAGNN_BF16 ? 2 : 4, rows = m > 0 ? m : 1;
   int64_t most = kPieceBytes / (rows * size) / 256 * 256;
   const int32_t least = rows * size * kPieceLeast <= kLeastBytes ? kPieceLeast : 256;
@@ -352,14 +381,12 @@ BwdPlan bwd_plan(int32_t dtype, int32_t prec, int32_t terms, int64_t m, int32_t 
   p.ldp = (int64_t)round_up((size_t)p.piece, 8);
   p.ldc = (int64_t)round_up((size_t)kdim, 8);
   // dW's products, in either order, of a whole piece and of the last (which may be cut into more parts)
-  const int32_t kw = padded_width(dtype, kdim);
+  const int32_t kw = p.outside ? (int32_t)(2 * p.ldc) : padded_width(dtype, kdim);
   const int32_t last = classes - (p.pieces - 1) * p.piece;
   for (int32_t n : {p.piece, last}) {
-    if (whole_weights(dtype, m * p.terms, kdim, n)) continue;
+    if (!p.outside && whole_weights(dtype, m * p.terms, kdim, n)) continue;
     p.weights_bytes = (size_t)padded_width(dtype, p.piece) * kw * 4;
-    size_t one = 0, two = 0;
-    grouped_gemm_bwd_workspace_bytes(m * p.terms, 1, kw, padded_width(dtype, n), &one);
-    grouped_gemm_bwd_workspace_bytes(m * p.terms, 1, padded_width(dtype, n), kw, &two);
+    const size_t one = grouped_weights_bytes(m * p.terms, kw, padded_width(dtype, n)), two = grouped_weights_bytes(m * p.terms, padded_width(dtype, n), kw);
     p.parts_bytes = one > p.parts_bytes ? one : p.parts_bytes;
     p.parts_bytes = two > p.parts_bytes ? two : p.parts_bytes;
     if (last == p.piece) break;
@@ -369,6 +396,7 @@ BwdPlan bwd_plan(int32_t dtype, int32_t prec, int32_t terms, int64_t m, int32_t 
   p.bounds = room.take(16);
   p.counts = room.take(kListBlocks * 4);
   p.rows = room.take((size_t)rows * p.terms * p.ldc * size);
+  p.weighted = room.take(p.outside ? (size_t)rows * 2 * p.ldc * size : 0);
   p.P = room.take((size_t)rows * p.terms * p.ldp * size);
   // dH's sums: of every share of a piece's classes
   const int64_t share = rows * p.terms * kdim * 4;
@@ -388,7 +416,7 @@ BwdPlan bwd_plan(int32_t dtype, int32_t prec, int32_t terms, int64_t m, int32_t 
 
 template <typename T>
 int list_labels(const BwdPlan& p, char* ws, const int32_t* labels, int64_t m, int32_t classes, const void* H, int64_t ldh, int32_t k, void* dH, int64_t lddh,
-                bool needed, float* clear, int32_t n_clear, hipStream_t s) {
+                bool needed, float* clear, int32_t n_clear, const float* weights, hipStream_t s) {
   // (many small blocks: 8192 rows of 1024 in blocks of 256 took 429 us)
   int64_t each = ceil_div(m, kListBlocks);
   if (each < 16) each = 16;
@@ -402,8 +430,12 @@ int list_labels(const BwdPlan& p, char* ws, const int32_t* labels, int64_t m, in
     label_count_kernel<<<dim3(blocks), kListThreads, 0, s>>>(labels, m, each, classes, counts);
     SAGNN_LAUNCH_CHECK();
   }
-  label_list_kernel<T><<<dim3(blocks), kListThreads, 0, s>>>(labels, m, each, classes, counts, map, bounds, (const T*)H, ldh, k, (T*)(ws + p.rows), p.ldc, p.terms,
-                                                            (T*)dH, lddh, lanes, needed, clear, n_clear);
+  auto list = [&](auto kernel) {
+    kernel<<<dim3(blocks), kListThreads, 0, s>>>(labels, m, each, classes, counts, map, bounds, (const T*)H, ldh, k, (T*)(ws + p.rows), p.ldc, p.terms, (T*)dH, lddh,
+                                                 lanes, needed, clear, n_clear, weights, (T*)(ws + p.weighted));
+  };
+  if (p.outside) list(label_list_kernel<T, true>);
+  else list(label_list_kernel<T, false>);
   SAGNN_LAUNCH_CHECK();
   return SAGNN_OK;
 }
@@ -425,7 +457,7 @@ SAGNN_EXPORT int softmax_xent_workspace_bytes(int32_t dtype, int64_t m, int32_t 
   if (backward) {
     *bytes = 0;                              // (for either kind of gradient)
     for (bool weighted : {false, true}) {
-      const size_t b = bwd_plan(dtype, prec, terms_of(dtype, m, weighted), m, kdim, n_classes).total;
+      const size_t b = bwd_plan(dtype, prec, weighted, m, kdim, n_classes).total;
       if (b > *bytes) *bytes = b;
     }
   } else {                                   // (room for any strides and alignments)
@@ -494,7 +526,7 @@ SAGNN_EXPORT int softmax_xent_bwd(int32_t dtype, const void* d_H, int64_t ldh, c
         if (!clear_of(out[o].p, out[o].bytes, out[q].p, out[q].bytes)) return SAGNN_EINVAL;
     }
   }
-  const BwdPlan p = bwd_plan(dtype, prec, terms_of(dtype, m, d_grad != nullptr), m, kdim, n_classes);
+  const BwdPlan p = bwd_plan(dtype, prec, d_grad != nullptr, m, kdim, n_classes);
   if (!d_ws) return SAGNN_EINVAL;
   if (ws_bytes < p.total) return SAGNN_ECAPACITY;
   char* ws = (char*)d_ws;
@@ -509,8 +541,8 @@ SAGNN_EXPORT int softmax_xent_bwd(int32_t dtype, const void* d_H, int64_t ldh, c
   const int32_t last = n_classes - (p.pieces - 1) * p.piece;
   const bool direct_bias = d_dbias && m <= grouped_tile_rows(logits(d_W, p.piece).tile) && m <= grouped_tile_rows(logits(d_W, last).tile);
   float* clear = direct_bias ? d_dbias : nullptr;
-  int rc = dtype == SAGNN_BF16 ? list_labels<__bf16>(p, ws, d_labels, m, n_classes, d_H, ldh, kdim, d_dH, lddh, !itself, clear, n_classes, s)
-                               : list_labels<float>(p, ws, d_labels, m, n_classes, d_H, ldh, kdim, d_dH, lddh, !itself, clear, n_classes, s);
+  int rc = dtype == SAGNN_BF16 ? list_labels<__bf16>(p, ws, d_labels, m, n_classes, d_H, ldh, kdim, d_dH, lddh, !itself, clear, n_classes, d_grad, s)
+                               : list_labels<float>(p, ws, d_labels, m, n_classes, d_H, ldh, kdim, d_dH, lddh, !itself, clear, n_classes, d_grad, s);
   const int32_t* bounds = (const int32_t*)(ws + p.bounds);
   const int32_t* term_bounds = bounds + (p.terms == 2 ? 2 : 0);
   const int64_t terms = m * p.terms;
@@ -522,7 +554,7 @@ SAGNN_EXPORT int softmax_xent_bwd(int32_t dtype, const void* d_H, int64_t ldh, c
     XentArgs a{};
     a.X = ws + p.rows; a.ldx = p.ldc * p.terms; a.W = (const char*)d_W + (size_t)at * (transW ? ldw : 1) * size; a.ldw = ldw; a.m = m; a.count = bounds + 1;
     a.all = itself ? d_H : nullptr; a.ldall = ldh; a.cols = n; a.sum = kdim; a.mode = p.terms == 2 ? kXentTwo : kXentGrads; a.bias = d_bias ? d_bias + at : nullptr; a.labels = d_labels; a.class0 = at; a.classes = n_classes;
-    a.map = (const int32_t*)(ws + p.map); a.row_lse = d_lse; a.grad = d_grad; a.grad_all = dtype == SAGNN_BF16 ? 1.f : (float)grad_all; a.scale = scale; a.P = ws + p.P; a.ldp = p.ldp;
+    a.map = (const int32_t*)(ws + p.map); a.row_lse = d_lse; a.grad = d_grad; a.outside = p.outside; a.grad_all = dtype == SAGNN_BF16 ? 1.f : (float)grad_all; a.scale = scale; a.P = ws + p.P; a.ldp = p.ldp;
     a.stored = (int32_t)round_up((size_t)n, 8); a.bias_parts = direct_bias ? d_dbias + at : d_dbias ? (float*)(ws + p.bias) : nullptr;
     a.padded = (int32_t)p.ldc;
     const TilePick tile = logits(a.W, n);
@@ -542,18 +574,18 @@ SAGNN_EXPORT int softmax_xent_bwd(int32_t dtype, const void* d_H, int64_t ldh, c
       if (pick.splits == 1) pick.share = n;
       XentArgs b{};
       b.X = a.P; b.ldx = p.ldp; b.W = a.W; b.ldw = ldw; b.m = terms; b.count = term_bounds + 1; b.scale = scale; b.cols = kdim; b.sum = n; b.mode = kXentRows; b.map = a.map;
-      b.sums = summed ? (float*)(ws + p.sums) : nullptr; b.add = at > 0; b.out = d_dH; b.ldo = lddh;
+      b.grad = p.outside ? d_grad : nullptr; b.sums = summed ? (float*)(ws + p.sums) : nullptr; b.add = at > 0; b.out = d_dH; b.ldo = lddh;
       b.padded = a.stored; b.wide = aligned16(d_dH) && lddh % 8 == 0 && kdim % 8 == 0;
       rc = launch(b, dtype, prec, pick, transW == 0, s);
       if (rc == SAGNN_OK && summed && at + n == n_classes) {
         const int64_t blocks = ceil_div(m * ceil_div(kdim, 4), 256);
         const dim3 grid((uint32_t)(blocks < 8192 ? blocks : 8192));
-        if (dtype == SAGNN_BF16) xent_rows_kernel<__bf16><<<grid, 256, 0, s>>>(b.sums, rows.splits, terms, p.terms, scale, bounds, kdim, b.map, (__bf16*)d_dH, lddh);
-        else xent_rows_kernel<float><<<grid, 256, 0, s>>>(b.sums, rows.splits, terms, p.terms, scale, bounds, kdim, b.map, (float*)d_dH, lddh);
+        if (dtype == SAGNN_BF16) xent_rows_kernel<__bf16><<<grid, 256, 0, s>>>(b.sums, rows.splits, terms, p.terms, scale, b.grad, bounds, kdim, b.map, (__bf16*)d_dH, lddh);
+        else xent_rows_kernel<float><<<grid, 256, 0, s>>>(b.sums, rows.splits, terms, p.terms, scale, b.grad, bounds, kdim, b.map, (float*)d_dH, lddh);
         SAGNN_LAUNCH_CHECK();
       }
     }
-    if (rc == SAGNN_OK && d_dW && whole_weights(dtype, terms, kdim, n)) {
+    if (rc == SAGNN_OK && d_dW && !p.outside && whole_weights(dtype, terms, kdim, n)) {
       XentWeightArgs w{};
       const void* whole = itself ? d_H : a.X;
       const int64_t ldwhole = itself ? ldh : p.ldc;
@@ -566,14 +598,17 @@ SAGNN_EXPORT int softmax_xent_bwd(int32_t dtype, const void* d_H, int64_t ldh, c
       rc = xent_weights_bf16(w, s);
     } else if (rc == SAGNN_OK && d_dW) {
       // (fp32 weights whose piece lies in one place are written there)
-      const bool there = dtype == SAGNN_F32 && (transW || p.pieces == 1);
+      const bool there = dtype == SAGNN_F32 && !p.outside && (transW || p.pieces == 1);
       float* dW = there ? (float*)d_dW + (size_t)at * (transW ? kdim : 1) : (float*)(ws + p.weights);
       GroupedArgs w{};
       w.off = term_bounds; w.groups = 1; w.m = terms; w.dW = dW; w.partial = (float*)(ws + p.parts);
-      const int32_t kw = padded_width(dtype, kdim), nw = padded_width(dtype, n);
-      w.X = transW ? a.P : a.X; w.ldx = transW ? p.ldp : p.ldc; w.kdim = transW ? nw : kw;
-      w.G = transW ? a.X : a.P; w.ldg = transW ? p.ldc : p.ldp; w.nout = transW ? kw : nw;
-      if (itself) {
+      // (weighted rows: their two terms are the first and the second half of one operand's columns, and dW their products' sum)
+      const int32_t kw = p.outside ? (int32_t)(2 * p.ldc) : padded_width(dtype, kdim), nw = padded_width(dtype, n);
+      const void* rows_of_h = p.outside ? ws + p.weighted : a.X;
+      const int64_t ldr = p.outside ? 2 * p.ldc : p.ldc;
+      w.X = transW ? a.P : rows_of_h; w.ldx = transW ? p.ldp : ldr; w.kdim = transW ? nw : kw;
+      w.G = transW ? rows_of_h : a.P; w.ldg = transW ? ldr : p.ldp; w.nout = transW ? kw : nw;
+      if (itself && !p.outside) {
         w.listed = bounds + 1;
         w.X2 = transW ? a.P : d_H; w.ldx2 = transW ? p.ldp : ldh;
         w.G2 = transW ? d_H : a.P; w.ldg2 = transW ? ldh : p.ldp;
@@ -585,8 +620,9 @@ SAGNN_EXPORT int softmax_xent_bwd(int32_t dtype, const void* d_H, int64_t ldh, c
         const int64_t blocks = ceil_div(rows * ceil_div(cols, 4), 256);
         const dim3 grid((uint32_t)(blocks < 4096 ? blocks : 4096));
         const size_t first = (size_t)at * (transW ? kdim : 1);
-        if (dtype == SAGNN_BF16) xent_convert_kernel<__bf16><<<grid, 256, 0, s>>>(dW, w.nout, rows, cols, scale, bounds, (__bf16*)d_dW + first, ldt);
-        else xent_convert_kernel<float><<<grid, 256, 0, s>>>(dW, w.nout, rows, cols, scale, bounds, (float*)d_dW + first, ldt);
+        const int64_t second = !p.outside ? 0 : transW ? p.ldc : p.ldc * (int64_t)w.nout;
+        if (dtype == SAGNN_BF16) xent_convert_kernel<__bf16><<<grid, 256, 0, s>>>(dW, w.nout, second, rows, cols, scale, bounds, (__bf16*)d_dW + first, ldt);
+        else xent_convert_kernel<float><<<grid, 256, 0, s>>>(dW, w.nout, second, rows, cols, scale, bounds, (float*)d_dW + first, ldt);
         SAGNN_LAUNCH_CHECK();
       }
     }
