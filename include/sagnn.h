@@ -752,8 +752,8 @@ int spmm_pack_rows_e4m3(const void* d_Q, int64_t ldq, const float* d_scale, int6
  * A label outside [0, n_classes) says that the row has none: its loss is 0, its row of dH zeros, and it is no part of dW and dbias, whatever its H holds; its lse is that of the formula.
  * dtype: type of H, W, dH and dW; bias, loss, lse, grad and dbias are fp32.  dW is dense and laid out like W.  prec: as in grouped_gemm_act.  Sums are fp32 or more, cut into runs as
  * there, their order fixed: the same bits every time.  Backward the classes are taken in pieces; a piece's P is rounded to dtype once, ahead of
- * its products, in bfloat16 without grad_all, which its sums are multiplied by.  Where the products take bfloat16 operands d_grad is no part of P either: dH's rows are
- * multiplied by it in fp32, and dW's product takes rows of H times d_grad, in two bfloat16 terms, off by 2^-16.  P's rounding puts each term of dH and dW off by 2^-8 of itself at most:
+ * its products.  Where those take bfloat16 operands grad_all and d_grad are no part of it: sums are multiplied by the first, dH's rows
+ * by the second in fp32, and dW's product takes rows of H times d_grad, in two bfloat16 terms, off by 2^-16.  P's rounding puts each term of dH and dW off by 2^-8 of itself at most:
  * in the norm their errors are 1.05 to 1.3 times those of their own rounding, the more the fewer classes there are.  Up to 512 bfloat16 rows, 1024 with d_grad, where one
  * label's rounding decides, P (with d_grad) is kept in two terms, off by 2^-16.  dbias is summed of what is not rounded.  Infinite and NaN logits give what the formula gives: a bias of -inf takes a class out.
  * Any kdim up to SAGNN_GROUPED_MAX_WIDTH, n_classes up to SAGNN_XENT_MAX_CLASSES, any leading dimensions not below the width, tensors aligned to their element; rows that begin on 16

@@ -31,7 +31,7 @@ struct XentArgs {
   const int32_t* map; const float* row_lse; float grad_all;
   const float* grad;                         // weights of the rows, or NULL; of the results of `rows` too
   bool outside;                              // they are no part of P
-  float scale;                               // what is not in P (bfloat16: the factor of all rows), of dbias and the results
+  float scale;                               // what is not in P (of bfloat16 products: the factor of all rows), of dbias and the results
   void* P; int64_t ldp; int32_t stored;      // columns that are stored, zeros behind `cols`
   float* bias_parts;                         // row tiles x cols, or NULL
   // rows: `splits` shares of the summed index, `share` of it each, with sums of their own, splits x m x cols, added to from piece to piece of the

@@ -234,11 +234,11 @@ __global__ __launch_bounds__(256) void xent_rows_kernel(const float* __restrict_
   }
 }
 
-// A piece's dW from fp32 into its place (no rows: zeros, whatever the scale is).  second: how far behind a value the rest of it is that weighted rows' second
+// A piece's dW from fp32 into its place, or times the scale where it is (no rows: zeros, whatever that is).  second: how far behind a value the rest of it is that weighted rows' second
 // terms make; 0: there is none
 template <typename T>
-__global__ __launch_bounds__(256) void xent_convert_kernel(const float* __restrict__ from, int64_t ldf, int64_t second, int64_t rows, int32_t cols, float factor,
-                                                           const int32_t* __restrict__ bounds, T* __restrict__ to, int64_t ldt) {
+__global__ __launch_bounds__(256) void xent_convert_kernel(const float* from, int64_t ldf, int64_t second, int64_t rows, int32_t cols, float factor,
+                                                           const int32_t* __restrict__ bounds, T* to, int64_t ldt) {
   const float scale = bounds[1] > 0 ? factor : 0.f;
   const int64_t fours = (cols + 3) / 4, all = rows * fours;
   for (int64_t i = blockIdx.x * 256ll + threadIdx.x; i < all; i += gridDim.x * 256ll) {
@@ -546,15 +546,17 @@ SAGNN_EXPORT int softmax_xent_bwd(int32_t dtype, const void* d_H, int64_t ldh, c
   const int32_t* bounds = (const int32_t*)(ws + p.bounds);
   const int32_t* term_bounds = bounds + (p.terms == 2 ? 2 : 0);
   const int64_t terms = m * p.terms;
-  // A factor of all rows is no part of a bfloat16 P: its rounding would be one for most labels' terms and shift all gradients by up to 2^-8
-  const float scale = dtype == SAGNN_BF16 ? (float)grad_all : 1.f;
+  // A factor of all rows is no part of a P that is rounded to bfloat16, here or on its way into the products: its rounding would be one for most labels'
+  // terms and shift all gradients by up to 2^-8
+  const bool rounded = products(dtype, prec) == SAGNN_GEMM_BF16;
+  const float scale = rounded ? (float)grad_all : 1.f;
   TilePick rows{};
   for (int32_t at = 0; at < n_classes && rc == SAGNN_OK; at += p.piece) {
     const int32_t n = n_classes - at < p.piece ? n_classes - at : p.piece;
     XentArgs a{};
     a.X = ws + p.rows; a.ldx = p.ldc * p.terms; a.W = (const char*)d_W + (size_t)at * (transW ? ldw : 1) * size; a.ldw = ldw; a.m = m; a.count = bounds + 1;
     a.all = itself ? d_H : nullptr; a.ldall = ldh; a.cols = n; a.sum = kdim; a.mode = p.terms == 2 ? kXentTwo : kXentGrads; a.bias = d_bias ? d_bias + at : nullptr; a.labels = d_labels; a.class0 = at; a.classes = n_classes;
-    a.map = (const int32_t*)(ws + p.map); a.row_lse = d_lse; a.grad = d_grad; a.outside = p.outside; a.grad_all = dtype == SAGNN_BF16 ? 1.f : (float)grad_all; a.scale = scale; a.P = ws + p.P; a.ldp = p.ldp;
+    a.map = (const int32_t*)(ws + p.map); a.row_lse = d_lse; a.grad = d_grad; a.outside = p.outside; a.grad_all = rounded ? 1.f : (float)grad_all; a.scale = scale; a.P = ws + p.P; a.ldp = p.ldp;
     a.stored = (int32_t)round_up((size_t)n, 8); a.bias_parts = direct_bias ? d_dbias + at : d_dbias ? (float*)(ws + p.bias) : nullptr;
     a.padded = (int32_t)p.ldc;
     const TilePick tile = logits(a.W, n);
@@ -614,7 +616,7 @@ SAGNN_EXPORT int softmax_xent_bwd(int32_t dtype, const void* d_H, int64_t ldh, c
         w.G2 = transW ? d_H : a.P; w.ldg2 = transW ? ldh : p.ldp;
       }
       rc = grouped_weights(w, dtype, prec, s);
-      if (rc == SAGNN_OK && !there) {
+      if (rc == SAGNN_OK && (!there || scale != 1.f)) {
         const int64_t rows = transW ? n : kdim, ldt = transW ? kdim : n_classes;
         const int32_t cols = transW ? kdim : n;
         const int64_t blocks = ceil_div(rows * ceil_div(cols, 4), 256);

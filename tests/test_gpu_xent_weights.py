@@ -117,3 +117,22 @@ def test_weighted_step_captured_and_replayed():
         graph.replay()
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(got, ref))
+
+
+@pytest.mark.parametrize("trans", [False, True])
+@pytest.mark.parametrize("m,k,n,labelled", [(20, 40, 4096, 1.0), (600, 72, 4096, 1.0), (3000, 100, 1024, 0.6), (2500, 512, 8192, 1.0), (40, 200, 65536, 1.0)])
+def test_a_factor_of_all_rows_is_not_rounded_on_its_way_into_products(m, k, n, labelled, trans):
+    """fp32 tensors whose products round operands: as for equal weights above."""
+    H, W, labels, _ = inputs(m, m, k, n, torch.bfloat16, False, False, labelled, False)
+    H, W, g = H.float(), W.float(), 1.0 + 2.0 ** -8
+    known = (labels >= 0) & (labels < n)
+    for h, w in ((H, torch.zeros_like(W)), (torch.zeros_like(H), W)):
+        w_ = w.t().contiguous() if trans else w
+        _, lse = sagnn.softmax_xent(h, w_, labels, transW=trans, prec=sagnn.GEMM_BF16)
+        dH, dW, _ = sagnn.softmax_xent_bwd(h, w_, labels, lse, g, transW=trans, prec=sagnn.GEMM_BF16)
+        rH, rW, aH, aW = unrounded(h[known], w, labels[known], g)
+        close(dH[known], rH, (1.0 / n + 6e-5) * aH, "dH")
+        close(dW.t() if trans else dW, rW, (1.0 / n + 6e-5) * aW, "dW")
+    for g in (float("inf"), float("nan")):
+        none = torch.full_like(labels, -1)
+        assert not any(t.any() for t in sagnn.softmax_xent_bwd(H, w_, none, lse, g, transW=trans, prec=sagnn.GEMM_BF16)[:2])
