@@ -148,25 +148,48 @@ __global__ __launch_bounds__(kListThreads) void label_list_kernel(const int32_t*
   }
 }
 
-// lse and loss of a row from its tiles of columns: 2^log_rows rows a workgroup, its other threads share their tiles
+// lse and loss of a row from its tiles of columns: 2^log_rows rows a workgroup, its other threads share their tiles, eight at a time.  Sums in 64 bits, and what moves
+// them to a new maximum too: there may be half a million tiles, and what their sum loses every class's gradient has (16.7 M classes below a larger one, in chains of
+// 32 bits: 1.3e-4).
+__device__ __forceinline__ double moved_sum(double sum, float from, float to) {
+  return sum == 0. || from == to ? sum : sum * exp((double)shift_of(from) - (double)shift_of(to));
+}
 __global__ __launch_bounds__(256) void xent_join_kernel(const float2* __restrict__ stats, const float* __restrict__ z_label, int64_t m, int32_t tiles,
                                                         const int32_t* __restrict__ labels, int32_t classes, int log_rows, float* __restrict__ loss,
                                                         float* __restrict__ lse) {
-  __shared__ float2 room[256];
-  const int rows = 1 << log_rows, own = threadIdx.x & (rows - 1), shares = 256 >> log_rows;
+  __shared__ float top[256];
+  __shared__ double room[256];
+  const int rows = 1 << log_rows, own = threadIdx.x & (rows - 1), shares = 256 >> log_rows, first = threadIdx.x >> log_rows;
   const int64_t r = ((int64_t)blockIdx.x << log_rows) + own;
-  float most = -INFINITY, sum = 0.f;
+  float most = -INFINITY;
+  double sum = 0.;
   if (r < m)
-#pragma unroll 4
-    for (int t = threadIdx.x >> log_rows; t < tiles; t += shares) {
-      const float2 p = stats[t * m + r];
-      join_stats(most, sum, p.x, p.y);
+    for (int t = first; t < tiles; t += 8 * shares) {
+      float2 p[8];
+      float up = most;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        p[i] = t + i * shares < tiles ? stats[(t + i * shares) * m + r] : make_float2(-INFINITY, 0.f);
+        up = fmaxf(up, p[i].x);
+      }
+      sum = moved_sum(sum, most, up);
+      most = up;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) sum += p[i].y == 0.f ? 0. : (double)p[i].y * (double)exp_of(shift_of(p[i].x) - shift_of(most));
     }
-  room[threadIdx.x] = make_float2(most, sum);
-  __syncthreads();
+  for (int half = shares / 2; half > 0; half /= 2) {
+    top[threadIdx.x] = most;
+    room[threadIdx.x] = sum;
+    __syncthreads();
+    if (first < half) {
+      const float most2 = top[threadIdx.x + half * rows], up = fmaxf(most, most2);
+      sum = moved_sum(sum, most, up) + moved_sum(room[threadIdx.x + half * rows], most2, up);
+      most = up;
+    }
+    __syncthreads();
+  }
   if (threadIdx.x >= rows || r >= m) return;
-  for (int t = 1; t < shares; ++t) join_stats(most, sum, room[(t << log_rows) + own].x, room[(t << log_rows) + own].y);
-  const float l = lse_of(most, sum);
+  const float l = shift_of(most) + logf((float)sum);
   lse[r] = l;
   loss[r] = known(labels[r], classes) ? l - z_label[r] : 0.f;
 }
@@ -497,8 +520,8 @@ SAGNN_EXPORT int softmax_xent_fwd(int32_t dtype, const void* d_H, int64_t ldh, c
   hipStream_t s = (hipStream_t)stream;
   const int rc = launch(a, dtype, prec, p.tile, transW != 0, s);
   if (rc != SAGNN_OK || p.total == 0) return rc;
-  // (16 threads to a row of many tiles: 8192 rows of 1024 of them, four threads to each, took 106 us)
-  const int log_rows = p.col_tiles > 16 ? 4 : 6;
+  // (16 threads to a row of many tiles: 8192 rows of 1024 of them, four threads to each, took 106 us; 64 or more where the tiles are a few megabytes or chains long)
+  const int log_rows = p.col_tiles <= 16 ? 6 : p.col_tiles <= 1024 && m * p.col_tiles > (1 << 20) ? 4 : m >= 4 ? 2 : 0;
   xent_join_kernel<<<dim3((uint32_t)ceil_div(m, 1 << log_rows)), 256, 0, s>>>(a.stats, a.z_label, m, p.col_tiles, d_labels, n_classes, log_rows, d_loss, d_lse);
   SAGNN_LAUNCH_CHECK();
   return SAGNN_OK;
