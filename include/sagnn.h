@@ -718,7 +718,7 @@ int dropout_add(int32_t dtype, const void* d_X, int64_t ldx, const void* d_R, in
  *   dR = rstd (G gamma - xh sum(G gamma xh) / C) + D,  dX = drop(dR),  dgamma[c] = sum over rows of G xh
  *
  * out_type: dtype, or SAGNN_E4M3: Y holds rows of 8 bits (ldy in bytes) and d_scale one float for each, Y = d_scale[r] q:
- * d_scale[r] = max |y| / 448, q = y / d_scale[r] rounded to nearest even.  A row whose scale would be below 2^-126 has scale 0 and zeros.  A NaN stays one.
+ * d_scale[r] = max |y| / 448, q = y / d_scale[r], both divisions in fp32, rounded to nearest even.  A row whose scale would be below 2^-126 has scale 0 and zeros.  A NaN stays one.
  * Y is made of the sum before that is rounded for S.  Squares are summed in 64 bits.  d_S, d_rstd: outputs, may be NULL (S for the next residual
  * and both for the backward pass); gamma, rstd, dgamma are fp32, gamma may be NULL (1).  Backward d_S is an input (the X of the forward call where nothing was added or
  * dropped); d_dX, d_dR, d_dgamma may be NULL each.  Sums of gradients are runs of fp32 of 384 terms at most, joined in 64 bits; their order is fixed: the same bits

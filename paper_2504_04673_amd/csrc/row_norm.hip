@@ -45,6 +45,16 @@ __device__ __forceinline__ float root_inverse(double x) {
   return (float)(e == e ? better : r);
 }
 
+// x / scale, the nearest value of 32 bits.  (A product with the reciprocal is off by two units at most and sends values next to the middle between two of 8 bits to the
+// other one.)  One correction by the remainder leaves a unit, a second the nearest value, as the reciprocal is (Markstein, 1990), if the remainders are whole: at 2^-10,
+// below which all is zero in 8 bits, from a scale of 2^-92 on.
+__device__ __forceinline__ float quotient(float x, float scale, float inverse, bool usual) {
+  if (!usual) return scale > 0.f ? x / scale : x * 0.f;
+  float q = x * inverse;
+  q = __builtin_fmaf(__builtin_fmaf(-q, scale, x), inverse, q);
+  return __builtin_fmaf(__builtin_fmaf(-q, scale, x), inverse, q);
+}
+
 struct RowArgs {
   const void* X; int64_t ldx;        // backward: the sums S
   const void* R; int64_t ldr;        // residual, or NULL; backward: gradient of S from elsewhere
@@ -155,20 +165,18 @@ __global__ __launch_bounds__(TEAM == 64 ? kThreads : TEAM) void rms_norm_kernel(
     if constexpr (EIGHT) {
       if constexpr (kWide) most = team_join<TEAM>(most, reinterpret_cast<float*>(room), [](float x, float y) { return fmaxf(x, y); });
       else most = lanes_most(most, L);
-      // the largest value is 448, the type's own; a scale that is no normal number (and its reciprocal infinite) is zero, and its row
+      // the largest value is 448, the type's own; a scale that is no normal number is zero, and its row
       float scale = most / 448.f;
       if (scale < 0x1p-126f) scale = 0.f;
       const float inverse = scale > 0.f ? 1.f / scale : 0.f;
+      const bool usual = scale >= 0x1p-92f && scale < INFINITY;
       if (lane == 0) a.scale[r] = scale;
 #pragma unroll
       for (int v = 0; v < V; ++v) {
         const int e = v * L + lane, there = a.C - e * 8;
         if (there <= 0) continue;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          const float q = s[v][i] * inverse;
-          s[v][i] = q > 448.f ? 448.f : q < -448.f ? -448.f : q;         // (a NaN stays one)
-        }
+        for (int i = 0; i < 8; ++i) s[v][i] = quotient(s[v][i], scale, inverse, usual);      // (448 and a unit at most, and that is 448 in 8 bits)
         store_bytes(reinterpret_cast<uint8_t*>(a.Y) + r * a.ldy + e * 8, to_e4m3(s[v]), there);
       }
     }

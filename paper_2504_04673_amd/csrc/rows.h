@@ -57,7 +57,7 @@ __device__ __forceinline__ void store_eight(S* p, const float (&y)[8], int there
     if (i < there && i >= (there & 4)) p[i] = w.x[i];
 }
 
-// Eight values of e4m3 (OCP: largest 448), to nearest even; none may be over 448.  Two at a time into a half of a word.
+// Eight values of e4m3 (OCP: largest 448), to nearest even; none may be as much as 464, the middle to what would be next.  Two at a time into a half of a word.
 __device__ __forceinline__ uint2 to_e4m3(const float (&v)[8]) {
   int lo = __builtin_amdgcn_cvt_pk_fp8_f32(v[0], v[1], 0, false), hi = __builtin_amdgcn_cvt_pk_fp8_f32(v[4], v[5], 0, false);
   lo = __builtin_amdgcn_cvt_pk_fp8_f32(v[2], v[3], lo, true);
