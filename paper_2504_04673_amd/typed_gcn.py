@@ -132,28 +132,28 @@ class TypedResidualGCN:
         return [*self.W1, *self.W2, *self.gamma, self.head, self.bias]
 
     def forward(self, H, step=0, training=True):
-        """The last block's normalised rows, and what the backward pass needs.  step: an integer, or an int64 tensor of one element on the device
+        """The last block's normalised rows, and what the backward pass needs, the share that fell too (none where training is not set).  step: an integer, or an int64 tensor of one element on the device
         (a captured graph counts it up)."""
         p = self.p if training else 0.0
         if training and self.p_in:
             H = sagnn.dropout_add(H, self.p_in, self.seed, step)
         Y, S, rstd = sagnn.rms_norm(H, self.gamma[0])
-        kept = [(S, rstd, None, None)]
+        kept = [(S, rstd, None, None, 0.0)]
         for i, (W1, W2) in enumerate(zip(self.W1, self.W2)):
             T = self.graph.multiply(Y, self.ws)
             U = sagnn.grouped_gemm_act(T, W1, self.graph.off, prec=self.prec, act=sagnn.ACT_RELU)
             Z = sagnn.grouped_gemm_act(U, W2, self.graph.off, prec=self.prec)
             Y, S, rstd = sagnn.rms_norm(Z, self.gamma[i + 1], residual=S, p=p, seed=self.seed + 1 + i, offset=step)
-            kept.append((S, rstd, T, U))
+            kept.append((S, rstd, T, U, p))
         return Y, kept
 
     def backward(self, G, kept, step=0, dhead=None, dbias=None):
-        """Gradients in the order of parameters(), from G = dLoss/dY and those of the classifier."""
+        """Gradients in the order of parameters(), from G = dLoss/dY and those of the classifier, with what forward returned and its step."""
         n = len(self.W1)
         dW1, dW2, dgamma, dS = [None] * n, [None] * n, [None] * (n + 1), None
         for i in reversed(range(n)):
-            S, rstd, T, U = kept[i + 1]
-            dZ, dS, dgamma[i + 1] = sagnn.rms_norm_bwd(S, G, rstd, self.gamma[i + 1], grad_sum=dS, p=self.p, seed=self.seed + 1 + i, offset=step)
+            S, rstd, T, U, p = kept[i + 1]
+            dZ, dS, dgamma[i + 1] = sagnn.rms_norm_bwd(S, G, rstd, self.gamma[i + 1], grad_sum=dS, p=p, seed=self.seed + 1 + i, offset=step)
             dU, dW2[i] = sagnn.grouped_gemm_bwd(U, self.W2[i], self.graph.off, dZ, mask=U, prec=self.prec)
             dT, dW1[i] = sagnn.grouped_gemm_bwd(T, self.W1[i], self.graph.off, dU, prec=self.prec)
             G = self.graph.multiply(dT, self.ws)
