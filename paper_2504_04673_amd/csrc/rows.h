@@ -4,8 +4,6 @@
 
 namespace sagnn {
 
-constexpr int kEight = 8;
-
 template <typename S, int N>
 struct __attribute__((packed)) LooseRun { S x[N]; };
 template <typename S, int N>
