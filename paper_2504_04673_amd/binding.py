@@ -1020,15 +1020,16 @@ def _rms_norm(X, lead, gamma, residual, eps, p, seed, offset, row0, kind, y, ldy
 def rms_norm(X, gamma=None, residual=None, eps: float = 1e-6, p: float = 0.0, seed: int = 0, offset=0, row0: int = 0, out=None, out_sum=None):
     """Root-mean-square norm of the rows of S = residual + dropout(X) (dropout_add's p, seed, offset, row0): Y = S rstd gamma,
     rstd = (mean(S^2) + eps)^-1/2.  X: m x C, float32 or bfloat16, residual like it; gamma: C, float32.  Returns (Y, S, rstd), S being X itself
-    where nothing is added or dropped, rstd float32; out_sum may be the residual, which is updated in place then."""
-    lead = _lead(X)
+    where nothing is added or dropped (None where out takes X's place then), rstd float32; out_sum may be the residual, which is updated in place then."""
+    lead, over = _lead(X), False
     if out is None:
         out = X.new_empty(lead[2:])
         y, ldy = out.data_ptr(), lead[3]
     else:
         y, ldy = _like(out, X, "out")
+        over = y == lead[0]
     S, rstd = _rms_norm(X, lead, gamma, residual, eps, p, seed, offset, row0, _DTYPE[X.dtype], y, ldy, None, out_sum)
-    return out, S, rstd
+    return out, None if over and S is X and out_sum is None else S, rstd
 
 
 def rms_norm_e4m3(X, gamma=None, residual=None, eps: float = 1e-6, p: float = 0.0, seed: int = 0, offset=0, row0: int = 0, out_sum=None):
