@@ -756,12 +756,14 @@ int spmm_pack_rows_e4m3(const void* d_Q, int64_t ldq, const float* d_scale, int6
  * by the second in fp32, and dW's product takes rows of H times d_grad, in two bfloat16 terms, off by 2^-16.  P's rounding puts each term of dH and dW off by 2^-8 of itself at most:
  * in the norm their errors are 1.05 to 1.3 times those of their own rounding, the more the fewer classes there are.  Up to 512 bfloat16 rows, 1024 with d_grad, where one
  * label's rounding decides, P (with d_grad) is kept in two terms, off by 2^-16.  dbias is summed of what is not rounded.  Infinite and NaN logits give what the formula gives: a bias of -inf takes a class out.
- * Any kdim up to SAGNN_GROUPED_MAX_WIDTH, n_classes up to SAGNN_XENT_MAX_CLASSES, any leading dimensions not below the width, tensors aligned to their element; rows that begin on 16
- * bytes are read faster.  d_dH, d_dW, d_dbias may be NULL each.  Outputs must not overlap inputs or each other.  Nothing is waited for.
- * d_ws: softmax_xent_workspace_bytes() bytes, 16-byte aligned; NULL where that is 0 (forward, few classes).  Forward it is 8 bytes for each row and some 128
- * to 256 classes; backward a copy of H, P of a piece (512 MB, or all classes' or 1024 classes' where those are fewer or more), both twice where P has two
- * terms, sums of dH in fp32 where it has, or where there are several pieces or shares of them, a piece's dW in fp32; with d_grad and bfloat16 products two
- * copies more of H and that dW twice.
+ * Any kdim up to SAGNN_GROUPED_MAX_WIDTH, n_classes up to SAGNN_XENT_MAX_CLASSES, fewer than 2^31 tiles of 32 rows by 32 classes (some 2^41 logits), any leading dimensions not below
+ * the width, tensors aligned to their element; rows that begin on 16 bytes are read faster.  d_dH, d_dW, d_dbias may be NULL each.  Outputs must not overlap inputs or each other.
+ * Nothing is waited for.
+ * d_ws: softmax_xent_workspace_bytes() bytes, 16-byte aligned; NULL where that is 0 (forward, few classes).  Forward it is 8 bytes for each row and 32 to 256 classes (what a tile has), and 4
+ * for each row; backward a copy of H, P of a piece, both twice where P has two terms; sums of dH in fp32 where it has, or where there are several pieces or shares of them; a piece's dW in
+ * fp32; with d_grad and bfloat16 products two copies more of H and that dW twice.  The size is for a call with d_grad or without.  A piece is as many classes as 512 MB of P hold, 1024 at
+ * least (256 where those were more than 4 GB) and 32768 at most, or all there are; but a 384th of all at least, since dH's sums are added over the pieces in turn:
+ * a million rows by two million classes in bfloat16 take 10.8 GB of P.
  */
 #define SAGNN_XENT_MAX_CLASSES 16777216
 int softmax_xent_workspace_bytes(int32_t dtype, int64_t m, int32_t kdim, int32_t n_classes, int32_t prec, int32_t backward, size_t* bytes);
