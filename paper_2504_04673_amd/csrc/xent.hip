@@ -177,19 +177,22 @@ __global__ __launch_bounds__(256) void xent_join_kernel(const float2* __restrict
 #pragma unroll
       for (int i = 0; i < 8; ++i) sum += p[i].y == 0.f ? 0. : (double)p[i].y * (double)exp_of(shift_of(p[i].x) - shift_of(most));
     }
+  float up = most;
+  top[threadIdx.x] = most;
+  __syncthreads();
   for (int half = shares / 2; half > 0; half /= 2) {
-    top[threadIdx.x] = most;
-    room[threadIdx.x] = sum;
+    if (first < half) top[threadIdx.x] = up = fmaxf(up, top[threadIdx.x + half * rows]);
     __syncthreads();
-    if (first < half) {
-      const float most2 = top[threadIdx.x + half * rows], up = fmaxf(most, most2);
-      sum = moved_sum(sum, most, up) + moved_sum(room[threadIdx.x + half * rows], most2, up);
-      most = up;
-    }
+  }
+  up = top[own];
+  room[threadIdx.x] = sum = moved_sum(sum, most, up);
+  __syncthreads();
+  for (int half = shares / 2; half > 0; half /= 2) {
+    if (first < half) room[threadIdx.x] = sum += room[threadIdx.x + half * rows];
     __syncthreads();
   }
   if (threadIdx.x >= rows || r >= m) return;
-  const float l = shift_of(most) + logf((float)sum);
+  const float l = shift_of(up) + logf((float)sum);
   lse[r] = l;
   loss[r] = known(labels[r], classes) ? l - z_label[r] : 0.f;
 }
@@ -520,8 +523,8 @@ SAGNN_EXPORT int softmax_xent_fwd(int32_t dtype, const void* d_H, int64_t ldh, c
   hipStream_t s = (hipStream_t)stream;
   const int rc = launch(a, dtype, prec, p.tile, transW != 0, s);
   if (rc != SAGNN_OK || p.total == 0) return rc;
-  // (16 threads to a row of many tiles: 8192 rows of 1024 of them, four threads to each, took 106 us; 64 or more where the tiles are a few megabytes or chains long)
-  const int log_rows = p.col_tiles <= 16 ? 6 : p.col_tiles <= 1024 && m * p.col_tiles > (1 << 20) ? 4 : m >= 4 ? 2 : 0;
+  // (16 threads to a row of many tiles: 8192 rows of 1024 of them, four threads to each, took 106 us; 64 or more where the tiles are two megabytes or chains long)
+  const int log_rows = p.col_tiles <= 16 ? 6 : p.col_tiles <= 1024 && m * p.col_tiles > (1 << 18) ? 4 : m >= 4 ? 2 : 0;
   xent_join_kernel<<<dim3((uint32_t)ceil_div(m, 1 << log_rows)), 256, 0, s>>>(a.stats, a.z_label, m, p.col_tiles, d_labels, n_classes, log_rows, d_loss, d_lse);
   SAGNN_LAUNCH_CHECK();
   return SAGNN_OK;
