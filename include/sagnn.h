@@ -761,12 +761,14 @@ int spmm_pack_rows_e4m3(const void* d_Q, int64_t ldq, const float* d_scale, int6
  * Nothing is waited for.
  * d_ws: softmax_xent_workspace_bytes() bytes, 16-byte aligned; NULL where that is 0 (forward, few classes).  Forward it is 8 bytes for each row and 32 to 256 classes (what a tile has), and 4
  * for each row; backward a copy of H, P of a piece, both twice where P has two terms; sums of dH in fp32 where it has, or where there are several pieces or shares of them; a piece's dW in
- * fp32; with d_grad and bfloat16 products two copies more of H and that dW twice.  The size is for a call with d_grad or without.  A piece is as many classes as 512 MB of P hold, 1024 at
+ * fp32; with d_grad and bfloat16 products two copies more of H and that dW twice.  softmax_xent_workspace_bytes() is enough with d_grad or without,
+ * softmax_xent_bwd_workspace_bytes() for calls with it (weighted = 1) or those without (0).  A piece is as many classes as 512 MB of P hold, 1024 at
  * least (256 where those were more than 4 GB) and 32768 at most, or all there are; but a 384th of all at least, since dH's sums are added over the pieces in turn:
  * a million rows by two million classes in bfloat16 take 10.8 GB of P.
  */
 #define SAGNN_XENT_MAX_CLASSES 16777216
 int softmax_xent_workspace_bytes(int32_t dtype, int64_t m, int32_t kdim, int32_t n_classes, int32_t prec, int32_t backward, size_t* bytes);
+int softmax_xent_bwd_workspace_bytes(int32_t dtype, int64_t m, int32_t kdim, int32_t n_classes, int32_t prec, int32_t weighted, size_t* bytes);
 int softmax_xent_fwd(int32_t dtype, const void* d_H, int64_t ldh, const void* d_W, int64_t ldw, int32_t transW, const float* d_bias,
                      const int32_t* d_labels, int64_t m, int32_t kdim, int32_t n_classes, int32_t prec, float* d_loss, float* d_lse, void* d_ws,
                      size_t ws_bytes, void* stream);

@@ -31,7 +31,7 @@ EXPORTS = [
     "group_norm_workspace_bytes", "group_norm_act_fwd", "group_norm_act_bwd",
     "grad_norm_workspace_bytes", "grad_global_norm", "grad_clip_norm", "grad_scale_to_norm",
     "dropout_add", "rms_norm_fwd", "rms_norm_bwd_workspace_bytes", "rms_norm_bwd", "spmm_pack_rows_e4m3",
-    "softmax_xent_workspace_bytes", "softmax_xent_fwd", "softmax_xent_bwd",
+    "softmax_xent_workspace_bytes", "softmax_xent_bwd_workspace_bytes", "softmax_xent_fwd", "softmax_xent_bwd",
 ]
 
 
@@ -180,6 +180,7 @@ def lib():
         L.rms_norm_bwd.argtypes = [i32, vp, i64, vp, i64, vp, i64, i64, i32, vp, vp, i32, u64, u64, vp, i64, vp, i64, vp, i64, vp, vp, sz, vp]
         L.spmm_pack_rows_e4m3.argtypes = [vp, i64, vp, i64, i32, vp, i64, i32, vp, i64, vp]
         L.softmax_xent_workspace_bytes.argtypes = [i32, i64, i32, i32, i32, i32, psz]
+        L.softmax_xent_bwd_workspace_bytes.argtypes = [i32, i64, i32, i32, i32, i32, psz]
         L.softmax_xent_fwd.argtypes = [i32, vp, i64, vp, i64, i32, vp, vp, i64, i32, i32, i32, vp, vp, vp, sz, vp]
         L.softmax_xent_bwd.argtypes = [i32, vp, i64, vp, i64, i32, vp, vp, vp, vp, f64, i64, i32, i32, i32, vp, i64, vp, vp, vp, sz, vp]
         for name in EXPORTS[3:]:
@@ -1106,7 +1107,7 @@ def softmax_xent_bwd(H, W, labels, lse, grad=1.0, bias=None, transW=False, prec=
     their mean) or m, float32.  Returns (dH, dW, dbias), the first two in H's type, dbias float32; None for what is not wanted or not there."""
     m, k, n, args = _xent_args(H, W, labels, bias, transW)
     rows = isinstance(grad, torch.Tensor)
-    need = _bytes_of("softmax_xent_workspace_bytes", args[0], m, k, n, prec, 1)
+    need = _bytes_of("softmax_xent_bwd_workspace_bytes", args[0], m, k, n, prec, int(rows))
     ws = H.new_empty(need, dtype=torch.uint8)
     dH = H.new_empty((m, k)) if want_dh else None
     dW = H.new_empty(W.shape) if want_dw else None

@@ -482,8 +482,9 @@ SAGNN_EXPORT int softmax_xent_workspace_bytes(int32_t dtype, int64_t m, int32_t 
   if (!bytes || !valid(dtype, 0, m, kdim, n_classes, prec) || (backward & ~1)) return SAGNN_EINVAL;
   if (backward) {
     *bytes = 0;                              // (for either kind of gradient)
-    for (bool weighted : {false, true}) {
-      const size_t b = bwd_plan(dtype, prec, weighted, m, kdim, n_classes).total;
+    for (int32_t weighted : {0, 1}) {
+      size_t b = 0;
+      softmax_xent_bwd_workspace_bytes(dtype, m, kdim, n_classes, prec, weighted, &b);
       if (b > *bytes) *bytes = b;
     }
   } else {                                   // (room for any strides and alignments)
@@ -493,6 +494,13 @@ SAGNN_EXPORT int softmax_xent_workspace_bytes(int32_t dtype, int64_t m, int32_t 
       if (b > *bytes) *bytes = b;
     }
   }
+  return SAGNN_OK;
+}
+
+SAGNN_EXPORT int softmax_xent_bwd_workspace_bytes(int32_t dtype, int64_t m, int32_t kdim, int32_t n_classes, int32_t prec, int32_t weighted, size_t* bytes) {
+  using namespace sagnn;
+  if (!bytes || !valid(dtype, 0, m, kdim, n_classes, prec) || (weighted & ~1)) return SAGNN_EINVAL;
+  *bytes = bwd_plan(dtype, prec, weighted != 0, m, kdim, n_classes).total;
   return SAGNN_OK;
 }
 
