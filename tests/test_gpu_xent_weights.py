@@ -51,12 +51,12 @@ def off(got, ref):
     return float((got.double() - ref).norm() / ref.norm())
 
 
-@pytest.mark.parametrize("kind", ["random", "equal", "by class"])
+@pytest.mark.parametrize("kind", ["none", "random", "equal", "by class"])
 @pytest.mark.parametrize("m,k,n,times_h,times_w", [(3000, 256, 2000, 1.1, 1.1), (20000, 128, 172, 1.25, 1.1)])
 def test_weighted_gradients_err_as_unweighted_ones_do(m, k, n, times_h, times_w, kind):
     H, W, labels, bias = inputs(m, m, k, n, torch.bfloat16, False, True, 1.0, False)
     r = gen(7)
-    g = {"random": torch.rand(m, generator=r, device="cuda"), "equal": torch.full((m,), 1.0 + 2.0 ** -8, device="cuda"),
+    g = {"none": 1.0 + 2.0 ** -8, "random": torch.rand(m, generator=r, device="cuda"), "equal": torch.full((m,), 1.0 + 2.0 ** -8, device="cuda"),
          "by class": torch.rand(n, generator=r, device="cuda")[labels.long()]}[kind]
     _, lse = sagnn.softmax_xent(H, W, labels, bias=bias)
     dH, dW, _ = sagnn.softmax_xent_bwd(H, W, labels, lse, g, bias=bias)
